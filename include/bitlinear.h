@@ -371,6 +371,128 @@ bl_status bl_gemm_w158a8_noalloc(const uint8_t* packed, const float* beta, int l
                                  int64_t M, int64_t N, int64_t K,
                                  int32_t* acc, float* y, bl_stream s);
 
+/* KEY/VALUE CACHE OF 8-BIT CODES, and the attention that reads it: what stands between the QKV and the output
+ * BitLinear of a layer when a model is served.  Three calls, each one descriptor (HOST memory, read during the call)
+ * and a stream: block tables and slot maps of a step from the requests' lengths; the rotary append of new tokens;
+ * causal attention over the cache for any number of new tokens per request.
+ *
+ * The cache is a pool of blocks of `block` tokens (16, 32, 64 or 128); a request's tokens fill the blocks that its row of a
+ * block table names.  Token j of a request is in block table[j / block] at offset j % block; its slot is
+ * that block * `block` + the offset.
+ *   k        codes [n_blocks][n_kv][block][head_dim]
+ *   v        codes [n_blocks][n_kv][head_dim][block]: transposed, so that sixteen tokens of a feature are 16 bytes, which
+ *            is what a lane hands to the matrix cores
+ *   k_scale, v_scale  fp32 [n_blocks][n_kv]: a code c stands for c * scale of its block and head
+ *   k_stride, v_stride  bytes from a block to the next (multiples of 16; at least n_kv * block * head_dim),
+ *   scale_stride        floats from a block's scales to the next's (at least n_kv): other layers' blocks may lie between
+ * kind BL_KV_INT8: codes are integers of -127..127; BL_KV_E4M3: OCP e4m3 values (no NaN codes).  head_dim 64 or 128.
+ * Scales are >= 0.  What no token has written may hold anything.  n_blocks * block < 2^31. */
+enum { BL_KV_INT8 = 0, BL_KV_E4M3 = 1 };
+enum { BL_KV_MAX_REQUESTS = 4096 };
+typedef struct {
+    int kind, block, n_kv, head_dim;
+    int64_t n_blocks;
+    void* k;
+    void* v;
+    float* k_scale;
+    float* v_scale;
+    int64_t k_stride, v_stride, scale_stride;
+} bl_kv_cache;
+
+/* Block tables and slot maps of a step, built on the GPU (nothing is read back, so that a step may sit in a HIP graph).
+ * Request b holds seq_len[b] tokens and brings new_len[b] more; new_len[b] < 0: it ends.
+ *   - Ended requests push their blocks on the stack free_list[0 .. free_count) in their order, and their length becomes 0
+ *     (what goes beyond free_cap is dropped).
+ *   - Every other request has new_len[b] rows of the batch, in order: q_start[0..B] are their first rows (no row beyond
+ *     `rows`).  It takes the blocks that it lacks from the top of the stack into its row of the table.
+ *   - Refused is a request whose rows do not all fit in `rows`, that would need more than max_blocks blocks, or whose
+ *     blocks the stack cannot give (then also every later one that needs a block).  It keeps what it has: no new tokens.
+ *   seq_len_out    lengths with the new tokens (may be seq_len itself)
+ *   free_count_out entries left on the stack (1 int; may be free_count itself)
+ *   start          [B] position of the first new token; -1: refused or ended
+ *   positions, slots  [rows] of each new token; 0 and -1 for the tokens of refused requests and behind the last row
+ *   bad            1 int, SET to the number of refused requests and of ended ones whose blocks were dropped
+ * table [B][table_stride], max_blocks <= table_stride entries of a row are used.  A seq_len outside 0 .. max_blocks * block
+ * is taken as the nearer end.  1 <= B <= BL_KV_MAX_REQUESTS, 1 <= rows <= 2^24, 0 <= free_cap < 2^31 (0: no stack,
+ * free_list may be NULL). */
+typedef struct {
+    int64_t B, rows, table_stride, free_cap;
+    int32_t block, max_blocks;
+    const int32_t* seq_len;
+    const int32_t* new_len;
+    const int32_t* free_count;
+    int32_t* table;
+    int32_t* free_list;
+    int32_t* seq_len_out;
+    int32_t* free_count_out;
+    int32_t* start;
+    int32_t* q_start;
+    int32_t* positions;
+    int32_t* slots;
+    int32_t* bad;
+} bl_kv_batch;
+bl_status bl_kv_tables(const bl_kv_batch* b, bl_stream s);
+
+/* New tokens into the cache: row t of the fused projection [Q | K | V] ((n_q + 2 * n_kv) heads, fp32 or bf16), rotary
+ * embedding on Q and K (x[i], x[i + d/2] -> x[i]*c - x[i+d/2]*s, x[i+d/2]*c + x[i]*s with c, s = cos, sin[position][i],
+ * fp32 [n_pos][head_dim/2]; every operation one rounded fp32 step; cos and sin NULL: no rotation and positions unused),
+ * Q to bf16, K and V to codes at slots[t].
+ * A block's scale for a head, T = 127 or 448 (e4m3), g the largest |value| of the block's new tokens, NaN passed over:
+ *   s = max(g, 1e-5f) * (1.0f / T); where the block holds tokens already (the first new offset is not 0): s = max(s, its old scale);
+ *   code = round(clamp(x * (1.0f / s), -T, T)) to the nearest integer or e4m3 value, ties to even;
+ *   the codes in front of the first new offset, if s grew: c = round(c * (old scale / s)).
+ * So a block always has the scale of the largest value in it, at the price of one more rounding of what it held
+ * each time that a new token raises it.
+ * A step's tokens of one block stand in rows as far apart as their slots (consecutive rows, as bl_kv_tables gives them; rows between
+ * them may go nowhere), and no block is written by two requests.  slots[t] = -1: K and V of the row go nowhere.  A slot outside the cache or a position
+ * outside 0 .. n_pos-1: the same, the Q row of such a position is zeros, and *bad (1 int or NULL) is INCREASED by one.
+ *   q_out     bf16 [T][n_q * head_dim] or NULL, rows q_stride values apart
+ *   qkv       rows qkv_stride values apart (a multiple of 4 for fp32, 8 for bf16); kind 0 fp32, 1 bf16
+ * n_q >= 0, 1 <= T <= 2^24; pointers 16-byte aligned (positions, slots, bad: 4), q_stride a multiple of 8. */
+enum { BL_KV_FROM_F32 = 0, BL_KV_FROM_BF16 = 1 };
+typedef struct {
+    bl_kv_cache cache;
+    const void* qkv;
+    int64_t qkv_stride, q_stride, T, n_pos;
+    int32_t qkv_kind, n_q;
+    const int32_t* positions;
+    const int32_t* slots;
+    const float* cos;
+    const float* sin;
+    uint16_t* q_out;
+    int32_t* bad;
+} bl_kv_tokens;
+bl_status bl_kv_append(const bl_kv_tokens* t, bl_stream s);
+
+/* Causal attention over the cache.  Request b's queries are rows q_start[b] .. q_start[b+1]-1 of q (bf16, n_q heads; query head h reads
+ * key/value head h / (n_q / n_kv)); they are its last tokens: query i of n has the position p = seq_len[b] - n + i and sees
+ * the tokens 0 .. p (window > 0: p - window + 1 .. p) that are in the cache.
+ *   out[row][h] = bf16( sum_j softmax_j( softmax_scale * <q, k_j> ) v_j ),  zeros where nothing is seen.
+ * Products with K take the codes as they are against q in two 8-bit pieces of 16 bits in all of its largest value (e4m3: two e4m3 pieces, 8 significant bits);
+ * softmax weights are rounded to fp16 (11 bits; those below 2^-20 of a row's largest to 2^-30 of it) in front of the product with V; maxima, sums and outputs are held in fp32.
+ *   q, out     rows q_stride / out_stride values apart (multiples of 8), 16-byte aligned.  Rows of no request are left alone.
+ *   table      [B][table_stride]; an entry outside 0 .. n_blocks-1: its tokens are not seen
+ *   seq_len    taken as the nearer end outside 0 .. max_blocks * block; q_start: ascending, inside 0 .. T
+ *   max_q      no request has more queries (one that has is not computed)
+ *   max_len    about the longest seq_len: sizes the split over a long axis only (0: max_blocks * block)
+ *   workspace  bl_attn_workspace_bytes(a) bytes (it depends on the sizes and max_q, not on the lengths), 256-byte aligned; no content is expected
+ * Up to four launches on `s`, none of which waits for the host.  1 <= B <= BL_KV_MAX_REQUESTS, 1 <= T <= 2^24, softmax_scale > 0, n_q a multiple of
+ * n_kv; max_blocks * block, T * n_q / n_kv and B * n_kv * max_blocks * block / 64 at most 2^30. */
+typedef struct {
+    bl_kv_cache cache;
+    const uint16_t* q;
+    int64_t q_stride, out_stride, table_stride, B, T;
+    const int32_t* q_start;
+    const int32_t* seq_len;
+    const int32_t* table;
+    int32_t n_q, max_blocks, max_q, max_len, window;
+    float softmax_scale;
+    uint16_t* out;
+    void* workspace;
+} bl_attn_desc;
+size_t    bl_attn_workspace_bytes(const bl_attn_desc* a);
+bl_status bl_attn_kv8(const bl_attn_desc* a, bl_stream s);
+
 /* Test hook: which decode kernel the M <= 64 entry points take, so that tests can put every
  * kernel through every case.  0 = the measured default, 1 = the dot4 kernel where it applies
  * (M <= 4), 2 = the row-resident matrix-core kernel, 3 = the streaming panel kernel where it

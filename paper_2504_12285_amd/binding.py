@@ -40,6 +40,10 @@ SIGNATURES = {
     "bl_stack_table_bytes_batched": (_sz, [_vp, _ci, _i64]),
     "bl_stack_build": (_ci, [_vp, _ci, _ci, _i64, _vp, _vp, _vp]),
     "bl_stack_run": (_ci, [_vp, _vp, _vp]),
+    "bl_kv_tables": (_ci, [_vp, _vp]),
+    "bl_kv_append": (_ci, [_vp, _vp]),
+    "bl_attn_workspace_bytes": (_sz, [_vp]),
+    "bl_attn_kv8": (_ci, [_vp, _vp]),
     "bl_debug_force_path": (_ci, [_ci]),
     "bl_probe_stream_read": (_ci, [_vp, _sz, _ci, _vp, _vp]),
     "bl_probe_stream_write": (_ci, [_vp, _i64, _i64, _ci, _vp]),
@@ -92,6 +96,40 @@ class StackPlan(ctypes.Structure):
                 ("wg_offset", _i64), ("prep_offset", _i64),
                 ("packed_bytes", _i64), ("table_bytes", _i64),
                 ("tokens", ctypes.c_int32), ("entries", ctypes.c_int32)]
+
+
+BL_KV_INT8, BL_KV_E4M3 = 0, 1
+BL_KV_FROM_F32, BL_KV_FROM_BF16 = 0, 1
+
+
+class KVCacheDesc(ctypes.Structure):
+    """Mirror of bl_kv_cache."""
+    _fields_ = [("kind", _ci), ("block", _ci), ("n_kv", _ci), ("head_dim", _ci), ("n_blocks", _i64),
+                ("k", _vp), ("v", _vp), ("k_scale", _vp), ("v_scale", _vp),
+                ("k_stride", _i64), ("v_stride", _i64), ("scale_stride", _i64)]
+
+
+class KVBatchDesc(ctypes.Structure):
+    """Mirror of bl_kv_batch."""
+    _fields_ = [("B", _i64), ("rows", _i64), ("table_stride", _i64), ("free_cap", _i64),
+                ("block", ctypes.c_int32), ("max_blocks", ctypes.c_int32)] + \
+               [(n, _vp) for n in ("seq_len", "new_len", "free_count", "table", "free_list", "seq_len_out", "free_count_out",
+                                   "start", "q_start", "positions", "slots", "bad")]
+
+
+class KVTokensDesc(ctypes.Structure):
+    """Mirror of bl_kv_tokens."""
+    _fields_ = [("cache", KVCacheDesc), ("qkv", _vp), ("qkv_stride", _i64), ("q_stride", _i64), ("T", _i64), ("n_pos", _i64),
+                ("qkv_kind", ctypes.c_int32), ("n_q", ctypes.c_int32)] + \
+               [(n, _vp) for n in ("positions", "slots", "cos", "sin", "q_out", "bad")]
+
+
+class AttnDesc(ctypes.Structure):
+    """Mirror of bl_attn_desc."""
+    _fields_ = [("cache", KVCacheDesc), ("q", _vp), ("q_stride", _i64), ("out_stride", _i64), ("table_stride", _i64), ("B", _i64),
+                ("T", _i64), ("q_start", _vp), ("seq_len", _vp), ("table", _vp)] + \
+               [(n, ctypes.c_int32) for n in ("n_q", "max_blocks", "max_q", "max_len", "window")] + \
+               [("softmax_scale", ctypes.c_float), ("out", _vp), ("workspace", _vp)]
 
 
 class BitLinearError(RuntimeError):
@@ -169,7 +207,7 @@ class _PythonForm:
     def quant(*args):
         return NotImplemented
 
-    product = decode = run = quant
+    product = decode = run = kv = quant
 
 
 def _first_native():
@@ -190,6 +228,7 @@ def _first_native():
         return _native
     _bl_torch.bind(*(ctypes.cast(fn, _vp).value for fn in (lib.bl_quant_act_int8, lib.bl_gemv_w158a8,
                                                             lib.bl_gemm_w158a8, lib.bl_bitlinear_decode, lib.bl_stack_run)))
+    _bl_torch.bind_kv(*(ctypes.cast(fn, _vp).value for fn in (lib.bl_kv_tables, lib.bl_kv_append, lib.bl_attn_kv8)))
     _native = _bl_torch
     return _native
 
@@ -438,3 +477,151 @@ def bl_quant_from_absmax(X, absmax, q=None, scale=None, rowsum=None):
     _check(load().bl_quant_from_absmax(_ptr(X), _ptr(absmax), M, K, _ptr(q), _ptr(scale), _ptr(rowsum), _stream()),
            "bl_quant_from_absmax")
     return q, scale, rowsum
+
+
+def _wants(t, what, dtype, device, shape=None, rows=False):
+    """The tensor as a call may take it: type, device, shape (None: any) and rows without gaps (all of it, unless `rows`)."""
+    torch = _get_torch()
+    if not isinstance(t, torch.Tensor):
+        raise TypeError("%s must be a tensor" % what)
+    if t.dtype != dtype:
+        raise TypeError("%s must be %s, is %s" % (what, dtype, t.dtype))
+    if t.device != device:
+        raise ValueError("%s is on %s, not on %s" % (what, t.device, device))
+    if shape is not None and (t.dim() != len(shape) or any(a is not None and a != b for a, b in zip(shape, t.shape))):
+        raise ValueError("%s must have the shape %s, has %s" % (what, tuple(shape), tuple(t.shape)))
+    if not (t.is_contiguous() or rows and t.dim() >= 2 and t[0].is_contiguous() and (t.shape[0] == 1 or t.stride(0) >= t[0].numel())):
+        raise ValueError("%s has gaps or another order" % what)
+    return t
+
+
+def _row_stride(t):
+    """Elements from a row to the next (a single row may carry any stride)."""
+    return t.stride(0) if t.shape[0] > 1 else t[0].numel()
+
+
+class KVCache:
+    """Key/value cache of 8-bit codes (bl_kv_cache): k [n_blocks][n_kv][block][head_dim], v [n_blocks][n_kv][head_dim][block], int8 or
+    float8_e4m3fn; k_scale, v_scale fp32 [n_blocks][n_kv].  Blocks may lie apart (views into a pool of several layers)."""
+
+    def __init__(self, k, v, k_scale, v_scale):
+        torch = _get_torch()
+        if k.dim() != 4 or k.dtype not in (torch.int8, torch.float8_e4m3fn):
+            raise TypeError("k must be int8 or float8_e4m3fn [n_blocks][n_kv][block][head_dim]")
+        n, h, block, dim = k.shape
+        _wants(k, "k", k.dtype, k.device, rows=True)
+        _wants(v, "v", k.dtype, k.device, (n, h, dim, block), rows=True)
+        _wants(k_scale, "k_scale", torch.float32, k.device, (n, h), rows=True)
+        _wants(v_scale, "v_scale", torch.float32, k.device, (n, h), rows=True)
+        if _row_stride(k_scale) != _row_stride(v_scale):
+            raise ValueError("k_scale and v_scale must have the same stride")
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.n_blocks, self.n_kv, self.block, self.head_dim = n, h, block, dim
+        self.desc = KVCacheDesc(BL_KV_INT8 if k.dtype == torch.int8 else BL_KV_E4M3, block, h, dim, n, _ptr(k), _ptr(v), _ptr(k_scale),
+                                _ptr(v_scale), _row_stride(k), _row_stride(v), _row_stride(k_scale))
+
+    @classmethod
+    def empty(cls, n_blocks, n_kv, block, head_dim, device, kind=BL_KV_INT8):
+        """A cache over memory of its own; nothing in it."""
+        torch = _get_torch()
+        dtype = torch.int8 if kind == BL_KV_INT8 else torch.float8_e4m3fn
+        k = torch.empty((n_blocks, n_kv, block, head_dim), dtype=dtype, device=device)
+        v = torch.empty((n_blocks, n_kv, head_dim, block), dtype=dtype, device=device)
+        scales = [torch.empty((n_blocks, n_kv), dtype=torch.float32, device=device) for _ in range(2)]
+        return cls(k, v, *scales)
+
+
+class _KVCall:
+    """A call whose descriptor stands over buffers that the caller keeps: filled once, run as often as wanted (their
+    contents may change in between, HIP graphs may replay it)."""
+
+    def run(self):
+        out = (_native or _first_native()).kv(self._which, ctypes.addressof(self.desc))
+        if out is not NotImplemented:
+            return _result(out, self._where)
+        _check(getattr(load(), self._where)(ctypes.byref(self.desc), _stream()), self._where)
+
+
+class KVTables(_KVCall):
+    """Block tables and slot maps of a step (bl_kv_tables).  seq_len, new_len int32 [B]; table int32 [B][max_blocks];
+    free_list int32 [any]; free_count int32 [1]; rows: rows of the batch.  Outputs: start, q_start, positions, slots, bad, and
+    seq_len_out, free_count_out (in_place: seq_len and free_count themselves, for a step that is run again and again)."""
+    _which, _where = 0, "bl_kv_tables"
+
+    def __init__(self, seq_len, new_len, table, free_list, free_count, block, rows, in_place=False):
+        torch = _get_torch()
+        i32, dev, B = torch.int32, seq_len.device, seq_len.shape[0]
+        _wants(seq_len, "seq_len", i32, dev, (B,))
+        _wants(new_len, "new_len", i32, dev, (B,))
+        _wants(table, "table", i32, dev, (B, None), rows=True)
+        _wants(free_list, "free_list", i32, dev, (None,))
+        _wants(free_count, "free_count", i32, dev, (1,))
+        self.seq_len, self.new_len, self.table, self.free_list, self.free_count = seq_len, new_len, table, free_list, free_count
+
+        def new(n):
+            return torch.empty(n, dtype=i32, device=dev)
+        self.seq_len_out, self.free_count_out = (seq_len, free_count) if in_place else (new(B), new(1))
+        self.start, self.q_start, self.positions, self.slots, self.bad = new(B), new(B + 1), new(rows), new(rows), new(1)
+        self.desc = KVBatchDesc(B, rows, _row_stride(table), free_list.shape[0], block, table.shape[1],
+                                *(_ptr(t) for t in (seq_len, new_len, free_count, table, free_list, self.seq_len_out, self.free_count_out,
+                                                    self.start, self.q_start, self.positions, self.slots, self.bad)))
+
+
+class KVAppend(_KVCall):
+    """New tokens into the cache (bl_kv_append).  qkv fp32 or bf16 [T][(n_q + 2 n_kv) * head_dim]; slots, positions int32 [T];
+    cos, sin fp32 [n_pos][head_dim / 2] or None (no rotation).  Output: q bf16 [T][n_q * head_dim].  bad: int32 [1] that counts, or None."""
+    _which, _where = 1, "bl_kv_append"
+
+    def __init__(self, cache, qkv, n_q, slots, positions=None, cos=None, sin=None, q=None, bad=None):
+        torch = _get_torch()
+        dev, dim = cache.k.device, cache.head_dim
+        if qkv.dtype not in (torch.float32, torch.bfloat16):
+            raise TypeError("qkv must be float32 or bfloat16")
+        T = qkv.shape[0]
+        _wants(qkv, "qkv", qkv.dtype, dev, (T, (n_q + 2 * cache.n_kv) * dim), rows=True)
+        _wants(slots, "slots", torch.int32, dev, (T,))
+        if cos is not None or sin is not None:
+            _wants(cos, "cos", torch.float32, dev, (None, dim // 2))
+            _wants(sin, "sin", torch.float32, dev, tuple(cos.shape))
+            _wants(positions, "positions", torch.int32, dev, (T,))
+        if q is None and n_q:
+            q = torch.empty((T, n_q * dim), dtype=torch.bfloat16, device=dev)
+        elif q is not None:
+            _wants(q, "q", torch.bfloat16, dev, (T, n_q * dim), rows=True)
+        if bad is not None:
+            _wants(bad, "bad", torch.int32, dev, (1,))
+        self.cache, self.qkv, self.slots, self.positions, self.cos, self.sin, self.q, self.bad = cache, qkv, slots, positions, cos, sin, q, bad
+        self.desc = KVTokensDesc(cache.desc, _ptr(qkv), _row_stride(qkv), 0 if q is None else _row_stride(q), T,
+                                 0 if cos is None else cos.shape[0], BL_KV_FROM_F32 if qkv.dtype == torch.float32 else BL_KV_FROM_BF16, n_q,
+                                 *(_ptr(t) for t in (positions, slots, cos, sin, q, bad)))
+
+
+class KVAttention(_KVCall):
+    """Causal attention over the cache (bl_attn_kv8).  q bf16 [T][n_q][head_dim] (or [T][n_q * head_dim] with n_q); q_start int32 [B + 1],
+    seq_len int32 [B], table int32 [B][max_blocks].  max_q: no request has more queries; max_len: about the longest length.
+    Output: out bf16 [T][n_q * head_dim]."""
+    _which, _where = 2, "bl_attn_kv8"
+
+    def __init__(self, cache, q, q_start, seq_len, table, n_q=None, max_q=1, max_len=0, softmax_scale=None, window=0, out=None, workspace=None):
+        torch = _get_torch()
+        dev, dim, T, B = cache.k.device, cache.head_dim, q.shape[0], seq_len.shape[0]
+        n_q = q.shape[1] if n_q is None else n_q
+        _wants(q, "q", torch.bfloat16, dev, (T, n_q, dim) if q.dim() == 3 else (T, n_q * dim), rows=True)
+        _wants(q_start, "q_start", torch.int32, dev, (B + 1,))
+        _wants(seq_len, "seq_len", torch.int32, dev, (B,))
+        _wants(table, "table", torch.int32, dev, (B, None), rows=True)
+        if out is None:
+            out = torch.empty((T, n_q * dim), dtype=torch.bfloat16, device=dev)
+        else:
+            _wants(out, "out", torch.bfloat16, dev, (T, n_q * dim), rows=True)
+        self.cache, self.q, self.q_start, self.seq_len, self.table, self.out = cache, q, q_start, seq_len, table, out
+        self.desc = AttnDesc(cache.desc, _ptr(q), _row_stride(q), _row_stride(out), _row_stride(table), B, T, _ptr(q_start), _ptr(seq_len),
+                             _ptr(table), n_q, table.shape[1], max_q, max_len, window, dim ** -0.5 if softmax_scale is None else softmax_scale,
+                             _ptr(out), None)
+        nbytes = load().bl_attn_workspace_bytes(ctypes.byref(self.desc))
+        if workspace is None:
+            workspace = _workspace(nbytes, dev)
+        elif _wants(workspace, "workspace", torch.uint8, dev).numel() < nbytes:
+            raise ValueError("workspace of %d bytes, %d are needed" % (workspace.numel(), nbytes))
+        self.workspace = workspace
+        self.desc.workspace = _ptr(workspace)

@@ -1,0 +1,957 @@
+/* Causal attention over the key/value cache of 8-bit codes (bitlinear.h, bl_attn_kv8).
+ *
+ * For one key/value head the rows of a request are its (query, head of the group) pairs: row r is query r / G, head r % G,
+ * G = n_q / n_kv.  Per row the softmax runs over tiles of 64 tokens with a running reference m and a running sum:
+ *     x_j = S_j * a + log2(vs)          S_j = <q pieces, codes of k_j>, a = softmax_scale * log2(e) * scale of q * ks
+ *     w_j = 2^(x_j - m + 6)             the weight with the scale vs of its V block in it
+ *     l  += w_j / vs,  O += w_j * codes of v_j,  out = O / l
+ * with one ks and vs for the 16 tokens that share a block.  m moves only when a tile brings an x more than 8 above it
+ * (weights then reach 2^14, inside fp16), so that most tiles rescale nothing and exchange nothing between lanes.
+ *
+ * S is computed transposed (tokens x rows), so that a lane holds the weights of ONE row for sixteen tokens, exactly what the
+ * second product wants of it: the weights never leave the lane.  Which tokens a lane gets is chosen by the
+ * order in which the rows of K are handed in, such that its V codes are consecutive in memory. */
+#include "bl_device.h"
+#include "bl_kv.h"
+
+typedef _Float16 at_v8h __attribute__((ext_vector_type(8)));
+typedef _Float16 at_v2h __attribute__((ext_vector_type(2)));
+typedef float at_v16f __attribute__((ext_vector_type(16)));
+typedef int at_v8i __attribute__((ext_vector_type(8)));
+typedef uint32_t at_v4u __attribute__((ext_vector_type(4)));
+
+#define AT_TILE 64                 /* tokens a tile */
+#define AT_THREADS 256
+#define AT_WAVES 4
+#define AT_FEW 16                  /* rows of a request and kv head up to which bl_attn_rows does it */
+#define AT_MANY 128                /* rows a workgroup of bl_attn_tile */
+#define AT_ROWS_GRID 512           /* workgroups of bl_attn_rows */
+#define AT_GROW 8.0f
+#define AT_LIFT 6.0f
+
+struct at_args {
+    const uint8_t* k;
+    const uint8_t* v;
+    const float* k_scale;
+    const float* v_scale;
+    const uint16_t* q;
+    const int* q_start;
+    const int* seq_len;
+    const int* table;
+    uint16_t* out;
+    float* part;                   /* workspace */
+    int64_t k_stride, v_stride, scale_stride, q_stride, out_stride, table_stride;
+    int n_blocks, n_kv, G, n_q, B, T, shift, max_tokens, window;
+    float factor;                  /* softmax_scale * log2(e) */
+    int splits;                    /* of bl_attn_tile */
+    int row_tiles;                 /* its grid: upper bound of row tiles */
+};
+
+/* ---- what both kernels share --------------------------------------------------------------------------------------- */
+
+__device__ __forceinline__ int at_uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ float at_xor(float v, int m) { return __shfl_xor(v, m); }
+
+/* A request: queries, tokens, and the tiles that its queries i0..i1 can see. */
+struct at_request {
+    int row0, n, len;
+};
+__device__ __forceinline__ at_request at_read(const at_args& A, int b) {
+    at_request r;
+    const int a = A.q_start[b], e = A.q_start[b + 1];
+    r.row0 = a < 0 ? 0 : a;
+    const int end = e > A.T ? A.T : e;
+    r.n = end > r.row0 ? end - r.row0 : 0;
+    const int L = A.seq_len[b];
+    r.len = L < 0 ? 0 : L > A.max_tokens ? A.max_tokens : L;
+    return r;
+}
+/* First token that query i sees, and the one behind its last. */
+__device__ __forceinline__ int at_from(const at_args& A, const at_request& r, int i) {
+    const int p = r.len - r.n + i - A.window + 1;
+    return A.window && p > 0 ? p : 0;
+}
+__device__ __forceinline__ int at_to(const at_request& r, int i) {
+    const int e = r.len - r.n + i + 1;
+    return e > 0 ? e : 0;
+}
+
+/* Sixteen codes of one feature (consecutive tokens) as fp16, exact. */
+template <int KIND>
+__device__ __forceinline__ void at_half16(bl_v4i c, at_v8h& lo, at_v8h& hi) {
+    uint32_t o[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if (KIND == BL_KV_INT8) {
+            /* 0x6400 | u is 1024 + u in fp16; u = c + 128 */
+            const uint32_t u = (uint32_t)c[i] ^ 0x80808080u;
+            const at_v2h off = {(_Float16)1152.0f, (_Float16)1152.0f};
+            o[2 * i] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(at_v2h, __builtin_amdgcn_perm(0x64646464u, u, 0x04010400u)) - off);
+            o[2 * i + 1] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(at_v2h, __builtin_amdgcn_perm(0x64646464u, u, 0x04030402u)) - off);
+        } else {
+            o[2 * i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(c[i], 1.0f, false));
+            o[2 * i + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(c[i], 1.0f, true));
+        }
+    }
+    lo = __builtin_bit_cast(at_v8h, (at_v4u){o[0], o[1], o[2], o[3]});
+    hi = __builtin_bit_cast(at_v8h, (at_v4u){o[4], o[5], o[6], o[7]});
+}
+/* The first n (0..16) codes of sixteen, zeros behind them. */
+__device__ __forceinline__ bl_v4i at_first(bl_v4i c, int n) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int k = n - 4 * i;
+        c[i] = k >= 4 ? c[i] : k <= 0 ? 0 : c[i] & (int)((1u << (8 * k)) - 1);
+    }
+    return c;
+}
+__device__ __forceinline__ uint32_t at_pack_half(float a, float b) {
+    const bl_v2f v = {a, b};
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, at_v2h));
+}
+
+/* Sixteen bf16 values of q as the two 8-bit pieces that are multiplied with codes.
+ * int8: t = rint(q * inv), |t| <= 127 * 256, t = 256 * hi + lo with lo in -128..127.
+ * e4m3: t = q * inv, inv a power of two, hi = e4m3(t), lo = e4m3(t - hi): exact down to 2^-9 of the row's largest. */
+template <int KIND>
+__device__ __forceinline__ void at_pieces(const uint32_t (&w)[8], float inv, bl_v4i& hi, bl_v4i& lo) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float t[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t x = w[2 * i + (j >> 1)];
+            t[j] = (j & 1 ? __uint_as_float(x & 0xffff0000u) : bl_bf16_to_f32(x & 0xffffu)) * inv;
+        }
+        if (KIND == BL_KV_INT8) {
+            uint32_t a = 0, b = 0;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int v = (int)rintf(t[j]), h = (v + 128) >> 8;
+                a |= (uint32_t)(h & 0xff) << (8 * j);
+                b |= (uint32_t)((v - 256 * h) & 0xff) << (8 * j);
+            }
+            hi[i] = (int)a, lo[i] = (int)b;
+        } else {
+            int a = __builtin_amdgcn_cvt_pk_fp8_f32(t[0], t[1], 0, false);
+            a = __builtin_amdgcn_cvt_pk_fp8_f32(t[2], t[3], a, true);
+            hi[i] = a;
+            int b = __builtin_amdgcn_cvt_pk_fp8_f32(t[0] - __builtin_amdgcn_cvt_f32_fp8(a, 0), t[1] - __builtin_amdgcn_cvt_f32_fp8(a, 1), 0, false);
+            b = __builtin_amdgcn_cvt_pk_fp8_f32(t[2] - __builtin_amdgcn_cvt_f32_fp8(a, 2), t[3] - __builtin_amdgcn_cvt_f32_fp8(a, 3), b, true);
+            lo[i] = b;
+        }
+    }
+}
+/* Multiplier of a row for at_pieces, and the scale of what it gives, from its largest |q| (0: all zero). */
+template <int KIND>
+__device__ __forceinline__ void at_row_scale(float most, float& inv, float& scale) {
+    if (KIND == BL_KV_INT8) {
+        inv = most > 0.0f ? bl_div_rn(32512.0f, most) : 0.0f;
+        scale = most * (1.0f / 32512.0f);
+    } else {
+        /* 2^e with most * 2^e in [128, 256) */
+        int e = 134 - (int)(__float_as_uint(most) >> 23);
+        e = e > 120 ? 120 : e < -120 ? -120 : e;
+        inv = most > 0.0f ? __uint_as_float((uint32_t)(127 + e) << 23) : 0.0f;
+        scale = __uint_as_float((uint32_t)(127 - e) << 23);
+    }
+}
+__device__ __forceinline__ float at_largest(const uint32_t (&w)[8], float most, bool& nan) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const uint32_t a = (w[i] << 16) & 0x7fffffffu, b = w[i] & 0x7fff0000u;
+        nan |= a > 0x7f800000u || b > 0x7f800000u;
+        most = bl_max_pos(most, bl_max_pos(__uint_as_float(a), __uint_as_float(b)));
+    }
+    return most;
+}
+
+/* Sum over the requests in front of b, and over all: f(b) each.  s: [AT_WAVES + 2]. */
+template <typename F>
+__device__ __forceinline__ void at_before(int B, int b, F f, int* s, int& before, int& all) {
+    int x = 0, y = 0;
+    for (int i = threadIdx.x; i < B; i += AT_THREADS) {
+        const int c = f(i);
+        y += c;
+        if (i < b) x += c;
+    }
+    x = bl_wave_sum(x), y = bl_wave_sum(y);
+    const int w = threadIdx.x >> 6;
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) s[w] = x, s[AT_WAVES + w] = y;
+    __syncthreads();
+    before = all = 0;
+#pragma unroll
+    for (int i = 0; i < AT_WAVES; ++i) before += s[i], all += s[AT_WAVES + i];
+}
+
+/* ---- few rows: the cache is streamed ------------------------------------------------------------------------------ */
+
+/* Tiles of request b in bl_attn_rows, per kv head: one at least where it has rows to write, none where it is another's. */
+__device__ __forceinline__ int at_few_tiles(const at_args& A, int b) {
+    const at_request r = at_read(A, b);
+    const int64_t rows = (int64_t)r.n * A.G;
+    if (rows == 0 || rows > AT_FEW) return 0;
+    const int t = (r.len + AT_TILE - 1) / AT_TILE - at_from(A, r, 0) / AT_TILE;
+    return t > 0 ? t : 1;
+}
+/* Tiles a workgroup does, of `all` in the launch. */
+__device__ __forceinline__ int at_share(int all) {
+    const int s = (all + AT_ROWS_GRID - 1) / AT_ROWS_GRID;
+    return s > AT_WAVES ? s : AT_WAVES;
+}
+template <int D>
+struct at_slot {                    /* a workgroup's partial result: rows x (D sums, m, l) */
+    static constexpr int floats = AT_FEW * (D + 2);
+};
+
+/* The tiles of all requests and kv heads stand in one line (request, head, tile); a workgroup takes an equal piece of it, and a
+ * piece may end one head's tiles and begin the next's.  What a piece has of an item that others share goes to the
+ * workspace (at most two such: at its ends) and bl_attn_rows_join adds it up.  Inside a piece the four waves
+ * take tiles in turn and meet in LDS at its end.
+ * A wave: K rows of a tile straight from memory into the registers that the matrix cores read (four 16 x 128 products of
+ * codes against the two pieces of q), then V the same way.  V of a tile and K of the next are in flight while one computes. */
+template <int KIND, int D>
+__global__ __launch_bounds__(AT_THREADS, 2) void bl_attn_rows(at_args A) {
+    constexpr int KS = D / 64, DT = D / 16;                 /* 64-byte steps of a K row, 16-feature tiles of V */
+    constexpr int PITCH = D + 4;
+    __shared__ int s_off[BL_KV_MAX_REQUESTS + 1];
+    __shared__ int s_scan[2 * AT_WAVES];
+    __shared__ float s_o[AT_WAVES][AT_FEW][PITCH];
+    __shared__ float s_m[AT_WAVES][AT_FEW], s_l[AT_WAVES][AT_FEW];
+    const int tid = threadIdx.x, lane = tid & 63, wave = at_uniform(tid >> 6);
+    const int col = lane & 15, grp = lane >> 4;
+    /* where each request's tiles start */
+    {
+        const int per = (A.B + AT_THREADS - 1) / AT_THREADS;
+        int mine = 0;
+        for (int i = 0; i < per; ++i) {
+            const int b = tid * per + i;
+            if (b < A.B) mine += at_few_tiles(A, b);
+        }
+        int x = mine;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int y = __shfl_up(x, d);
+            if (lane >= d) x += y;
+        }
+        if (lane == 63) s_scan[wave] = x;
+        __syncthreads();
+        int before = x - mine, all = 0;
+#pragma unroll
+        for (int w = 0; w < AT_WAVES; ++w) {
+            if (w < wave) before += s_scan[w];
+            all += s_scan[w];
+        }
+        for (int i = 0; i < per; ++i) {
+            const int b = tid * per + i;
+            if (b < A.B) {
+                s_off[b] = before;
+                before += at_few_tiles(A, b);
+            }
+        }
+        if (tid == 0) s_off[A.B] = all;
+        __syncthreads();
+    }
+    const int64_t all = (int64_t)s_off[A.B] * A.n_kv;
+    const int share = at_share((int)all);
+    int x0 = (int)blockIdx.x * share;
+    const int x1 = x0 + share < all ? x0 + share : (int)all;
+    const int bs1 = (1 << A.shift) - 1;
+
+    while (x0 < x1) {
+        int lo = 0, hi = A.B;                               /* s_off[lo] * n_kv <= x0 < s_off[hi] * n_kv */
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if ((int64_t)s_off[mid] * A.n_kv <= x0) lo = mid;
+            else hi = mid;
+        }
+        const int b = at_uniform(lo);
+        const int c = at_uniform(s_off[b + 1] - s_off[b]);
+        const int r0 = x0 - at_uniform(s_off[b]) * A.n_kv;
+        const int h = r0 / c, t0 = r0 % c;
+        const int seg = c - t0 < x1 - x0 ? c - t0 : x1 - x0;
+        const at_request R = at_read(A, b);
+        const int rows = R.n * A.G;
+        const int tile0 = at_from(A, R, 0) / AT_TILE + t0;
+        const int* pages = A.table + b * A.table_stride;
+
+        /* this lane's row: limits and the pieces of q */
+        const int qi = col < rows ? col / A.G : 0;
+        const int see0 = at_from(A, R, qi), see1 = col < rows ? at_to(R, qi) : 0;
+        const int all_from = at_from(A, R, R.n - 1), all_to = at_to(R, 0);     /* tokens that every row sees: [all_from, all_to) */
+        bl_v4i qh[KS], ql[KS];
+        float a_row;
+        {
+            uint32_t w[KS][8];
+            const uint16_t* src = A.q + (R.row0 + qi) * A.q_stride + (h * A.G + (col < rows ? col % A.G : 0)) * D;
+            float most = 0.0f;
+            bool nan = false;
+#pragma unroll
+            for (int s = 0; s < KS; ++s) {
+                const at_v4u u0 = *bl_gc<at_v4u>(src + s * 64 + grp * 16), u1 = *bl_gc<at_v4u>(src + s * 64 + grp * 16 + 8);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) w[s][j] = u0[j], w[s][4 + j] = u1[j];
+                most = at_largest(w[s], most, nan);
+            }
+            most = bl_max_pos(most, at_xor(most, 16));
+            most = bl_max_pos(most, at_xor(most, 32));
+            float inv, scale;
+            at_row_scale<KIND>(most, inv, scale);
+            const uint64_t nans = __ballot(nan);
+            if (nans && ((nans >> col) & 0x0001000100010001ull)) scale = __uint_as_float(0x7fc00000u);
+            a_row = scale * A.factor;
+#pragma unroll
+            for (int s = 0; s < KS; ++s) at_pieces<KIND>(w[s], inv, qh[s], ql[s]);
+        }
+
+        bl_v4f o[DT];
+#pragma unroll
+        for (int i = 0; i < DT; ++i) o[i] = (bl_v4f){0, 0, 0, 0};
+        float m = -INFINITY, l = 0.0f;
+
+        const int tend = tile0 + seg;
+        const int64_t head_k = ((int64_t)h << A.shift) * D, head_v = head_k;
+        /* Blocks of the lane's K row and of its sixteen V tokens; -1: nothing to see there. */
+        auto page_of = [&](int token) -> int {
+            int p = -1;
+            if (token < R.len) {
+                p = pages[token >> A.shift];
+                p = (unsigned)p < (unsigned)A.n_blocks ? p : -1;
+            }
+            return p;
+        };
+        const int kgrp = (col >> 2) * 16, krow = col & 3;
+        auto load_k = [&](int tile, int page, bl_v4i (&k)[4][KS]) {
+            const int tok = tile * AT_TILE + kgrp;
+            const uint8_t* p = A.k + (int64_t)(page < 0 ? 0 : page) * A.k_stride + head_k + (int64_t)((tok & bs1) + krow) * D + grp * 16;
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int s = 0; s < KS; ++s) k[t][s] = __builtin_nontemporal_load(bl_gc<bl_v4i>(p + t * 4 * D + s * 64));
+        };
+        int tile = tile0 + wave;
+        if (tile < tend) {
+            bl_v4i k[4][KS];
+            int pk = page_of(tile * AT_TILE + kgrp), pv = page_of(tile * AT_TILE + grp * 16);
+            load_k(tile, pk, k);
+            float ks = A.k_scale[(int64_t)(pv < 0 ? 0 : pv) * A.scale_stride + h], vs = A.v_scale[(int64_t)(pv < 0 ? 0 : pv) * A.scale_stride + h];
+            int pk1 = page_of((tile + AT_WAVES) * AT_TILE + kgrp), pv1 = page_of((tile + AT_WAVES) * AT_TILE + grp * 16);
+            for (; tile < tend; tile += AT_WAVES) {
+                const int tok = tile * AT_TILE + grp * 16;            /* first of this lane's sixteen tokens */
+                bl_v4i v[DT];
+                {
+                    const uint8_t* p = A.v + (int64_t)(pv < 0 ? 0 : pv) * A.v_stride + head_v + ((int64_t)col << A.shift) + (tok & bs1);
+#pragma unroll
+                    for (int i = 0; i < DT; ++i) v[i] = __builtin_nontemporal_load(bl_gc<bl_v4i>(p + ((int64_t)(16 * i) << A.shift)));
+                }
+                bl_v4f sf[4];
+                if constexpr (KIND == BL_KV_INT8) {
+                    bl_v4i sh[4], sl[4];
+                    const bl_v4i z = {0, 0, 0, 0};
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) {
+                        sh[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(k[t][0], qh[0], z, 0, 0, 0);
+                        sl[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(k[t][0], ql[0], z, 0, 0, 0);
+                        if constexpr (KS == 2) {
+                            sh[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(k[t][1], qh[1], sh[t], 0, 0, 0);
+                            sl[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(k[t][1], ql[1], sl[t], 0, 0, 0);
+                        }
+                    }
+                    bl_mfma_fence();
+#pragma unroll
+                    for (int t = 0; t < 4; ++t)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) sf[t][i] = (float)((sh[t][i] << 8) + sl[t][i]);   /* |.| < 2^31: exact until here */
+                } else {
+                    at_v8i q0, q1;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        q0[i] = i < 4 ? qh[0][i] : KS == 2 ? qh[KS - 1][i - 4] : 0;
+                        q1[i] = i < 4 ? ql[0][i] : KS == 2 ? ql[KS - 1][i - 4] : 0;
+                    }
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) {
+                        at_v8i kk;
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) kk[i] = i < 4 ? k[t][0][i] : KS == 2 ? k[t][KS - 1][i - 4] : 0;
+                        sf[t] = (bl_v4f){0, 0, 0, 0};
+                        sf[t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(kk, q0, sf[t], 0, 0, 0, 0, 0, 0);
+                        sf[t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(kk, q1, sf[t], 0, 0, 0, 0, 0, 0);
+                    }
+                    bl_mfma_fence();
+                }
+                /* the next tile's K while this one computes, and what comes behind it */
+                const int next = tile + AT_WAVES;
+                const int pv_next = pv1;
+                const float ks0 = ks, vs0 = vs;
+                if (next < tend) load_k(next, pk1, k);
+                ks = A.k_scale[(int64_t)(pv1 < 0 ? 0 : pv1) * A.scale_stride + h];
+                vs = A.v_scale[(int64_t)(pv1 < 0 ? 0 : pv1) * A.scale_stride + h];
+                pk1 = page_of((next + AT_WAVES) * AT_TILE + kgrp);
+                pv1 = page_of((next + AT_WAVES) * AT_TILE + grp * 16);
+
+                const float a = a_row * ks0;
+                const float vsc = fmaxf(vs0, 0x1p-100f), lv = __builtin_amdgcn_logf(vsc);
+                const bool whole = tile * AT_TILE >= all_from && tile * AT_TILE + AT_TILE <= all_to && __all(pv >= 0);
+                float best = -INFINITY;
+                if (whole) {
+#pragma unroll
+                    for (int t = 0; t < 4; ++t)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            sf[t][i] *= a;
+                            best = fmaxf(best, sf[t][i]);
+                        }
+                } else {
+                    const int end = pv < 0 ? 0 : see1;
+#pragma unroll
+                    for (int t = 0; t < 4; ++t)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const int j = tok + 4 * t + i;
+                            sf[t][i] = j >= see0 && j < end ? sf[t][i] * a : -INFINITY;
+                            best = fmaxf(best, sf[t][i]);
+                        }
+                }
+                best += lv;
+                if (__any(best > m + AT_GROW)) {
+                    float top = fmaxf(m, best);
+                    top = fmaxf(top, at_xor(top, 16));
+                    top = fmaxf(top, at_xor(top, 32));
+                    const float f = top > m ? __builtin_amdgcn_exp2f(m - top) : 1.0f;
+                    l *= f;
+#pragma unroll
+                    for (int i = 0; i < DT; ++i) o[i] *= f;
+                    m = top;
+                }
+                const float shift = lv + AT_LIFT - m;
+                float sum = 0.0f;
+#pragma unroll
+                for (int t = 0; t < 4; ++t)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        /* (where nothing is seen yet, m = -inf and the argument -inf + inf: 0 is meant) */
+                        float w = __builtin_amdgcn_exp2f(sf[t][i] + shift);
+                        if (!whole) w = sf[t][i] == -INFINITY ? 0.0f : w;
+                        sf[t][i] = w;
+                        sum += w;
+                    }
+                l += sum * __builtin_amdgcn_rcpf(vsc);
+                const at_v4u p0 = {at_pack_half(sf[0][0], sf[0][1]), at_pack_half(sf[0][2], sf[0][3]), at_pack_half(sf[1][0], sf[1][1]), at_pack_half(sf[1][2], sf[1][3])};
+                const at_v4u p1 = {at_pack_half(sf[2][0], sf[2][1]), at_pack_half(sf[2][2], sf[2][3]), at_pack_half(sf[3][0], sf[3][1]), at_pack_half(sf[3][2], sf[3][3])};
+                if (!whole) {
+                    /* what no token has written may be anything, a NaN times 0 too */
+                    const int there = pv < 0 ? 0 : R.len - tok;
+#pragma unroll
+                    for (int i = 0; i < DT; ++i) v[i] = at_first(v[i], there);
+                }
+#pragma unroll
+                for (int i = 0; i < DT; ++i) {
+                    at_v8h v0, v1;
+                    at_half16<KIND>(v[i], v0, v1);
+                    o[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, __builtin_bit_cast(at_v8h, p0), o[i], 0, 0, 0);
+                    o[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, __builtin_bit_cast(at_v8h, p1), o[i], 0, 0, 0);
+                }
+                pv = pv_next;
+            }
+            bl_mfma_fence();
+        }
+        /* the four waves' shares of the row sums and outputs meet */
+        l += at_xor(l, 16);
+        l += at_xor(l, 32);
+        if (grp == 0) s_m[wave][col] = m, s_l[wave][col] = l;
+#pragma unroll
+        for (int i = 0; i < DT; ++i) *(bl_v4f*)&s_o[wave][col][16 * i + 4 * grp] = o[i];
+        __syncthreads();
+        const bool alone = seg == c;
+        {
+            constexpr int PER = D / 16;
+            const int r = tid >> 4, d0 = (tid & 15) * PER;
+            if (r < rows) {
+                float top = -INFINITY;
+#pragma unroll
+                for (int w = 0; w < AT_WAVES; ++w) top = fmaxf(top, s_m[w][r]);
+                float sum = 0.0f, y[PER];
+#pragma unroll
+                for (int j = 0; j < PER; ++j) y[j] = 0.0f;
+#pragma unroll
+                for (int w = 0; w < AT_WAVES; ++w) {
+                    const float f = s_m[w][r] == top ? 1.0f : __builtin_amdgcn_exp2f(s_m[w][r] - top);
+                    sum += s_l[w][r] * f;
+#pragma unroll
+                    for (int j = 0; j < PER; ++j) y[j] += s_o[w][r][d0 + j] * f;
+                }
+                if (alone) {
+                    const float inv = sum == 0.0f ? 0.0f : bl_div_rn(1.0f, sum);
+                    uint32_t* to = (uint32_t*)(A.out + (R.row0 + r / A.G) * A.out_stride + (h * A.G + r % A.G) * D + d0);
+#pragma unroll
+                    for (int j = 0; j < PER; j += 2) to[j / 2] = bl_pack2_bf16(y[j] * inv, y[j + 1] * inv);
+                } else {
+                    float* to = A.part + (int64_t)(2 * blockIdx.x + (t0 == 0)) * at_slot<D>::floats;
+#pragma unroll
+                    for (int j = 0; j < PER; ++j) to[r * D + d0 + j] = y[j];
+                    if (d0 == 0) to[AT_FEW * D + 2 * r] = top, to[AT_FEW * D + 2 * r + 1] = sum;
+                }
+            }
+        }
+        __syncthreads();
+        x0 += seg;
+    }
+}
+
+/* Adds up what several workgroups of bl_attn_rows have of one item.  Workgroup: an item; sixteen threads a row. */
+template <int D>
+__global__ __launch_bounds__(AT_THREADS) void bl_attn_rows_join(at_args A) {
+    __shared__ int s_sum[2 * AT_WAVES];
+    const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x;
+    int before, all;
+    at_before(A.B, b, [&](int i) { return at_few_tiles(A, i); }, s_sum, before, all);
+    const int c = at_few_tiles(A, b);
+    if (c == 0) return;
+    const int share = at_share(all * A.n_kv);
+    const int first = before * A.n_kv + h * c;
+    const int w0 = first / share, w1 = (first + c - 1) / share;
+    if (w0 == w1) return;                                    /* one workgroup had all of it and wrote the result */
+    const at_request R = at_read(A, b);
+    constexpr int PER = D / 16;
+    const int r = tid >> 4, d0 = (tid & 15) * PER;
+    if (r >= R.n * A.G) return;
+    float top = -INFINITY;
+    for (int w = w0; w <= w1; ++w) {
+        const float* from = A.part + (int64_t)(2 * w + (w * share <= first)) * at_slot<D>::floats;
+        top = fmaxf(top, from[AT_FEW * D + 2 * r]);
+    }
+    float sum = 0.0f, y[PER];
+#pragma unroll
+    for (int j = 0; j < PER; ++j) y[j] = 0.0f;
+    for (int w = w0; w <= w1; ++w) {
+        const float* from = A.part + (int64_t)(2 * w + (w * share <= first)) * at_slot<D>::floats;
+        const float m = from[AT_FEW * D + 2 * r];
+        const float f = m == top ? 1.0f : __builtin_amdgcn_exp2f(m - top);
+        sum += from[AT_FEW * D + 2 * r + 1] * f;
+#pragma unroll
+        for (int j = 0; j < PER; ++j) y[j] += from[r * D + d0 + j] * f;
+    }
+    const float inv = sum == 0.0f ? 0.0f : bl_div_rn(1.0f, sum);
+    uint32_t* to = (uint32_t*)(A.out + (R.row0 + r / A.G) * A.out_stride + (h * A.G + r % A.G) * D + d0);
+#pragma unroll
+    for (int j = 0; j < PER; j += 2) to[j / 2] = bl_pack2_bf16(y[j] * inv, y[j + 1] * inv);
+}
+
+/* ---- many rows: the matrix cores work -------------------------------------------------------------------------------- */
+
+__device__ __forceinline__ int at_many_tiles(const at_args& A, int b) {
+    const at_request r = at_read(A, b);
+    const int64_t rows = (int64_t)r.n * A.G;
+    return rows > AT_FEW ? (int)((rows + AT_MANY - 1) / AT_MANY) : 0;
+}
+
+/* A workgroup: 128 rows of one request and kv head, 32 a wave, over a range of its tiles (all that its rows see, or one of
+ * `splits` equal pieces).  K codes lie in LDS as they are (16-byte units XOR-ed with the row: a read of 32 rows meets every
+ * bank), V as fp16, converted once by the thread that loads it; two buffers, one barrier a tile.  Products of 32 tokens x
+ * 32 rows (S^T) and 32 features x 32 rows (O^T): a lane has one row. */
+template <int KIND, int D>
+__global__ __launch_bounds__(AT_THREADS, 2) void bl_attn_tile(at_args A) {
+    constexpr int CH = D / 16;                              /* 16-byte units of a K row */
+    constexpr int KB = AT_TILE * D, VB = D * AT_TILE * 2;
+    constexpr int KS = D / 32, DT = D / 32;
+    __shared__ __attribute__((aligned(16))) uint8_t s_k[2][KB];
+    __shared__ __attribute__((aligned(16))) uint8_t s_v[2][VB];
+    __shared__ int s_find[3];
+    __shared__ int s_scan[2 * AT_WAVES];
+    const int tid = threadIdx.x, lane = tid & 63, wave = at_uniform(tid >> 6);
+    const int col = lane & 31, half = lane >> 5;
+    /* whose tile: blockIdx.x = (row tile * n_kv + head) * splits + piece */
+    const int piece = (int)blockIdx.x % A.splits, h = (int)blockIdx.x / A.splits % A.n_kv, want = (int)blockIdx.x / A.splits / A.n_kv;
+    {
+        const int per = (A.B + AT_THREADS - 1) / AT_THREADS;
+        int mine = 0;
+        for (int i = 0; i < per; ++i) {
+            const int b = tid * per + i;
+            if (b < A.B) mine += at_many_tiles(A, b);
+        }
+        int x = mine;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int y = __shfl_up(x, d);
+            if (lane >= d) x += y;
+        }
+        if (lane == 63) s_scan[wave] = x;
+        if (tid == 0) s_find[0] = -1;
+        __syncthreads();
+        int before = x - mine;
+#pragma unroll
+        for (int w = 0; w < AT_WAVES; ++w)
+            if (w < wave) before += s_scan[w];
+        for (int i = 0; i < per; ++i) {
+            const int b = tid * per + i;
+            if (b < A.B) {
+                const int c = at_many_tiles(A, b);
+                if (want >= before && want < before + c) s_find[0] = b, s_find[1] = want - before, s_find[2] = c;
+                before += c;
+            }
+        }
+        __syncthreads();
+    }
+    const int b = at_uniform(s_find[0]);
+    if (b < 0) return;
+    const int rt = at_uniform(s_find[2]) - 1 - at_uniform(s_find[1]);      /* the last rows see most: first */
+    const at_request R = at_read(A, b);
+    const int rows = R.n * A.G, bs1 = (1 << A.shift) - 1;
+    const int rbase = rt * AT_MANY, rend = rbase + AT_MANY < rows ? rbase + AT_MANY : rows;
+    const int tok0 = at_from(A, R, rbase / A.G), tok1 = at_to(R, (rend - 1) / A.G);
+    int tile = tok0 / AT_TILE, tend = (tok1 + AT_TILE - 1) / AT_TILE;
+    if (tend < tile) tend = tile;
+    {
+        const int n = (tend - tile + A.splits - 1) / A.splits;
+        tile += piece * n;
+        tend = tile + n < tend ? tile + n : tend;
+    }
+    const int* pages = A.table + b * A.table_stride;
+
+    /* this lane's row */
+    const int row = rbase + wave * 32 + col;
+    const bool live = row < rows;
+    const int qi = live ? row / A.G : 0, qh_i = h * A.G + (live ? row % A.G : 0);
+    const int see0 = at_from(A, R, qi), see1 = live ? at_to(R, qi) : 0;
+    /* tokens that some row of this wave sees, and that all do */
+    const int wfirst = rbase + wave * 32, wlast = wfirst + 31 < rows ? wfirst + 31 : rows - 1;
+    const bool has_rows = wfirst < rows;
+    const int any_from = has_rows ? at_from(A, R, wfirst / A.G) : 0, any_to = has_rows ? at_to(R, wlast / A.G) : 0;
+    const int all_from = has_rows ? at_from(A, R, wlast / A.G) : 0, all_to = has_rows ? at_to(R, wfirst / A.G) : 0;
+    bl_v4i qh[KS], ql[KS];
+    float a_row;
+    {
+        uint32_t w[KS][8];
+        const uint16_t* src = A.q + (R.row0 + qi) * A.q_stride + qh_i * D;
+        float most = 0.0f;
+        bool nan = false;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+            const at_v4u u0 = *bl_gc<at_v4u>(src + s * 32 + half * 16), u1 = *bl_gc<at_v4u>(src + s * 32 + half * 16 + 8);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[s][j] = u0[j], w[s][4 + j] = u1[j];
+            most = at_largest(w[s], most, nan);
+        }
+        most = bl_max_pos(most, at_xor(most, 32));
+        float inv, scale;
+        at_row_scale<KIND>(most, inv, scale);
+        const uint64_t nans = __ballot(nan);
+        if (nans && ((nans >> col) & 0x0000000100000001ull)) scale = __uint_as_float(0x7fc00000u);
+        a_row = scale * A.factor;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) at_pieces<KIND>(w[s], inv, qh[s], ql[s]);
+    }
+    at_v16f o[DT];
+#pragma unroll
+    for (int i = 0; i < DT; ++i)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) o[i][j] = 0.0f;
+    float m = -INFINITY, l = 0.0f;
+
+    const int64_t head = ((int64_t)h << A.shift) * D;
+    auto page_of = [&](int token) -> int {
+        int p = -1;
+        if (token < R.len) {
+            p = pages[token >> A.shift];
+            p = (unsigned)p < (unsigned)A.n_blocks ? p : -1;
+        }
+        return p;
+    };
+    /* loading: D/64 16-byte units of K and of V a thread */
+    constexpr int U = D / 64;
+    constexpr int TPK = CH / U;                              /* threads a K row */
+    constexpr int TPV = 4 / U;                               /* threads a V row */
+    const int kt = tid / TPK, kc = tid % TPK * U;
+    const int vd = tid / TPV, vg = tid % TPV * U;
+    bl_v4i lk[U], lv_[U];
+    auto load = [&](int t) {
+        const int tok = t * AT_TILE;
+        const int pk = page_of(tok + (kt & ~15));
+        const uint8_t* p = A.k + (int64_t)(pk < 0 ? 0 : pk) * A.k_stride + head + (int64_t)((tok + kt) & bs1) * D + kc * 16;
+#pragma unroll
+        for (int u = 0; u < U; ++u) lk[u] = *bl_gc<bl_v4i>(p + u * 16);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int g = tok + (vg + u) * 16, pv = page_of(g);
+            const uint8_t* pp = A.v + (int64_t)(pv < 0 ? 0 : pv) * A.v_stride + head + ((int64_t)vd << A.shift) + (g & bs1);
+            lv_[u] = *bl_gc<bl_v4i>(pp);
+            const int there = pv < 0 ? 0 : R.len - g;
+            if (there < 16) lv_[u] = at_first(lv_[u], there);
+        }
+    };
+    auto store = [&](int buf) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int swz = CH == 8 ? kt & 7 : (kt >> 1) & 3;
+            *(bl_v4i*)&s_k[buf][kt * D + (((kc + u) ^ swz) * 16)] = lk[u];
+            at_v8h a, c;
+            at_half16<KIND>(lv_[u], a, c);
+            *(at_v8h*)&s_v[buf][vd * 128 + ((((vg + u) * 2) ^ (vd & 7)) * 16)] = a;
+            *(at_v8h*)&s_v[buf][vd * 128 + ((((vg + u) * 2 + 1) ^ (vd & 7)) * 16)] = c;
+        }
+    };
+    if (tile < tend) {
+        load(tile);
+        store(0);
+    }
+    __syncthreads();
+    int buf = 0;
+    for (; tile < tend; ++tile, buf ^= 1) {
+        const int tok = tile * AT_TILE;
+        const bool more = tile + 1 < tend;
+        if (more) load(tile + 1);
+        if (tok < any_to && tok + AT_TILE > any_from) {
+            float ks[4], vs[4];
+            bool seen = true;
+            bool there[4];
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const int p = at_uniform(page_of(tok + 16 * g));
+                there[g] = p >= 0;
+                seen &= p >= 0;
+                ks[g] = A.k_scale[(int64_t)(p < 0 ? 0 : p) * A.scale_stride + h];
+                vs[g] = fmaxf(A.v_scale[(int64_t)(p < 0 ? 0 : p) * A.scale_stride + h], 0x1p-100f);
+            }
+            const bool whole = seen && tok >= all_from && tok + AT_TILE <= all_to;
+            /* row r = 8a + 4f + b of the first product's tile tt is token 32 tt + 16 (a/2) + 8 f + 4 (a%2) + b */
+            const int kr = (col >> 4) * 16 + ((col >> 2) & 1) * 8 + ((col >> 3) & 1) * 4 + (col & 3);
+            float sf[2][16];
+#pragma unroll
+            for (int tt = 0; tt < 2; ++tt) {
+                const int kt2 = tt * 32 + kr, swz = CH == 8 ? kt2 & 7 : (kt2 >> 1) & 3;
+                bl_v4i kk[KS];
+#pragma unroll
+                for (int s = 0; s < KS; ++s) kk[s] = *(const bl_v4i*)&s_k[buf][kt2 * D + (((2 * s + half) ^ swz) * 16)];
+                if constexpr (KIND == BL_KV_INT8) {
+                    bl_v16i sh, sl;
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) sh[j] = sl[j] = 0;
+#pragma unroll
+                    for (int s = 0; s < KS; ++s) {
+                        sh = __builtin_amdgcn_mfma_i32_32x32x32_i8(kk[s], qh[s], sh, 0, 0, 0);
+                        sl = __builtin_amdgcn_mfma_i32_32x32x32_i8(kk[s], ql[s], sl, 0, 0, 0);
+                    }
+                    bl_mfma_fence();
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) sf[tt][j] = (float)((sh[j] << 8) + sl[j]);
+                } else {
+                    at_v16f s16;
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) s16[j] = 0.0f;
+#pragma unroll
+                    for (int s = 0; s < KS; s += 2) {
+                        at_v8i ka, qa, qb;
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) ka[j] = kk[s + j / 4][j % 4], qa[j] = qh[s + j / 4][j % 4], qb[j] = ql[s + j / 4][j % 4];
+                        s16 = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(ka, qa, s16, 0, 0, 0, 0, 0, 0);
+                        s16 = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(ka, qb, s16, 0, 0, 0, 0, 0, 0);
+                    }
+                    bl_mfma_fence();
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) sf[tt][j] = s16[j];
+                }
+            }
+            float best = -INFINITY, lv[4];
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const float a = a_row * ks[g];
+                lv[g] = __builtin_amdgcn_logf(vs[g]);
+                float top = -INFINITY;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    float& x = sf[g >> 1][(g & 1) * 8 + j];
+                    const int t = tok + 16 * g + 8 * half + j;
+                    x *= a;
+                    if (!whole) x = there[g] && t >= see0 && t < see1 ? x : -INFINITY;
+                    top = fmaxf(top, x);
+                }
+                best = fmaxf(best, top + lv[g]);
+            }
+            if (__any(best > m + AT_GROW)) {
+                float top = fmaxf(m, best);
+                top = fmaxf(top, at_xor(top, 32));
+                const float f = top > m ? __builtin_amdgcn_exp2f(m - top) : 1.0f;
+                l *= f;
+#pragma unroll
+                for (int i = 0; i < DT; ++i)
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) o[i][j] *= f;
+                m = top;
+            }
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const float shift = lv[g] + AT_LIFT - m;
+                float sum = 0.0f, w[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float x = sf[g >> 1][(g & 1) * 8 + j];
+                    w[j] = __builtin_amdgcn_exp2f(x + shift);
+                    if (!whole) w[j] = x == -INFINITY ? 0.0f : w[j];
+                    sum += w[j];
+                }
+                l += sum * __builtin_amdgcn_rcpf(vs[g]);
+                const at_v4u p = {at_pack_half(w[0], w[1]), at_pack_half(w[2], w[3]), at_pack_half(w[4], w[5]), at_pack_half(w[6], w[7])};
+#pragma unroll
+                for (int i = 0; i < DT; ++i) {
+                    const int d = 32 * i + col;
+                    const at_v8h vv = *(const at_v8h*)&s_v[buf][d * 128 + (((2 * g + half) ^ (d & 7)) * 16)];
+                    o[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vv, __builtin_bit_cast(at_v8h, p), o[i], 0, 0, 0);
+                }
+            }
+        }
+        if (more) store(buf ^ 1);
+        __syncthreads();
+    }
+    bl_mfma_fence();
+    l += at_xor(l, 32);
+    if (!live) return;
+    if (A.splits == 1) {
+        const float inv = l == 0.0f ? 0.0f : bl_div_rn(1.0f, l);
+        uint16_t* to = A.out + (R.row0 + qi) * A.out_stride + qh_i * D;
+#pragma unroll
+        for (int i = 0; i < DT; ++i)
+#pragma unroll
+            for (int j = 0; j < 16; j += 4) {
+                const bl_v2u u = {bl_pack2_bf16(o[i][j] * inv, o[i][j + 1] * inv), bl_pack2_bf16(o[i][j + 2] * inv, o[i][j + 3] * inv)};
+                *bl_g((bl_v2u*)(to + 32 * i + 2 * j + 4 * half)) = u;
+            }
+    } else {
+        const int64_t at = (int64_t)piece * A.T * A.n_q + (int64_t)(R.row0 + qi) * A.n_q + qh_i;
+        float* to = A.part + at * D;
+#pragma unroll
+        for (int i = 0; i < DT; ++i)
+#pragma unroll
+            for (int j = 0; j < 16; j += 4) *bl_g((bl_v4f*)(to + 32 * i + 2 * j + 4 * half)) = (bl_v4f){o[i][j], o[i][j + 1], o[i][j + 2], o[i][j + 3]};
+        if (half == 0) {
+            float* ml = A.part + (int64_t)A.splits * A.T * A.n_q * D + 2 * at;
+            ml[0] = m, ml[1] = l;
+        }
+    }
+}
+
+/* Adds up the pieces of a split: D / 8 threads a (row of the batch, head). */
+template <int D>
+__global__ __launch_bounds__(AT_THREADS) void bl_attn_tile_join(at_args A) {
+    constexpr int TPR = D / 8;
+    const int64_t at = (int64_t)blockIdx.x * (AT_THREADS / TPR) + threadIdx.x / TPR, all = (int64_t)A.T * A.n_q;
+    if (at >= all) return;
+    const int row = (int)(at / A.n_q), d0 = (threadIdx.x % TPR) * 8;
+    int lo = 0, hi = A.B;                                     /* whose row it is: q_start[lo] <= row < q_start[hi] */
+    if (row < A.q_start[0] || row >= A.q_start[A.B]) return;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (A.q_start[mid] <= row) lo = mid;
+        else hi = mid;
+    }
+    const at_request R = at_read(A, lo);
+    if ((int64_t)R.n * A.G <= AT_FEW) return;
+    const float* ml = A.part + A.splits * all * D;
+    float top = -INFINITY;
+    for (int s = 0; s < A.splits; ++s) top = fmaxf(top, ml[2 * (s * all + at)]);
+    float sum = 0.0f, y[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    for (int s = 0; s < A.splits; ++s) {
+        const float mm = ml[2 * (s * all + at)];
+        const float f = mm == top ? 1.0f : __builtin_amdgcn_exp2f(mm - top);
+        sum += ml[2 * (s * all + at) + 1] * f;
+        const float* from = A.part + (s * all + at) * D + d0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) y[j] += from[j] * f;
+    }
+    const float inv = sum == 0.0f ? 0.0f : bl_div_rn(1.0f, sum);
+    const at_v4u u = {bl_pack2_bf16(y[0] * inv, y[1] * inv), bl_pack2_bf16(y[2] * inv, y[3] * inv), bl_pack2_bf16(y[4] * inv, y[5] * inv), bl_pack2_bf16(y[6] * inv, y[7] * inv)};
+    *(at_v4u*)(A.out + row * A.out_stride + (at % A.n_q) * D + d0) = u;
+}
+
+/* ---- host ------------------------------------------------------------------------------------------------------------- */
+
+struct at_plan {
+    bool few, many;
+    int splits, row_tiles;
+    size_t few_bytes, bytes;
+};
+
+static bl_status at_check(const bl_attn_desc* a) {
+    if (!a) return BL_ERR_NULL;
+    if (const bl_status rc = bl_kv_cache_check(&a->cache)) return rc;
+    if (!a->q || !a->q_start || !a->seq_len || !a->table || !a->out) return BL_ERR_NULL;
+    const int64_t most = (int64_t)1 << 40, width = (int64_t)a->n_q * a->cache.head_dim;
+    if (a->B < 1 || a->B > BL_KV_MAX_REQUESTS || a->T < 1 || a->T > BL_MAX_DIM || a->n_q < 1 || a->n_q > 65535 || a->n_q % a->cache.n_kv ||
+        a->max_blocks < 1 || (int64_t)a->max_blocks * a->cache.block > ((int64_t)1 << 30) || a->table_stride < a->max_blocks || a->table_stride > most ||
+        a->max_q < 1 || a->max_len < 0 || a->window < 0 || a->q_stride < width || a->q_stride > most || a->out_stride < width || a->out_stride > most ||
+        a->T * (a->n_q / a->cache.n_kv) > ((int64_t)1 << 30) || a->B * a->cache.n_kv * ((int64_t)a->max_blocks * a->cache.block / AT_TILE + 2) > ((int64_t)1 << 30))
+        return BL_ERR_SHAPE;
+    if (!(a->softmax_scale > 0.0f) || a->softmax_scale > 3e38f) return BL_ERR_VALUE;
+    if (!bl_aligned(a->q, 16) || !bl_aligned(a->out, 16) || a->q_stride % 8 || a->out_stride % 8 || !bl_aligned(a->q_start, 4) ||
+        !bl_aligned(a->seq_len, 4) || !bl_aligned(a->table, 4))
+        return BL_ERR_ALIGN;
+    return BL_OK;
+}
+
+static at_plan at_make_plan(const bl_attn_desc* a) {
+    at_plan p;
+    const int G = a->n_q / a->cache.n_kv, D = a->cache.head_dim;
+    const int64_t rows = (int64_t)(a->max_q < a->T ? a->max_q : a->T) * G;
+    p.few = G <= AT_FEW;
+    p.many = rows > AT_FEW;
+    const int64_t part = a->T < a->B ? a->T : a->B;           /* requests with rows */
+    p.row_tiles = (int)(a->T * G / AT_MANY + part);
+    p.splits = 1;
+    if (p.many) {
+        /* pieces until the workgroups fill the chip twice over, of eight tiles at least */
+        const int64_t items = (int64_t)((a->T * G + AT_MANY - 1) / AT_MANY) * a->cache.n_kv;
+        const int64_t len = a->max_len > 0 ? a->max_len : (int64_t)a->max_blocks * a->cache.block;
+        int64_t s = items < 512 ? 512 / items : 1;
+        const int64_t by_len = len / (8 * AT_TILE);
+        s = s > by_len ? by_len : s;
+        p.splits = s < 1 ? 1 : s > 64 ? 64 : (int)s;
+    }
+    p.few_bytes = p.few ? (size_t)AT_ROWS_GRID * 2 * AT_FEW * (D + 2) * sizeof(float) : 0;
+    p.bytes = p.few_bytes + (p.splits > 1 ? (size_t)p.splits * a->T * a->n_q * (D + 2) * sizeof(float) : 0);
+    return p;
+}
+
+extern "C" size_t bl_attn_workspace_bytes(const bl_attn_desc* a) {
+    return at_check(a) == BL_OK ? at_make_plan(a).bytes : 0;
+}
+
+template <int KIND, int D>
+static void at_launch(at_args A, const at_plan& p, const bl_attn_desc* a, hipStream_t st) {
+    float* base = (float*)a->workspace;
+    if (p.few) {
+        A.part = base;
+        bl_attn_rows<KIND, D><<<AT_ROWS_GRID, AT_THREADS, 0, st>>>(A);
+        bl_attn_rows_join<D><<<dim3((unsigned)A.n_kv, (unsigned)A.B), AT_THREADS, 0, st>>>(A);
+    }
+    if (p.many) {
+        A.part = base + p.few_bytes / sizeof(float);
+        bl_attn_tile<KIND, D><<<(unsigned)((int64_t)p.row_tiles * A.n_kv * p.splits), AT_THREADS, 0, st>>>(A);
+        if (p.splits > 1) {
+            const int64_t rows = (int64_t)A.T * A.n_q, per = AT_THREADS / (D / 8);
+            bl_attn_tile_join<D><<<(unsigned)((rows + per - 1) / per), AT_THREADS, 0, st>>>(A);
+        }
+    }
+}
+
+extern "C" bl_status bl_attn_kv8(const bl_attn_desc* a, bl_stream s) {
+    if (const bl_status rc = at_check(a)) return rc;
+    const at_plan p = at_make_plan(a);
+    if (p.bytes && !a->workspace) return BL_ERR_WORKSPACE;
+    if (!bl_aligned(a->workspace, 256)) return BL_ERR_ALIGN;
+    const bl_kv_cache& c = a->cache;
+    if ((int64_t)p.row_tiles * c.n_kv * p.splits > 0x7fffffff) return BL_ERR_SHAPE;
+    at_args A = {};
+    A.k = (const uint8_t*)c.k, A.v = (const uint8_t*)c.v, A.k_scale = c.k_scale, A.v_scale = c.v_scale;
+    A.q = a->q, A.q_start = a->q_start, A.seq_len = a->seq_len, A.table = a->table, A.out = a->out;
+    A.k_stride = c.k_stride, A.v_stride = c.v_stride, A.scale_stride = c.scale_stride;
+    A.q_stride = a->q_stride, A.out_stride = a->out_stride, A.table_stride = a->table_stride;
+    A.n_blocks = (int)c.n_blocks, A.n_kv = c.n_kv, A.G = a->n_q / c.n_kv, A.n_q = a->n_q, A.B = (int)a->B, A.T = (int)a->T;
+    A.shift = bl_log2(c.block), A.max_tokens = a->max_blocks * c.block, A.window = a->window;
+    A.factor = a->softmax_scale * 1.44269504f;
+    A.splits = p.splits, A.row_tiles = p.row_tiles;
+    const hipStream_t st = (hipStream_t)s;
+    if (c.kind == BL_KV_INT8) c.head_dim == 128 ? at_launch<BL_KV_INT8, 128>(A, p, a, st) : at_launch<BL_KV_INT8, 64>(A, p, a, st);
+    else c.head_dim == 128 ? at_launch<BL_KV_E4M3, 128>(A, p, a, st) : at_launch<BL_KV_E4M3, 64>(A, p, a, st);
+    return hipGetLastError() == hipSuccess ? BL_OK : BL_ERR_HIP;
+}

@@ -1,0 +1,462 @@
+/* Key/value cache of 8-bit codes: the block tables of a step and the rotary append of its tokens (bitlinear.h). */
+#include "bl_device.h"
+#include "bl_kv.h"
+
+/* ---- block tables and slot maps ---------------------------------------------------------------------------------- */
+
+#define TAB_THREADS 1024
+#define TAB_WAVES (TAB_THREADS / BL_WAVE)
+#define TAB_PER (BL_KV_MAX_REQUESTS / TAB_THREADS)
+#define TAB_ROWS_INSIDE 4096       /* rows whose slots the table kernel writes itself */
+
+/* Sum of v over the threads in front of this one, and over all (in *total).  s: TAB_WAVES values, reused after a barrier. */
+__device__ __forceinline__ int64_t tab_scan(int64_t v, int64_t* s, int64_t* total) {
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    int64_t x = v;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int64_t y = __shfl_up(x, d);
+        if (lane >= d) x += y;
+    }
+    __syncthreads();
+    if (lane == 63) s[w] = x;
+    __syncthreads();
+    int64_t before = 0, all = 0;
+#pragma unroll
+    for (int i = 0; i < TAB_WAVES; ++i) {
+        const int64_t t = s[i];
+        before += i < w ? t : 0;
+        all += t;
+    }
+    *total = all;
+    return before + x - v;
+}
+
+/* Position and slot of row t of the batch: its request by bisection in the B + 1 ascending first rows. */
+__device__ __forceinline__ void tab_row(int64_t t, int B, const int* q_start, const int* start, const int32_t* table, int64_t table_stride,
+                                        int shift, int32_t* positions, int32_t* slots) {
+    int pos = 0, slot = -1;
+    if (t < q_start[B]) {
+        int lo = 0, hi = B;                      /* q_start[lo] <= t < q_start[hi] */
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (q_start[mid] <= t) lo = mid;
+            else hi = mid;
+        }
+        if (start[lo] >= 0) {
+            pos = start[lo] + (int)(t - q_start[lo]);
+            slot = (int)(((uint32_t)table[lo * table_stride + (pos >> shift)] << shift) + (uint32_t)(pos & ((1 << shift) - 1)));
+        }
+    }
+    positions[t] = pos;
+    slots[t] = slot;
+}
+
+struct tab_args {
+    bl_kv_batch b;
+    int shift;
+};
+
+/* One workgroup: a handful of requests, or a few thousand, is latency and not work.  Three sums over the requests (rows
+ * and returned blocks, then demand, which needs them), the copies between stack and table by whole waves, then the rows.
+ * A thread holds TAB_PER consecutive requests where there are more than threads. */
+__global__ __launch_bounds__(TAB_THREADS) void bl_kv_tables_kernel(tab_args A) {
+    const bl_kv_batch& b = A.b;
+    __shared__ int64_t s_sum[TAB_WAVES];
+    __shared__ int s_start[BL_KV_MAX_REQUESTS], s_row[BL_KV_MAX_REQUESTS + 1];
+    __shared__ int s_taken, s_bad;
+    const int tid = threadIdx.x, B = (int)b.B, shift = A.shift, bs1 = (1 << shift) - 1;
+    const int per = (B + TAB_THREADS - 1) / TAB_THREADS;
+    if (tid == 0) s_taken = s_bad = 0;
+    int old[TAB_PER], n[TAB_PER];
+    int64_t rows = 0, back = 0;
+#pragma unroll
+    for (int i = 0; i < TAB_PER; ++i) {
+        const int r = tid * per + i;
+        old[i] = n[i] = 0;
+        if (i < per && r < B) {
+            const int64_t most = (int64_t)b.max_blocks << shift;
+            const int64_t L = b.seq_len[r];
+            old[i] = (int)(L < 0 ? 0 : L > most ? most : L);
+            n[i] = b.new_len[r];
+        }
+        if (n[i] < 0) back += (old[i] + bs1) >> shift;
+        else rows += n[i];
+    }
+    const int64_t cap = b.free_cap;
+    int64_t there = b.free_count[0];
+    there = there < 0 ? 0 : there > cap ? cap : there;
+    int64_t all_rows, all_back;
+    int64_t row = tab_scan(rows, s_sum, &all_rows);
+    int64_t at = there + tab_scan(back, s_sum, &all_back);
+    const int lane = tid & 63;
+    /* ended requests: their blocks to the stack, a request at a time by its whole wave */
+#pragma unroll
+    for (int i = 0; i < TAB_PER; ++i) {
+        if (i >= per) break;
+        const int r = tid * per + i, have = n[i] < 0 ? (old[i] + bs1) >> shift : 0;
+        uint64_t todo = __ballot(have > 0);
+        const int64_t mine = at;
+        if (have > 0 && mine + have > cap) atomicAdd(&s_bad, 1);
+        at += have;
+        while (todo) {
+            const int l = __builtin_ctzll(todo);
+            todo &= todo - 1;
+            const int h = __shfl(have, l), rr = __shfl(r, l);
+            const int64_t to = __shfl(mine, l);
+            for (int j = lane; j < h && to + j < cap; j += 64) b.free_list[to + j] = b.table[rr * b.table_stride + j];
+        }
+    }
+    there = there + all_back > cap ? cap : there + all_back;
+    /* demand */
+    int64_t want = 0, row_i = row;
+    int w_i[TAB_PER];
+    bool fits[TAB_PER];
+#pragma unroll
+    for (int i = 0; i < TAB_PER; ++i) {
+        const int64_t need = ((int64_t)old[i] + (n[i] > 0 ? n[i] : 0) + bs1) >> shift;
+        row_i += n[i] > 0 ? n[i] : 0;
+        fits[i] = n[i] >= 0 && need <= b.max_blocks && row_i <= b.rows;
+        w_i[i] = fits[i] ? (int)(need - ((old[i] + bs1) >> shift)) : 0;
+        want += w_i[i];
+    }
+    int64_t all_want;
+    int64_t upto = tab_scan(want, s_sum, &all_want);       /* (its barriers: the stack is whole behind them) */
+    row_i = row;
+#pragma unroll
+    for (int i = 0; i < TAB_PER; ++i) {
+        if (i >= per) break;
+        const int r = tid * per + i;
+        const bool live = r < B;
+        const int64_t before = upto;
+        upto += w_i[i];
+        const bool ok = live && fits[i] && (w_i[i] == 0 || upto <= there);
+        if (live && n[i] >= 0 && !ok) atomicAdd(&s_bad, 1);
+        if (ok && w_i[i] > 0) atomicMax(&s_taken, (int)upto);
+        if (live) {
+            const int first = (int)(row_i < b.rows ? row_i : b.rows), st = ok ? old[i] : -1;
+            s_start[r] = b.start[r] = st;
+            s_row[r] = b.q_start[r] = first;
+            b.seq_len_out[r] = n[i] < 0 ? 0 : ok ? old[i] + n[i] : old[i];
+        }
+        row_i += n[i] > 0 ? n[i] : 0;
+        const int have = (old[i] + bs1) >> shift;
+        uint64_t todo = __ballot(ok && w_i[i] > 0);
+        while (todo) {
+            const int l = __builtin_ctzll(todo);
+            todo &= todo - 1;
+            const int w = __shfl(w_i[i], l), rr = __shfl(r, l), h = __shfl(have, l);
+            const int64_t from = there - 1 - __shfl(before, l);
+            for (int j = lane; j < w; j += 64) b.table[rr * b.table_stride + h + j] = b.free_list[from - j];
+        }
+    }
+    if (tid == 0) s_row[B] = b.q_start[B] = (int)(all_rows < b.rows ? all_rows : b.rows);
+    __syncthreads();
+    if (tid == 0) {
+        b.free_count_out[0] = (int)there - s_taken;
+        b.bad[0] = s_bad;
+    }
+    if (b.rows <= TAB_ROWS_INSIDE)
+        for (int64_t t = tid; t < b.rows; t += TAB_THREADS) tab_row(t, B, s_row, s_start, b.table, b.table_stride, shift, b.positions, b.slots);
+}
+
+/* The rows of a large batch, behind the table kernel: one thread a row. */
+__global__ __launch_bounds__(256) void bl_kv_slots_kernel(tab_args A) {
+    const bl_kv_batch& b = A.b;
+    const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (t < b.rows) tab_row(t, (int)b.B, b.q_start, b.start, b.table, b.table_stride, A.shift, b.positions, b.slots);
+}
+
+extern "C" bl_status bl_kv_tables(const bl_kv_batch* b, bl_stream s) {
+    if (!b || !b->seq_len || !b->new_len || !b->free_count || !b->table || (!b->free_list && b->free_cap) || !b->seq_len_out || !b->free_count_out || !b->start ||
+        !b->q_start || !b->positions || !b->slots || !b->bad)
+        return BL_ERR_NULL;
+    if (!bl_kv_block_ok(b->block) || b->B < 1 || b->B > BL_KV_MAX_REQUESTS || b->rows < 1 || b->rows > BL_MAX_DIM || b->max_blocks < 1 ||
+        (int64_t)b->max_blocks * b->block > 0x7fffffff || b->table_stride < b->max_blocks || b->table_stride > ((int64_t)1 << 40) || b->free_cap < 0 ||
+        b->free_cap > 0x7fffffff)
+        return BL_ERR_SHAPE;
+    const void* p[] = {b->seq_len, b->new_len, b->free_count, b->table, b->free_list, b->seq_len_out, b->free_count_out, b->start, b->q_start, b->positions, b->slots, b->bad};
+    for (const void* q : p)
+        if (!bl_aligned(q, 4)) return BL_ERR_ALIGN;
+    tab_args A = {*b, bl_log2(b->block)};
+    bl_kv_tables_kernel<<<1, TAB_THREADS, 0, (hipStream_t)s>>>(A);
+    if (b->rows > TAB_ROWS_INSIDE) bl_kv_slots_kernel<<<(unsigned)((b->rows + 255) / 256), 256, 0, (hipStream_t)s>>>(A);
+    return hipGetLastError() == hipSuccess ? BL_OK : BL_ERR_HIP;
+}
+
+/* ---- rotary append ----------------------------------------------------------------------------------------------- */
+
+#define APP_THREADS 256
+
+struct app_args {
+    bl_kv_tokens t;
+    int shift, window;                     /* log2(block); rows of a workgroup */
+};
+
+/* Four consecutive values of a row. */
+template <int SRC>
+__device__ __forceinline__ void app_load4(const void* row, int64_t i, float (&v)[4]) {
+    if (SRC == BL_KV_FROM_F32) {
+        const bl_v4f x = *bl_gc<bl_v4f>((const float*)row + i);
+        v[0] = x[0], v[1] = x[1], v[2] = x[2], v[3] = x[3];
+    } else {
+        const bl_v2u x = *bl_gc<bl_v2u>((const uint16_t*)row + i);
+        v[0] = bl_bf16_to_f32(x[0] & 0xffff), v[1] = __uint_as_float(x[0] & 0xffff0000u);
+        v[2] = bl_bf16_to_f32(x[1] & 0xffff), v[3] = __uint_as_float(x[1] & 0xffff0000u);
+    }
+}
+template <int SRC>
+__device__ __forceinline__ const void* app_row(const app_args& A, int64_t t) {
+    return SRC == BL_KV_FROM_F32 ? (const void*)((const float*)A.t.qkv + t * A.t.qkv_stride) : (const void*)((const uint16_t*)A.t.qkv + t * A.t.qkv_stride);
+}
+/* Values i..i+3 and i+D/2..i+D/2+3 of head h of a row, turned by the angles of position pos where `turn`. */
+template <int SRC, int D>
+__device__ __forceinline__ void app_pair(const app_args& A, const void* row, int h, int i, bool turn, int64_t pos, float (&a)[4], float (&b)[4]) {
+    app_load4<SRC>(row, (int64_t)h * D + i, a);
+    app_load4<SRC>(row, (int64_t)h * D + i + D / 2, b);
+    if (turn) {
+        const bl_v4f c = *bl_gc<bl_v4f>(A.t.cos + pos * (D / 2) + i), s = *bl_gc<bl_v4f>(A.t.sin + pos * (D / 2) + i);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const float x = a[j], y = b[j];
+            a[j] = x * c[j] - y * s[j];
+            b[j] = y * c[j] + x * s[j];
+        }
+    }
+}
+
+/* A value as its code (the low 8 bits). */
+template <int KIND>
+__device__ __forceinline__ uint32_t app_code(float y) {
+    constexpr float T = KIND == BL_KV_INT8 ? 127.0f : 448.0f;
+    y = fminf(fmaxf(y, -T), T);                       /* (a NaN becomes -T) */
+    if (KIND == BL_KV_INT8) return (uint32_t)(int)rintf(y) & 0xff;
+    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y, y, 0, false) & 0xff;
+}
+template <int KIND>
+__device__ __forceinline__ float app_value(uint32_t c) {
+    return KIND == BL_KV_INT8 ? (float)(int8_t)c : __builtin_amdgcn_cvt_f32_fp8((int)c, 0);
+}
+template <int KIND>
+__device__ __forceinline__ uint32_t app_word(const float (&y)[4], float inv) {
+    return app_code<KIND>(y[0] * inv) | app_code<KIND>(y[1] * inv) << 8 | app_code<KIND>(y[2] * inv) << 16 | app_code<KIND>(y[3] * inv) << 24;
+}
+/* The first `bytes` (1..4) codes of a word moved to a scale that is 1/ratio times as large; the other bytes are not written. */
+template <int KIND>
+__device__ __forceinline__ void app_move(uint8_t* p, int bytes, float ratio) {
+    if (bytes == 4) {
+        const uint32_t w = *(const uint32_t*)p;
+        uint32_t o = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) o |= app_code<KIND>(app_value<KIND>((w >> (8 * j)) & 0xff) * ratio) << (8 * j);
+        *(uint32_t*)p = o;
+    } else {
+        for (int j = 0; j < bytes; ++j) p[j] = (uint8_t)app_code<KIND>(app_value<KIND>(p[j]) * ratio);
+    }
+}
+
+/* Whether row t goes into the cache. */
+__device__ __forceinline__ bool app_goes(const app_args& A, int slot, int64_t t) {
+    if (slot < 0 || (int64_t)slot >= A.t.cache.n_blocks << A.shift) return false;
+    if (!A.t.cos) return true;
+    const int pos = A.t.positions[t];
+    return pos >= 0 && pos < A.t.n_pos;
+}
+
+/* blockIdx.x: `window` consecutive rows; blockIdx.y: a kv head's K (y even) or V (y odd), or behind those the rows' Q heads.
+ * K and V: a run is the rows that go to one block (row t + k to the slot k further); the workgroup in whose window it starts does it whole.  Its values (at most block x D fp32) stay in registers between the maximum and the rounding: read once.
+ * Eight values of a row a thread (four and their rotary partners), D/8 threads a row.
+ * Bound by HBM for prompts, by the launch and the chain slots -> rows -> maximum -> codes for single tokens. */
+template <int SRC, int KIND, int D, int NP>
+__global__ __launch_bounds__(APP_THREADS) void bl_kv_append_kernel(app_args A) {
+    constexpr int TPR = D / 8, ROWS = APP_THREADS / TPR;          /* threads a row, rows a pass */
+    constexpr float T = KIND == BL_KV_INT8 ? 127.0f : 448.0f;
+    constexpr int VPAD = 4;                                        /* bytes behind a feature's codes in LDS: other banks */
+    __shared__ float s_max[APP_THREADS / BL_WAVE];
+    __shared__ uint32_t s_v[D * (NP * ROWS + VPAD) / 4];
+    const bl_kv_cache& C = A.t.cache;
+    const int tid = threadIdx.x, H = C.n_kv, bs = 1 << A.shift;
+    const int64_t first = (int64_t)blockIdx.x * A.window, T_all = A.t.T;
+    const int64_t last = first + A.window < T_all ? first + A.window : T_all;
+    const int sub = tid % TPR, rowi = tid / TPR, i4 = sub * 4;
+    if ((int)blockIdx.y >= 2 * H) {
+        /* Q of the rows: units of eight values, thread by thread */
+        const int part = (int)blockIdx.y - 2 * H, parts = (int)gridDim.y - 2 * H;
+        const int units = A.t.n_q * TPR;
+        for (int64_t t = first; t < last; ++t) {
+            const int slot = A.t.slots[t];
+            const int64_t pos = A.t.cos ? A.t.positions[t] : 0;
+            const bool there = !A.t.cos || (pos >= 0 && pos < A.t.n_pos);
+            if (part == 0 && tid == 0 && A.t.bad && (!there || slot < -1 || (int64_t)slot >= C.n_blocks << A.shift)) atomicAdd(A.t.bad, 1);
+            if (!A.t.q_out) continue;
+            const void* row = app_row<SRC>(A, t);
+            uint16_t* o = A.t.q_out + t * A.t.q_stride;
+            for (int u = part * APP_THREADS + tid; u < units; u += parts * APP_THREADS) {
+                const int h = u / TPR, i = u % TPR * 4;
+                float a[4] = {0, 0, 0, 0}, b[4] = {0, 0, 0, 0};
+                if (there) app_pair<SRC, D>(A, row, h, i, A.t.cos != nullptr, pos, a, b);
+                const bl_v2u lo = {bl_pack2_bf16(a[0], a[1]), bl_pack2_bf16(a[2], a[3])}, hi = {bl_pack2_bf16(b[0], b[1]), bl_pack2_bf16(b[2], b[3])};
+                *bl_g((bl_v2u*)(o + h * D + i)) = lo;
+                *bl_g((bl_v2u*)(o + h * D + D / 2 + i)) = hi;
+            }
+        }
+        return;
+    }
+    const int h = (int)blockIdx.y >> 1;
+    const bool is_v = blockIdx.y & 1;
+    const int head = A.t.n_q + (is_v ? H : 0) + h;
+    for (int64_t t0 = first; t0 < last; ++t0) {
+        const int slot = A.t.slots[t0];
+        if (!app_goes(A, slot, t0)) continue;
+        const int off = slot & (bs - 1);
+        /* Rows that stand where this block's tokens in front of this one would: the first of them does the block.  Then the
+         * block's rows from this one on, a bit each (a row may be missing: a slot of -1, a bad position). */
+        uint64_t m0, m1 = 0;
+        {
+            const int lane = tid & 63;
+            auto member = [&](int k) {                    /* row t0 + k, the slot k further */
+                const int64_t t = t0 + k;
+                return t >= 0 && t < T_all && off + k >= 0 && off + k < bs && A.t.slots[t] == slot + k && app_goes(A, slot + k, t);
+            };
+            uint64_t earlier = off ? __ballot(member(-1 - lane)) : 0;
+            if (off > 64) earlier |= __ballot(member(-65 - lane));
+            if (earlier) continue;
+            m0 = __ballot(member(lane));
+            if (bs > 64) m1 = __ballot(member(64 + lane));
+        }
+        const int n = m1 ? 128 - __builtin_clzll(m1) : 64 - __builtin_clzll(m0);
+        auto has = [&](int r) { return r < n && (((r < 64 ? m0 : m1) >> (r & 63)) & 1); };
+        /* values and their maximum */
+        float a[NP][4], b[NP][4], most = 0.0f;
+#pragma unroll
+        for (int p = 0; p < NP; ++p) {
+            const int r = p * ROWS + rowi;
+            if (has(r)) {
+                app_pair<SRC, D>(A, app_row<SRC>(A, t0 + r), head, i4, !is_v && A.t.cos, A.t.cos ? A.t.positions[t0 + r] : 0, a[p], b[p]);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) most = fmaxf(most, fmaxf(fabsf(a[p][j]), fabsf(b[p][j])));   /* fmaxf passes over a NaN */
+            }
+        }
+        most = bl_wave_max(most);
+        __syncthreads();
+        if ((tid & 63) == 0) s_max[tid >> 6] = most;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < APP_THREADS / BL_WAVE; ++w) most = fmaxf(most, s_max[w]);
+        const int64_t blk = slot >> A.shift;
+        float* where = (is_v ? C.v_scale : C.k_scale) + blk * C.scale_stride + h;
+        uint8_t* codes = (uint8_t*)(is_v ? C.v : C.k) + blk * (is_v ? C.v_stride : C.k_stride) + ((int64_t)h << A.shift) * D;
+        float scale = fmaxf(most, 1e-5f) * (1.0f / T);
+        if (off > 0) {
+            const float old = *where;
+            if (scale > old) {
+                /* what the block holds moves to the larger scale */
+                const float ratio = bl_div_rn(old, scale);
+                if (!is_v) {
+                    for (int i = tid; i < off * D / 4; i += APP_THREADS) app_move<KIND>(codes + 4 * i, 4, ratio);
+                } else {
+                    const int words = (off + 3) / 4;
+                    for (int i = tid; i < D * words; i += APP_THREADS) {
+                        const int d = i / words, w = i % words, left = off - 4 * w;
+                        app_move<KIND>(codes + ((int64_t)d << A.shift) + 4 * w, left < 4 ? left : 4, ratio);
+                    }
+                }
+            } else {
+                scale = fmaxf(scale, old);
+            }
+            __syncthreads();                              /* everyone has read the old scale */
+        }
+        if (tid == 0) *where = scale;
+        const float inv = bl_div_rn(1.0f, scale);
+        if (!is_v) {
+#pragma unroll
+            for (int p = 0; p < NP; ++p) {
+                const int r = p * ROWS + rowi;
+                if (has(r)) {
+                    uint8_t* o = codes + (off + r) * D + i4;
+                    *(uint32_t*)o = app_word<KIND>(a[p], inv);
+                    *(uint32_t*)(o + D / 2) = app_word<KIND>(b[p], inv);
+                }
+            }
+        } else if (n == 1) {
+            if (rowi == 0) {
+                const uint32_t lo = app_word<KIND>(a[0], inv), hi = app_word<KIND>(b[0], inv);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    codes[((int64_t)(i4 + j) << A.shift) + off] = (uint8_t)(lo >> (8 * j));
+                    codes[((int64_t)(i4 + D / 2 + j) << A.shift) + off] = (uint8_t)(hi >> (8 * j));
+                }
+            }
+        } else {
+            /* through LDS, where a feature's codes come to stand together as they do in the block (token offset as byte) */
+            const int pitch = NP * ROWS + VPAD;
+            uint8_t* sv = (uint8_t*)s_v;
+#pragma unroll
+            for (int p = 0; p < NP; ++p) {
+                const int r = p * ROWS + rowi;
+                if (has(r)) {
+                    const uint32_t lo = app_word<KIND>(a[p], inv), hi = app_word<KIND>(b[p], inv);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        sv[(i4 + j) * pitch + off + r] = (uint8_t)(lo >> (8 * j));
+                        sv[(i4 + D / 2 + j) * pitch + off + r] = (uint8_t)(hi >> (8 * j));
+                    }
+                }
+            }
+            __syncthreads();
+            const int words = bs / 4, w0 = off / 4, w1 = (off + n + 3) / 4;
+            for (int i = tid; i < D * words; i += APP_THREADS) {
+                const int d = i / words, w = i % words;
+                if (w < w0 || w >= w1) continue;
+                const uint8_t* from = sv + d * pitch + 4 * w;
+                uint8_t* to = codes + ((int64_t)d << A.shift) + 4 * w;
+                const int r = 4 * w - off;
+                if (r >= 0 && has(r) && has(r + 1) && has(r + 2) && has(r + 3)) {
+                    *(uint32_t*)to = *(const uint32_t*)from;
+                } else {
+                    for (int j = 0; j < 4; ++j)
+                        if (r + j >= 0 && has(r + j)) to[j] = from[j];
+                }
+            }
+        }
+        __syncthreads();                                  /* s_max and s_v are free again */
+    }
+}
+
+template <int SRC, int KIND, int D>
+static void app_launch(const app_args& A, dim3 grid, hipStream_t st) {
+    const int passes = (1 << A.shift) * D / (8 * APP_THREADS);
+    if (passes <= 1) bl_kv_append_kernel<SRC, KIND, D, 1><<<grid, APP_THREADS, 0, st>>>(A);
+    else if (passes == 2) bl_kv_append_kernel<SRC, KIND, D, 2><<<grid, APP_THREADS, 0, st>>>(A);
+    else if (D == 64 || passes == 4) bl_kv_append_kernel<SRC, KIND, D, 4><<<grid, APP_THREADS, 0, st>>>(A);
+    else if constexpr (D == 128) bl_kv_append_kernel<SRC, KIND, D, 8><<<grid, APP_THREADS, 0, st>>>(A);
+}
+
+extern "C" bl_status bl_kv_append(const bl_kv_tokens* t, bl_stream s) {
+    if (!t || !t->qkv || !t->slots) return BL_ERR_NULL;
+    if (const bl_status rc = bl_kv_cache_check(&t->cache)) return rc;
+    if (!t->cos != !t->sin || (t->cos && !t->positions)) return BL_ERR_NULL;
+    if (t->qkv_kind != BL_KV_FROM_F32 && t->qkv_kind != BL_KV_FROM_BF16) return BL_ERR_VALUE;
+    const int D = t->cache.head_dim, unit = t->qkv_kind == BL_KV_FROM_F32 ? 4 : 8;
+    const int64_t most = (int64_t)1 << 40;
+    if (t->T < 1 || t->T > BL_MAX_DIM || t->n_q < 0 || t->n_q > 65535 || t->qkv_stride < (t->n_q + 2 * (int64_t)t->cache.n_kv) * D || t->qkv_stride > most ||
+        (t->cos && (t->n_pos < 1 || t->n_pos > 0x7fffffff)) || (t->q_out && (t->n_q < 1 || t->q_stride < (int64_t)t->n_q * D || t->q_stride > most)))
+        return BL_ERR_SHAPE;
+    if (!bl_aligned(t->qkv, 16) || t->qkv_stride % unit || !bl_aligned(t->cos, 16) || !bl_aligned(t->sin, 16) || !bl_aligned(t->slots, 4) ||
+        !bl_aligned(t->positions, 4) || !bl_aligned(t->bad, 4) || !bl_aligned(t->q_out, 16) || (t->q_out && t->q_stride % 8))
+        return BL_ERR_ALIGN;
+    app_args A = {*t, bl_log2(t->cache.block), 1};
+    /* rows a workgroup: one where they are few (each is a run of its own in a decode step), more where they are many (the
+     * runs of prompts start in few windows, and a workgroup without one is not free) */
+    while (A.window < 16 && t->T > 512 * A.window) A.window *= 2;
+    const dim3 grid((unsigned)((t->T + A.window - 1) / A.window), (unsigned)(2 * t->cache.n_kv + 1));
+    const hipStream_t st = (hipStream_t)s;
+    const bool f32 = t->qkv_kind == BL_KV_FROM_F32, i8 = t->cache.kind == BL_KV_INT8;
+#define APP(S, K) (D == 128 ? app_launch<S, K, 128>(A, grid, st) : app_launch<S, K, 64>(A, grid, st))
+    if (f32 && i8) APP(BL_KV_FROM_F32, BL_KV_INT8);
+    else if (f32) APP(BL_KV_FROM_F32, BL_KV_E4M3);
+    else if (i8) APP(BL_KV_FROM_BF16, BL_KV_INT8);
+    else APP(BL_KV_FROM_BF16, BL_KV_E4M3);
+#undef APP
+    return hipGetLastError() == hipSuccess ? BL_OK : BL_ERR_HIP;
+}

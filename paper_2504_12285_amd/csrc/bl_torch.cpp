@@ -25,6 +25,8 @@ product_fn g_product[2];                 /* gemv, gemm */
 decode_fn g_decode;
 typedef bl_status (*run_fn)(void*, const bl_stack_plan*, bl_stream);
 run_fn g_run;
+typedef bl_status (*kv_fn)(const void*, bl_stream);
+kv_fn g_kv[3];                           /* tables, append, attention */
 
 /* A tensor argument: exactly torch.Tensor or None. */
 bool get(PyObject* o, const at::Tensor** t) {
@@ -184,6 +186,21 @@ PyObject* run(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
+/* which, address of the host's descriptor */
+PyObject* kv(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded([&]() -> PyObject* {
+        int64_t which, desc;
+        if (n != 2 || !plain() || !get(a[0], &which) || which < 0 || which > 2 || !get(a[1], &desc) || !desc) return nullptr;
+        const bl_stream st = stream();
+        bl_status rc;
+        Py_BEGIN_ALLOW_THREADS
+        rc = g_kv[which]((const void*)desc, st);
+        Py_END_ALLOW_THREADS
+        if (rc != BL_OK) return PyLong_FromLong(rc);
+        Py_RETURN_NONE;
+    });
+}
+
 /* The addresses of bl_quant_act_int8, bl_gemv_w158a8, bl_gemm_w158a8, bl_bitlinear_decode and bl_stack_run in the
  * loaded library. */
 PyObject* bind(PyObject*, PyObject* args) {
@@ -197,6 +214,14 @@ PyObject* bind(PyObject*, PyObject* args) {
     Py_RETURN_NONE;
 }
 
+/* The addresses of bl_kv_tables, bl_kv_append and bl_attn_kv8 in the loaded library. */
+PyObject* bind_kv(PyObject*, PyObject* args) {
+    unsigned long long f[3];
+    if (!PyArg_ParseTuple(args, "KKK", f, f + 1, f + 2)) return nullptr;
+    for (int i = 0; i < 3; ++i) g_kv[i] = (kv_fn)f[i];
+    Py_RETURN_NONE;
+}
+
 /* The current stream as the calls above see it (compared with the binding's own in a test). */
 PyObject* current_stream(PyObject*, PyObject*) { return PyLong_FromUnsignedLongLong((unsigned long long)stream()); }
 
@@ -204,7 +229,9 @@ PyMethodDef methods[] = {{"quant", (PyCFunction)(void (*)(void))quant, METH_FAST
                          {"product", (PyCFunction)(void (*)(void))product, METH_FASTCALL, nullptr},
                          {"decode", (PyCFunction)(void (*)(void))decode, METH_FASTCALL, nullptr},
                          {"run", (PyCFunction)(void (*)(void))run, METH_FASTCALL, nullptr},
+                         {"kv", (PyCFunction)(void (*)(void))kv, METH_FASTCALL, nullptr},
                          {"bind", bind, METH_VARARGS, nullptr},
+                         {"bind_kv", bind_kv, METH_VARARGS, nullptr},
                          {"current_stream", current_stream, METH_NOARGS, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 /* (the doc string is what tells a build against another torch) */
