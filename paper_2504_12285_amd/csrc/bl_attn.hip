@@ -44,7 +44,7 @@ struct at_args {
     int n_blocks, n_kv, G, n_q, B, T, shift, max_tokens, window;
     float factor;                  /* softmax_scale * log2(e) */
     int splits;                    /* of bl_attn_tile */
-    int row_tiles;                 /* its grid: upper bound of row tiles */
+    int part_skip;                 /* floats in front of the partial results of bl_attn_rows: where each request's tiles end */
 };
 
 /* ---- what both kernels share --------------------------------------------------------------------------------------- */
@@ -166,23 +166,32 @@ __device__ __forceinline__ float at_largest(const uint32_t (&w)[8], float most, 
     return most;
 }
 
-/* Sum over the requests in front of b, and over all: f(b) each.  s: [AT_WAVES + 2]. */
+/* Sum over the lanes up to this one: inside rows of 16, then across them. */
+__device__ __forceinline__ int at_scan(int v) {
+    v += bl_dpp<0x111>(v);                                  /* row_shr 1, 2, 4, 8 */
+    v += bl_dpp<0x112>(v);
+    v += bl_dpp<0x114>(v);
+    v += bl_dpp<0x118>(v);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);   /* row_bcast 15 into rows 1 and 3 */
+    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);   /* row_bcast 31 into rows 2 and 3 */
+    return v;
+}
+/* f(b) summed up to and with request b, for all of them, into s_upto; per thread consecutive requests.  s: AT_WAVES values. */
 template <typename F>
-__device__ __forceinline__ void at_before(int B, int b, F f, int* s, int& before, int& all) {
-    int x = 0, y = 0;
-    for (int i = threadIdx.x; i < B; i += AT_THREADS) {
-        const int c = f(i);
-        y += c;
-        if (i < b) x += c;
-    }
-    x = bl_wave_sum(x), y = bl_wave_sum(y);
-    const int w = threadIdx.x >> 6;
+__device__ __forceinline__ void at_sums(int B, F f, int* s_upto, int* s) {
+    const int per = (B + AT_THREADS - 1) / AT_THREADS, tid = threadIdx.x;
+    int mine = 0;
+    for (int i = 0; i < per; ++i)
+        if (tid * per + i < B) mine += f(tid * per + i);
+    const int x = at_scan(mine);
+    if ((tid & 63) == 63) s[tid >> 6] = x;
     __syncthreads();
-    if ((threadIdx.x & 63) == 0) s[w] = x, s[AT_WAVES + w] = y;
-    __syncthreads();
-    before = all = 0;
+    int sum = x - mine;
 #pragma unroll
-    for (int i = 0; i < AT_WAVES; ++i) before += s[i], all += s[AT_WAVES + i];
+    for (int w = 0; w < AT_WAVES; ++w) sum += w < (tid >> 6) ? s[w] : 0;
+    for (int i = 0; i < per; ++i)
+        if (tid * per + i < B) s_upto[tid * per + i] = sum += f(tid * per + i);
+    __syncthreads();
 }
 
 /* ---- few rows: the cache is streamed ------------------------------------------------------------------------------ */
@@ -215,60 +224,49 @@ template <int KIND, int D>
 __global__ __launch_bounds__(AT_THREADS, 2) void bl_attn_rows(at_args A) {
     constexpr int KS = D / 64, DT = D / 16;                 /* 64-byte steps of a K row, 16-feature tiles of V */
     constexpr int PITCH = D + 4;
-    __shared__ int s_off[BL_KV_MAX_REQUESTS + 1];
-    __shared__ int s_scan[2 * AT_WAVES];
+    __shared__ int s_upto[BL_KV_MAX_REQUESTS];
+    __shared__ int s_scan[AT_WAVES];
     __shared__ float s_o[AT_WAVES][AT_FEW][PITCH];
     __shared__ float s_m[AT_WAVES][AT_FEW], s_l[AT_WAVES][AT_FEW];
     const int tid = threadIdx.x, lane = tid & 63, wave = at_uniform(tid >> 6);
     const int col = lane & 15, grp = lane >> 4;
-    /* where each request's tiles start */
-    {
-        const int per = (A.B + AT_THREADS - 1) / AT_THREADS;
-        int mine = 0;
-        for (int i = 0; i < per; ++i) {
-            const int b = tid * per + i;
-            if (b < A.B) mine += at_few_tiles(A, b);
-        }
-        int x = mine;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const int y = __shfl_up(x, d);
-            if (lane >= d) x += y;
-        }
-        if (lane == 63) s_scan[wave] = x;
-        __syncthreads();
-        int before = x - mine, all = 0;
-#pragma unroll
-        for (int w = 0; w < AT_WAVES; ++w) {
-            if (w < wave) before += s_scan[w];
-            all += s_scan[w];
-        }
-        for (int i = 0; i < per; ++i) {
-            const int b = tid * per + i;
-            if (b < A.B) {
-                s_off[b] = before;
-                before += at_few_tiles(A, b);
-            }
-        }
-        if (tid == 0) s_off[A.B] = all;
-        __syncthreads();
+    /* where each request's tiles end: up to 64 requests by every wave for itself, a lane each, more through LDS */
+    const bool small = A.B <= 64;
+    int upto = 0;
+    int* head_part = (int*)A.part;                           /* bl_attn_rows_join reads them there */
+    if (small) {
+        upto = at_scan(lane < A.B ? at_few_tiles(A, lane) : 0);
+        if (blockIdx.x == 0 && tid < A.B) head_part[tid] = upto;
+    } else {
+        at_sums(A.B, [&](int b) { return at_few_tiles(A, b); }, s_upto, s_scan);
+        if (blockIdx.x == 0)
+            for (int b = tid; b < A.B; b += AT_THREADS) head_part[b] = s_upto[b];
     }
-    const int64_t all = (int64_t)s_off[A.B] * A.n_kv;
-    const int share = at_share((int)all);
+    float* const part = A.part + A.part_skip;
+    const int all = (small ? __builtin_amdgcn_readlane(upto, 63) : at_uniform(s_upto[A.B - 1])) * A.n_kv;
+    const int share = at_share(all);
     int x0 = (int)blockIdx.x * share;
-    const int x1 = x0 + share < all ? x0 + share : (int)all;
+    const int x1 = x0 + share < all ? x0 + share : all;
     const int bs1 = (1 << A.shift) - 1;
 
     while (x0 < x1) {
-        int lo = 0, hi = A.B;                               /* s_off[lo] * n_kv <= x0 < s_off[hi] * n_kv */
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) >> 1;
-            if ((int64_t)s_off[mid] * A.n_kv <= x0) lo = mid;
-            else hi = mid;
+        const int at = x0 / A.n_kv;                          /* the first request whose tiles end behind it */
+        int b, before;
+        if (small) {
+            b = __builtin_ctzll(__ballot(upto > at));
+            before = b ? __builtin_amdgcn_readlane(upto, b - 1) : 0;
+        } else {
+            int lo = -1, hi = A.B - 1;
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) >> 1;
+                if (s_upto[mid] > at) hi = mid;
+                else lo = mid;
+            }
+            b = at_uniform(hi);
+            before = b ? at_uniform(s_upto[b - 1]) : 0;
         }
-        const int b = at_uniform(lo);
-        const int c = at_uniform(s_off[b + 1] - s_off[b]);
-        const int r0 = x0 - at_uniform(s_off[b]) * A.n_kv;
+        const int c = (small ? __builtin_amdgcn_readlane(upto, b) : at_uniform(s_upto[b])) - before;
+        const int r0 = x0 - before * A.n_kv;
         const int h = r0 / c, t0 = r0 % c;
         const int seg = c - t0 < x1 - x0 ? c - t0 : x1 - x0;
         const at_request R = at_read(A, b);
@@ -488,7 +486,7 @@ __global__ __launch_bounds__(AT_THREADS, 2) void bl_attn_rows(at_args A) {
 #pragma unroll
                     for (int j = 0; j < PER; j += 2) to[j / 2] = bl_pack2_bf16(y[j] * inv, y[j + 1] * inv);
                 } else {
-                    float* to = A.part + (int64_t)(2 * blockIdx.x + (t0 == 0)) * at_slot<D>::floats;
+                    float* to = part + (int64_t)(2 * blockIdx.x + (t0 == 0)) * at_slot<D>::floats;
 #pragma unroll
                     for (int j = 0; j < PER; ++j) to[r * D + d0 + j] = y[j];
                     if (d0 == 0) to[AT_FEW * D + 2 * r] = top, to[AT_FEW * D + 2 * r + 1] = sum;
@@ -500,43 +498,62 @@ __global__ __launch_bounds__(AT_THREADS, 2) void bl_attn_rows(at_args A) {
     }
 }
 
-/* Adds up what several workgroups of bl_attn_rows have of one item.  Workgroup: an item; sixteen threads a row. */
+/* Adds up what several workgroups of bl_attn_rows have of one item.  Workgroup: a row; D / 4 threads a partial result, four
+ * partial results of a thread in flight; they meet in LDS. */
 template <int D>
 __global__ __launch_bounds__(AT_THREADS) void bl_attn_rows_join(at_args A) {
-    __shared__ int s_sum[2 * AT_WAVES];
-    const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x;
-    int before, all;
-    at_before(A.B, b, [&](int i) { return at_few_tiles(A, i); }, s_sum, before, all);
-    const int c = at_few_tiles(A, b);
+    constexpr int TPP = D / 4, GROUPS = AT_THREADS / TPP;
+    __shared__ float s_m[GROUPS], s_l[GROUPS], s_y[GROUPS][D];
+    const int h = blockIdx.x, b = blockIdx.y, r = blockIdx.z, tid = threadIdx.x;
+    const int* upto = (const int*)A.part;
+    const int before = b ? upto[b - 1] : 0, c = upto[b] - before;
     if (c == 0) return;
-    const int share = at_share(all * A.n_kv);
+    const int share = at_share(upto[A.B - 1] * A.n_kv);
     const int first = before * A.n_kv + h * c;
     const int w0 = first / share, w1 = (first + c - 1) / share;
     if (w0 == w1) return;                                    /* one workgroup had all of it and wrote the result */
     const at_request R = at_read(A, b);
-    constexpr int PER = D / 16;
-    const int r = tid >> 4, d0 = (tid & 15) * PER;
     if (r >= R.n * A.G) return;
-    float top = -INFINITY;
-    for (int w = w0; w <= w1; ++w) {
-        const float* from = A.part + (int64_t)(2 * w + (w * share <= first)) * at_slot<D>::floats;
-        top = fmaxf(top, from[AT_FEW * D + 2 * r]);
+    const float* part = A.part + A.part_skip;
+    const int g = tid / TPP, d = tid % TPP * 4;
+    float top = -INFINITY, sum = 0.0f;
+    bl_v4f y = {0, 0, 0, 0};
+    for (int w = w0 + g; w <= w1; w += 4 * GROUPS) {
+        float m[4], l[4], best = top;
+        bl_v4f v[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int ww = w + u * GROUPS;
+            const float* from = part + (int64_t)(2 * ww + (ww * share <= first)) * at_slot<D>::floats;
+            m[u] = -INFINITY, l[u] = 0.0f, v[u] = (bl_v4f){0, 0, 0, 0};
+            if (ww <= w1) {
+                m[u] = from[AT_FEW * D + 2 * r], l[u] = from[AT_FEW * D + 2 * r + 1];
+                v[u] = *bl_gc<bl_v4f>(from + r * D + d);
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) best = fmaxf(best, m[u]);
+        const float f = top == best ? 1.0f : __builtin_amdgcn_exp2f(top - best);
+        sum *= f, y *= f, top = best;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const float e = m[u] == top ? 1.0f : __builtin_amdgcn_exp2f(m[u] - top);
+            sum += l[u] * e, y += v[u] * e;
+        }
     }
-    float sum = 0.0f, y[PER];
-#pragma unroll
-    for (int j = 0; j < PER; ++j) y[j] = 0.0f;
-    for (int w = w0; w <= w1; ++w) {
-        const float* from = A.part + (int64_t)(2 * w + (w * share <= first)) * at_slot<D>::floats;
-        const float m = from[AT_FEW * D + 2 * r];
-        const float f = m == top ? 1.0f : __builtin_amdgcn_exp2f(m - top);
-        sum += from[AT_FEW * D + 2 * r + 1] * f;
-#pragma unroll
-        for (int j = 0; j < PER; ++j) y[j] += from[r * D + d0 + j] * f;
+    if (d == 0) s_m[g] = top, s_l[g] = sum;
+    *(bl_v4f*)&s_y[g][d] = y;
+    __syncthreads();
+    if (g) return;
+    for (int i = 1; i < GROUPS; ++i) top = fmaxf(top, s_m[i]);
+    sum = 0.0f, y = (bl_v4f){0, 0, 0, 0};
+    for (int i = 0; i < GROUPS; ++i) {
+        const float e = s_m[i] == top ? 1.0f : __builtin_amdgcn_exp2f(s_m[i] - top);
+        sum += s_l[i] * e, y += *(const bl_v4f*)&s_y[i][d] * e;
     }
     const float inv = sum == 0.0f ? 0.0f : bl_div_rn(1.0f, sum);
-    uint32_t* to = (uint32_t*)(A.out + (R.row0 + r / A.G) * A.out_stride + (h * A.G + r % A.G) * D + d0);
-#pragma unroll
-    for (int j = 0; j < PER; j += 2) to[j / 2] = bl_pack2_bf16(y[j] * inv, y[j + 1] * inv);
+    const bl_v2u u = {bl_pack2_bf16(y[0] * inv, y[1] * inv), bl_pack2_bf16(y[2] * inv, y[3] * inv)};
+    *bl_g((bl_v2u*)(A.out + (R.row0 + r / A.G) * A.out_stride + (h * A.G + r % A.G) * D + d)) = u;
 }
 
 /* ---- many rows: the matrix cores work -------------------------------------------------------------------------------- */
@@ -558,45 +575,35 @@ __global__ __launch_bounds__(AT_THREADS, 2) void bl_attn_tile(at_args A) {
     constexpr int KS = D / 32, DT = D / 32;
     __shared__ __attribute__((aligned(16))) uint8_t s_k[2][KB];
     __shared__ __attribute__((aligned(16))) uint8_t s_v[2][VB];
-    __shared__ int s_find[3];
-    __shared__ int s_scan[2 * AT_WAVES];
+    __shared__ int s_scan[AT_WAVES];
+    static_assert(sizeof(s_v) >= BL_KV_MAX_REQUESTS * sizeof(int), "the requests' sums stand there at first");
     const int tid = threadIdx.x, lane = tid & 63, wave = at_uniform(tid >> 6);
     const int col = lane & 31, half = lane >> 5;
     /* whose tile: blockIdx.x = (row tile * n_kv + head) * splits + piece */
     const int piece = (int)blockIdx.x % A.splits, h = (int)blockIdx.x / A.splits % A.n_kv, want = (int)blockIdx.x / A.splits / A.n_kv;
-    {
-        const int per = (A.B + AT_THREADS - 1) / AT_THREADS;
-        int mine = 0;
-        for (int i = 0; i < per; ++i) {
-            const int b = tid * per + i;
-            if (b < A.B) mine += at_many_tiles(A, b);
+    int b, before, c;
+    if (A.B <= 64) {
+        const int upto = at_scan(lane < A.B ? at_many_tiles(A, lane) : 0);
+        if (want >= __builtin_amdgcn_readlane(upto, 63)) return;
+        b = __builtin_ctzll(__ballot(upto > want));
+        before = b ? __builtin_amdgcn_readlane(upto, b - 1) : 0;
+        c = __builtin_amdgcn_readlane(upto, b) - before;
+    } else {
+        int* s_upto = (int*)s_v;
+        at_sums(A.B, [&](int i) { return at_many_tiles(A, i); }, s_upto, s_scan);
+        if (want >= s_upto[A.B - 1]) return;
+        int lo = -1, hi = A.B - 1;
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (s_upto[mid] > want) hi = mid;
+            else lo = mid;
         }
-        int x = mine;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const int y = __shfl_up(x, d);
-            if (lane >= d) x += y;
-        }
-        if (lane == 63) s_scan[wave] = x;
-        if (tid == 0) s_find[0] = -1;
-        __syncthreads();
-        int before = x - mine;
-#pragma unroll
-        for (int w = 0; w < AT_WAVES; ++w)
-            if (w < wave) before += s_scan[w];
-        for (int i = 0; i < per; ++i) {
-            const int b = tid * per + i;
-            if (b < A.B) {
-                const int c = at_many_tiles(A, b);
-                if (want >= before && want < before + c) s_find[0] = b, s_find[1] = want - before, s_find[2] = c;
-                before += c;
-            }
-        }
+        b = at_uniform(hi);
+        before = b ? at_uniform(s_upto[b - 1]) : 0;
+        c = at_uniform(s_upto[b]) - before;
         __syncthreads();
     }
-    const int b = at_uniform(s_find[0]);
-    if (b < 0) return;
-    const int rt = at_uniform(s_find[2]) - 1 - at_uniform(s_find[1]);      /* the last rows see most: first */
+    const int rt = c - 1 - (want - before);                  /* the last rows see most: first */
     const at_request R = at_read(A, b);
     const int rows = R.n * A.G, bs1 = (1 << A.shift) - 1;
     const int rbase = rt * AT_MANY, rend = rbase + AT_MANY < rows ? rbase + AT_MANY : rows;
@@ -868,7 +875,7 @@ __global__ __launch_bounds__(AT_THREADS) void bl_attn_tile_join(at_args A) {
 
 struct at_plan {
     bool few, many;
-    int splits, row_tiles;
+    int splits, row_tiles, skip, rows;
     size_t few_bytes, bytes;
 };
 
@@ -907,7 +914,9 @@ static at_plan at_make_plan(const bl_attn_desc* a) {
         s = s > by_len ? by_len : s;
         p.splits = s < 1 ? 1 : s > 64 ? 64 : (int)s;
     }
-    p.few_bytes = p.few ? (size_t)AT_ROWS_GRID * 2 * AT_FEW * (D + 2) * sizeof(float) : 0;
+    p.skip = p.few ? (int)((a->B + 63) / 64 * 64) : 0;
+    p.few_bytes = p.few ? ((size_t)AT_ROWS_GRID * 2 * AT_FEW * (D + 2) + p.skip) * sizeof(float) : 0;
+    p.rows = (int)(rows < AT_FEW ? rows : AT_FEW);
     p.bytes = p.few_bytes + (p.splits > 1 ? (size_t)p.splits * a->T * a->n_q * (D + 2) * sizeof(float) : 0);
     return p;
 }
@@ -922,7 +931,7 @@ static void at_launch(at_args A, const at_plan& p, const bl_attn_desc* a, hipStr
     if (p.few) {
         A.part = base;
         bl_attn_rows<KIND, D><<<AT_ROWS_GRID, AT_THREADS, 0, st>>>(A);
-        bl_attn_rows_join<D><<<dim3((unsigned)A.n_kv, (unsigned)A.B), AT_THREADS, 0, st>>>(A);
+        bl_attn_rows_join<D><<<dim3((unsigned)A.n_kv, (unsigned)A.B, (unsigned)p.rows), AT_THREADS, 0, st>>>(A);
     }
     if (p.many) {
         A.part = base + p.few_bytes / sizeof(float);
@@ -949,7 +958,7 @@ extern "C" bl_status bl_attn_kv8(const bl_attn_desc* a, bl_stream s) {
     A.n_blocks = (int)c.n_blocks, A.n_kv = c.n_kv, A.G = a->n_q / c.n_kv, A.n_q = a->n_q, A.B = (int)a->B, A.T = (int)a->T;
     A.shift = bl_log2(c.block), A.max_tokens = a->max_blocks * c.block, A.window = a->window;
     A.factor = a->softmax_scale * 1.44269504f;
-    A.splits = p.splits, A.row_tiles = p.row_tiles;
+    A.splits = p.splits, A.part_skip = p.skip;
     const hipStream_t st = (hipStream_t)s;
     if (c.kind == BL_KV_INT8) c.head_dim == 128 ? at_launch<BL_KV_INT8, 128>(A, p, a, st) : at_launch<BL_KV_INT8, 64>(A, p, a, st);
     else c.head_dim == 128 ? at_launch<BL_KV_E4M3, 128>(A, p, a, st) : at_launch<BL_KV_E4M3, 64>(A, p, a, st);

@@ -190,7 +190,7 @@ extern "C" bl_status bl_kv_tables(const bl_kv_batch* b, bl_stream s) {
 
 struct app_args {
     bl_kv_tokens t;
-    int shift, window;                     /* log2(block); rows of a workgroup */
+    int shift, window, windows;            /* log2(block); rows of a K/V workgroup, and how many such there are */
 };
 
 /* Four consecutive values of a row. */
@@ -263,100 +263,97 @@ __device__ __forceinline__ bool app_goes(const app_args& A, int slot, int64_t t)
     return pos >= 0 && pos < A.t.n_pos;
 }
 
-/* blockIdx.x: `window` consecutive rows; blockIdx.y: a kv head's K (y even) or V (y odd), or behind those the rows' Q heads.
- * K and V: a run is the rows that go to one block (row t + k to the slot k further); the workgroup in whose window it starts does it whole.  Its values (at most block x D fp32) stay in registers between the maximum and the rounding: read once.
- * Eight values of a row a thread (four and their rotary partners), D/8 threads a row.
- * Bound by HBM for prompts, by the launch and the chain slots -> rows -> maximum -> codes for single tokens. */
-template <int SRC, int KIND, int D, int NP>
-__global__ __launch_bounds__(APP_THREADS) void bl_kv_append_kernel(app_args A) {
-    constexpr int TPR = D / 8, ROWS = APP_THREADS / TPR;          /* threads a row, rows a pass */
+/* K and V: a run is the rows that go to one block (row t + k to the slot k further).  A workgroup looks at `window` rows, one a
+ * lane, and does the runs that start there, WAVES waves for K or V of a head, 4 / WAVES of these beside each other: a unit's values
+ * (block x D fp32 at most) stay in registers between the maximum and the rounding, so that a row is read once.
+ * A thread has four values of a row and their rotary partners, D / 8 threads a row, NP rows. */
+template <int SRC, int KIND, int D, int NP, int WAVES>
+__device__ __forceinline__ void app_cache_rows(const app_args& A, int64_t first, int pair) {
+    constexpr int UNITS = APP_THREADS / BL_WAVE / WAVES;
+    constexpr int TPR = D / 8, UT = WAVES * BL_WAVE, ROWS = UT / TPR;   /* threads a row, threads a unit, rows a pass */
     constexpr float T = KIND == BL_KV_INT8 ? 127.0f : 448.0f;
-    constexpr int VPAD = 4;                                        /* bytes behind a feature's codes in LDS: other banks */
+    constexpr int PITCH = NP * ROWS + 4;                                /* of a feature's codes in LDS: 4 bytes more, other banks */
     __shared__ float s_max[APP_THREADS / BL_WAVE];
-    __shared__ uint32_t s_v[D * (NP * ROWS + VPAD) / 4];
+    __shared__ uint32_t s_v[UNITS][D * PITCH / 4];
     const bl_kv_cache& C = A.t.cache;
-    const int tid = threadIdx.x, H = C.n_kv, bs = 1 << A.shift;
-    const int64_t first = (int64_t)blockIdx.x * A.window, T_all = A.t.T;
-    const int64_t last = first + A.window < T_all ? first + A.window : T_all;
+    const int lane = threadIdx.x & 63, H = C.n_kv, bs = 1 << A.shift;
+    const int unit = (int)threadIdx.x / UT, tid = (int)threadIdx.x % UT;
+    const int which = pair * UNITS + unit;                              /* kv head * 2 + (0: K, 1: V) */
+    const bool live = which < 2 * H, is_v = which & 1;
+    const int h = live ? which >> 1 : 0, head = A.t.n_q + (is_v ? H : 0) + h;
     const int sub = tid % TPR, rowi = tid / TPR, i4 = sub * 4;
-    if ((int)blockIdx.y >= 2 * H) {
-        /* Q of the rows: units of eight values, thread by thread */
-        const int part = (int)blockIdx.y - 2 * H, parts = (int)gridDim.y - 2 * H;
-        const int units = A.t.n_q * TPR;
-        for (int64_t t = first; t < last; ++t) {
+    const int64_t T_all = A.t.T;
+    uint64_t todo;
+    {
+        const int64_t t = first + lane;
+        bool goes = false, goes_on = false;
+        if (lane < A.window && t < T_all) {
             const int slot = A.t.slots[t];
-            const int64_t pos = A.t.cos ? A.t.positions[t] : 0;
-            const bool there = !A.t.cos || (pos >= 0 && pos < A.t.n_pos);
-            if (part == 0 && tid == 0 && A.t.bad && (!there || slot < -1 || (int64_t)slot >= C.n_blocks << A.shift)) atomicAdd(A.t.bad, 1);
-            if (!A.t.q_out) continue;
-            const void* row = app_row<SRC>(A, t);
-            uint16_t* o = A.t.q_out + t * A.t.q_stride;
-            for (int u = part * APP_THREADS + tid; u < units; u += parts * APP_THREADS) {
-                const int h = u / TPR, i = u % TPR * 4;
-                float a[4] = {0, 0, 0, 0}, b[4] = {0, 0, 0, 0};
-                if (there) app_pair<SRC, D>(A, row, h, i, A.t.cos != nullptr, pos, a, b);
-                const bl_v2u lo = {bl_pack2_bf16(a[0], a[1]), bl_pack2_bf16(a[2], a[3])}, hi = {bl_pack2_bf16(b[0], b[1]), bl_pack2_bf16(b[2], b[3])};
-                *bl_g((bl_v2u*)(o + h * D + i)) = lo;
-                *bl_g((bl_v2u*)(o + h * D + D / 2 + i)) = hi;
+            goes = app_goes(A, slot, t);
+            if (goes && (slot & (bs - 1)) && t > 0 && A.t.slots[t - 1] == slot - 1) goes_on = app_goes(A, slot - 1, t - 1);
+            if (A.t.bad && pair == 0 && threadIdx.x < 64) {
+                const int pos = A.t.cos ? A.t.positions[t] : 0;
+                if (slot < -1 || (int64_t)slot >= C.n_blocks << A.shift || (A.t.cos && (pos < 0 || pos >= A.t.n_pos))) atomicAdd(A.t.bad, 1);
             }
         }
-        return;
+        todo = __ballot(goes && !goes_on);
     }
-    const int h = (int)blockIdx.y >> 1;
-    const bool is_v = blockIdx.y & 1;
-    const int head = A.t.n_q + (is_v ? H : 0) + h;
-    for (int64_t t0 = first; t0 < last; ++t0) {
-        const int slot = A.t.slots[t0];
-        if (!app_goes(A, slot, t0)) continue;
-        const int off = slot & (bs - 1);
+    while (todo) {
+        const int64_t t0 = first + __builtin_ctzll(todo);
+        todo &= todo - 1;
+        const int slot = A.t.slots[t0], off = slot & (bs - 1);
         /* Rows that stand where this block's tokens in front of this one would: the first of them does the block.  Then the
          * block's rows from this one on, a bit each (a row may be missing: a slot of -1, a bad position). */
         uint64_t m0, m1 = 0;
         {
-            const int lane = tid & 63;
-            auto member = [&](int k) {                    /* row t0 + k, the slot k further */
+            auto member = [&](int k) {                                  /* row t0 + k, the slot k further */
                 const int64_t t = t0 + k;
                 return t >= 0 && t < T_all && off + k >= 0 && off + k < bs && A.t.slots[t] == slot + k && app_goes(A, slot + k, t);
             };
+            m0 = __ballot(member(lane));
+            if (bs > 64) m1 = __ballot(member(64 + lane));
             uint64_t earlier = off ? __ballot(member(-1 - lane)) : 0;
             if (off > 64) earlier |= __ballot(member(-65 - lane));
             if (earlier) continue;
-            m0 = __ballot(member(lane));
-            if (bs > 64) m1 = __ballot(member(64 + lane));
         }
         const int n = m1 ? 128 - __builtin_clzll(m1) : 64 - __builtin_clzll(m0);
         auto has = [&](int r) { return r < n && (((r < 64 ? m0 : m1) >> (r & 63)) & 1); };
+        const int64_t blk = slot >> A.shift;
+        float* where = (is_v ? C.v_scale : C.k_scale) + blk * C.scale_stride + h;
+        uint8_t* codes = (uint8_t*)(is_v ? C.v : C.k) + blk * (is_v ? C.v_stride : C.k_stride) + ((int64_t)h << A.shift) * D;
         /* values and their maximum */
+        const float old = off > 0 ? *where : 0.0f;
         float a[NP][4], b[NP][4], most = 0.0f;
 #pragma unroll
         for (int p = 0; p < NP; ++p) {
             const int r = p * ROWS + rowi;
-            if (has(r)) {
-                app_pair<SRC, D>(A, app_row<SRC>(A, t0 + r), head, i4, !is_v && A.t.cos, A.t.cos ? A.t.positions[t0 + r] : 0, a[p], b[p]);
+            if (live && has(r)) app_pair<SRC, D>(A, app_row<SRC>(A, t0 + r), head, i4, !is_v && A.t.cos, A.t.cos ? A.t.positions[t0 + r] : 0, a[p], b[p]);
+            else
 #pragma unroll
-                for (int j = 0; j < 4; ++j) most = fmaxf(most, fmaxf(fabsf(a[p][j]), fabsf(b[p][j])));   /* fmaxf passes over a NaN */
-            }
+                for (int j = 0; j < 4; ++j) a[p][j] = b[p][j] = 0.0f;
         }
-        most = bl_wave_max(most);
-        __syncthreads();
-        if ((tid & 63) == 0) s_max[tid >> 6] = most;
-        __syncthreads();
 #pragma unroll
-        for (int w = 0; w < APP_THREADS / BL_WAVE; ++w) most = fmaxf(most, s_max[w]);
-        const int64_t blk = slot >> A.shift;
-        float* where = (is_v ? C.v_scale : C.k_scale) + blk * C.scale_stride + h;
-        uint8_t* codes = (uint8_t*)(is_v ? C.v : C.k) + blk * (is_v ? C.v_stride : C.k_stride) + ((int64_t)h << A.shift) * D;
+        for (int p = 0; p < NP; ++p)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) most = fmaxf(most, fmaxf(fabsf(a[p][j]), fabsf(b[p][j])));   /* fmaxf passes over a NaN */
+        most = bl_wave_max(most);
+        if (WAVES > 1) {
+            __syncthreads();                                            /* (s_max and s_v of the run before are read) */
+            if (lane == 0) s_max[threadIdx.x >> 6] = most;
+            __syncthreads();
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) most = fmaxf(most, s_max[unit * WAVES + w]);
+        }
         float scale = fmaxf(most, 1e-5f) * (1.0f / T);
         if (off > 0) {
-            const float old = *where;
             if (scale > old) {
                 /* what the block holds moves to the larger scale */
                 const float ratio = bl_div_rn(old, scale);
-                if (!is_v) {
-                    for (int i = tid; i < off * D / 4; i += APP_THREADS) app_move<KIND>(codes + 4 * i, 4, ratio);
-                } else {
+                if (live && !is_v) {
+                    for (int i = tid; i < off * D / 4; i += UT) app_move<KIND>(codes + 4 * i, 4, ratio);
+                } else if (live) {
                     const int words = (off + 3) / 4;
-                    for (int i = tid; i < D * words; i += APP_THREADS) {
+                    for (int i = tid; i < D * words; i += UT) {
                         const int d = i / words, w = i % words, left = off - 4 * w;
                         app_move<KIND>(codes + ((int64_t)d << A.shift) + 4 * w, left < 4 ? left : 4, ratio);
                     }
@@ -364,22 +361,21 @@ __global__ __launch_bounds__(APP_THREADS) void bl_kv_append_kernel(app_args A) {
             } else {
                 scale = fmaxf(scale, old);
             }
-            __syncthreads();                              /* everyone has read the old scale */
         }
-        if (tid == 0) *where = scale;
+        if (live && tid == 0) *where = scale;                           /* (every thread of the unit has read the old one in front of the maximum) */
         const float inv = bl_div_rn(1.0f, scale);
         if (!is_v) {
 #pragma unroll
             for (int p = 0; p < NP; ++p) {
                 const int r = p * ROWS + rowi;
-                if (has(r)) {
+                if (live && has(r)) {
                     uint8_t* o = codes + (off + r) * D + i4;
                     *(uint32_t*)o = app_word<KIND>(a[p], inv);
                     *(uint32_t*)(o + D / 2) = app_word<KIND>(b[p], inv);
                 }
             }
         } else if (n == 1) {
-            if (rowi == 0) {
+            if (live && rowi == 0) {
                 const uint32_t lo = app_word<KIND>(a[0], inv), hi = app_word<KIND>(b[0], inv);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
@@ -389,8 +385,7 @@ __global__ __launch_bounds__(APP_THREADS) void bl_kv_append_kernel(app_args A) {
             }
         } else {
             /* through LDS, where a feature's codes come to stand together as they do in the block (token offset as byte) */
-            const int pitch = NP * ROWS + VPAD;
-            uint8_t* sv = (uint8_t*)s_v;
+            uint8_t* sv = (uint8_t*)s_v[unit];
 #pragma unroll
             for (int p = 0; p < NP; ++p) {
                 const int r = p * ROWS + rowi;
@@ -398,38 +393,86 @@ __global__ __launch_bounds__(APP_THREADS) void bl_kv_append_kernel(app_args A) {
                     const uint32_t lo = app_word<KIND>(a[p], inv), hi = app_word<KIND>(b[p], inv);
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        sv[(i4 + j) * pitch + off + r] = (uint8_t)(lo >> (8 * j));
-                        sv[(i4 + D / 2 + j) * pitch + off + r] = (uint8_t)(hi >> (8 * j));
+                        sv[(i4 + j) * PITCH + off + r] = (uint8_t)(lo >> (8 * j));
+                        sv[(i4 + D / 2 + j) * PITCH + off + r] = (uint8_t)(hi >> (8 * j));
                     }
                 }
             }
+        }
+        if (n > 1) {
             __syncthreads();
-            const int words = bs / 4, w0 = off / 4, w1 = (off + n + 3) / 4;
-            for (int i = tid; i < D * words; i += APP_THREADS) {
-                const int d = i / words, w = i % words;
-                if (w < w0 || w >= w1) continue;
-                const uint8_t* from = sv + d * pitch + 4 * w;
-                uint8_t* to = codes + ((int64_t)d << A.shift) + 4 * w;
-                const int r = 4 * w - off;
-                if (r >= 0 && has(r) && has(r + 1) && has(r + 2) && has(r + 3)) {
-                    *(uint32_t*)to = *(const uint32_t*)from;
-                } else {
-                    for (int j = 0; j < 4; ++j)
-                        if (r + j >= 0 && has(r + j)) to[j] = from[j];
+            if (live && is_v) {
+                const uint8_t* sv = (const uint8_t*)s_v[unit];
+                const int lw = A.shift - 2, words = 1 << lw, w0 = off / 4, w1 = (off + n + 3) / 4;
+                for (int i = tid; i < D << lw; i += UT) {
+                    const int d = i >> lw, w = i & (words - 1);
+                    if (w < w0 || w >= w1) continue;
+                    const uint8_t* from = sv + d * PITCH + 4 * w;
+                    uint8_t* to = codes + 4 * i;
+                    const int r = 4 * w - off;
+                    if (r >= 0 && has(r) && has(r + 1) && has(r + 2) && has(r + 3)) {
+                        *(uint32_t*)to = *(const uint32_t*)from;
+                    } else {
+                        for (int j = 0; j < 4; ++j)
+                            if (r + j >= 0 && has(r + j)) to[j] = from[j];
+                    }
                 }
             }
+            if (WAVES == 1) __syncthreads();                            /* s_v is free again */
         }
-        __syncthreads();                                  /* s_max and s_v are free again */
     }
 }
 
-template <int SRC, int KIND, int D>
-static void app_launch(const app_args& A, dim3 grid, hipStream_t st) {
-    const int passes = (1 << A.shift) * D / (8 * APP_THREADS);
-    if (passes <= 1) bl_kv_append_kernel<SRC, KIND, D, 1><<<grid, APP_THREADS, 0, st>>>(A);
-    else if (passes == 2) bl_kv_append_kernel<SRC, KIND, D, 2><<<grid, APP_THREADS, 0, st>>>(A);
-    else if (D == 64 || passes == 4) bl_kv_append_kernel<SRC, KIND, D, 4><<<grid, APP_THREADS, 0, st>>>(A);
-    else if constexpr (D == 128) bl_kv_append_kernel<SRC, KIND, D, 8><<<grid, APP_THREADS, 0, st>>>(A);
+/* Q of `per` * 256 units of eight values and their partners, beginning at unit0. */
+template <int SRC, int D>
+__device__ __forceinline__ void app_query_units(const app_args& A, uint32_t unit0, int per, uint32_t units_row, uint32_t all) {
+    constexpr int TPH = D / 16;                                         /* units a head */
+    for (int k = 0; k < per; ++k) {
+        const uint32_t u = unit0 + k * APP_THREADS + threadIdx.x;
+        if (u >= all) return;
+        const uint32_t t = u / units_row, r = u % units_row;
+        const int h = (int)(r / TPH), i = (int)(r % TPH) * 8;
+        const int64_t pos = A.t.cos ? A.t.positions[t] : 0;
+        float a[2][4] = {}, b[2][4] = {};
+        if (!A.t.cos || (pos >= 0 && pos < A.t.n_pos)) {
+            const void* row = app_row<SRC>(A, t);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) app_pair<SRC, D>(A, row, h, i + 4 * j, A.t.cos != nullptr, pos, a[j], b[j]);
+        }
+        uint16_t* o = A.t.q_out + (int64_t)t * A.t.q_stride + h * D + i;
+        typedef uint32_t v4u __attribute__((ext_vector_type(4)));
+        *bl_g((v4u*)o) = (v4u){bl_pack2_bf16(a[0][0], a[0][1]), bl_pack2_bf16(a[0][2], a[0][3]), bl_pack2_bf16(a[1][0], a[1][1]), bl_pack2_bf16(a[1][2], a[1][3])};
+        *bl_g((v4u*)(o + D / 2)) = (v4u){bl_pack2_bf16(b[0][0], b[0][1]), bl_pack2_bf16(b[0][2], b[0][3]), bl_pack2_bf16(b[1][0], b[1][1]), bl_pack2_bf16(b[1][2], b[1][3])};
+    }
+}
+
+/* Workgroups of K and V (window x head pairs) first, those of Q behind them. */
+template <int SRC, int KIND, int D, int NP, int WAVES>
+__global__ __launch_bounds__(APP_THREADS) void bl_kv_append_kernel(app_args A, int kv_blocks, int per, uint32_t units_row, uint32_t all) {
+    const int x = (int)blockIdx.x;
+    if (x < kv_blocks) app_cache_rows<SRC, KIND, D, NP, WAVES>(A, (int64_t)(x % A.windows) * A.window, x / A.windows);
+    else app_query_units<SRC, D>(A, (uint32_t)(x - kv_blocks) * (uint32_t)per * APP_THREADS, per, units_row, all);
+}
+
+template <int SRC, int KIND, int D, int NP, int WAVES>
+static bl_status app_launch(const app_args& A, hipStream_t st) {
+    constexpr int UNITS = APP_THREADS / BL_WAVE / WAVES;
+    const int64_t units_row = A.t.q_out ? (int64_t)A.t.n_q * (D / 16) : 0, all = A.t.T * units_row;
+    /* two units a thread where that leaves more workgroups than the chip holds */
+    const int per = all > (int64_t)4096 * APP_THREADS ? 2 : 1;
+    const int64_t kv = (int64_t)A.windows * ((2 * A.t.cache.n_kv + UNITS - 1) / UNITS), q = (all + per * APP_THREADS - 1) / (per * APP_THREADS);
+    if (all > 0xf0000000ll || kv + q > 0x7fffffff) return BL_ERR_SHAPE;
+    bl_kv_append_kernel<SRC, KIND, D, NP, WAVES><<<(unsigned)(kv + q), APP_THREADS, 0, st>>>(A, (int)kv, per, units_row ? (uint32_t)units_row : 1, (uint32_t)all);
+    return BL_OK;
+}
+/* Waves and passes by the block's size: 1024 to 2048 values of a block and head are one wave's, 16384 four waves' in eight passes. */
+template <int SRC, int KIND>
+static bl_status app_choose(const app_args& A, hipStream_t st) {
+    if (A.t.cache.head_dim == 128)
+        return A.shift == 4 ? app_launch<SRC, KIND, 128, 4, 1>(A, st) : A.shift == 5 ? app_launch<SRC, KIND, 128, 4, 2>(A, st)
+             : A.shift == 6 ? app_launch<SRC, KIND, 128, 4, 4>(A, st) : app_launch<SRC, KIND, 128, 8, 4>(A, st);
+    return A.shift == 4 ? app_launch<SRC, KIND, 64, 2, 1>(A, st) : A.shift == 5 ? app_launch<SRC, KIND, 64, 4, 1>(A, st)
+         : A.shift == 6 ? app_launch<SRC, KIND, 64, 4, 2>(A, st) : app_launch<SRC, KIND, 64, 4, 4>(A, st);
 }
 
 extern "C" bl_status bl_kv_append(const bl_kv_tokens* t, bl_stream s) {
@@ -445,18 +488,15 @@ extern "C" bl_status bl_kv_append(const bl_kv_tokens* t, bl_stream s) {
     if (!bl_aligned(t->qkv, 16) || t->qkv_stride % unit || !bl_aligned(t->cos, 16) || !bl_aligned(t->sin, 16) || !bl_aligned(t->slots, 4) ||
         !bl_aligned(t->positions, 4) || !bl_aligned(t->bad, 4) || !bl_aligned(t->q_out, 16) || (t->q_out && t->q_stride % 8))
         return BL_ERR_ALIGN;
-    app_args A = {*t, bl_log2(t->cache.block), 1};
-    /* rows a workgroup: one where they are few (each is a run of its own in a decode step), more where they are many (the
+    app_args A = {*t, bl_log2(t->cache.block), 1, 0};
+    /* rows a K/V workgroup: one where they are few (each is a run of its own in a decode step), more where they are many (the
      * runs of prompts start in few windows, and a workgroup without one is not free) */
-    while (A.window < 16 && t->T > 512 * A.window) A.window *= 2;
-    const dim3 grid((unsigned)((t->T + A.window - 1) / A.window), (unsigned)(2 * t->cache.n_kv + 1));
+    while (A.window < 16 && t->T > 256 * A.window) A.window *= 2;
+    A.windows = (int)((t->T + A.window - 1) / A.window);
     const hipStream_t st = (hipStream_t)s;
     const bool f32 = t->qkv_kind == BL_KV_FROM_F32, i8 = t->cache.kind == BL_KV_INT8;
-#define APP(S, K) (D == 128 ? app_launch<S, K, 128>(A, grid, st) : app_launch<S, K, 64>(A, grid, st))
-    if (f32 && i8) APP(BL_KV_FROM_F32, BL_KV_INT8);
-    else if (f32) APP(BL_KV_FROM_F32, BL_KV_E4M3);
-    else if (i8) APP(BL_KV_FROM_BF16, BL_KV_INT8);
-    else APP(BL_KV_FROM_BF16, BL_KV_E4M3);
-#undef APP
+    const bl_status rc = f32 ? i8 ? app_choose<BL_KV_FROM_F32, BL_KV_INT8>(A, st) : app_choose<BL_KV_FROM_F32, BL_KV_E4M3>(A, st)
+                             : i8 ? app_choose<BL_KV_FROM_BF16, BL_KV_INT8>(A, st) : app_choose<BL_KV_FROM_BF16, BL_KV_E4M3>(A, st);
+    if (rc) return rc;
     return hipGetLastError() == hipSuccess ? BL_OK : BL_ERR_HIP;
 }
