@@ -383,7 +383,7 @@ bl_status bl_gemm_w158a8_noalloc(const uint8_t* packed, const float* beta, int l
  *   v        codes [n_blocks][n_kv][head_dim][block]: transposed, so that sixteen tokens of a feature are 16 bytes, which
  *            is what a lane hands to the matrix cores
  *   k_scale, v_scale  fp32 [n_blocks][n_kv]: a code c stands for c * scale of its block and head
- *   k_stride, v_stride  bytes from a block to the next (multiples of 16; at least n_kv * block * head_dim),
+ *   k_stride, v_stride  bytes from a block to the next (multiples of 16; at least n_kv * block * head_dim, below 2^36),
  *   scale_stride        floats from a block's scales to the next's (at least n_kv): other layers' blocks may lie between
  * kind BL_KV_INT8: codes are integers of -127..127; BL_KV_E4M3: OCP e4m3 values (no NaN codes).  head_dim 64 or 128.
  * Scales are >= 0.  What no token has written may hold anything.  n_blocks * block < 2^31. */

@@ -40,7 +40,8 @@ struct at_args {
     const int* table;
     uint16_t* out;
     float* part;                   /* workspace */
-    int64_t k_stride, v_stride, scale_stride, q_stride, out_stride, table_stride;
+    uint32_t k_units, v_units;     /* 16-byte units from a block to the next */
+    int64_t scale_stride, q_stride, out_stride, table_stride;
     int n_blocks, n_kv, G, n_q, B, T, shift, max_tokens, window;
     float factor;                  /* softmax_scale * log2(e) */
     int splits;                    /* of bl_attn_tile */
@@ -165,6 +166,12 @@ __device__ __forceinline__ float at_largest(const uint32_t (&w)[8], float most, 
     }
     return most;
 }
+
+/* What is added to a score of a block whose V scale has the logarithm lv.  Where a row has seen nothing yet (m = -inf), or lv is
+ * none, a masked score of -inf has to stay -inf: no infinity of the other sign is added. */
+__device__ __forceinline__ float at_shift(float lv, float m) { return fminf(lv + AT_LIFT - m, 1e30f); }
+/* Bytes from block 0 to block b, `units` of 16 bytes a block. */
+__device__ __forceinline__ int64_t at_far(int b, uint32_t units) { return (int64_t)(((uint64_t)(uint32_t)b * units) << 4); }
 
 /* Sum over the lanes up to this one: inside rows of 16, then across them. */
 __device__ __forceinline__ int at_scan(int v) {
@@ -322,7 +329,7 @@ __global__ __launch_bounds__(AT_THREADS, 2) void bl_attn_rows(at_args A) {
         const int kgrp = (col >> 2) * 16, krow = col & 3;
         auto load_k = [&](int tile, int page, bl_v4i (&k)[4][KS]) {
             const int tok = tile * AT_TILE + kgrp;
-            const uint8_t* p = A.k + (int64_t)(page < 0 ? 0 : page) * A.k_stride + head_k + (int64_t)((tok & bs1) + krow) * D + grp * 16;
+            const uint8_t* p = A.k + at_far(page < 0 ? 0 : page, A.k_units) + head_k + (int64_t)((tok & bs1) + krow) * D + grp * 16;
 #pragma unroll
             for (int t = 0; t < 4; ++t)
 #pragma unroll
@@ -339,7 +346,7 @@ __global__ __launch_bounds__(AT_THREADS, 2) void bl_attn_rows(at_args A) {
                 const int tok = tile * AT_TILE + grp * 16;            /* first of this lane's sixteen tokens */
                 bl_v4i v[DT];
                 {
-                    const uint8_t* p = A.v + (int64_t)(pv < 0 ? 0 : pv) * A.v_stride + head_v + ((int64_t)col << A.shift) + (tok & bs1);
+                    const uint8_t* p = A.v + at_far(pv < 0 ? 0 : pv, A.v_units) + head_v + ((int64_t)col << A.shift) + (tok & bs1);
 #pragma unroll
                     for (int i = 0; i < DT; ++i) v[i] = __builtin_nontemporal_load(bl_gc<bl_v4i>(p + ((int64_t)(16 * i) << A.shift)));
                 }
@@ -392,16 +399,8 @@ __global__ __launch_bounds__(AT_THREADS, 2) void bl_attn_rows(at_args A) {
                 const float a = a_row * ks0;
                 const float vsc = fmaxf(vs0, 0x1p-100f), lv = __builtin_amdgcn_logf(vsc);
                 const bool whole = tile * AT_TILE >= all_from && tile * AT_TILE + AT_TILE <= all_to && __all(pv >= 0);
-                float best = -INFINITY;
-                if (whole) {
-#pragma unroll
-                    for (int t = 0; t < 4; ++t)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            sf[t][i] *= a;
-                            best = fmaxf(best, sf[t][i]);
-                        }
-                } else {
+                if (!whole) {
+                    /* masked scores are -inf, the others have their factor already (0 * -inf is none) */
                     const int end = pv < 0 ? 0 : see1;
 #pragma unroll
                     for (int t = 0; t < 4; ++t)
@@ -409,10 +408,14 @@ __global__ __launch_bounds__(AT_THREADS, 2) void bl_attn_rows(at_args A) {
                         for (int i = 0; i < 4; ++i) {
                             const int j = tok + 4 * t + i;
                             sf[t][i] = j >= see0 && j < end ? sf[t][i] * a : -INFINITY;
-                            best = fmaxf(best, sf[t][i]);
                         }
                 }
-                best += lv;
+                float best = sf[0][0];
+#pragma unroll
+                for (int t = 0; t < 4; ++t)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) best = fmaxf(best, sf[t][i]);
+                best = __builtin_fmaf(best, whole ? a : 1.0f, lv);
                 if (__any(best > m + AT_GROW)) {
                     float top = fmaxf(m, best);
                     top = fmaxf(top, at_xor(top, 16));
@@ -423,21 +426,18 @@ __global__ __launch_bounds__(AT_THREADS, 2) void bl_attn_rows(at_args A) {
                     for (int i = 0; i < DT; ++i) o[i] *= f;
                     m = top;
                 }
-                const float shift = lv + AT_LIFT - m;
+                const float shift = at_shift(lv, m);
                 float sum = 0.0f;
 #pragma unroll
                 for (int t = 0; t < 4; ++t)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        /* (where nothing is seen yet, m = -inf and the argument -inf + inf: 0 is meant) */
-                        float w = __builtin_amdgcn_exp2f(sf[t][i] + shift);
-                        if (!whole) w = sf[t][i] == -INFINITY ? 0.0f : w;
-                        sf[t][i] = w;
-                        sum += w;
+                        sf[t][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sf[t][i], whole ? a : 1.0f, shift));
+                        sum += sf[t][i];                     /* (fp32: fp16 would lose a block whose V scale is small beside others) */
                     }
-                l += sum * __builtin_amdgcn_rcpf(vsc);
                 const at_v4u p0 = {at_pack_half(sf[0][0], sf[0][1]), at_pack_half(sf[0][2], sf[0][3]), at_pack_half(sf[1][0], sf[1][1]), at_pack_half(sf[1][2], sf[1][3])};
                 const at_v4u p1 = {at_pack_half(sf[2][0], sf[2][1]), at_pack_half(sf[2][2], sf[2][3]), at_pack_half(sf[3][0], sf[3][1]), at_pack_half(sf[3][2], sf[3][3])};
+                l = __builtin_fmaf(sum, __builtin_amdgcn_rcpf(vsc), l);
                 if (!whole) {
                     /* what no token has written may be anything, a NaN times 0 too */
                     const int there = pv < 0 ? 0 : R.len - tok;
@@ -579,19 +579,26 @@ __global__ __launch_bounds__(AT_THREADS, 2) void bl_attn_tile(at_args A) {
     static_assert(sizeof(s_v) >= BL_KV_MAX_REQUESTS * sizeof(int), "the requests' sums stand there at first");
     const int tid = threadIdx.x, lane = tid & 63, wave = at_uniform(tid >> 6);
     const int col = lane & 31, half = lane >> 5;
-    /* whose tile: blockIdx.x = (row tile * n_kv + head) * splits + piece */
-    const int piece = (int)blockIdx.x % A.splits, h = (int)blockIdx.x / A.splits % A.n_kv, want = (int)blockIdx.x / A.splits / A.n_kv;
-    int b, before, c;
+    /* whose tile: place = (row tile * n_kv + head) * splits + piece, a request's heavy tiles first */
+    int place = (int)blockIdx.x, piece, h, want, b, before, c;
+    auto take = [&](int all) {
+        /* Of the 512 workgroups that the chip holds the second 256 go the other way round, so that a unit has a heavy one
+         * and a light one. */
+        const int n = all * A.n_kv * A.splits, both = n < 512 ? n : 512;
+        if (place >= 256 && place < both) place = 255 + both - place;
+        piece = place % A.splits, h = place / A.splits % A.n_kv, want = place / A.splits / A.n_kv;
+        return place < n;
+    };
     if (A.B <= 64) {
         const int upto = at_scan(lane < A.B ? at_many_tiles(A, lane) : 0);
-        if (want >= __builtin_amdgcn_readlane(upto, 63)) return;
+        if (!take(__builtin_amdgcn_readlane(upto, 63))) return;
         b = __builtin_ctzll(__ballot(upto > want));
         before = b ? __builtin_amdgcn_readlane(upto, b - 1) : 0;
         c = __builtin_amdgcn_readlane(upto, b) - before;
     } else {
         int* s_upto = (int*)s_v;
         at_sums(A.B, [&](int i) { return at_many_tiles(A, i); }, s_upto, s_scan);
-        if (want >= s_upto[A.B - 1]) return;
+        if (!take(at_uniform(s_upto[A.B - 1]))) return;
         int lo = -1, hi = A.B - 1;
         while (hi - lo > 1) {
             const int mid = (lo + hi) >> 1;
@@ -658,70 +665,75 @@ __global__ __launch_bounds__(AT_THREADS, 2) void bl_attn_tile(at_args A) {
     float m = -INFINITY, l = 0.0f;
 
     const int64_t head = ((int64_t)h << A.shift) * D;
-    auto page_of = [&](int token) -> int {
-        int p = -1;
-        if (token < R.len) {
-            p = pages[token >> A.shift];
-            p = (unsigned)p < (unsigned)A.n_blocks ? p : -1;
-        }
-        return p;
-    };
-    /* loading: D/64 16-byte units of K and of V a thread */
+    /* Loading: D/64 16-byte units of K and of V a thread.  A tile's blocks are read two tiles ahead (lane g: the block of its
+     * tokens 16g..), its codes and scales one tile ahead, so that no load waits for another's address. */
     constexpr int U = D / 64;
     constexpr int TPK = CH / U;                              /* threads a K row */
     constexpr int TPV = 4 / U;                               /* threads a V row */
     const int kt = tid / TPK, kc = tid % TPK * U;
     const int vd = tid / TPV, vg = tid % TPV * U;
+    const uint8_t* const kbase = A.k + head + kc * 16;
+    const uint8_t* const vbase = A.v + head + ((int64_t)vd << A.shift);
+    struct tile_blocks {
+        int k, v[U], g;                                      /* of the thread's K row, of its V units, of the lane's group (lane & 3) */
+    };
+    auto block_of = [&](int t, int group) -> int {
+        const int token = t * AT_TILE + 16 * group;
+        return t < tend && token < R.len ? pages[token >> A.shift] : -1;
+    };
+    auto fetch_blocks = [&](int t) -> tile_blocks {
+        tile_blocks x;
+        x.k = block_of(t, kt >> 4), x.g = block_of(t, lane & 3);
+#pragma unroll
+        for (int u = 0; u < U; ++u) x.v[u] = block_of(t, vg + u);
+        return x;
+    };
+    auto there = [&](int block) { return (unsigned)block < (unsigned)A.n_blocks; };
     bl_v4i lk[U], lv_[U];
-    auto load = [&](int t) {
+    float ks_next = 0.0f, vs_next = 0.0f;
+    auto load = [&](int t, const tile_blocks& x) {
         const int tok = t * AT_TILE;
-        const int pk = page_of(tok + (kt & ~15));
-        const uint8_t* p = A.k + (int64_t)(pk < 0 ? 0 : pk) * A.k_stride + head + (int64_t)((tok + kt) & bs1) * D + kc * 16;
+        const uint8_t* p = kbase + at_far(there(x.k) ? x.k : 0, A.k_units) + ((tok + kt) & bs1) * D;
 #pragma unroll
         for (int u = 0; u < U; ++u) lk[u] = *bl_gc<bl_v4i>(p + u * 16);
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int g = tok + (vg + u) * 16, pv = page_of(g);
-            const uint8_t* pp = A.v + (int64_t)(pv < 0 ? 0 : pv) * A.v_stride + head + ((int64_t)vd << A.shift) + (g & bs1);
-            lv_[u] = *bl_gc<bl_v4i>(pp);
-            const int there = pv < 0 ? 0 : R.len - g;
-            if (there < 16) lv_[u] = at_first(lv_[u], there);
-        }
+        for (int u = 0; u < U; ++u) lv_[u] = *bl_gc<bl_v4i>(vbase + at_far(there(x.v[u]) ? x.v[u] : 0, A.v_units) + ((tok + 16 * (vg + u)) & bs1));
+        const int64_t sc = (int64_t)(there(x.g) ? x.g : 0) * A.scale_stride + h;
+        ks_next = A.k_scale[sc], vs_next = A.v_scale[sc];
     };
-    auto store = [&](int buf) {
+    auto store = [&](int buf, int t, const tile_blocks& x) {
+        const bool inside = (t + 1) * AT_TILE <= R.len && __all(there(x.g));
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int swz = CH == 8 ? kt & 7 : (kt >> 1) & 3;
             *(bl_v4i*)&s_k[buf][kt * D + (((kc + u) ^ swz) * 16)] = lk[u];
+            /* what no token has written may be anything, a NaN times 0 too */
+            if (!inside) lv_[u] = at_first(lv_[u], there(x.v[u]) ? R.len - t * AT_TILE - 16 * (vg + u) : 0);
             at_v8h a, c;
             at_half16<KIND>(lv_[u], a, c);
             *(at_v8h*)&s_v[buf][vd * 128 + ((((vg + u) * 2) ^ (vd & 7)) * 16)] = a;
             *(at_v8h*)&s_v[buf][vd * 128 + ((((vg + u) * 2 + 1) ^ (vd & 7)) * 16)] = c;
         }
     };
+    tile_blocks blk0 = fetch_blocks(tile), blk1 = fetch_blocks(tile + 1);     /* of the tile computed, and of the next */
     if (tile < tend) {
-        load(tile);
-        store(0);
+        load(tile, blk0);
+        store(0, tile, blk0);
     }
     __syncthreads();
-    int buf = 0;
-    for (; tile < tend; ++tile, buf ^= 1) {
+    for (int buf = 0; tile < tend; ++tile, buf ^= 1) {
         const int tok = tile * AT_TILE;
         const bool more = tile + 1 < tend;
-        if (more) load(tile + 1);
+        const float ks_v = ks_next, vs_v = fmaxf(vs_next, 0x1p-100f);
+        if (more) load(tile + 1, blk1);
+        const tile_blocks blk2 = fetch_blocks(tile + 2);
         if (tok < any_to && tok + AT_TILE > any_from) {
-            float ks[4], vs[4];
-            bool seen = true;
-            bool there[4];
+            const float lv_v = __builtin_amdgcn_logf(vs_v), rv_v = __builtin_amdgcn_rcpf(vs_v);
+            const unsigned groups = (unsigned)__ballot(there(blk0.g)) & 15u;
+            const bool whole = groups == 15u && tok >= all_from && tok + AT_TILE <= all_to;
+            float a[4], lv[4];
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const int p = at_uniform(page_of(tok + 16 * g));
-                there[g] = p >= 0;
-                seen &= p >= 0;
-                ks[g] = A.k_scale[(int64_t)(p < 0 ? 0 : p) * A.scale_stride + h];
-                vs[g] = fmaxf(A.v_scale[(int64_t)(p < 0 ? 0 : p) * A.scale_stride + h], 0x1p-100f);
-            }
-            const bool whole = seen && tok >= all_from && tok + AT_TILE <= all_to;
+            for (int g = 0; g < 4; ++g) a[g] = a_row * bl_lane_f(ks_v, g), lv[g] = bl_lane_f(lv_v, g);
             /* row r = 8a + 4f + b of the first product's tile tt is token 32 tt + 16 (a/2) + 8 f + 4 (a%2) + b */
             const int kr = (col >> 4) * 16 + ((col >> 2) & 1) * 8 + ((col >> 3) & 1) * 4 + (col & 3);
             float sf[2][16];
@@ -760,21 +772,26 @@ __global__ __launch_bounds__(AT_THREADS, 2) void bl_attn_tile(at_args A) {
                     for (int j = 0; j < 16; ++j) sf[tt][j] = s16[j];
                 }
             }
-            float best = -INFINITY, lv[4];
+            if (!whole) {
+                /* masked scores are -inf, the others have their factor already (0 * -inf is none) */
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        float& x = sf[g >> 1][(g & 1) * 8 + j];
+                        const int t = tok + 16 * g + 8 * half + j;
+                        x = (groups >> g & 1) && t >= see0 && t < see1 ? x * a[g] : -INFINITY;
+                    }
+                    a[g] = 1.0f;
+                }
+            }
+            float best = -INFINITY;
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
-                const float a = a_row * ks[g];
-                lv[g] = __builtin_amdgcn_logf(vs[g]);
-                float top = -INFINITY;
+                float top = sf[g >> 1][(g & 1) * 8];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    float& x = sf[g >> 1][(g & 1) * 8 + j];
-                    const int t = tok + 16 * g + 8 * half + j;
-                    x *= a;
-                    if (!whole) x = there[g] && t >= see0 && t < see1 ? x : -INFINITY;
-                    top = fmaxf(top, x);
-                }
-                best = fmaxf(best, top + lv[g]);
+                for (int j = 1; j < 8; ++j) top = fmaxf(top, sf[g >> 1][(g & 1) * 8 + j]);
+                best = fmaxf(best, __builtin_fmaf(top, a[g], lv[g]));
             }
             if (__any(best > m + AT_GROW)) {
                 float top = fmaxf(m, best);
@@ -789,17 +806,15 @@ __global__ __launch_bounds__(AT_THREADS, 2) void bl_attn_tile(at_args A) {
             }
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
-                const float shift = lv[g] + AT_LIFT - m;
-                float sum = 0.0f, w[8];
+                const float shift = at_shift(lv[g], m);
+                float w[8], sum = 0.0f;
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    const float x = sf[g >> 1][(g & 1) * 8 + j];
-                    w[j] = __builtin_amdgcn_exp2f(x + shift);
-                    if (!whole) w[j] = x == -INFINITY ? 0.0f : w[j];
-                    sum += w[j];
+                    w[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(sf[g >> 1][(g & 1) * 8 + j], a[g], shift));
+                    sum += w[j];                             /* (fp32: fp16 would lose a block whose V scale is small beside others) */
                 }
-                l += sum * __builtin_amdgcn_rcpf(vs[g]);
                 const at_v4u p = {at_pack_half(w[0], w[1]), at_pack_half(w[2], w[3]), at_pack_half(w[4], w[5]), at_pack_half(w[6], w[7])};
+                l = __builtin_fmaf(sum, bl_lane_f(rv_v, g), l);
 #pragma unroll
                 for (int i = 0; i < DT; ++i) {
                     const int d = 32 * i + col;
@@ -808,7 +823,8 @@ __global__ __launch_bounds__(AT_THREADS, 2) void bl_attn_tile(at_args A) {
                 }
             }
         }
-        if (more) store(buf ^ 1);
+        if (more) store(buf ^ 1, tile + 1, blk1);
+        blk0 = blk1, blk1 = blk2;
         __syncthreads();
     }
     bl_mfma_fence();
@@ -953,7 +969,7 @@ extern "C" bl_status bl_attn_kv8(const bl_attn_desc* a, bl_stream s) {
     at_args A = {};
     A.k = (const uint8_t*)c.k, A.v = (const uint8_t*)c.v, A.k_scale = c.k_scale, A.v_scale = c.v_scale;
     A.q = a->q, A.q_start = a->q_start, A.seq_len = a->seq_len, A.table = a->table, A.out = a->out;
-    A.k_stride = c.k_stride, A.v_stride = c.v_stride, A.scale_stride = c.scale_stride;
+    A.k_units = (uint32_t)(c.k_stride / 16), A.v_units = (uint32_t)(c.v_stride / 16), A.scale_stride = c.scale_stride;
     A.q_stride = a->q_stride, A.out_stride = a->out_stride, A.table_stride = a->table_stride;
     A.n_blocks = (int)c.n_blocks, A.n_kv = c.n_kv, A.G = a->n_q / c.n_kv, A.n_q = a->n_q, A.B = (int)a->B, A.T = (int)a->T;
     A.shift = bl_log2(c.block), A.max_tokens = a->max_blocks * c.block, A.window = a->window;
