@@ -565,8 +565,8 @@ __device__ __forceinline__ int at_many_tiles(const at_args& A, int b) {
 }
 
 /* A workgroup: 128 rows of one request and kv head, 32 a wave, over a range of its tiles (all that its rows see, or one of
- * `splits` equal pieces).  K codes lie in LDS as they are (16-byte units XOR-ed with the row: a read of 32 rows meets every
- * bank), V as fp16, converted once by the thread that loads it; two buffers, one barrier a tile.  Products of 32 tokens x
+ * `splits` equal pieces).  K codes lie in LDS as they are (16-byte units XOR-ed with the row, so that sixteen lanes of a
+ * read fall on all 64 banks), V as fp16, converted once by the thread that loads it; two buffers, one barrier a tile.  Products of 32 tokens x
  * 32 rows (S^T) and 32 features x 32 rows (O^T): a lane has one row. */
 template <int KIND, int D>
 __global__ __launch_bounds__(AT_THREADS, 2) void bl_attn_tile(at_args A) {
@@ -665,113 +665,148 @@ __global__ __launch_bounds__(AT_THREADS, 2) void bl_attn_tile(at_args A) {
     float m = -INFINITY, l = 0.0f;
 
     const int64_t head = ((int64_t)h << A.shift) * D;
-    /* Loading: D/64 16-byte units of K and of V a thread.  A tile's blocks are read two tiles ahead (lane g: the block of its
-     * tokens 16g..), its codes and scales one tile ahead, so that no load waits for another's address. */
+    /* Loading: a wave's sixteen tokens, D/64 16-byte units of K and of V a lane.  They lie in one block, so that the block's place is
+     * a scalar and the lanes' offsets never change.  A tile's blocks are read two tiles ahead (lane g: the block of its
+     * tokens 16g..), its codes and scales one tile ahead: no load waits for another's address. */
     constexpr int U = D / 64;
-    constexpr int TPK = CH / U;                              /* threads a K row */
-    constexpr int TPV = 4 / U;                               /* threads a V row */
-    const int kt = tid / TPK, kc = tid % TPK * U;
-    const int vd = tid / TPV, vg = tid % TPV * U;
-    const uint8_t* const kbase = A.k + head + kc * 16;
-    const uint8_t* const vbase = A.v + head + ((int64_t)vd << A.shift);
-    struct tile_blocks {
-        int k, v[U], g;                                      /* of the thread's K row, of its V units, of the lane's group (lane & 3) */
-    };
-    auto block_of = [&](int t, int group) -> int {
-        const int token = t * AT_TILE + 16 * group;
+    const int kt = lane >> 2, kc = (lane & 3) * U;           /* K: four lanes a row */
+    const int k_off = kt * D + kc * 16, v_off = lane << A.shift;          /* V: features lane and lane + 64 */
+    auto fetch_blocks = [&](int t) -> int {
+        const int token = t * AT_TILE + 16 * (lane & 3);
         return t < tend && token < R.len ? pages[token >> A.shift] : -1;
-    };
-    auto fetch_blocks = [&](int t) -> tile_blocks {
-        tile_blocks x;
-        x.k = block_of(t, kt >> 4), x.g = block_of(t, lane & 3);
-#pragma unroll
-        for (int u = 0; u < U; ++u) x.v[u] = block_of(t, vg + u);
-        return x;
     };
     auto there = [&](int block) { return (unsigned)block < (unsigned)A.n_blocks; };
     bl_v4i lk[U], lv_[U];
     float ks_next = 0.0f, vs_next = 0.0f;
-    auto load = [&](int t, const tile_blocks& x) {
-        const int tok = t * AT_TILE;
-        const uint8_t* p = kbase + at_far(there(x.k) ? x.k : 0, A.k_units) + ((tok + kt) & bs1) * D;
+    auto load = [&](int t, int blocks) {
+        const int mine = __builtin_amdgcn_readlane(blocks, wave), in = (t * AT_TILE + 16 * wave) & bs1;
+        const uint8_t* kp = A.k + head + at_far(there(mine) ? mine : 0, A.k_units) + in * D;
+        const uint8_t* vp = A.v + head + at_far(there(mine) ? mine : 0, A.v_units) + in;
 #pragma unroll
-        for (int u = 0; u < U; ++u) lk[u] = *bl_gc<bl_v4i>(p + u * 16);
+        for (int u = 0; u < U; ++u) lk[u] = *bl_gc<bl_v4i>(kp + k_off + u * 16);
 #pragma unroll
-        for (int u = 0; u < U; ++u) lv_[u] = *bl_gc<bl_v4i>(vbase + at_far(there(x.v[u]) ? x.v[u] : 0, A.v_units) + ((tok + 16 * (vg + u)) & bs1));
-        const int64_t sc = (int64_t)(there(x.g) ? x.g : 0) * A.scale_stride + h;
+        for (int u = 0; u < U; ++u) lv_[u] = *bl_gc<bl_v4i>(vp + v_off + (u * 64 << A.shift));
+        const int64_t sc = (int64_t)(there(blocks) ? blocks : 0) * A.scale_stride + h;
         ks_next = A.k_scale[sc], vs_next = A.v_scale[sc];
     };
-    auto store = [&](int buf, int t, const tile_blocks& x) {
-        const bool inside = (t + 1) * AT_TILE <= R.len && __all(there(x.g));
+    const int k_row = 16 * wave + kt, k_swz = CH == 8 ? (k_row >> 1) & 7 : (k_row >> 2) & 3;
+    /* What no token has written may be anything, and a NaN times 0 is none: zeros behind the last token of tile t. */
+    auto mend = [&](int t, int blocks) {
+        const int n = there(__builtin_amdgcn_readlane(blocks, wave)) ? R.len - t * AT_TILE - 16 * wave : 0;
+        if (n < 16)
+#pragma unroll
+            for (int u = 0; u < U; ++u) lv_[u] = at_first(lv_[u], n);
+    };
+    auto store = [&](int buf) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int swz = CH == 8 ? kt & 7 : (kt >> 1) & 3;
-            *(bl_v4i*)&s_k[buf][kt * D + (((kc + u) ^ swz) * 16)] = lk[u];
-            /* what no token has written may be anything, a NaN times 0 too */
-            if (!inside) lv_[u] = at_first(lv_[u], there(x.v[u]) ? R.len - t * AT_TILE - 16 * (vg + u) : 0);
+            *(bl_v4i*)&s_k[buf][k_row * D + (((kc + u) ^ k_swz) * 16)] = lk[u];
             at_v8h a, c;
             at_half16<KIND>(lv_[u], a, c);
-            *(at_v8h*)&s_v[buf][vd * 128 + ((((vg + u) * 2) ^ (vd & 7)) * 16)] = a;
-            *(at_v8h*)&s_v[buf][vd * 128 + ((((vg + u) * 2 + 1) ^ (vd & 7)) * 16)] = c;
+            const int d = lane + 64 * u;
+            *(at_v8h*)&s_v[buf][d * 128 + (((2 * wave) ^ ((d >> 1) & 7)) * 16)] = a;
+            *(at_v8h*)&s_v[buf][d * 128 + (((2 * wave + 1) ^ ((d >> 1) & 7)) * 16)] = c;
         }
     };
-    tile_blocks blk0 = fetch_blocks(tile), blk1 = fetch_blocks(tile + 1);     /* of the tile computed, and of the next */
+    /* of the tile computed and of the next two */
+    int blk0 = fetch_blocks(tile), blk1 = fetch_blocks(tile + 1), blk2 = fetch_blocks(tile + 2);
+    float ks_v = 0.0f, vs_v = 0.0f, ks_1 = 0.0f, vs_1 = 0.0f;
     if (tile < tend) {
         load(tile, blk0);
-        store(0, tile, blk0);
+        ks_v = ks_next, vs_v = vs_next;
+        mend(tile, blk0);
+        store(0);
+        load(tile + 1, blk1);
+        ks_1 = ks_next, vs_1 = vs_next;
     }
     __syncthreads();
+    /* row r = 8a + 4f + b of the first product's tile tt is token 32 tt + 16 (a/2) + 8 f + 4 (a%2) + b */
+    const int kr = (col >> 4) * 16 + ((col >> 2) & 1) * 8 + ((col >> 3) & 1) * 4 + (col & 3);
+    const int kr_swz = CH == 8 ? (kr >> 1) & 7 : (kr >> 2) & 3;
+    /* One step: the next tile's codes go to LDS and the one's behind it are asked for while the first product runs, its second
+     * half runs over the first half's conversion, and each group's weights are made while the one's before it are multiplied. */
     for (int buf = 0; tile < tend; ++tile, buf ^= 1) {
         const int tok = tile * AT_TILE;
-        const bool more = tile + 1 < tend;
-        const float ks_v = ks_next, vs_v = fmaxf(vs_next, 0x1p-100f);
-        if (more) load(tile + 1, blk1);
-        const tile_blocks blk2 = fetch_blocks(tile + 2);
+        const int blk3 = fetch_blocks(tile + 3);
+        mend(tile + 1, blk1);
         if (tok < any_to && tok + AT_TILE > any_from) {
-            const float lv_v = __builtin_amdgcn_logf(vs_v), rv_v = __builtin_amdgcn_rcpf(vs_v);
-            const unsigned groups = (unsigned)__ballot(there(blk0.g)) & 15u;
+            float sf[2][16];
+            bl_v4i kk[2][KS];
+#pragma unroll
+            for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+                for (int s = 0; s < KS; ++s) kk[tt][s] = *(const bl_v4i*)&s_k[buf][(tt * 32 + kr) * D + (((2 * s + half) ^ kr_swz) * 16)];
+            auto v_part = [&](int g, int i) { return *(const at_v8h*)&s_v[buf][(32 * i + col) * 128 + (((2 * g + half) ^ ((col >> 1) & 7)) * 16)]; };
+            at_v8h vv[2][DT];
+            if constexpr (KIND == BL_KV_INT8) {
+                bl_v16i sh[2], sl[2];
+#pragma unroll
+                for (int j = 0; j < 16; ++j) sh[0][j] = sl[0][j] = sh[1][j] = sl[1][j] = 0;
+#pragma unroll
+                for (int s = 0; s < KS; ++s) {
+                    sh[0] = __builtin_amdgcn_mfma_i32_32x32x32_i8(kk[0][s], qh[s], sh[0], 0, 0, 0);
+                    sl[0] = __builtin_amdgcn_mfma_i32_32x32x32_i8(kk[0][s], ql[s], sl[0], 0, 0, 0);
+                }
+                store(buf ^ 1);
+#pragma unroll
+                for (int s = 0; s < 2 * KS; ++s) {
+                    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x002, D / 16, 0);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+                sh[1] = __builtin_amdgcn_mfma_i32_32x32x32_i8(kk[1][0], qh[0], sh[1], 0, 0, 0);
+                sl[1] = __builtin_amdgcn_mfma_i32_32x32x32_i8(kk[1][0], ql[0], sl[1], 0, 0, 0);
+                load(tile + 2, blk2);
+                __builtin_amdgcn_sched_barrier(0);          /* (two products between the first half's last and its first reader) */
+#pragma unroll
+                for (int s = 1; s < KS; ++s) {
+                    sh[1] = __builtin_amdgcn_mfma_i32_32x32x32_i8(kk[1][s], qh[s], sh[1], 0, 0, 0);
+                    sl[1] = __builtin_amdgcn_mfma_i32_32x32x32_i8(kk[1][s], ql[s], sl[1], 0, 0, 0);
+                }
+#pragma unroll
+                for (int j = 0; j < 16; ++j) sf[0][j] = (float)((sh[0][j] << 8) + sl[0][j]);
+#pragma unroll
+                for (int s = 2; s < 2 * KS; ++s) {
+                    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x002, 32 / (2 * KS - 2) + 1, 0);
+                }
+                bl_mfma_fence();
+#pragma unroll
+                for (int i = 0; i < DT; ++i) vv[0][i] = v_part(0, i);
+#pragma unroll
+                for (int j = 0; j < 16; ++j) sf[1][j] = (float)((sh[1][j] << 8) + sl[1][j]);
+            } else {
+                at_v16f s16[2];
+#pragma unroll
+                for (int j = 0; j < 16; ++j) s16[0][j] = s16[1][j] = 0.0f;
+#pragma unroll
+                for (int s = 0; s < KS; s += 2)
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) {
+                        at_v8i ka, qa;
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) ka[j] = kk[u & 1][s + j / 4][j % 4], qa[j] = u < 2 ? qh[s + j / 4][j % 4] : ql[s + j / 4][j % 4];
+                        s16[u & 1] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(ka, qa, s16[u & 1], 0, 0, 0, 0, 0, 0);
+                    }
+                store(buf ^ 1);
+                load(tile + 2, blk2);
+#pragma unroll
+                for (int i = 0; i < DT; ++i) vv[0][i] = v_part(0, i);
+#pragma unroll
+                for (int s = 0; s < 2 * KS; ++s) {
+                    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x002, D / 16, 0);
+                }
+                bl_mfma_fence();
+#pragma unroll
+                for (int j = 0; j < 16; ++j) sf[0][j] = s16[0][j], sf[1][j] = s16[1][j];
+            }
+            const float vs_c = fmaxf(vs_v, 0x1p-100f), lv_v = __builtin_amdgcn_logf(vs_c), rv_v = __builtin_amdgcn_rcpf(vs_c);
+            const unsigned groups = (unsigned)__ballot(there(blk0)) & 15u;
             const bool whole = groups == 15u && tok >= all_from && tok + AT_TILE <= all_to;
             float a[4], lv[4];
 #pragma unroll
             for (int g = 0; g < 4; ++g) a[g] = a_row * bl_lane_f(ks_v, g), lv[g] = bl_lane_f(lv_v, g);
-            /* row r = 8a + 4f + b of the first product's tile tt is token 32 tt + 16 (a/2) + 8 f + 4 (a%2) + b */
-            const int kr = (col >> 4) * 16 + ((col >> 2) & 1) * 8 + ((col >> 3) & 1) * 4 + (col & 3);
-            float sf[2][16];
-#pragma unroll
-            for (int tt = 0; tt < 2; ++tt) {
-                const int kt2 = tt * 32 + kr, swz = CH == 8 ? kt2 & 7 : (kt2 >> 1) & 3;
-                bl_v4i kk[KS];
-#pragma unroll
-                for (int s = 0; s < KS; ++s) kk[s] = *(const bl_v4i*)&s_k[buf][kt2 * D + (((2 * s + half) ^ swz) * 16)];
-                if constexpr (KIND == BL_KV_INT8) {
-                    bl_v16i sh, sl;
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) sh[j] = sl[j] = 0;
-#pragma unroll
-                    for (int s = 0; s < KS; ++s) {
-                        sh = __builtin_amdgcn_mfma_i32_32x32x32_i8(kk[s], qh[s], sh, 0, 0, 0);
-                        sl = __builtin_amdgcn_mfma_i32_32x32x32_i8(kk[s], ql[s], sl, 0, 0, 0);
-                    }
-                    bl_mfma_fence();
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) sf[tt][j] = (float)((sh[j] << 8) + sl[j]);
-                } else {
-                    at_v16f s16;
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) s16[j] = 0.0f;
-#pragma unroll
-                    for (int s = 0; s < KS; s += 2) {
-                        at_v8i ka, qa, qb;
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) ka[j] = kk[s + j / 4][j % 4], qa[j] = qh[s + j / 4][j % 4], qb[j] = ql[s + j / 4][j % 4];
-                        s16 = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(ka, qa, s16, 0, 0, 0, 0, 0, 0);
-                        s16 = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(ka, qb, s16, 0, 0, 0, 0, 0, 0);
-                    }
-                    bl_mfma_fence();
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) sf[tt][j] = s16[j];
-                }
-            }
             if (!whole) {
                 /* masked scores are -inf, the others have their factor already (0 * -inf is none) */
 #pragma unroll
@@ -804,8 +839,7 @@ __global__ __launch_bounds__(AT_THREADS, 2) void bl_attn_tile(at_args A) {
                     for (int j = 0; j < 16; ++j) o[i][j] *= f;
                 m = top;
             }
-#pragma unroll
-            for (int g = 0; g < 4; ++g) {
+            auto weights = [&](int g) {
                 const float shift = at_shift(lv[g], m);
                 float w[8], sum = 0.0f;
 #pragma unroll
@@ -813,18 +847,38 @@ __global__ __launch_bounds__(AT_THREADS, 2) void bl_attn_tile(at_args A) {
                     w[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(sf[g >> 1][(g & 1) * 8 + j], a[g], shift));
                     sum += w[j];                             /* (fp32: fp16 would lose a block whose V scale is small beside others) */
                 }
-                const at_v4u p = {at_pack_half(w[0], w[1]), at_pack_half(w[2], w[3]), at_pack_half(w[4], w[5]), at_pack_half(w[6], w[7])};
                 l = __builtin_fmaf(sum, bl_lane_f(rv_v, g), l);
+                return __builtin_bit_cast(at_v8h, (at_v4u){at_pack_half(w[0], w[1]), at_pack_half(w[2], w[3]), at_pack_half(w[4], w[5]), at_pack_half(w[6], w[7])});
+            };
+            at_v8h p = weights(0);
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int i = 0; i < DT; ++i) {
-                    const int d = 32 * i + col;
-                    const at_v8h vv = *(const at_v8h*)&s_v[buf][d * 128 + (((2 * g + half) ^ (d & 7)) * 16)];
-                    o[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vv, __builtin_bit_cast(at_v8h, p), o[i], 0, 0, 0);
+            for (int g = 0; g < 4; ++g) {
+                at_v8h next = p;
+                if (g < 3) {
+#pragma unroll
+                    for (int i = 0; i < DT; ++i) vv[(g + 1) & 1][i] = v_part(g + 1, i);
                 }
+#pragma unroll
+                for (int i = 0; i < DT; ++i) o[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vv[g & 1][i], p, o[i], 0, 0, 0);
+                if (g < 3) {
+                    next = weights(g + 1);
+                    __builtin_amdgcn_sched_group_barrier(0x100, DT, 0);
+#pragma unroll
+                    for (int i = 0; i < DT; ++i) {
+                        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                        __builtin_amdgcn_sched_group_barrier(0x002, 32 / DT + 1, 0);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                p = next;
             }
+        } else {
+            store(buf ^ 1);
+            load(tile + 2, blk2);
         }
-        if (more) store(buf ^ 1, tile + 1, blk1);
-        blk0 = blk1, blk1 = blk2;
+        blk0 = blk1, blk1 = blk2, blk2 = blk3;
+        ks_v = ks_1, vs_v = vs_1, ks_1 = ks_next, vs_1 = vs_next;
         __syncthreads();
     }
     bl_mfma_fence();
