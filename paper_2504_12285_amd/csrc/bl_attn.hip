@@ -23,9 +23,9 @@ typedef uint32_t at_v4u __attribute__((ext_vector_type(4)));
 #define AT_TILE 64                 /* tokens a tile */
 #define AT_THREADS 256
 #define AT_WAVES 4
-#define AT_FEW 16                  /* rows of a request and kv head up to which bl_attn_rows does it */
-#define AT_MANY 128                /* rows a workgroup of bl_attn_tile */
-#define AT_ROWS_GRID 512           /* workgroups of bl_attn_rows */
+#define AT_FEW 16                  /* rows of a request and kv head up to which at_few does it */
+#define AT_MANY 128                /* rows a workgroup of at_many */
+#define AT_ROWS_GRID 512           /* workgroups of at_few: two a unit */
 #define AT_GROW 8.0f
 #define AT_LIFT 6.0f
 
@@ -39,13 +39,15 @@ struct at_args {
     const int* seq_len;
     const int* table;
     uint16_t* out;
-    float* part;                   /* workspace */
+    float* part;                   /* workspace of at_few, and of at_many */
+    float* many_part;
     uint32_t k_units, v_units;     /* 16-byte units from a block to the next */
     int64_t scale_stride, q_stride, out_stride, table_stride;
     int n_blocks, n_kv, G, n_q, B, T, shift, max_tokens, window;
     float factor;                  /* softmax_scale * log2(e) */
-    int splits;                    /* of bl_attn_tile */
-    int part_skip;                 /* floats in front of the partial results of bl_attn_rows: where each request's tiles end */
+    int few_rows;                  /* rows of a request and kv head up to which at_few does it: AT_FEW, or 0 where it is not launched */
+    int splits;                    /* of at_many */
+    int part_skip;                 /* floats in front of the partial results of at_few: where each request's tiles end */
 };
 
 /* ---- what both kernels share --------------------------------------------------------------------------------------- */
@@ -203,7 +205,7 @@ __device__ __forceinline__ void at_sums(int B, F f, int* s_upto, int* s) {
 
 /* ---- few rows: the cache is streamed ------------------------------------------------------------------------------ */
 
-/* Tiles of request b in bl_attn_rows, per kv head: one at least where it has rows to write, none where it is another's. */
+/* Tiles of request b in at_few, per kv head: one at least where it has rows to write, none where it is another's. */
 __device__ __forceinline__ int at_few_tiles(const at_args& A, int b) {
     const at_request r = at_read(A, b);
     const int64_t rows = (int64_t)r.n * A.G;
@@ -223,36 +225,42 @@ struct at_slot {                    /* a workgroup's partial result: rows x (D s
 
 /* The tiles of all requests and kv heads stand in one line (request, head, tile); a workgroup takes an equal piece of it, and a
  * piece may end one head's tiles and begin the next's.  What a piece has of an item that others share goes to the
- * workspace (at most two such: at its ends) and bl_attn_rows_join adds it up.  Inside a piece the four waves
+ * workspace (at most two such: at its ends) and bl_attn_join adds it up.  Inside a piece the four waves
  * take tiles in turn and meet in LDS at its end.
  * A wave: K rows of a tile straight from memory into the registers that the matrix cores read (four 16 x 128 products of
  * codes against the two pieces of q), then V the same way.  V of a tile and K of the next are in flight while one computes. */
+template <int D>
+struct at_few_lds {
+    int upto[BL_KV_MAX_REQUESTS];
+    int scan[AT_WAVES];
+    float o[AT_WAVES][AT_FEW][D + 4];
+    float m[AT_WAVES][AT_FEW], l[AT_WAVES][AT_FEW];
+};
 template <int KIND, int D>
-__global__ __launch_bounds__(AT_THREADS, 2) void bl_attn_rows(at_args A) {
+__device__ __forceinline__ void at_few(const at_args& A, int group, at_few_lds<D>& lds) {
     constexpr int KS = D / 64, DT = D / 16;                 /* 64-byte steps of a K row, 16-feature tiles of V */
-    constexpr int PITCH = D + 4;
-    __shared__ int s_upto[BL_KV_MAX_REQUESTS];
-    __shared__ int s_scan[AT_WAVES];
-    __shared__ float s_o[AT_WAVES][AT_FEW][PITCH];
-    __shared__ float s_m[AT_WAVES][AT_FEW], s_l[AT_WAVES][AT_FEW];
+    int (&s_upto)[BL_KV_MAX_REQUESTS] = lds.upto;
+    auto& s_o = lds.o;
+    auto& s_m = lds.m;
+    auto& s_l = lds.l;
     const int tid = threadIdx.x, lane = tid & 63, wave = at_uniform(tid >> 6);
     const int col = lane & 15, grp = lane >> 4;
     /* where each request's tiles end: up to 64 requests by every wave for itself, a lane each, more through LDS */
     const bool small = A.B <= 64;
     int upto = 0;
-    int* head_part = (int*)A.part;                           /* bl_attn_rows_join reads them there */
+    int* head_part = (int*)A.part;                           /* bl_attn_join reads them there */
     if (small) {
         upto = at_scan(lane < A.B ? at_few_tiles(A, lane) : 0);
-        if (blockIdx.x == 0 && tid < A.B) head_part[tid] = upto;
+        if (group == 0 && tid < A.B) head_part[tid] = upto;
     } else {
-        at_sums(A.B, [&](int b) { return at_few_tiles(A, b); }, s_upto, s_scan);
-        if (blockIdx.x == 0)
+        at_sums(A.B, [&](int b) { return at_few_tiles(A, b); }, s_upto, lds.scan);
+        if (group == 0)
             for (int b = tid; b < A.B; b += AT_THREADS) head_part[b] = s_upto[b];
     }
     float* const part = A.part + A.part_skip;
     const int all = (small ? __builtin_amdgcn_readlane(upto, 63) : at_uniform(s_upto[A.B - 1])) * A.n_kv;
     const int share = at_share(all);
-    int x0 = (int)blockIdx.x * share;
+    int x0 = group * share;
     const int x1 = x0 + share < all ? x0 + share : all;
     const int bs1 = (1 << A.shift) - 1;
 
@@ -486,7 +494,7 @@ __global__ __launch_bounds__(AT_THREADS, 2) void bl_attn_rows(at_args A) {
 #pragma unroll
                     for (int j = 0; j < PER; j += 2) to[j / 2] = bl_pack2_bf16(y[j] * inv, y[j + 1] * inv);
                 } else {
-                    float* to = part + (int64_t)(2 * blockIdx.x + (t0 == 0)) * at_slot<D>::floats;
+                    float* to = part + (int64_t)(2 * group + (t0 == 0)) * at_slot<D>::floats;
 #pragma unroll
                     for (int j = 0; j < PER; ++j) to[r * D + d0 + j] = y[j];
                     if (d0 == 0) to[AT_FEW * D + 2 * r] = top, to[AT_FEW * D + 2 * r + 1] = sum;
@@ -498,62 +506,86 @@ __global__ __launch_bounds__(AT_THREADS, 2) void bl_attn_rows(at_args A) {
     }
 }
 
-/* Adds up what several workgroups of bl_attn_rows have of one item.  Workgroup: a row; D / 4 threads a partial result, four
- * partial results of a thread in flight; they meet in LDS. */
+/* Adds up what several workgroups of at_few have of one item: of the item that the boundary between workgroups edge - 1 and
+ * edge cuts, where no earlier boundary does.  D / 4 threads (a group) a partial result of a row, four in flight.  Few partial
+ * results: a group takes a row, all in the workgroup turn = 0.  Many: the groups share those of a row and meet in LDS, and
+ * the rows are shared by `turns` workgroups. */
 template <int D>
-__global__ __launch_bounds__(AT_THREADS) void bl_attn_rows_join(at_args A) {
+struct at_join_lds {
+    float m[AT_THREADS / (D / 4)], l[AT_THREADS / (D / 4)], y[AT_THREADS / (D / 4)][D];
+};
+template <int D>
+__device__ __forceinline__ void at_few_join(const at_args& A, int edge, int turn, int turns, at_join_lds<D>& lds) {
     constexpr int TPP = D / 4, GROUPS = AT_THREADS / TPP;
-    __shared__ float s_m[GROUPS], s_l[GROUPS], s_y[GROUPS][D];
-    const int h = blockIdx.x, b = blockIdx.y, r = blockIdx.z, tid = threadIdx.x;
+    const int tid = threadIdx.x, lane = tid & 63;
     const int* upto = (const int*)A.part;
+    const int all = upto[A.B - 1] * A.n_kv, share = at_share(all);
+    const int64_t pos = (int64_t)edge * share;
+    if (pos >= all) return;
+    /* the request whose tiles the boundary lies among: the first whose tiles end behind it, 64 at a look */
+    const int at = (int)pos / A.n_kv;
+    int b = 0;
+    if (A.B > 64) {
+        const int i = lane * 64 + 63;
+        b = __builtin_ctzll(__ballot(upto[i < A.B ? i : A.B - 1] > at)) * 64;
+    }
+    b += __builtin_ctzll(__ballot(upto[b + lane < A.B ? b + lane : A.B - 1] > at));
     const int before = b ? upto[b - 1] : 0, c = upto[b] - before;
-    if (c == 0) return;
-    const int share = at_share(upto[A.B - 1] * A.n_kv);
-    const int first = before * A.n_kv + h * c;
+    const int first = before * A.n_kv + ((int)pos - before * A.n_kv) / c * c, h = (first - before * A.n_kv) / c;
     const int w0 = first / share, w1 = (first + c - 1) / share;
-    if (w0 == w1) return;                                    /* one workgroup had all of it and wrote the result */
+    if (w0 != edge - 1 || w1 < edge) return;
     const at_request R = at_read(A, b);
-    if (r >= R.n * A.G) return;
     const float* part = A.part + A.part_skip;
-    const int g = tid / TPP, d = tid % TPP * 4;
-    float top = -INFINITY, sum = 0.0f;
-    bl_v4f y = {0, 0, 0, 0};
-    for (int w = w0 + g; w <= w1; w += 4 * GROUPS) {
-        float m[4], l[4], best = top;
-        bl_v4f v[4];
+    const int g = tid / TPP, d = tid % TPP * 4, rows = R.n * A.G;
+    const bool shared_row = w1 - w0 >= 8;
+    if (!shared_row && turn) return;
+    for (int r = shared_row ? turn : g; r < rows; r += shared_row ? turns : GROUPS) {
+        const int step = shared_row ? GROUPS : 1;
+        float top = -INFINITY, sum = 0.0f;
+        bl_v4f y = {0, 0, 0, 0};
+        for (int w = w0 + (shared_row ? g : 0); w <= w1; w += 4 * step) {
+            float m[4], l[4], best = top;
+            bl_v4f v[4];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            const int ww = w + u * GROUPS;
-            const float* from = part + (int64_t)(2 * ww + (ww * share <= first)) * at_slot<D>::floats;
-            m[u] = -INFINITY, l[u] = 0.0f, v[u] = (bl_v4f){0, 0, 0, 0};
-            if (ww <= w1) {
-                m[u] = from[AT_FEW * D + 2 * r], l[u] = from[AT_FEW * D + 2 * r + 1];
-                v[u] = *bl_gc<bl_v4f>(from + r * D + d);
+            for (int u = 0; u < 4; ++u) {
+                const int ww = w + u * step;
+                const float* from = part + (int64_t)(2 * ww + (ww * share <= first)) * at_slot<D>::floats;
+                m[u] = -INFINITY, l[u] = 0.0f, v[u] = (bl_v4f){0, 0, 0, 0};
+                if (ww <= w1) {
+                    m[u] = from[AT_FEW * D + 2 * r], l[u] = from[AT_FEW * D + 2 * r + 1];
+                    v[u] = *bl_gc<bl_v4f>(from + r * D + d);
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u) best = fmaxf(best, m[u]);
+            const float f = top == best ? 1.0f : __builtin_amdgcn_exp2f(top - best);
+            sum *= f, y *= f, top = best;
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const float e = m[u] == top ? 1.0f : __builtin_amdgcn_exp2f(m[u] - top);
+                sum += l[u] * e, y += v[u] * e;
             }
         }
-#pragma unroll
-        for (int u = 0; u < 4; ++u) best = fmaxf(best, m[u]);
-        const float f = top == best ? 1.0f : __builtin_amdgcn_exp2f(top - best);
-        sum *= f, y *= f, top = best;
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            const float e = m[u] == top ? 1.0f : __builtin_amdgcn_exp2f(m[u] - top);
-            sum += l[u] * e, y += v[u] * e;
+        if (shared_row) {
+            if (d == 0) lds.m[g] = top, lds.l[g] = sum;
+            *(bl_v4f*)&lds.y[g][d] = y;
+            __syncthreads();
+            if (g == 0) {
+                for (int i = 1; i < GROUPS; ++i) top = fmaxf(top, lds.m[i]);
+                sum = 0.0f, y = (bl_v4f){0, 0, 0, 0};
+                for (int i = 0; i < GROUPS; ++i) {
+                    const float e = lds.m[i] == top ? 1.0f : __builtin_amdgcn_exp2f(lds.m[i] - top);
+                    sum += lds.l[i] * e, y += *(const bl_v4f*)&lds.y[i][d] * e;
+                }
+            }
+            __syncthreads();
+        }
+        if (!shared_row || g == 0) {
+            const float inv = sum == 0.0f ? 0.0f : bl_div_rn(1.0f, sum);
+            const bl_v2u u = {bl_pack2_bf16(y[0] * inv, y[1] * inv), bl_pack2_bf16(y[2] * inv, y[3] * inv)};
+            *bl_g((bl_v2u*)(A.out + (R.row0 + r / A.G) * A.out_stride + (h * A.G + r % A.G) * D + d)) = u;
         }
     }
-    if (d == 0) s_m[g] = top, s_l[g] = sum;
-    *(bl_v4f*)&s_y[g][d] = y;
-    __syncthreads();
-    if (g) return;
-    for (int i = 1; i < GROUPS; ++i) top = fmaxf(top, s_m[i]);
-    sum = 0.0f, y = (bl_v4f){0, 0, 0, 0};
-    for (int i = 0; i < GROUPS; ++i) {
-        const float e = s_m[i] == top ? 1.0f : __builtin_amdgcn_exp2f(s_m[i] - top);
-        sum += s_l[i] * e, y += *(const bl_v4f*)&s_y[i][d] * e;
-    }
-    const float inv = sum == 0.0f ? 0.0f : bl_div_rn(1.0f, sum);
-    const bl_v2u u = {bl_pack2_bf16(y[0] * inv, y[1] * inv), bl_pack2_bf16(y[2] * inv, y[3] * inv)};
-    *bl_g((bl_v2u*)(A.out + (R.row0 + r / A.G) * A.out_stride + (h * A.G + r % A.G) * D + d)) = u;
 }
 
 /* ---- many rows: the matrix cores work -------------------------------------------------------------------------------- */
@@ -561,26 +593,32 @@ __global__ __launch_bounds__(AT_THREADS) void bl_attn_rows_join(at_args A) {
 __device__ __forceinline__ int at_many_tiles(const at_args& A, int b) {
     const at_request r = at_read(A, b);
     const int64_t rows = (int64_t)r.n * A.G;
-    return rows > AT_FEW ? (int)((rows + AT_MANY - 1) / AT_MANY) : 0;
+    return rows > A.few_rows ? (int)((rows + AT_MANY - 1) / AT_MANY) : 0;
 }
 
 /* A workgroup: 128 rows of one request and kv head, 32 a wave, over a range of its tiles (all that its rows see, or one of
  * `splits` equal pieces).  K codes lie in LDS as they are (16-byte units XOR-ed with the row, so that sixteen lanes of a
  * read fall on all 64 banks), V as fp16, converted once by the thread that loads it; two buffers, one barrier a tile.  Products of 32 tokens x
  * 32 rows (S^T) and 32 features x 32 rows (O^T): a lane has one row. */
+template <int D>
+struct at_many_lds {
+    union {
+        uint8_t v[2][D * AT_TILE * 2];
+        int upto[BL_KV_MAX_REQUESTS];                       /* at first */
+    };
+    uint8_t k[2][AT_TILE * D];
+    int scan[AT_WAVES];
+};
 template <int KIND, int D>
-__global__ __launch_bounds__(AT_THREADS, 2) void bl_attn_tile(at_args A) {
+__device__ __forceinline__ void at_many(const at_args& A, int place, at_many_lds<D>& lds) {
     constexpr int CH = D / 16;                              /* 16-byte units of a K row */
-    constexpr int KB = AT_TILE * D, VB = D * AT_TILE * 2;
     constexpr int KS = D / 32, DT = D / 32;
-    __shared__ __attribute__((aligned(16))) uint8_t s_k[2][KB];
-    __shared__ __attribute__((aligned(16))) uint8_t s_v[2][VB];
-    __shared__ int s_scan[AT_WAVES];
-    static_assert(sizeof(s_v) >= BL_KV_MAX_REQUESTS * sizeof(int), "the requests' sums stand there at first");
+    auto& s_k = lds.k;
+    auto& s_v = lds.v;
     const int tid = threadIdx.x, lane = tid & 63, wave = at_uniform(tid >> 6);
     const int col = lane & 31, half = lane >> 5;
     /* whose tile: place = (row tile * n_kv + head) * splits + piece, a request's heavy tiles first */
-    int place = (int)blockIdx.x, piece, h, want, b, before, c;
+    int piece, h, want, b, before, c;
     auto take = [&](int all) {
         /* Of the 512 workgroups that the chip holds the second 256 go the other way round, so that a unit has a heavy one
          * and a light one. */
@@ -596,8 +634,8 @@ __global__ __launch_bounds__(AT_THREADS, 2) void bl_attn_tile(at_args A) {
         before = b ? __builtin_amdgcn_readlane(upto, b - 1) : 0;
         c = __builtin_amdgcn_readlane(upto, b) - before;
     } else {
-        int* s_upto = (int*)s_v;
-        at_sums(A.B, [&](int i) { return at_many_tiles(A, i); }, s_upto, s_scan);
+        int* s_upto = lds.upto;
+        at_sums(A.B, [&](int i) { return at_many_tiles(A, i); }, s_upto, lds.scan);
         if (!take(at_uniform(s_upto[A.B - 1]))) return;
         int lo = -1, hi = A.B - 1;
         while (hi - lo > 1) {
@@ -896,13 +934,13 @@ __global__ __launch_bounds__(AT_THREADS, 2) void bl_attn_tile(at_args A) {
             }
     } else {
         const int64_t at = (int64_t)piece * A.T * A.n_q + (int64_t)(R.row0 + qi) * A.n_q + qh_i;
-        float* to = A.part + at * D;
+        float* to = A.many_part + at * D;
 #pragma unroll
         for (int i = 0; i < DT; ++i)
 #pragma unroll
             for (int j = 0; j < 16; j += 4) *bl_g((bl_v4f*)(to + 32 * i + 2 * j + 4 * half)) = (bl_v4f){o[i][j], o[i][j + 1], o[i][j + 2], o[i][j + 3]};
         if (half == 0) {
-            float* ml = A.part + (int64_t)A.splits * A.T * A.n_q * D + 2 * at;
+            float* ml = A.many_part + (int64_t)A.splits * A.T * A.n_q * D + 2 * at;
             ml[0] = m, ml[1] = l;
         }
     }
@@ -910,9 +948,9 @@ __global__ __launch_bounds__(AT_THREADS, 2) void bl_attn_tile(at_args A) {
 
 /* Adds up the pieces of a split: D / 8 threads a (row of the batch, head). */
 template <int D>
-__global__ __launch_bounds__(AT_THREADS) void bl_attn_tile_join(at_args A) {
+__device__ __forceinline__ void at_many_join(const at_args& A, int group) {
     constexpr int TPR = D / 8;
-    const int64_t at = (int64_t)blockIdx.x * (AT_THREADS / TPR) + threadIdx.x / TPR, all = (int64_t)A.T * A.n_q;
+    const int64_t at = (int64_t)group * (AT_THREADS / TPR) + threadIdx.x / TPR, all = (int64_t)A.T * A.n_q;
     if (at >= all) return;
     const int row = (int)(at / A.n_q), d0 = (threadIdx.x % TPR) * 8;
     int lo = 0, hi = A.B;                                     /* whose row it is: q_start[lo] <= row < q_start[hi] */
@@ -923,8 +961,8 @@ __global__ __launch_bounds__(AT_THREADS) void bl_attn_tile_join(at_args A) {
         else hi = mid;
     }
     const at_request R = at_read(A, lo);
-    if ((int64_t)R.n * A.G <= AT_FEW) return;
-    const float* ml = A.part + A.splits * all * D;
+    if ((int64_t)R.n * A.G <= A.few_rows) return;
+    const float* ml = A.many_part + A.splits * all * D;
     float top = -INFINITY;
     for (int s = 0; s < A.splits; ++s) top = fmaxf(top, ml[2 * (s * all + at)]);
     float sum = 0.0f, y[8] = {0, 0, 0, 0, 0, 0, 0, 0};
@@ -932,13 +970,41 @@ __global__ __launch_bounds__(AT_THREADS) void bl_attn_tile_join(at_args A) {
         const float mm = ml[2 * (s * all + at)];
         const float f = mm == top ? 1.0f : __builtin_amdgcn_exp2f(mm - top);
         sum += ml[2 * (s * all + at) + 1] * f;
-        const float* from = A.part + (s * all + at) * D + d0;
+        const float* from = A.many_part + (s * all + at) * D + d0;
 #pragma unroll
         for (int j = 0; j < 8; ++j) y[j] += from[j] * f;
     }
     const float inv = sum == 0.0f ? 0.0f : bl_div_rn(1.0f, sum);
     const at_v4u u = {bl_pack2_bf16(y[0] * inv, y[1] * inv), bl_pack2_bf16(y[2] * inv, y[3] * inv), bl_pack2_bf16(y[4] * inv, y[5] * inv), bl_pack2_bf16(y[6] * inv, y[7] * inv)};
     *(at_v4u*)(A.out + row * A.out_stride + (at % A.n_q) * D + d0) = u;
+}
+
+/* ---- launches ---------------------------------------------------------------------------------------------------------- */
+
+/* A batch without long runs of rows: at_few alone. */
+template <int KIND, int D>
+__global__ __launch_bounds__(AT_THREADS, 2) void bl_attn_few(at_args A) {
+    __shared__ __attribute__((aligned(16))) at_few_lds<D> lds;
+    at_few<KIND, D>(A, (int)blockIdx.x, lds);
+}
+/* Any batch, in one launch: the matrix cores' work first; what streams the cache fills the units as that ends. */
+template <int KIND, int D>
+__global__ __launch_bounds__(AT_THREADS, 2) void bl_attn_any(at_args A, int many) {
+    union lds_t {
+        at_few_lds<D> few;
+        at_many_lds<D> many;
+    };
+    __shared__ __attribute__((aligned(16))) uint8_t lds[sizeof(lds_t)];
+    if ((int)blockIdx.x < many) at_many<KIND, D>(A, (int)blockIdx.x, ((lds_t*)lds)->many);
+    else at_few<KIND, D>(A, (int)blockIdx.x - many, ((lds_t*)lds)->few);
+}
+/* Partial results of both: `few` workgroups for those of at_few, turns x (AT_ROWS_GRID - 1), the others for a split. */
+template <int D>
+__global__ __launch_bounds__(AT_THREADS) void bl_attn_join(at_args A, int few) {
+    __shared__ __attribute__((aligned(16))) at_join_lds<D> lds;
+    const int x = (int)blockIdx.x;
+    if (x < few) at_few_join<D>(A, x % (AT_ROWS_GRID - 1) + 1, x / (AT_ROWS_GRID - 1), few / (AT_ROWS_GRID - 1), lds);
+    else at_many_join<D>(A, x - few);
 }
 
 /* ---- host ------------------------------------------------------------------------------------------------------------- */
@@ -970,8 +1036,8 @@ static at_plan at_make_plan(const bl_attn_desc* a) {
     at_plan p;
     const int G = a->n_q / a->cache.n_kv, D = a->cache.head_dim;
     const int64_t rows = (int64_t)(a->max_q < a->T ? a->max_q : a->T) * G;
-    p.few = G <= AT_FEW;
     p.many = rows > AT_FEW;
+    p.few = G <= AT_FEW && !(p.many && a->B == 1);            /* (one request: of one kind or the other) */
     const int64_t part = a->T < a->B ? a->T : a->B;           /* requests with rows */
     p.row_tiles = (int)(a->T * G / AT_MANY + part);
     p.splits = 1;
@@ -997,20 +1063,19 @@ extern "C" size_t bl_attn_workspace_bytes(const bl_attn_desc* a) {
 
 template <int KIND, int D>
 static void at_launch(at_args A, const at_plan& p, const bl_attn_desc* a, hipStream_t st) {
-    float* base = (float*)a->workspace;
-    if (p.few) {
-        A.part = base;
-        bl_attn_rows<KIND, D><<<AT_ROWS_GRID, AT_THREADS, 0, st>>>(A);
-        bl_attn_rows_join<D><<<dim3((unsigned)A.n_kv, (unsigned)A.B, (unsigned)p.rows), AT_THREADS, 0, st>>>(A);
-    }
+    A.part = (float*)a->workspace;
+    A.many_part = A.part + p.few_bytes / sizeof(float);
+    const int few = p.few ? AT_ROWS_GRID : 0;
     if (p.many) {
-        A.part = base + p.few_bytes / sizeof(float);
-        bl_attn_tile<KIND, D><<<(unsigned)((int64_t)p.row_tiles * A.n_kv * p.splits), AT_THREADS, 0, st>>>(A);
-        if (p.splits > 1) {
-            const int64_t rows = (int64_t)A.T * A.n_q, per = AT_THREADS / (D / 8);
-            bl_attn_tile_join<D><<<(unsigned)((rows + per - 1) / per), AT_THREADS, 0, st>>>(A);
-        }
+        const int many = p.row_tiles * A.n_kv * p.splits;
+        bl_attn_any<KIND, D><<<(unsigned)(many + few), AT_THREADS, 0, st>>>(A, many);
+    } else {
+        bl_attn_few<KIND, D><<<(unsigned)few, AT_THREADS, 0, st>>>(A);
     }
+    const int64_t rows = (int64_t)A.T * A.n_q, per = AT_THREADS / (D / 8);
+    const int few_join = p.few ? (AT_ROWS_GRID - 1) * (p.rows < 4 ? p.rows : 4) : 0;
+    const int64_t join = few_join + (p.splits > 1 ? (rows + per - 1) / per : 0);
+    if (join) bl_attn_join<D><<<(unsigned)join, AT_THREADS, 0, st>>>(A, few_join);
 }
 
 extern "C" bl_status bl_attn_kv8(const bl_attn_desc* a, bl_stream s) {
@@ -1019,7 +1084,7 @@ extern "C" bl_status bl_attn_kv8(const bl_attn_desc* a, bl_stream s) {
     if (p.bytes && !a->workspace) return BL_ERR_WORKSPACE;
     if (!bl_aligned(a->workspace, 256)) return BL_ERR_ALIGN;
     const bl_kv_cache& c = a->cache;
-    if ((int64_t)p.row_tiles * c.n_kv * p.splits > 0x7fffffff) return BL_ERR_SHAPE;
+    if ((int64_t)p.row_tiles * c.n_kv * p.splits > 0x7fff0000) return BL_ERR_SHAPE;
     at_args A = {};
     A.k = (const uint8_t*)c.k, A.v = (const uint8_t*)c.v, A.k_scale = c.k_scale, A.v_scale = c.v_scale;
     A.q = a->q, A.q_start = a->q_start, A.seq_len = a->seq_len, A.table = a->table, A.out = a->out;
@@ -1028,7 +1093,7 @@ extern "C" bl_status bl_attn_kv8(const bl_attn_desc* a, bl_stream s) {
     A.n_blocks = (int)c.n_blocks, A.n_kv = c.n_kv, A.G = a->n_q / c.n_kv, A.n_q = a->n_q, A.B = (int)a->B, A.T = (int)a->T;
     A.shift = bl_log2(c.block), A.max_tokens = a->max_blocks * c.block, A.window = a->window;
     A.factor = a->softmax_scale * 1.44269504f;
-    A.splits = p.splits, A.part_skip = p.skip;
+    A.few_rows = p.few ? AT_FEW : 0, A.splits = p.splits, A.part_skip = p.skip;
     const hipStream_t st = (hipStream_t)s;
     if (c.kind == BL_KV_INT8) c.head_dim == 128 ? at_launch<BL_KV_INT8, 128>(A, p, a, st) : at_launch<BL_KV_INT8, 64>(A, p, a, st);
     else c.head_dim == 128 ? at_launch<BL_KV_E4M3, 128>(A, p, a, st) : at_launch<BL_KV_E4M3, 64>(A, p, a, st);
