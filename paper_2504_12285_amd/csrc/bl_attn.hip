@@ -26,6 +26,7 @@ typedef uint32_t at_v4u __attribute__((ext_vector_type(4)));
 #define AT_FEW 16                  /* rows of a request and kv head up to which at_few does it */
 #define AT_MANY 128                /* rows a workgroup of at_many */
 #define AT_ROWS_GRID 512           /* workgroups of at_few: two a unit */
+#define AT_STREAMS (AT_ROWS_GRID * AT_WAVES)
 #define AT_GROW 8.0f
 #define AT_LIFT 6.0f
 
@@ -206,384 +207,518 @@ __device__ __forceinline__ void at_sums(int B, F f, int* s_upto, int* s) {
 /* ---- few rows: the cache is streamed ------------------------------------------------------------------------------ */
 
 /* Tiles of request b in at_few, per kv head: one at least where it has rows to write, none where it is another's. */
-__device__ __forceinline__ int at_few_tiles(const at_args& A, int b) {
-    const at_request r = at_read(A, b);
+__device__ __forceinline__ int at_few_tiles(const at_args& A, const at_request& r) {
     const int64_t rows = (int64_t)r.n * A.G;
     if (rows == 0 || rows > AT_FEW) return 0;
     const int t = (r.len + AT_TILE - 1) / AT_TILE - at_from(A, r, 0) / AT_TILE;
     return t > 0 ? t : 1;
 }
-/* Tiles a workgroup does, of `all` in the launch. */
+/* Tiles a wave does, of `all` in the launch. */
 __device__ __forceinline__ int at_share(int all) {
-    const int s = (all + AT_ROWS_GRID - 1) / AT_ROWS_GRID;
-    return s > AT_WAVES ? s : AT_WAVES;
+    const int s = (all + AT_STREAMS - 1) / AT_STREAMS;
+    return s > 1 ? s : 1;
 }
 template <int D>
-struct at_slot {                    /* a workgroup's partial result: rows x (D sums, m, l) */
+struct at_slot {                    /* a wave's partial result: rows x (D sums, m, l) */
     static constexpr int floats = AT_FEW * (D + 2);
 };
 
-/* The tiles of all requests and kv heads stand in one line (request, head, tile); a workgroup takes an equal piece of it, and a
+/* The tiles of all requests and kv heads stand in one line (request, head, tile); a wave takes an equal piece of it, and a
  * piece may end one head's tiles and begin the next's.  What a piece has of an item that others share goes to the
- * workspace (at most two such: at its ends) and bl_attn_join adds it up.  Inside a piece the four waves
- * take tiles in turn and meet in LDS at its end.
- * A wave: K rows of a tile straight from memory into the registers that the matrix cores read (four 16 x 128 products of
- * codes against the two pieces of q), then V the same way.  V of a tile and K of the next are in flight while one computes. */
+ * workspace (at most two such: at its ends) and bl_attn_join adds it up.  The four pieces of a workgroup that lie in one item
+ * (at_together) are taken tile by tile in turn instead, and meet in LDS: a quarter of the partial results.
+ * K rows of a tile go straight from memory into the registers that the matrix cores read (four 16 x 128 products of
+ * codes against the two pieces of q), then V the same way.  V of a tile and K of the next are in flight while one computes,
+ * and the block numbers of the one behind: also across the items of a piece. */
+/* Whether workgroup g's four pieces, whole ones, lie in the item of tiles first .. last of the line. */
+__device__ __forceinline__ bool at_together(int g, int share, int first, int last) {
+    return (int64_t)g * AT_WAVES * share >= first && (int64_t)(g + 1) * AT_WAVES * share - 1 <= last;
+}
+template <int D>
+struct at_meet_lds {                /* the waves' shares of one item */
+    float o[AT_WAVES][AT_FEW][D + 4], m[AT_WAVES][AT_FEW], l[AT_WAVES][AT_FEW];
+};
 template <int D>
 struct at_few_lds {
     int upto[BL_KV_MAX_REQUESTS];
+    int2 request[BL_KV_MAX_REQUESTS];                        /* first row * 32 + queries (31: 31 or more, not at_few's), tokens */
     int scan[AT_WAVES];
-    float o[AT_WAVES][AT_FEW][D + 4];
-    float m[AT_WAVES][AT_FEW], l[AT_WAVES][AT_FEW];
 };
-template <int KIND, int D>
+struct at_spot {
+    int b, h, t, c, tile0;          /* request, kv head, tile of c, first tile */
+};
+template <int KIND, int D, bool WIDE>
 __device__ __forceinline__ void at_few(const at_args& A, int group, at_few_lds<D>& lds) {
     constexpr int KS = D / 64, DT = D / 16;                 /* 64-byte steps of a K row, 16-feature tiles of V */
-    int (&s_upto)[BL_KV_MAX_REQUESTS] = lds.upto;
-    auto& s_o = lds.o;
-    auto& s_m = lds.m;
-    auto& s_l = lds.l;
     const int tid = threadIdx.x, lane = tid & 63, wave = at_uniform(tid >> 6);
     const int col = lane & 15, grp = lane >> 4;
     /* where each request's tiles end: up to 64 requests by every wave for itself, a lane each, more through LDS */
     const bool small = A.B <= 64;
     int upto = 0;
-    int* head_part = (int*)A.part;                           /* bl_attn_join reads them there */
+    at_request mine = {0, 0, 0};
+    int4* const heads = (int4*)A.part;                       /* bl_attn_join reads them there: tiles up to it, first row, queries */
     if (small) {
-        upto = at_scan(lane < A.B ? at_few_tiles(A, lane) : 0);
-        if (group == 0 && tid < A.B) head_part[tid] = upto;
+        if (lane < A.B) {
+            mine = at_read(A, lane);
+            upto = at_few_tiles(A, mine);
+        }
+        upto = at_scan(upto);
+        if (group == 0 && tid < A.B) heads[tid] = make_int4(upto, mine.row0, mine.n, 0);
     } else {
-        at_sums(A.B, [&](int b) { return at_few_tiles(A, b); }, s_upto, lds.scan);
-        if (group == 0)
-            for (int b = tid; b < A.B; b += AT_THREADS) head_part[b] = s_upto[b];
+        at_sums(A.B, [&](int b) { return at_few_tiles(A, at_read(A, b)); }, lds.upto, lds.scan);
+        for (int b = tid; b < A.B; b += AT_THREADS) {
+            const at_request r = at_read(A, b);
+            lds.request[b] = make_int2(r.row0 << 5 | (r.n < 31 ? r.n : 31), r.len);
+            if (group == 0) heads[b] = make_int4(lds.upto[b], r.row0, r.n, 0);
+        }
+        __syncthreads();
     }
-    float* const part = A.part + A.part_skip;
-    const int all = (small ? __builtin_amdgcn_readlane(upto, 63) : at_uniform(s_upto[A.B - 1])) * A.n_kv;
-    const int share = at_share(all);
-    int x0 = group * share;
-    const int x1 = x0 + share < all ? x0 + share : all;
-    const int bs1 = (1 << A.shift) - 1;
-
-    while (x0 < x1) {
-        const int at = x0 / A.n_kv;                          /* the first request whose tiles end behind it */
-        int b, before;
+    auto upto_of = [&](int b) { return small ? __builtin_amdgcn_readlane(upto, b) : at_uniform(lds.upto[b]); };
+    auto request = [&](int b) -> at_request {
+        if (small) return {__builtin_amdgcn_readlane(mine.row0, b), __builtin_amdgcn_readlane(mine.n, b), __builtin_amdgcn_readlane(mine.len, b)};
+        const int2 r = lds.request[b];
+        const int x = at_uniform(r.x);
+        return {x >> 5, x & 31, at_uniform(r.y)};
+    };
+    const int all = upto_of(small ? 63 : A.B - 1) * A.n_kv, share = at_share(all);
+    int stream = group * AT_WAVES;
+    if ((int64_t)stream * share >= all) return;
+    /* the request that has tile `at` of the line (of one kv head) */
+    auto find = [&](int at, at_spot& s) -> int {
         if (small) {
-            b = __builtin_ctzll(__ballot(upto > at));
-            before = b ? __builtin_amdgcn_readlane(upto, b - 1) : 0;
+            s.b = __builtin_ctzll(__ballot(upto > at));
         } else {
             int lo = -1, hi = A.B - 1;
             while (hi - lo > 1) {
                 const int mid = (lo + hi) >> 1;
-                if (s_upto[mid] > at) hi = mid;
+                if (lds.upto[mid] > at) hi = mid;
                 else lo = mid;
             }
-            b = at_uniform(hi);
-            before = b ? at_uniform(s_upto[b - 1]) : 0;
+            s.b = at_uniform(hi);
         }
-        const int c = (small ? __builtin_amdgcn_readlane(upto, b) : at_uniform(s_upto[b])) - before;
-        const int r0 = x0 - before * A.n_kv;
-        const int h = r0 / c, t0 = r0 % c;
-        const int seg = c - t0 < x1 - x0 ? c - t0 : x1 - x0;
-        const at_request R = at_read(A, b);
-        const int rows = R.n * A.G;
-        const int tile0 = at_from(A, R, 0) / AT_TILE + t0;
-        const int* pages = A.table + b * A.table_stride;
+        const int before = s.b ? upto_of(s.b - 1) : 0;
+        s.c = upto_of(s.b) - before, s.tile0 = at_from(A, request(s.b), 0) / AT_TILE;
+        return before;
+    };
+    at_spot cur, next, after;                                /* the tile computed, the one loaded, the one whose blocks are read */
+    auto go_to = [&](int x) {
+        const int before = find(x / A.n_kv, cur) * A.n_kv, r = x - before;
+        cur.h = r / cur.c, cur.t = r % cur.c;
+        return before + cur.h * cur.c;
+    };
+    int count = share;
+    const int first = go_to(stream * share);
+    const bool together = at_together(group, share, first, first + cur.c - 1);
+    const int begun0 = cur.t;
+    if (together) {
+        cur.t += wave;
+    } else {
+        stream += wave;
+        const int64_t x0 = (int64_t)stream * share;
+        if (x0 >= all) return;
+        if (wave) go_to((int)x0);
+        if (count > all - (int)x0) count = all - (int)x0;
+    }
+    auto advance = [&](at_spot s) -> at_spot {
+        if (together) {
+            s.t += AT_WAVES;
+        } else if (++s.t == s.c) {
+            s.t = 0;
+            if (++s.h == A.n_kv) {
+                s.h = 0;
+                find(upto_of(s.b), s);
+            }
+        }
+        return s;
+    };
+    next = count > 1 ? advance(cur) : cur;
+    after = count > 2 ? advance(next) : next;
 
-        /* this lane's row: limits and the pieces of q */
-        const int qi = col < rows ? col / A.G : 0;
-        const int see0 = at_from(A, R, qi), see1 = col < rows ? at_to(R, qi) : 0;
-        const int all_from = at_from(A, R, R.n - 1), all_to = at_to(R, 0);     /* tokens that every row sees: [all_from, all_to) */
-        bl_v4i qh[KS], ql[KS];
-        float a_row;
+    const int bs1 = (1 << A.shift) - 1;
+    const int kgrp = (col >> 2) * 16, krow = col & 3;        /* this lane's K row: token kgrp + krow + 4 t of product t; its V: tokens 16 grp .. */
+    const int qi_of = col / A.G, qh_of = col % A.G;
+    struct blocks {
+        int k, v;                                            /* as the table has them; -1: no token there */
+    };
+    auto read_blocks = [&](const at_spot& s) -> blocks {
+        const int len = request(s.b).len, tok = (s.tile0 + s.t) * AT_TILE;
+        const int* pages = A.table + s.b * A.table_stride;
+        return {tok + kgrp < len ? pages[(tok + kgrp) >> A.shift] : -1, tok + 16 * grp < len ? pages[(tok + 16 * grp) >> A.shift] : -1};
+    };
+    auto place = [&](int block) { return (unsigned)block < (unsigned)A.n_blocks ? block : 0; };
+    auto load_k = [&](const at_spot& s, int block, bl_v4i (&k)[4][KS]) {
+        const int in = ((s.tile0 + s.t) * AT_TILE + kgrp) & bs1;
+        const uint8_t* p = A.k + (((int64_t)s.h << A.shift) * D) + at_far(place(block), A.k_units) + (in + krow) * D + grp * 16;
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int i = 0; i < KS; ++i) k[t][i] = __builtin_nontemporal_load(bl_gc<bl_v4i>(p + t * 4 * D + i * 64));
+    };
+    at_v4u raw[KS][2];
+    auto load_q = [&](const at_spot& s) {
+        const at_request R = request(s.b);
+        const bool has = col < R.n * A.G;
+        const uint16_t* src = A.q + (R.row0 + (has ? qi_of : 0)) * A.q_stride + (s.h * A.G + (has ? qh_of : 0)) * D;
+#pragma unroll
+        for (int i = 0; i < KS; ++i) raw[i][0] = *bl_gc<at_v4u>(src + i * 64 + grp * 16), raw[i][1] = *bl_gc<at_v4u>(src + i * 64 + grp * 16 + 8);
+    };
+    bl_v4i qh[KS], ql[KS];
+    float a_row;
+    auto make_pieces = [&]() {
+        float most = 0.0f;
+        bool nan = false;
+        uint32_t w[KS][8];
+#pragma unroll
+        for (int i = 0; i < KS; ++i) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) w[i][j] = raw[i][j >> 2][j & 3];
+            most = at_largest(w[i], most, nan);
+        }
+        most = bl_max_pos(most, at_xor(most, 16));
+        most = bl_max_pos(most, at_xor(most, 32));
+        float inv, scale;
+        at_row_scale<KIND>(most, inv, scale);
+        const uint64_t nans = __ballot(nan);
+        if (nans && ((nans >> col) & 0x0001000100010001ull)) scale = __uint_as_float(0x7fc00000u);
+        a_row = scale * A.factor;
+#pragma unroll
+        for (int i = 0; i < KS; ++i) at_pieces<KIND>(w[i], inv, qh[i], ql[i]);
+    };
+
+    bl_v4i k[4][KS];
+    load_q(cur);
+    const blocks first_blocks = read_blocks(cur);
+    blocks next_blocks = read_blocks(next);
+    int pv = first_blocks.v;
+    load_k(cur, first_blocks.k, k);
+    float ks, vs;
+    {
+        const int64_t at = (int64_t)place(pv) * A.scale_stride + cur.h;
+        ks = A.k_scale[at], vs = A.v_scale[at];
+    }
+    make_pieces();
+    bl_v4f o[DT];
+#pragma unroll
+    for (int i = 0; i < DT; ++i) o[i] = (bl_v4f){0, 0, 0, 0};
+    float m = -INFINITY, l = 0.0f;
+    int begun = cur.t;                                       /* the item's first tile that is this wave's */
+    const at_request request_kept = request(cur.b);
+
+    for (int left = count; left > 0; --left) {
+        const at_request R = request(cur.b);
+        const int tok0 = (cur.tile0 + cur.t) * AT_TILE, tok = tok0 + grp * 16;    /* first of the tile's tokens, and of this lane's sixteen */
+        bl_v4i v[DT];
         {
-            uint32_t w[KS][8];
-            const uint16_t* src = A.q + (R.row0 + qi) * A.q_stride + (h * A.G + (col < rows ? col % A.G : 0)) * D;
-            float most = 0.0f;
-            bool nan = false;
+            const uint8_t* p = A.v + (((int64_t)cur.h << A.shift) * D) + at_far(place(pv), A.v_units) + ((int64_t)col << A.shift) + (tok & bs1);
+            /* A tile has half of every 128-byte line of a block of 128 tokens (WIDE): the other half is to stay until the next
+             * tile's turn.  Two requests of 131071 and 92681 tokens 134 -> 117 us; blocks of 64 without the hint 55 -> 60 us. */
 #pragma unroll
-            for (int s = 0; s < KS; ++s) {
-                const at_v4u u0 = *bl_gc<at_v4u>(src + s * 64 + grp * 16), u1 = *bl_gc<at_v4u>(src + s * 64 + grp * 16 + 8);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) w[s][j] = u0[j], w[s][4 + j] = u1[j];
-                most = at_largest(w[s], most, nan);
+            for (int i = 0; i < DT; ++i) {
+                const bl_v4i BL_G* at = bl_gc<bl_v4i>(p + ((int64_t)(16 * i) << A.shift));
+                v[i] = WIDE ? *at : __builtin_nontemporal_load(at);
             }
-            most = bl_max_pos(most, at_xor(most, 16));
-            most = bl_max_pos(most, at_xor(most, 32));
-            float inv, scale;
-            at_row_scale<KIND>(most, inv, scale);
-            const uint64_t nans = __ballot(nan);
-            if (nans && ((nans >> col) & 0x0001000100010001ull)) scale = __uint_as_float(0x7fc00000u);
-            a_row = scale * A.factor;
-#pragma unroll
-            for (int s = 0; s < KS; ++s) at_pieces<KIND>(w[s], inv, qh[s], ql[s]);
         }
-
-        bl_v4f o[DT];
+        bl_v4f sf[4];
+        if constexpr (KIND == BL_KV_INT8) {
+            bl_v4i sh[4], sl[4];
+            const bl_v4i z = {0, 0, 0, 0};
 #pragma unroll
-        for (int i = 0; i < DT; ++i) o[i] = (bl_v4f){0, 0, 0, 0};
-        float m = -INFINITY, l = 0.0f;
-
-        const int tend = tile0 + seg;
-        const int64_t head_k = ((int64_t)h << A.shift) * D, head_v = head_k;
-        /* Blocks of the lane's K row and of its sixteen V tokens; -1: nothing to see there. */
-        auto page_of = [&](int token) -> int {
-            int p = -1;
-            if (token < R.len) {
-                p = pages[token >> A.shift];
-                p = (unsigned)p < (unsigned)A.n_blocks ? p : -1;
+            for (int t = 0; t < 4; ++t) {
+                sh[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(k[t][0], qh[0], z, 0, 0, 0);
+                sl[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(k[t][0], ql[0], z, 0, 0, 0);
+                if constexpr (KS == 2) {
+                    sh[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(k[t][1], qh[1], sh[t], 0, 0, 0);
+                    sl[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(k[t][1], ql[1], sl[t], 0, 0, 0);
+                }
             }
-            return p;
-        };
-        const int kgrp = (col >> 2) * 16, krow = col & 3;
-        auto load_k = [&](int tile, int page, bl_v4i (&k)[4][KS]) {
-            const int tok = tile * AT_TILE + kgrp;
-            const uint8_t* p = A.k + at_far(page < 0 ? 0 : page, A.k_units) + head_k + (int64_t)((tok & bs1) + krow) * D + grp * 16;
+            bl_mfma_fence();
 #pragma unroll
             for (int t = 0; t < 4; ++t)
 #pragma unroll
-                for (int s = 0; s < KS; ++s) k[t][s] = __builtin_nontemporal_load(bl_gc<bl_v4i>(p + t * 4 * D + s * 64));
-        };
-        int tile = tile0 + wave;
-        if (tile < tend) {
-            bl_v4i k[4][KS];
-            int pk = page_of(tile * AT_TILE + kgrp), pv = page_of(tile * AT_TILE + grp * 16);
-            load_k(tile, pk, k);
-            float ks = A.k_scale[(int64_t)(pv < 0 ? 0 : pv) * A.scale_stride + h], vs = A.v_scale[(int64_t)(pv < 0 ? 0 : pv) * A.scale_stride + h];
-            int pk1 = page_of((tile + AT_WAVES) * AT_TILE + kgrp), pv1 = page_of((tile + AT_WAVES) * AT_TILE + grp * 16);
-            for (; tile < tend; tile += AT_WAVES) {
-                const int tok = tile * AT_TILE + grp * 16;            /* first of this lane's sixteen tokens */
-                bl_v4i v[DT];
-                {
-                    const uint8_t* p = A.v + at_far(pv < 0 ? 0 : pv, A.v_units) + head_v + ((int64_t)col << A.shift) + (tok & bs1);
+                for (int i = 0; i < 4; ++i) sf[t][i] = (float)((sh[t][i] << 8) + sl[t][i]);   /* |.| < 2^31: exact until here */
+        } else {
+            at_v8i q0, q1;
 #pragma unroll
-                    for (int i = 0; i < DT; ++i) v[i] = __builtin_nontemporal_load(bl_gc<bl_v4i>(p + ((int64_t)(16 * i) << A.shift)));
-                }
-                bl_v4f sf[4];
-                if constexpr (KIND == BL_KV_INT8) {
-                    bl_v4i sh[4], sl[4];
-                    const bl_v4i z = {0, 0, 0, 0};
+            for (int i = 0; i < 8; ++i) {
+                q0[i] = i < 4 ? qh[0][i] : KS == 2 ? qh[KS - 1][i - 4] : 0;
+                q1[i] = i < 4 ? ql[0][i] : KS == 2 ? ql[KS - 1][i - 4] : 0;
+            }
 #pragma unroll
-                    for (int t = 0; t < 4; ++t) {
-                        sh[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(k[t][0], qh[0], z, 0, 0, 0);
-                        sl[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(k[t][0], ql[0], z, 0, 0, 0);
-                        if constexpr (KS == 2) {
-                            sh[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(k[t][1], qh[1], sh[t], 0, 0, 0);
-                            sl[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(k[t][1], ql[1], sl[t], 0, 0, 0);
-                        }
-                    }
-                    bl_mfma_fence();
+            for (int t = 0; t < 4; ++t) {
+                at_v8i kk;
 #pragma unroll
-                    for (int t = 0; t < 4; ++t)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) sf[t][i] = (float)((sh[t][i] << 8) + sl[t][i]);   /* |.| < 2^31: exact until here */
-                } else {
-                    at_v8i q0, q1;
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        q0[i] = i < 4 ? qh[0][i] : KS == 2 ? qh[KS - 1][i - 4] : 0;
-                        q1[i] = i < 4 ? ql[0][i] : KS == 2 ? ql[KS - 1][i - 4] : 0;
-                    }
-#pragma unroll
-                    for (int t = 0; t < 4; ++t) {
-                        at_v8i kk;
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) kk[i] = i < 4 ? k[t][0][i] : KS == 2 ? k[t][KS - 1][i - 4] : 0;
-                        sf[t] = (bl_v4f){0, 0, 0, 0};
-                        sf[t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(kk, q0, sf[t], 0, 0, 0, 0, 0, 0);
-                        sf[t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(kk, q1, sf[t], 0, 0, 0, 0, 0, 0);
-                    }
-                    bl_mfma_fence();
-                }
-                /* the next tile's K while this one computes, and what comes behind it */
-                const int next = tile + AT_WAVES;
-                const int pv_next = pv1;
-                const float ks0 = ks, vs0 = vs;
-                if (next < tend) load_k(next, pk1, k);
-                ks = A.k_scale[(int64_t)(pv1 < 0 ? 0 : pv1) * A.scale_stride + h];
-                vs = A.v_scale[(int64_t)(pv1 < 0 ? 0 : pv1) * A.scale_stride + h];
-                pk1 = page_of((next + AT_WAVES) * AT_TILE + kgrp);
-                pv1 = page_of((next + AT_WAVES) * AT_TILE + grp * 16);
-
-                const float a = a_row * ks0;
-                const float vsc = fmaxf(vs0, 0x1p-100f), lv = __builtin_amdgcn_logf(vsc);
-                const bool whole = tile * AT_TILE >= all_from && tile * AT_TILE + AT_TILE <= all_to && __all(pv >= 0);
-                if (!whole) {
-                    /* masked scores are -inf, the others have their factor already (0 * -inf is none) */
-                    const int end = pv < 0 ? 0 : see1;
-#pragma unroll
-                    for (int t = 0; t < 4; ++t)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const int j = tok + 4 * t + i;
-                            sf[t][i] = j >= see0 && j < end ? sf[t][i] * a : -INFINITY;
-                        }
-                }
-                float best = sf[0][0];
-#pragma unroll
-                for (int t = 0; t < 4; ++t)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) best = fmaxf(best, sf[t][i]);
-                best = __builtin_fmaf(best, whole ? a : 1.0f, lv);
-                if (__any(best > m + AT_GROW)) {
-                    float top = fmaxf(m, best);
-                    top = fmaxf(top, at_xor(top, 16));
-                    top = fmaxf(top, at_xor(top, 32));
-                    const float f = top > m ? __builtin_amdgcn_exp2f(m - top) : 1.0f;
-                    l *= f;
-#pragma unroll
-                    for (int i = 0; i < DT; ++i) o[i] *= f;
-                    m = top;
-                }
-                const float shift = at_shift(lv, m);
-                float sum = 0.0f;
-#pragma unroll
-                for (int t = 0; t < 4; ++t)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        sf[t][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sf[t][i], whole ? a : 1.0f, shift));
-                        sum += sf[t][i];                     /* (fp32: fp16 would lose a block whose V scale is small beside others) */
-                    }
-                const at_v4u p0 = {at_pack_half(sf[0][0], sf[0][1]), at_pack_half(sf[0][2], sf[0][3]), at_pack_half(sf[1][0], sf[1][1]), at_pack_half(sf[1][2], sf[1][3])};
-                const at_v4u p1 = {at_pack_half(sf[2][0], sf[2][1]), at_pack_half(sf[2][2], sf[2][3]), at_pack_half(sf[3][0], sf[3][1]), at_pack_half(sf[3][2], sf[3][3])};
-                l = __builtin_fmaf(sum, __builtin_amdgcn_rcpf(vsc), l);
-                if (!whole) {
-                    /* what no token has written may be anything, a NaN times 0 too */
-                    const int there = pv < 0 ? 0 : R.len - tok;
-#pragma unroll
-                    for (int i = 0; i < DT; ++i) v[i] = at_first(v[i], there);
-                }
-#pragma unroll
-                for (int i = 0; i < DT; ++i) {
-                    at_v8h v0, v1;
-                    at_half16<KIND>(v[i], v0, v1);
-                    o[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, __builtin_bit_cast(at_v8h, p0), o[i], 0, 0, 0);
-                    o[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, __builtin_bit_cast(at_v8h, p1), o[i], 0, 0, 0);
-                }
-                pv = pv_next;
+                for (int i = 0; i < 8; ++i) kk[i] = i < 4 ? k[t][0][i] : KS == 2 ? k[t][KS - 1][i - 4] : 0;
+                sf[t] = (bl_v4f){0, 0, 0, 0};
+                sf[t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(kk, q0, sf[t], 0, 0, 0, 0, 0, 0);
+                sf[t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(kk, q1, sf[t], 0, 0, 0, 0, 0, 0);
             }
             bl_mfma_fence();
         }
-        /* the four waves' shares of the row sums and outputs meet */
-        l += at_xor(l, 16);
-        l += at_xor(l, 32);
-        if (grp == 0) s_m[wave][col] = m, s_l[wave][col] = l;
+        /* what the next tile needs, while this one computes */
+        const float ks0 = ks, vs0 = vs;
+        const int pv_next = next_blocks.v;
+        const bool turns = !together && cur.t + 1 == cur.c;  /* the item ends here, and this wave goes on with the next */
+        if (left > 1) {
+            load_k(next, next_blocks.k, k);
+            const int64_t at = (int64_t)place(pv_next) * A.scale_stride + next.h;
+            ks = A.k_scale[at], vs = A.v_scale[at];
+            if (turns) load_q(next);
+            next_blocks = read_blocks(after);
+        }
+        const int qi = col < R.n * A.G ? qi_of : 0;
+        const float a = a_row * ks0;
+        const float vsc = fmaxf(vs0, 0x1p-100f), lv = __builtin_amdgcn_logf(vsc);
+        const bool there = (unsigned)pv < (unsigned)A.n_blocks;
+        const bool whole = tok0 >= at_from(A, R, R.n - 1) && tok0 + AT_TILE <= at_to(R, 0) && __all(there);
+        if (!whole) {
+            /* masked scores are -inf, the others have their factor already (0 * -inf is none) */
+            const int see0 = at_from(A, R, qi), see1 = there && col < R.n * A.G ? at_to(R, qi) : 0;
 #pragma unroll
-        for (int i = 0; i < DT; ++i) *(bl_v4f*)&s_o[wave][col][16 * i + 4 * grp] = o[i];
-        __syncthreads();
-        const bool alone = seg == c;
-        {
-            constexpr int PER = D / 16;
-            const int r = tid >> 4, d0 = (tid & 15) * PER;
-            if (r < rows) {
-                float top = -INFINITY;
+            for (int t = 0; t < 4; ++t)
 #pragma unroll
-                for (int w = 0; w < AT_WAVES; ++w) top = fmaxf(top, s_m[w][r]);
-                float sum = 0.0f, y[PER];
-#pragma unroll
-                for (int j = 0; j < PER; ++j) y[j] = 0.0f;
-#pragma unroll
-                for (int w = 0; w < AT_WAVES; ++w) {
-                    const float f = s_m[w][r] == top ? 1.0f : __builtin_amdgcn_exp2f(s_m[w][r] - top);
-                    sum += s_l[w][r] * f;
-#pragma unroll
-                    for (int j = 0; j < PER; ++j) y[j] += s_o[w][r][d0 + j] * f;
+                for (int i = 0; i < 4; ++i) {
+                    const int j = tok + 4 * t + i;
+                    sf[t][i] = j >= see0 && j < see1 ? sf[t][i] * a : -INFINITY;
                 }
-                if (alone) {
-                    const float inv = sum == 0.0f ? 0.0f : bl_div_rn(1.0f, sum);
-                    uint32_t* to = (uint32_t*)(A.out + (R.row0 + r / A.G) * A.out_stride + (h * A.G + r % A.G) * D + d0);
+        }
+        float best = sf[0][0];
 #pragma unroll
-                    for (int j = 0; j < PER; j += 2) to[j / 2] = bl_pack2_bf16(y[j] * inv, y[j + 1] * inv);
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) best = fmaxf(best, sf[t][i]);
+        best = __builtin_fmaf(best, whole ? a : 1.0f, lv);
+        if (__any(best > m + AT_GROW)) {
+            float top = fmaxf(m, best);
+            top = fmaxf(top, at_xor(top, 16));
+            top = fmaxf(top, at_xor(top, 32));
+            const float f = top > m ? __builtin_amdgcn_exp2f(m - top) : 1.0f;
+            l *= f;
+#pragma unroll
+            for (int i = 0; i < DT; ++i) o[i] *= f;
+            m = top;
+        }
+        const float shift = at_shift(lv, m);
+        float sum = 0.0f;
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                sf[t][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sf[t][i], whole ? a : 1.0f, shift));
+                sum += sf[t][i];                             /* (fp32: fp16 would lose a block whose V scale is small beside others) */
+            }
+        l = __builtin_fmaf(sum, __builtin_amdgcn_rcpf(vsc), l);
+        const at_v4u p0 = {at_pack_half(sf[0][0], sf[0][1]), at_pack_half(sf[0][2], sf[0][3]), at_pack_half(sf[1][0], sf[1][1]), at_pack_half(sf[1][2], sf[1][3])};
+        const at_v4u p1 = {at_pack_half(sf[2][0], sf[2][1]), at_pack_half(sf[2][2], sf[2][3]), at_pack_half(sf[3][0], sf[3][1]), at_pack_half(sf[3][2], sf[3][3])};
+        if (!whole) {
+            /* what no token has written may be anything, a NaN times 0 too */
+            const int n = there ? R.len - tok : 0;
+#pragma unroll
+            for (int i = 0; i < DT; ++i) v[i] = at_first(v[i], n);
+        }
+#pragma unroll
+        for (int i = 0; i < DT; ++i) {
+            at_v8h v0, v1;
+            at_half16<KIND>(v[i], v0, v1);
+            o[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, __builtin_bit_cast(at_v8h, p0), o[i], 0, 0, 0);
+            o[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, __builtin_bit_cast(at_v8h, p1), o[i], 0, 0, 0);
+        }
+        if (turns || (left == 1 && !together)) {
+            bl_mfma_fence();
+            l += at_xor(l, 16);
+            l += at_xor(l, 32);
+            if (col < R.n * A.G) {
+                if (turns && begun == 0) {
+                    const float inv = l == 0.0f ? 0.0f : bl_div_rn(1.0f, l);
+                    uint16_t* to = A.out + (R.row0 + qi_of) * A.out_stride + (cur.h * A.G + qh_of) * D + 4 * grp;
+#pragma unroll
+                    for (int i = 0; i < DT; ++i) {
+                        const bl_v2u u = {bl_pack2_bf16(o[i][0] * inv, o[i][1] * inv), bl_pack2_bf16(o[i][2] * inv, o[i][3] * inv)};
+                        *bl_g((bl_v2u*)(to + 16 * i)) = u;
+                    }
                 } else {
-                    float* to = part + (int64_t)(2 * group + (t0 == 0)) * at_slot<D>::floats;
+                    float* to = A.part + A.part_skip + (int64_t)(2 * stream + (begun == 0)) * at_slot<D>::floats;
 #pragma unroll
-                    for (int j = 0; j < PER; ++j) to[r * D + d0 + j] = y[j];
-                    if (d0 == 0) to[AT_FEW * D + 2 * r] = top, to[AT_FEW * D + 2 * r + 1] = sum;
+                    for (int i = 0; i < DT; ++i) *bl_g((bl_v4f*)(to + col * D + 16 * i + 4 * grp)) = o[i];
+                    if (grp == 0) to[AT_FEW * D + 2 * col] = m, to[AT_FEW * D + 2 * col + 1] = l;
                 }
             }
+            if (left > 1) {
+                make_pieces();
+                begun = 0, m = -INFINITY, l = 0.0f;
+#pragma unroll
+                for (int i = 0; i < DT; ++i) o[i] = (bl_v4f){0, 0, 0, 0};
+            }
         }
-        __syncthreads();
-        x0 += seg;
+        if (left > 1) cur = next;
+        next = after, pv = pv_next;
+        if (left > 3) after = advance(after);
+    }
+    if (!together) return;
+    at_meet_lds<D>& meet = *(at_meet_lds<D>*)&lds;
+    bl_mfma_fence();
+    l += at_xor(l, 16);
+    l += at_xor(l, 32);
+    __syncthreads();                                         /* (nobody reads the requests there any more) */
+    if (grp == 0) meet.m[wave][col] = m, meet.l[wave][col] = l;
+#pragma unroll
+    for (int i = 0; i < DT; ++i) *(bl_v4f*)&meet.o[wave][col][16 * i + 4 * grp] = o[i];
+    __syncthreads();
+    const at_request R = request_kept;
+    constexpr int PER = D / 16;
+    const int r = tid >> 4, d0 = (tid & 15) * PER;
+    if (r >= R.n * A.G) return;
+    float top = -INFINITY, sum = 0.0f, y[PER];
+#pragma unroll
+    for (int w = 0; w < AT_WAVES; ++w) top = fmaxf(top, meet.m[w][r]);
+#pragma unroll
+    for (int j = 0; j < PER; ++j) y[j] = 0.0f;
+#pragma unroll
+    for (int w = 0; w < AT_WAVES; ++w) {
+        const float f = meet.m[w][r] == top ? 1.0f : __builtin_amdgcn_exp2f(meet.m[w][r] - top);
+        sum += meet.l[w][r] * f;
+#pragma unroll
+        for (int j = 0; j < PER; ++j) y[j] += meet.o[w][r][d0 + j] * f;
+    }
+    if (cur.c == share * AT_WAVES) {                         /* all of the item */
+        const float inv = sum == 0.0f ? 0.0f : bl_div_rn(1.0f, sum);
+        uint32_t* to = (uint32_t*)(A.out + (R.row0 + r / A.G) * A.out_stride + (cur.h * A.G + r % A.G) * D + d0);
+#pragma unroll
+        for (int j = 0; j < PER; j += 2) to[j / 2] = bl_pack2_bf16(y[j] * inv, y[j + 1] * inv);
+    } else {
+        float* to = A.part + A.part_skip + (int64_t)(2 * stream + (begun0 == 0)) * at_slot<D>::floats;
+#pragma unroll
+        for (int j = 0; j < PER; ++j) to[r * D + d0 + j] = y[j];
+        if (d0 == 0) to[AT_FEW * D + 2 * r] = top, to[AT_FEW * D + 2 * r + 1] = sum;
     }
 }
 
-/* Adds up what several workgroups of at_few have of one item: of the item that the boundary between workgroups edge - 1 and
- * edge cuts, where no earlier boundary does.  D / 4 threads (a group) a partial result of a row, four in flight.  Few partial
- * results: a group takes a row, all in the workgroup turn = 0.  Many: the groups share those of a row and meet in LDS, and
- * the rows are shared by `turns` workgroups. */
+/* Adds up what several waves of at_few have of one item: of the item that the boundary between waves edge - 1 and edge cuts,
+ * where no earlier boundary does.  A workgroup has AT_WAVES boundaries and the rows turn, turn + turns, ...  D / 4 threads
+ * (a group) a partial result of a row, sixteen in flight.  The wave of the boundary does it, a row a group; where there are
+ * more than AT_JOIN_ALONE the groups of all waves share those of a row and meet in LDS. */
+#define AT_JOIN_ALONE 32
+struct at_cut {
+    int row0, rows, h, first, w0, head, ga, inner, g1, parts;   /* pieces w0 .. of `head` waves, of `inner` workgroups from ga, of waves from 4 g1 */
+};
+struct at_sum {
+    float m, l;
+    bl_v4f y;
+};
 template <int D>
 struct at_join_lds {
     float m[AT_THREADS / (D / 4)], l[AT_THREADS / (D / 4)], y[AT_THREADS / (D / 4)][D];
+    at_cut cut[AT_WAVES];
 };
+__device__ __forceinline__ at_sum at_add(const at_sum& a, const at_sum& b) {
+    at_sum r;
+    r.m = fmaxf(a.m, b.m);
+    const float e = a.m == r.m ? 1.0f : __builtin_amdgcn_exp2f(a.m - r.m), f = b.m == r.m ? 1.0f : __builtin_amdgcn_exp2f(b.m - r.m);
+    r.l = a.l * e + b.l * f;
+    r.y = a.y * e + b.y * f;
+    return r;
+}
+/* Partial results begin, begin + step, ... of row r, features d .. d + 3. */
 template <int D>
-__device__ __forceinline__ void at_few_join(const at_args& A, int edge, int turn, int turns, at_join_lds<D>& lds) {
-    constexpr int TPP = D / 4, GROUPS = AT_THREADS / TPP;
-    const int tid = threadIdx.x, lane = tid & 63;
-    const int* upto = (const int*)A.part;
-    const int all = upto[A.B - 1] * A.n_kv, share = at_share(all);
-    const int64_t pos = (int64_t)edge * share;
-    if (pos >= all) return;
-    /* the request whose tiles the boundary lies among: the first whose tiles end behind it, 64 at a look */
-    const int at = (int)pos / A.n_kv;
-    int b = 0;
-    if (A.B > 64) {
-        const int i = lane * 64 + 63;
-        b = __builtin_ctzll(__ballot(upto[i < A.B ? i : A.B - 1] > at)) * 64;
-    }
-    b += __builtin_ctzll(__ballot(upto[b + lane < A.B ? b + lane : A.B - 1] > at));
-    const int before = b ? upto[b - 1] : 0, c = upto[b] - before;
-    const int first = before * A.n_kv + ((int)pos - before * A.n_kv) / c * c, h = (first - before * A.n_kv) / c;
-    const int w0 = first / share, w1 = (first + c - 1) / share;
-    if (w0 != edge - 1 || w1 < edge) return;
-    const at_request R = at_read(A, b);
+__device__ __forceinline__ at_sum at_gather(const at_args& A, const at_cut& c, int share, int r, int d, int begin, int step) {
+    constexpr int IN = 16;
     const float* part = A.part + A.part_skip;
-    const int g = tid / TPP, d = tid % TPP * 4, rows = R.n * A.G;
-    const bool shared_row = w1 - w0 >= 8;
-    if (!shared_row && turn) return;
-    for (int r = shared_row ? turn : g; r < rows; r += shared_row ? turns : GROUPS) {
-        const int step = shared_row ? GROUPS : 1;
-        float top = -INFINITY, sum = 0.0f;
-        bl_v4f y = {0, 0, 0, 0};
-        for (int w = w0 + (shared_row ? g : 0); w <= w1; w += 4 * step) {
-            float m[4], l[4], best = top;
-            bl_v4f v[4];
+    at_sum s = {-INFINITY, 0.0f, {0, 0, 0, 0}};
+    for (int i = begin; i < c.parts; i += IN * step) {
+        float m[IN], l[IN], best = s.m;
+        bl_v4f v[IN];
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                const int ww = w + u * step;
-                const float* from = part + (int64_t)(2 * ww + (ww * share <= first)) * at_slot<D>::floats;
-                m[u] = -INFINITY, l[u] = 0.0f, v[u] = (bl_v4f){0, 0, 0, 0};
-                if (ww <= w1) {
-                    m[u] = from[AT_FEW * D + 2 * r], l[u] = from[AT_FEW * D + 2 * r + 1];
-                    v[u] = *bl_gc<bl_v4f>(from + r * D + d);
-                }
-            }
-#pragma unroll
-            for (int u = 0; u < 4; ++u) best = fmaxf(best, m[u]);
-            const float f = top == best ? 1.0f : __builtin_amdgcn_exp2f(top - best);
-            sum *= f, y *= f, top = best;
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                const float e = m[u] == top ? 1.0f : __builtin_amdgcn_exp2f(m[u] - top);
-                sum += l[u] * e, y += v[u] * e;
+        for (int u = 0; u < IN; ++u) {
+            const int p = i + u * step;
+            const int w = p < c.head ? c.w0 + p : p < c.head + c.inner ? (c.ga + p - c.head) * AT_WAVES : c.g1 * AT_WAVES + p - c.head - c.inner;
+            const float* from = part + (int64_t)(2 * w + (w * share <= c.first)) * at_slot<D>::floats;
+            m[u] = -INFINITY, l[u] = 0.0f, v[u] = (bl_v4f){0, 0, 0, 0};
+            if (p < c.parts) {
+                const bl_v2f ml = *bl_gc<bl_v2f>(from + AT_FEW * D + 2 * r);
+                m[u] = ml[0], l[u] = ml[1];
+                v[u] = *bl_gc<bl_v4f>(from + r * D + d);
             }
         }
-        if (shared_row) {
-            if (d == 0) lds.m[g] = top, lds.l[g] = sum;
-            *(bl_v4f*)&lds.y[g][d] = y;
+#pragma unroll
+        for (int u = 0; u < IN; ++u) best = fmaxf(best, m[u]);
+        const float f = s.m == best ? 1.0f : __builtin_amdgcn_exp2f(s.m - best);
+        s.l *= f, s.y *= f, s.m = best;
+#pragma unroll
+        for (int u = 0; u < IN; ++u) {
+            const float e = m[u] == best ? 1.0f : __builtin_amdgcn_exp2f(m[u] - best);
+            s.l += l[u] * e, s.y += v[u] * e;
+        }
+    }
+    return s;
+}
+template <int D>
+__device__ __forceinline__ void at_joined(const at_args& A, const at_cut& c, int r, int d, const at_sum& s) {
+    const float inv = s.l == 0.0f ? 0.0f : bl_div_rn(1.0f, s.l);
+    const bl_v2u u = {bl_pack2_bf16(s.y[0] * inv, s.y[1] * inv), bl_pack2_bf16(s.y[2] * inv, s.y[3] * inv)};
+    *bl_g((bl_v2u*)(A.out + (c.row0 + r / A.G) * A.out_stride + (c.h * A.G + r % A.G) * D + d)) = u;
+}
+template <int D>
+__device__ __forceinline__ void at_few_join(const at_args& A, int group, int turn, int turns, at_join_lds<D>& lds) {
+    constexpr int TPP = D / 4, GROUPS = AT_THREADS / TPP, PER_WAVE = GROUPS / AT_WAVES;
+    const int tid = threadIdx.x, lane = tid & 63, wave = at_uniform(tid >> 6), d = tid % TPP * 4;
+    const int4* heads = (const int4*)A.part;
+    /* 64 requests at a look: the first whose tiles end behind tile `at` of a head's line is this boundary's */
+    int4 here = {0, 0, 0, 0};
+    int total, b0 = 0;
+    const bool small = A.B <= 64;
+    if (small) {
+        here = heads[lane < A.B ? lane : A.B - 1];
+        total = __builtin_amdgcn_readlane(here.x, 63);
+    } else {
+        total = heads[A.B - 1].x;
+    }
+    const int all = total * A.n_kv, share = at_share(all), edge = group * AT_WAVES + wave + 1;
+    if ((int64_t)(group * AT_WAVES + 1) * share >= all) return;
+    at_cut c = {};
+    if ((int64_t)edge * share < all) {
+        const int pos = edge * share, at = pos / A.n_kv;
+        if (!small) {
+            const int i = lane * 64 + 63;
+            b0 = __builtin_ctzll(__ballot(heads[i < A.B ? i : A.B - 1].x > at)) * 64;
+            here = heads[b0 + lane < A.B ? b0 + lane : A.B - 1];
+        }
+        const int i = __builtin_ctzll(__ballot(here.x > at));
+        const int before = i ? __builtin_amdgcn_readlane(here.x, i - 1) : b0 ? at_uniform(heads[b0 - 1].x) : 0;
+        const int n = __builtin_amdgcn_readlane(here.x, i) - before;
+        c.h = (pos - before * A.n_kv) / n, c.first = before * A.n_kv + c.h * n;
+        const int last = c.first + n - 1, w1 = last / share;
+        c.w0 = c.first / share;
+        const int g0 = c.w0 / AT_WAVES;
+        c.g1 = w1 / AT_WAVES;
+        const bool in0 = at_together(g0, share, c.first, last), in1 = at_together(c.g1, share, c.first, last);
+        c.head = in0 ? 0 : (w1 < g0 * AT_WAVES + AT_WAVES - 1 ? w1 : g0 * AT_WAVES + AT_WAVES - 1) - c.w0 + 1;
+        c.ga = in0 ? g0 : g0 + 1;
+        c.inner = (in1 ? c.g1 + 1 : c.g1) - c.ga;
+        c.inner = c.inner < 0 ? 0 : c.inner;
+        c.parts = c.head + c.inner + (in1 || c.g1 == g0 ? 0 : w1 - c.g1 * AT_WAVES + 1);
+        if (c.w0 != edge - 1) c.parts = 0;                               /* not this boundary's */
+        c.row0 = __builtin_amdgcn_readlane(here.y, i), c.rows = __builtin_amdgcn_readlane(here.z, i) * A.G;
+    }
+    const bool together = c.parts > AT_JOIN_ALONE;
+    if (!together && c.parts > 1)
+        for (int r = turn * PER_WAVE + lane / TPP; r < c.rows; r += turns * PER_WAVE) at_joined<D>(A, c, r, d, at_gather<D>(A, c, share, r, d, 0, 1));
+    if (lane == 0) {
+        if (!together) c.rows = 0;
+        lds.cut[wave] = c;
+    }
+    __syncthreads();
+    for (int i = 0; i < AT_WAVES; ++i) {
+        const at_cut x = lds.cut[i];
+        for (int r = turn; r < x.rows; r += turns) {
+            const int g = tid / TPP;
+            at_sum s = at_gather<D>(A, x, share, r, d, g, GROUPS);
+            if (d == 0) lds.m[g] = s.m, lds.l[g] = s.l;
+            *(bl_v4f*)&lds.y[g][d] = s.y;
             __syncthreads();
             if (g == 0) {
-                for (int i = 1; i < GROUPS; ++i) top = fmaxf(top, lds.m[i]);
-                sum = 0.0f, y = (bl_v4f){0, 0, 0, 0};
-                for (int i = 0; i < GROUPS; ++i) {
-                    const float e = lds.m[i] == top ? 1.0f : __builtin_amdgcn_exp2f(lds.m[i] - top);
-                    sum += lds.l[i] * e, y += *(const bl_v4f*)&lds.y[i][d] * e;
-                }
+                for (int j = 1; j < GROUPS; ++j) s = at_add(s, {lds.m[j], lds.l[j], *(const bl_v4f*)&lds.y[j][d]});
+                at_joined<D>(A, x, r, d, s);
             }
             __syncthreads();
-        }
-        if (!shared_row || g == 0) {
-            const float inv = sum == 0.0f ? 0.0f : bl_div_rn(1.0f, sum);
-            const bl_v2u u = {bl_pack2_bf16(y[0] * inv, y[1] * inv), bl_pack2_bf16(y[2] * inv, y[3] * inv)};
-            *bl_g((bl_v2u*)(A.out + (R.row0 + r / A.G) * A.out_stride + (h * A.G + r % A.G) * D + d)) = u;
         }
     }
 }
@@ -982,13 +1117,13 @@ __device__ __forceinline__ void at_many_join(const at_args& A, int group) {
 /* ---- launches ---------------------------------------------------------------------------------------------------------- */
 
 /* A batch without long runs of rows: at_few alone. */
-template <int KIND, int D>
+template <int KIND, int D, bool WIDE>
 __global__ __launch_bounds__(AT_THREADS, 2) void bl_attn_few(at_args A) {
     __shared__ __attribute__((aligned(16))) at_few_lds<D> lds;
-    at_few<KIND, D>(A, (int)blockIdx.x, lds);
+    at_few<KIND, D, WIDE>(A, (int)blockIdx.x, lds);
 }
 /* Any batch, in one launch: the matrix cores' work first; what streams the cache fills the units as that ends. */
-template <int KIND, int D>
+template <int KIND, int D, bool WIDE>
 __global__ __launch_bounds__(AT_THREADS, 2) void bl_attn_any(at_args A, int many) {
     union lds_t {
         at_few_lds<D> few;
@@ -996,14 +1131,14 @@ __global__ __launch_bounds__(AT_THREADS, 2) void bl_attn_any(at_args A, int many
     };
     __shared__ __attribute__((aligned(16))) uint8_t lds[sizeof(lds_t)];
     if ((int)blockIdx.x < many) at_many<KIND, D>(A, (int)blockIdx.x, ((lds_t*)lds)->many);
-    else at_few<KIND, D>(A, (int)blockIdx.x - many, ((lds_t*)lds)->few);
+    else at_few<KIND, D, WIDE>(A, (int)blockIdx.x - many, ((lds_t*)lds)->few);
 }
-/* Partial results of both: `few` workgroups for those of at_few, turns x (AT_ROWS_GRID - 1), the others for a split. */
+/* Partial results of both: `few` workgroups for those of at_few, turns x AT_ROWS_GRID, the others for a split. */
 template <int D>
 __global__ __launch_bounds__(AT_THREADS) void bl_attn_join(at_args A, int few) {
     __shared__ __attribute__((aligned(16))) at_join_lds<D> lds;
     const int x = (int)blockIdx.x;
-    if (x < few) at_few_join<D>(A, x % (AT_ROWS_GRID - 1) + 1, x / (AT_ROWS_GRID - 1), few / (AT_ROWS_GRID - 1), lds);
+    if (x < few) at_few_join<D>(A, x % AT_ROWS_GRID, x / AT_ROWS_GRID, few / AT_ROWS_GRID, lds);
     else at_many_join<D>(A, x - few);
 }
 
@@ -1050,8 +1185,8 @@ static at_plan at_make_plan(const bl_attn_desc* a) {
         s = s > by_len ? by_len : s;
         p.splits = s < 1 ? 1 : s > 64 ? 64 : (int)s;
     }
-    p.skip = p.few ? (int)((a->B + 63) / 64 * 64) : 0;
-    p.few_bytes = p.few ? ((size_t)AT_ROWS_GRID * 2 * AT_FEW * (D + 2) + p.skip) * sizeof(float) : 0;
+    p.skip = p.few ? (int)((a->B + 15) / 16 * 64) : 0;
+    p.few_bytes = p.few ? ((size_t)AT_STREAMS * 2 * AT_FEW * (D + 2) + p.skip) * sizeof(float) : 0;
     p.rows = (int)(rows < AT_FEW ? rows : AT_FEW);
     p.bytes = p.few_bytes + (p.splits > 1 ? (size_t)p.splits * a->T * a->n_q * (D + 2) * sizeof(float) : 0);
     return p;
@@ -1061,19 +1196,19 @@ extern "C" size_t bl_attn_workspace_bytes(const bl_attn_desc* a) {
     return at_check(a) == BL_OK ? at_make_plan(a).bytes : 0;
 }
 
-template <int KIND, int D>
+template <int KIND, int D, bool WIDE>
 static void at_launch(at_args A, const at_plan& p, const bl_attn_desc* a, hipStream_t st) {
     A.part = (float*)a->workspace;
     A.many_part = A.part + p.few_bytes / sizeof(float);
     const int few = p.few ? AT_ROWS_GRID : 0;
     if (p.many) {
         const int many = p.row_tiles * A.n_kv * p.splits;
-        bl_attn_any<KIND, D><<<(unsigned)(many + few), AT_THREADS, 0, st>>>(A, many);
+        bl_attn_any<KIND, D, WIDE><<<(unsigned)(many + few), AT_THREADS, 0, st>>>(A, many);
     } else {
-        bl_attn_few<KIND, D><<<(unsigned)few, AT_THREADS, 0, st>>>(A);
+        bl_attn_few<KIND, D, WIDE><<<(unsigned)few, AT_THREADS, 0, st>>>(A);
     }
     const int64_t rows = (int64_t)A.T * A.n_q, per = AT_THREADS / (D / 8);
-    const int few_join = p.few ? (AT_ROWS_GRID - 1) * (p.rows < 4 ? p.rows : 4) : 0;
+    const int few_join = p.few ? AT_ROWS_GRID * ((p.rows + 256 / D - 1) / (256 / D)) : 0;      /* (D / 4 lanes a row of a wave) */
     const int64_t join = few_join + (p.splits > 1 ? (rows + per - 1) / per : 0);
     if (join) bl_attn_join<D><<<(unsigned)join, AT_THREADS, 0, st>>>(A, few_join);
 }
@@ -1095,7 +1230,9 @@ extern "C" bl_status bl_attn_kv8(const bl_attn_desc* a, bl_stream s) {
     A.factor = a->softmax_scale * 1.44269504f;
     A.few_rows = p.few ? AT_FEW : 0, A.splits = p.splits, A.part_skip = p.skip;
     const hipStream_t st = (hipStream_t)s;
-    if (c.kind == BL_KV_INT8) c.head_dim == 128 ? at_launch<BL_KV_INT8, 128>(A, p, a, st) : at_launch<BL_KV_INT8, 64>(A, p, a, st);
-    else c.head_dim == 128 ? at_launch<BL_KV_E4M3, 128>(A, p, a, st) : at_launch<BL_KV_E4M3, 64>(A, p, a, st);
+#define AT(K, D) (c.block == 128 ? at_launch<K, D, true>(A, p, a, st) : at_launch<K, D, false>(A, p, a, st))
+    if (c.kind == BL_KV_INT8) c.head_dim == 128 ? AT(BL_KV_INT8, 128) : AT(BL_KV_INT8, 64);
+    else c.head_dim == 128 ? AT(BL_KV_E4M3, 128) : AT(BL_KV_E4M3, 64);
+#undef AT
     return hipGetLastError() == hipSuccess ? BL_OK : BL_ERR_HIP;
 }
