@@ -594,7 +594,7 @@ __device__ __forceinline__ void at_few(const at_args& A, int group, at_few_lds<D
 
 /* Adds up what several waves of at_few have of one item: of the item that the boundary between waves edge - 1 and edge cuts,
  * where no earlier boundary does.  A workgroup has AT_WAVES boundaries and the rows turn, turn + turns, ...  D / 4 threads
- * (a group) a partial result of a row, sixteen in flight.  The wave of the boundary does it, a row a group; where there are
+ * (a group) a partial result of a row.  The wave of the boundary does it, a row a group; where there are
  * more than AT_JOIN_ALONE the groups of all waves share those of a row and meet in LDS. */
 #define AT_JOIN_ALONE 32
 struct at_cut {
@@ -617,10 +617,9 @@ __device__ __forceinline__ at_sum at_add(const at_sum& a, const at_sum& b) {
     r.y = a.y * e + b.y * f;
     return r;
 }
-/* Partial results begin, begin + step, ... of row r, features d .. d + 3. */
-template <int D>
+/* Partial results begin, begin + step, ... of row r, features d .. d + 3, IN of them in flight. */
+template <int D, int IN>
 __device__ __forceinline__ at_sum at_gather(const at_args& A, const at_cut& c, int share, int r, int d, int begin, int step) {
-    constexpr int IN = 16;
     const float* part = A.part + A.part_skip;
     at_sum s = {-INFINITY, 0.0f, {0, 0, 0, 0}};
     for (int i = begin; i < c.parts; i += IN * step) {
@@ -656,7 +655,7 @@ __device__ __forceinline__ void at_joined(const at_args& A, const at_cut& c, int
     const bl_v2u u = {bl_pack2_bf16(s.y[0] * inv, s.y[1] * inv), bl_pack2_bf16(s.y[2] * inv, s.y[3] * inv)};
     *bl_g((bl_v2u*)(A.out + (c.row0 + r / A.G) * A.out_stride + (c.h * A.G + r % A.G) * D + d)) = u;
 }
-template <int D>
+template <int D, int IN>
 __device__ __forceinline__ void at_few_join(const at_args& A, int group, int turn, int turns, at_join_lds<D>& lds) {
     constexpr int TPP = D / 4, GROUPS = AT_THREADS / TPP, PER_WAVE = GROUPS / AT_WAVES;
     const int tid = threadIdx.x, lane = tid & 63, wave = at_uniform(tid >> 6), d = tid % TPP * 4;
@@ -700,7 +699,7 @@ __device__ __forceinline__ void at_few_join(const at_args& A, int group, int tur
     }
     const bool together = c.parts > AT_JOIN_ALONE;
     if (!together && c.parts > 1)
-        for (int r = turn * PER_WAVE + lane / TPP; r < c.rows; r += turns * PER_WAVE) at_joined<D>(A, c, r, d, at_gather<D>(A, c, share, r, d, 0, 1));
+        for (int r = turn * PER_WAVE + lane / TPP; r < c.rows; r += turns * PER_WAVE) at_joined<D>(A, c, r, d, at_gather<D, IN>(A, c, share, r, d, 0, 1));
     if (lane == 0) {
         if (!together) c.rows = 0;
         lds.cut[wave] = c;
@@ -710,7 +709,7 @@ __device__ __forceinline__ void at_few_join(const at_args& A, int group, int tur
         const at_cut x = lds.cut[i];
         for (int r = turn; r < x.rows; r += turns) {
             const int g = tid / TPP;
-            at_sum s = at_gather<D>(A, x, share, r, d, g, GROUPS);
+            at_sum s = at_gather<D, IN>(A, x, share, r, d, g, GROUPS);
             if (d == 0) lds.m[g] = s.m, lds.l[g] = s.l;
             *(bl_v4f*)&lds.y[g][d] = s.y;
             __syncthreads();
@@ -1081,14 +1080,27 @@ __device__ __forceinline__ void at_many(const at_args& A, int place, at_many_lds
     }
 }
 
-/* Adds up the pieces of a split: D / 8 threads a (row of the batch, head). */
+/* Adds up the pieces of a split: D / 4 threads a (row of the batch, head), four pieces in flight. */
 template <int D>
 __device__ __forceinline__ void at_many_join(const at_args& A, int group) {
-    constexpr int TPR = D / 8;
+    constexpr int TPR = D / 4, IN = 4;
     const int64_t at = (int64_t)group * (AT_THREADS / TPR) + threadIdx.x / TPR, all = (int64_t)A.T * A.n_q;
     if (at >= all) return;
-    const int row = (int)(at / A.n_q), d0 = (threadIdx.x % TPR) * 8;
-    int lo = 0, hi = A.B;                                     /* whose row it is: q_start[lo] <= row < q_start[hi] */
+    const int row = (int)(at / A.n_q), d0 = (threadIdx.x % TPR) * 4;
+    const float* ml = A.many_part + A.splits * all * D;
+    auto piece = [&](int i) -> at_sum {
+        at_sum x = {-INFINITY, 0.0f, {0, 0, 0, 0}};
+        if (i < A.splits) {
+            const int64_t from = i * all + at;
+            const bl_v2f t = *bl_gc<bl_v2f>(ml + 2 * from);
+            x.m = t[0], x.l = t[1], x.y = *bl_gc<bl_v4f>(A.many_part + from * D + d0);
+        }
+        return x;
+    };
+    at_sum x[IN];
+#pragma unroll
+    for (int u = 0; u < IN; ++u) x[u] = piece(u);
+    int lo = 0, hi = A.B;                                     /* whose row it is, while those come: q_start[lo] <= row < q_start[hi] */
     if (row < A.q_start[0] || row >= A.q_start[A.B]) return;
     while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
@@ -1097,21 +1109,18 @@ __device__ __forceinline__ void at_many_join(const at_args& A, int group) {
     }
     const at_request R = at_read(A, lo);
     if ((int64_t)R.n * A.G <= A.few_rows) return;
-    const float* ml = A.many_part + A.splits * all * D;
-    float top = -INFINITY;
-    for (int s = 0; s < A.splits; ++s) top = fmaxf(top, ml[2 * (s * all + at)]);
-    float sum = 0.0f, y[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    for (int s = 0; s < A.splits; ++s) {
-        const float mm = ml[2 * (s * all + at)];
-        const float f = mm == top ? 1.0f : __builtin_amdgcn_exp2f(mm - top);
-        sum += ml[2 * (s * all + at) + 1] * f;
-        const float* from = A.many_part + (s * all + at) * D + d0;
+    at_sum s = x[0];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) y[j] += from[j] * f;
+    for (int u = 1; u < IN; ++u) s = at_add(s, x[u]);
+    for (int i = IN; i < A.splits; i += IN) {
+#pragma unroll
+        for (int u = 0; u < IN; ++u) x[u] = piece(i + u);
+#pragma unroll
+        for (int u = 0; u < IN; ++u) s = at_add(s, x[u]);
     }
-    const float inv = sum == 0.0f ? 0.0f : bl_div_rn(1.0f, sum);
-    const at_v4u u = {bl_pack2_bf16(y[0] * inv, y[1] * inv), bl_pack2_bf16(y[2] * inv, y[3] * inv), bl_pack2_bf16(y[4] * inv, y[5] * inv), bl_pack2_bf16(y[6] * inv, y[7] * inv)};
-    *(at_v4u*)(A.out + row * A.out_stride + (at % A.n_q) * D + d0) = u;
+    const float inv = s.l == 0.0f ? 0.0f : bl_div_rn(1.0f, s.l);
+    const bl_v2u u = {bl_pack2_bf16(s.y[0] * inv, s.y[1] * inv), bl_pack2_bf16(s.y[2] * inv, s.y[3] * inv)};
+    *bl_g((bl_v2u*)(A.out + row * A.out_stride + (at % A.n_q) * D + d0)) = u;
 }
 
 /* ---- launches ---------------------------------------------------------------------------------------------------------- */
@@ -1121,6 +1130,12 @@ template <int KIND, int D, bool WIDE>
 __global__ __launch_bounds__(AT_THREADS, 2) void bl_attn_few(at_args A) {
     __shared__ __attribute__((aligned(16))) at_few_lds<D> lds;
     at_few<KIND, D, WIDE>(A, (int)blockIdx.x, lds);
+}
+/* One request, or groups of more heads than at_few has rows: at_many alone. */
+template <int KIND, int D>
+__global__ __launch_bounds__(AT_THREADS, 2) void bl_attn_many(at_args A) {
+    __shared__ __attribute__((aligned(16))) at_many_lds<D> lds;
+    at_many<KIND, D>(A, (int)blockIdx.x, lds);
 }
 /* Any batch, in one launch: the matrix cores' work first; what streams the cache fills the units as that ends. */
 template <int KIND, int D, bool WIDE>
@@ -1134,11 +1149,12 @@ __global__ __launch_bounds__(AT_THREADS, 2) void bl_attn_any(at_args A, int many
     else at_few<KIND, D, WIDE>(A, (int)blockIdx.x - many, ((lds_t*)lds)->few);
 }
 /* Partial results of both: `few` workgroups for those of at_few, turns x AT_ROWS_GRID, the others for a split. */
-template <int D>
+template <int D, bool MANY>
 __global__ __launch_bounds__(AT_THREADS) void bl_attn_join(at_args A, int few) {
     __shared__ __attribute__((aligned(16))) at_join_lds<D> lds;
     const int x = (int)blockIdx.x;
-    if (x < few) at_few_join<D>(A, x % AT_ROWS_GRID, x / AT_ROWS_GRID, few / AT_ROWS_GRID, lds);
+    /* (sixteen partial results in flight are 122 registers: where a split's rows stand beside them, their loads need the waves more) */
+    if (!MANY || x < few) at_few_join<D, MANY ? 4 : 16>(A, x % AT_ROWS_GRID, x / AT_ROWS_GRID, few / AT_ROWS_GRID, lds);
     else at_many_join<D>(A, x - few);
 }
 
@@ -1203,14 +1219,16 @@ static void at_launch(at_args A, const at_plan& p, const bl_attn_desc* a, hipStr
     const int few = p.few ? AT_ROWS_GRID : 0;
     if (p.many) {
         const int many = p.row_tiles * A.n_kv * p.splits;
-        bl_attn_any<KIND, D, WIDE><<<(unsigned)(many + few), AT_THREADS, 0, st>>>(A, many);
+        if (few) bl_attn_any<KIND, D, WIDE><<<(unsigned)(many + few), AT_THREADS, 0, st>>>(A, many);
+        else bl_attn_many<KIND, D><<<(unsigned)many, AT_THREADS, 0, st>>>(A);
     } else {
         bl_attn_few<KIND, D, WIDE><<<(unsigned)few, AT_THREADS, 0, st>>>(A);
     }
-    const int64_t rows = (int64_t)A.T * A.n_q, per = AT_THREADS / (D / 8);
+    const int64_t rows = (int64_t)A.T * A.n_q, per = AT_THREADS / (D / 4);
     const int few_join = p.few ? AT_ROWS_GRID * ((p.rows + 256 / D - 1) / (256 / D)) : 0;      /* (D / 4 lanes a row of a wave) */
     const int64_t join = few_join + (p.splits > 1 ? (rows + per - 1) / per : 0);
-    if (join) bl_attn_join<D><<<(unsigned)join, AT_THREADS, 0, st>>>(A, few_join);
+    if (p.splits > 1) bl_attn_join<D, true><<<(unsigned)join, AT_THREADS, 0, st>>>(A, few_join);
+    else if (join) bl_attn_join<D, false><<<(unsigned)join, AT_THREADS, 0, st>>>(A, few_join);
 }
 
 extern "C" bl_status bl_attn_kv8(const bl_attn_desc* a, bl_stream s) {
