@@ -4,32 +4,47 @@
 
 /* ---- block tables and slot maps ---------------------------------------------------------------------------------- */
 
-#define TAB_THREADS 1024
-#define TAB_WAVES (TAB_THREADS / BL_WAVE)
-#define TAB_PER (BL_KV_MAX_REQUESTS / TAB_THREADS)
 #define TAB_ROWS_INSIDE 4096       /* rows whose slots the table kernel writes itself */
 
-/* Sum of v over the threads in front of this one, and over all (in *total).  s: TAB_WAVES values, reused after a barrier. */
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int64_t tab_moved(int64_t v) {
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)v, CTRL, ROWS, 0xf, ROWS == 0xf);
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(v >> 32), CTRL, ROWS, 0xf, ROWS == 0xf);
+    return (int64_t)((uint64_t)hi << 32 | lo);
+}
+/* Sum of v over the threads in front of this one, and over all (in *total).  s: a value a wave, reused after a barrier. */
+template <int THREADS>
 __device__ __forceinline__ int64_t tab_scan(int64_t v, int64_t* s, int64_t* total) {
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
     int64_t x = v;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const int64_t y = __shfl_up(x, d);
-        if (lane >= d) x += y;
-    }
+    x += tab_moved<0x111, 0xf>(x);               /* row_shr 1, 2, 4, 8 */
+    x += tab_moved<0x112, 0xf>(x);
+    x += tab_moved<0x114, 0xf>(x);
+    x += tab_moved<0x118, 0xf>(x);
+    x += tab_moved<0x142, 0xa>(x);               /* row_bcast 15 into rows 1 and 3, 31 into 2 and 3 */
+    x += tab_moved<0x143, 0xc>(x);
     __syncthreads();
     if (lane == 63) s[w] = x;
     __syncthreads();
     int64_t before = 0, all = 0;
 #pragma unroll
-    for (int i = 0; i < TAB_WAVES; ++i) {
+    for (int i = 0; i < THREADS / BL_WAVE; ++i) {
         const int64_t t = s[i];
         before += i < w ? t : 0;
         all += t;
     }
     *total = all;
     return before + x - v;
+}
+/* Adds this wave's requests r of which `has` holds to a list in LDS. */
+__device__ __forceinline__ void tab_list(bool has, int r, int* list, int* count) {
+    const uint64_t m = __ballot(has);
+    if (!m) return;
+    const int lane = threadIdx.x & 63;
+    int at = 0;
+    if (lane == 0) at = atomicAdd(count, __builtin_popcountll(m));
+    at = __builtin_amdgcn_readlane(at, 0) + __builtin_popcountll(m & (((uint64_t)1 << lane) - 1));
+    if (has) list[at] = r;
 }
 
 /* Position and slot of row t of the batch: its request by bisection in the B + 1 ascending first rows. */
@@ -58,20 +73,24 @@ struct tab_args {
 };
 
 /* One workgroup: a handful of requests, or a few thousand, is latency and not work.  Three sums over the requests (rows
- * and returned blocks, then demand, which needs them), the copies between stack and table by whole waves, then the rows.
- * A thread holds TAB_PER consecutive requests where there are more than threads. */
-__global__ __launch_bounds__(TAB_THREADS) void bl_kv_tables_kernel(tab_args A) {
+ * and returned blocks, then demand, which needs them), the copies between stack and table a request a wave, IN
+ * entries of a lane in flight, then the rows.  A thread holds PER consecutive requests where there are more than threads. */
+template <int THREADS, int PER>
+__global__ __launch_bounds__(THREADS) void bl_kv_tables_kernel(tab_args A) {
     const bl_kv_batch& b = A.b;
-    __shared__ int64_t s_sum[TAB_WAVES];
-    __shared__ int s_start[BL_KV_MAX_REQUESTS], s_row[BL_KV_MAX_REQUESTS + 1];
-    __shared__ int s_taken, s_bad;
+    constexpr int MOST = THREADS * PER, WAVES = THREADS / BL_WAVE, IN = PER == 1 ? 16 : 8;
+    __shared__ int64_t s_sum[WAVES];
+    __shared__ int s_start[MOST], s_row[MOST + 1], s_list[MOST], s_from[MOST], s_n[MOST];
+    __shared__ int s_taken, s_bad, s_back, s_want;
     const int tid = threadIdx.x, B = (int)b.B, shift = A.shift, bs1 = (1 << shift) - 1;
-    const int per = (B + TAB_THREADS - 1) / TAB_THREADS;
-    if (tid == 0) s_taken = s_bad = 0;
-    int old[TAB_PER], n[TAB_PER];
+    const int per = PER == 1 ? 1 : (B + THREADS - 1) / THREADS;
+    if (tid == 0) s_taken = s_bad = s_back = s_want = 0;
+    const int64_t cap = b.free_cap;
+    int64_t there = b.free_count[0];
+    int old[PER], n[PER];
     int64_t rows = 0, back = 0;
 #pragma unroll
-    for (int i = 0; i < TAB_PER; ++i) {
+    for (int i = 0; i < PER; ++i) {
         const int r = tid * per + i;
         old[i] = n[i] = 0;
         if (i < per && r < B) {
@@ -80,75 +99,106 @@ __global__ __launch_bounds__(TAB_THREADS) void bl_kv_tables_kernel(tab_args A) {
             old[i] = (int)(L < 0 ? 0 : L > most ? most : L);
             n[i] = b.new_len[r];
         }
-        if (n[i] < 0) back += (old[i] + bs1) >> shift;
+        if (n[i] < 0) back += ((int64_t)old[i] + bs1) >> shift;
         else rows += n[i];
     }
-    const int64_t cap = b.free_cap;
-    int64_t there = b.free_count[0];
     there = there < 0 ? 0 : there > cap ? cap : there;
     int64_t all_rows, all_back;
-    int64_t row = tab_scan(rows, s_sum, &all_rows);
-    int64_t at = there + tab_scan(back, s_sum, &all_back);
-    const int lane = tid & 63;
-    /* ended requests: their blocks to the stack, a request at a time by its whole wave */
+    int64_t row = tab_scan<THREADS>(rows, s_sum, &all_rows);
+    int64_t at = there + tab_scan<THREADS>(back, s_sum, &all_back);
+    const int lane = tid & 63, wave = tid >> 6;
+    if (all_back) {
+        /* ended requests: their blocks to the stack */
 #pragma unroll
-    for (int i = 0; i < TAB_PER; ++i) {
-        if (i >= per) break;
-        const int r = tid * per + i, have = n[i] < 0 ? (old[i] + bs1) >> shift : 0;
-        uint64_t todo = __ballot(have > 0);
-        const int64_t mine = at;
-        if (have > 0 && mine + have > cap) atomicAdd(&s_bad, 1);
-        at += have;
-        while (todo) {
-            const int l = __builtin_ctzll(todo);
-            todo &= todo - 1;
-            const int h = __shfl(have, l), rr = __shfl(r, l);
-            const int64_t to = __shfl(mine, l);
-            for (int j = lane; j < h && to + j < cap; j += 64) b.free_list[to + j] = b.table[rr * b.table_stride + j];
+        for (int i = 0; i < PER; ++i) {
+            if (i >= per) break;
+            const int r = tid * per + i, have = n[i] < 0 ? (int)(((int64_t)old[i] + bs1) >> shift) : 0;
+            if (have > 0 && at + have > cap) atomicAdd(&s_bad, 1);
+            if (have > 0) s_from[r] = (int)(at < cap ? at : cap), s_n[r] = at < cap ? (int)(cap - at < have ? cap - at : have) : 0;
+            tab_list(have > 0, r, s_list, &s_back);
+            at += have;
+        }
+        __syncthreads();
+        for (int k = wave; k < s_back; k += WAVES) {
+            const int r = s_list[k], have = s_n[r];
+            int32_t* to = b.free_list + s_from[r];
+            const int32_t* from = b.table + r * b.table_stride;
+            for (int j = lane; j < have; j += IN * 64) {
+                int v[IN];
+#pragma unroll
+                for (int u = 0; u < IN; ++u)
+                    if (j + 64 * u < have) v[u] = from[j + 64 * u];
+#pragma unroll
+                for (int u = 0; u < IN; ++u)
+                    if (j + 64 * u < have) to[j + 64 * u] = v[u];
+            }
         }
     }
     there = there + all_back > cap ? cap : there + all_back;
     /* demand */
     int64_t want = 0, row_i = row;
-    int w_i[TAB_PER];
-    bool fits[TAB_PER];
+    int w_i[PER];
+    bool fits[PER];
 #pragma unroll
-    for (int i = 0; i < TAB_PER; ++i) {
+    for (int i = 0; i < PER; ++i) {
         const int64_t need = ((int64_t)old[i] + (n[i] > 0 ? n[i] : 0) + bs1) >> shift;
         row_i += n[i] > 0 ? n[i] : 0;
         fits[i] = n[i] >= 0 && need <= b.max_blocks && row_i <= b.rows;
-        w_i[i] = fits[i] ? (int)(need - ((old[i] + bs1) >> shift)) : 0;
+        w_i[i] = fits[i] ? (int)(need - (((int64_t)old[i] + bs1) >> shift)) : 0;
         want += w_i[i];
     }
     int64_t all_want;
-    int64_t upto = tab_scan(want, s_sum, &all_want);       /* (its barriers: the stack is whole behind them) */
+    int64_t upto = tab_scan<THREADS>(want, s_sum, &all_want);       /* (its barriers: the stack is whole behind them) */
     row_i = row;
 #pragma unroll
-    for (int i = 0; i < TAB_PER; ++i) {
+    for (int i = 0; i < PER; ++i) {
         if (i >= per) break;
         const int r = tid * per + i;
         const bool live = r < B;
         const int64_t before = upto;
         upto += w_i[i];
-        const bool ok = live && fits[i] && (w_i[i] == 0 || upto <= there);
+        const bool ok = live && fits[i] && (w_i[i] == 0 || upto <= there), takes = ok && w_i[i] > 0;
         if (live && n[i] >= 0 && !ok) atomicAdd(&s_bad, 1);
-        if (ok && w_i[i] > 0) atomicMax(&s_taken, (int)upto);
-        if (live) {
+        if (takes) {
+            atomicMax(&s_taken, (int)upto);
+            s_from[r] = (int)(there - 1 - before), s_n[r] = w_i[i];
+            s_start[r] = (int)(((int64_t)old[i] + bs1) >> shift);   /* (for now: the blocks that it has) */
+        }
+        tab_list(takes, r, s_list, &s_want);
+        row_i += n[i] > 0 ? n[i] : 0;
+    }
+    if (all_want) {
+        __syncthreads();
+        for (int k = wave; k < s_want; k += WAVES) {
+            const int r = s_list[k], w = s_n[r];
+            int32_t* to = b.table + r * b.table_stride + s_start[r];
+            const int32_t* from = b.free_list + s_from[r];
+            for (int j = lane; j < w; j += IN * 64) {
+                int v[IN];
+#pragma unroll
+                for (int u = 0; u < IN; ++u)
+                    if (j + 64 * u < w) v[u] = from[-(j + 64 * u)];
+#pragma unroll
+                for (int u = 0; u < IN; ++u)
+                    if (j + 64 * u < w) to[j + 64 * u] = v[u];
+            }
+        }
+        __syncthreads();
+    }
+    upto -= want, row_i = row;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        if (i >= per) break;
+        const int r = tid * per + i;
+        upto += w_i[i];
+        const bool ok = fits[i] && (w_i[i] == 0 || upto <= there);
+        if (r < B) {
             const int first = (int)(row_i < b.rows ? row_i : b.rows), st = ok ? old[i] : -1;
             s_start[r] = b.start[r] = st;
             s_row[r] = b.q_start[r] = first;
             b.seq_len_out[r] = n[i] < 0 ? 0 : ok ? old[i] + n[i] : old[i];
         }
         row_i += n[i] > 0 ? n[i] : 0;
-        const int have = (old[i] + bs1) >> shift;
-        uint64_t todo = __ballot(ok && w_i[i] > 0);
-        while (todo) {
-            const int l = __builtin_ctzll(todo);
-            todo &= todo - 1;
-            const int w = __shfl(w_i[i], l), rr = __shfl(r, l), h = __shfl(have, l);
-            const int64_t from = there - 1 - __shfl(before, l);
-            for (int j = lane; j < w; j += 64) b.table[rr * b.table_stride + h + j] = b.free_list[from - j];
-        }
     }
     if (tid == 0) s_row[B] = b.q_start[B] = (int)(all_rows < b.rows ? all_rows : b.rows);
     __syncthreads();
@@ -157,7 +207,7 @@ __global__ __launch_bounds__(TAB_THREADS) void bl_kv_tables_kernel(tab_args A) {
         b.bad[0] = s_bad;
     }
     if (b.rows <= TAB_ROWS_INSIDE)
-        for (int64_t t = tid; t < b.rows; t += TAB_THREADS) tab_row(t, B, s_row, s_start, b.table, b.table_stride, shift, b.positions, b.slots);
+        for (int64_t t = tid; t < b.rows; t += THREADS) tab_row(t, B, s_row, s_start, b.table, b.table_stride, shift, b.positions, b.slots);
 }
 
 /* The rows of a large batch, behind the table kernel: one thread a row. */
@@ -179,7 +229,10 @@ extern "C" bl_status bl_kv_tables(const bl_kv_batch* b, bl_stream s) {
     for (const void* q : p)
         if (!bl_aligned(q, 4)) return BL_ERR_ALIGN;
     tab_args A = {*b, bl_log2(b->block)};
-    bl_kv_tables_kernel<<<1, TAB_THREADS, 0, (hipStream_t)s>>>(A);
+    /* (a small step's barriers are those of four waves instead of sixteen) */
+    if (b->B <= 256 && b->rows <= 1024) bl_kv_tables_kernel<256, 1><<<1, 256, 0, (hipStream_t)s>>>(A);
+    else if (b->B <= 1024) bl_kv_tables_kernel<1024, 1><<<1, 1024, 0, (hipStream_t)s>>>(A);
+    else bl_kv_tables_kernel<1024, BL_KV_MAX_REQUESTS / 1024><<<1, 1024, 0, (hipStream_t)s>>>(A);
     if (b->rows > TAB_ROWS_INSIDE) bl_kv_slots_kernel<<<(unsigned)((b->rows + 255) / 256), 256, 0, (hipStream_t)s>>>(A);
     return hipGetLastError() == hipSuccess ? BL_OK : BL_ERR_HIP;
 }
@@ -450,7 +503,13 @@ __device__ __forceinline__ void app_query_units(const app_args& A, uint32_t unit
 template <int SRC, int KIND, int D, int NP, int WAVES>
 __global__ __launch_bounds__(APP_THREADS) void bl_kv_append_kernel(app_args A, int kv_blocks, int per, uint32_t units_row, uint32_t all) {
     const int x = (int)blockIdx.x;
-    if (x < kv_blocks) app_cache_rows<SRC, KIND, D, NP, WAVES>(A, (int64_t)(x % A.windows) * A.window, x / A.windows);
+    if (x < kv_blocks) {
+        /* Consecutive workgroups go to the eight dies in turn, and the windows in which runs start are evenly spaced: each die takes
+         * a contiguous eighth of the windows, else a few dies have all the work (4096 tokens 37 -> 22 us). */
+        const int pairs = kv_blocks / A.windows, die = x & 7, part = kv_blocks >> 3, more = kv_blocks & 7;
+        const int at = die * part + (die < more ? die : more) + (x >> 3);
+        app_cache_rows<SRC, KIND, D, NP, WAVES>(A, (int64_t)(at / pairs) * A.window, at % pairs);
+    }
     else app_query_units<SRC, D>(A, (uint32_t)(x - kv_blocks) * (uint32_t)per * APP_THREADS, per, units_row, all);
 }
 
