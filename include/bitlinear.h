@@ -448,7 +448,7 @@ bl_status bl_kv_tables(const bl_kv_batch* b, bl_stream s);
  * outside 0 .. n_pos-1: the same, the Q row of such a position is zeros, and *bad (1 int or NULL) is INCREASED by one.
  *   q_out     bf16 [T][n_q * head_dim] or NULL, rows q_stride values apart
  *   qkv       rows qkv_stride values apart (a multiple of 4 for fp32, 8 for bf16); kind 0 fp32, 1 bf16
- * n_q >= 0, 1 <= T <= 2^24; pointers 16-byte aligned (positions, slots, bad: 4), q_stride a multiple of 8. */
+ * n_q >= 0, 1 <= T <= 2^24, T * n_q * head_dim at most 2^36; pointers 16-byte aligned (positions, slots, bad: 4), q_stride a multiple of 8. */
 enum { BL_KV_FROM_F32 = 0, BL_KV_FROM_BF16 = 1 };
 typedef struct {
     bl_kv_cache cache;

@@ -246,6 +246,7 @@ struct app_args {
     int shift, window, windows;            /* log2(block); rows of a K/V workgroup, and how many such there are */
 };
 
+typedef uint32_t app_v4u __attribute__((ext_vector_type(4)));
 /* Four consecutive values of a row. */
 template <int SRC>
 __device__ __forceinline__ void app_load4(const void* row, int64_t i, float (&v)[4]) {
@@ -308,14 +309,6 @@ __device__ __forceinline__ void app_move(uint8_t* p, int bytes, float ratio) {
     }
 }
 
-/* Whether row t goes into the cache. */
-__device__ __forceinline__ bool app_goes(const app_args& A, int slot, int64_t t) {
-    if (slot < 0 || (int64_t)slot >= A.t.cache.n_blocks << A.shift) return false;
-    if (!A.t.cos) return true;
-    const int pos = A.t.positions[t];
-    return pos >= 0 && pos < A.t.n_pos;
-}
-
 /* K and V: a run is the rows that go to one block (row t + k to the slot k further).  A workgroup looks at `window` rows, one a
  * lane, and does the runs that start there, WAVES waves for K or V of a head, 4 / WAVES of these beside each other: a unit's values
  * (block x D fp32 at most) stay in registers between the maximum and the rounding, so that a row is read once.
@@ -336,37 +329,43 @@ __device__ __forceinline__ void app_cache_rows(const app_args& A, int64_t first,
     const int h = live ? which >> 1 : 0, head = A.t.n_q + (is_v ? H : 0) + h;
     const int sub = tid % TPR, rowi = tid / TPR, i4 = sub * 4;
     const int64_t T_all = A.t.T;
-    uint64_t todo;
+    /* Slots and positions of the rows around, all that this needs of them, in one go: [0..2] are the rows from `first` on,
+     * [3..4] those in front of it, downwards.  What goes nowhere has the slot -1. */
+    constexpr int SETS = 5;
+    int slots[SETS], places[SETS];
     {
-        const int64_t t = first + lane;
-        bool goes = false, goes_on = false;
-        if (lane < A.window && t < T_all) {
-            const int slot = A.t.slots[t];
-            goes = app_goes(A, slot, t);
-            if (goes && (slot & (bs - 1)) && t > 0 && A.t.slots[t - 1] == slot - 1) goes_on = app_goes(A, slot - 1, t - 1);
-            if (A.t.bad && pair == 0 && threadIdx.x < 64) {
-                const int pos = A.t.cos ? A.t.positions[t] : 0;
-                if (slot < -1 || (int64_t)slot >= C.n_blocks << A.shift || (A.t.cos && (pos < 0 || pos >= A.t.n_pos))) atomicAdd(A.t.bad, 1);
-            }
+        int64_t at[SETS];
+        bool in[SETS];
+#pragma unroll
+        for (int k = 0; k < SETS; ++k) {
+            at[k] = k < 3 ? first + 64 * k + lane : first - 1 - 64 * (k - 3) - lane;
+            in[k] = at[k] >= 0 && at[k] < T_all && (bs == 128 || (k != 2 && k != 4));      /* (a block of 64 ends within 80 rows) */
+            slots[k] = in[k] ? A.t.slots[at[k]] : -1;
+            places[k] = in[k] && A.t.cos ? A.t.positions[at[k]] : 0;
         }
-        todo = __ballot(goes && !goes_on);
+        if (A.t.bad && pair == 0 && threadIdx.x < A.window && in[0] &&
+            (slots[0] < -1 || (int64_t)slots[0] >= C.n_blocks << A.shift || (A.t.cos && (places[0] < 0 || places[0] >= A.t.n_pos))))
+            atomicAdd(A.t.bad, 1);
+#pragma unroll
+        for (int k = 0; k < SETS; ++k)
+            if (slots[k] < 0 || (int64_t)slots[k] >= C.n_blocks << A.shift || (A.t.cos && (places[k] < 0 || places[k] >= A.t.n_pos))) slots[k] = -1;
     }
+    uint64_t todo = __ballot(lane < A.window && slots[0] >= 0);
     while (todo) {
-        const int64_t t0 = first + __builtin_ctzll(todo);
-        todo &= todo - 1;
-        const int slot = A.t.slots[t0], off = slot & (bs - 1);
-        /* Rows that stand where this block's tokens in front of this one would: the first of them does the block.  Then the
-         * block's rows from this one on, a bit each (a row may be missing: a slot of -1, a bad position). */
-        uint64_t m0, m1 = 0;
+        const int l0 = __builtin_ctzll(todo);
+        const int64_t t0 = first + l0;
+        const int slot = __builtin_amdgcn_readlane(slots[0], l0), off = slot & (bs - 1);
+        /* The block's rows, a bit each: row t0 + k goes to the slot k further (one may be missing: a slot of -1, a bad position).
+         * The first of them does the block. */
+        uint64_t m0, m1;
         {
-            auto member = [&](int k) {                                  /* row t0 + k, the slot k further */
-                const int64_t t = t0 + k;
-                return t >= 0 && t < T_all && off + k >= 0 && off + k < bs && A.t.slots[t] == slot + k && app_goes(A, slot + k, t);
-            };
-            m0 = __ballot(member(lane));
-            if (bs > 64) m1 = __ballot(member(64 + lane));
-            uint64_t earlier = off ? __ballot(member(-1 - lane)) : 0;
-            if (off > 64) earlier |= __ballot(member(-65 - lane));
+            auto member = [&](int set, int k) { return slots[set] >= 0 && slots[set] == slot + k && off + k >= 0 && off + k < bs; };
+            const uint64_t a0 = __ballot(member(0, lane - l0)), a1 = __ballot(member(1, 64 + lane - l0)), a2 = bs == 128 ? __ballot(member(2, 128 + lane - l0)) : 0;
+            m0 = l0 ? a0 >> l0 | a1 << (64 - l0) : a0;
+            m1 = l0 ? a1 >> l0 | a2 << (64 - l0) : a1;
+            todo &= ~a0;                                                /* (none of these begins another run) */
+            uint64_t earlier = __ballot(member(3, -1 - lane - l0));
+            if (bs == 128) earlier |= __ballot(member(4, -65 - lane - l0));
             if (earlier) continue;
         }
         const int n = m1 ? 128 - __builtin_clzll(m1) : 64 - __builtin_clzll(m0);
@@ -380,7 +379,17 @@ __device__ __forceinline__ void app_cache_rows(const app_args& A, int64_t first,
 #pragma unroll
         for (int p = 0; p < NP; ++p) {
             const int r = p * ROWS + rowi;
-            if (live && has(r)) app_pair<SRC, D>(A, app_row<SRC>(A, t0 + r), head, i4, !is_v && A.t.cos, A.t.cos ? A.t.positions[t0 + r] : 0, a[p], b[p]);
+            int place = 0;                                              /* the row's position, from the lane that has it */
+            if (A.t.cos) {
+                place = __shfl(places[0], (l0 + r) & 63);
+                const int next = __shfl(places[1], (l0 + r) & 63);
+                if (l0 + r >= 64) place = next;
+                if (bs == 128) {
+                    const int third = __shfl(places[2], (l0 + r) & 63);
+                    if (l0 + r >= 128) place = third;
+                }
+            }
+            if (live && has(r)) app_pair<SRC, D>(A, app_row<SRC>(A, t0 + r), head, i4, !is_v && A.t.cos, place, a[p], b[p]);
             else
 #pragma unroll
                 for (int j = 0; j < 4; ++j) a[p][j] = b[p][j] = 0.0f;
@@ -476,32 +485,62 @@ __device__ __forceinline__ void app_cache_rows(const app_args& A, int64_t first,
     }
 }
 
-/* Q of `per` * 256 units of eight values and their partners, beginning at unit0. */
-template <int SRC, int D>
-__device__ __forceinline__ void app_query_units(const app_args& A, uint32_t unit0, int per, uint32_t units_row, uint32_t all) {
-    constexpr int TPH = D / 16;                                         /* units a head */
-    for (int k = 0; k < per; ++k) {
-        const uint32_t u = unit0 + k * APP_THREADS + threadIdx.x;
-        if (u >= all) return;
-        const uint32_t t = u / units_row, r = u % units_row;
-        const int h = (int)(r / TPH), i = (int)(r % TPH) * 8;
-        const int64_t pos = A.t.cos ? A.t.positions[t] : 0;
-        float a[2][4] = {}, b[2][4] = {};
-        if (!A.t.cos || (pos >= 0 && pos < A.t.n_pos)) {
-            const void* row = app_row<SRC>(A, t);
+/* Eight consecutive values of a row. */
+template <int SRC>
+__device__ __forceinline__ void app_load8(const void* row, int64_t i, float (&v)[8]) {
+    if (SRC == BL_KV_FROM_F32) {
+        float a[4], b[4];
+        app_load4<SRC>(row, i, a), app_load4<SRC>(row, i + 4, b);
 #pragma unroll
-            for (int j = 0; j < 2; ++j) app_pair<SRC, D>(A, row, h, i + 4 * j, A.t.cos != nullptr, pos, a[j], b[j]);
-        }
-        uint16_t* o = A.t.q_out + (int64_t)t * A.t.q_stride + h * D + i;
-        typedef uint32_t v4u __attribute__((ext_vector_type(4)));
-        *bl_g((v4u*)o) = (v4u){bl_pack2_bf16(a[0][0], a[0][1]), bl_pack2_bf16(a[0][2], a[0][3]), bl_pack2_bf16(a[1][0], a[1][1]), bl_pack2_bf16(a[1][2], a[1][3])};
-        *bl_g((v4u*)(o + D / 2)) = (v4u){bl_pack2_bf16(b[0][0], b[0][1]), bl_pack2_bf16(b[0][2], b[0][3]), bl_pack2_bf16(b[1][0], b[1][1]), bl_pack2_bf16(b[1][2], b[1][3])};
+        for (int j = 0; j < 4; ++j) v[j] = a[j], v[4 + j] = b[j];
+    } else {
+        const app_v4u x = *bl_gc<app_v4u>((const uint16_t*)row + i);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[2 * j] = bl_bf16_to_f32(x[j] & 0xffff), v[2 * j + 1] = __uint_as_float(x[j] & 0xffff0000u);
     }
+}
+/* Q: a thread has eight values and their partners, the same ones of APP_HEADS heads of a row (their angles are read once). */
+#define APP_HEADS 2
+template <int SRC, int D>
+__device__ __forceinline__ void app_query_units(const app_args& A, uint32_t u, uint32_t units_row, uint32_t all) {
+    constexpr int TPH = D / 16;                                         /* threads a head */
+    if (u >= all) return;
+    const uint32_t t = u / units_row, r = u % units_row;
+    const int h0 = (int)(r / TPH) * APP_HEADS, i = (int)(r % TPH) * 8;
+    const int64_t pos = A.t.cos ? A.t.positions[t] : 0;
+    const bool there = !A.t.cos || (pos >= 0 && pos < A.t.n_pos);
+    const void* row = app_row<SRC>(A, t);
+    float a[APP_HEADS][8], b[APP_HEADS][8], c[8], s[8];
+#pragma unroll
+    for (int k = 0; k < APP_HEADS; ++k)
+        if (h0 + k < A.t.n_q) {
+            app_load8<SRC>(row, (int64_t)(h0 + k) * D + i, a[k]);
+            app_load8<SRC>(row, (int64_t)(h0 + k) * D + i + D / 2, b[k]);
+        }
+    if (A.t.cos && there) {
+        app_load8<BL_KV_FROM_F32>(A.t.cos + pos * (D / 2), i, c);
+        app_load8<BL_KV_FROM_F32>(A.t.sin + pos * (D / 2), i, s);
+    }
+#pragma unroll
+    for (int k = 0; k < APP_HEADS; ++k)
+        if (h0 + k < A.t.n_q) {
+            if (A.t.cos) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float x = a[k][j], y = b[k][j];
+                    a[k][j] = there ? x * c[j] - y * s[j] : 0.0f;
+                    b[k][j] = there ? y * c[j] + x * s[j] : 0.0f;
+                }
+            }
+            uint16_t* o = A.t.q_out + (int64_t)t * A.t.q_stride + (h0 + k) * D + i;
+            *bl_g((app_v4u*)o) = (app_v4u){bl_pack2_bf16(a[k][0], a[k][1]), bl_pack2_bf16(a[k][2], a[k][3]), bl_pack2_bf16(a[k][4], a[k][5]), bl_pack2_bf16(a[k][6], a[k][7])};
+            *bl_g((app_v4u*)(o + D / 2)) = (app_v4u){bl_pack2_bf16(b[k][0], b[k][1]), bl_pack2_bf16(b[k][2], b[k][3]), bl_pack2_bf16(b[k][4], b[k][5]), bl_pack2_bf16(b[k][6], b[k][7])};
+        }
 }
 
 /* Workgroups of K and V (window x head pairs) first, those of Q behind them. */
 template <int SRC, int KIND, int D, int NP, int WAVES>
-__global__ __launch_bounds__(APP_THREADS) void bl_kv_append_kernel(app_args A, int kv_blocks, int per, uint32_t units_row, uint32_t all) {
+__global__ __launch_bounds__(APP_THREADS) void bl_kv_append_kernel(app_args A, int kv_blocks, uint32_t units_row, uint32_t all) {
     const int x = (int)blockIdx.x;
     if (x < kv_blocks) {
         /* Consecutive workgroups go to the eight dies in turn, and the windows in which runs start are evenly spaced: each die takes
@@ -510,18 +549,16 @@ __global__ __launch_bounds__(APP_THREADS) void bl_kv_append_kernel(app_args A, i
         const int at = die * part + (die < more ? die : more) + (x >> 3);
         app_cache_rows<SRC, KIND, D, NP, WAVES>(A, (int64_t)(at / pairs) * A.window, at % pairs);
     }
-    else app_query_units<SRC, D>(A, (uint32_t)(x - kv_blocks) * (uint32_t)per * APP_THREADS, per, units_row, all);
+    else app_query_units<SRC, D>(A, (uint32_t)(x - kv_blocks) * APP_THREADS + threadIdx.x, units_row, all);
 }
 
 template <int SRC, int KIND, int D, int NP, int WAVES>
 static bl_status app_launch(const app_args& A, hipStream_t st) {
     constexpr int UNITS = APP_THREADS / BL_WAVE / WAVES;
-    const int64_t units_row = A.t.q_out ? (int64_t)A.t.n_q * (D / 16) : 0, all = A.t.T * units_row;
-    /* two units a thread where that leaves more workgroups than the chip holds */
-    const int per = all > (int64_t)4096 * APP_THREADS ? 2 : 1;
-    const int64_t kv = (int64_t)A.windows * ((2 * A.t.cache.n_kv + UNITS - 1) / UNITS), q = (all + per * APP_THREADS - 1) / (per * APP_THREADS);
+    const int64_t units_row = A.t.q_out ? (int64_t)((A.t.n_q + APP_HEADS - 1) / APP_HEADS) * (D / 16) : 0, all = A.t.T * units_row;
+    const int64_t kv = (int64_t)A.windows * ((2 * A.t.cache.n_kv + UNITS - 1) / UNITS), q = (all + APP_THREADS - 1) / APP_THREADS;
     if (all > 0xf0000000ll || kv + q > 0x7fffffff) return BL_ERR_SHAPE;
-    bl_kv_append_kernel<SRC, KIND, D, NP, WAVES><<<(unsigned)(kv + q), APP_THREADS, 0, st>>>(A, (int)kv, per, units_row ? (uint32_t)units_row : 1, (uint32_t)all);
+    bl_kv_append_kernel<SRC, KIND, D, NP, WAVES><<<(unsigned)(kv + q), APP_THREADS, 0, st>>>(A, (int)kv, units_row ? (uint32_t)units_row : 1, (uint32_t)all);
     return BL_OK;
 }
 /* Waves and passes by the block's size: 1024 to 2048 values of a block and head are one wave's, 16384 four waves' in eight passes. */
