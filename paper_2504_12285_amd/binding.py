@@ -598,11 +598,12 @@ class KVAppend(_KVCall):
 
 class KVAttention(_KVCall):
     """Causal attention over the cache (bl_attn_kv8).  q bf16 [T][n_q][head_dim] (or [T][n_q * head_dim] with n_q); q_start int32 [B + 1],
-    seq_len int32 [B], table int32 [B][max_blocks].  max_q: no request has more queries; max_len: about the longest length.
-    Output: out bf16 [T][n_q * head_dim]."""
+    seq_len int32 [B], table int32 [B][max_blocks].  max_q: no request has more queries (None: all T rows may be one request's);
+    max_len: about the longest length.  Output: out bf16 [T][n_q * head_dim].  The workspace may serve several handles whose runs
+    follow each other on one stream."""
     _which, _where = 2, "bl_attn_kv8"
 
-    def __init__(self, cache, q, q_start, seq_len, table, n_q=None, max_q=1, max_len=0, softmax_scale=None, window=0, out=None, workspace=None):
+    def __init__(self, cache, q, q_start, seq_len, table, n_q=None, max_q=None, max_len=0, softmax_scale=None, window=0, out=None, workspace=None):
         torch = _get_torch()
         dev, dim, T, B = cache.k.device, cache.head_dim, q.shape[0], seq_len.shape[0]
         n_q = q.shape[1] if n_q is None else n_q
@@ -616,7 +617,7 @@ class KVAttention(_KVCall):
             _wants(out, "out", torch.bfloat16, dev, (T, n_q * dim), rows=True)
         self.cache, self.q, self.q_start, self.seq_len, self.table, self.out = cache, q, q_start, seq_len, table, out
         self.desc = AttnDesc(cache.desc, _ptr(q), _row_stride(q), _row_stride(out), _row_stride(table), B, T, _ptr(q_start), _ptr(seq_len),
-                             _ptr(table), n_q, table.shape[1], max_q, max_len, window, dim ** -0.5 if softmax_scale is None else softmax_scale,
+                             _ptr(table), n_q, table.shape[1], T if max_q is None else max_q, max_len, window, dim ** -0.5 if softmax_scale is None else softmax_scale,
                              _ptr(out), None)
         nbytes = load().bl_attn_workspace_bytes(ctypes.byref(self.desc))
         if workspace is None:

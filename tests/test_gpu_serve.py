@@ -48,7 +48,7 @@ def test_prompts_decode_steps_and_ends(model, kind):
         check_attention(layers, lens, [max(n, 0) for n in new], kind)
 
 
-@pytest.mark.parametrize("few_rows, new", [(2, (1, 1)), (10, (6, 4))])
+@pytest.mark.parametrize("few_rows, new", [(1, (1, 0)), (10, (6, 4))])
 def test_every_route_of_the_products_gives_the_same_rows(model, few_rows, new):
     """The same tokens through steps of few rows (products with their producers inside, or the grouped product) and of many (the
     prefill product): the arithmetic is the same bit for bit up to the attention, so the first layer's codes and scales are too."""
@@ -60,8 +60,11 @@ def test_every_route_of_the_products_gives_the_same_rows(model, few_rows, new):
     many.step(torch.cat([x, torch.zeros(100 - few_rows, 2560, device=DEV)]), n)
     a, b = few.caches[0], many.caches[0]
     for name in ("k_scale", "v_scale"):
-        assert torch.equal(getattr(a, name)[few.table[:, 0].long()], getattr(b, name)[many.table[:, 0].long()])
+        for r in range(2):
+            assert new[r] == 0 or torch.equal(getattr(a, name)[int(few.table[r, 0])], getattr(b, name)[int(many.table[r, 0])])
     for r in range(2):
+        if new[r] == 0:
+            continue
         i, j = int(few.table[r, 0]), int(many.table[r, 0])
         assert torch.equal(a.k[i, :, :new[r]], b.k[j, :, :new[r]]) and torch.equal(a.v[i, :, :, :new[r]], b.v[j, :, :, :new[r]])
     check_attention(few, list(new), list(new), 0)
