@@ -25,8 +25,8 @@ typedef uint32_t at_v4u __attribute__((ext_vector_type(4)));
 #define AT_WAVES 4
 #define AT_FEW 16                  /* rows of a request and kv head up to which at_few does it */
 #define AT_MANY 128                /* rows a workgroup of at_many */
-#define AT_ROWS_GRID 512           /* workgroups of at_few: two a unit */
-#define AT_STREAMS (AT_ROWS_GRID * AT_WAVES)
+#define AT_STREAM_GROUPS 512       /* workgroups of at_few: two a unit */
+#define AT_STREAMS (AT_STREAM_GROUPS * AT_WAVES)
 #define AT_GROW 8.0f
 #define AT_LIFT 6.0f
 
@@ -752,25 +752,18 @@ __device__ __forceinline__ void at_many(const at_args& A, int place, at_many_lds
     const int tid = threadIdx.x, lane = tid & 63, wave = at_uniform(tid >> 6);
     const int col = lane & 31, half = lane >> 5;
     /* whose tile: place = (row tile * n_kv + head) * splits + piece, a request's heavy tiles first */
-    int piece, h, want, b, before, c;
-    auto take = [&](int all) {
-        /* Of the 512 workgroups that the chip holds the second 256 go the other way round, so that a unit has a heavy one
-         * and a light one. */
-        const int n = all * A.n_kv * A.splits, both = n < 512 ? n : 512;
-        if (place >= 256 && place < both) place = 255 + both - place;
-        piece = place % A.splits, h = place / A.splits % A.n_kv, want = place / A.splits / A.n_kv;
-        return place < n;
-    };
+    const int piece = place % A.splits, h = place / A.splits % A.n_kv, want = place / A.splits / A.n_kv;
+    int b, before, c;
     if (A.B <= 64) {
         const int upto = at_scan(lane < A.B ? at_many_tiles(A, lane) : 0);
-        if (!take(__builtin_amdgcn_readlane(upto, 63))) return;
+        if (want >= __builtin_amdgcn_readlane(upto, 63)) return;
         b = __builtin_ctzll(__ballot(upto > want));
         before = b ? __builtin_amdgcn_readlane(upto, b - 1) : 0;
         c = __builtin_amdgcn_readlane(upto, b) - before;
     } else {
         int* s_upto = lds.upto;
         at_sums(A.B, [&](int i) { return at_many_tiles(A, i); }, s_upto, lds.scan);
-        if (!take(at_uniform(s_upto[A.B - 1]))) return;
+        if (want >= at_uniform(s_upto[A.B - 1])) return;
         int lo = -1, hi = A.B - 1;
         while (hi - lo > 1) {
             const int mid = (lo + hi) >> 1;
@@ -1148,13 +1141,13 @@ __global__ __launch_bounds__(AT_THREADS, 2) void bl_attn_any(at_args A, int many
     if ((int)blockIdx.x < many) at_many<KIND, D>(A, (int)blockIdx.x, ((lds_t*)lds)->many);
     else at_few<KIND, D, WIDE>(A, (int)blockIdx.x - many, ((lds_t*)lds)->few);
 }
-/* Partial results of both: `few` workgroups for those of at_few, turns x AT_ROWS_GRID, the others for a split. */
+/* Partial results of both: `few` workgroups for those of at_few, turns x AT_STREAM_GROUPS, the others for a split. */
 template <int D, bool MANY>
 __global__ __launch_bounds__(AT_THREADS) void bl_attn_join(at_args A, int few) {
     __shared__ __attribute__((aligned(16))) at_join_lds<D> lds;
     const int x = (int)blockIdx.x;
     /* (sixteen partial results in flight are 122 registers: where a split's rows stand beside them, their loads need the waves more) */
-    if (!MANY || x < few) at_few_join<D, MANY ? 4 : 16>(A, x % AT_ROWS_GRID, x / AT_ROWS_GRID, few / AT_ROWS_GRID, lds);
+    if (!MANY || x < few) at_few_join<D, MANY ? 4 : 16>(A, x % AT_STREAM_GROUPS, x / AT_STREAM_GROUPS, few / AT_STREAM_GROUPS, lds);
     else at_many_join<D>(A, x - few);
 }
 
@@ -1217,7 +1210,7 @@ template <int KIND, int D, bool WIDE>
 static void at_launch(at_args A, const at_plan& p, const bl_attn_desc* a, hipStream_t st) {
     A.part = (float*)a->workspace;
     A.many_part = A.part + p.few_bytes / sizeof(float);
-    const int few = p.few ? AT_ROWS_GRID : 0;
+    const int few = p.few ? AT_STREAM_GROUPS : 0;
     if (p.many) {
         const int many = p.row_tiles * A.n_kv * p.splits;
         if (few) bl_attn_any<KIND, D, WIDE><<<(unsigned)(many + few), AT_THREADS, 0, st>>>(A, many);
@@ -1226,7 +1219,7 @@ static void at_launch(at_args A, const at_plan& p, const bl_attn_desc* a, hipStr
         bl_attn_few<KIND, D, WIDE><<<(unsigned)few, AT_THREADS, 0, st>>>(A);
     }
     const int64_t rows = (int64_t)A.T * A.n_q, per = AT_THREADS / (D / 4);
-    const int few_join = p.few ? AT_ROWS_GRID * ((p.rows + 256 / D - 1) / (256 / D)) : 0;      /* (D / 4 lanes a row of a wave) */
+    const int few_join = p.few ? AT_STREAM_GROUPS * ((p.rows + 256 / D - 1) / (256 / D)) : 0;      /* (D / 4 lanes a row of a wave) */
     const int64_t join = few_join + (p.splits > 1 ? (rows + per - 1) / per : 0);
     if (p.splits > 1) bl_attn_join<D, true><<<(unsigned)join, AT_THREADS, 0, st>>>(A, few_join);
     else if (join) bl_attn_join<D, false><<<(unsigned)join, AT_THREADS, 0, st>>>(A, few_join);
