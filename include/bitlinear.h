@@ -468,7 +468,8 @@ bl_status bl_kv_append(const bl_kv_tokens* t, bl_stream s);
  * key/value head h / (n_q / n_kv)); they are its last tokens: query i of n has the position p = seq_len[b] - n + i and sees
  * the tokens 0 .. p (window > 0: p - window + 1 .. p) that are in the cache.
  *   out[row][h] = bf16( sum_j softmax_j( softmax_scale * <q, k_j> ) v_j ),  zeros where nothing is seen.
- * Products with K take the codes as they are against q in two 8-bit pieces of 16 bits in all of its largest value (e4m3: two e4m3 pieces, 8 significant bits);
+ * Products with K take the codes as they are against q in two 8-bit pieces of 16 bits in all of its largest value (e4m3: two e4m3 pieces, 8 significant bits;
+ * int8 with heads of 64 and many queries: q in fp16 times a power of two);
  * softmax weights are rounded to fp16 (11 bits; those below 2^-20 of a row's largest to 2^-30 of it) in front of the product with V; maxima, sums and outputs are held in fp32.
  *   q, out     rows q_stride / out_stride values apart (multiples of 8), 16-byte aligned.  Rows of no request are left alone.
  *   table      [B][table_stride]; an entry outside 0 .. n_blocks-1: its tokens are not seen

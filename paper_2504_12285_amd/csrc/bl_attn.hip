@@ -146,18 +146,22 @@ __device__ __forceinline__ void at_pieces(const uint32_t (&w)[8], float inv, bl_
         }
     }
 }
-/* Multiplier of a row for at_pieces, and the scale of what it gives, from its largest |q| (0: all zero). */
+/* Multiplier of a row of q, and the scale of what it gives, from its largest |q| (0: all zero).
+ * A power of two that takes the largest to [2^(e-127), 2^(e-126)). */
+__device__ __forceinline__ void at_power_scale(float most, int e, float& inv, float& scale) {
+    e -= (int)(__float_as_uint(most) >> 23);
+    e = e > 120 ? 120 : e < -120 ? -120 : e;
+    inv = most > 0.0f ? __uint_as_float((uint32_t)(127 + e) << 23) : 0.0f;
+    scale = __uint_as_float((uint32_t)(127 - e) << 23);
+}
+/* For at_pieces: 32512 / largest (int8), or to [128, 256). */
 template <int KIND>
 __device__ __forceinline__ void at_row_scale(float most, float& inv, float& scale) {
     if (KIND == BL_KV_INT8) {
         inv = most > 0.0f ? bl_div_rn(32512.0f, most) : 0.0f;
         scale = most * (1.0f / 32512.0f);
     } else {
-        /* 2^e with most * 2^e in [128, 256) */
-        int e = 134 - (int)(__float_as_uint(most) >> 23);
-        e = e > 120 ? 120 : e < -120 ? -120 : e;
-        inv = most > 0.0f ? __uint_as_float((uint32_t)(127 + e) << 23) : 0.0f;
-        scale = __uint_as_float((uint32_t)(127 - e) << 23);
+        at_power_scale(most, 134, inv, scale);
     }
 }
 __device__ __forceinline__ float at_largest(const uint32_t (&w)[8], float most, bool& nan) {
@@ -731,39 +735,55 @@ __device__ __forceinline__ int at_many_tiles(const at_args& A, int b) {
 }
 
 /* A workgroup: 128 rows of one request and kv head, 32 a wave, over a range of its tiles (all that its rows see, or one of
- * `splits` equal pieces).  K codes lie in LDS as they are (16-byte units XOR-ed with the row, so that sixteen lanes of a
- * read fall on all 64 banks), V as fp16, converted once by the thread that loads it; two buffers, one barrier a tile.  Products of 32 tokens x
+ * `splits` equal pieces).  V lies in LDS as fp16, converted once by the thread that
+ * loads it, K as its codes, which the matrix cores multiply with the two pieces of q, or (int8, heads of 64) as fp16 too: the pieces'
+ * products cost two vector instructions a score more, their conversion is one instruction for half a byte, and a third wave fits (8000
+ * tokens, 32 + 8 heads: 417 -> 369 us; heads of 128: 388 -> 401, LDS reads).  16-byte units are XOR-ed with the row, so that sixteen
+ * lanes of a read fall on all 64 banks; two buffers, one barrier a tile.  Products of 32 tokens x
  * 32 rows (S^T) and 32 features x 32 rows (O^T): a lane has one row. */
-template <int D>
+template <int KIND, int D>
+struct at_many_k {                  /* bytes of a K value in LDS */
+    static constexpr int bytes = KIND == BL_KV_INT8 && D == 64 ? 2 : 1;
+};
+template <int KIND, int D>
 struct at_many_lds {
     union {
         uint8_t v[2][D * AT_TILE * 2];
         int upto[BL_KV_MAX_REQUESTS];                       /* at first */
     };
-    uint8_t k[2][AT_TILE * D];
+    uint8_t k[2][AT_TILE * D * at_many_k<KIND, D>::bytes];
     int scan[AT_WAVES];
 };
 template <int KIND, int D>
-__device__ __forceinline__ void at_many(const at_args& A, int place, at_many_lds<D>& lds) {
-    constexpr int CH = D / 16;                              /* 16-byte units of a K row */
+__device__ __forceinline__ void at_many(const at_args& A, int place, at_many_lds<KIND, D>& lds) {
+    constexpr bool HALF = at_many_k<KIND, D>::bytes == 2;
+    constexpr int KROW = D * at_many_k<KIND, D>::bytes;        /* bytes of a K row in LDS, 16-byte units XOR-ed by k_mix(row) */
     constexpr int KS = D / 32, DT = D / 32;
+    auto k_mix = [](int row) { return KROW == 128 ? (row >> 1) & 7 : (row >> 2) & 3; };
     auto& s_k = lds.k;
     auto& s_v = lds.v;
     const int tid = threadIdx.x, lane = tid & 63, wave = at_uniform(tid >> 6);
     const int col = lane & 31, half = lane >> 5;
     /* whose tile: place = (row tile * n_kv + head) * splits + piece, a request's heavy tiles first */
-    const int piece = place % A.splits, h = place / A.splits % A.n_kv, want = place / A.splits / A.n_kv;
-    int b, before, c;
+    int piece, h, want, b, before, c;
+    auto take = [&](int all) {
+        /* Heads of 128: of the 512 workgroups that the chip holds the second 256 go the other way round, so that a unit has a heavy
+         * one and a light one: two prompts of 1600 tokens 72 -> 57 us, one of 6000 244 -> 236 (heads of 64, three to a unit: 52 -> 58). */
+        const int n = all * A.n_kv * A.splits, both = n < 512 ? n : 512;
+        if (D == 128 && place >= 256 && place < both) place = 255 + both - place;
+        piece = place % A.splits, h = place / A.splits % A.n_kv, want = place / A.splits / A.n_kv;
+        return place < n;
+    };
     if (A.B <= 64) {
         const int upto = at_scan(lane < A.B ? at_many_tiles(A, lane) : 0);
-        if (want >= __builtin_amdgcn_readlane(upto, 63)) return;
+        if (!take(__builtin_amdgcn_readlane(upto, 63))) return;
         b = __builtin_ctzll(__ballot(upto > want));
         before = b ? __builtin_amdgcn_readlane(upto, b - 1) : 0;
         c = __builtin_amdgcn_readlane(upto, b) - before;
     } else {
         int* s_upto = lds.upto;
         at_sums(A.B, [&](int i) { return at_many_tiles(A, i); }, s_upto, lds.scan);
-        if (want >= at_uniform(s_upto[A.B - 1])) return;
+        if (!take(at_uniform(s_upto[A.B - 1]))) return;
         int lo = -1, hi = A.B - 1;
         while (hi - lo > 1) {
             const int mid = (lo + hi) >> 1;
@@ -799,6 +819,9 @@ __device__ __forceinline__ void at_many(const at_args& A, int place, at_many_lds
     const bool has_rows = wfirst < rows;
     const int any_from = has_rows ? at_from(A, R, wfirst / A.G) : 0, any_to = has_rows ? at_to(R, wlast / A.G) : 0;
     const int all_from = has_rows ? at_from(A, R, wlast / A.G) : 0, all_to = has_rows ? at_to(R, wfirst / A.G) : 0;
+    /* this lane's part of q: as fp16 (HALF: values d = 16 s + 8 half .. + 7, times a power of two, exact down to 2^-27 of the
+     * row's largest), or as two 8-bit pieces (values d = 32 s + 16 half .. + 15) */
+    at_v8h qf[2 * KS];
     bl_v4i qh[KS], ql[KS];
     float a_row;
     {
@@ -808,19 +831,35 @@ __device__ __forceinline__ void at_many(const at_args& A, int place, at_many_lds
         bool nan = false;
 #pragma unroll
         for (int s = 0; s < KS; ++s) {
-            const at_v4u u0 = *bl_gc<at_v4u>(src + s * 32 + half * 16), u1 = *bl_gc<at_v4u>(src + s * 32 + half * 16 + 8);
+            const at_v4u u0 = *bl_gc<at_v4u>(src + s * 32 + half * (HALF ? 8 : 16)), u1 = *bl_gc<at_v4u>(src + s * 32 + (HALF ? 16 + half * 8 : half * 16 + 8));
 #pragma unroll
             for (int j = 0; j < 4; ++j) w[s][j] = u0[j], w[s][4 + j] = u1[j];
             most = at_largest(w[s], most, nan);
         }
         most = bl_max_pos(most, at_xor(most, 32));
         float inv, scale;
-        at_row_scale<KIND>(most, inv, scale);
+        if (HALF) at_power_scale(most, 137, inv, scale);
+        else at_row_scale<KIND>(most, inv, scale);
         const uint64_t nans = __ballot(nan);
         if (nans && ((nans >> col) & 0x0000000100000001ull)) scale = __uint_as_float(0x7fc00000u);
         a_row = scale * A.factor;
 #pragma unroll
-        for (int s = 0; s < KS; ++s) at_pieces<KIND>(w[s], inv, qh[s], ql[s]);
+        for (int s = 0; s < KS; ++s) {
+            if constexpr (HALF) {
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    at_v4u t;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const uint32_t v = w[s][4 * x + j];
+                        t[j] = at_pack_half(bl_bf16_to_f32(v & 0xffffu) * inv, __uint_as_float(v & 0xffff0000u) * inv);
+                    }
+                    qf[2 * s + x] = __builtin_bit_cast(at_v8h, t);
+                }
+            } else {
+                at_pieces<KIND>(w[s], inv, qh[s], ql[s]);
+            }
+        }
     }
     at_v16f o[DT];
 #pragma unroll
@@ -854,7 +893,7 @@ __device__ __forceinline__ void at_many(const at_args& A, int place, at_many_lds
         const int64_t sc = (int64_t)(there(blocks) ? blocks : 0) * A.scale_stride + h;
         ks_next = A.k_scale[sc], vs_next = A.v_scale[sc];
     };
-    const int k_row = 16 * wave + kt, k_swz = CH == 8 ? (k_row >> 1) & 7 : (k_row >> 2) & 3;
+    const int k_row = 16 * wave + kt, k_swz = k_mix(k_row);
     /* What no token has written may be anything, and a NaN times 0 is none: zeros behind the last token of tile t. */
     auto mend = [&](int t, int blocks) {
         const int n = there(__builtin_amdgcn_readlane(blocks, wave)) ? R.len - t * AT_TILE - 16 * wave : 0;
@@ -865,8 +904,14 @@ __device__ __forceinline__ void at_many(const at_args& A, int place, at_many_lds
     auto store = [&](int buf) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            *(bl_v4i*)&s_k[buf][k_row * D + (((kc + u) ^ k_swz) * 16)] = lk[u];
             at_v8h a, c;
+            if constexpr (HALF) {
+                at_half16<KIND>(lk[u], a, c);
+                *(at_v8h*)&s_k[buf][k_row * KROW + (((2 * (kc + u)) ^ k_swz) * 16)] = a;
+                *(at_v8h*)&s_k[buf][k_row * KROW + (((2 * (kc + u) + 1) ^ k_swz) * 16)] = c;
+            } else {
+                *(bl_v4i*)&s_k[buf][k_row * KROW + (((kc + u) ^ k_swz) * 16)] = lk[u];
+            }
             at_half16<KIND>(lv_[u], a, c);
             const int d = lane + 64 * u;
             *(at_v8h*)&s_v[buf][d * 128 + (((2 * wave) ^ ((d >> 1) & 7)) * 16)] = a;
@@ -887,23 +932,24 @@ __device__ __forceinline__ void at_many(const at_args& A, int place, at_many_lds
     __syncthreads();
     /* row r = 8a + 4f + b of the first product's tile tt is token 32 tt + 16 (a/2) + 8 f + 4 (a%2) + b */
     const int kr = (col >> 4) * 16 + ((col >> 2) & 1) * 8 + ((col >> 3) & 1) * 4 + (col & 3);
-    const int kr_swz = CH == 8 ? (kr >> 1) & 7 : (kr >> 2) & 3;
-    /* One step: the next tile's codes go to LDS and the one's behind it are asked for while the first product runs, its second
-     * half runs over the first half's conversion, and each group's weights are made while the one's before it are multiplied. */
+    const int kr_swz = k_mix(kr);
+    /* One step: the next tile goes to LDS and the one's behind it is asked for while the first product runs, and each group's
+     * weights are made while the one's before it are multiplied. */
     for (int buf = 0; tile < tend; ++tile, buf ^= 1) {
         const int tok = tile * AT_TILE;
         const int blk3 = fetch_blocks(tile + 3);
         mend(tile + 1, blk1);
         if (tok < any_to && tok + AT_TILE > any_from) {
             float sf[2][16];
-            bl_v4i kk[2][KS];
-#pragma unroll
-            for (int tt = 0; tt < 2; ++tt)
-#pragma unroll
-                for (int s = 0; s < KS; ++s) kk[tt][s] = *(const bl_v4i*)&s_k[buf][(tt * 32 + kr) * D + (((2 * s + half) ^ kr_swz) * 16)];
             auto v_part = [&](int g, int i) { return *(const at_v8h*)&s_v[buf][(32 * i + col) * 128 + (((2 * g + half) ^ ((col >> 1) & 7)) * 16)]; };
+            auto k_part = [&](int tt, int i) { return *(const bl_v4i*)&s_k[buf][(tt * 32 + kr) * KROW + (((2 * i + half) ^ kr_swz) * 16)]; };
             at_v8h vv[2][DT];
-            if constexpr (KIND == BL_KV_INT8) {
+            constexpr int UNITS = KROW / 32;                 /* a lane's 16-byte units of a K row */
+            bl_v4i kk[2][UNITS];
+#pragma unroll
+            for (int i = 0; i < UNITS; ++i) kk[0][i] = k_part(0, i), kk[1][i] = k_part(1, i);
+            if constexpr (KIND == BL_KV_INT8 && !HALF) {
+                /* the second half's products run over the first half's conversion */
                 bl_v16i sh[2], sl[2];
 #pragma unroll
                 for (int j = 0; j < 16; ++j) sh[0][j] = sl[0][j] = sh[1][j] = sl[1][j] = 0;
@@ -944,23 +990,31 @@ __device__ __forceinline__ void at_many(const at_args& A, int place, at_many_lds
                 at_v16f s16[2];
 #pragma unroll
                 for (int j = 0; j < 16; ++j) s16[0][j] = s16[1][j] = 0.0f;
+                constexpr int STEPS = HALF ? 2 * KS : KS / 2, EACH = HALF ? 2 : 4;      /* k steps, products of one */
 #pragma unroll
-                for (int s = 0; s < KS; s += 2)
+                for (int s = 0; s < STEPS; ++s) {
+                    if constexpr (HALF) {
 #pragma unroll
-                    for (int u = 0; u < 4; ++u) {
-                        at_v8i ka, qa;
+                        for (int u = 0; u < 2; ++u) s16[u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(at_v8h, kk[u][s]), qf[s], s16[u], 0, 0, 0);
+                    } else {
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) ka[j] = kk[u & 1][s + j / 4][j % 4], qa[j] = u < 2 ? qh[s + j / 4][j % 4] : ql[s + j / 4][j % 4];
-                        s16[u & 1] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(ka, qa, s16[u & 1], 0, 0, 0, 0, 0, 0);
+                        for (int u = 0; u < 4; ++u) {
+                            at_v8i ka, qa;
+#pragma unroll
+                            for (int j = 0; j < 8; ++j)
+                                ka[j] = kk[u & 1][2 * s + j / 4][j % 4], qa[j] = u < 2 ? qh[2 * s + j / 4][j % 4] : ql[2 * s + j / 4][j % 4];
+                            s16[u & 1] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(ka, qa, s16[u & 1], 0, 0, 0, 0, 0, 0);
+                        }
                     }
+                }
                 store(buf ^ 1);
                 load(tile + 2, blk2);
 #pragma unroll
                 for (int i = 0; i < DT; ++i) vv[0][i] = v_part(0, i);
 #pragma unroll
-                for (int s = 0; s < 2 * KS; ++s) {
+                for (int s = 0; s < STEPS * EACH; ++s) {
                     __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-                    __builtin_amdgcn_sched_group_barrier(0x002, D / 16, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x002, HALF ? 6 : D / 16, 0);
                 }
                 bl_mfma_fence();
 #pragma unroll
@@ -1127,7 +1181,7 @@ __global__ __launch_bounds__(AT_THREADS, 2) void bl_attn_few(at_args A) {
 /* One request, or groups of more heads than at_few has rows: at_many alone. */
 template <int KIND, int D>
 __global__ __launch_bounds__(AT_THREADS, 2) void bl_attn_many(at_args A) {
-    __shared__ __attribute__((aligned(16))) at_many_lds<D> lds;
+    __shared__ __attribute__((aligned(16))) at_many_lds<KIND, D> lds;
     at_many<KIND, D>(A, (int)blockIdx.x, lds);
 }
 /* Any batch, in one launch: the matrix cores' work first; what streams the cache fills the units as that ends. */
@@ -1135,7 +1189,7 @@ template <int KIND, int D, bool WIDE>
 __global__ __launch_bounds__(AT_THREADS, 2) void bl_attn_any(at_args A, int many) {
     union lds_t {
         at_few_lds<D> few;
-        at_many_lds<D> many;
+        at_many_lds<KIND, D> many;
     };
     __shared__ __attribute__((aligned(16))) uint8_t lds[sizeof(lds_t)];
     if ((int)blockIdx.x < many) at_many<KIND, D>(A, (int)blockIdx.x, ((lds_t*)lds)->many);
