@@ -233,7 +233,10 @@ struct at_slot {                    /* a wave's partial result: rows x (D sums, 
  * (at_together) are taken tile by tile in turn instead, and meet in LDS: a quarter of the partial results.
  * K rows of a tile go straight from memory into the registers that the matrix cores read (four 16 x 128 products of
  * codes against the two pieces of q), then V the same way.  V of a tile and K of the next are in flight while one computes,
- * and the block numbers of the one behind: also across the items of a piece. */
+ * and the block numbers of the one behind: also across the items of a piece.
+ * Bound by the cache's stream: 64 requests over 8192 tokens, 241 MB, 46 us = 5.2 TB/s; two over 131071, 513 MB, 97 us = 5.3 (a read that
+ * does nothing else 7.0; what is fetched is what the codes take).  About 5 us are the chain lengths -> blocks -> codes and
+ * the last waves.  The codes' conversion and the softmax are 460 vector instructions a tile: a third of what its 16 KB allow. */
 /* Whether workgroup g's four pieces, whole ones, lie in the item of tiles first .. last of the line. */
 __device__ __forceinline__ bool at_together(int g, int share, int first, int last) {
     return (int64_t)g * AT_WAVES * share >= first && (int64_t)(g + 1) * AT_WAVES * share - 1 <= last;
@@ -599,7 +602,8 @@ __device__ __forceinline__ void at_few(const at_args& A, int group, at_few_lds<D
 /* Adds up what several waves of at_few have of one item: of the item that the boundary between waves edge - 1 and edge cuts,
  * where no earlier boundary does.  A workgroup has AT_WAVES boundaries and the rows turn, turn + turns, ...  D / 4 threads
  * (a group) a partial result of a row.  The wave of the boundary does it, a row a group; where there are
- * more than AT_JOIN_ALONE the groups of all waves share those of a row and meet in LDS. */
+ * more than AT_JOIN_ALONE the groups of all waves share those of a row and meet in LDS.  5 to 9 us: a kernel boundary and
+ * two dependent reads of what other dies have just written. */
 #define AT_JOIN_ALONE 32
 struct at_cut {
     int row0, rows, h, first, w0, head, ga, inner, g1, parts;   /* pieces w0 .. of `head` waves, of `inner` workgroups from ga, of waves from 4 g1 */
@@ -739,7 +743,10 @@ __device__ __forceinline__ int at_many_tiles(const at_args& A, int b) {
  * loads it, K as its codes, which the matrix cores multiply with the two pieces of q, or (int8, heads of 64) as fp16 too: the pieces'
  * products cost two vector instructions a score more, their conversion is one instruction for half a byte, and a third wave fits (8000
  * tokens, 32 + 8 heads: 417 -> 369 us; heads of 128: 388 -> 401, LDS reads).  16-byte units are XOR-ed with the row, so that sixteen
- * lanes of a read fall on all 64 banks; two buffers, one barrier a tile.  Products of 32 tokens x
+ * lanes of a read fall on all 64 banks; two buffers, one barrier a tile.
+ * Bound by vector instructions (376 a wave and tile beside 1024 matrix clocks; vector units busy 52 % of the time, matrix cores
+ * 32 %) where the workgroups are many: 8000 tokens of 20 + 5 heads of 128 845 TFLOP/s, e4m3 925 (a library bf16 product of 8192^3: 1224).  A prompt of
+ * 4096: 120 us = 717, where the last rows' 64 tiles one after the other are all of it; cutting them in two took 145 us (the halves' 42 MB).  Products of 32 tokens x
  * 32 rows (S^T) and 32 features x 32 rows (O^T): a lane has one row. */
 template <int KIND, int D>
 struct at_many_k {                  /* bytes of a K value in LDS */
