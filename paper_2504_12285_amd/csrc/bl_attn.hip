@@ -231,6 +231,7 @@ struct at_slot {                    /* a wave's partial result: rows x (D sums, 
  * piece may end one head's tiles and begin the next's.  What a piece has of an item that others share goes to the
  * workspace (at most two such: at its ends) and bl_attn_join adds it up.  The four pieces of a workgroup that lie in one item
  * (at_together) are taken tile by tile in turn instead, and meet in LDS: a quarter of the partial results.
+ * ITEM: a workgroup has one item whole, so that nothing is left to join (short contexts).
  * K rows of a tile go straight from memory into the registers that the matrix cores read (four 16 x 128 products of
  * codes against the two pieces of q), then V the same way.  V of a tile and K of the next are in flight while one computes,
  * and the block numbers of the one behind: also across the items of a piece.
@@ -254,42 +255,23 @@ struct at_few_lds {
 struct at_spot {
     int b, h, t, c, tile0;          /* request, kv head, tile of c, first tile */
 };
-template <int KIND, int D, bool WIDE>
+template <int KIND, int D, bool WIDE, bool ITEM>
 __device__ __forceinline__ void at_few(const at_args& A, int group, at_few_lds<D>& lds) {
     constexpr int KS = D / 64, DT = D / 16;                 /* 64-byte steps of a K row, 16-feature tiles of V */
     const int tid = threadIdx.x, lane = tid & 63, wave = at_uniform(tid >> 6);
     const int col = lane & 15, grp = lane >> 4;
-    /* where each request's tiles end: up to 64 requests by every wave for itself, a lane each, more through LDS */
-    const bool small = A.B <= 64;
-    int upto = 0;
+    at_spot cur, next, after;                                /* the tile computed, the one loaded, the one whose blocks are read */
+    int upto = 0, all = 0, share = 1, stream = group * AT_WAVES, count, begun0 = 0;
+    bool together = true, small = true, alone = true;       /* the waves take one item's tiles in turn; have all of it */
     at_request mine = {0, 0, 0};
-    int4* const heads = (int4*)A.part;                       /* bl_attn_join reads them there: tiles up to it, first row, queries */
-    if (small) {
-        if (lane < A.B) {
-            mine = at_read(A, lane);
-            upto = at_few_tiles(A, mine);
-        }
-        upto = at_scan(upto);
-        if (group == 0 && tid < A.B) heads[tid] = make_int4(upto, mine.row0, mine.n, 0);
-    } else {
-        at_sums(A.B, [&](int b) { return at_few_tiles(A, at_read(A, b)); }, lds.upto, lds.scan);
-        for (int b = tid; b < A.B; b += AT_THREADS) {
-            const at_request r = at_read(A, b);
-            lds.request[b] = make_int2(r.row0 << 5 | (r.n < 31 ? r.n : 31), r.len);
-            if (group == 0) heads[b] = make_int4(lds.upto[b], r.row0, r.n, 0);
-        }
-        __syncthreads();
-    }
     auto upto_of = [&](int b) { return small ? __builtin_amdgcn_readlane(upto, b) : at_uniform(lds.upto[b]); };
     auto request = [&](int b) -> at_request {
+        if (ITEM) return mine;
         if (small) return {__builtin_amdgcn_readlane(mine.row0, b), __builtin_amdgcn_readlane(mine.n, b), __builtin_amdgcn_readlane(mine.len, b)};
         const int2 r = lds.request[b];
         const int x = at_uniform(r.x);
         return {x >> 5, x & 31, at_uniform(r.y)};
     };
-    const int all = upto_of(small ? 63 : A.B - 1) * A.n_kv, share = at_share(all);
-    int stream = group * AT_WAVES;
-    if ((int64_t)stream * share >= all) return;
     /* the request that has tile `at` of the line (of one kv head) */
     auto find = [&](int at, at_spot& s) -> int {
         if (small) {
@@ -307,27 +289,57 @@ __device__ __forceinline__ void at_few(const at_args& A, int group, at_few_lds<D
         s.c = upto_of(s.b) - before, s.tile0 = at_from(A, request(s.b), 0) / AT_TILE;
         return before;
     };
-    at_spot cur, next, after;                                /* the tile computed, the one loaded, the one whose blocks are read */
     auto go_to = [&](int x) {
         const int before = find(x / A.n_kv, cur) * A.n_kv, r = x - before;
         cur.h = r / cur.c, cur.t = r % cur.c;
         return before + cur.h * cur.c;
     };
-    int count = share;
-    const int first = go_to(stream * share);
-    const bool together = at_together(group, share, first, first + cur.c - 1);
-    const int begun0 = cur.t;
-    if (together) {
-        cur.t += wave;
+    if constexpr (ITEM) {
+        cur.b = group / A.n_kv, cur.h = group % A.n_kv;
+        mine = at_read(A, cur.b);
+        mine = {at_uniform(mine.row0), at_uniform(mine.n), at_uniform(mine.len)};
+        cur.c = at_few_tiles(A, mine), cur.t = wave;
+        if (!cur.c) return;
+        cur.tile0 = at_from(A, mine, 0) / AT_TILE;
+        count = (cur.c - wave + AT_WAVES - 1) / AT_WAVES;     /* (none for some waves of a short item: they bring nothing to the meeting) */
     } else {
-        stream += wave;
-        const int64_t x0 = (int64_t)stream * share;
-        if (x0 >= all) return;
-        if (wave) go_to((int)x0);
-        if (count > all - (int)x0) count = all - (int)x0;
+        /* where each request's tiles end: up to 64 requests by every wave for itself, a lane each, more through LDS */
+        small = A.B <= 64;
+        int4* const heads = (int4*)A.part;                   /* bl_attn_join reads them there: tiles up to it, first row, queries */
+        if (small) {
+            if (lane < A.B) {
+                mine = at_read(A, lane);
+                upto = at_few_tiles(A, mine);
+            }
+            upto = at_scan(upto);
+            if (group == 0 && tid < A.B) heads[tid] = make_int4(upto, mine.row0, mine.n, 0);
+        } else {
+            at_sums(A.B, [&](int b) { return at_few_tiles(A, at_read(A, b)); }, lds.upto, lds.scan);
+            for (int b = tid; b < A.B; b += AT_THREADS) {
+                const at_request r = at_read(A, b);
+                lds.request[b] = make_int2(r.row0 << 5 | (r.n < 31 ? r.n : 31), r.len);
+                if (group == 0) heads[b] = make_int4(lds.upto[b], r.row0, r.n, 0);
+            }
+            __syncthreads();
+        }
+        all = upto_of(small ? 63 : A.B - 1) * A.n_kv, share = at_share(all);
+        if ((int64_t)stream * share >= all) return;
+        count = share;
+        const int first = go_to(stream * share);
+        together = at_together(group, share, first, first + cur.c - 1);
+        begun0 = cur.t, alone = cur.c == share * AT_WAVES;
+        if (together) {
+            cur.t += wave;
+        } else {
+            stream += wave;
+            const int64_t x0 = (int64_t)stream * share;
+            if (x0 >= all) return;
+            if (wave) go_to((int)x0);
+            if (count > all - (int)x0) count = all - (int)x0;
+        }
     }
     auto advance = [&](at_spot s) -> at_spot {
-        if (together) {
+        if (ITEM || together) {
             s.t += AT_WAVES;
         } else if (++s.t == s.c) {
             s.t = 0;
@@ -464,7 +476,7 @@ __device__ __forceinline__ void at_few(const at_args& A, int group, at_few_lds<D
         /* what the next tile needs, while this one computes */
         const float ks0 = ks, vs0 = vs;
         const int pv_next = next_blocks.v;
-        const bool turns = !together && cur.t + 1 == cur.c;  /* the item ends here, and this wave goes on with the next */
+        const bool turns = !ITEM && !together && cur.t + 1 == cur.c;  /* the item ends here, and this wave goes on with the next */
         if (left > 1) {
             load_k(next, next_blocks.k, k);
             const int64_t at = (int64_t)place(pv_next) * A.scale_stride + next.h;
@@ -529,7 +541,7 @@ __device__ __forceinline__ void at_few(const at_args& A, int group, at_few_lds<D
             o[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, __builtin_bit_cast(at_v8h, p0), o[i], 0, 0, 0);
             o[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, __builtin_bit_cast(at_v8h, p1), o[i], 0, 0, 0);
         }
-        if (turns || (left == 1 && !together)) {
+        if (turns || (!ITEM && left == 1 && !together)) {
             bl_mfma_fence();
             l += at_xor(l, 16);
             l += at_xor(l, 32);
@@ -560,7 +572,7 @@ __device__ __forceinline__ void at_few(const at_args& A, int group, at_few_lds<D
         next = after, pv = pv_next;
         if (left > 3) after = advance(after);
     }
-    if (!together) return;
+    if (!ITEM && !together) return;
     at_meet_lds<D>& meet = *(at_meet_lds<D>*)&lds;
     bl_mfma_fence();
     l += at_xor(l, 16);
@@ -586,7 +598,7 @@ __device__ __forceinline__ void at_few(const at_args& A, int group, at_few_lds<D
 #pragma unroll
         for (int j = 0; j < PER; ++j) y[j] += meet.o[w][r][d0 + j] * f;
     }
-    if (cur.c == share * AT_WAVES) {                         /* all of the item */
+    if (ITEM || alone) {
         const float inv = sum == 0.0f ? 0.0f : bl_div_rn(1.0f, sum);
         uint32_t* to = (uint32_t*)(A.out + (R.row0 + r / A.G) * A.out_stride + (cur.h * A.G + r % A.G) * D + d0);
 #pragma unroll
@@ -1180,10 +1192,10 @@ __device__ __forceinline__ void at_many_join(const at_args& A, int group) {
 /* ---- launches ---------------------------------------------------------------------------------------------------------- */
 
 /* A batch without long runs of rows: at_few alone. */
-template <int KIND, int D, bool WIDE>
+template <int KIND, int D, bool WIDE, bool ITEM>
 __global__ __launch_bounds__(AT_THREADS, 2) void bl_attn_few(at_args A) {
     __shared__ __attribute__((aligned(16))) at_few_lds<D> lds;
-    at_few<KIND, D, WIDE>(A, (int)blockIdx.x, lds);
+    at_few<KIND, D, WIDE, ITEM>(A, (int)blockIdx.x, lds);
 }
 /* One request, or groups of more heads than at_few has rows: at_many alone. */
 template <int KIND, int D>
@@ -1200,7 +1212,7 @@ __global__ __launch_bounds__(AT_THREADS, 2) void bl_attn_any(at_args A, int many
     };
     __shared__ __attribute__((aligned(16))) uint8_t lds[sizeof(lds_t)];
     if ((int)blockIdx.x < many) at_many<KIND, D>(A, (int)blockIdx.x, ((lds_t*)lds)->many);
-    else at_few<KIND, D, WIDE>(A, (int)blockIdx.x - many, ((lds_t*)lds)->few);
+    else at_few<KIND, D, WIDE, false>(A, (int)blockIdx.x - many, ((lds_t*)lds)->few);
 }
 /* Partial results of both: `few` workgroups for those of at_few, turns x AT_STREAM_GROUPS, the others for a split. */
 template <int D, bool MANY>
@@ -1216,6 +1228,7 @@ __global__ __launch_bounds__(AT_THREADS) void bl_attn_join(at_args A, int few) {
 
 struct at_plan {
     bool few, many;
+    int items;                     /* workgroups, an item each; 0: streams */
     int splits, row_tiles, skip, rows;
     size_t few_bytes, bytes;
 };
@@ -1243,6 +1256,11 @@ static at_plan at_make_plan(const bl_attn_desc* a) {
     const int64_t rows = (int64_t)(a->max_q < a->T ? a->max_q : a->T) * G;
     p.many = rows > AT_FEW;
     p.few = G <= AT_FEW && !(p.many && a->B == 1);            /* (one request: of one kind or the other) */
+    /* An item a workgroup, without a join, while its tokens are few, twice as many where there are items for every unit: one request of 512
+     * tokens 7.8 us against 11.5 as streams, of 1500 14.7 against 11.8; 256 requests (spread 4) of 2048 75 against 78, of 4096 140
+     * against 136 (heads of 128; of 64: 1024 7.7 and 10.2, 2048 11.5 and 10.0). */
+    const int64_t tokens = a->max_len > 0 ? a->max_len : (int64_t)a->max_blocks * a->cache.block, items = a->B * a->cache.n_kv;
+    p.items = !p.many && tokens <= (D == 128 ? 1024 : 1280) * (items >= 1024 ? 2 : 1) ? (int)items : 0;
     const int64_t part = a->T < a->B ? a->T : a->B;           /* requests with rows */
     p.row_tiles = (int)(a->T * G / AT_MANY + part);
     p.splits = 1;
@@ -1277,7 +1295,11 @@ static void at_launch(at_args A, const at_plan& p, const bl_attn_desc* a, hipStr
         if (few) bl_attn_any<KIND, D, WIDE><<<(unsigned)(many + few), AT_THREADS, 0, st>>>(A, many);
         else bl_attn_many<KIND, D><<<(unsigned)many, AT_THREADS, 0, st>>>(A);
     } else {
-        bl_attn_few<KIND, D, WIDE><<<(unsigned)few, AT_THREADS, 0, st>>>(A);
+        if (p.items) {
+            bl_attn_few<KIND, D, WIDE, true><<<(unsigned)p.items, AT_THREADS, 0, st>>>(A);
+            return;
+        }
+        bl_attn_few<KIND, D, WIDE, false><<<(unsigned)few, AT_THREADS, 0, st>>>(A);
     }
     const int64_t rows = (int64_t)A.T * A.n_q, per = AT_THREADS / (D / 4);
     const int few_join = p.few ? AT_STREAM_GROUPS * ((p.rows + 256 / D - 1) / (256 / D)) : 0;      /* (D / 4 lanes a row of a wave) */

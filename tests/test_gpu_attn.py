@@ -143,6 +143,19 @@ def test_prompts(kind, block, heads):
 
 
 @pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("max_len", [100, 1000000])
+@pytest.mark.parametrize("heads, block, window", [((20, 5, 128), 64, 0), ((8, 8, 64), 16, 0), ((6, 2, 64), 128, 70), ((16, 1, 128), 32, 300)])
+def test_every_hint_of_the_length_gives_the_same_rows(kind, max_len, heads, block, window):
+    """A small hint gives every request and head a workgroup of its own, a large one splits them all over the chip; what the
+    lengths are does not matter to either."""
+    G = heads[0] // heads[1]
+    reqs = [(t, min(t, 1 + i % (16 // G))) for i, t in enumerate(LENGTHS + [5000])]
+    Batch(reqs, heads, block, kind, seed=max_len % 7).check(max_len=max_len, window=window)
+    many = [(1 + 13 * i % 200, i % 4 and 1) for i in range(400)]
+    Batch(many, heads, block, kind, seed=3).check(max_len=max_len, window=window, rows=range(0, 400, 37))
+
+
+@pytest.mark.parametrize("kind", KINDS)
 def test_a_long_prompt_and_chunks(kind):
     Batch([(1500, 1500)], (4, 1, 128), 64, kind).check()
     Batch([(3000, 130), (2000, 600), (1999, 1), (10, 10)], (8, 2, 64), 32, kind).check()
