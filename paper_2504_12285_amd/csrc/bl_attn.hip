@@ -1256,10 +1256,15 @@ static at_plan at_make_plan(const bl_attn_desc* a) {
     const int64_t rows = (int64_t)(a->max_q < a->T ? a->max_q : a->T) * G;
     p.many = rows > AT_FEW;
     p.few = G <= AT_FEW && !(p.many && a->B == 1);            /* (one request: of one kind or the other) */
+    /* Tokens that the rows of a workgroup see (the length alone under a window of 1000, 16 requests of 4 queries over 8000: 23.5 us, so 12.5;
+     * 64 queries, a window of 500: 22.5 and 19.7). */
+    int64_t tokens = a->max_len > 0 ? a->max_len : (int64_t)a->max_blocks * a->cache.block;
+    const int64_t wide = (int64_t)a->window + (a->max_q < AT_MANY ? a->max_q : AT_MANY);
+    if (a->window && tokens > wide) tokens = wide;
     /* An item a workgroup, without a join, while its tokens are few, twice as many where there are items for every unit: one request of 512
      * tokens 7.8 us against 11.5 as streams, of 1500 14.7 against 11.8; 256 requests (spread 4) of 2048 75 against 78, of 4096 140
      * against 136 (heads of 128; of 64: 1024 7.7 and 10.2, 2048 11.5 and 10.0). */
-    const int64_t tokens = a->max_len > 0 ? a->max_len : (int64_t)a->max_blocks * a->cache.block, items = a->B * a->cache.n_kv;
+    const int64_t items = a->B * a->cache.n_kv;
     p.items = !p.many && tokens <= (D == 128 ? 1024 : 1280) * (items >= 1024 ? 2 : 1) ? (int)items : 0;
     const int64_t part = a->T < a->B ? a->T : a->B;           /* requests with rows */
     p.row_tiles = (int)(a->T * G / AT_MANY + part);
@@ -1268,9 +1273,8 @@ static at_plan at_make_plan(const bl_attn_desc* a) {
         /* pieces until the workgroups fill the chip twice over, of four tiles at least (64 queries over 1000 tokens: of eight 33.5 us, of four
          * 19.9, of two 17.4; over 4000: 27.1, 23.1 and 27.1) */
         const int64_t items = (int64_t)((a->T * G + AT_MANY - 1) / AT_MANY) * a->cache.n_kv;
-        const int64_t len = a->max_len > 0 ? a->max_len : (int64_t)a->max_blocks * a->cache.block;
         int64_t s = items < 512 ? 512 / items : 1;
-        const int64_t by_len = len / (4 * AT_TILE);
+        const int64_t by_len = tokens / (4 * AT_TILE);
         s = s > by_len ? by_len : s;
         p.splits = s < 1 ? 1 : s > 64 ? 64 : (int)s;
     }
