@@ -231,7 +231,7 @@ struct at_slot {                    /* a wave's partial result: rows x (D sums, 
  * piece may end one head's tiles and begin the next's.  What a piece has of an item that others share goes to the
  * workspace (at most two such: at its ends) and bl_attn_join adds it up.  The four pieces of a workgroup that lie in one item
  * (at_together) are taken tile by tile in turn instead, and meet in LDS: a quarter of the partial results.
- * ITEM: a workgroup has one item whole, so that nothing is left to join (short contexts).
+ * ITEM (0, or the waves of a workgroup): a workgroup has one item whole, so that nothing is left to join (short contexts).
  * K rows of a tile go straight from memory into the registers that the matrix cores read (four 16 x 128 products of
  * codes against the two pieces of q), then V the same way.  V of a tile and K of the next are in flight while one computes,
  * and the block numbers of the one behind: also across the items of a piece.
@@ -242,9 +242,9 @@ struct at_slot {                    /* a wave's partial result: rows x (D sums, 
 __device__ __forceinline__ bool at_together(int g, int share, int first, int last) {
     return (int64_t)g * AT_WAVES * share >= first && (int64_t)(g + 1) * AT_WAVES * share - 1 <= last;
 }
-template <int D>
+template <int D, int WAVES>
 struct at_meet_lds {                /* the waves' shares of one item */
-    float o[AT_WAVES][AT_FEW][D + 4], m[AT_WAVES][AT_FEW], l[AT_WAVES][AT_FEW];
+    float o[WAVES][AT_FEW][D + 4], m[WAVES][AT_FEW], l[WAVES][AT_FEW];
 };
 template <int D>
 struct at_few_lds {
@@ -252,12 +252,18 @@ struct at_few_lds {
     int2 request[BL_KV_MAX_REQUESTS];                        /* first row * 32 + queries (31: 31 or more, not at_few's), tokens */
     int scan[AT_WAVES];
 };
+template <int D>
+union at_stream_lds {
+    at_few_lds<D> few;
+    at_meet_lds<D, AT_WAVES> meet;
+};
 struct at_spot {
     int b, h, t, c, tile0;          /* request, kv head, tile of c, first tile */
 };
-template <int KIND, int D, bool WIDE, bool ITEM>
-__device__ __forceinline__ void at_few(const at_args& A, int group, at_few_lds<D>& lds) {
-    constexpr int KS = D / 64, DT = D / 16;                 /* 64-byte steps of a K row, 16-feature tiles of V */
+template <int KIND, int D, bool WIDE, int ITEM>
+__device__ __forceinline__ void at_few(const at_args& A, int group, uint8_t* lds_bytes) {
+    constexpr int KS = D / 64, DT = D / 16, WAVES = ITEM ? ITEM : AT_WAVES;     /* 64-byte steps of a K row, 16-feature tiles of V */
+    at_few_lds<D>& lds = *(at_few_lds<D>*)lds_bytes;
     const int tid = threadIdx.x, lane = tid & 63, wave = at_uniform(tid >> 6);
     const int col = lane & 15, grp = lane >> 4;
     at_spot cur, next, after;                                /* the tile computed, the one loaded, the one whose blocks are read */
@@ -301,7 +307,7 @@ __device__ __forceinline__ void at_few(const at_args& A, int group, at_few_lds<D
         cur.c = at_few_tiles(A, mine), cur.t = wave;
         if (!cur.c) return;
         cur.tile0 = at_from(A, mine, 0) / AT_TILE;
-        count = (cur.c - wave + AT_WAVES - 1) / AT_WAVES;     /* (none for some waves of a short item: they bring nothing to the meeting) */
+        count = (cur.c - wave + WAVES - 1) / WAVES;     /* (none for some waves of a short item: they bring nothing to the meeting) */
     } else {
         /* where each request's tiles end: up to 64 requests by every wave for itself, a lane each, more through LDS */
         small = A.B <= 64;
@@ -340,7 +346,7 @@ __device__ __forceinline__ void at_few(const at_args& A, int group, at_few_lds<D
     }
     auto advance = [&](at_spot s) -> at_spot {
         if (ITEM || together) {
-            s.t += AT_WAVES;
+            s.t += WAVES;
         } else if (++s.t == s.c) {
             s.t = 0;
             if (++s.h == A.n_kv) {
@@ -573,7 +579,7 @@ __device__ __forceinline__ void at_few(const at_args& A, int group, at_few_lds<D
         if (left > 3) after = advance(after);
     }
     if (!ITEM && !together) return;
-    at_meet_lds<D>& meet = *(at_meet_lds<D>*)&lds;
+    at_meet_lds<D, WAVES>& meet = *(at_meet_lds<D, WAVES>*)lds_bytes;
     bl_mfma_fence();
     l += at_xor(l, 16);
     l += at_xor(l, 32);
@@ -588,11 +594,11 @@ __device__ __forceinline__ void at_few(const at_args& A, int group, at_few_lds<D
     if (r >= R.n * A.G) return;
     float top = -INFINITY, sum = 0.0f, y[PER];
 #pragma unroll
-    for (int w = 0; w < AT_WAVES; ++w) top = fmaxf(top, meet.m[w][r]);
+    for (int w = 0; w < WAVES; ++w) top = fmaxf(top, meet.m[w][r]);
 #pragma unroll
     for (int j = 0; j < PER; ++j) y[j] = 0.0f;
 #pragma unroll
-    for (int w = 0; w < AT_WAVES; ++w) {
+    for (int w = 0; w < WAVES; ++w) {
         const float f = meet.m[w][r] == top ? 1.0f : __builtin_amdgcn_exp2f(meet.m[w][r] - top);
         sum += meet.l[w][r] * f;
 #pragma unroll
@@ -1192,9 +1198,10 @@ __device__ __forceinline__ void at_many_join(const at_args& A, int group) {
 /* ---- launches ---------------------------------------------------------------------------------------------------------- */
 
 /* A batch without long runs of rows: at_few alone. */
-template <int KIND, int D, bool WIDE, bool ITEM>
-__global__ __launch_bounds__(AT_THREADS, 2) void bl_attn_few(at_args A) {
-    __shared__ __attribute__((aligned(16))) at_few_lds<D> lds;
+template <int KIND, int D, bool WIDE, int ITEM>
+__global__ __launch_bounds__(ITEM ? ITEM * BL_WAVE : AT_THREADS, 2) void bl_attn_few(at_args A) {
+    constexpr size_t bytes = ITEM ? sizeof(at_meet_lds<D, ITEM ? ITEM : 1>) : sizeof(at_stream_lds<D>);
+    __shared__ __attribute__((aligned(16))) uint8_t lds[bytes];
     at_few<KIND, D, WIDE, ITEM>(A, (int)blockIdx.x, lds);
 }
 /* One request, or groups of more heads than at_few has rows: at_many alone. */
@@ -1207,12 +1214,12 @@ __global__ __launch_bounds__(AT_THREADS, 2) void bl_attn_many(at_args A) {
 template <int KIND, int D, bool WIDE>
 __global__ __launch_bounds__(AT_THREADS, 2) void bl_attn_any(at_args A, int many) {
     union lds_t {
-        at_few_lds<D> few;
+        at_stream_lds<D> few;
         at_many_lds<KIND, D> many;
     };
     __shared__ __attribute__((aligned(16))) uint8_t lds[sizeof(lds_t)];
     if ((int)blockIdx.x < many) at_many<KIND, D>(A, (int)blockIdx.x, ((lds_t*)lds)->many);
-    else at_few<KIND, D, WIDE, false>(A, (int)blockIdx.x - many, ((lds_t*)lds)->few);
+    else at_few<KIND, D, WIDE, 0>(A, (int)blockIdx.x - many, lds);
 }
 /* Partial results of both: `few` workgroups for those of at_few, turns x AT_STREAM_GROUPS, the others for a split. */
 template <int D, bool MANY>
@@ -1261,11 +1268,16 @@ static at_plan at_make_plan(const bl_attn_desc* a) {
     int64_t tokens = a->max_len > 0 ? a->max_len : (int64_t)a->max_blocks * a->cache.block;
     const int64_t wide = (int64_t)a->window + (a->max_q < AT_MANY ? a->max_q : AT_MANY);
     if (a->window && tokens > wide) tokens = wide;
-    /* An item a workgroup, without a join, while its tokens are few, twice as many where there are items for every unit: one request of 512
-     * tokens 7.8 us against 11.5 as streams, of 1500 14.7 against 11.8; 256 requests (spread 4) of 2048 75 against 78, of 4096 140
-     * against 136 (heads of 128; of 64: 1024 7.7 and 10.2, 2048 11.5 and 10.0). */
+    /* An item a workgroup, without a join, while its tokens are few, more where there are items for every unit.  Time in us as items and as
+     * streams, equal lengths / spread over a quarter to the whole:
+     * heads of 128: 5 items (of one request) of 512 tokens 8 and 11, 1024 11 and 11, 2048 18 and 11; 160 of 1500 17 and 21 / 16 and 20;
+     *   320 of 1500 32 and 32 / 26 and 27, of 2048 41 and 37 / 34 and 28; 1280 of 2048 106 and 120 / 74 and 79, of 4096 140 and 136;
+     * heads of 64: 8 of 1024 7.7 and 11.8, 2048 10 and 11.5, 4096 16 and 12; 128 of 4096 17.2 and 19.4 / 16.5 and 17.1; 1024 of 4096 83 and 89 / 54 and 58.
+     * Heads of 64 where there is an item a unit at most: eight waves, which have more loads on their way (128 of 2048 13.0 -> 11.0; 512 of 512 12.8 -> 14.6).
+     * Heads of 128 gain nothing from them (18 -> 19.5): four lanes that stand together read four lines of K, and a unit takes a line a clock. */
     const int64_t items = a->B * a->cache.n_kv;
-    p.items = !p.many && tokens <= (D == 128 ? 1024 : 1280) * (items >= 1024 ? 2 : 1) ? (int)items : 0;
+    const int64_t most = D == 128 ? items >= 1024 ? 2048 : items >= 128 ? 1536 : 1024 : items >= 128 ? 4096 : 2048;
+    p.items = !p.many && tokens <= most ? (int)items : 0;
     const int64_t part = a->T < a->B ? a->T : a->B;           /* requests with rows */
     p.row_tiles = (int)(a->T * G / AT_MANY + part);
     p.splits = 1;
@@ -1300,10 +1312,11 @@ static void at_launch(at_args A, const at_plan& p, const bl_attn_desc* a, hipStr
         else bl_attn_many<KIND, D><<<(unsigned)many, AT_THREADS, 0, st>>>(A);
     } else {
         if (p.items) {
-            bl_attn_few<KIND, D, WIDE, true><<<(unsigned)p.items, AT_THREADS, 0, st>>>(A);
+            if (D == 64 && p.items <= 256) bl_attn_few<KIND, D, WIDE, D == 64 ? 8 : 4><<<(unsigned)p.items, 8 * BL_WAVE, 0, st>>>(A);
+            else bl_attn_few<KIND, D, WIDE, 4><<<(unsigned)p.items, 4 * BL_WAVE, 0, st>>>(A);
             return;
         }
-        bl_attn_few<KIND, D, WIDE, false><<<(unsigned)few, AT_THREADS, 0, st>>>(A);
+        bl_attn_few<KIND, D, WIDE, 0><<<(unsigned)few, AT_THREADS, 0, st>>>(A);
     }
     const int64_t rows = (int64_t)A.T * A.n_q, per = AT_THREADS / (D / 4);
     const int few_join = p.few ? AT_STREAM_GROUPS * ((p.rows + 256 / D - 1) / (256 / D)) : 0;      /* (D / 4 lanes a row of a wave) */

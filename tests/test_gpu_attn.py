@@ -386,3 +386,75 @@ def test_captured_and_on_another_stream():
         eager = b.handle()
         eager.run()
         assert torch.equal(eager.out, h.out)
+
+
+FAR = 1000000                       # as a hint of the length: nothing is short enough for a workgroup of its own
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("heads, block", [((20, 5, 128), 64), ((8, 2, 128), 128), ((8, 2, 64), 16), ((16, 1, 64), 128)])
+def test_wide_windows(kind, heads, block):
+    """Windows that leave too much for a workgroup of its own, between others of every length."""
+    reqs = [(5000, 1), (64, 1), (9000, 2), (0, 0), (6000, 1), (17, 1), (2500, 2), (4097, 1)]
+    for window in (1100, 2300, 4500):
+        Batch(reqs, heads, block, kind, seed=window).check(window=window, max_len=FAR)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("heads", [(8, 8, 64), (4, 2, 64), (10, 5, 128)])
+@pytest.mark.parametrize("count", [3, 30, 200])
+def test_workgroups_of_four_and_of_eight_waves(kind, heads, count):
+    """Requests and heads below and above a workgroup for every unit; lengths from none to all that one takes."""
+    reqs = [((0, 1, 64, 65, 300, 511, 513, 900, 1024)[i % 9], i % 9 and 1 + i % 2) for i in range(count)]
+    Batch(reqs, heads, 32, kind, seed=count).check(max_len=1024, rows=range(0, count, 1 + count // 20))
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("heads", [(8, 2, 64), (8, 2, 128)])
+def test_streams_of_blocks_that_are_not_there(kind, heads):
+    b = Batch([(500, 2), (300, 1), (129, 1), (5000, 2)], heads, 32, kind)
+    n = b.k.shape[0]
+    b.table[0, 3], b.table[0, 7], b.table[0, 8], b.table[1, 0], b.table[1, 9], b.table[3, 100] = n, -1, 2**31 - 1, -2**31, n + 5, -1
+    b.table[2, :] = -7
+    h = b.check(rows=(0, 1, 3), max_len=FAR)
+    assert not h.out[b.starts[2]:b.starts[3]].any()
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("heads", [(8, 2, 64), (8, 2, 128)])
+def test_streams_beside_what_no_token_has_written(kind, heads):
+    b = Batch([(t, min(t, 2)) for t in (1, 17, 70, 129, 255, 1000, 4999)], heads, 64, kind)
+    want = b.handle(max_len=FAR)
+    want.run()
+    junk = -128 if kind == "int8" else 0x7f
+    for i, (t, _) in enumerate(b.reqs):
+        last, used = int(b.table[i, (t - 1) // 64]), (t - 1) % 64 + 1
+        b.k.view(torch.int8)[last, :, used:] = junk
+        b.v.view(torch.int8)[last, :, :, used:] = junk
+    for u in b.unused:
+        b.ks[u], b.vs[u] = float("nan"), float("inf")
+        b.k.view(torch.int8)[u] = junk
+    got = b.handle(max_len=FAR)
+    got.run()
+    assert torch.equal(want.out, got.out)
+    b.check(max_len=FAR)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_streams_of_block_scales_of_all_sizes(kind):
+    b = Batch([(700, 1), (90, 3), (400, 2)], (4, 2, 64), 16, kind)
+    g = torch.Generator(device=DEV).manual_seed(1)
+    b.vs = b.vs * torch.exp2(torch.randint(-20, 12, b.vs.shape, generator=g, device=DEV).float())
+    b.check(max_len=FAR)
+    b.vs[int(b.table[0, 0])] = 0.0
+    b.ks[int(b.table[1, 1])] = 0.0
+    b.check(max_len=FAR)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_streams_of_requests_without_tokens_for_all_their_queries(kind):
+    b = Batch([(0, 2), (5, 8), (64, 3), (0, 1)], (4, 2, 64), 16, kind)
+    h = b.handle(max_len=FAR)
+    h.out.fill_(float("nan"))
+    h.run()
+    assert not h.out[:5].any() and not h.out[b.starts[3]:].any() and bool(h.out[5:b.starts[3]].abs().amax(1).gt(0).all())
