@@ -405,12 +405,13 @@ typedef struct {
  *     (what goes beyond free_cap is dropped).
  *   - Every other request has new_len[b] rows of the batch, in order: q_start[0..B] are their first rows (no row beyond
  *     `rows`).  It takes the blocks that it lacks from the top of the stack into its row of the table.
- *   - Refused is a request whose rows do not all fit in `rows`, that would need more than max_blocks blocks, or whose
+ *   - Refused is a request whose rows end beyond `rows` (those of refused ones count; also one of no rows behind such), that would need more than max_blocks blocks, or whose
  *     blocks the stack cannot give (then also every later one that needs a block).  It keeps what it has: no new tokens.
  *   seq_len_out    lengths with the new tokens (may be seq_len itself)
  *   free_count_out entries left on the stack (1 int; may be free_count itself)
  *   start          [B] position of the first new token; -1: refused or ended
  *   positions, slots  [rows] of each new token; 0 and -1 for the tokens of refused requests and behind the last row
+ *                     (-2 where the table's entry names no block: negative, or of slots beyond 2^31 - 1)
  *   bad            1 int, SET to the number of refused requests and of ended ones whose blocks were dropped
  * table [B][table_stride], max_blocks <= table_stride entries of a row are used.  A seq_len outside 0 .. max_blocks * block
  * is taken as the nearer end.  1 <= B <= BL_KV_MAX_REQUESTS, 1 <= rows <= 2^24, 0 <= free_cap < 2^31 (0: no stack,

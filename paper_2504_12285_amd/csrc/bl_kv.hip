@@ -60,7 +60,8 @@ __device__ __forceinline__ void tab_row(int64_t t, int B, const int* q_start, co
         }
         if (start[lo] >= 0) {
             pos = start[lo] + (int)(t - q_start[lo]);
-            slot = (int)(((uint32_t)table[lo * table_stride + (pos >> shift)] << shift) + (uint32_t)(pos & ((1 << shift) - 1)));
+            const uint32_t block = (uint32_t)table[lo * table_stride + (pos >> shift)];
+            slot = block < 0x80000000u >> shift ? (int)((block << shift) + (uint32_t)(pos & ((1 << shift) - 1))) : -2;    /* (no block: not another's slot) */
         }
     }
     positions[t] = pos;

@@ -153,3 +153,16 @@ def test_replayed_steps_keep_their_own_books():
         seq, count, start, q_start, pos, slots, bad = oracle(seq, new, table, free, count, block, 12)
         assert h.seq_len.tolist() == seq and h.free_count.tolist() == [count] and h.slots.tolist() == slots and h.bad.tolist() == [bad]
         assert h.table.tolist() == table and h.free_list.tolist() == free
+
+
+@pytest.mark.parametrize("block", [16, 128])
+def test_entries_that_name_no_block(block):
+    """Neither a negative entry nor one whose slots pass 31 bits becomes the slot of another block (or -1: a row that goes nowhere)."""
+    from paper_2504_12285_amd import binding as bl
+
+    def t(v):
+        return torch.tensor(v, dtype=torch.int32, device="cuda:0")
+    entries = [-1, 2**31 // block, 2**31 - 1, -2**31, 2**31 // block - 1, 2**32 // block]
+    h = bl.KVTables(t([block - 1] * 6), t([1] * 6), t([[e, 5] for e in entries]), t([0]), t([0]), block, 7)
+    h.run()
+    assert h.slots.tolist() == [-2, -2, -2, -2, 2**31 - 1, -2, -1] and h.bad.tolist() == [0]
