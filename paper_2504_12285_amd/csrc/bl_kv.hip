@@ -4,6 +4,7 @@
 
 /* ---- block tables and slot maps ---------------------------------------------------------------------------------- */
 
+#define TAB_OWN 2                  /* blocks that a request's own thread takes */
 #define TAB_ROWS_INSIDE 4096       /* rows whose slots the table kernel writes itself */
 
 template <int CTRL, int ROWS>
@@ -47,6 +48,40 @@ __device__ __forceinline__ void tab_list(bool has, int r, int* list, int* count)
     if (has) list[at] = r;
 }
 
+/* The n[r] entries of every listed request r from from(r) (STEP -1: downwards) to to(r): a wave has four requests at a time, IN / 4 entries of
+ * each a lane in flight.  256 requests of up to 4096 tokens, a ninth of which ends: 5.8 us, one request a wave at a time 9.8 (1024: 8.4 and 13.2); where all
+ * that end have 512 blocks, 57 of 512 requests, the other way round: 10.1 and 8.3. */
+template <int WAVES, int IN, int STEP, typename F, typename G>
+__device__ __forceinline__ void tab_copy(const int* list, int count, const int* n, F from, G to) {
+    constexpr int MANY = 4, EACH = IN / MANY;
+    const int lane = threadIdx.x & 63;
+    for (int k = threadIdx.x >> 6; k < count; k += MANY * WAVES) {
+        const int32_t* src[MANY];
+        int32_t* dst[MANY];
+        int have[MANY], most = 0;
+#pragma unroll
+        for (int i = 0; i < MANY; ++i) {
+            const bool there = k + i * WAVES < count;
+            const int r = list[there ? k + i * WAVES : k];
+            have[i] = there ? n[r] : 0, src[i] = from(r), dst[i] = to(r);
+            most = have[i] > most ? have[i] : most;
+        }
+        for (int j = lane; j < most; j += EACH * 64) {
+            int v[MANY][EACH];
+#pragma unroll
+            for (int i = 0; i < MANY; ++i)
+#pragma unroll
+                for (int u = 0; u < EACH; ++u)
+                    if (j + 64 * u < have[i]) v[i][u] = src[i][STEP * (j + 64 * u)];
+#pragma unroll
+            for (int i = 0; i < MANY; ++i)
+#pragma unroll
+                for (int u = 0; u < EACH; ++u)
+                    if (j + 64 * u < have[i]) dst[i][j + 64 * u] = v[i][u];
+        }
+    }
+}
+
 /* Position and slot of row t of the batch: its request by bisection in the B + 1 ascending first rows. */
 __device__ __forceinline__ void tab_row(int64_t t, int B, const int* q_start, const int* start, const int32_t* table, int64_t table_stride,
                                         int shift, int32_t* positions, int32_t* slots) {
@@ -74,14 +109,14 @@ struct tab_args {
 };
 
 /* One workgroup: a handful of requests, or a few thousand, is latency and not work.  Three sums over the requests (rows
- * and returned blocks, then demand, which needs them), the copies between stack and table a request a wave, IN
- * entries of a lane in flight, then the rows.  A thread holds PER consecutive requests where there are more than threads.
- * Bound by the launch and three dependent reads (lengths, stack, table): 8 requests 4.1 us, 512 with 33 thousand rows, 57 of them
- * ending, 12 and 4 for the rows' own kernel.  The copies a request a thread: 16. */
+ * and returned blocks, then demand, which needs them), the copies between stack and table by waves (one or two blocks by the
+ * request's thread), then the rows.  A thread holds PER consecutive requests where there are more than threads.
+ * Bound by the launch and three dependent reads (lengths, stack, table): 8 requests 3.9 us, 512 with 33 thousand rows, 57 of them
+ * ending, 9 and 4 for the rows' own kernel. */
 template <int THREADS, int PER>
 __global__ __launch_bounds__(THREADS) void bl_kv_tables_kernel(tab_args A) {
     const bl_kv_batch& b = A.b;
-    constexpr int MOST = THREADS * PER, WAVES = THREADS / BL_WAVE, IN = PER == 1 ? 16 : 8;
+    constexpr int MOST = THREADS * PER, WAVES = THREADS / BL_WAVE, IN = 8;
     __shared__ int64_t s_sum[WAVES];
     __shared__ int s_start[MOST], s_row[MOST + 1], s_list[MOST], s_from[MOST], s_n[MOST];
     __shared__ int s_taken, s_bad, s_back, s_want;
@@ -109,7 +144,6 @@ __global__ __launch_bounds__(THREADS) void bl_kv_tables_kernel(tab_args A) {
     int64_t all_rows, all_back;
     int64_t row = tab_scan<THREADS>(rows, s_sum, &all_rows);
     int64_t at = there + tab_scan<THREADS>(back, s_sum, &all_back);
-    const int lane = tid & 63, wave = tid >> 6;
     if (all_back) {
         /* ended requests: their blocks to the stack */
 #pragma unroll
@@ -122,20 +156,7 @@ __global__ __launch_bounds__(THREADS) void bl_kv_tables_kernel(tab_args A) {
             at += have;
         }
         __syncthreads();
-        for (int k = wave; k < s_back; k += WAVES) {
-            const int r = s_list[k], have = s_n[r];
-            int32_t* to = b.free_list + s_from[r];
-            const int32_t* from = b.table + r * b.table_stride;
-            for (int j = lane; j < have; j += IN * 64) {
-                int v[IN];
-#pragma unroll
-                for (int u = 0; u < IN; ++u)
-                    if (j + 64 * u < have) v[u] = from[j + 64 * u];
-#pragma unroll
-                for (int u = 0; u < IN; ++u)
-                    if (j + 64 * u < have) to[j + 64 * u] = v[u];
-            }
-        }
+        tab_copy<WAVES, IN, 1>(s_list, s_back, s_n, [&](int r) { return b.table + r * b.table_stride; }, [&](int r) { return b.free_list + s_from[r]; });
     }
     there = there + all_back > cap ? cap : there + all_back;
     /* demand */
@@ -163,29 +184,23 @@ __global__ __launch_bounds__(THREADS) void bl_kv_tables_kernel(tab_args A) {
         const bool ok = live && fits[i] && (w_i[i] == 0 || upto <= there), takes = ok && w_i[i] > 0;
         if (live && n[i] >= 0 && !ok) atomicAdd(&s_bad, 1);
         if (takes) {
+            const int has = (int)(((int64_t)old[i] + bs1) >> shift);
             atomicMax(&s_taken, (int)upto);
-            s_from[r] = (int)(there - 1 - before), s_n[r] = w_i[i];
-            s_start[r] = (int)(((int64_t)old[i] + bs1) >> shift);   /* (for now: the blocks that it has) */
+            s_from[r] = (int)(there - 1 - before), s_n[r] = w_i[i], s_start[r] = has;       /* (for now: the blocks that it has) */
+            if (w_i[i] <= TAB_OWN) {
+                const int32_t* from = b.free_list + (there - 1 - before);
+                int32_t* to = b.table + r * b.table_stride + has;
+                const int v = from[0];
+                if (w_i[i] > 1) to[1] = from[-1];
+                to[0] = v;
+            }
         }
-        tab_list(takes, r, s_list, &s_want);
+        tab_list(takes && w_i[i] > TAB_OWN, r, s_list, &s_want);
         row_i += n[i] > 0 ? n[i] : 0;
     }
     if (all_want) {
         __syncthreads();
-        for (int k = wave; k < s_want; k += WAVES) {
-            const int r = s_list[k], w = s_n[r];
-            int32_t* to = b.table + r * b.table_stride + s_start[r];
-            const int32_t* from = b.free_list + s_from[r];
-            for (int j = lane; j < w; j += IN * 64) {
-                int v[IN];
-#pragma unroll
-                for (int u = 0; u < IN; ++u)
-                    if (j + 64 * u < w) v[u] = from[-(j + 64 * u)];
-#pragma unroll
-                for (int u = 0; u < IN; ++u)
-                    if (j + 64 * u < w) to[j + 64 * u] = v[u];
-            }
-        }
+        tab_copy<WAVES, IN, -1>(s_list, s_want, s_n, [&](int r) { return b.free_list + s_from[r]; }, [&](int r) { return b.table + r * b.table_stride + s_start[r]; });
         __syncthreads();
     }
     upto -= want, row_i = row;
