@@ -478,7 +478,7 @@ bl_status bl_kv_append(const bl_kv_tokens* t, bl_stream s);
  *   max_q      no request has more queries (one that has is not computed)
  *   max_len    about the longest seq_len: sizes the split over a long axis only (0: max_blocks * block)
  *   workspace  bl_attn_workspace_bytes(a) bytes (it depends on the sizes, max_q, max_len and window of the descriptor, not on seq_len), 256-byte aligned; no content is expected
- * Up to four launches on `s`, none of which waits for the host.  1 <= B <= BL_KV_MAX_REQUESTS, 1 <= T <= 2^24, softmax_scale > 0, n_q a multiple of
+ * One launch on `s`, or two, neither of which waits for the host.  1 <= B <= BL_KV_MAX_REQUESTS, 1 <= T <= 2^24, softmax_scale > 0, n_q a multiple of
  * n_kv; max_blocks * block, T * n_q / n_kv and B * n_kv * max_blocks * block / 64 at most 2^30. */
 typedef struct {
     bl_kv_cache cache;

@@ -1211,7 +1211,7 @@ __global__ __launch_bounds__(AT_THREADS, 2) void bl_attn_many(at_args A) {
     at_many<KIND, D>(A, (int)blockIdx.x, lds);
 }
 /* Any batch, in one launch: the matrix cores' work first; what streams the cache fills the units as that ends. */
-template <int KIND, int D, bool WIDE>
+template <int KIND, int D, bool WIDE, int ITEM>
 __global__ __launch_bounds__(AT_THREADS, 2) void bl_attn_any(at_args A, int many) {
     union lds_t {
         at_stream_lds<D> few;
@@ -1219,7 +1219,7 @@ __global__ __launch_bounds__(AT_THREADS, 2) void bl_attn_any(at_args A, int many
     };
     __shared__ __attribute__((aligned(16))) uint8_t lds[sizeof(lds_t)];
     if ((int)blockIdx.x < many) at_many<KIND, D>(A, (int)blockIdx.x, ((lds_t*)lds)->many);
-    else at_few<KIND, D, WIDE, 0>(A, (int)blockIdx.x - many, lds);
+    else at_few<KIND, D, WIDE, ITEM>(A, (int)blockIdx.x - many, lds);
 }
 /* Partial results of both: `few` workgroups for those of at_few, turns x AT_STREAM_GROUPS, the others for a split. */
 template <int D, bool MANY>
@@ -1274,10 +1274,13 @@ static at_plan at_make_plan(const bl_attn_desc* a) {
      *   320 of 1500 32 and 32 / 26 and 27, of 2048 41 and 37 / 34 and 28; 1280 of 2048 106 and 120 / 74 and 79, of 4096 140 and 136;
      * heads of 64: 8 of 1024 7.7 and 11.8, 2048 10 and 11.5, 4096 16 and 12; 128 of 4096 17.2 and 19.4 / 16.5 and 17.1; 1024 of 4096 83 and 89 / 54 and 58.
      * Heads of 64 where there is an item a unit at most: eight waves, which have more loads on their way (128 of 2048 13.0 -> 11.0; 512 of 512 12.8 -> 14.6).
+     * Beside many rows (four waves then): 3 of 100 queries and one of one, 300 tokens, 19.6 -> 17.0; 4 of 200 and 252 of one, heads of 64, 48.2 -> 37.5;
+     *   but 3 of 89 and 3 of one over 1802, heads of 64, 22.1 -> 25.6.
      * Heads of 128 gain nothing from them (18 -> 19.5): four lanes that stand together read four lines of K, and a unit takes a line a clock. */
     const int64_t items = a->B * a->cache.n_kv;
-    const int64_t most = D == 128 ? items >= 1024 ? 2048 : items >= 128 ? 1536 : 1024 : items >= 128 ? 4096 : 2048;
-    p.items = !p.many && tokens <= most ? (int)items : 0;
+    const int64_t alone = D == 128 ? items >= 1024 ? 2048 : items >= 128 ? 1536 : 1024 : items >= 128 ? 4096 : 2048;
+    const int64_t most = D == 64 && p.many ? alone * 5 / 8 : alone;
+    p.items = p.few && tokens <= most ? (int)items : 0;
     const int64_t part = a->T < a->B ? a->T : a->B;           /* requests with rows */
     p.row_tiles = (int)(a->T * G / AT_MANY + part);
     p.splits = 1;
@@ -1305,10 +1308,11 @@ template <int KIND, int D, bool WIDE>
 static void at_launch(at_args A, const at_plan& p, const bl_attn_desc* a, hipStream_t st) {
     A.part = (float*)a->workspace;
     A.many_part = A.part + p.few_bytes / sizeof(float);
-    const int few = p.few ? AT_STREAM_GROUPS : 0;
+    const int few = !p.few ? 0 : p.items ? p.items : AT_STREAM_GROUPS;
     if (p.many) {
         const int many = p.row_tiles * A.n_kv * p.splits;
-        if (few) bl_attn_any<KIND, D, WIDE><<<(unsigned)(many + few), AT_THREADS, 0, st>>>(A, many);
+        if (few && p.items) bl_attn_any<KIND, D, WIDE, AT_WAVES><<<(unsigned)(many + few), AT_THREADS, 0, st>>>(A, many);
+        else if (few) bl_attn_any<KIND, D, WIDE, 0><<<(unsigned)(many + few), AT_THREADS, 0, st>>>(A, many);
         else bl_attn_many<KIND, D><<<(unsigned)many, AT_THREADS, 0, st>>>(A);
     } else {
         if (p.items) {
@@ -1319,7 +1323,7 @@ static void at_launch(at_args A, const at_plan& p, const bl_attn_desc* a, hipStr
         bl_attn_few<KIND, D, WIDE, 0><<<(unsigned)few, AT_THREADS, 0, st>>>(A);
     }
     const int64_t rows = (int64_t)A.T * A.n_q, per = AT_THREADS / (D / 4);
-    const int few_join = p.few ? AT_STREAM_GROUPS * ((p.rows + 256 / D - 1) / (256 / D)) : 0;      /* (D / 4 lanes a row of a wave) */
+    const int few_join = p.few && !p.items ? AT_STREAM_GROUPS * ((p.rows + 256 / D - 1) / (256 / D)) : 0;      /* (D / 4 lanes a row of a wave) */
     const int64_t join = few_join + (p.splits > 1 ? (rows + per - 1) / per : 0);
     if (p.splits > 1) bl_attn_join<D, true><<<(unsigned)join, AT_THREADS, 0, st>>>(A, few_join);
     else if (join) bl_attn_join<D, false><<<(unsigned)join, AT_THREADS, 0, st>>>(A, few_join);
@@ -1331,7 +1335,7 @@ extern "C" bl_status bl_attn_kv8(const bl_attn_desc* a, bl_stream s) {
     if (p.bytes && !a->workspace) return BL_ERR_WORKSPACE;
     if (!bl_aligned(a->workspace, 256)) return BL_ERR_ALIGN;
     const bl_kv_cache& c = a->cache;
-    if ((int64_t)p.row_tiles * c.n_kv * p.splits > 0x7fff0000) return BL_ERR_SHAPE;
+    if ((int64_t)p.row_tiles * c.n_kv * p.splits + p.items > 0x7fff0000) return BL_ERR_SHAPE;
     at_args A = {};
     A.k = (const uint8_t*)c.k, A.v = (const uint8_t*)c.v, A.k_scale = c.k_scale, A.v_scale = c.v_scale;
     A.q = a->q, A.q_start = a->q_start, A.seq_len = a->seq_len, A.table = a->table, A.out = a->out;

@@ -458,3 +458,13 @@ def test_streams_of_requests_without_tokens_for_all_their_queries(kind):
     h.out.fill_(float("nan"))
     h.run()
     assert not h.out[:5].any() and not h.out[b.starts[3]:].any() and bool(h.out[5:b.starts[3]].abs().amax(1).gt(0).all())
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("heads, block", [((20, 5, 128), 64), ((8, 2, 64), 16), ((8, 8, 64), 128)])
+@pytest.mark.parametrize("hint", [100, 1000, FAR])
+def test_prompts_beside_single_tokens_of_every_length(kind, heads, block, hint):
+    """One launch: rows of prompts, and single tokens by items or by streams as the hint of the length has it."""
+    reqs = [(t, (t if i % 3 == 0 else min(t, 1 + i % 2)) if t < 800 else min(t, 1 + 69 * (i % 2))) for i, t in enumerate(LENGTHS)]
+    Batch(reqs, heads, block, kind, seed=hint % 5).check(max_len=hint)
+    Batch(reqs, heads, block, kind, seed=hint % 5).check(max_len=hint, window=90)
