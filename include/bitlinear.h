@@ -473,7 +473,8 @@ bl_status bl_kv_append(const bl_kv_tokens* t, bl_stream s);
  * int8 with heads of 64 and many queries: q in fp16 times a power of two);
  * softmax weights are rounded to fp16 (11 bits; those below 2^-20 of a row's largest to 2^-30 of it) in front of the product with V; maxima, sums and outputs are held in fp32.
  *   q, out     rows q_stride / out_stride values apart (multiples of 8), 16-byte aligned.  Rows of no request are left alone.
- *   table      [B][table_stride]; an entry outside 0 .. n_blocks-1: its tokens are not seen
+ *   table      [B][table_stride]; an entry outside 0 .. n_blocks-1: its tokens are not seen.  Blocks in front of every query's window
+ *              may be another request's, or anyone's
  *   seq_len    taken as the nearer end outside 0 .. max_blocks * block; q_start: ascending, inside 0 .. T
  *   max_q      no request has more queries (one that has is not computed)
  *   max_len    about the longest seq_len: sizes the split over a long axis only (0: max_blocks * block)

@@ -365,10 +365,13 @@ __device__ __forceinline__ void at_few(const at_args& A, int group, uint8_t* lds
     struct blocks {
         int k, v;                                            /* as the table has them; -1: no token there */
     };
+    /* (sixteen tokens in front of all windows are not there: their block may be another's by now, and a NaN in it times a weight of 0 is none) */
     auto read_blocks = [&](const at_spot& s) -> blocks {
-        const int len = request(s.b).len, tok = (s.tile0 + s.t) * AT_TILE;
+        const at_request r = request(s.b);
+        const int tok = (s.tile0 + s.t) * AT_TILE, low = at_from(A, r, 0) - 15;
         const int* pages = A.table + s.b * A.table_stride;
-        return {tok + kgrp < len ? pages[(tok + kgrp) >> A.shift] : -1, tok + 16 * grp < len ? pages[(tok + 16 * grp) >> A.shift] : -1};
+        auto seen = [&](int t) { return t < r.len && t >= low; };
+        return {seen(tok + kgrp) ? pages[(tok + kgrp) >> A.shift] : -1, seen(tok + 16 * grp) ? pages[(tok + 16 * grp) >> A.shift] : -1};
     };
     auto place = [&](int block) { return (unsigned)block < (unsigned)A.n_blocks ? block : 0; };
     auto load_k = [&](const at_spot& s, int block, bl_v4i (&k)[4][KS]) {
@@ -902,7 +905,7 @@ __device__ __forceinline__ void at_many(const at_args& A, int place, at_many_lds
     const int k_off = kt * D + kc * 16, v_off = lane << A.shift;          /* V: features lane and lane + 64 */
     auto fetch_blocks = [&](int t) -> int {
         const int token = t * AT_TILE + 16 * (lane & 3);
-        return t < tend && token < R.len ? pages[token >> A.shift] : -1;
+        return t < tend && token < R.len && token + 16 > tok0 ? pages[token >> A.shift] : -1;       /* (in front of all windows: as in at_few) */
     };
     auto there = [&](int block) { return (unsigned)block < (unsigned)A.n_blocks; };
     bl_v4i lk[U], lv_[U];

@@ -468,3 +468,26 @@ def test_prompts_beside_single_tokens_of_every_length(kind, heads, block, hint):
     reqs = [(t, (t if i % 3 == 0 else min(t, 1 + i % 2)) if t < 800 else min(t, 1 + 69 * (i % 2))) for i, t in enumerate(LENGTHS)]
     Batch(reqs, heads, block, kind, seed=hint % 5).check(max_len=hint)
     Batch(reqs, heads, block, kind, seed=hint % 5).check(max_len=hint, window=90)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("block", [16, 32, 64])
+@pytest.mark.parametrize("heads", [(4, 2, 64), (4, 2, 128)])
+@pytest.mark.parametrize("n, max_len", [(1, 0), (2, FAR), (40, 0)])
+def test_blocks_in_front_of_a_window_may_hold_anything(kind, block, heads, n, max_len):
+    """A table may still name blocks that no window of the request reaches any more: they are another's by then, or nobody's."""
+    window = 70
+    b = Batch([(500, n), (1000, n), (90, n), (333, n)], heads, block, kind)
+    want = b.check(window=window, max_len=max_len)
+    junk, u = -128 if kind == "int8" else 0x7f, b.unused                  # the lowest integer; a NaN code
+    for x in u:
+        b.k.view(torch.int8)[x] = junk
+        b.v.view(torch.int8)[x] = junk
+        b.ks[x] = float("nan")
+        b.vs[x] = float("inf") if x == u[0] else float("nan")
+    for i, (t, m) in enumerate(b.reqs):
+        for j in range(max(0, t - m - window + 1) // block):
+            b.table[i, j] = u[j % 2]
+    got = b.handle(window=window, max_len=max_len)
+    got.run()
+    assert torch.equal(want.out, got.out)
