@@ -476,7 +476,7 @@ bl_status bl_kv_append(const bl_kv_tokens* t, bl_stream s);
  *   table      [B][table_stride]; an entry outside 0 .. n_blocks-1: its tokens are not seen.  Blocks in front of every query's window
  *              may be another request's, or anyone's
  *   seq_len    taken as the nearer end outside 0 .. max_blocks * block; q_start: ascending, inside 0 .. T
- *   max_q      no request has more queries (one that has is not computed)
+ *   max_q      no request has more queries (the rows of one that has are computed all the same, or are NaN: nothing else is ever left in them)
  *   max_len    about the longest seq_len: sizes the split over a long axis only (0: max_blocks * block)
  *   workspace  bl_attn_workspace_bytes(a) bytes (it depends on the sizes, max_q, max_len and window of the descriptor, not on seq_len), 256-byte aligned; no content is expected
  * One launch on `s`, or two, neither of which waits for the host.  1 <= B <= BL_KV_MAX_REQUESTS, 1 <= T <= 2^24, softmax_scale > 0, n_q a multiple of

@@ -598,7 +598,8 @@ class KVAppend(_KVCall):
 
 class KVAttention(_KVCall):
     """Causal attention over the cache (bl_attn_kv8).  q bf16 [T][n_q][head_dim] (or [T][n_q * head_dim] with n_q); q_start int32 [B + 1],
-    seq_len int32 [B], table int32 [B][max_blocks].  max_q: no request has more queries (None: all T rows may be one request's);
+    seq_len int32 [B], table int32 [B][max_blocks].  max_q: no request has more queries (None: all T rows may be one request's; rows of
+    one that has more may be NaN);
     max_len: about the longest length.  Output: out bf16 [T][n_q * head_dim].  The workspace may serve several handles whose runs
     follow each other on one stream."""
     _which, _where = 2, "bl_attn_kv8"

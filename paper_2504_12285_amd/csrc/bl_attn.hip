@@ -217,6 +217,14 @@ __device__ __forceinline__ int at_few_tiles(const at_args& A, const at_request& 
     const int t = (r.len + AT_TILE - 1) / AT_TILE - at_from(A, r, 0) / AT_TILE;
     return t > 0 ? t : 1;
 }
+/* Head h's rows of a request that brings more queries than the launch was made for (max_q), where none of its kernels does them: no numbers, so that
+ * what the output held before passes for no result.  `threads` threads share them. */
+template <int D>
+__device__ __forceinline__ void at_no_rows(const at_args& A, const at_request& r, int h, int thread, int threads) {
+    const int units = A.G * (D / 8);                         /* of 16 bytes */
+    for (int64_t i = thread; i < (int64_t)r.n * units; i += threads)
+        *bl_g((at_v4u*)(A.out + (r.row0 + i / units) * A.out_stride + (int64_t)h * A.G * D + i % units * 8)) = (at_v4u){0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u};
+}
 /* Tiles a wave does, of `all` in the launch. */
 __device__ __forceinline__ int at_share(int all) {
     const int s = (all + AT_STREAMS - 1) / AT_STREAMS;
@@ -232,6 +240,7 @@ struct at_slot {                    /* a wave's partial result: rows x (D sums, 
  * workspace (at most two such: at its ends) and bl_attn_join adds it up.  The four pieces of a workgroup that lie in one item
  * (at_together) are taken tile by tile in turn instead, and meet in LDS: a quarter of the partial results.
  * ITEM (0, or the waves of a workgroup): a workgroup has one item whole, so that nothing is left to join (short contexts).
+ * ALONE: no at_many stands beside it; requests of more than AT_FEW rows then get no numbers (in the streams' form a lane's own work: an error's speed).
  * K rows of a tile go straight from memory into the registers that the matrix cores read (four 16 x 128 products of
  * codes against the two pieces of q), then V the same way.  V of a tile and K of the next are in flight while one computes,
  * and the block numbers of the one behind: also across the items of a piece.
@@ -260,7 +269,7 @@ union at_stream_lds {
 struct at_spot {
     int b, h, t, c, tile0;          /* request, kv head, tile of c, first tile */
 };
-template <int KIND, int D, bool WIDE, int ITEM>
+template <int KIND, int D, bool WIDE, int ITEM, bool ALONE>
 __device__ __forceinline__ void at_few(const at_args& A, int group, uint8_t* lds_bytes) {
     constexpr int KS = D / 64, DT = D / 16, WAVES = ITEM ? ITEM : AT_WAVES;     /* 64-byte steps of a K row, 16-feature tiles of V */
     at_few_lds<D>& lds = *(at_few_lds<D>*)lds_bytes;
@@ -305,7 +314,10 @@ __device__ __forceinline__ void at_few(const at_args& A, int group, uint8_t* lds
         mine = at_read(A, cur.b);
         mine = {at_uniform(mine.row0), at_uniform(mine.n), at_uniform(mine.len)};
         cur.c = at_few_tiles(A, mine), cur.t = wave;
-        if (!cur.c) return;
+        if (!cur.c) {
+            if (ALONE) at_no_rows<D>(A, mine, cur.h, tid, WAVES * BL_WAVE);
+            return;
+        }
         cur.tile0 = at_from(A, mine, 0) / AT_TILE;
         count = (cur.c - wave + WAVES - 1) / WAVES;     /* (none for some waves of a short item: they bring nothing to the meeting) */
     } else {
@@ -316,6 +328,8 @@ __device__ __forceinline__ void at_few(const at_args& A, int group, uint8_t* lds
             if (lane < A.B) {
                 mine = at_read(A, lane);
                 upto = at_few_tiles(A, mine);
+                if (ALONE && __builtin_expect(mine.n * A.G > AT_FEW, 0))
+                    for (int h = group; h < A.n_kv; h += AT_STREAM_GROUPS) at_no_rows<D>(A, mine, h, wave, AT_WAVES);
             }
             upto = at_scan(upto);
             if (group == 0 && tid < A.B) heads[tid] = make_int4(upto, mine.row0, mine.n, 0);
@@ -325,6 +339,8 @@ __device__ __forceinline__ void at_few(const at_args& A, int group, uint8_t* lds
                 const at_request r = at_read(A, b);
                 lds.request[b] = make_int2(r.row0 << 5 | (r.n < 31 ? r.n : 31), r.len);
                 if (group == 0) heads[b] = make_int4(lds.upto[b], r.row0, r.n, 0);
+                if (ALONE && __builtin_expect(r.n * A.G > AT_FEW, 0))
+                    for (int h = group; h < A.n_kv; h += AT_STREAM_GROUPS) at_no_rows<D>(A, r, h, 0, 1);
             }
             __syncthreads();
         }
@@ -1205,7 +1221,7 @@ template <int KIND, int D, bool WIDE, int ITEM>
 __global__ __launch_bounds__(ITEM ? ITEM * BL_WAVE : AT_THREADS, 2) void bl_attn_few(at_args A) {
     constexpr size_t bytes = ITEM ? sizeof(at_meet_lds<D, ITEM ? ITEM : 1>) : sizeof(at_stream_lds<D>);
     __shared__ __attribute__((aligned(16))) uint8_t lds[bytes];
-    at_few<KIND, D, WIDE, ITEM>(A, (int)blockIdx.x, lds);
+    at_few<KIND, D, WIDE, ITEM, true>(A, (int)blockIdx.x, lds);
 }
 /* One request, or groups of more heads than at_few has rows: at_many alone. */
 template <int KIND, int D>
@@ -1222,7 +1238,7 @@ __global__ __launch_bounds__(AT_THREADS, 2) void bl_attn_any(at_args A, int many
     };
     __shared__ __attribute__((aligned(16))) uint8_t lds[sizeof(lds_t)];
     if ((int)blockIdx.x < many) at_many<KIND, D>(A, (int)blockIdx.x, ((lds_t*)lds)->many);
-    else at_few<KIND, D, WIDE, ITEM>(A, (int)blockIdx.x - many, lds);
+    else at_few<KIND, D, WIDE, ITEM, false>(A, (int)blockIdx.x - many, lds);
 }
 /* Partial results of both: `few` workgroups for those of at_few, turns x AT_STREAM_GROUPS, the others for a split. */
 template <int D, bool MANY>

@@ -491,3 +491,21 @@ def test_blocks_in_front_of_a_window_may_hold_anything(kind, block, heads, n, ma
     got = b.handle(window=window, max_len=max_len)
     got.run()
     assert torch.equal(want.out, got.out)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("max_len", [100, FAR])
+@pytest.mark.parametrize("heads", [(8, 2, 64), (20, 5, 128)])
+@pytest.mark.parametrize("count", [3, 70])
+def test_more_queries_than_announced_give_no_numbers(kind, max_len, heads, count):
+    """A request whose rows no kernel of the launch does: nothing that the output held before passes for its result, and the rows of the
+    others are theirs."""
+    reqs = [((60, 30, 200)[i % 3], (1, 5, 4)[i % 3] if i != 1 else 21) for i in range(count)]
+    b = Batch(reqs, heads, 32, kind, seed=count)
+    h = b.handle(max_q=1, max_len=max_len)
+    h.out.fill_(7.0)
+    h.run()
+    over = [i for i, (_, n) in enumerate(reqs) if n * (heads[0] // heads[1]) > 16]
+    for i in over:
+        assert bool(h.out[b.starts[i]:b.starts[i + 1]].isnan().all()), i
+    b.compare(h.out, only=[i for i in range(count) if i not in over][:30])
