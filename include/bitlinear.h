@@ -372,7 +372,7 @@ bl_status bl_gemm_w158a8_noalloc(const uint8_t* packed, const float* beta, int l
                                  int32_t* acc, float* y, bl_stream s);
 
 /* KEY/VALUE CACHE OF 8-BIT CODES, and the attention that reads it: what stands between the QKV and the output
- * BitLinear of a layer when a model is served.  Three calls, each one descriptor (HOST memory, read during the call)
+ * BitLinear of a layer when a model is served.  Three calls (the first also with a limit), each one descriptor (HOST memory, read during the call)
  * and a stream: block tables and slot maps of a step from the requests' lengths; the rotary append of new tokens;
  * causal attention over the cache for any number of new tokens per request.
  *
@@ -433,6 +433,14 @@ typedef struct {
     int32_t* bad;
 } bl_kv_batch;
 bl_status bl_kv_tables(const bl_kv_batch* b, bl_stream s);
+
+/* The same with a limit: a request that brings more than max_new tokens (at least 1) is refused too, its rows counted like those of
+ * the other refused ones.  For a step whose attention takes max_new as its max_q. */
+typedef struct {
+    bl_kv_batch batch;
+    int64_t max_new;
+} bl_kv_limited_batch;
+bl_status bl_kv_tables_limited(const bl_kv_limited_batch* b, bl_stream s);
 
 /* New tokens into the cache: row t of the fused projection [Q | K | V] ((n_q + 2 * n_kv) heads, fp32 or bf16), rotary
  * embedding on Q and K (x[i], x[i + d/2] -> x[i]*c - x[i+d/2]*s, x[i+d/2]*c + x[i]*s with c, s = cos, sin[position][i],

@@ -41,6 +41,7 @@ SIGNATURES = {
     "bl_stack_build": (_ci, [_vp, _ci, _ci, _i64, _vp, _vp, _vp]),
     "bl_stack_run": (_ci, [_vp, _vp, _vp]),
     "bl_kv_tables": (_ci, [_vp, _vp]),
+    "bl_kv_tables_limited": (_ci, [_vp, _vp]),
     "bl_kv_append": (_ci, [_vp, _vp]),
     "bl_attn_workspace_bytes": (_sz, [_vp]),
     "bl_attn_kv8": (_ci, [_vp, _vp]),
@@ -115,6 +116,11 @@ class KVBatchDesc(ctypes.Structure):
                 ("block", ctypes.c_int32), ("max_blocks", ctypes.c_int32)] + \
                [(n, _vp) for n in ("seq_len", "new_len", "free_count", "table", "free_list", "seq_len_out", "free_count_out",
                                    "start", "q_start", "positions", "slots", "bad")]
+
+
+class KVLimitedBatchDesc(ctypes.Structure):
+    """Mirror of bl_kv_limited_batch."""
+    _fields_ = [("batch", KVBatchDesc), ("max_new", _i64)]
 
 
 class KVTokensDesc(ctypes.Structure):
@@ -228,7 +234,7 @@ def _first_native():
         return _native
     _bl_torch.bind(*(ctypes.cast(fn, _vp).value for fn in (lib.bl_quant_act_int8, lib.bl_gemv_w158a8,
                                                             lib.bl_gemm_w158a8, lib.bl_bitlinear_decode, lib.bl_stack_run)))
-    _bl_torch.bind_kv(*(ctypes.cast(fn, _vp).value for fn in (lib.bl_kv_tables, lib.bl_kv_append, lib.bl_attn_kv8)))
+    _bl_torch.bind_kv(*(ctypes.cast(fn, _vp).value for fn in (lib.bl_kv_tables, lib.bl_kv_append, lib.bl_attn_kv8, lib.bl_kv_tables_limited)))
     _native = _bl_torch
     return _native
 
@@ -545,10 +551,11 @@ class _KVCall:
 class KVTables(_KVCall):
     """Block tables and slot maps of a step (bl_kv_tables).  seq_len, new_len int32 [B]; table int32 [B][max_blocks];
     free_list int32 [any]; free_count int32 [1]; rows: rows of the batch.  Outputs: start, q_start, positions, slots, bad, and
-    seq_len_out, free_count_out (in_place: seq_len and free_count themselves, for a step that is run again and again)."""
+    seq_len_out, free_count_out (in_place: seq_len and free_count themselves, for a step that is run again and again).
+    max_new: a request that brings more tokens is refused (bl_kv_tables_limited); None: no such limit."""
     _which, _where = 0, "bl_kv_tables"
 
-    def __init__(self, seq_len, new_len, table, free_list, free_count, block, rows, in_place=False):
+    def __init__(self, seq_len, new_len, table, free_list, free_count, block, rows, in_place=False, max_new=None):
         torch = _get_torch()
         i32, dev, B = torch.int32, seq_len.device, seq_len.shape[0]
         _wants(seq_len, "seq_len", i32, dev, (B,))
@@ -565,6 +572,9 @@ class KVTables(_KVCall):
         self.desc = KVBatchDesc(B, rows, _row_stride(table), free_list.shape[0], block, table.shape[1],
                                 *(_ptr(t) for t in (seq_len, new_len, free_count, table, free_list, self.seq_len_out, self.free_count_out,
                                                     self.start, self.q_start, self.positions, self.slots, self.bad)))
+        if max_new is not None:
+            self._which, self._where = 3, "bl_kv_tables_limited"
+            self.desc = KVLimitedBatchDesc(self.desc, max_new)
 
 
 class KVAppend(_KVCall):

@@ -26,7 +26,7 @@ decode_fn g_decode;
 typedef bl_status (*run_fn)(void*, const bl_stack_plan*, bl_stream);
 run_fn g_run;
 typedef bl_status (*kv_fn)(const void*, bl_stream);
-kv_fn g_kv[3];                           /* tables, append, attention */
+kv_fn g_kv[4];                           /* tables, append, attention, tables with a limit */
 
 /* A tensor argument: exactly torch.Tensor or None. */
 bool get(PyObject* o, const at::Tensor** t) {
@@ -190,7 +190,7 @@ PyObject* run(PyObject*, PyObject* const* a, Py_ssize_t n) {
 PyObject* kv(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return guarded([&]() -> PyObject* {
         int64_t which, desc;
-        if (n != 2 || !plain() || !get(a[0], &which) || which < 0 || which > 2 || !get(a[1], &desc) || !desc) return nullptr;
+        if (n != 2 || !plain() || !get(a[0], &which) || which < 0 || which > 3 || !get(a[1], &desc) || !desc) return nullptr;
         const bl_stream st = stream();
         bl_status rc;
         Py_BEGIN_ALLOW_THREADS
@@ -214,11 +214,11 @@ PyObject* bind(PyObject*, PyObject* args) {
     Py_RETURN_NONE;
 }
 
-/* The addresses of bl_kv_tables, bl_kv_append and bl_attn_kv8 in the loaded library. */
+/* The addresses of bl_kv_tables, bl_kv_append, bl_attn_kv8 and bl_kv_tables_limited in the loaded library. */
 PyObject* bind_kv(PyObject*, PyObject* args) {
-    unsigned long long f[3];
-    if (!PyArg_ParseTuple(args, "KKK", f, f + 1, f + 2)) return nullptr;
-    for (int i = 0; i < 3; ++i) g_kv[i] = (kv_fn)f[i];
+    unsigned long long f[4];
+    if (!PyArg_ParseTuple(args, "KKKK", f, f + 1, f + 2, f + 3)) return nullptr;
+    for (int i = 0; i < 4; ++i) g_kv[i] = (kv_fn)f[i];
     Py_RETURN_NONE;
 }
 

@@ -30,7 +30,7 @@ def rotary_angles(n_pos, device, base=500000.0, dim=HEAD_DIM):
 class CachedLayers:
     """Layers, their caches and the buffers of a step.  weights: per layer a dict name -> (packed, beta); gains: per layer a
     dict name -> fp32 [K] or None.  requests: places in the batch; rows: new tokens of a step at most; max_new: of one
-    request; max_blocks: blocks of one request; n_blocks: of the pool (each layer has a cache of that many)."""
+    request (one that brings more is refused: tables.bad counts it, tables.start is -1); max_blocks: blocks of one request; n_blocks: of the pool (each layer has a cache of that many)."""
 
     def __init__(self, weights, gains, requests, rows, max_blocks, n_blocks, device, layout=bl.BL_LAYOUT_K16, block=64,
                  kind=bl.BL_KV_INT8, max_new=None, window=0, eps=1e-5):
@@ -43,7 +43,8 @@ class CachedLayers:
         self.table = torch.full((requests, max_blocks), -1, **i32)
         self.free_list = torch.arange(n_blocks - 1, -1, -1, **i32)
         self.free_count = torch.full((1,), n_blocks, **i32)
-        self.tables = bl.KVTables(self.seq_len, self.new_len, self.table, self.free_list, self.free_count, block, rows, in_place=True)
+        self.tables = bl.KVTables(self.seq_len, self.new_len, self.table, self.free_list, self.free_count, block, rows, in_place=True,
+                                  max_new=max_new)
         cos, sin = rotary_angles(max_blocks * block, device)
         self.bad = torch.zeros(1, **i32)
         q = torch.empty((rows, N_Q * HEAD_DIM), dtype=torch.bfloat16, device=device)
@@ -54,7 +55,7 @@ class CachedLayers:
         space = None
         self.attend = []
         for c in self.caches:
-            a = bl.KVAttention(c, q, self.tables.q_start, self.seq_len, self.table, n_q=N_Q, max_q=max_new or rows, window=window, out=out,
+            a = bl.KVAttention(c, q, self.tables.q_start, self.seq_len, self.table, n_q=N_Q, max_q=rows if max_new is None else max_new, window=window, out=out,
                                workspace=space)
             space = a.workspace
             self.attend.append(a)

@@ -166,3 +166,39 @@ def test_entries_that_name_no_block(block):
     h = bl.KVTables(t([block - 1] * 6), t([1] * 6), t([[e, 5] for e in entries]), t([0]), t([0]), block, 7)
     h.run()
     assert h.slots.tolist() == [-2, -2, -2, -2, 2**31 - 1, -2, -1] and h.bad.tolist() == [0]
+
+
+@pytest.mark.parametrize("B, most", [(5, 3), (200, 40), (300, 17), (1100, 6), (4096, 1)])
+def test_requests_of_more_tokens_than_the_limit_are_refused(B, most):
+    """Against the definition where nothing else refuses: the pool, the table and the batch are large enough for all."""
+    from paper_2504_12285_amd import binding as bl
+
+    def t(v):
+        return torch.tensor(v, dtype=torch.int32, device="cuda:0")
+    r, block, width = random.Random(B), 16, 12
+    old = [r.randrange(60) for _ in range(B)]
+    new = [r.choice([-1, 0, 1, most, most + 1, most + 30]) for _ in range(B)]
+    held = [-(-n // block) for n in old]
+    ids = list(range(sum(held) + 8 * B))
+    r.shuffle(ids)
+    table = [[ids.pop() for _ in range(u)] + [-1] * (width - u) for u in held]
+    rows, count = sum(max(0, n) for n in new) + 2, len(ids)
+    h = bl.KVTables(t(old), t(new), t(table), t(ids + [-1] * sum(held)), t([count]), block, rows, max_new=most)
+    h.run()
+    good = [0 <= n <= most for n in new]
+    want = [-(-(o + n) // block) - u if g else -u if n < 0 else 0 for o, n, u, g in zip(old, new, held, good)]
+    start, slots, after, q_start, bad = h.start.tolist(), h.slots.tolist(), h.table.tolist(), h.q_start.tolist(), h.bad.tolist()
+    assert start == [o if g else -1 for o, g in zip(old, good)] and bad == [sum(n > most for n in new)]
+    assert h.seq_len_out.tolist() == [0 if n < 0 else o + n if g else o for o, n, g in zip(old, new, good)]
+    assert h.free_count_out.tolist() == [count - sum(want)]
+    at, used = 0, []
+    for b in range(B):
+        assert q_start[b] == at
+        for i in range(max(0, new[b])):
+            p = old[b] + i
+            assert slots[at + i] == (after[b][p // block] * block + p % block if good[b] else -1)
+        at += max(0, new[b])
+        assert good[b] or after[b] == table[b]
+        if new[b] >= 0:
+            used += after[b][:held[b] + max(0, want[b])]
+    assert q_start[B] == at and slots[at:] == [-1] * (rows - at) and len(set(used)) == len(used)

@@ -104,3 +104,18 @@ def test_a_pool_that_runs_dry_refuses(model):
     assert layers.seq_len.tolist() == [250, 0, 250]        # the first would need a ninth block
     assert layers.tables.start.tolist() == [-1, -1, 200] and int(layers.tables.bad) == 1
     assert layers.tables.slots[:7].eq(-1).all() and int(layers.bad) == 0
+
+
+def test_a_request_of_more_tokens_than_max_new_is_refused(model):
+    """Five tokens where four are the most: nothing of them reaches the caches or the lengths, and the others' rows are those of a step
+    without them."""
+    layers, alone = served(model, 3, 12, max_new=4), served(model, 3, 12, max_new=4)
+    g = torch.Generator(device=DEV).manual_seed(6)
+    x = torch.randn(12, 2560, generator=g, device=DEV)
+    y = layers.step(x, torch.tensor([3, 5, 4], dtype=torch.int32, device=DEV)).clone()
+    assert layers.seq_len.tolist() == [3, 0, 4] and layers.tables.start.tolist() == [0, -1, 0]
+    assert int(layers.tables.bad) == 1 and int(layers.bad) == 0 and int(layers.free_count) == 28
+    rest = torch.cat([x[:3], x[8:], x[:5]])
+    z = alone.step(rest, torch.tensor([3, 0, 4], dtype=torch.int32, device=DEV))
+    assert int(alone.tables.bad) == 0
+    assert torch.equal(y[:3], z[:3]) and torch.equal(y[8:12], z[3:7])

@@ -149,3 +149,25 @@ def test_the_binding_takes_what_a_descriptor_can_stand_for(lib):
                 dict(workspace=torch.zeros(8, dtype=torch.uint8))):
         with pytest.raises((TypeError, ValueError)):
             bl.KVAttention(**dict(dict(cache=c, q=q, q_start=start, seq_len=n, table=table), **bad))
+
+
+@pytest.mark.parametrize("limit, more, status", [(0, {}, SHAPE), (-3, {}, SHAPE), (1, dict(seq_len=None), NULL), (1, dict(B=0), SHAPE), (1 << 40, dict(block=24), SHAPE),
+                                                 (5, dict(slots=P + 1), ALIGN)])
+def test_tables_with_a_limit_refuse(lib, limit, more, status):
+    assert lib.bl_kv_tables_limited(ctypes.byref(bl.KVLimitedBatchDesc(tables(**more), limit)), None) == status
+    assert lib.bl_kv_tables_limited(None, None) == NULL
+
+
+def test_a_limit_stands_in_the_handle_and_in_the_layers(lib):
+    from paper_2504_12285_amd import serve
+    i32 = torch.int32
+    n = torch.zeros(3, dtype=i32)
+    args = (n, n, torch.zeros(3, 4, dtype=i32), torch.zeros(9, dtype=i32), torch.zeros(1, dtype=i32), 16, 5)
+    assert ctypes.sizeof(bl.KVLimitedBatchDesc) == 144
+    assert isinstance(bl.KVTables(*args).desc, bl.KVBatchDesc)
+    h = bl.KVTables(*args, max_new=2)
+    assert h.desc.max_new == 2 and h.desc.batch.rows == 5 and h._where == "bl_kv_tables_limited"
+    layers = serve.CachedLayers([{}], [{}], requests=2, rows=6, max_blocks=3, n_blocks=6, device="cpu", max_new=4)
+    assert layers.tables.desc.max_new == 4 and layers.attend[0].desc.max_q == 4
+    free = serve.CachedLayers([{}], [{}], requests=2, rows=6, max_blocks=3, n_blocks=6, device="cpu")
+    assert isinstance(free.tables.desc, bl.KVBatchDesc) and free.attend[0].desc.max_q == 6
