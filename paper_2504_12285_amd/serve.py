@@ -6,7 +6,7 @@
 
 Layer, per token: qkv = BL_qkv(norm(x)); Q, K turned, K and V into the cache; a = attention; o = BL_o(norm(a)); h1 = x + o;
 gu = BL_gu(norm(h1)); x' = h1 + BL_down(norm(relu(g)^2 * u)).  Orchestration only: every arithmetic step runs inside the HIP
-kernels reached through the C-ABI.  A step reads nothing back and allocates nothing, so that it may be captured in a HIP graph.
+kernels reached through the C-ABI; what is done here is that rows without a slot are cleared.  A step reads nothing back and allocates nothing, so that it may be captured in a HIP graph.
 
 `python -m paper_2504_12285_amd.serve` runs prompts and decode steps on random weights and prints their times.
 """
@@ -45,6 +45,7 @@ class CachedLayers:
         self.free_count = torch.full((1,), n_blocks, **i32)
         self.tables = bl.KVTables(self.seq_len, self.new_len, self.table, self.free_list, self.free_count, block, rows, in_place=True,
                                   max_new=max_new)
+        self.nowhere = torch.zeros(rows, dtype=torch.bool, device=device)
         cos, sin = rotary_angles(max_blocks * block, device)
         self.bad = torch.zeros(1, **i32)
         q = torch.empty((rows, N_Q * HEAD_DIM), dtype=torch.bfloat16, device=device)
@@ -78,7 +79,8 @@ class CachedLayers:
             bl.bl_gemm_w158a8_res(packed, beta, self.layout, q, B.scale, B.rowsum, N, residual, want_acc=False, y=out)
 
     def run(self):
-        """One step over what x and new_len hold; the result is in buffers.x_next."""
+        """One step over what x and new_len hold; the result is in buffers.x_next.  Rows whose token has no slot (of a refused request,
+        padding) went through the products and an attention that knows nothing of them: they are zeros at the end."""
         B = self.buffers
         self.tables.run()
         x, y = self.x, B.x_next
@@ -90,11 +92,13 @@ class CachedLayers:
             self._product(i, "gate_up", bl.make_producer(bl.BL_PROD_RESIDUAL, x, B.o, B.h1, **self._norm(i, "gate_up")), B.gu)
             self._product(i, "down", bl.make_producer(bl.BL_PROD_RELU2_GATE, B.gu, **self._norm(i, "down")), y, residual=B.h1)
             x = y                               # (the layer has read x when its last product writes)
-        return y
+        torch.lt(self.tables.slots, 0, out=self.nowhere)
+        return y.masked_fill_(self.nowhere[:, None], 0.0)
 
     def step(self, x, new_len):
         """x: fp32 [rows][2560], the rows of the requests' new tokens in order (rows behind them are padding); new_len: int32
-        [requests], tokens that each brings, -1: it ends.  Returns the rows' hidden states (a buffer of the next step)."""
+        [requests], tokens that each brings, -1: it ends.  Returns the rows' hidden states (a buffer of the next step); those of a refused
+        request (tables.bad of them, tables.start is -1) and of padding are zeros."""
         self.x.copy_(x)
         self.new_len.copy_(new_len)
         return self.run()

@@ -119,3 +119,26 @@ def test_a_request_of_more_tokens_than_max_new_is_refused(model):
     z = alone.step(rest, torch.tensor([3, 0, 4], dtype=torch.int32, device=DEV))
     assert int(alone.tables.bad) == 0
     assert torch.equal(y[:3], z[:3]) and torch.equal(y[8:12], z[3:7])
+
+
+def test_rows_of_refused_requests_and_padding_are_zeros(model):
+    """Too many tokens, and too little of the pool; a captured step too."""
+    layers = served(model, 3, 700, max_new=300)
+    x = torch.randn(700, 2560, generator=torch.Generator(device=DEV).manual_seed(8), device=DEV)
+    y = layers.step(x, torch.tensor([250, 301, 100], dtype=torch.int32, device=DEV))
+    assert layers.tables.start.tolist() == [0, -1, 0]
+    assert bool(y[:250].abs().amax(1).gt(0).all()) and not y[250:551].any() and bool(y[551:651].abs().amax(1).gt(0).all()) and not y[651:].any()
+    y = layers.step(x, torch.tensor([7, 200, 30], dtype=torch.int32, device=DEV))
+    assert layers.tables.start.tolist() == [-1, 0, 100]          # the first would need a ninth block
+    assert not y[:7].any() and bool(y[7:237].abs().amax(1).gt(0).all()) and not y[237:].any()
+    small = served(model, 2, 3, max_new=1)
+    small.step(x[:3], torch.tensor([1, 1], dtype=torch.int32, device=DEV))
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        small.run()
+    for new, zeros in (([1, 1], [2]), ([2, 1], [0, 1]), ([0, 1], [1, 2]), ([1, 2], [1, 2])):
+        small.new_len.copy_(torch.tensor(new, dtype=torch.int32, device=DEV))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert [i for i in range(3) if not small.buffers.x_next[i].any()] == zeros
