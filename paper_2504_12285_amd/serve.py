@@ -10,6 +10,8 @@ kernels reached through the C-ABI; what is done here is that rows without a slot
 
 `python -m paper_2504_12285_amd.serve` runs prompts and decode steps on random weights and prints their times.
 """
+import time
+
 import torch
 
 from . import binding as bl
@@ -112,8 +114,17 @@ def random_layers(n, device, seed=0, layout=bl.BL_LAYOUT_K16):
     return weights, [{name: None for name in SHAPES} for _ in range(n)]
 
 
+def time_prompts(layers, x, lens):
+    """Seconds of the step that brings prompts of `lens` tokens to places that are all empty at its start (whatever they hold now ends first)."""
+    layers.step(x, torch.full_like(lens, -1))
+    torch.cuda.synchronize()
+    t = time.perf_counter()
+    y = layers.step(x, lens)
+    torch.cuda.synchronize()
+    return time.perf_counter() - t, y
+
+
 def main(layers=4, requests=8, prompt=1000, steps=64):
-    import time
     dev = torch.device("cuda:0")
     weights, gains = random_layers(layers, dev)
     blocks = (prompt + steps) // 64 + 2
@@ -123,12 +134,8 @@ def main(layers=4, requests=8, prompt=1000, steps=64):
     fill = CachedLayers(weights, gains, requests, rows, blocks, requests * blocks, dev, max_new=prompt)
     x = torch.randn(rows, SHAPES["down"][0], generator=g, device=dev)
     fill.step(x, lens)
-    torch.cuda.synchronize()
-    t = time.perf_counter()
-    y = fill.step(x, torch.full_like(lens, -1))          # everyone ends: the pool is whole again
-    y = fill.step(x, lens)
-    torch.cuda.synchronize()
-    print("%d prompts, %d tokens, %d layers: %.2f ms" % (requests, rows, layers, (time.perf_counter() - t) * 1e3 / 2))
+    t, y = time_prompts(fill, x, lens)
+    print("%d prompts, %d tokens, %d layers: %.2f ms" % (requests, rows, layers, t * 1e3))
     # decode: the same state with a row for each request, captured once and replayed
     decode = CachedLayers(weights, gains, requests, requests, blocks, requests * blocks, dev, max_new=1)
     for name in ("seq_len", "table", "free_list", "free_count"):

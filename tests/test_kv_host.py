@@ -171,3 +171,23 @@ def test_a_limit_stands_in_the_handle_and_in_the_layers(lib):
     assert layers.tables.desc.max_new == 4 and layers.attend[0].desc.max_q == 4
     free = serve.CachedLayers([{}], [{}], requests=2, rows=6, max_blocks=3, n_blocks=6, device="cpu")
     assert isinstance(free.tables.desc, bl.KVBatchDesc) and free.attend[0].desc.max_q == 6
+
+
+def test_the_time_of_prompts_is_that_of_their_step_alone(monkeypatch):
+    """What the places held ends, and is waited for, before the clock is read: the time between its two readings holds one step, the prompts'."""
+    from paper_2504_12285_amd import serve
+    log = []
+
+    class Layers:
+        def step(self, x, new_len):
+            log.append(new_len.tolist())
+            return x
+
+    def clock():
+        log.append("clock")
+        return 3.0 * log.count("clock")
+    monkeypatch.setattr(serve.torch.cuda, "synchronize", lambda: log.append("wait"))
+    monkeypatch.setattr(serve.time, "perf_counter", clock)
+    x, lens = torch.zeros(7, 2560), torch.tensor([4, 3], dtype=torch.int32)
+    seconds, y = serve.time_prompts(Layers(), x, lens)
+    assert log == [[-1, -1], "wait", "clock", [4, 3], "wait", "clock"] and seconds == 3.0 and y is x
