@@ -191,3 +191,14 @@ def test_the_time_of_prompts_is_that_of_their_step_alone(monkeypatch):
     x, lens = torch.zeros(7, 2560), torch.tensor([4, 3], dtype=torch.int32)
     seconds, y = serve.time_prompts(Layers(), x, lens)
     assert log == [[-1, -1], "wait", "clock", [4, 3], "wait", "clock"] and seconds == 3.0 and y is x
+
+
+@pytest.mark.parametrize("more", [dict(), dict(window=100, max_blocks=500, table_stride=500), dict(max_q=7, max_len=300)])
+def test_items_need_no_room_for_partial_results(lib, more):
+    """Short contexts and short windows leave nothing to join: 256 bytes, and a split's own pieces where there is one."""
+    a = attention(**more)
+    T, n_q, D = a.T, a.n_q, a.cache.head_dim
+    assert (lib.bl_attn_workspace_bytes(ctypes.byref(a)) - 256) % (T * n_q * (D + 2) * 4) == 0
+    assert lib.bl_attn_workspace_bytes(ctypes.byref(a)) < 1 << 20
+    streams = attention(max_blocks=500, table_stride=500)
+    assert lib.bl_attn_workspace_bytes(ctypes.byref(streams)) == 256 + 2048 * 2 * 16 * 130 * 4
