@@ -476,7 +476,8 @@ bl_status bl_kv_append(const bl_kv_tokens* t, bl_stream s);
 /* Causal attention over the cache.  Request b's queries are rows q_start[b] .. q_start[b+1]-1 of q (bf16, n_q heads; query head h reads
  * key/value head h / (n_q / n_kv)); they are its last tokens: query i of n has the position p = seq_len[b] - n + i and sees
  * the tokens 0 .. p (window > 0: p - window + 1 .. p) that are in the cache.
- *   out[row][h] = bf16( sum_j softmax_j( softmax_scale * <q, k_j> ) v_j ),  zeros where nothing is seen.
+ *   out[row][h] = bf16( sum_j softmax_j( softmax_scale * <q, k_j> ) v_j ),  zeros where nothing is seen.  A NaN or an infinity
+ * in q makes its own row and head NaN.
  * Products with K take the codes as they are against q in two 8-bit pieces of 16 bits in all of its largest value (e4m3: two e4m3 pieces, 8 significant bits;
  * int8 with heads of 64 and many queries: q in fp16 times a power of two);
  * softmax weights are rounded to fp16 (11 bits; those below 2^-20 of a row's largest to 2^-30 of it) in front of the product with V; maxima, sums and outputs are held in fp32.

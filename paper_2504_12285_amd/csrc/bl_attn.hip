@@ -164,11 +164,12 @@ __device__ __forceinline__ void at_row_scale(float most, float& inv, float& scal
         at_power_scale(most, 134, inv, scale);
     }
 }
-__device__ __forceinline__ float at_largest(const uint32_t (&w)[8], float most, bool& nan) {
+/* The largest |value| so far, and whether one is no finite number (such a row of q gives NaN, whatever its conversion makes of it). */
+__device__ __forceinline__ float at_largest(const uint32_t (&w)[8], float most, bool& odd) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const uint32_t a = (w[i] << 16) & 0x7fffffffu, b = w[i] & 0x7fff0000u;
-        nan |= a > 0x7f800000u || b > 0x7f800000u;
+        odd |= a >= 0x7f800000u || b >= 0x7f800000u;
         most = bl_max_pos(most, bl_max_pos(__uint_as_float(a), __uint_as_float(b)));
     }
     return most;
@@ -410,20 +411,20 @@ __device__ __forceinline__ void at_few(const at_args& A, int group, uint8_t* lds
     float a_row;
     auto make_pieces = [&]() {
         float most = 0.0f;
-        bool nan = false;
+        bool odd = false;
         uint32_t w[KS][8];
 #pragma unroll
         for (int i = 0; i < KS; ++i) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) w[i][j] = raw[i][j >> 2][j & 3];
-            most = at_largest(w[i], most, nan);
+            most = at_largest(w[i], most, odd);
         }
         most = bl_max_pos(most, at_xor(most, 16));
         most = bl_max_pos(most, at_xor(most, 32));
         float inv, scale;
         at_row_scale<KIND>(most, inv, scale);
-        const uint64_t nans = __ballot(nan);
-        if (nans && ((nans >> col) & 0x0001000100010001ull)) scale = __uint_as_float(0x7fc00000u);
+        const uint64_t odds = __ballot(odd);
+        if (odds && ((odds >> col) & 0x0001000100010001ull)) scale = __uint_as_float(0x7fc00000u);
         a_row = scale * A.factor;
 #pragma unroll
         for (int i = 0; i < KS; ++i) at_pieces<KIND>(w[i], inv, qh[i], ql[i]);
@@ -872,20 +873,20 @@ __device__ __forceinline__ void at_many(const at_args& A, int place, at_many_lds
         uint32_t w[KS][8];
         const uint16_t* src = A.q + (R.row0 + qi) * A.q_stride + qh_i * D;
         float most = 0.0f;
-        bool nan = false;
+        bool odd = false;
 #pragma unroll
         for (int s = 0; s < KS; ++s) {
             const at_v4u u0 = *bl_gc<at_v4u>(src + s * 32 + half * (HALF ? 8 : 16)), u1 = *bl_gc<at_v4u>(src + s * 32 + (HALF ? 16 + half * 8 : half * 16 + 8));
 #pragma unroll
             for (int j = 0; j < 4; ++j) w[s][j] = u0[j], w[s][4 + j] = u1[j];
-            most = at_largest(w[s], most, nan);
+            most = at_largest(w[s], most, odd);
         }
         most = bl_max_pos(most, at_xor(most, 32));
         float inv, scale;
         if (HALF) at_power_scale(most, 137, inv, scale);
         else at_row_scale<KIND>(most, inv, scale);
-        const uint64_t nans = __ballot(nan);
-        if (nans && ((nans >> col) & 0x0000000100000001ull)) scale = __uint_as_float(0x7fc00000u);
+        const uint64_t odds = __ballot(odd);
+        if (odds && ((odds >> col) & 0x0000000100000001ull)) scale = __uint_as_float(0x7fc00000u);
         a_row = scale * A.factor;
 #pragma unroll
         for (int s = 0; s < KS; ++s) {

@@ -509,3 +509,20 @@ def test_more_queries_than_announced_give_no_numbers(kind, max_len, heads, count
     for i in over:
         assert bool(h.out[b.starts[i]:b.starts[i + 1]].isnan().all()), i
     b.compare(h.out, only=[i for i in range(count) if i not in over][:30])
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("value", [math.inf, -math.inf])
+@pytest.mark.parametrize("n, heads, max_len", [(1, (4, 2, 64), 0), (2, (4, 2, 128), FAR), (40, (4, 2, 64), 0), (40, (4, 2, 128), 0)])
+def test_an_infinite_query_spoils_its_own_row(kind, value, n, heads, max_len):
+    b = Batch([(200, n), (100, n)], heads, 32, kind)
+    want = b.handle(max_len=max_len)
+    want.run()
+    b.q = b.q.clone()
+    b.q[0, 1, 7] = value
+    got = b.handle(max_len=max_len)
+    got.run()
+    x, y = got.out.view(-1, *heads[::2]), want.out.view(-1, *heads[::2])
+    assert bool(x[0, 1].isnan().all())
+    x[0, 1] = y[0, 1]
+    assert torch.equal(x, y)
