@@ -6,6 +6,7 @@ libbitlinear_hip.so.  PyTorch supplies device memory and the current stream.
 There is no CPU fallback: if the library is missing, load() raises.
 """
 import ctypes
+import math
 import os
 import warnings
 
@@ -502,8 +503,8 @@ def _wants(t, what, dtype, device, shape=None, rows=False):
 
 
 def _row_stride(t):
-    """Elements from a row to the next (a single row may carry any stride)."""
-    return t.stride(0) if t.shape[0] > 1 else t[0].numel()
+    """Elements from a row to the next (a single row may carry any stride, and there may be none)."""
+    return t.stride(0) if t.shape[0] > 1 else math.prod(t.shape[1:])
 
 
 class KVCache:

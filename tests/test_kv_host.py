@@ -202,3 +202,21 @@ def test_items_need_no_room_for_partial_results(lib, more):
     assert lib.bl_attn_workspace_bytes(ctypes.byref(a)) < 1 << 20
     streams = attention(max_blocks=500, table_stride=500)
     assert lib.bl_attn_workspace_bytes(ctypes.byref(streams)) == 256 + 2048 * 2 * 16 * 130 * 4
+
+
+def test_calls_without_rows_are_refused_as_others_are(lib):
+    """No token, no request, no block: the handle stands, and the call says that it is refused."""
+    i32 = torch.int32
+
+    def new(n):
+        return [torch.zeros(n, 2, 16, 64, dtype=torch.int8), torch.zeros(n, 2, 64, 16, dtype=torch.int8), torch.zeros(n, 2), torch.zeros(n, 2)]
+    none, c = torch.zeros(0, dtype=i32), bl.KVCache(*new(3))
+    t = bl.KVTables(none, none, torch.zeros(0, 4, dtype=i32), torch.zeros(9, dtype=i32), torch.zeros(1, dtype=i32), 16, 5)
+    assert lib.bl_kv_tables(ctypes.byref(t.desc), None) in (NULL, SHAPE)
+    a = bl.KVAppend(c, torch.zeros(0, 8 * 64), 4, none)
+    assert lib.bl_kv_append(ctypes.byref(a.desc), None) in (NULL, SHAPE)
+    a = bl.KVAppend(bl.KVCache(*new(0)), torch.zeros(2, 8 * 64), 4, torch.zeros(2, dtype=i32))
+    assert lib.bl_kv_append(ctypes.byref(a.desc), None) in (NULL, SHAPE)
+    for q, b in ((0, 3), (5, 0)):
+        h = bl.KVAttention(c, torch.zeros(q, 4, 64, dtype=torch.bfloat16), torch.zeros(b + 1, dtype=i32), torch.zeros(b, dtype=i32), torch.zeros(b, 4, dtype=i32))
+        assert lib.bl_attn_kv8(ctypes.byref(h.desc), None) in (NULL, SHAPE)
