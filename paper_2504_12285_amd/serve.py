@@ -101,6 +101,9 @@ class CachedLayers:
         """x: fp32 [rows][2560], the rows of the requests' new tokens in order (rows behind them are padding); new_len: int32
         [requests], tokens that each brings, -1: it ends.  Returns the rows' hidden states (a buffer of the next step); those of a refused
         request (tables.bad of them, tables.start is -1) and of padding are zeros."""
+        for t, own, name in ((x, self.x, "x"), (new_len, self.new_len, "new_len")):
+            if t.shape != own.shape:             # (a copy would repeat a single row for all)
+                raise ValueError("%s must have the shape %s, has %s" % (name, tuple(own.shape), tuple(t.shape)))
         self.x.copy_(x)
         self.new_len.copy_(new_len)
         return self.run()

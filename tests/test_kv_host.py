@@ -220,3 +220,13 @@ def test_calls_without_rows_are_refused_as_others_are(lib):
     for q, b in ((0, 3), (5, 0)):
         h = bl.KVAttention(c, torch.zeros(q, 4, 64, dtype=torch.bfloat16), torch.zeros(b + 1, dtype=i32), torch.zeros(b, dtype=i32), torch.zeros(b, 4, dtype=i32))
         assert lib.bl_attn_kv8(ctypes.byref(h.desc), None) in (NULL, SHAPE)
+
+
+@pytest.mark.parametrize("x, new_len", [((1, 2560), (2,)), ((2560,), (2,)), ((6, 1), (2,)), ((6, 2560), (1,)), ((6, 2560), ()), ((5, 2560), (2,)), ((6, 2560), (3,))])
+def test_a_step_of_other_shapes_is_refused(lib, x, new_len):
+    """One row is no batch: it is not repeated for all of them."""
+    from paper_2504_12285_amd import serve
+    layers = serve.CachedLayers([{}], [{}], requests=2, rows=6, max_blocks=3, n_blocks=6, device="cpu")
+    with pytest.raises(ValueError):
+        layers.step(torch.ones(x), torch.ones(new_len, dtype=torch.int32))
+    assert not layers.x.any() and not layers.new_len.any()
