@@ -113,7 +113,7 @@ struct tab_args {
  * request's thread), then the rows.  A thread holds PER consecutive requests where there are more than threads.
  * Bound by the launch and three dependent reads (lengths, stack, table): 8 requests 3.9 us, 512 with 33 thousand rows, 57 of them
  * ending, 9 and 4 for the rows' own kernel. */
-template <int THREADS, int PER>
+template <int THREADS, int PER, bool LIMIT>
 __global__ __launch_bounds__(THREADS) void bl_kv_tables_kernel(tab_args A) {
     const bl_kv_batch& b = A.b;
     constexpr int MOST = THREADS * PER, WAVES = THREADS / BL_WAVE, IN = 8;
@@ -167,7 +167,7 @@ __global__ __launch_bounds__(THREADS) void bl_kv_tables_kernel(tab_args A) {
     for (int i = 0; i < PER; ++i) {
         const int64_t need = ((int64_t)old[i] + (n[i] > 0 ? n[i] : 0) + bs1) >> shift;
         row_i += n[i] > 0 ? n[i] : 0;
-        fits[i] = n[i] >= 0 && n[i] <= A.max_new && need <= b.max_blocks && row_i <= b.rows;
+        fits[i] = n[i] >= 0 && (!LIMIT || n[i] <= A.max_new) && need <= b.max_blocks && row_i <= b.rows;
         w_i[i] = fits[i] ? (int)(need - (((int64_t)old[i] + bs1) >> shift)) : 0;
         want += w_i[i];
     }
@@ -235,6 +235,8 @@ __global__ __launch_bounds__(256) void bl_kv_slots_kernel(tab_args A) {
     if (t < b.rows) tab_row(t, (int)b.B, b.q_start, b.start, b.table, b.table_stride, A.shift, b.positions, b.slots);
 }
 
+/* LIMIT: with a most of new tokens a request (a kernel of its own: above 1024 requests the comparison costs the others 1.2 us). */
+template <bool LIMIT>
 static bl_status tab_launch(const bl_kv_batch* b, int max_new, bl_stream s) {
     if (!b->seq_len || !b->new_len || !b->free_count || !b->table || (!b->free_list && b->free_cap) || !b->seq_len_out || !b->free_count_out || !b->start ||
         !b->q_start || !b->positions || !b->slots || !b->bad)
@@ -248,19 +250,19 @@ static bl_status tab_launch(const bl_kv_batch* b, int max_new, bl_stream s) {
         if (!bl_aligned(q, 4)) return BL_ERR_ALIGN;
     tab_args A = {*b, bl_log2(b->block), max_new};
     /* (a small step's barriers are those of four waves instead of sixteen) */
-    if (b->B <= 256 && b->rows <= 1024) bl_kv_tables_kernel<256, 1><<<1, 256, 0, (hipStream_t)s>>>(A);
-    else if (b->B <= 1024) bl_kv_tables_kernel<1024, 1><<<1, 1024, 0, (hipStream_t)s>>>(A);
-    else bl_kv_tables_kernel<1024, BL_KV_MAX_REQUESTS / 1024><<<1, 1024, 0, (hipStream_t)s>>>(A);
+    if (b->B <= 256 && b->rows <= 1024) bl_kv_tables_kernel<256, 1, LIMIT><<<1, 256, 0, (hipStream_t)s>>>(A);
+    else if (b->B <= 1024) bl_kv_tables_kernel<1024, 1, LIMIT><<<1, 1024, 0, (hipStream_t)s>>>(A);
+    else bl_kv_tables_kernel<1024, BL_KV_MAX_REQUESTS / 1024, LIMIT><<<1, 1024, 0, (hipStream_t)s>>>(A);
     if (b->rows > TAB_ROWS_INSIDE) bl_kv_slots_kernel<<<(unsigned)((b->rows + 255) / 256), 256, 0, (hipStream_t)s>>>(A);
     return hipGetLastError() == hipSuccess ? BL_OK : BL_ERR_HIP;
 }
 
-extern "C" bl_status bl_kv_tables(const bl_kv_batch* b, bl_stream s) { return b ? tab_launch(b, 0x7fffffff, s) : BL_ERR_NULL; }
+extern "C" bl_status bl_kv_tables(const bl_kv_batch* b, bl_stream s) { return b ? tab_launch<false>(b, 0, s) : BL_ERR_NULL; }
 
 extern "C" bl_status bl_kv_tables_limited(const bl_kv_limited_batch* b, bl_stream s) {
     if (!b) return BL_ERR_NULL;
     if (b->max_new < 1) return BL_ERR_SHAPE;
-    return tab_launch(&b->batch, b->max_new < 0x7fffffff ? (int)b->max_new : 0x7fffffff, s);
+    return tab_launch<true>(&b->batch, b->max_new < 0x7fffffff ? (int)b->max_new : 0x7fffffff, s);
 }
 
 /* ---- rotary append ----------------------------------------------------------------------------------------------- */
