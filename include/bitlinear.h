@@ -450,6 +450,7 @@ bl_status bl_kv_tables_limited(const bl_kv_limited_batch* b, bl_stream s);
  *   s = max(g, 1e-5f) * (1.0f / T); where the block holds tokens already (the first new offset is not 0): s = max(s, its old scale);
  *   code = round(clamp(x * (1.0f / s), -T, T)) to the nearest integer or e4m3 value, ties to even;
  *   the codes in front of the first new offset, if s grew: c = round(c * (old scale / s)).
+ * The cache holds no NaN: a NaN's code is that of -T.  An infinity makes s infinite, and what reads that block and head is no result.
  * So a block always has the scale of the largest value in it, at the price of one more rounding of what it held
  * each time that a new token raises it.
  * A step's tokens of one block stand in rows as far apart as their slots (consecutive rows, as bl_kv_tables gives them; rows between

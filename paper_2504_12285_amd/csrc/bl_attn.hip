@@ -23,7 +23,10 @@ typedef uint32_t at_v4u __attribute__((ext_vector_type(4)));
 #define AT_TILE 64                 /* tokens a tile */
 #define AT_THREADS 256
 #define AT_WAVES 4
-#define AT_FEW 16                  /* rows of a request and kv head up to which at_few does it */
+/* Rows of a request and kv head up to which at_few does it: the columns of its products.  Fewer by at_many, measured, us, at_few against it: heads of 128, 8 to 16
+ * rows, one request over 1000 tokens 10.4 to 11.8 against 16.5, over 8000 15.5 to 18.6 against 21, 64 over 4000 73 to 83 against 140; heads of 64, one over
+ * 1000 6.8 against 13, 64 over 4000 45 against 106 to 121; the other way only one over 8000, heads of 64, 22 to 26 against 18. */
+#define AT_FEW 16
 #define AT_MANY 128                /* rows a workgroup of at_many */
 #define AT_STREAM_GROUPS 512       /* workgroups of at_few: two a unit */
 #define AT_STREAMS (AT_STREAM_GROUPS * AT_WAVES)
@@ -641,7 +644,8 @@ __device__ __forceinline__ void at_few(const at_args& A, int group, uint8_t* lds
  * where no earlier boundary does.  A workgroup has AT_WAVES boundaries and the rows turn, turn + turns, ...  D / 4 threads
  * (a group) a partial result of a row.  The wave of the boundary does it, a row a group; where there are
  * more than AT_JOIN_ALONE the groups of all waves share those of a row and meet in LDS.  5 to 9 us: a kernel boundary and
- * two dependent reads of what other dies have just written. */
+ * two dependent reads of what other dies have just written.  Both launches with a bound of 8 / 32 / 128 parts, five heads of 128: one request over 4096
+ * tokens 14.1 / 11.5 / 11.2 us, over 16000 17.9 / 18.0 / 21.4, over 131071 41 / 41 / 51; 16 over 8192 43.9 / 38.4 / 38.4. */
 #define AT_JOIN_ALONE 32
 struct at_cut {
     int row0, rows, h, first, w0, head, ga, inner, g1, parts;   /* pieces w0 .. of `head` waves, of `inner` workgroups from ga, of waves from 4 g1 */
@@ -783,8 +787,8 @@ __device__ __forceinline__ int at_many_tiles(const at_args& A, int b) {
  * tokens, 32 + 8 heads: 417 -> 369 us; heads of 128: 388 -> 401, LDS reads).  16-byte units are XOR-ed with the row, so that sixteen
  * lanes of a read fall on all 64 banks; two buffers, one barrier a tile.
  * Bound by vector instructions (376 a wave and tile beside 1024 matrix clocks; vector units busy 52 % of the time, matrix cores
- * 32 %) where the workgroups are many: 8000 tokens of 20 + 5 heads of 128 845 TFLOP/s, e4m3 925 (a library bf16 product of 8192^3: 1224).  A prompt of
- * 4096: 120 us = 717, where the last rows' 64 tiles one after the other are all of it; cutting them in two took 145 us (the halves' 42 MB).  Products of 32 tokens x
+ * 32 %) where the workgroups are many: 8000 tokens of 20 + 5 heads of 128 832 TFLOP/s, e4m3 911 (a library bf16 product of 8192^3: 1224).  A prompt of
+ * 4096: 121 us = 711, where the last rows' 64 tiles one after the other are all of it; cutting them in two took 145 us (the halves' 42 MB).  Products of 32 tokens x
  * 32 rows (S^T) and 32 features x 32 rows (O^T): a lane has one row. */
 template <int KIND, int D>
 struct at_many_k {                  /* bytes of a K value in LDS */
@@ -1294,8 +1298,9 @@ static at_plan at_make_plan(const bl_attn_desc* a) {
      *   320 of 1500 32 and 32 / 26 and 27, of 2048 41 and 37 / 34 and 28; 1280 of 2048 106 and 120 / 74 and 79, of 4096 140 and 136;
      * heads of 64: 8 of 1024 7.7 and 11.8, 2048 10 and 11.5, 4096 16 and 12; 128 of 4096 17.2 and 19.4 / 16.5 and 17.1; 1024 of 4096 83 and 89 / 54 and 58.
      * Heads of 64 where there is an item a unit at most: eight waves, which have more loads on their way (128 of 2048 13.0 -> 11.0; 512 of 512 12.8 -> 14.6).
-     * Beside many rows (four waves then): 3 of 100 queries and one of one, 300 tokens, 19.6 -> 17.0; 4 of 200 and 252 of one, heads of 64, 48.2 -> 37.5;
-     *   but 3 of 89 and 3 of one over 1802, heads of 64, 22.1 -> 25.6.
+     * Beside many rows (four waves then), heads of 64, streams and items: 4 requests over 300 15.2 and 13.1; 16 over 1000 33 and 29, 64 28 and 26, 256 50 and 39;
+     *   256 over 2000 79 and 67; 32 over 2000 25.4 and 26.4; 6 over 1802 23.8 and 25.2; 16 over 2500 26.4 and 26.5; but 64 over 3500 60 and 58, 256 over 4000
+     *   140 and 127, where five eighths leave them to the streams.  Heads of 128: the same within 1 % over all of these.
      * Heads of 128 gain nothing from them (18 -> 19.5): four lanes that stand together read four lines of K, and a unit takes a line a clock. */
     const int64_t items = a->B * a->cache.n_kv;
     const int64_t alone = D == 128 ? items >= 1024 ? 2048 : items >= 128 ? 1536 : 1024 : items >= 128 ? 4096 : 2048;

@@ -4,8 +4,12 @@
 
 /* ---- block tables and slot maps ---------------------------------------------------------------------------------- */
 
-#define TAB_OWN 2                  /* blocks that a request's own thread takes */
-#define TAB_ROWS_INSIDE 4096       /* rows whose slots the table kernel writes itself */
+/* Blocks that a request's own thread takes; more are copied by waves.  256 requests of one / two / three / four new blocks each: by the thread 9.5 / 9.6 /
+ * 10.0 / 10.1 us, by waves 13.8 / 13.8 / 14.1 / 13.9; 8 requests 3.3 / 3.5 / 4.0 / 4.2 and 4.2 / 4.3 / 4.5 / 4.6.  (Three and four would gain, left as it is.) */
+#define TAB_OWN 2
+/* Rows whose slots the table kernel writes itself; a second launch does more.  8, 64 and 400 requests, itself against the launch: some 2000 rows
+ * 6.2, 7.1, 7.5 us against 7.6, 8.8, 10.0; 4500 rows 7.1, 8.7, 9.3 against 7.5, 9.0, 10.0; 9000 rows 9.2, 12.9, 12.6 against 7.5, 10.2, 10.1. */
+#define TAB_ROWS_INSIDE 4096
 
 template <int CTRL, int ROWS>
 __device__ __forceinline__ int64_t tab_moved(int64_t v) {
@@ -112,7 +116,7 @@ struct tab_args {
  * and returned blocks, then demand, which needs them), the copies between stack and table by waves (one or two blocks by the
  * request's thread), then the rows.  A thread holds PER consecutive requests where there are more than threads.
  * Bound by the launch and three dependent reads (lengths, stack, table): 8 requests 3.9 us, 512 with 33 thousand rows, 57 of them
- * ending, 9 and 4 for the rows' own kernel. */
+ * ending, 9 and 4 for the rows' own kernel.  Above 1024 requests (PER 4: 30 vector registers spilled) 1025 take 12.7 us, 2048 17.2, 4096 30. */
 template <int THREADS, int PER, bool LIMIT>
 __global__ __launch_bounds__(THREADS) void bl_kv_tables_kernel(tab_args A) {
     const bl_kv_batch& b = A.b;
@@ -249,7 +253,8 @@ static bl_status tab_launch(const bl_kv_batch* b, int max_new, bl_stream s) {
     for (const void* q : p)
         if (!bl_aligned(q, 4)) return BL_ERR_ALIGN;
     tab_args A = {*b, bl_log2(b->block), max_new};
-    /* (a small step's barriers are those of four waves instead of sixteen) */
+    /* A small step's barriers are those of four waves instead of sixteen: 1, 64 and 256 decoding requests 2.8, 4.4 and 5.8 us, with sixteen 4.3, 5.9 and
+     * 6.5; beside a chunk of 1024 rows the rows' loop has the more of it: 64 and 256 requests 7.6 and 9.4 us with four, 7.2 and 7.8 with sixteen. */
     if (b->B <= 256 && b->rows <= 1024) bl_kv_tables_kernel<256, 1, LIMIT><<<1, 256, 0, (hipStream_t)s>>>(A);
     else if (b->B <= 1024) bl_kv_tables_kernel<1024, 1, LIMIT><<<1, 1024, 0, (hipStream_t)s>>>(A);
     else bl_kv_tables_kernel<1024, BL_KV_MAX_REQUESTS / 1024, LIMIT><<<1, 1024, 0, (hipStream_t)s>>>(A);
@@ -616,7 +621,9 @@ extern "C" bl_status bl_kv_append(const bl_kv_tokens* t, bl_stream s) {
         return BL_ERR_ALIGN;
     app_args A = {*t, bl_log2(t->cache.block), 1, 0};
     /* rows a K/V workgroup: one where they are few (each is a run of its own in a decode step), more where they are many (the
-     * runs of prompts start in few windows, and a workgroup without one is not free) */
+     * runs of prompts start in few windows, and a workgroup without one is not free).  Windows of 1, 2, 4, 8 and 16 rows, us: 64 single tokens 5.0, 6.2,
+     * 9.4, 16, 29; 1024 of them 25, 22, 23, 24, 37; 4096 104, 88, 80, 79, 90; a prompt of 512 13, 8.4, 8.4, 8.3, 8.3; of 1024 25, 15, 11.4, 10.3, 10.1;
+     * of 4096 92, 55, 36, 26, 21. */
     while (A.window < 16 && t->T > 256 * A.window) A.window *= 2;
     A.windows = (int)((t->T + A.window - 1) / A.window);
     const hipStream_t st = (hipStream_t)s;
