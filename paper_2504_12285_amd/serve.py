@@ -37,6 +37,7 @@ class CachedLayers:
     def __init__(self, weights, gains, requests, rows, max_blocks, n_blocks, device, layout=bl.BL_LAYOUT_K16, block=64,
                  kind=bl.BL_KV_INT8, max_new=None, window=0, eps=1e-5):
         i32 = dict(dtype=torch.int32, device=device)
+        max_new = max_new or None                # (0: no limit)
         self.weights, self.gains, self.layout, self.rows, self.eps = weights, gains, layout, rows, eps
         self.buffers = ChainBuffers(rows, device)
         self.x = torch.zeros((rows, SHAPES["down"][0]), dtype=torch.float32, device=device)

@@ -230,3 +230,9 @@ def test_a_step_of_other_shapes_is_refused(lib, x, new_len):
     with pytest.raises(ValueError):
         layers.step(torch.ones(x), torch.ones(new_len, dtype=torch.int32))
     assert not layers.x.any() and not layers.new_len.any()
+
+
+def test_a_limit_of_none_stays_none(lib):
+    from paper_2504_12285_amd import serve
+    layers = serve.CachedLayers([{}], [{}], requests=2, rows=6, max_blocks=3, n_blocks=6, device="cpu", max_new=0)
+    assert isinstance(layers.tables.desc, bl.KVBatchDesc) and layers.attend[0].desc.max_q == 6
