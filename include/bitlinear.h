@@ -442,6 +442,16 @@ typedef struct {
 } bl_kv_limited_batch;
 bl_status bl_kv_tables_limited(const bl_kv_limited_batch* b, bl_stream s);
 
+/* The same for requests whose first blocks are another's too (a shared prefix): an ended request gives back the blocks of its row from
+ * held[b] on only (held [B]; negative is 0).  Row and length of such a request are set up by its owner: seq_len[b] = held[b] * block where
+ * its own tokens begin.  max_new as above; 0: no limit. */
+typedef struct {
+    bl_kv_batch batch;
+    int64_t max_new;
+    const int32_t* held;
+} bl_kv_held_batch;
+bl_status bl_kv_tables_held(const bl_kv_held_batch* b, bl_stream s);
+
 /* New tokens into the cache: row t of the fused projection [Q | K | V] ((n_q + 2 * n_kv) heads, fp32 or bf16), rotary
  * embedding on Q and K (x[i], x[i + d/2] -> x[i]*c - x[i+d/2]*s, x[i+d/2]*c + x[i]*s with c, s = cos, sin[position][i],
  * fp32 [n_pos][head_dim/2]; every operation one rounded fp32 step; cos and sin NULL: no rotation and positions unused),
@@ -474,6 +484,18 @@ typedef struct {
 } bl_kv_tokens;
 bl_status bl_kv_append(const bl_kv_tokens* t, bl_stream s);
 
+/* The same with an RMS norm of every Q and K head in front of the rotation (V is left alone): per row and head
+ *   ss = sum_i x[i]^2 with exact fp64 squares and an fp64 sum; r = fp32(1 / sqrt(ss / head_dim + eps)) in fp64; x[i] = (x[i] * r) * gain[i]
+ * (gain NULL: no second product), every product one rounded fp32 step.  An infinity or a NaN in a head makes that head's NaN or zeros, and no other's.
+ *   q_gain, k_gain  fp32 [head_dim] or NULL, 16-byte aligned, for all heads;  eps > 0 */
+typedef struct {
+    bl_kv_tokens tokens;
+    const float* q_gain;
+    const float* k_gain;
+    float eps;
+} bl_kv_norm_tokens;
+bl_status bl_kv_append_norm(const bl_kv_norm_tokens* t, bl_stream s);
+
 /* Causal attention over the cache.  Request b's queries are rows q_start[b] .. q_start[b+1]-1 of q (bf16, n_q heads; query head h reads
  * key/value head h / (n_q / n_kv)); they are its last tokens: query i of n has the position p = seq_len[b] - n + i and sees
  * the tokens 0 .. p (window > 0: p - window + 1 .. p) that are in the cache.
@@ -505,6 +527,71 @@ typedef struct {
 } bl_attn_desc;
 size_t    bl_attn_workspace_bytes(const bl_attn_desc* a);
 bl_status bl_attn_kv8(const bl_attn_desc* a, bl_stream s);
+
+/* The same where requests share long prefixes, each of which is read once for all of its requests.  Request b belongs to the group
+ * group[b] (outside 0 .. n_groups-1: to none; a group's requests need not stand together).  The tokens of its first S =
+ * shared_blocks[group[b]] blocks (taken as the nearer end outside 0 .. max_shared) are those of row group[b] of shared_table; its own row of `table` names the blocks from S on (what
+ * stands in front of them there is not read).  Everything else, and every result, is as bl_attn_kv8 has it for a table whose rows begin with the group's: lengths and
+ * positions count the prefix, causality and window hold inside it too, a request may be shorter than it.  Where the group's tables say the same, only the
+ * order of the sums is another.
+ *   shared_table   [n_groups][shared_stride], max_shared <= shared_stride entries of a row are used; its blocks are whole (every token written)
+ *   max_own        about the most tokens that a request has behind its shared blocks: sizes a split only (0: as attn.max_len)
+ *   attn.workspace bl_attn_shared_workspace_bytes(a) bytes
+ * 1 <= n_groups <= BL_KV_MAX_REQUESTS, max_shared >= 1 (max_shared * block at most 2^30). */
+typedef struct {
+    bl_attn_desc attn;
+    const int32_t* group;
+    const int32_t* shared_blocks;
+    const int32_t* shared_table;
+    int64_t shared_stride, n_groups;
+    int32_t max_shared, max_own;
+} bl_attn_shared_desc;
+size_t    bl_attn_shared_workspace_bytes(const bl_attn_shared_desc* a);
+bl_status bl_attn_kv8_shared(const bl_attn_shared_desc* a, bl_stream s);
+
+/* A MATRIX OF 8-BIT FLOATING POINT CODES (OCP e4m3) with a scale for each block of 128 x 128: what a model keeps that is not ternary, its
+ * vocabulary above all.  Weight [n][k] stands for codes[n * stride + k] * scale[n / 128 * scale_stride + k / 128] (blocks at the edges are cut off).
+ * K % 64 == 0; stride, bytes from a row to the next, a multiple of 16; codes 16-byte aligned. */
+typedef struct {
+    const uint8_t* codes;
+    const float* scale;
+    int64_t N, K, stride, scale_stride;
+} bl_f8_matrix;
+enum { BL_F8_OUT_F32 = 0, BL_F8_OUT_BF16 = 1 };
+
+/* Product with it, M >= 1 rows.  The rows X[m][k] are the bf16 values of a producer (norm included, as for the BitLinears); each group of 128
+ * consecutive k of a row gets a scale of its own:
+ *   g = max |X| of the group; s = max(g, 1e-5f) * (1.0f / 448.0f); code = e4m3(X * (1.0f / s)), every step one rounded fp32
+ *   operation, ties to even;
+ *   y[m][n] = sum over the groups b of (s[m][b] * scale[n / 128][b]) * sum_k code[m][k] * codes[n][k], in fp32, then to the output's type.
+ * A row with a NaN or an infinity in it is NaN.
+ *   y          fp32 or bf16 [M][N], rows y_stride values apart (16-byte aligned rows are faster)
+ *   workspace  bl_f8_workspace_bytes(p) bytes, 256-byte aligned; no content is expected
+ * M, N, K <= 2^24 and (M / 128) * (N / 128) * 16 < 2^31, both rounded up. */
+typedef struct {
+    bl_f8_matrix w;
+    bl_producer prod;
+    int64_t M, y_stride;
+    void* y;
+    int32_t y_kind;
+    void* workspace;
+} bl_f8_product;
+size_t    bl_f8_workspace_bytes(const bl_f8_product* p);
+bl_status bl_f8_linear(const bl_f8_product* p, bl_stream s);
+
+/* Rows of it: out[t][k] = (codes[ids[t]][k] * scale) * multiplier, each one rounded fp32 step, then to the output's type.  An id outside
+ * 0 .. N-1: zeros, and *bad (1 int or NULL) is INCREASED by one, but for -1 (no token).
+ *   out  fp32 or bf16 [T][K], rows out_stride values apart, 16-byte aligned.  1 <= T <= 2^24. */
+typedef struct {
+    bl_f8_matrix w;
+    const int32_t* ids;
+    int64_t T, out_stride;
+    void* out;
+    int32_t out_kind;
+    float multiplier;
+    int32_t* bad;
+} bl_f8_lookup;
+bl_status bl_f8_embed(const bl_f8_lookup* l, bl_stream s);
 
 /* Test hook: which decode kernel the M <= 64 entry points take, so that tests can put every
  * kernel through every case.  0 = the measured default, 1 = the dot4 kernel where it applies

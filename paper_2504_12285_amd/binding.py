@@ -43,9 +43,16 @@ SIGNATURES = {
     "bl_stack_run": (_ci, [_vp, _vp, _vp]),
     "bl_kv_tables": (_ci, [_vp, _vp]),
     "bl_kv_tables_limited": (_ci, [_vp, _vp]),
+    "bl_kv_tables_held": (_ci, [_vp, _vp]),
     "bl_kv_append": (_ci, [_vp, _vp]),
+    "bl_kv_append_norm": (_ci, [_vp, _vp]),
     "bl_attn_workspace_bytes": (_sz, [_vp]),
     "bl_attn_kv8": (_ci, [_vp, _vp]),
+    "bl_attn_shared_workspace_bytes": (_sz, [_vp]),
+    "bl_attn_kv8_shared": (_ci, [_vp, _vp]),
+    "bl_f8_workspace_bytes": (_sz, [_vp]),
+    "bl_f8_linear": (_ci, [_vp, _vp]),
+    "bl_f8_embed": (_ci, [_vp, _vp]),
     "bl_debug_force_path": (_ci, [_ci]),
     "bl_probe_stream_read": (_ci, [_vp, _sz, _ci, _vp, _vp]),
     "bl_probe_stream_write": (_ci, [_vp, _i64, _i64, _ci, _vp]),
@@ -124,11 +131,21 @@ class KVLimitedBatchDesc(ctypes.Structure):
     _fields_ = [("batch", KVBatchDesc), ("max_new", _i64)]
 
 
+class KVHeldBatchDesc(ctypes.Structure):
+    """Mirror of bl_kv_held_batch."""
+    _fields_ = [("batch", KVBatchDesc), ("max_new", _i64), ("held", _vp)]
+
+
 class KVTokensDesc(ctypes.Structure):
     """Mirror of bl_kv_tokens."""
     _fields_ = [("cache", KVCacheDesc), ("qkv", _vp), ("qkv_stride", _i64), ("q_stride", _i64), ("T", _i64), ("n_pos", _i64),
                 ("qkv_kind", ctypes.c_int32), ("n_q", ctypes.c_int32)] + \
                [(n, _vp) for n in ("positions", "slots", "cos", "sin", "q_out", "bad")]
+
+
+class KVNormTokensDesc(ctypes.Structure):
+    """Mirror of bl_kv_norm_tokens."""
+    _fields_ = [("tokens", KVTokensDesc), ("q_gain", _vp), ("k_gain", _vp), ("eps", ctypes.c_float)]
 
 
 class AttnDesc(ctypes.Structure):
@@ -137,6 +154,31 @@ class AttnDesc(ctypes.Structure):
                 ("T", _i64), ("q_start", _vp), ("seq_len", _vp), ("table", _vp)] + \
                [(n, ctypes.c_int32) for n in ("n_q", "max_blocks", "max_q", "max_len", "window")] + \
                [("softmax_scale", ctypes.c_float), ("out", _vp), ("workspace", _vp)]
+
+
+class AttnSharedDesc(ctypes.Structure):
+    """Mirror of bl_attn_shared_desc."""
+    _fields_ = [("attn", AttnDesc), ("group", _vp), ("shared_blocks", _vp), ("shared_table", _vp), ("shared_stride", _i64), ("n_groups", _i64),
+                ("max_shared", ctypes.c_int32), ("max_own", ctypes.c_int32)]
+
+
+BL_F8_OUT_F32, BL_F8_OUT_BF16 = 0, 1
+
+
+class F8MatrixDesc(ctypes.Structure):
+    """Mirror of bl_f8_matrix."""
+    _fields_ = [("codes", _vp), ("scale", _vp), ("N", _i64), ("K", _i64), ("stride", _i64), ("scale_stride", _i64)]
+
+
+class F8ProductDesc(ctypes.Structure):
+    """Mirror of bl_f8_product."""
+    _fields_ = [("w", F8MatrixDesc), ("prod", Producer), ("M", _i64), ("y_stride", _i64), ("y", _vp), ("y_kind", ctypes.c_int32), ("workspace", _vp)]
+
+
+class F8LookupDesc(ctypes.Structure):
+    """Mirror of bl_f8_lookup."""
+    _fields_ = [("w", F8MatrixDesc), ("ids", _vp), ("T", _i64), ("out_stride", _i64), ("out", _vp), ("out_kind", ctypes.c_int32),
+                ("multiplier", ctypes.c_float), ("bad", _vp)]
 
 
 class BitLinearError(RuntimeError):
@@ -235,7 +277,8 @@ def _first_native():
         return _native
     _bl_torch.bind(*(ctypes.cast(fn, _vp).value for fn in (lib.bl_quant_act_int8, lib.bl_gemv_w158a8,
                                                             lib.bl_gemm_w158a8, lib.bl_bitlinear_decode, lib.bl_stack_run)))
-    _bl_torch.bind_kv(*(ctypes.cast(fn, _vp).value for fn in (lib.bl_kv_tables, lib.bl_kv_append, lib.bl_attn_kv8, lib.bl_kv_tables_limited)))
+    _bl_torch.bind_kv(*(ctypes.cast(fn, _vp).value for fn in (lib.bl_kv_tables, lib.bl_kv_append, lib.bl_attn_kv8, lib.bl_kv_tables_limited, lib.bl_kv_tables_held,
+                                                               lib.bl_kv_append_norm, lib.bl_attn_kv8_shared, lib.bl_f8_linear, lib.bl_f8_embed)))
     _native = _bl_torch
     return _native
 
@@ -553,10 +596,11 @@ class KVTables(_KVCall):
     """Block tables and slot maps of a step (bl_kv_tables).  seq_len, new_len int32 [B]; table int32 [B][max_blocks];
     free_list int32 [any]; free_count int32 [1]; rows: rows of the batch.  Outputs: start, q_start, positions, slots, bad, and
     seq_len_out, free_count_out (in_place: seq_len and free_count themselves, for a step that is run again and again).
-    max_new: a request that brings more tokens is refused (bl_kv_tables_limited); None: no such limit."""
+    max_new: a request that brings more tokens is refused (bl_kv_tables_limited); None: no such limit.
+    held: int32 [B], blocks in front of each row that an ended request does not give back (bl_kv_tables_held)."""
     _which, _where = 0, "bl_kv_tables"
 
-    def __init__(self, seq_len, new_len, table, free_list, free_count, block, rows, in_place=False, max_new=None):
+    def __init__(self, seq_len, new_len, table, free_list, free_count, block, rows, in_place=False, max_new=None, held=None):
         torch = _get_torch()
         i32, dev, B = torch.int32, seq_len.device, seq_len.shape[0]
         _wants(seq_len, "seq_len", i32, dev, (B,))
@@ -573,7 +617,14 @@ class KVTables(_KVCall):
         self.desc = KVBatchDesc(B, rows, _row_stride(table), free_list.shape[0], block, table.shape[1],
                                 *(_ptr(t) for t in (seq_len, new_len, free_count, table, free_list, self.seq_len_out, self.free_count_out,
                                                     self.start, self.q_start, self.positions, self.slots, self.bad)))
-        if max_new is not None:
+        self.held = held
+        if held is not None:
+            _wants(held, "held", i32, dev, (B,))
+            if max_new is not None and max_new < 1:
+                raise ValueError("max_new must be at least 1, is %d" % max_new)
+            self._which, self._where = 4, "bl_kv_tables_held"
+            self.desc = KVHeldBatchDesc(self.desc, 0 if max_new is None else max_new, _ptr(held))
+        elif max_new is not None:
             self._which, self._where = 3, "bl_kv_tables_limited"
             self.desc = KVLimitedBatchDesc(self.desc, max_new)
 
@@ -607,6 +658,19 @@ class KVAppend(_KVCall):
                                  *(_ptr(t) for t in (positions, slots, cos, sin, q, bad)))
 
 
+class KVNormAppend(KVAppend):
+    """KVAppend with an RMS norm of every Q and K head in front of the rotation (bl_kv_append_norm).  q_gain, k_gain: fp32 [head_dim] or None."""
+    _which, _where = 5, "bl_kv_append_norm"
+
+    def __init__(self, cache, qkv, n_q, slots, positions=None, cos=None, sin=None, q=None, bad=None, q_gain=None, k_gain=None, eps=1e-5):
+        super().__init__(cache, qkv, n_q, slots, positions, cos, sin, q, bad)
+        for t, name in ((q_gain, "q_gain"), (k_gain, "k_gain")):
+            if t is not None:
+                _wants(t, name, _get_torch().float32, cache.k.device, (cache.head_dim,))
+        self.q_gain, self.k_gain = q_gain, k_gain
+        self.desc = KVNormTokensDesc(self.desc, _ptr(q_gain), _ptr(k_gain), eps)
+
+
 class KVAttention(_KVCall):
     """Causal attention over the cache (bl_attn_kv8).  q bf16 [T][n_q][head_dim] (or [T][n_q * head_dim] with n_q); q_start int32 [B + 1],
     seq_len int32 [B], table int32 [B][max_blocks].  max_q: no request has more queries (None: all T rows may be one request's; rows of
@@ -631,10 +695,128 @@ class KVAttention(_KVCall):
         self.desc = AttnDesc(cache.desc, _ptr(q), _row_stride(q), _row_stride(out), _row_stride(table), B, T, _ptr(q_start), _ptr(seq_len),
                              _ptr(table), n_q, table.shape[1], T if max_q is None else max_q, max_len, window, dim ** -0.5 if softmax_scale is None else softmax_scale,
                              _ptr(out), None)
-        nbytes = load().bl_attn_workspace_bytes(ctypes.byref(self.desc))
-        if workspace is None:
-            workspace = _workspace(nbytes, dev)
-        elif _wants(workspace, "workspace", torch.uint8, dev).numel() < nbytes:
-            raise ValueError("workspace of %d bytes, %d are needed" % (workspace.numel(), nbytes))
-        self.workspace = workspace
-        self.desc.workspace = _ptr(workspace)
+        self._space(workspace, dev)
+
+    def _space(self, workspace, dev):
+        self.workspace = _space_of(load().bl_attn_workspace_bytes(ctypes.byref(self.desc)), workspace, dev)
+        self.desc.workspace = _ptr(self.workspace)
+
+
+def _space_of(nbytes, workspace, dev):
+    """A workspace of nbytes: the caller's, if it is large enough, or a new one."""
+    if workspace is None:
+        return _workspace(nbytes, dev)
+    if _wants(workspace, "workspace", _get_torch().uint8, dev).numel() < nbytes:
+        raise ValueError("workspace of %d bytes, %d are needed" % (workspace.numel(), nbytes))
+    return workspace
+
+
+class KVSharedAttention(KVAttention):
+    """KVAttention where requests share prefixes, each read once for all of its requests (bl_attn_kv8_shared).  group: int32 [B], the group of
+    each request (outside 0 .. n_groups - 1: none); shared_table int32 [n_groups][max_shared], shared_blocks int32 [n_groups]: the blocks of a
+    group's prefix.  max_own: about the most tokens of a request behind its prefix.  Everything else is KVAttention's."""
+    _which, _where = 6, "bl_attn_kv8_shared"
+
+    def __init__(self, cache, q, q_start, seq_len, table, group, shared_table, shared_blocks, n_q=None, max_q=None, max_len=0, max_own=0,
+                 softmax_scale=None, window=0, out=None, workspace=None):
+        i32, dev = _get_torch().int32, cache.k.device
+        _wants(group, "group", i32, dev, (seq_len.shape[0],))
+        _wants(shared_table, "shared_table", i32, dev, (None, None), rows=True)
+        _wants(shared_blocks, "shared_blocks", i32, dev, (shared_table.shape[0],))
+        self.group, self.shared_table, self.shared_blocks, self.max_own = group, shared_table, shared_blocks, max_own
+        super().__init__(cache, q, q_start, seq_len, table, n_q, max_q, max_len, softmax_scale, window, out, workspace)
+
+    def _space(self, workspace, dev):
+        t = self.shared_table
+        self.desc = AttnSharedDesc(self.desc, _ptr(self.group), _ptr(self.shared_blocks), _ptr(t), _row_stride(t), t.shape[0], t.shape[1], self.max_own)
+        self.workspace = _space_of(load().bl_attn_shared_workspace_bytes(ctypes.byref(self.desc)), workspace, dev)
+        self.desc.attn.workspace = _ptr(self.workspace)
+
+
+class F8Matrix:
+    """A matrix of 8-bit floating point codes (bl_f8_matrix): codes float8_e4m3fn [N][K] (rows may lie apart), scale fp32
+    [ceil(N / 128)][ceil(K / 128)], one for each block of 128 x 128."""
+
+    def __init__(self, codes, scale):
+        torch = _get_torch()
+        if codes.dim() != 2:
+            raise ValueError("codes must be [N][K]")
+        N, K = codes.shape
+        _wants(codes, "codes", torch.float8_e4m3fn, codes.device, rows=True)
+        _wants(scale, "scale", torch.float32, codes.device, (-(-N // 128), -(-K // 128)), rows=True)
+        self.codes, self.scale, self.N, self.K = codes, scale, N, K
+        self.desc = F8MatrixDesc(_ptr(codes), _ptr(scale), N, K, _row_stride(codes), _row_stride(scale))
+
+    @classmethod
+    def quantise(cls, W):
+        """Codes and scales of a matrix of numbers, once when a model is loaded: a block's scale is its largest |value| / 448."""
+        torch = _get_torch()
+        N, K = W.shape
+        high, wide = -(-N // 128), -(-K // 128)
+        codes = torch.empty((N, K), dtype=torch.float8_e4m3fn, device=W.device)
+        scale = torch.empty((high, wide), dtype=torch.float32, device=W.device)
+        for i in range(0, high, 64):                             # (a vocabulary's matrix in 32 bits is not made whole)
+            part = W[128 * i:128 * (i + 64)].float()
+            rows = -(-part.shape[0] // 128)
+            x = torch.zeros((rows * 128, wide * 128), dtype=torch.float32, device=W.device)
+            x[:part.shape[0], :K] = part
+            x = x.view(rows, 128, wide, 128)
+            s = x.abs().amax((1, 3), keepdim=True).clamp(min=1e-12) / 448.0
+            codes[128 * i:128 * i + part.shape[0]] = (x / s).clamp(-448.0, 448.0).view(rows * 128, wide * 128)[:part.shape[0], :K].to(codes.dtype)
+            scale[i:i + rows] = s[:, 0, :, 0]
+        return cls(codes, scale)
+
+
+def _f8_kind(dtype):
+    torch = _get_torch()
+    if dtype not in (torch.float32, torch.bfloat16):
+        raise TypeError("outputs are float32 or bfloat16, not %s" % dtype)
+    return BL_F8_OUT_F32 if dtype == torch.float32 else BL_F8_OUT_BF16
+
+
+class F8Linear(_KVCall):
+    """y = rows times the matrix's transpose (bl_f8_linear).  x: bf16 or fp32 [M][K], with norm=True normalised on the way (gain fp32 [K] or
+    None); or prod, a producer of make_producer whose tensors the caller keeps, and M.  Output: y [M][N] of `dtype` (or of y's).  The workspace
+    may serve several handles whose runs follow each other on one stream."""
+    _which, _where = 7, "bl_f8_linear"
+
+    def __init__(self, matrix, x=None, y=None, dtype=None, norm=False, gain=None, eps=1e-5, workspace=None, prod=None, M=None):
+        torch = _get_torch()
+        dev = matrix.codes.device
+        if (x is None) == (prod is None) or (prod is None) != (M is None):
+            raise ValueError("x, or prod and M")
+        if x is not None:
+            if x.dtype not in (torch.float32, torch.bfloat16):
+                raise TypeError("x must be float32 or bfloat16")
+            _wants(x, "x", x.dtype, dev, (None, matrix.K))
+            if gain is not None:
+                _wants(gain, "gain", torch.float32, dev, (matrix.K,))
+            M = x.shape[0]
+            prod = make_producer(BL_PROD_F32 if x.dtype == torch.float32 else BL_PROD_BF16, x, norm=norm, gain=gain, eps=eps)
+        if y is None:
+            y = torch.empty((M, matrix.N), dtype=torch.float32 if dtype is None else dtype, device=dev)
+        else:
+            _wants(y, "y", y.dtype if dtype is None else dtype, dev, (M, matrix.N), rows=True)
+        self.matrix, self.x, self.gain, self.y = matrix, x, gain, y
+        self.desc = F8ProductDesc(matrix.desc, prod, M, _row_stride(y), _ptr(y), _f8_kind(y.dtype), None)
+        self.workspace = _space_of(load().bl_f8_workspace_bytes(ctypes.byref(self.desc)), workspace, dev)
+        self.desc.workspace = _ptr(self.workspace)
+
+
+class F8Embedding(_KVCall):
+    """Rows of the matrix times a number (bl_f8_embed).  ids: int32 [T]; those outside the matrix give zeros, and but for -1 are counted in bad
+    (int32 [1] or None).  Output: out [T][K] of `dtype` (or of out's)."""
+    _which, _where = 8, "bl_f8_embed"
+
+    def __init__(self, matrix, ids, out=None, dtype=None, multiplier=1.0, bad=None):
+        torch = _get_torch()
+        dev = matrix.codes.device
+        _wants(ids, "ids", torch.int32, dev, (None,))
+        if out is None:
+            out = torch.empty((ids.shape[0], matrix.K), dtype=torch.float32 if dtype is None else dtype, device=dev)
+        else:
+            _wants(out, "out", out.dtype if dtype is None else dtype, dev, (ids.shape[0], matrix.K), rows=True)
+        if bad is not None:
+            _wants(bad, "bad", torch.int32, dev, (1,))
+        self.matrix, self.ids, self.out, self.bad = matrix, ids, out, bad
+        self.desc = F8LookupDesc(matrix.desc, _ptr(ids), ids.shape[0], _row_stride(out), _ptr(out), _f8_kind(out.dtype), multiplier, _ptr(bad))

@@ -52,6 +52,13 @@ struct at_args {
     int few_rows;                  /* rows of a request and kv head up to which at_few does it: AT_FEW, or 0 where it is not launched */
     int splits;                    /* of at_many */
     int part_skip;                 /* floats in front of the partial results of at_few: where each request's tiles end */
+    /* of prefixes that requests share (bl_attn_kv8_shared) */
+    const int* group;
+    const int* shared_blocks;
+    const int* shared_table;
+    int64_t shared_stride;
+    int2* pieces;                  /* [T] of each row: partial results of its group's prefix, and of its own tokens (-1: no numbers) */
+    int n_groups, max_shared, group_splits, few_splits;
 };
 
 /* ---- what both kernels share --------------------------------------------------------------------------------------- */
@@ -62,6 +69,7 @@ __device__ __forceinline__ float at_xor(float v, int m) { return __shfl_xor(v, m
 /* A request: queries, tokens, and the tiles that its queries i0..i1 can see. */
 struct at_request {
     int row0, n, len;
+    int skip = 0;                  /* tokens in front that its group has */
 };
 __device__ __forceinline__ at_request at_read(const at_args& A, int b) {
     at_request r;
@@ -73,10 +81,22 @@ __device__ __forceinline__ at_request at_read(const at_args& A, int b) {
     r.len = L < 0 ? 0 : L > A.max_tokens ? A.max_tokens : L;
     return r;
 }
+/* Tokens of group g's prefix; 0 where there is no such group. */
+__device__ __forceinline__ int at_shared_tokens(const at_args& A, int g) {
+    if ((unsigned)g >= (unsigned)A.n_groups) return 0;
+    const int s = A.shared_blocks[g];
+    return (s < 0 ? 0 : s > A.max_shared ? A.max_shared : s) << A.shift;
+}
+template <bool SHARED>
+__device__ __forceinline__ at_request at_read_own(const at_args& A, int b) {
+    at_request r = at_read(A, b);
+    if (SHARED) r.skip = at_shared_tokens(A, A.group[b]);
+    return r;
+}
 /* First token that query i sees, and the one behind its last. */
 __device__ __forceinline__ int at_from(const at_args& A, const at_request& r, int i) {
-    const int p = r.len - r.n + i - A.window + 1;
-    return A.window && p > 0 ? p : 0;
+    const int p = r.len - r.n + i - A.window + 1, f = A.window && p > 0 ? p : 0;
+    return f > r.skip ? f : r.skip;
 }
 __device__ __forceinline__ int at_to(const at_request& r, int i) {
     const int e = r.len - r.n + i + 1;
@@ -229,6 +249,14 @@ __device__ __forceinline__ void at_no_rows(const at_args& A, const at_request& r
     for (int64_t i = thread; i < (int64_t)r.n * units; i += threads)
         *bl_g((at_v4u*)(A.out + (r.row0 + i / units) * A.out_stride + (int64_t)h * A.G * D + i % units * 8)) = (at_v4u){0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u};
 }
+/* Tiles of a piece where `tiles` are split, and how many pieces have some. */
+__device__ __forceinline__ int at_piece(int tiles, int splits) { return (tiles + splits - 1) / splits; }
+__device__ __forceinline__ int at_piece_count(int tiles, int splits) {
+    const int each = at_piece(tiles, splits);
+    return each ? (tiles + each - 1) / each : 0;
+}
+/* Where piece `piece` of (row, head) stands among the partial results: at * D values, and at * 2 for its reference and sum behind all of these. */
+__device__ __forceinline__ int64_t at_part_at(const at_args& A, int piece, int row, int head) { return ((int64_t)piece * A.T + row) * A.n_q + head; }
 /* Tiles a wave does, of `all` in the launch. */
 __device__ __forceinline__ int at_share(int all) {
     const int s = (all + AT_STREAMS - 1) / AT_STREAMS;
@@ -244,6 +272,7 @@ struct at_slot {                    /* a wave's partial result: rows x (D sums, 
  * workspace (at most two such: at its ends) and bl_attn_join adds it up.  The four pieces of a workgroup that lie in one item
  * (at_together) are taken tile by tile in turn instead, and meet in LDS: a quarter of the partial results.
  * ITEM (0, or the waves of a workgroup): a workgroup has one item whole, so that nothing is left to join (short contexts).
+ * SHARED: a workgroup has one of `few_splits` pieces of what an item has behind its group's prefix, and leaves a partial result.
  * ALONE: no at_many stands beside it; requests of more than AT_FEW rows then get no numbers (in the streams' form a lane's own work: an error's speed).
  * K rows of a tile go straight from memory into the registers that the matrix cores read (four 16 x 128 products of
  * codes against the two pieces of q), then V the same way.  V of a tile and K of the next are in flight while one computes,
@@ -273,7 +302,7 @@ union at_stream_lds {
 struct at_spot {
     int b, h, t, c, tile0;          /* request, kv head, tile of c, first tile */
 };
-template <int KIND, int D, bool WIDE, int ITEM, bool ALONE>
+template <int KIND, int D, bool WIDE, int ITEM, bool ALONE, bool SHARED = false>
 __device__ __forceinline__ void at_few(const at_args& A, int group, uint8_t* lds_bytes) {
     constexpr int KS = D / 64, DT = D / 16, WAVES = ITEM ? ITEM : AT_WAVES;     /* 64-byte steps of a K row, 16-feature tiles of V */
     at_few_lds<D>& lds = *(at_few_lds<D>*)lds_bytes;
@@ -313,16 +342,31 @@ __device__ __forceinline__ void at_few(const at_args& A, int group, uint8_t* lds
         cur.h = r / cur.c, cur.t = r % cur.c;
         return before + cur.h * cur.c;
     };
+    int piece = 0;
     if constexpr (ITEM) {
+        if (SHARED) piece = group % A.few_splits, group /= A.few_splits;
         cur.b = group / A.n_kv, cur.h = group % A.n_kv;
-        mine = at_read(A, cur.b);
-        mine = {at_uniform(mine.row0), at_uniform(mine.n), at_uniform(mine.len)};
+        mine = at_read_own<SHARED>(A, cur.b);
+        mine = {at_uniform(mine.row0), at_uniform(mine.n), at_uniform(mine.len), SHARED ? at_uniform(mine.skip) : 0};
         cur.c = at_few_tiles(A, mine), cur.t = wave;
         if (!cur.c) {
-            if (ALONE) at_no_rows<D>(A, mine, cur.h, tid, WAVES * BL_WAVE);
+            if (SHARED) {
+                if (ALONE && piece == 0 && cur.h == 0)
+                    for (int i = tid; i < mine.n; i += AT_THREADS) A.pieces[mine.row0 + i] = make_int2(-1, -1);
+            } else if (ALONE) {
+                at_no_rows<D>(A, mine, cur.h, tid, WAVES * BL_WAVE);
+            }
             return;
         }
         cur.tile0 = at_from(A, mine, 0) / AT_TILE;
+        if (SHARED) {
+            const int each = at_piece(cur.c, A.few_splits), all = cur.c;
+            if (piece == 0 && cur.h == 0 && tid < mine.n)
+                A.pieces[mine.row0 + tid] = make_int2(at_piece_count((mine.skip + AT_TILE - 1) / AT_TILE, A.group_splits), at_piece_count(all, A.few_splits));
+            cur.tile0 += piece * each;
+            cur.c = all - piece * each < each ? all - piece * each : each;
+            if (cur.c <= 0) return;
+        }
         count = (cur.c - wave + WAVES - 1) / WAVES;     /* (none for some waves of a short item: they bring nothing to the meeting) */
     } else {
         /* where each request's tiles end: up to 64 requests by every wave for itself, a lane each, more through LDS */
@@ -388,7 +432,7 @@ __device__ __forceinline__ void at_few(const at_args& A, int group, uint8_t* lds
     /* (sixteen tokens in front of all windows are not there: their block may be another's by now, and a NaN in it times a weight of 0 is none) */
     auto read_blocks = [&](const at_spot& s) -> blocks {
         const at_request r = request(s.b);
-        const int tok = (s.tile0 + s.t) * AT_TILE, low = at_from(A, r, 0) - 15;
+        const int tok = (s.tile0 + s.t) * AT_TILE, low = at_from(A, r, 0) - 15;     /* (a prefix ends with a block: at a multiple of sixteen) */
         const int* pages = A.table + s.b * A.table_stride;
         auto seen = [&](int t) { return t < r.len && t >= low; };
         return {seen(tok + kgrp) ? pages[(tok + kgrp) >> A.shift] : -1, seen(tok + 16 * grp) ? pages[(tok + 16 * grp) >> A.shift] : -1};
@@ -627,7 +671,13 @@ __device__ __forceinline__ void at_few(const at_args& A, int group, uint8_t* lds
 #pragma unroll
         for (int j = 0; j < PER; ++j) y[j] += meet.o[w][r][d0 + j] * f;
     }
-    if (ITEM || alone) {
+    if (SHARED) {
+        const int64_t at = at_part_at(A, A.group_splits + piece, R.row0 + r / A.G, cur.h * A.G + r % A.G);
+        float* to = A.many_part + at * D + d0;
+#pragma unroll
+        for (int j = 0; j < PER; j += 4) *bl_g((bl_v4f*)(to + j)) = (bl_v4f){y[j], y[j + 1], y[j + 2], y[j + 3]};
+        if (d0 == 0) *bl_g((bl_v2f*)(A.many_part + (int64_t)A.splits * A.T * A.n_q * D + 2 * at)) = (bl_v2f){top, sum};
+    } else if (ITEM || alone) {
         const float inv = sum == 0.0f ? 0.0f : bl_div_rn(1.0f, sum);
         uint32_t* to = (uint32_t*)(A.out + (R.row0 + r / A.G) * A.out_stride + (cur.h * A.G + r % A.G) * D + d0);
 #pragma unroll
@@ -802,9 +852,15 @@ struct at_many_lds {
     };
     uint8_t k[2][AT_TILE * D * at_many_k<KIND, D>::bytes];
     int scan[AT_WAVES];
+    int2 query[AT_MANY];                                    /* AT_PREFIX: row and position of the tile's queries */
+    int2 ends[AT_WAVES];
 };
-template <int KIND, int D>
+/* What a workgroup of at_many has: rows of a request over all that they see; over what stands behind their group's prefix (AT_OWN); or rows of all
+ * requests of a group over its prefix (AT_PREFIX), which are gathered: their places in the batch are found by each workgroup, by sums over the requests. */
+enum { AT_ALL, AT_OWN, AT_PREFIX };
+template <int KIND, int D, int MODE = AT_ALL>
 __device__ __forceinline__ void at_many(const at_args& A, int place, at_many_lds<KIND, D>& lds) {
+    const int splits = MODE == AT_PREFIX ? A.group_splits : MODE == AT_OWN ? A.splits - A.group_splits : A.splits;
     constexpr bool HALF = at_many_k<KIND, D>::bytes == 2;
     constexpr int KROW = D * at_many_k<KIND, D>::bytes;        /* bytes of a K row in LDS, 16-byte units XOR-ed by k_mix(row) */
     constexpr int KS = D / 32, DT = D / 32;
@@ -818,12 +874,34 @@ __device__ __forceinline__ void at_many(const at_args& A, int place, at_many_lds
     auto take = [&](int all) {
         /* Heads of 128: of the 512 workgroups that the chip holds the second 256 go the other way round, so that a unit has a heavy
          * one and a light one: two prompts of 1600 tokens 72 -> 57 us, one of 6000 244 -> 236 (heads of 64, three to a unit: 52 -> 58). */
-        const int n = all * A.n_kv * A.splits, both = n < 512 ? n : 512;
+        const int n = all * A.n_kv * splits, both = n < 512 ? n : 512;
         if (D == 128 && place >= 256 && place < both) place = 255 + both - place;
-        piece = place % A.splits, h = place / A.splits % A.n_kv, want = place / A.splits / A.n_kv;
+        piece = place % splits, h = place / splits % A.n_kv, want = place / splits / A.n_kv;
         return place < n;
     };
-    if (A.B <= 64) {
+    if constexpr (MODE == AT_PREFIX) {
+        /* tiles of every group, then the group that has this one */
+        int* s_upto = lds.upto;
+        for (int g = tid; g < A.n_groups; g += AT_THREADS) s_upto[g] = 0;
+        __syncthreads();
+        for (int i = tid; i < A.B; i += AT_THREADS) {
+            const int g = A.group[i], n = at_read(A, i).n;
+            if ((unsigned)g < (unsigned)A.n_groups && n) atomicAdd(&s_upto[g], n);
+        }
+        __syncthreads();
+        at_sums(A.n_groups, [&](int g) { return at_shared_tokens(A, g) ? (int)(((int64_t)s_upto[g] * A.G + AT_MANY - 1) / AT_MANY) : 0; }, s_upto, lds.scan);
+        if (!take(at_uniform(s_upto[A.n_groups - 1]))) return;
+        int lo = -1, hi = A.n_groups - 1;
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (s_upto[mid] > want) hi = mid;
+            else lo = mid;
+        }
+        b = at_uniform(hi);
+        before = b ? at_uniform(s_upto[b - 1]) : 0;
+        c = at_uniform(s_upto[b]) - before;
+        __syncthreads();
+    } else if (A.B <= 64) {
         const int upto = at_scan(lane < A.B ? at_many_tiles(A, lane) : 0);
         if (!take(__builtin_amdgcn_readlane(upto, 63))) return;
         b = __builtin_ctzll(__ballot(upto > want));
@@ -845,29 +923,76 @@ __device__ __forceinline__ void at_many(const at_args& A, int place, at_many_lds
         __syncthreads();
     }
     const int rt = c - 1 - (want - before);                  /* the last rows see most: first */
-    const at_request R = at_read(A, b);
-    const int rows = R.n * A.G, bs1 = (1 << A.shift) - 1;
-    const int rbase = rt * AT_MANY, rend = rbase + AT_MANY < rows ? rbase + AT_MANY : rows;
-    const int tok0 = at_from(A, R, rbase / A.G), tok1 = at_to(R, (rend - 1) / A.G);
-    int tile = tok0 / AT_TILE, tend = (tok1 + AT_TILE - 1) / AT_TILE;
-    if (tend < tile) tend = tile;
-    {
-        const int n = (tend - tile + A.splits - 1) / A.splits;
-        tile += piece * n;
-        tend = tile + n < tend ? tile + n : tend;
+    at_request R;
+    if constexpr (MODE == AT_PREFIX) R = {0, 0, at_shared_tokens(A, b)};
+    else R = at_read_own<MODE == AT_OWN>(A, b);
+    const int bs1 = (1 << A.shift) - 1;
+    int rows = R.n * A.G;
+    if constexpr (MODE == AT_PREFIX) {
+        /* the group's queries, request by request: those of this tile */
+        auto news = [&](int i) { return A.group[i] == b ? at_read(A, i).n : 0; };
+        at_sums(A.B, news, lds.upto, lds.scan);
+        const int queries = at_uniform(lds.upto[A.B - 1]);
+        rows = queries * A.G;
+        const int q0 = rt * AT_MANY / A.G, q1 = (rt * AT_MANY + AT_MANY - 1) / A.G + 1;
+        for (int i = tid; i < A.B; i += AT_THREADS) {
+            const int end = lds.upto[i], begin = i ? lds.upto[i - 1] : 0;
+            if (end <= q0 || begin >= q1 || end == begin) continue;
+            const at_request r = at_read(A, i);
+            for (int j = begin > q0 ? begin : q0; j < (end < q1 ? end : q1); ++j) lds.query[j - q0] = make_int2(r.row0 + j - begin, r.len - r.n + j - begin);
+        }
+        __syncthreads();
     }
-    const int* pages = A.table + b * A.table_stride;
-
-    /* this lane's row */
+    const int rbase = rt * AT_MANY, rend = rbase + AT_MANY < rows ? rbase + AT_MANY : rows;
+    /* this lane's row: its place in the batch, its head, and the tokens that it sees */
     const int row = rbase + wave * 32 + col;
     const bool live = row < rows;
     const int qi = live ? row / A.G : 0, qh_i = h * A.G + (live ? row % A.G : 0);
-    const int see0 = at_from(A, R, qi), see1 = live ? at_to(R, qi) : 0;
-    /* tokens that some row of this wave sees, and that all do */
+    int at_row, see0, see1;
+    if constexpr (MODE == AT_PREFIX) {
+        const int2 q = lds.query[live ? qi - rbase / A.G : 0];
+        const int from = A.window ? q.y - A.window + 1 : 0;
+        at_row = q.x, see0 = from > 0 ? from : 0, see1 = !live || q.y < 0 ? 0 : q.y + 1 < R.len ? q.y + 1 : R.len;
+    } else {
+        at_row = R.row0 + qi, see0 = at_from(A, R, qi), see1 = live ? at_to(R, qi) : 0;
+    }
+    /* tokens that some row of this wave sees, and that all do; tokens that some row of the workgroup sees */
     const int wfirst = rbase + wave * 32, wlast = wfirst + 31 < rows ? wfirst + 31 : rows - 1;
     const bool has_rows = wfirst < rows;
-    const int any_from = has_rows ? at_from(A, R, wfirst / A.G) : 0, any_to = has_rows ? at_to(R, wlast / A.G) : 0;
-    const int all_from = has_rows ? at_from(A, R, wlast / A.G) : 0, all_to = has_rows ? at_to(R, wfirst / A.G) : 0;
+    int any_from, any_to, all_from, all_to, tok0, tok1;
+    if constexpr (MODE == AT_PREFIX) {
+        any_from = all_from = see0, any_to = all_to = see1;
+        if (!live) any_from = all_to = 0x7fffffff, all_from = any_to = 0;
+#pragma unroll
+        for (int x = 1; x < 32; x <<= 1) {
+            any_from = min(any_from, __shfl_xor(any_from, x)), any_to = max(any_to, __shfl_xor(any_to, x));
+            all_from = max(all_from, __shfl_xor(all_from, x)), all_to = min(all_to, __shfl_xor(all_to, x));
+        }
+        any_from = at_uniform(any_from), any_to = at_uniform(any_to), all_from = at_uniform(all_from), all_to = at_uniform(all_to);
+        if (lane == 0) lds.ends[wave] = make_int2(any_from, any_to);
+        __syncthreads();
+        tok0 = 0x7fffffff, tok1 = 0;
+#pragma unroll
+        for (int w = 0; w < AT_WAVES; ++w) tok0 = min(tok0, lds.ends[w].x), tok1 = max(tok1, lds.ends[w].y);
+        tok0 = at_uniform(tok0), tok1 = at_uniform(tok1);
+    } else {
+        tok0 = at_from(A, R, rbase / A.G), tok1 = at_to(R, (rend - 1) / A.G);
+        any_from = has_rows ? at_from(A, R, wfirst / A.G) : 0, any_to = has_rows ? at_to(R, wlast / A.G) : 0;
+        all_from = has_rows ? at_from(A, R, wlast / A.G) : 0, all_to = has_rows ? at_to(R, wfirst / A.G) : 0;
+    }
+    int tile = tok0 / AT_TILE, tend = (tok1 + AT_TILE - 1) / AT_TILE;
+    if (tend < tile) tend = tile;
+    if constexpr (MODE == AT_PREFIX) {
+        /* equal pieces of the whole prefix, so that every row of the group has the same */
+        const int all = (R.len + AT_TILE - 1) / AT_TILE, n = at_piece(all, splits);
+        if (piece * n >= all) return;
+        tile = max(tile, piece * n), tend = min(tend, piece * n + n);
+    } else {
+        const int n = (tend - tile + splits - 1) / splits;
+        tile += piece * n;
+        tend = tile + n < tend ? tile + n : tend;
+    }
+    const int* pages = MODE == AT_PREFIX ? A.shared_table + b * A.shared_stride : A.table + b * A.table_stride;
     /* this lane's part of q: as fp16 (HALF: values d = 16 s + 8 half .. + 7, times a power of two, exact down to 2^-27 of the
      * row's largest), or as two 8-bit pieces (values d = 32 s + 16 half .. + 15) */
     at_v8h qf[2 * KS];
@@ -875,7 +1000,7 @@ __device__ __forceinline__ void at_many(const at_args& A, int place, at_many_lds
     float a_row;
     {
         uint32_t w[KS][8];
-        const uint16_t* src = A.q + (R.row0 + qi) * A.q_stride + qh_i * D;
+        const uint16_t* src = A.q + at_row * A.q_stride + qh_i * D;
         float most = 0.0f;
         bool odd = false;
 #pragma unroll
@@ -1152,9 +1277,11 @@ __device__ __forceinline__ void at_many(const at_args& A, int place, at_many_lds
     bl_mfma_fence();
     l += at_xor(l, 32);
     if (!live) return;
-    if (A.splits == 1) {
+    if (MODE == AT_OWN && h == 0 && piece == 0 && half == 0 && row % A.G == 0)
+        A.pieces[at_row] = make_int2(at_piece_count((R.skip + AT_TILE - 1) / AT_TILE, A.group_splits), splits);
+    if (MODE == AT_ALL && A.splits == 1) {
         const float inv = l == 0.0f ? 0.0f : bl_div_rn(1.0f, l);
-        uint16_t* to = A.out + (R.row0 + qi) * A.out_stride + qh_i * D;
+        uint16_t* to = A.out + at_row * A.out_stride + qh_i * D;
 #pragma unroll
         for (int i = 0; i < DT; ++i)
 #pragma unroll
@@ -1163,7 +1290,7 @@ __device__ __forceinline__ void at_many(const at_args& A, int place, at_many_lds
                 *bl_g((bl_v2u*)(to + 32 * i + 2 * j + 4 * half)) = u;
             }
     } else {
-        const int64_t at = (int64_t)piece * A.T * A.n_q + (int64_t)(R.row0 + qi) * A.n_q + qh_i;
+        const int64_t at = at_part_at(A, MODE == AT_OWN ? A.group_splits + piece : piece, at_row, qh_i);
         float* to = A.many_part + at * D;
 #pragma unroll
         for (int i = 0; i < DT; ++i)
@@ -1219,6 +1346,38 @@ __device__ __forceinline__ void at_many_join(const at_args& A, int group) {
     *bl_g((bl_v2u*)(A.out + row * A.out_stride + (at % A.n_q) * D + d0)) = u;
 }
 
+/* The same for rows of requests that share prefixes: pieces 0 .. of the prefix and group_splits .. of the rest, as many as the row's entry says. */
+template <int D>
+__global__ __launch_bounds__(AT_THREADS) void bl_attn_shared_join(at_args A) {
+    constexpr int TPR = D / 4, IN = 4;
+    const int64_t at = (int64_t)blockIdx.x * (AT_THREADS / TPR) + threadIdx.x / TPR, all = (int64_t)A.T * A.n_q;
+    if (at >= all) return;
+    const int row = (int)(at / A.n_q), d0 = (threadIdx.x % TPR) * 4;
+    if (row < A.q_start[0] || row >= A.q_start[A.B]) return;
+    const int2 n = A.pieces[row];
+    const float* ml = A.many_part + A.splits * all * D;
+    const int count = n.x + n.y;
+    at_sum s = {-INFINITY, 0.0f, {0, 0, 0, 0}};
+    for (int i = 0; i < count; i += IN) {
+        at_sum x[IN];
+#pragma unroll
+        for (int u = 0; u < IN; ++u) {
+            x[u] = {-INFINITY, 0.0f, {0, 0, 0, 0}};
+            if (i + u < count) {
+                const int64_t from = (i + u < n.x ? i + u : A.group_splits + i + u - n.x) * all + at;
+                const bl_v2f t = *bl_gc<bl_v2f>(ml + 2 * from);
+                x[u].m = t[0], x[u].l = t[1], x[u].y = *bl_gc<bl_v4f>(A.many_part + from * D + d0);
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < IN; ++u) s = at_add(s, x[u]);
+    }
+    const float inv = s.l == 0.0f ? 0.0f : bl_div_rn(1.0f, s.l);
+    bl_v2u u = {bl_pack2_bf16(s.y[0] * inv, s.y[1] * inv), bl_pack2_bf16(s.y[2] * inv, s.y[3] * inv)};
+    if (n.y < 0) u = (bl_v2u){0x7fc07fc0u, 0x7fc07fc0u};      /* more queries than the launch was made for */
+    *bl_g((bl_v2u*)(A.out + row * A.out_stride + (at % A.n_q) * D + d0)) = u;
+}
+
 /* ---- launches ---------------------------------------------------------------------------------------------------------- */
 
 /* A batch without long runs of rows: at_few alone. */
@@ -1244,6 +1403,19 @@ __global__ __launch_bounds__(AT_THREADS, 2) void bl_attn_any(at_args A, int many
     __shared__ __attribute__((aligned(16))) uint8_t lds[sizeof(lds_t)];
     if ((int)blockIdx.x < many) at_many<KIND, D>(A, (int)blockIdx.x, ((lds_t*)lds)->many);
     else at_few<KIND, D, WIDE, ITEM, false>(A, (int)blockIdx.x - many, lds);
+}
+/* Requests that share prefixes: workgroups of the prefixes, of many rows behind them, and of few. */
+template <int KIND, int D, bool WIDE, bool MANY>
+__global__ __launch_bounds__(AT_THREADS, 2) void bl_attn_shared(at_args A, int prefix, int many) {
+    union lds_t {
+        at_meet_lds<D, AT_WAVES> few;
+        at_many_lds<KIND, D> many;
+    };
+    __shared__ __attribute__((aligned(16))) uint8_t lds[sizeof(lds_t)];
+    const int x = (int)blockIdx.x;
+    if (x < prefix) at_many<KIND, D, AT_PREFIX>(A, x, ((lds_t*)lds)->many);
+    else if (MANY && x < prefix + many) at_many<KIND, D, AT_OWN>(A, x - prefix, ((lds_t*)lds)->many);
+    else at_few<KIND, D, WIDE, AT_WAVES, !MANY, true>(A, x - prefix - many, lds);
 }
 /* Partial results of both: `few` workgroups for those of at_few, turns x AT_STREAM_GROUPS, the others for a split. */
 template <int D, bool MANY>
@@ -1330,6 +1502,19 @@ extern "C" size_t bl_attn_workspace_bytes(const bl_attn_desc* a) {
     return at_check(a) == BL_OK ? at_make_plan(a).bytes : 0;
 }
 
+static at_args at_make_args(const bl_attn_desc* a) {
+    const bl_kv_cache& c = a->cache;
+    at_args A = {};
+    A.k = (const uint8_t*)c.k, A.v = (const uint8_t*)c.v, A.k_scale = c.k_scale, A.v_scale = c.v_scale;
+    A.q = a->q, A.q_start = a->q_start, A.seq_len = a->seq_len, A.table = a->table, A.out = a->out;
+    A.k_units = (uint32_t)(c.k_stride / 16), A.v_units = (uint32_t)(c.v_stride / 16), A.scale_stride = c.scale_stride;
+    A.q_stride = a->q_stride, A.out_stride = a->out_stride, A.table_stride = a->table_stride;
+    A.n_blocks = (int)c.n_blocks, A.n_kv = c.n_kv, A.G = a->n_q / c.n_kv, A.n_q = a->n_q, A.B = (int)a->B, A.T = (int)a->T;
+    A.shift = bl_log2(c.block), A.max_tokens = a->max_blocks * c.block, A.window = a->window < 1 << 30 ? a->window : 1 << 30;
+    A.factor = a->softmax_scale * 1.44269504f;
+    return A;
+}
+
 template <int KIND, int D, bool WIDE>
 static void at_launch(at_args A, const at_plan& p, const bl_attn_desc* a, hipStream_t st) {
     A.part = (float*)a->workspace;
@@ -1362,17 +1547,90 @@ extern "C" bl_status bl_attn_kv8(const bl_attn_desc* a, bl_stream s) {
     if (!bl_aligned(a->workspace, 256)) return BL_ERR_ALIGN;
     const bl_kv_cache& c = a->cache;
     if ((int64_t)p.row_tiles * c.n_kv * p.splits + p.items > 0x7fff0000) return BL_ERR_SHAPE;
-    at_args A = {};
-    A.k = (const uint8_t*)c.k, A.v = (const uint8_t*)c.v, A.k_scale = c.k_scale, A.v_scale = c.v_scale;
-    A.q = a->q, A.q_start = a->q_start, A.seq_len = a->seq_len, A.table = a->table, A.out = a->out;
-    A.k_units = (uint32_t)(c.k_stride / 16), A.v_units = (uint32_t)(c.v_stride / 16), A.scale_stride = c.scale_stride;
-    A.q_stride = a->q_stride, A.out_stride = a->out_stride, A.table_stride = a->table_stride;
-    A.n_blocks = (int)c.n_blocks, A.n_kv = c.n_kv, A.G = a->n_q / c.n_kv, A.n_q = a->n_q, A.B = (int)a->B, A.T = (int)a->T;
-    A.shift = bl_log2(c.block), A.max_tokens = a->max_blocks * c.block, A.window = a->window < 1 << 30 ? a->window : 1 << 30;
-    A.factor = a->softmax_scale * 1.44269504f;
+    at_args A = at_make_args(a);
     A.few_rows = p.few ? AT_FEW : 0, A.splits = p.splits, A.part_skip = p.skip;
     const hipStream_t st = (hipStream_t)s;
 #define AT(K, D) (c.block == 128 ? at_launch<K, D, true>(A, p, a, st) : at_launch<K, D, false>(A, p, a, st))
+    if (c.kind == BL_KV_INT8) c.head_dim == 128 ? AT(BL_KV_INT8, 128) : AT(BL_KV_INT8, 64);
+    else c.head_dim == 128 ? AT(BL_KV_E4M3, 128) : AT(BL_KV_E4M3, 64);
+#undef AT
+    return hipGetLastError() == hipSuccess ? BL_OK : BL_ERR_HIP;
+}
+
+/* ---- shared prefixes, host ------------------------------------------------------------------------------------------------ */
+
+struct at_shared_plan {
+    bool few, many;
+    int group_splits, few_splits, many_splits, splits;
+    int64_t prefix_tiles, many_tiles;
+    size_t pieces, bytes;          /* of the rows' entries in front, and in all */
+};
+
+static bl_status at_check_shared(const bl_attn_shared_desc* a) {
+    if (!a) return BL_ERR_NULL;
+    if (const bl_status rc = at_check(&a->attn)) return rc;
+    if (!a->group || !a->shared_blocks || !a->shared_table) return BL_ERR_NULL;
+    if (a->n_groups < 1 || a->n_groups > BL_KV_MAX_REQUESTS || a->max_shared < 1 || (int64_t)a->max_shared * a->attn.cache.block > ((int64_t)1 << 30) ||
+        a->shared_stride < a->max_shared || a->shared_stride > ((int64_t)1 << 40) || a->max_own < 0)
+        return BL_ERR_SHAPE;
+    if (!bl_aligned(a->group, 4) || !bl_aligned(a->shared_blocks, 4) || !bl_aligned(a->shared_table, 4)) return BL_ERR_ALIGN;
+    return BL_OK;
+}
+
+static at_shared_plan at_make_shared_plan(const bl_attn_shared_desc* s) {
+    const bl_attn_desc* a = &s->attn;
+    at_shared_plan p;
+    const int G = a->n_q / a->cache.n_kv, D = a->cache.head_dim;
+    p.many = (int64_t)(a->max_q < a->T ? a->max_q : a->T) * G > AT_FEW, p.few = G <= AT_FEW;
+    const int64_t tiles = (a->T * G + AT_MANY - 1) / AT_MANY, part = a->T < a->B ? a->T : a->B, groups = s->n_groups < part ? s->n_groups : part;
+    int64_t own = s->max_own > 0 ? s->max_own : a->max_len > 0 ? a->max_len : (int64_t)a->max_blocks * a->cache.block;
+    const int64_t wide = (int64_t)a->window + (a->max_q < AT_MANY ? a->max_q : AT_MANY);
+    if (a->window && own > wide) own = wide;
+    auto pieces = [](int64_t items, int64_t tokens, int64_t each, int64_t most) -> int {
+        int64_t n = items < 512 ? 512 / items : 1;
+        n = n < tokens / each ? n : tokens / each;
+        return (int)(n < 1 ? 1 : n < most ? n : most);
+    };
+    p.group_splits = pieces(tiles * a->cache.n_kv, (int64_t)s->max_shared * a->cache.block, 4 * AT_TILE, 64);
+    p.few_splits = p.few ? pieces(part * a->cache.n_kv, own, 4 * AT_TILE, 32) : 0;
+    p.many_splits = p.many ? pieces(tiles * a->cache.n_kv, own, 4 * AT_TILE, 32) : 0;
+    p.splits = p.group_splits + (p.few_splits > p.many_splits ? p.few_splits : p.many_splits);
+    if (p.many) p.many_splits = p.splits - p.group_splits;
+    p.prefix_tiles = a->T * G / AT_MANY + groups, p.many_tiles = p.many ? a->T * G / AT_MANY + part : 0;
+    p.pieces = ((size_t)a->T * sizeof(int2) + 255) / 256 * 256;
+    p.bytes = p.pieces + (size_t)p.splits * a->T * a->n_q * (D + 2) * sizeof(float);
+    return p;
+}
+
+extern "C" size_t bl_attn_shared_workspace_bytes(const bl_attn_shared_desc* a) {
+    return at_check_shared(a) == BL_OK ? at_make_shared_plan(a).bytes : 0;
+}
+
+template <int KIND, int D, bool WIDE>
+static void at_shared_launch(const at_args& A, const at_shared_plan& p, hipStream_t st) {
+    const int prefix = (int)(p.prefix_tiles * A.n_kv * p.group_splits), many = (int)(p.many_tiles * A.n_kv * p.many_splits);
+    const int few = p.few ? A.B * A.n_kv * p.few_splits : 0;
+    if (p.many) bl_attn_shared<KIND, D, WIDE, true><<<(unsigned)(prefix + many + few), AT_THREADS, 0, st>>>(A, prefix, many);
+    else bl_attn_shared<KIND, D, WIDE, false><<<(unsigned)(prefix + few), AT_THREADS, 0, st>>>(A, prefix, 0);
+    const int64_t rows = (int64_t)A.T * A.n_q, per = AT_THREADS / (D / 4);
+    bl_attn_shared_join<D><<<(unsigned)((rows + per - 1) / per), AT_THREADS, 0, st>>>(A);
+}
+
+extern "C" bl_status bl_attn_kv8_shared(const bl_attn_shared_desc* s, bl_stream stream) {
+    if (const bl_status rc = at_check_shared(s)) return rc;
+    const bl_attn_desc* a = &s->attn;
+    const at_shared_plan p = at_make_shared_plan(s);
+    if (!a->workspace) return BL_ERR_WORKSPACE;
+    if (!bl_aligned(a->workspace, 256)) return BL_ERR_ALIGN;
+    const bl_kv_cache& c = a->cache;
+    if (c.n_kv * (p.prefix_tiles * p.group_splits + p.many_tiles * p.many_splits + a->B * p.few_splits) > 0x7fff0000) return BL_ERR_SHAPE;
+    at_args A = at_make_args(a);
+    A.few_rows = p.few ? AT_FEW : 0, A.splits = p.splits, A.group_splits = p.group_splits, A.few_splits = p.few_splits;
+    A.group = s->group, A.shared_blocks = s->shared_blocks, A.shared_table = s->shared_table, A.shared_stride = s->shared_stride;
+    A.n_groups = (int)s->n_groups, A.max_shared = s->max_shared;
+    A.pieces = (int2*)a->workspace, A.many_part = (float*)((char*)a->workspace + p.pieces);
+    const hipStream_t st = (hipStream_t)stream;
+#define AT(K, D) (c.block == 128 ? at_shared_launch<K, D, true>(A, p, st) : at_shared_launch<K, D, false>(A, p, st))
     if (c.kind == BL_KV_INT8) c.head_dim == 128 ? AT(BL_KV_INT8, 128) : AT(BL_KV_INT8, 64);
     else c.head_dim == 128 ? AT(BL_KV_E4M3, 128) : AT(BL_KV_E4M3, 64);
 #undef AT

@@ -1,0 +1,590 @@
+/* Products and lookups of a matrix of 8-bit floating point codes (OCP e4m3) with a scale for each block of 128 x 128 (bitlinear.h,
+ * bl_f8_linear, bl_f8_embed).
+ *
+ *     y[m][n] = sum_b s[m][b] * ws[n / 128][b] * P,   P = sum of c[m][k] * w[n][k] over the block's 128 k
+ *
+ * c and s: the row's codes and scales, made from its bf16 values.  P comes from the matrix cores and is scaled and added in fp32.  The weights are the first operand and the tokens the second, so that a lane has one token and its scale,
+ * and four consecutive weight rows, which is a run of the output.  A lane's 32 codes of a block are 16 from offset 16 g and 16 from 64 + 16 g,
+ * g = lane / 16: the order of k inside a block is free as long as both operands have the same. */
+#include <atomic>
+
+#include "bl_device.h"
+#include "bl_host.h"
+#include "bl_producer.h"
+
+typedef int f8_v8i __attribute__((ext_vector_type(8)));
+typedef _Float16 f8_v8h __attribute__((ext_vector_type(8)));
+typedef _Float16 f8_v2h __attribute__((ext_vector_type(2)));
+typedef uint32_t f8_v4u __attribute__((ext_vector_type(4)));
+
+#define F8_BLOCK 128
+#define F8_TOP 448.0f
+
+struct f8_args {
+    const uint8_t* w;
+    const float* ws;
+    int64_t w_stride, ws_stride;
+    uint8_t* codes;                /* [M][nb * 128] */
+    float* scales;                 /* [nb][M] */
+    void* y;
+    int64_t y_stride;
+    float* part;                   /* [splits][M][N] where the k loop is split */
+    int M, N, K, nb;
+    int bf16, wide;                /* output type; rows of y are 16-byte aligned */
+    int splits, tiles_m, tiles_n;
+};
+
+__device__ __forceinline__ f8_v8i f8_join(bl_v4i a, bl_v4i b) { return f8_v8i{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]}; }
+/* The codes are opened to fp16, which holds every one of them, and multiplied there: products are exact and sums have 32 bits.  The matrix cores take the codes
+ * as they are too, at twice the rate, but line a block's products up with the largest and cut what falls below: 1.4e-5 of the sum's size on normal values
+ * (fp16: 1e-8), 2^-12 of sum |c w| where sizes are spread over all that e4m3 has: fewer bits than an fp32 output stands for. */
+struct f8_halves {                 /* 32 codes of a lane */
+    f8_v8h v[4];
+};
+__device__ __forceinline__ f8_halves f8_open(f8_v8i c) {
+    f8_halves h;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        f8_v4u u;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            u[j] = __builtin_bit_cast(uint32_t, j & 1 ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(c[2 * i + j / 2], 1.0f, true) : __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(c[2 * i + j / 2], 1.0f, false));
+        h.v[i] = __builtin_bit_cast(f8_v8h, u);
+    }
+    return h;
+}
+__device__ __forceinline__ bl_v4f f8_product(const f8_halves& w, const f8_halves& x) {
+    bl_v4f p = {0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) p = __builtin_amdgcn_mfma_f32_16x16x32_f16(w.v[i], x.v[i], p, 0, 0, 0);
+    return p;
+}
+
+/* ---- rows to codes ----------------------------------------------------------------------------------------------------- */
+
+/* The scale of a group whose largest |value| is g (a NaN counts as the largest; fmaxf then gives the floor, and the NaN's own code
+ * spoils the row, as an infinity does, which meets the factor 0). */
+__device__ __forceinline__ float f8_scale(float g) { return fmaxf(g, 1e-5f) * (1.0f / F8_TOP); }
+__device__ __forceinline__ int f8_codes4(uint32_t a, uint32_t b, float inv) {
+    const int c = __builtin_amdgcn_cvt_pk_fp8_f32(bl_bf16_to_f32(a & 0xffffu) * inv, __uint_as_float(a & 0xffff0000u) * inv, 0, false);
+    return __builtin_amdgcn_cvt_pk_fp8_f32(bl_bf16_to_f32(b & 0xffffu) * inv, __uint_as_float(b & 0xffff0000u) * inv, c, true);
+}
+__device__ __forceinline__ bl_v4i f8_codes16(const uint4& lo, const uint4& hi, float inv) {
+    return bl_v4i{f8_codes4(lo.x, lo.y, inv), f8_codes4(lo.z, lo.w, inv), f8_codes4(hi.x, hi.y, inv), f8_codes4(hi.z, hi.w, inv)};
+}
+__device__ __forceinline__ float f8_largest16(const uint4& lo, const uint4& hi) {
+    return bl_max_pos(bl_absmax8_bf16<false>(lo), bl_absmax8_bf16<false>(hi));
+}
+
+/* A workgroup a token, a thread 16 values: eight threads have a group of 128.  Zeros behind K in the last block. */
+__global__ __launch_bounds__(256) void bl_f8_rows(f8_args A, bl_prod_dev P) {
+    __shared__ double s4[4];
+    const int m = (int)blockIdx.x, tid = threadIdx.x, groups = A.K / 16, all = A.nb * 8;
+    uint4 xv[4];
+    float rn = 0.0f;
+    if (P.norm) rn = bl_norm_produce2(P, m, A.K, true, s4, xv);
+    uint8_t* to = A.codes + (int64_t)m * all * 16;
+    auto unit = [&](int u, uint4 lo, uint4 hi) {
+        float g = f8_largest16(lo, hi);
+        g = bl_max_pos(g, bl_dppf<BL_DPP_QUAD_XOR1>(g));
+        g = bl_max_pos(g, bl_dppf<BL_DPP_QUAD_XOR2>(g));
+        g = bl_max_pos(g, bl_dppf<BL_DPP_ROW_HALF_MIRROR>(g));
+        const float s = f8_scale(g);
+        *(bl_v4i*)(to + (int64_t)u * 16) = f8_codes16(lo, hi, bl_div_rn(1.0f, s));
+        if ((u & 7) == 0) A.scales[(int64_t)(u >> 3) * A.M + m] = s;
+    };
+    const uint4 zero = make_uint4(0, 0, 0, 0);
+    if (P.norm) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int u = tid + 256 * j;
+            if (u < all) unit(u, u < groups ? xv[2 * j] : zero, u < groups ? xv[2 * j + 1] : zero);
+        }
+    }
+    for (int u = tid + (P.norm ? 512 : 0); u < all; u += 256) {
+        uint4 lo = zero, hi = zero;
+        if (u < groups) bl_produce16<true>(P, m, u, A.K, !P.norm, rn, lo, hi);
+        unit(u, lo, hi);
+    }
+}
+
+/* ---- output -------------------------------------------------------------------------------------------------------------- */
+
+__device__ __forceinline__ uint16_t f8_bf16(float v) { return (uint16_t)bl_pack2_bf16(v, v); }
+/* Four consecutive outputs n .. n + 3 of row m. */
+__device__ __forceinline__ void f8_store4(const f8_args& A, int m, int n, const float (&v)[4]) {
+    const int64_t at = (int64_t)m * A.y_stride + n;
+    if (A.wide && n + 4 <= A.N) {
+        if (A.bf16) *bl_g((bl_v2u*)((uint16_t*)A.y + at)) = (bl_v2u){bl_pack2_bf16(v[0], v[1]), bl_pack2_bf16(v[2], v[3])};
+        else *bl_g((bl_v4f*)((float*)A.y + at)) = (bl_v4f){v[0], v[1], v[2], v[3]};
+    } else {
+        for (int i = 0; i < 4 && n + i < A.N; ++i) {
+            if (A.bf16) ((uint16_t*)A.y)[at + i] = f8_bf16(v[i]);
+            else ((float*)A.y)[at + i] = v[i];
+        }
+    }
+}
+
+/* ---- stream: few tokens ---------------------------------------------------------------------------------------------------- */
+
+/* Up to 16 * MT tokens.  A workgroup of eight waves walks strips of 16 weight rows; wave w has the blocks w, w + 8, .. of k (KB of them at most), for
+ * which it keeps the tokens' codes and scales in registers, and meets the others' sums in LDS.  The next strip's codes are in flight while one is
+ * multiplied; one barrier a strip.  FUSED: the rows are made here, by every workgroup: a lane has what its token needs for
+ * its own blocks, so that only the sum of squares of a norm crosses waves. */
+#define F8_WAVES 8
+template <int MT, int KB, bool FUSED>
+__global__ __launch_bounds__(F8_WAVES * 64, KB * (MT + 1) <= 6 ? 4 : 2) void bl_f8_stream(f8_args A, bl_prod_dev P) {
+    __shared__ __attribute__((aligned(16))) float red[2][F8_WAVES][MT * 16][16];
+    __shared__ double squares[F8_WAVES][16];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 15, g = lane >> 4;
+    const int strips = (A.N + 15) / 16, stride = (int)gridDim.x;
+    const bl_v4i zero = {0, 0, 0, 0};
+    bl_v4i w[KB][2];
+    float ws[KB];
+    /* slot j of a strip: loaded for the next as soon as it has been read */
+    auto load = [&](int strip, int j) {
+        const int n = strip * 16 + r, b = wave + F8_WAVES * j;
+        w[j][0] = w[j][1] = zero, ws[j] = 0.0f;
+        if (b < A.nb) {
+            const uint8_t* at = A.w + (n < A.N ? n : A.N - 1) * A.w_stride + g * 16 + b * F8_BLOCK;
+            w[j][0] = __builtin_nontemporal_load(bl_gc<bl_v4i>(at));
+            if (b * F8_BLOCK + 64 < A.K) w[j][1] = __builtin_nontemporal_load(bl_gc<bl_v4i>(at + 64));
+            ws[j] = A.ws[(int64_t)(strip >> 3) * A.ws_stride + b];
+        }
+    };
+    int strip = (int)blockIdx.x;
+#pragma unroll
+    for (int j = 0; j < KB; ++j) load(strip, j);
+    f8_v8i x[MT][KB] = {};
+    float xs[MT][KB] = {};
+    if constexpr (FUSED) {
+        static_assert(MT == 1, "rows are made for one tile of tokens");
+        float rn = 0.0f;
+        if (P.norm) {
+            double ss = 0.0;
+            if (r < A.M) {
+#pragma unroll 1
+                for (int j = 0; j < KB; ++j) {
+                    const int b = wave + F8_WAVES * j;
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+                        if (b * F8_BLOCK + 64 * i < A.K) {
+                            float v[16];
+                            bl_produce16_f32(P, r, b * 8 + 4 * i + g, A.K, false, v);
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) ss += (double)v[e] * (double)v[e];
+                        }
+                }
+            }
+            ss += __shfl_xor(ss, 16);
+            ss += __shfl_xor(ss, 32);
+            if (lane < 16) squares[wave][lane] = ss;
+            __syncthreads();
+            double sum = 0.0;
+#pragma unroll
+            for (int w = 0; w < F8_WAVES; ++w) sum += squares[w][r];
+            rn = (float)(1.0 / sqrt(sum / (double)A.K + (double)P.eps));
+        }
+#pragma unroll 1
+        for (int at = 0; at < KB; ++at) {                     /* (one block's values in registers at a time) */
+            const int b = wave + F8_WAVES * at;
+            uint4 lo[2], hi[2];
+            float most = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                lo[i] = hi[i] = make_uint4(0, 0, 0, 0);
+                if (r < A.M && b * F8_BLOCK + 64 * i < A.K) bl_produce16<true>(P, r, b * 8 + 4 * i + g, A.K, blockIdx.x == 0, rn, lo[i], hi[i]);
+                most = bl_max_pos(most, f8_largest16(lo[i], hi[i]));
+            }
+            most = bl_max_pos(most, __shfl_xor(most, 16));
+            most = bl_max_pos(most, __shfl_xor(most, 32));
+            const float scale = f8_scale(most), inv = bl_div_rn(1.0f, scale);
+            const f8_v8i c = f8_join(f8_codes16(lo[0], hi[0], inv), f8_codes16(lo[1], hi[1], inv));
+#pragma unroll
+            for (int j = 0; j < KB; ++j)
+                if (j == at) x[0][j] = c, xs[0][j] = scale;
+        }
+    } else {
+#pragma unroll
+        for (int t = 0; t < MT; ++t) {
+            const int m = t * 16 + r < A.M ? t * 16 + r : A.M - 1;
+            const uint8_t* row = A.codes + (int64_t)m * A.nb * F8_BLOCK + g * 16;
+#pragma unroll
+            for (int j = 0; j < KB; ++j) {
+                const int b = wave + F8_WAVES * j;
+                x[t][j] = f8_join(zero, zero), xs[t][j] = 0.0f;
+                if (b < A.nb) {
+                    x[t][j] = f8_join(*bl_gc<bl_v4i>(row + b * F8_BLOCK), *bl_gc<bl_v4i>(row + b * F8_BLOCK + 64));
+                    xs[t][j] = A.scales[(int64_t)b * A.M + m];
+                }
+            }
+        }
+    }
+    int buf = 0;
+    for (; strip < strips; strip += stride, buf ^= 1) {
+        /* (the tokens' codes are opened again for every strip: as fp16 they would take twice the registers) */
+#pragma unroll
+        for (int t = 0; t < MT; ++t)
+#pragma unroll
+            for (int j = 0; j < KB; ++j) asm volatile("" : "+v"(x[t][j]));
+        const int next = strip + stride < strips ? strip + stride : strip;
+        bl_v4f acc[MT], p[2][MT];
+        float f[2][MT];
+#pragma unroll
+        for (int t = 0; t < MT; ++t) acc[t] = (bl_v4f){0, 0, 0, 0};
+        auto add = [&](int at) {
+#pragma unroll
+            for (int t = 0; t < MT; ++t)
+#pragma unroll
+                for (int v = 0; v < 4; ++v) acc[t][v] = __builtin_fmaf(p[at][t][v], f[at][t], acc[t][v]);
+        };
+#pragma unroll
+        for (int j = 0; j < KB; ++j) {
+            const f8_halves h = f8_open(f8_join(w[j][0], w[j][1]));
+#pragma unroll
+            for (int t = 0; t < MT; ++t) f[j & 1][t] = xs[t][j] * ws[j];
+            load(next, j);
+#pragma unroll
+            for (int t = 0; t < MT; ++t) p[j & 1][t] = f8_product(h, f8_open(x[t][j]));
+            __builtin_amdgcn_sched_barrier(0);                /* (four products at least between a block's last and its first reader) */
+            if (j > 0) add((j - 1) & 1);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        bl_mfma_fence();
+        add((KB - 1) & 1);
+#pragma unroll
+        for (int t = 0; t < MT; ++t)
+            if (t * 16 + r < A.M) *(bl_v4f*)&red[buf][wave][t * 16 + r][4 * g] = acc[t];
+        asm volatile("" ::: "memory");
+        BL_WAIT_LGKM0();
+        __builtin_amdgcn_s_barrier();                         /* (the loads of the next strip stay in flight) */
+        asm volatile("" ::: "memory");
+        for (int i = tid; i < A.M * 16; i += F8_WAVES * 64) {
+            const int m = i >> 4, n = strip * 16 + (i & 15);
+            float v = 0.0f;
+#pragma unroll
+            for (int w = 0; w < F8_WAVES; ++w) v += red[buf][w][m][i & 15];
+            if (n < A.N) {
+                const int64_t at = m * A.y_stride + n;
+                if (A.bf16) ((uint16_t*)A.y)[at] = f8_bf16(v);
+                else ((float*)A.y)[at] = v;
+            }
+        }
+    }
+}
+
+/* ---- tiles: any number of tokens ------------------------------------------------------------------------------------------ */
+
+/* BM tokens x BN weight rows a workgroup, WM x WN waves, S stages of one block of k (128) in LDS.  Rows of 128 bytes; unit u (16 bytes) of row r lies
+ * at unit u ^ (r / 2 % 8), so that sixteen lanes of a read fall on all banks; the loads that go straight to LDS pick their units accordingly.
+ * In the last block of a K that is no multiple of 128 the units behind K are the weights' first four again: their codes meet zeros (and a
+ * NaN among them spoils the row anyway). */
+template <int BM, int BN, int WM, int WN, int S>
+__global__ __launch_bounds__(WM * WN * 64, 2) void bl_f8_tile(f8_args A) {
+    constexpr int NW = WM * WN, TM = BM / WM / 16, TN = BN / WN / 16, STAGE = (BM + BN) * F8_BLOCK, LOADS = (BM + BN) / 8 / NW;
+    extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 15, g = lane >> 4;
+    const int wm = wave % WM, wn = wave / WM;
+    /* consecutive workgroups go to the eight dies in turn: each takes a contiguous eighth of the tiles, tokens first */
+    int place;
+    {
+        const int all = (int)gridDim.x, die = (int)blockIdx.x & 7, part = all >> 3, more = all & 7;
+        place = die * part + (die < more ? die : more) + ((int)blockIdx.x >> 3);
+    }
+    const int split = place % A.splits, tile = place / A.splits, m0 = tile % A.tiles_m * BM, n0 = tile / A.tiles_m * BN;
+    const int b0 = (int)((int64_t)A.nb * split / A.splits), b1 = (int)((int64_t)A.nb * (split + 1) / A.splits);
+    const int half = A.K % F8_BLOCK ? A.nb - 1 : -1;          /* the block of which only half is there */
+    const uint8_t* from[LOADS];
+    int unit[LOADS];
+#pragma unroll
+    for (int j = 0; j < LOADS; ++j) {
+        const int p = j * NW + wave;                          /* 1024 bytes, eight rows */
+        const bool is_x = p < BM / 8;
+        const int row = (is_x ? p : p - BM / 8) * 8 + lane / 8;
+        unit[j] = (lane & 7) ^ (row >> 1 & 7);
+        if (is_x) {
+            const int m = m0 + row < A.M ? m0 + row : A.M - 1;
+            from[j] = A.codes + (int64_t)m * A.nb * F8_BLOCK;
+        } else {
+            const int n = n0 + row < A.N ? n0 + row : A.N - 1;
+            from[j] = A.w + n * A.w_stride;
+        }
+    }
+    auto load = [&](int b, int stage) {
+        uint8_t* to = lds + stage * STAGE;
+#pragma unroll
+        for (int j = 0; j < LOADS; ++j) {
+            const int p = j * NW + wave, u = b == half && p >= BM / 8 ? unit[j] & 3 : unit[j];
+            __builtin_amdgcn_global_load_lds((bl_gptr)(from[j] + (int64_t)b * F8_BLOCK + u * 16), (bl_lptr)(to + p * 1024), 16, 0, 0);
+        }
+    };
+    float xs[TM], xn[TM], ws, wsn;
+    const int mrow = m0 + wm * (BM / WM) + r;
+    const float* wscale = A.ws + (int64_t)((n0 + wn * (BN / WN)) / F8_BLOCK < (A.N - 1) / F8_BLOCK ? (n0 + wn * (BN / WN)) / F8_BLOCK : (A.N - 1) / F8_BLOCK) * A.ws_stride;
+    auto load_scales = [&](int b) {
+#pragma unroll
+        for (int t = 0; t < TM; ++t) xn[t] = A.scales[(int64_t)b * A.M + (mrow + 16 * t < A.M ? mrow + 16 * t : A.M - 1)];
+        wsn = wscale[b];
+    };
+    bl_v4f acc[TN][TM];
+#pragma unroll
+    for (int i = 0; i < TN; ++i)
+#pragma unroll
+        for (int t = 0; t < TM; ++t) acc[i][t] = (bl_v4f){0, 0, 0, 0};
+    load_scales(b0);
+#pragma unroll
+    for (int s = 0; s < S - 1; ++s) load(b0 + s < b1 ? b0 + s : b1 - 1, s);
+    const int x_at = (wm * (BM / WM) + r) * F8_BLOCK, w_at = BM * F8_BLOCK + (wn * (BN / WN) + r) * F8_BLOCK, swz = (r >> 1) & 7;
+    int stage = 0;
+    for (int b = b0; b < b1; ++b) {
+#pragma unroll
+        for (int t = 0; t < TM; ++t) xs[t] = xn[t];
+        ws = wsn;
+        BL_WAIT_VM((S - 2) * LOADS);
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        load_scales(b + 1 < b1 ? b + 1 : b);
+        load(b + S - 1 < b1 ? b + S - 1 : b1 - 1, stage == 0 ? S - 1 : stage - 1);
+        const uint8_t* at = lds + stage * STAGE;
+        auto part = [&](int base, int t) {
+            const uint8_t* p = at + base + t * 16 * F8_BLOCK;
+            return f8_join(*(const bl_v4i*)(p + ((g ^ swz) << 4)), *(const bl_v4i*)(p + (((g + 4) ^ swz) << 4)));
+        };
+        f8_halves x[TM];
+#pragma unroll
+        for (int t = 0; t < TM; ++t) x[t] = f8_open(part(x_at, t));
+        float f[TM];
+#pragma unroll
+        for (int t = 0; t < TM; ++t) f[t] = xs[t] * ws;
+        bl_v4f p[2][TM];
+        auto add = [&](int i) {
+#pragma unroll
+            for (int t = 0; t < TM; ++t)
+#pragma unroll
+                for (int v = 0; v < 4; ++v) acc[i][t][v] = __builtin_fmaf(p[i & 1][t][v], f[t], acc[i][t][v]);
+        };
+#pragma unroll
+        for (int i = 0; i < TN; ++i) {
+            const f8_halves w = f8_open(part(w_at, i));
+#pragma unroll
+            for (int t = 0; t < TM; ++t) p[i & 1][t] = (bl_v4f){0, 0, 0, 0};
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+#pragma unroll
+                for (int t = 0; t < TM; ++t) p[i & 1][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(w.v[k], x[t].v[k], p[i & 1][t], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);                /* (a group of products between another's last and its first reader) */
+            if (i > 0) add(i - 1);
+        }
+        bl_mfma_fence();
+        add(TN - 1);
+        BL_WAIT_LGKM0();
+        stage = stage == S - 1 ? 0 : stage + 1;
+    }
+    BL_WAIT_VM(0);
+#pragma unroll
+    for (int t = 0; t < TM; ++t) {
+        const int m = mrow + 16 * t;
+        if (m >= A.M) continue;
+#pragma unroll
+        for (int i = 0; i < TN; ++i) {
+            const int n = n0 + wn * (BN / WN) + 16 * i + 4 * g;
+            if (n >= A.N) continue;
+            const float v[4] = {acc[i][t][0], acc[i][t][1], acc[i][t][2], acc[i][t][3]};
+            if (A.splits == 1) {
+                f8_store4(A, m, n, v);
+            } else {
+                float* to = A.part + ((int64_t)split * A.M + m) * A.N + n;
+                for (int j = 0; j < 4 && n + j < A.N; ++j) to[j] = v[j];
+            }
+        }
+    }
+}
+
+/* The pieces of a split k loop, added in their order. */
+__global__ __launch_bounds__(256) void bl_f8_join(f8_args A) {
+    const int64_t all = (int64_t)A.M * A.N;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
+        float v = A.part[i];
+        for (int s = 1; s < A.splits; ++s) v += A.part[s * all + i];
+        const int64_t at = i / A.N * A.y_stride + i % A.N;
+        if (A.bf16) ((uint16_t*)A.y)[at] = f8_bf16(v);
+        else ((float*)A.y)[at] = v;
+    }
+}
+
+/* ---- lookup -------------------------------------------------------------------------------------------------------------- */
+
+struct f8_lookup_args {
+    const uint8_t* w;
+    const float* ws;
+    int64_t w_stride, ws_stride, out_stride, all;
+    const int* ids;
+    void* out;
+    int* bad;
+    int N, units;                  /* units of a row, 16 bytes of the output each */
+    float multiplier;
+};
+/* A thread 16 bytes of the output. */
+template <bool BF16>
+__global__ __launch_bounds__(256) void bl_f8_embed_kernel(f8_lookup_args A) {
+    constexpr int V = BF16 ? 8 : 4;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < A.all; i += (int64_t)gridDim.x * 256) {
+        const int64_t t = i / A.units;
+        const int u = (int)(i - t * A.units), id = A.ids[t];
+        const bool there = (unsigned)id < (unsigned)A.N;
+        if (!there && id != -1 && u == 0 && A.bad) atomicAdd(A.bad, 1);
+        const uint8_t* row = A.w + (there ? id : 0) * A.w_stride;
+        const float s = A.ws[(int64_t)((there ? id : 0) / F8_BLOCK) * A.ws_stride + u * V / F8_BLOCK];
+        uint32_t c[V / 4];
+        if constexpr (BF16) {
+            const bl_v2u x = *bl_gc<bl_v2u>(row + u * V);
+            c[0] = x[0], c[1] = x[1];
+        } else {
+            c[0] = *bl_gc<uint32_t>(row + u * V);
+        }
+        float v[V];
+#pragma unroll
+        for (int j = 0; j < V / 4; ++j) {
+            const float f[4] = {__builtin_amdgcn_cvt_f32_fp8((int)c[j], 0), __builtin_amdgcn_cvt_f32_fp8((int)c[j], 1),
+                                __builtin_amdgcn_cvt_f32_fp8((int)c[j], 2), __builtin_amdgcn_cvt_f32_fp8((int)c[j], 3)};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[4 * j + e] = there ? (f[e] * s) * A.multiplier : 0.0f;
+        }
+        if constexpr (BF16) {
+            *bl_g((bl_v4i*)((uint16_t*)A.out + t * A.out_stride + u * V)) =
+                (bl_v4i){(int)bl_pack2_bf16(v[0], v[1]), (int)bl_pack2_bf16(v[2], v[3]), (int)bl_pack2_bf16(v[4], v[5]), (int)bl_pack2_bf16(v[6], v[7])};
+        } else {
+            *bl_g((bl_v4f*)((float*)A.out + t * A.out_stride + u * V)) = (bl_v4f){v[0], v[1], v[2], v[3]};
+        }
+    }
+}
+
+/* ---- host ---------------------------------------------------------------------------------------------------------------- */
+
+static bl_status f8_check(const bl_f8_matrix* w) {
+    if (!w->codes || !w->scale) return BL_ERR_NULL;
+    const int64_t most = (int64_t)1 << 40;
+    if (!bl_shape_ok(w->N, w->K) || w->K % 64 || w->stride < w->K || w->stride > most || w->scale_stride < (w->K + F8_BLOCK - 1) / F8_BLOCK || w->scale_stride > most)
+        return BL_ERR_SHAPE;
+    if (!bl_aligned(w->codes, 16) || w->stride % 16 || !bl_aligned(w->scale, 4)) return BL_ERR_ALIGN;
+    return BL_OK;
+}
+
+struct f8_plan {
+    int splits, tokens, blocks;    /* of the stream: tiles of 16 tokens (0: not it), blocks of k a wave */
+    bool fused;
+    size_t codes, scales, bytes;   /* of the workspace: bytes of the codes, of the scales behind them, of all */
+};
+static size_t f8_round(size_t n) { return (n + 255) / 256 * 256; }
+static f8_plan f8_make_plan(const bl_f8_product* p) {
+    f8_plan q;
+    const int64_t nb = (p->w.K + F8_BLOCK - 1) / F8_BLOCK;
+    q.splits = 1;
+    /* the stream, while a wave's registers hold its blocks of every token beside two strips' */
+    q.tokens = (int)((p->M + 15) / 16 < 5 ? (p->M + 15) / 16 : 0), q.blocks = (int)((nb + F8_WAVES - 1) / F8_WAVES < 9 ? (nb + F8_WAVES - 1) / F8_WAVES : 9);
+    q.blocks = q.blocks <= 4 ? q.blocks : q.blocks <= 6 ? 6 : q.blocks <= 8 ? 8 : 9;
+    if (q.tokens * q.blocks == 0 || q.blocks > 8 || q.blocks * (q.tokens + 1) > 18) q.tokens = 0;
+    q.fused = q.tokens == 1;
+    if (q.tokens) {
+        q.codes = q.fused ? 0 : f8_round((size_t)p->M * nb * F8_BLOCK), q.scales = q.fused ? 0 : f8_round((size_t)p->M * nb * sizeof(float));
+        q.bytes = q.codes + q.scales;
+        return q;
+    }
+    q.codes = f8_round((size_t)p->M * nb * F8_BLOCK), q.scales = f8_round((size_t)p->M * nb * sizeof(float));
+    const int64_t tiles = ((p->M + 127) / 128) * ((p->w.N + 127) / 128);
+    int64_t s = tiles < 256 ? 256 / tiles : 1;
+    if (s > nb / 4) s = nb / 4;
+    q.splits = s < 1 ? 1 : s > 16 ? 16 : (int)s;
+    q.bytes = q.codes + q.scales + (q.splits > 1 ? (size_t)q.splits * p->M * p->w.N * sizeof(float) : 0);
+    return q;
+}
+
+static bl_status f8_check_product(const bl_f8_product* p, bl_prod_dev* prod) {
+    if (!p) return BL_ERR_NULL;
+    if (const bl_status rc = f8_check(&p->w)) return rc;
+    if (!p->y || !p->prod.in0) return BL_ERR_NULL;
+    if (p->y_kind != BL_F8_OUT_F32 && p->y_kind != BL_F8_OUT_BF16) return BL_ERR_VALUE;
+    if (p->M < 1 || p->M > BL_MAX_DIM || p->y_stride < p->w.N || p->y_stride > ((int64_t)1 << 40)) return BL_ERR_SHAPE;
+    if (!bl_aligned(p->y, p->y_kind == BL_F8_OUT_F32 ? 4 : 2)) return BL_ERR_ALIGN;
+    if (!bl_make_prod(p->prod, nullptr, p->w.K, prod)) return BL_ERR_VALUE;
+    /* (tiles are counted in 32 bits) */
+    if (((p->M + 127) / 128) * ((p->w.N + 127) / 128) * 16 > 0x7fffffff) return BL_ERR_SHAPE;
+    return BL_OK;
+}
+
+extern "C" size_t bl_f8_workspace_bytes(const bl_f8_product* p) {
+    bl_prod_dev prod;
+    return f8_check_product(p, &prod) == BL_OK ? f8_make_plan(p).bytes : 0;
+}
+
+template <int MT, int KB, bool FUSED>
+static void f8_stream_kernel(const f8_args& A, const bl_prod_dev& P, hipStream_t st) {
+    const int strips = (A.N + 15) / 16, most = KB * (MT + 1) <= 6 ? 512 : 256;
+    bl_f8_stream<MT, KB, FUSED><<<(unsigned)(strips < most ? strips : most), F8_WAVES * 64, 0, st>>>(A, P);
+}
+static bl_status f8_stream_launch(const f8_args& A, const bl_prod_dev& P, const f8_plan& q, hipStream_t st) {
+#define F8_STREAM(T, B) case (T) * 16 + (B): f8_stream_kernel<T, B, (T) == 1>(A, P, st); break
+    switch (q.tokens * 16 + q.blocks) {
+        F8_STREAM(1, 1); F8_STREAM(1, 2); F8_STREAM(1, 3); F8_STREAM(1, 4); F8_STREAM(1, 6); F8_STREAM(1, 8);
+        F8_STREAM(2, 1); F8_STREAM(2, 2); F8_STREAM(2, 3); F8_STREAM(2, 4); F8_STREAM(2, 6);
+        F8_STREAM(3, 1); F8_STREAM(3, 2); F8_STREAM(3, 3); F8_STREAM(3, 4);
+        F8_STREAM(4, 1); F8_STREAM(4, 2); F8_STREAM(4, 3);
+        default: return BL_ERR_SHAPE;
+    }
+#undef F8_STREAM
+    return hipGetLastError() == hipSuccess ? BL_OK : BL_ERR_HIP;
+}
+template <int BM, int BN, int WM, int WN, int S>
+static bl_status f8_tile_launch(f8_args& A, hipStream_t st) {
+    constexpr int bytes = S * (BM + BN) * F8_BLOCK;
+    const auto kern = bl_f8_tile<BM, BN, WM, WN, S>;
+    static std::atomic<bool> attr_set;
+    if (!attr_set.load(std::memory_order_acquire)) {
+        if (hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) != hipSuccess) return BL_ERR_HIP;
+        attr_set.store(true, std::memory_order_release);
+    }
+    A.tiles_m = (A.M + BM - 1) / BM, A.tiles_n = (A.N + BN - 1) / BN;
+    kern<<<(unsigned)(A.tiles_m * A.tiles_n * A.splits), WM * WN * 64, bytes, st>>>(A);
+    return hipGetLastError() == hipSuccess ? BL_OK : BL_ERR_HIP;
+}
+
+extern "C" bl_status bl_f8_linear(const bl_f8_product* p, bl_stream s) {
+    bl_prod_dev prod;
+    if (const bl_status rc = f8_check_product(p, &prod)) return rc;
+    const f8_plan q = f8_make_plan(p);
+    if (q.bytes && !p->workspace) return BL_ERR_WORKSPACE;
+    if (!bl_aligned(p->workspace, 256)) return BL_ERR_ALIGN;
+    f8_args A = {};
+    A.w = p->w.codes, A.ws = p->w.scale, A.w_stride = p->w.stride, A.ws_stride = p->w.scale_stride;
+    A.codes = (uint8_t*)p->workspace, A.scales = (float*)(A.codes + q.codes), A.part = (float*)(A.codes + q.codes + q.scales);
+    A.y = p->y, A.y_stride = p->y_stride, A.M = (int)p->M, A.N = (int)p->w.N, A.K = (int)p->w.K, A.nb = (A.K + F8_BLOCK - 1) / F8_BLOCK;
+    A.bf16 = p->y_kind == BL_F8_OUT_BF16, A.wide = bl_aligned(p->y, 16) && p->y_stride % (A.bf16 ? 8 : 4) == 0, A.splits = q.splits;
+    const hipStream_t st = (hipStream_t)s;
+    if (!q.fused) bl_f8_rows<<<(unsigned)A.M, 256, 0, st>>>(A, prod);
+    if (q.tokens) return f8_stream_launch(A, prod, q, st);
+    const bl_status rc = f8_tile_launch<128, 128, 2, 2, 2>(A, st);
+    if (rc) return rc;
+    if (A.splits > 1) {
+        const int64_t blocks = ((int64_t)A.M * A.N + 255) / 256;
+        bl_f8_join<<<(unsigned)(blocks < 65536 ? blocks : 65536), 256, 0, st>>>(A);
+    }
+    return hipGetLastError() == hipSuccess ? BL_OK : BL_ERR_HIP;
+}
+
+extern "C" bl_status bl_f8_embed(const bl_f8_lookup* l, bl_stream s) {
+    if (!l) return BL_ERR_NULL;
+    if (const bl_status rc = f8_check(&l->w)) return rc;
+    if (!l->ids || !l->out) return BL_ERR_NULL;
+    if (l->out_kind != BL_F8_OUT_F32 && l->out_kind != BL_F8_OUT_BF16) return BL_ERR_VALUE;
+    if (l->T < 1 || l->T > BL_MAX_DIM || l->out_stride < l->w.K || l->out_stride > ((int64_t)1 << 40)) return BL_ERR_SHAPE;
+    const int V = l->out_kind == BL_F8_OUT_F32 ? 4 : 8;
+    if (!bl_aligned(l->ids, 4) || !bl_aligned(l->bad, 4) || !bl_aligned(l->out, 16) || l->out_stride % V) return BL_ERR_ALIGN;
+    f8_lookup_args A = {l->w.codes, l->w.scale, l->w.stride, l->w.scale_stride, l->out_stride, l->T * (l->w.K / V), l->ids, l->out, l->bad,
+                        (int)l->w.N, (int)(l->w.K / V), l->multiplier};
+    const int64_t blocks = (A.all + 255) / 256;
+    const unsigned grid = (unsigned)(blocks < 1 << 20 ? blocks : 1 << 20);
+    if (V == 8) bl_f8_embed_kernel<true><<<grid, 256, 0, (hipStream_t)s>>>(A);
+    else bl_f8_embed_kernel<false><<<grid, 256, 0, (hipStream_t)s>>>(A);
+    return hipGetLastError() == hipSuccess ? BL_OK : BL_ERR_HIP;
+}

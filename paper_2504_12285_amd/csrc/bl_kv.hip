@@ -110,6 +110,7 @@ __device__ __forceinline__ void tab_row(int64_t t, int B, const int* q_start, co
 struct tab_args {
     bl_kv_batch b;
     int shift, max_new;
+    const int32_t* held;
 };
 
 /* One workgroup: a handful of requests, or a few thousand, is latency and not work.  Three sums over the requests (rows
@@ -117,7 +118,7 @@ struct tab_args {
  * request's thread), then the rows.  A thread holds PER consecutive requests where there are more than threads.
  * Bound by the launch and three dependent reads (lengths, stack, table): 8 requests 3.9 us, 512 with 33 thousand rows, 57 of them
  * ending, 9 and 4 for the rows' own kernel.  Above 1024 requests (PER 4: 30 vector registers spilled) 1025 take 12.7 us, 2048 17.2, 4096 30. */
-template <int THREADS, int PER, bool LIMIT>
+template <int THREADS, int PER, bool LIMIT, bool HELD>
 __global__ __launch_bounds__(THREADS) void bl_kv_tables_kernel(tab_args A) {
     const bl_kv_batch& b = A.b;
     constexpr int MOST = THREADS * PER, WAVES = THREADS / BL_WAVE, IN = 8;
@@ -129,19 +130,24 @@ __global__ __launch_bounds__(THREADS) void bl_kv_tables_kernel(tab_args A) {
     if (tid == 0) s_taken = s_bad = s_back = s_want = 0;
     const int64_t cap = b.free_cap;
     int64_t there = b.free_count[0];
-    int old[PER], n[PER];
+    int old[PER], n[PER], hold[PER];                          /* hold: blocks in front that an ended request does not give back */
     int64_t rows = 0, back = 0;
+    auto gives = [&](int i) -> int {
+        const int have = (int)(((int64_t)old[i] + bs1) >> shift);
+        return n[i] >= 0 ? 0 : !HELD ? have : have > hold[i] ? have - hold[i] : 0;
+    };
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
         const int r = tid * per + i;
-        old[i] = n[i] = 0;
+        old[i] = n[i] = hold[i] = 0;
         if (i < per && r < B) {
+            if (HELD) hold[i] = A.held[r] > 0 ? A.held[r] : 0;
             const int64_t most = (int64_t)b.max_blocks << shift;
             const int64_t L = b.seq_len[r];
             old[i] = (int)(L < 0 ? 0 : L > most ? most : L);
             n[i] = b.new_len[r];
         }
-        if (n[i] < 0) back += ((int64_t)old[i] + bs1) >> shift;
+        if (n[i] < 0) back += gives(i);
         else rows += n[i];
     }
     there = there < 0 ? 0 : there > cap ? cap : there;
@@ -153,14 +159,15 @@ __global__ __launch_bounds__(THREADS) void bl_kv_tables_kernel(tab_args A) {
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             if (i >= per) break;
-            const int r = tid * per + i, have = n[i] < 0 ? (int)(((int64_t)old[i] + bs1) >> shift) : 0;
+            const int r = tid * per + i, have = gives(i);
+            if (HELD && have > 0) s_start[r] = hold[i];       /* (for now) */
             if (have > 0 && at + have > cap) atomicAdd(&s_bad, 1);
             if (have > 0) s_from[r] = (int)(at < cap ? at : cap), s_n[r] = at < cap ? (int)(cap - at < have ? cap - at : have) : 0;
             tab_list(have > 0, r, s_list, &s_back);
             at += have;
         }
         __syncthreads();
-        tab_copy<WAVES, IN, 1>(s_list, s_back, s_n, [&](int r) { return b.table + r * b.table_stride; }, [&](int r) { return b.free_list + s_from[r]; });
+        tab_copy<WAVES, IN, 1>(s_list, s_back, s_n, [&](int r) { return b.table + r * b.table_stride + (HELD ? s_start[r] : 0); }, [&](int r) { return b.free_list + s_from[r]; });
     }
     there = there + all_back > cap ? cap : there + all_back;
     /* demand */
@@ -239,9 +246,10 @@ __global__ __launch_bounds__(256) void bl_kv_slots_kernel(tab_args A) {
     if (t < b.rows) tab_row(t, (int)b.B, b.q_start, b.start, b.table, b.table_stride, A.shift, b.positions, b.slots);
 }
 
-/* LIMIT: with a most of new tokens a request (a kernel of its own: above 1024 requests the comparison costs the others 1.2 us). */
-template <bool LIMIT>
-static bl_status tab_launch(const bl_kv_batch* b, int max_new, bl_stream s) {
+/* LIMIT: with a most of new tokens a request (a kernel of its own: above 1024 requests the comparison costs the others 1.2 us).
+ * HELD: with blocks in front that are not given back (a kernel of its own too). */
+template <bool LIMIT, bool HELD = false>
+static bl_status tab_launch(const bl_kv_batch* b, int max_new, bl_stream s, const int32_t* held = nullptr) {
     if (!b->seq_len || !b->new_len || !b->free_count || !b->table || (!b->free_list && b->free_cap) || !b->seq_len_out || !b->free_count_out || !b->start ||
         !b->q_start || !b->positions || !b->slots || !b->bad)
         return BL_ERR_NULL;
@@ -252,12 +260,12 @@ static bl_status tab_launch(const bl_kv_batch* b, int max_new, bl_stream s) {
     const void* p[] = {b->seq_len, b->new_len, b->free_count, b->table, b->free_list, b->seq_len_out, b->free_count_out, b->start, b->q_start, b->positions, b->slots, b->bad};
     for (const void* q : p)
         if (!bl_aligned(q, 4)) return BL_ERR_ALIGN;
-    tab_args A = {*b, bl_log2(b->block), max_new};
+    tab_args A = {*b, bl_log2(b->block), max_new, held};
     /* A small step's barriers are those of four waves instead of sixteen: 1, 64 and 256 decoding requests 2.8, 4.4 and 5.8 us, with sixteen 4.3, 5.9 and
      * 6.5; beside a chunk of 1024 rows the rows' loop has the more of it: 64 and 256 requests 7.6 and 9.4 us with four, 7.2 and 7.8 with sixteen. */
-    if (b->B <= 256 && b->rows <= 1024) bl_kv_tables_kernel<256, 1, LIMIT><<<1, 256, 0, (hipStream_t)s>>>(A);
-    else if (b->B <= 1024) bl_kv_tables_kernel<1024, 1, LIMIT><<<1, 1024, 0, (hipStream_t)s>>>(A);
-    else bl_kv_tables_kernel<1024, BL_KV_MAX_REQUESTS / 1024, LIMIT><<<1, 1024, 0, (hipStream_t)s>>>(A);
+    if (b->B <= 256 && b->rows <= 1024) bl_kv_tables_kernel<256, 1, LIMIT, HELD><<<1, 256, 0, (hipStream_t)s>>>(A);
+    else if (b->B <= 1024) bl_kv_tables_kernel<1024, 1, LIMIT, HELD><<<1, 1024, 0, (hipStream_t)s>>>(A);
+    else bl_kv_tables_kernel<1024, BL_KV_MAX_REQUESTS / 1024, LIMIT, HELD><<<1, 1024, 0, (hipStream_t)s>>>(A);
     if (b->rows > TAB_ROWS_INSIDE) bl_kv_slots_kernel<<<(unsigned)((b->rows + 255) / 256), 256, 0, (hipStream_t)s>>>(A);
     return hipGetLastError() == hipSuccess ? BL_OK : BL_ERR_HIP;
 }
@@ -270,6 +278,13 @@ extern "C" bl_status bl_kv_tables_limited(const bl_kv_limited_batch* b, bl_strea
     return tab_launch<true>(&b->batch, b->max_new < 0x7fffffff ? (int)b->max_new : 0x7fffffff, s);
 }
 
+extern "C" bl_status bl_kv_tables_held(const bl_kv_held_batch* b, bl_stream s) {
+    if (!b || !b->held) return BL_ERR_NULL;
+    if (b->max_new < 0) return BL_ERR_SHAPE;
+    if (!bl_aligned(b->held, 4)) return BL_ERR_ALIGN;
+    return tab_launch<true, true>(&b->batch, b->max_new && b->max_new < 0x7fffffff ? (int)b->max_new : 0x7fffffff, s, b->held);
+}
+
 /* ---- rotary append ----------------------------------------------------------------------------------------------- */
 
 #define APP_THREADS 256
@@ -277,7 +292,45 @@ extern "C" bl_status bl_kv_tables_limited(const bl_kv_limited_batch* b, bl_strea
 struct app_args {
     bl_kv_tokens t;
     int shift, window, windows;            /* log2(block); rows of a K/V workgroup, and how many such there are */
+    const float* q_gain;                   /* of the norms, or NULL */
+    const float* k_gain;
+    float eps;
 };
+
+/* Sum of v over aligned groups of G lanes (4, 8 or 16), the same bits in every lane. */
+template <int CTRL>
+__device__ __forceinline__ double app_moved(double v) {
+    const uint64_t u = __builtin_bit_cast(uint64_t, v);
+    return __builtin_bit_cast(double, (uint64_t)(uint32_t)bl_dpp<CTRL>((int)(u >> 32)) << 32 | (uint32_t)bl_dpp<CTRL>((int)(uint32_t)u));
+}
+template <int G>
+__device__ __forceinline__ double app_sum(double v) {
+    static_assert(G == 4 || G == 8 || G == 16, "group size");
+    v += app_moved<BL_DPP_QUAD_XOR1>(v);
+    v += app_moved<BL_DPP_QUAD_XOR2>(v);
+    if (G >= 8) v += app_moved<BL_DPP_ROW_HALF_MIRROR>(v);
+    if (G >= 16) v += app_moved<BL_DPP_ROW_MIRROR>(v);
+    return v;
+}
+/* RMS norm of a head whose D values lie in G lanes, 2 * N each: the mean square in 64 bits (its squares are exact there), so that the factor of 32 bits is
+ * the same whatever the order of the sum; then two rounded products. */
+template <int G, int D, int N>
+__device__ __forceinline__ void app_norm(float (&a)[N], float (&b)[N], float eps, const float* gain, int i) {
+    double ss = 0.0;
+#pragma unroll
+    for (int j = 0; j < N; ++j) ss += (double)a[j] * (double)a[j] + (double)b[j] * (double)b[j];
+    const float r = (float)(1.0 / sqrt(app_sum<G>(ss) / (double)D + (double)eps));
+#pragma unroll
+    for (int j = 0; j < N; ++j) a[j] *= r, b[j] *= r;
+    if (gain) {
+#pragma unroll
+        for (int j = 0; j < N; j += 4) {
+            const bl_v4f x = *bl_gc<bl_v4f>(gain + i + j), y = *bl_gc<bl_v4f>(gain + i + j + D / 2);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) a[j + e] *= x[e], b[j + e] *= y[e];
+        }
+    }
+}
 
 typedef uint32_t app_v4u __attribute__((ext_vector_type(4)));
 /* Four consecutive values of a row. */
@@ -296,11 +349,13 @@ template <int SRC>
 __device__ __forceinline__ const void* app_row(const app_args& A, int64_t t) {
     return SRC == BL_KV_FROM_F32 ? (const void*)((const float*)A.t.qkv + t * A.t.qkv_stride) : (const void*)((const uint16_t*)A.t.qkv + t * A.t.qkv_stride);
 }
-/* Values i..i+3 and i+D/2..i+D/2+3 of head h of a row, turned by the angles of position pos where `turn`. */
-template <int SRC, int D>
-__device__ __forceinline__ void app_pair(const app_args& A, const void* row, int h, int i, bool turn, int64_t pos, float (&a)[4], float (&b)[4]) {
+/* Values i..i+3 and i+D/2..i+D/2+3 of head h of a row, normed (NORM: where `key`; the row's D / 8 lanes are here together), turned by the
+ * angles of position pos where `turn`. */
+template <int SRC, int D, bool NORM>
+__device__ __forceinline__ void app_pair(const app_args& A, const void* row, int h, int i, bool key, bool turn, int64_t pos, float (&a)[4], float (&b)[4]) {
     app_load4<SRC>(row, (int64_t)h * D + i, a);
     app_load4<SRC>(row, (int64_t)h * D + i + D / 2, b);
+    if (NORM && key) app_norm<D / 8, D>(a, b, A.eps, A.k_gain, i);
     if (turn) {
         const bl_v4f c = *bl_gc<bl_v4f>(A.t.cos + pos * (D / 2) + i), s = *bl_gc<bl_v4f>(A.t.sin + pos * (D / 2) + i);
 #pragma unroll
@@ -348,7 +403,7 @@ __device__ __forceinline__ void app_move(uint8_t* p, int bytes, float ratio) {
  * A thread has four values of a row and their rotary partners, D / 8 threads a row, NP rows.
  * Bound by HBM for prompts: 4096 tokens of 20 + 5 heads of 128 from fp32, 91 MB, 20.7 us = 4.4 TB/s (a large copy: 4.7); 19613 tokens of
  * 32 + 8 heads of 64 from bf16 into blocks of 16, 226 MB, 60 us = 3.8.  By the launch and the chain slots -> rows -> maximum -> codes for single tokens: 4.2 us. */
-template <int SRC, int KIND, int D, int NP, int WAVES>
+template <int SRC, int KIND, int D, int NP, int WAVES, bool NORM>
 __device__ __forceinline__ void app_cache_rows(const app_args& A, int64_t first, int pair) {
     constexpr int UNITS = APP_THREADS / BL_WAVE / WAVES;
     constexpr int TPR = D / 8, UT = WAVES * BL_WAVE, ROWS = UT / TPR;   /* threads a row, threads a unit, rows a pass */
@@ -424,7 +479,7 @@ __device__ __forceinline__ void app_cache_rows(const app_args& A, int64_t first,
                     if (l0 + r >= 128) place = third;
                 }
             }
-            if (live && has(r)) app_pair<SRC, D>(A, app_row<SRC>(A, t0 + r), head, i4, !is_v && A.t.cos, place, a[p], b[p]);
+            if (live && has(r)) app_pair<SRC, D, NORM>(A, app_row<SRC>(A, t0 + r), head, i4, !is_v, !is_v && A.t.cos, place, a[p], b[p]);
             else
 #pragma unroll
                 for (int j = 0; j < 4; ++j) a[p][j] = b[p][j] = 0.0f;
@@ -536,7 +591,7 @@ __device__ __forceinline__ void app_load8(const void* row, int64_t i, float (&v)
 }
 /* Q: a thread has eight values and their partners, the same ones of APP_HEADS heads of a row (their angles are read once). */
 #define APP_HEADS 2
-template <int SRC, int D>
+template <int SRC, int D, bool NORM>
 __device__ __forceinline__ void app_query_units(const app_args& A, uint32_t u, uint32_t units_row, uint32_t all) {
     constexpr int TPH = D / 16;                                         /* threads a head */
     if (u >= all) return;
@@ -559,6 +614,7 @@ __device__ __forceinline__ void app_query_units(const app_args& A, uint32_t u, u
 #pragma unroll
     for (int k = 0; k < APP_HEADS; ++k)
         if (h0 + k < A.t.n_q) {
+            if (NORM) app_norm<TPH, D>(a[k], b[k], A.eps, A.q_gain, i);
             if (A.t.cos) {
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
@@ -574,7 +630,7 @@ __device__ __forceinline__ void app_query_units(const app_args& A, uint32_t u, u
 }
 
 /* Workgroups of K and V (window x head pairs) first, those of Q behind them. */
-template <int SRC, int KIND, int D, int NP, int WAVES>
+template <int SRC, int KIND, int D, int NP, int WAVES, bool NORM>
 __global__ __launch_bounds__(APP_THREADS) void bl_kv_append_kernel(app_args A, int kv_blocks, uint32_t units_row, uint32_t all) {
     const int x = (int)blockIdx.x;
     if (x < kv_blocks) {
@@ -582,32 +638,34 @@ __global__ __launch_bounds__(APP_THREADS) void bl_kv_append_kernel(app_args A, i
          * a contiguous eighth of the windows, else a few dies have all the work (4096 tokens 37 -> 22 us). */
         const int pairs = kv_blocks / A.windows, die = x & 7, part = kv_blocks >> 3, more = kv_blocks & 7;
         const int at = die * part + (die < more ? die : more) + (x >> 3);
-        app_cache_rows<SRC, KIND, D, NP, WAVES>(A, (int64_t)(at / pairs) * A.window, at % pairs);
+        app_cache_rows<SRC, KIND, D, NP, WAVES, NORM>(A, (int64_t)(at / pairs) * A.window, at % pairs);
     }
-    else app_query_units<SRC, D>(A, (uint32_t)(x - kv_blocks) * APP_THREADS + threadIdx.x, units_row, all);
+    else app_query_units<SRC, D, NORM>(A, (uint32_t)(x - kv_blocks) * APP_THREADS + threadIdx.x, units_row, all);
 }
 
-template <int SRC, int KIND, int D, int NP, int WAVES>
+template <bool NORM, int SRC, int KIND, int D, int NP, int WAVES>
 static bl_status app_launch(const app_args& A, hipStream_t st) {
     constexpr int UNITS = APP_THREADS / BL_WAVE / WAVES;
     const int64_t units_row = A.t.q_out ? (int64_t)((A.t.n_q + APP_HEADS - 1) / APP_HEADS) * (D / 16) : 0, all = A.t.T * units_row;
     const int64_t kv = (int64_t)A.windows * ((2 * A.t.cache.n_kv + UNITS - 1) / UNITS), q = (all + APP_THREADS - 1) / APP_THREADS;
     if (all > 0xf0000000ll || kv + q > 0x7fffffff) return BL_ERR_SHAPE;
-    bl_kv_append_kernel<SRC, KIND, D, NP, WAVES><<<(unsigned)(kv + q), APP_THREADS, 0, st>>>(A, (int)kv, units_row ? (uint32_t)units_row : 1, (uint32_t)all);
+    bl_kv_append_kernel<SRC, KIND, D, NP, WAVES, NORM><<<(unsigned)(kv + q), APP_THREADS, 0, st>>>(A, (int)kv, units_row ? (uint32_t)units_row : 1, (uint32_t)all);
     return BL_OK;
 }
 /* Waves and passes by the block's size: 1024 to 2048 values of a block and head are one wave's, 16384 four waves' in eight passes. */
-template <int SRC, int KIND>
+template <bool NORM, int SRC, int KIND>
 static bl_status app_choose(const app_args& A, hipStream_t st) {
     if (A.t.cache.head_dim == 128)
-        return A.shift == 4 ? app_launch<SRC, KIND, 128, 4, 1>(A, st) : A.shift == 5 ? app_launch<SRC, KIND, 128, 4, 2>(A, st)
-             : A.shift == 6 ? app_launch<SRC, KIND, 128, 4, 4>(A, st) : app_launch<SRC, KIND, 128, 8, 4>(A, st);
-    return A.shift == 4 ? app_launch<SRC, KIND, 64, 2, 1>(A, st) : A.shift == 5 ? app_launch<SRC, KIND, 64, 4, 1>(A, st)
-         : A.shift == 6 ? app_launch<SRC, KIND, 64, 4, 2>(A, st) : app_launch<SRC, KIND, 64, 4, 4>(A, st);
+        return A.shift == 4 ? app_launch<NORM, SRC, KIND, 128, 4, 1>(A, st) : A.shift == 5 ? app_launch<NORM, SRC, KIND, 128, 4, 2>(A, st)
+             : A.shift == 6 ? app_launch<NORM, SRC, KIND, 128, 4, 4>(A, st) : app_launch<NORM, SRC, KIND, 128, 8, 4>(A, st);
+    return A.shift == 4 ? app_launch<NORM, SRC, KIND, 64, 2, 1>(A, st) : A.shift == 5 ? app_launch<NORM, SRC, KIND, 64, 4, 1>(A, st)
+         : A.shift == 6 ? app_launch<NORM, SRC, KIND, 64, 4, 2>(A, st) : app_launch<NORM, SRC, KIND, 64, 4, 4>(A, st);
 }
 
-extern "C" bl_status bl_kv_append(const bl_kv_tokens* t, bl_stream s) {
-    if (!t || !t->qkv || !t->slots) return BL_ERR_NULL;
+/* NORM: the norms of bl_kv_append_norm (kernels of their own). */
+template <bool NORM>
+static bl_status app_run(const bl_kv_tokens* t, const float* q_gain, const float* k_gain, float eps, bl_stream s) {
+    if (!t->qkv || !t->slots) return BL_ERR_NULL;
     if (const bl_status rc = bl_kv_cache_check(&t->cache)) return rc;
     if (!t->cos != !t->sin || (t->cos && !t->positions)) return BL_ERR_NULL;
     if (t->qkv_kind != BL_KV_FROM_F32 && t->qkv_kind != BL_KV_FROM_BF16) return BL_ERR_VALUE;
@@ -619,7 +677,7 @@ extern "C" bl_status bl_kv_append(const bl_kv_tokens* t, bl_stream s) {
     if (!bl_aligned(t->qkv, 16) || t->qkv_stride % unit || !bl_aligned(t->cos, 16) || !bl_aligned(t->sin, 16) || !bl_aligned(t->slots, 4) ||
         !bl_aligned(t->positions, 4) || !bl_aligned(t->bad, 4) || !bl_aligned(t->q_out, 16) || (t->q_out && t->q_stride % 8))
         return BL_ERR_ALIGN;
-    app_args A = {*t, bl_log2(t->cache.block), 1, 0};
+    app_args A = {*t, bl_log2(t->cache.block), 1, 0, q_gain, k_gain, eps};
     /* rows a K/V workgroup: one where they are few (each is a run of its own in a decode step), more where they are many (the
      * runs of prompts start in few windows, and a workgroup without one is not free).  Windows of 1, 2, 4, 8 and 16 rows, us: 64 single tokens 5.0, 6.2,
      * 9.4, 16, 29; 1024 of them 25, 22, 23, 24, 37; 4096 104, 88, 80, 79, 90; a prompt of 512 13, 8.4, 8.4, 8.3, 8.3; of 1024 25, 15, 11.4, 10.3, 10.1;
@@ -628,8 +686,17 @@ extern "C" bl_status bl_kv_append(const bl_kv_tokens* t, bl_stream s) {
     A.windows = (int)((t->T + A.window - 1) / A.window);
     const hipStream_t st = (hipStream_t)s;
     const bool f32 = t->qkv_kind == BL_KV_FROM_F32, i8 = t->cache.kind == BL_KV_INT8;
-    const bl_status rc = f32 ? i8 ? app_choose<BL_KV_FROM_F32, BL_KV_INT8>(A, st) : app_choose<BL_KV_FROM_F32, BL_KV_E4M3>(A, st)
-                             : i8 ? app_choose<BL_KV_FROM_BF16, BL_KV_INT8>(A, st) : app_choose<BL_KV_FROM_BF16, BL_KV_E4M3>(A, st);
+    const bl_status rc = f32 ? i8 ? app_choose<NORM, BL_KV_FROM_F32, BL_KV_INT8>(A, st) : app_choose<NORM, BL_KV_FROM_F32, BL_KV_E4M3>(A, st)
+                             : i8 ? app_choose<NORM, BL_KV_FROM_BF16, BL_KV_INT8>(A, st) : app_choose<NORM, BL_KV_FROM_BF16, BL_KV_E4M3>(A, st);
     if (rc) return rc;
     return hipGetLastError() == hipSuccess ? BL_OK : BL_ERR_HIP;
+}
+
+extern "C" bl_status bl_kv_append(const bl_kv_tokens* t, bl_stream s) { return t ? app_run<false>(t, nullptr, nullptr, 0.0f, s) : BL_ERR_NULL; }
+
+extern "C" bl_status bl_kv_append_norm(const bl_kv_norm_tokens* t, bl_stream s) {
+    if (!t) return BL_ERR_NULL;
+    if (!(t->eps > 0.0f) || t->eps > 3e38f) return BL_ERR_VALUE;
+    if (!bl_aligned(t->q_gain, 16) || !bl_aligned(t->k_gain, 16)) return BL_ERR_ALIGN;
+    return app_run<true>(&t->tokens, t->q_gain, t->k_gain, t->eps, s);
 }

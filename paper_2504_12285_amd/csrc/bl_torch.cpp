@@ -26,7 +26,9 @@ decode_fn g_decode;
 typedef bl_status (*run_fn)(void*, const bl_stack_plan*, bl_stream);
 run_fn g_run;
 typedef bl_status (*kv_fn)(const void*, bl_stream);
-kv_fn g_kv[4];                           /* tables, append, attention, tables with a limit */
+/* tables, append, attention, tables with a limit, tables with held blocks, append with norms, attention over shared prefixes, 8-bit float product and lookup */
+constexpr int CALLS = 9;
+kv_fn g_kv[CALLS];
 
 /* A tensor argument: exactly torch.Tensor or None. */
 bool get(PyObject* o, const at::Tensor** t) {
@@ -190,7 +192,7 @@ PyObject* run(PyObject*, PyObject* const* a, Py_ssize_t n) {
 PyObject* kv(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return guarded([&]() -> PyObject* {
         int64_t which, desc;
-        if (n != 2 || !plain() || !get(a[0], &which) || which < 0 || which > 3 || !get(a[1], &desc) || !desc) return nullptr;
+        if (n != 2 || !plain() || !get(a[0], &which) || which < 0 || which >= CALLS || !get(a[1], &desc) || !desc) return nullptr;
         const bl_stream st = stream();
         bl_status rc;
         Py_BEGIN_ALLOW_THREADS
@@ -214,11 +216,12 @@ PyObject* bind(PyObject*, PyObject* args) {
     Py_RETURN_NONE;
 }
 
-/* The addresses of bl_kv_tables, bl_kv_append, bl_attn_kv8 and bl_kv_tables_limited in the loaded library. */
+/* The addresses of bl_kv_tables, bl_kv_append, bl_attn_kv8, bl_kv_tables_limited, bl_kv_tables_held, bl_kv_append_norm, bl_attn_kv8_shared, bl_f8_linear and
+ * bl_f8_embed in the loaded library. */
 PyObject* bind_kv(PyObject*, PyObject* args) {
-    unsigned long long f[4];
-    if (!PyArg_ParseTuple(args, "KKKK", f, f + 1, f + 2, f + 3)) return nullptr;
-    for (int i = 0; i < 4; ++i) g_kv[i] = (kv_fn)f[i];
+    unsigned long long f[CALLS];
+    if (!PyArg_ParseTuple(args, "KKKKKKKKK", f, f + 1, f + 2, f + 3, f + 4, f + 5, f + 6, f + 7, f + 8)) return nullptr;
+    for (int i = 0; i < CALLS; ++i) g_kv[i] = (kv_fn)f[i];
     Py_RETURN_NONE;
 }
 

@@ -1,0 +1,161 @@
+"""Calls of the 8-bit float matrix, of shared prefixes and of the append with norms on the host: every refusal comes before any GPU work, sizes are
+right, and the binding takes only tensors that a descriptor can stand for.  Needs no GPU."""
+import ctypes
+
+import pytest
+
+from paper_2504_12285_amd import binding as bl
+from test_kv_host import ALIGN, BAD_ATTENTION, BAD_CACHES, NULL, P, SHAPE, VALUE, WORKSPACE, attention, cache, lib, tables, tokens  # noqa: F401
+
+torch = pytest.importorskip("torch")
+
+
+def held(batch=None, **more):
+    return bl.KVHeldBatchDesc(**dict(dict(batch=batch or tables(), max_new=0, held=P), **more))
+
+
+@pytest.mark.parametrize("d, status", [(dict(held=None), NULL), (dict(held=P + 2), ALIGN), (dict(max_new=-1), SHAPE), (dict(batch=tables(B=0)), SHAPE),
+                                       (dict(batch=tables(bad=None)), NULL)])
+def test_held_tables_refuse(lib, d, status):  # noqa: F811
+    assert lib.bl_kv_tables_held(ctypes.byref(held(**d)), None) == status
+    assert lib.bl_kv_tables_held(None, None) == NULL
+
+
+def norm(t=None, **more):
+    return bl.KVNormTokensDesc(**dict(dict(tokens=t or tokens(), q_gain=P, k_gain=P, eps=1e-5), **more))
+
+
+@pytest.mark.parametrize("d, status", [(dict(eps=0.0), VALUE), (dict(eps=-1.0), VALUE), (dict(eps=float("nan")), VALUE), (dict(eps=float("inf")), VALUE),
+                                       (dict(q_gain=P + 4), ALIGN), (dict(k_gain=P + 8), ALIGN), (dict(t=tokens(T=0)), SHAPE), (dict(t=tokens(qkv=None)), NULL),
+                                       (dict(t=tokens(qkv_stride=30 * 128 - 4)), SHAPE)])
+def test_append_with_norms_refuses(lib, d, status):  # noqa: F811
+    assert lib.bl_kv_append_norm(ctypes.byref(norm(**d)), None) == status
+    assert lib.bl_kv_append_norm(None, None) == NULL
+
+
+def shared(a=None, **more):
+    return bl.AttnSharedDesc(**dict(dict(attn=a or attention(), group=P, shared_blocks=P, shared_table=P, shared_stride=6, n_groups=3, max_shared=6, max_own=0), **more))
+
+
+@pytest.mark.parametrize("d, status", [(dict(group=None), NULL), (dict(shared_blocks=None), NULL), (dict(shared_table=None), NULL), (dict(n_groups=0), SHAPE),
+                                       (dict(n_groups=4097), SHAPE), (dict(max_shared=0), SHAPE), (dict(max_shared=7), SHAPE), (dict(max_own=-1), SHAPE),
+                                       (dict(max_shared=1 << 25, shared_stride=1 << 25), SHAPE), (dict(group=P + 2), ALIGN), (dict(shared_table=P + 1), ALIGN),
+                                       (dict(shared_blocks=P + 3), ALIGN)])
+def test_shared_attention_refuses(lib, d, status):  # noqa: F811
+    s = shared(**d)
+    assert lib.bl_attn_kv8_shared(ctypes.byref(s), None) == status
+    assert lib.bl_attn_shared_workspace_bytes(ctypes.byref(s)) == 0
+    assert lib.bl_attn_kv8_shared(None, None) == NULL
+
+
+@pytest.mark.parametrize("more, status", BAD_ATTENTION)
+def test_shared_attention_refuses_what_attention_does(lib, more, status):  # noqa: F811
+    assert lib.bl_attn_kv8_shared(ctypes.byref(shared(attention(**more))), None) == status
+
+
+@pytest.mark.parametrize("more, status", BAD_CACHES)
+def test_a_bad_cache_is_refused(lib, more, status):  # noqa: F811
+    assert lib.bl_attn_kv8_shared(ctypes.byref(shared(attention(cache(**more)))), None) == status
+    assert lib.bl_kv_append_norm(ctypes.byref(norm(tokens(cache(**more)))), None) == status
+
+
+def test_shared_attention_wants_its_workspace(lib):  # noqa: F811
+    assert lib.bl_attn_kv8_shared(ctypes.byref(shared(attention(workspace=None))), None) == WORKSPACE
+    assert lib.bl_attn_kv8_shared(ctypes.byref(shared(attention(workspace=P + 16))), None) == ALIGN
+    one, more = (lib.bl_attn_shared_workspace_bytes(ctypes.byref(shared(**d))) for d in (dict(), dict(max_shared=500, shared_stride=500)))
+    assert 0 < one < more
+
+
+def matrix(**more):
+    return bl.F8MatrixDesc(**dict(dict(codes=P, scale=P, N=200, K=192, stride=192, scale_stride=2), **more))
+
+
+BAD_MATRICES = [(dict(codes=None), NULL), (dict(scale=None), NULL), (dict(N=0), SHAPE), (dict(K=0), SHAPE), (dict(K=200, stride=256), SHAPE), (dict(K=32), SHAPE),
+                (dict(stride=128), SHAPE), (dict(scale_stride=1), SHAPE), (dict(N=(1 << 24) + 1), SHAPE), (dict(codes=P + 8), ALIGN), (dict(stride=200), ALIGN),
+                (dict(scale=P + 2), ALIGN)]
+
+
+def product(w=None, prod=None, **more):
+    d = dict(w=w or matrix(), prod=prod or bl.Producer(kind=bl.BL_PROD_F32, in0=P), M=3, y_stride=200, y=P, y_kind=0, workspace=P)
+    return bl.F8ProductDesc(**dict(d, **more))
+
+
+def lookup(w=None, **more):
+    return bl.F8LookupDesc(**dict(dict(w=w or matrix(), ids=P, T=4, out_stride=192, out=P, out_kind=0, multiplier=1.0, bad=P), **more))
+
+
+@pytest.mark.parametrize("more, status", BAD_MATRICES)
+def test_a_bad_matrix_is_refused(lib, more, status):  # noqa: F811
+    assert lib.bl_f8_linear(ctypes.byref(product(matrix(**more))), None) == status
+    assert lib.bl_f8_workspace_bytes(ctypes.byref(product(matrix(**more)))) == 0
+    assert lib.bl_f8_embed(ctypes.byref(lookup(matrix(**more))), None) == status
+
+
+@pytest.mark.parametrize("d, status", [(dict(y=None), NULL), (dict(prod=bl.Producer(kind=bl.BL_PROD_F32)), NULL), (dict(prod=bl.Producer(kind=9, in0=P)), VALUE),
+                                       (dict(prod=bl.Producer(kind=bl.BL_PROD_RESIDUAL, in0=P)), VALUE), (dict(prod=bl.Producer(kind=bl.BL_PROD_F32, in0=P + 4)), VALUE),
+                                       (dict(prod=bl.Producer(kind=bl.BL_PROD_F32, in0=P, norm=1, eps=-1.0)), VALUE), (dict(y_kind=2), VALUE), (dict(M=0), SHAPE),
+                                       (dict(M=(1 << 24) + 1), SHAPE), (dict(y_stride=199), SHAPE), (dict(y=P + 2), ALIGN), (dict(y=P + 1, y_kind=1), ALIGN),
+                                       (dict(w=matrix(N=1 << 24), M=1 << 24, y_stride=1 << 24), SHAPE), (dict(workspace=P + 16), ALIGN)])
+def test_product_refuses(lib, d, status):  # noqa: F811
+    assert lib.bl_f8_linear(ctypes.byref(product(**d)), None) == status
+    assert lib.bl_f8_linear(None, None) == NULL
+
+
+def test_product_wants_its_workspace(lib):  # noqa: F811
+    p = product(M=300, workspace=None)
+    assert lib.bl_f8_workspace_bytes(ctypes.byref(p)) >= 300 * 256 and lib.bl_f8_linear(ctypes.byref(p), None) == WORKSPACE
+
+
+@pytest.mark.parametrize("d, status", [(dict(ids=None), NULL), (dict(out=None), NULL), (dict(T=0), SHAPE), (dict(T=(1 << 24) + 1), SHAPE), (dict(out_stride=128), SHAPE),
+                                       (dict(out_kind=3), VALUE), (dict(out=P + 8), ALIGN), (dict(out_stride=194), ALIGN), (dict(out_stride=196, out_kind=1), ALIGN),
+                                       (dict(ids=P + 2), ALIGN), (dict(bad=P + 1), ALIGN)])
+def test_lookup_refuses(lib, d, status):  # noqa: F811
+    assert lib.bl_f8_embed(ctypes.byref(lookup(**d)), None) == status
+    assert lib.bl_f8_embed(None, None) == NULL
+
+
+def test_descriptors_have_the_size_of_the_header_s():
+    assert [ctypes.sizeof(c) for c in (bl.KVHeldBatchDesc, bl.KVNormTokensDesc, bl.AttnSharedDesc, bl.F8MatrixDesc, bl.F8ProductDesc, bl.F8LookupDesc)] == \
+        [152, 200, 240, 48, 152, 96]
+
+
+def test_the_binding_takes_what_a_descriptor_can_stand_for(lib):  # noqa: F811
+    f8, i32 = torch.float8_e4m3fn, torch.int32
+    pool = torch.zeros(200, 256, dtype=torch.uint8).view(f8)
+    m = bl.F8Matrix(pool[:, :192], torch.zeros(2, 2))
+    assert (m.desc.N, m.desc.K, m.desc.stride, m.desc.scale_stride) == (200, 192, 256, 2)
+    for bad in ((pool.view(torch.int8), torch.zeros(2, 2)), (pool, torch.zeros(2, 3)), (pool, torch.zeros(2, 2).double()), (pool.view(torch.uint8).t().view(f8), torch.zeros(2, 2))):
+        with pytest.raises((TypeError, ValueError)):
+            bl.F8Matrix(*bad)
+    x = torch.zeros(3, 192)
+    h = bl.F8Linear(m, x, dtype=torch.bfloat16)
+    assert h.y.shape == (3, 200) and h.desc.y_kind == bl.BL_F8_OUT_BF16 and h.workspace.numel() >= 3 * 256
+    assert bl.F8Linear(m, x, y=torch.zeros(3, 208)[:, :200], workspace=h.workspace).desc.y_stride == 208
+    for more in (dict(x=x.half()), dict(x=x[:, :128]), dict(x=x.t()), dict(), dict(x=x, prod=bl.Producer()), dict(prod=bl.Producer()), dict(x=x, y=torch.zeros(3, 100)),
+                 dict(x=x, gain=torch.zeros(3)), dict(x=x, dtype=torch.float16), dict(x=x, workspace=torch.zeros(8, dtype=torch.uint8))):
+        with pytest.raises((TypeError, ValueError)):
+            bl.F8Linear(m, **more)
+    ids = torch.zeros(5, dtype=i32)
+    assert bl.F8Embedding(m, ids).out.shape == (5, 192)
+    for more in (dict(ids=ids.long()), dict(ids=ids, out=torch.zeros(5, 200)), dict(ids=ids, bad=torch.zeros(2, dtype=i32)), dict(ids=ids, dtype=torch.int8)):
+        with pytest.raises((TypeError, ValueError)):
+            bl.F8Embedding(m, **more)
+    c = bl.KVCache.empty(6, 2, 16, 64, "cpu")
+    n, q, table = torch.zeros(3, dtype=i32), torch.zeros(4, 4, 64, dtype=torch.bfloat16), torch.zeros(3, 4, dtype=i32)
+    args = dict(cache=c, q=q, q_start=torch.zeros(4, dtype=i32), seq_len=n, table=table, group=n, shared_table=torch.zeros(2, 3, dtype=i32),
+                shared_blocks=torch.zeros(2, dtype=i32))
+    h = bl.KVSharedAttention(**args)
+    assert (h.desc.n_groups, h.desc.max_shared, h.desc.shared_stride) == (2, 3, 3)
+    for more in (dict(group=n[:2]), dict(group=n.long()), dict(shared_blocks=n), dict(shared_table=n), dict(workspace=torch.zeros(8, dtype=torch.uint8))):
+        with pytest.raises((TypeError, ValueError)):
+            bl.KVSharedAttention(**dict(args, **more))
+    a = dict(cache=c, qkv=torch.zeros(3, 6 * 64), n_q=2, slots=n)
+    assert bl.KVNormAppend(**a, q_gain=torch.zeros(64)).desc.k_gain is None
+    for more in (dict(q_gain=torch.zeros(32)), dict(k_gain=torch.zeros(64).double())):
+        with pytest.raises((TypeError, ValueError)):
+            bl.KVNormAppend(**a, **more)
+    t = bl.KVTables(n, n, table, torch.zeros(9, dtype=i32), torch.zeros(1, dtype=i32), 16, 5, held=n, max_new=3)
+    assert t.desc.max_new == 3 and t._where == "bl_kv_tables_held"
+    for more in (dict(held=n[:2]), dict(held=n, max_new=0)):
+        with pytest.raises((TypeError, ValueError)):
+            bl.KVTables(n, n, table, torch.zeros(9, dtype=i32), torch.zeros(1, dtype=i32), 16, 5, **more)
