@@ -57,8 +57,8 @@ struct at_args {
     const int* shared_blocks;
     const int* shared_table;
     int64_t shared_stride;
-    int2* pieces;                  /* [T] of each row: partial results of its group's prefix, and of its own tokens (-1: no numbers) */
-    int n_groups, max_shared, group_splits, few_splits;
+    int2* pieces;                  /* [T] of each row: partial results of its group's prefix, and of its own tokens (none of both: it is done; -1: no numbers) */
+    int n_groups, max_shared, group_splits, few_splits, many_splits;
 };
 
 /* ---- what both kernels share --------------------------------------------------------------------------------------- */
@@ -71,6 +71,8 @@ struct at_request {
     int row0, n, len;
     int skip = 0;                  /* tokens in front that its group has */
 };
+/* Rows of a request and kv head from which it is no part of its group: they fill tiles of at_many by themselves, which read the prefix from the caches then. */
+#define AT_APART AT_MANY
 __device__ __forceinline__ at_request at_read(const at_args& A, int b) {
     at_request r;
     const int a = A.q_start[b], e = A.q_start[b + 1];
@@ -87,6 +89,7 @@ __device__ __forceinline__ int at_shared_tokens(const at_args& A, int g) {
     const int s = A.shared_blocks[g];
     return (s < 0 ? 0 : s > A.max_shared ? A.max_shared : s) << A.shift;
 }
+__device__ __forceinline__ bool at_grouped(const at_args& A, int n) { return n * A.G < AT_APART; }
 template <bool SHARED>
 __device__ __forceinline__ at_request at_read_own(const at_args& A, int b) {
     at_request r = at_read(A, b);
@@ -343,6 +346,7 @@ __device__ __forceinline__ void at_few(const at_args& A, int group, uint8_t* lds
         return before + cur.h * cur.c;
     };
     int piece = 0;
+    bool whole_item = !SHARED;
     if constexpr (ITEM) {
         if (SHARED) piece = group % A.few_splits, group /= A.few_splits;
         cur.b = group / A.n_kv, cur.h = group % A.n_kv;
@@ -360,9 +364,10 @@ __device__ __forceinline__ void at_few(const at_args& A, int group, uint8_t* lds
         }
         cur.tile0 = at_from(A, mine, 0) / AT_TILE;
         if (SHARED) {
-            const int each = at_piece(cur.c, A.few_splits), all = cur.c;
+            const int each = at_piece(cur.c, A.few_splits), all = cur.c, n = at_piece_count(all, A.few_splits);
+            whole_item = mine.skip == 0 && n == 1;
             if (piece == 0 && cur.h == 0 && tid < mine.n)
-                A.pieces[mine.row0 + tid] = make_int2(at_piece_count((mine.skip + AT_TILE - 1) / AT_TILE, A.group_splits), at_piece_count(all, A.few_splits));
+                A.pieces[mine.row0 + tid] = whole_item ? make_int2(0, 0) : make_int2(at_piece_count((mine.skip + AT_TILE - 1) / AT_TILE, A.group_splits), n);
             cur.tile0 += piece * each;
             cur.c = all - piece * each < each ? all - piece * each : each;
             if (cur.c <= 0) return;
@@ -671,13 +676,13 @@ __device__ __forceinline__ void at_few(const at_args& A, int group, uint8_t* lds
 #pragma unroll
         for (int j = 0; j < PER; ++j) y[j] += meet.o[w][r][d0 + j] * f;
     }
-    if (SHARED) {
+    if (SHARED && !whole_item) {
         const int64_t at = at_part_at(A, A.group_splits + piece, R.row0 + r / A.G, cur.h * A.G + r % A.G);
         float* to = A.many_part + at * D + d0;
 #pragma unroll
         for (int j = 0; j < PER; j += 4) *bl_g((bl_v4f*)(to + j)) = (bl_v4f){y[j], y[j + 1], y[j + 2], y[j + 3]};
         if (d0 == 0) *bl_g((bl_v2f*)(A.many_part + (int64_t)A.splits * A.T * A.n_q * D + 2 * at)) = (bl_v2f){top, sum};
-    } else if (ITEM || alone) {
+    } else if (ITEM || alone) {                              /* (SHARED: nobody else has a part of it) */
         const float inv = sum == 0.0f ? 0.0f : bl_div_rn(1.0f, sum);
         uint32_t* to = (uint32_t*)(A.out + (R.row0 + r / A.G) * A.out_stride + (cur.h * A.G + r % A.G) * D + d0);
 #pragma unroll
@@ -854,13 +859,14 @@ struct at_many_lds {
     int scan[AT_WAVES];
     int2 query[AT_MANY];                                    /* AT_PREFIX: row and position of the tile's queries */
     int2 ends[AT_WAVES];
+    int found[5];                                           /* the group of the tile, tiles in front of it and of it, its tokens and rows */
 };
 /* What a workgroup of at_many has: rows of a request over all that they see; over what stands behind their group's prefix (AT_OWN); or rows of all
  * requests of a group over its prefix (AT_PREFIX), which are gathered: their places in the batch are found by each workgroup, by sums over the requests. */
 enum { AT_ALL, AT_OWN, AT_PREFIX };
 template <int KIND, int D, int MODE = AT_ALL>
 __device__ __forceinline__ void at_many(const at_args& A, int place, at_many_lds<KIND, D>& lds) {
-    const int splits = MODE == AT_PREFIX ? A.group_splits : MODE == AT_OWN ? A.splits - A.group_splits : A.splits;
+    const int splits = MODE == AT_PREFIX ? A.group_splits : MODE == AT_OWN ? A.many_splits : A.splits;
     constexpr bool HALF = at_many_k<KIND, D>::bytes == 2;
     constexpr int KROW = D * at_many_k<KIND, D>::bytes;        /* bytes of a K row in LDS, 16-byte units XOR-ed by k_mix(row) */
     constexpr int KS = D / 32, DT = D / 32;
@@ -870,7 +876,7 @@ __device__ __forceinline__ void at_many(const at_args& A, int place, at_many_lds
     const int tid = threadIdx.x, lane = tid & 63, wave = at_uniform(tid >> 6);
     const int col = lane & 31, half = lane >> 5;
     /* whose tile: place = (row tile * n_kv + head) * splits + piece, a request's heavy tiles first */
-    int piece, h, want, b, before, c;
+    int piece, h, want, b, before, c, rt;
     auto take = [&](int all) {
         /* Heads of 128: of the 512 workgroups that the chip holds the second 256 go the other way round, so that a unit has a heavy
          * one and a light one: two prompts of 1600 tokens 72 -> 57 us, one of 6000 244 -> 236 (heads of 64, three to a unit: 52 -> 58). */
@@ -879,28 +885,89 @@ __device__ __forceinline__ void at_many(const at_args& A, int place, at_many_lds
         piece = place % splits, h = place / splits % A.n_kv, want = place / splits / A.n_kv;
         return place < n;
     };
+    at_request R = {};
+    int group_rows = 0;
     if constexpr (MODE == AT_PREFIX) {
-        /* tiles of every group, then the group that has this one */
         int* s_upto = lds.upto;
-        for (int g = tid; g < A.n_groups; g += AT_THREADS) s_upto[g] = 0;
-        __syncthreads();
-        for (int i = tid; i < A.B; i += AT_THREADS) {
-            const int g = A.group[i], n = at_read(A, i).n;
-            if ((unsigned)g < (unsigned)A.n_groups && n) atomicAdd(&s_upto[g], n);
+        /* Which group has this tile, and the batch rows of the tile's queries: sums over the groups, then over the requests.  A thread has one of each where there
+         * are no more than threads, so that all of it hangs on one round of loads. */
+        auto queries = [&](int q0, int q1, int begin, int end, int row0, int len) {
+            for (int j = begin > q0 ? begin : q0; j < (end < q1 ? end : q1); ++j) lds.query[j - q0] = make_int2(row0 + j - begin, len - (end - begin) + j - begin);
+        };
+        auto range = [&](int& q0, int& q1) {
+            rt = c - 1 - (want - before);
+            q0 = rt * AT_MANY / A.G, q1 = (rt * AT_MANY + AT_MANY - 1) / A.G + 1;
+        };
+        if (A.B <= AT_THREADS && A.n_groups <= AT_THREADS) {
+            int group = -1, tokens = 0;
+            at_request r = {};
+            if (tid < A.B) group = A.group[tid], r = at_read(A, tid);
+            if (tid < A.n_groups) tokens = at_shared_tokens(A, tid);
+            if ((unsigned)group >= (unsigned)A.n_groups || !at_grouped(A, r.n)) r.n = 0;
+            s_upto[tid] = 0;
+            __syncthreads();
+            if (r.n) atomicAdd(&s_upto[group], r.n);
+            __syncthreads();
+            const int rows = s_upto[tid] * A.G, tiles = tokens ? (rows + AT_MANY - 1) / AT_MANY : 0;
+            auto sums = [&](int v, int* total) {             /* over the threads up to this one */
+                const int x = at_scan(v);
+                if (lane == 63) lds.scan[wave] = x;
+                __syncthreads();
+                int add = 0, all = 0;
+#pragma unroll
+                for (int w = 0; w < AT_WAVES; ++w) add += w < wave ? lds.scan[w] : 0, all += lds.scan[w];
+                *total = all;
+                return x + add;
+            };
+            int all;
+            const int upto = sums(tiles, &all);
+            if (!take(at_uniform(all))) return;
+            if (tiles && upto > want && upto - tiles <= want) lds.found[0] = tid, lds.found[1] = upto - tiles, lds.found[2] = tiles, lds.found[3] = tokens, lds.found[4] = rows;
+            __syncthreads();
+            b = at_uniform(lds.found[0]), before = at_uniform(lds.found[1]), c = at_uniform(lds.found[2]);
+            R.len = at_uniform(lds.found[3]), group_rows = at_uniform(lds.found[4]);
+            int q0, q1;
+            range(q0, q1);
+            const int n = group == b ? r.n : 0, end = sums(n, &all);
+            if (n) queries(q0, q1, end - n, end, r.row0, r.len);
+            __syncthreads();
+        } else {
+            auto news = [&](int i) {
+                const int n = at_read(A, i).n;
+                return at_grouped(A, n) ? n : 0;
+            };
+            for (int g = tid; g < A.n_groups; g += AT_THREADS) s_upto[g] = 0;
+            __syncthreads();
+            for (int i = tid; i < A.B; i += AT_THREADS) {
+                const int g = A.group[i], n = news(i);
+                if ((unsigned)g < (unsigned)A.n_groups && n) atomicAdd(&s_upto[g], n);
+            }
+            __syncthreads();
+            at_sums(A.n_groups, [&](int g) { return at_shared_tokens(A, g) ? (int)(((int64_t)s_upto[g] * A.G + AT_MANY - 1) / AT_MANY) : 0; }, s_upto, lds.scan);
+            if (!take(at_uniform(s_upto[A.n_groups - 1]))) return;
+            int lo = -1, hi = A.n_groups - 1;
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) >> 1;
+                if (s_upto[mid] > want) hi = mid;
+                else lo = mid;
+            }
+            b = at_uniform(hi);
+            before = b ? at_uniform(s_upto[b - 1]) : 0;
+            c = at_uniform(s_upto[b]) - before;
+            R.len = at_shared_tokens(A, b);
+            __syncthreads();
+            at_sums(A.B, [&](int i) { return A.group[i] == b ? news(i) : 0; }, s_upto, lds.scan);
+            group_rows = at_uniform(s_upto[A.B - 1]) * A.G;
+            int q0, q1;
+            range(q0, q1);
+            for (int i = tid; i < A.B; i += AT_THREADS) {
+                const int end = s_upto[i], begin = i ? s_upto[i - 1] : 0;
+                if (end <= q0 || begin >= q1 || end == begin) continue;
+                const at_request r = at_read(A, i);
+                queries(q0, q1, begin, end, r.row0, r.len);
+            }
+            __syncthreads();
         }
-        __syncthreads();
-        at_sums(A.n_groups, [&](int g) { return at_shared_tokens(A, g) ? (int)(((int64_t)s_upto[g] * A.G + AT_MANY - 1) / AT_MANY) : 0; }, s_upto, lds.scan);
-        if (!take(at_uniform(s_upto[A.n_groups - 1]))) return;
-        int lo = -1, hi = A.n_groups - 1;
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) >> 1;
-            if (s_upto[mid] > want) hi = mid;
-            else lo = mid;
-        }
-        b = at_uniform(hi);
-        before = b ? at_uniform(s_upto[b - 1]) : 0;
-        c = at_uniform(s_upto[b]) - before;
-        __syncthreads();
     } else if (A.B <= 64) {
         const int upto = at_scan(lane < A.B ? at_many_tiles(A, lane) : 0);
         if (!take(__builtin_amdgcn_readlane(upto, 63))) return;
@@ -922,26 +989,19 @@ __device__ __forceinline__ void at_many(const at_args& A, int place, at_many_lds
         c = at_uniform(s_upto[b]) - before;
         __syncthreads();
     }
-    const int rt = c - 1 - (want - before);                  /* the last rows see most: first */
-    at_request R;
-    if constexpr (MODE == AT_PREFIX) R = {0, 0, at_shared_tokens(A, b)};
-    else R = at_read_own<MODE == AT_OWN>(A, b);
     const int bs1 = (1 << A.shift) - 1;
-    int rows = R.n * A.G;
+    int rows, front = 0;                                     /* front: tokens of AT_OWN that its group's table has */
+    const int* front_pages = nullptr;
     if constexpr (MODE == AT_PREFIX) {
-        /* the group's queries, request by request: those of this tile */
-        auto news = [&](int i) { return A.group[i] == b ? at_read(A, i).n : 0; };
-        at_sums(A.B, news, lds.upto, lds.scan);
-        const int queries = at_uniform(lds.upto[A.B - 1]);
-        rows = queries * A.G;
-        const int q0 = rt * AT_MANY / A.G, q1 = (rt * AT_MANY + AT_MANY - 1) / A.G + 1;
-        for (int i = tid; i < A.B; i += AT_THREADS) {
-            const int end = lds.upto[i], begin = i ? lds.upto[i - 1] : 0;
-            if (end <= q0 || begin >= q1 || end == begin) continue;
-            const at_request r = at_read(A, i);
-            for (int j = begin > q0 ? begin : q0; j < (end < q1 ? end : q1); ++j) lds.query[j - q0] = make_int2(r.row0 + j - begin, r.len - r.n + j - begin);
+        rows = group_rows;
+    } else {
+        rt = c - 1 - (want - before);                        /* the last rows see most: first */
+        R = at_read_own<MODE == AT_OWN>(A, b);
+        rows = R.n * A.G;
+        if (MODE == AT_OWN && R.skip && !at_grouped(A, R.n)) {
+            front = R.skip, R.skip = 0;
+            front_pages = A.shared_table + (int64_t)A.group[b] * A.shared_stride;
         }
-        __syncthreads();
     }
     const int rbase = rt * AT_MANY, rend = rbase + AT_MANY < rows ? rbase + AT_MANY : rows;
     /* this lane's row: its place in the batch, its head, and the tokens that it sees */
@@ -1051,7 +1111,8 @@ __device__ __forceinline__ void at_many(const at_args& A, int place, at_many_lds
     const int k_off = kt * D + kc * 16, v_off = lane << A.shift;          /* V: features lane and lane + 64 */
     auto fetch_blocks = [&](int t) -> int {
         const int token = t * AT_TILE + 16 * (lane & 3);
-        return t < tend && token < R.len && token + 16 > tok0 ? pages[token >> A.shift] : -1;       /* (in front of all windows: as in at_few) */
+        const int* from = MODE == AT_OWN && token < front ? front_pages : pages;
+        return t < tend && token < R.len && token + 16 > tok0 ? from[token >> A.shift] : -1;       /* (in front of all windows: as in at_few) */
     };
     auto there = [&](int block) { return (unsigned)block < (unsigned)A.n_blocks; };
     bl_v4i lk[U], lv_[U];
@@ -1277,9 +1338,10 @@ __device__ __forceinline__ void at_many(const at_args& A, int place, at_many_lds
     bl_mfma_fence();
     l += at_xor(l, 32);
     if (!live) return;
+    const bool whole_rows = MODE == AT_ALL ? A.splits == 1 : MODE == AT_OWN && R.skip == 0 && splits == 1;
     if (MODE == AT_OWN && h == 0 && piece == 0 && half == 0 && row % A.G == 0)
-        A.pieces[at_row] = make_int2(at_piece_count((R.skip + AT_TILE - 1) / AT_TILE, A.group_splits), splits);
-    if (MODE == AT_ALL && A.splits == 1) {
+        A.pieces[at_row] = whole_rows ? make_int2(0, 0) : make_int2(at_piece_count((R.skip + AT_TILE - 1) / AT_TILE, A.group_splits), splits);
+    if (whole_rows) {
         const float inv = l == 0.0f ? 0.0f : bl_div_rn(1.0f, l);
         uint16_t* to = A.out + at_row * A.out_stride + qh_i * D;
 #pragma unroll
@@ -1346,25 +1408,30 @@ __device__ __forceinline__ void at_many_join(const at_args& A, int group) {
     *bl_g((bl_v2u*)(A.out + row * A.out_stride + (at % A.n_q) * D + d0)) = u;
 }
 
-/* The same for rows of requests that share prefixes: pieces 0 .. of the prefix and group_splits .. of the rest, as many as the row's entry says. */
-template <int D>
+/* The same for rows of requests that share prefixes: pieces 0 .. of the prefix and group_splits .. of the rest, as many as the row's entry says.  LANES groups of
+ * D / 4 threads share a row's pieces and meet in LDS. */
+template <int D, int LANES>
 __global__ __launch_bounds__(AT_THREADS) void bl_attn_shared_join(at_args A) {
-    constexpr int TPR = D / 4, IN = 4;
-    const int64_t at = (int64_t)blockIdx.x * (AT_THREADS / TPR) + threadIdx.x / TPR, all = (int64_t)A.T * A.n_q;
-    if (at >= all) return;
+    constexpr int TPR = D / 4, IN = 4, GROUPS = AT_THREADS / TPR, ROWS = GROUPS / LANES;
+    __shared__ float s_m[GROUPS], s_l[GROUPS];
+    __shared__ __attribute__((aligned(16))) float s_y[GROUPS][D];
+    const int group = threadIdx.x / TPR, part = group / ROWS;               /* (a wave's groups have other rows: their loads are of neighbours) */
+    const int64_t at = (int64_t)blockIdx.x * ROWS + group % ROWS, all = (int64_t)A.T * A.n_q;
     const int row = (int)(at / A.n_q), d0 = (threadIdx.x % TPR) * 4;
-    if (row < A.q_start[0] || row >= A.q_start[A.B]) return;
-    const int2 n = A.pieces[row];
+    int2 n = {0, 0};
+    if (at < all && row >= A.q_start[0] && row < A.q_start[A.B]) n = A.pieces[row];
+    n.x = min(n.x, A.group_splits), n.y = min(n.y, A.splits - A.group_splits);       /* (first rows that do not ascend lead to no place outside) */
     const float* ml = A.many_part + A.splits * all * D;
-    const int count = n.x + n.y;
+    const int count = max(n.x, 0) + max(n.y, 0);
     at_sum s = {-INFINITY, 0.0f, {0, 0, 0, 0}};
-    for (int i = 0; i < count; i += IN) {
+    for (int i = part; i < count; i += IN * LANES) {
         at_sum x[IN];
 #pragma unroll
         for (int u = 0; u < IN; ++u) {
             x[u] = {-INFINITY, 0.0f, {0, 0, 0, 0}};
-            if (i + u < count) {
-                const int64_t from = (i + u < n.x ? i + u : A.group_splits + i + u - n.x) * all + at;
+            const int p = i + u * LANES;
+            if (p < count) {
+                const int64_t from = (p < n.x ? p : A.group_splits + p - n.x) * all + at;
                 const bl_v2f t = *bl_gc<bl_v2f>(ml + 2 * from);
                 x[u].m = t[0], x[u].l = t[1], x[u].y = *bl_gc<bl_v4f>(A.many_part + from * D + d0);
             }
@@ -1372,6 +1439,15 @@ __global__ __launch_bounds__(AT_THREADS) void bl_attn_shared_join(at_args A) {
 #pragma unroll
         for (int u = 0; u < IN; ++u) s = at_add(s, x[u]);
     }
+    if (LANES > 1) {
+        if (d0 == 0) s_m[group] = s.m, s_l[group] = s.l;
+        *(bl_v4f*)&s_y[group][d0] = s.y;
+        __syncthreads();
+        if (part) return;
+#pragma unroll
+        for (int j = 1; j < LANES; ++j) s = at_add(s, {s_m[j * ROWS + group], s_l[j * ROWS + group], *(const bl_v4f*)&s_y[j * ROWS + group][d0]});
+    }
+    if (n.x == 0 && n.y == 0) return;                        /* of no request, or done */
     const float inv = s.l == 0.0f ? 0.0f : bl_div_rn(1.0f, s.l);
     bl_v2u u = {bl_pack2_bf16(s.y[0] * inv, s.y[1] * inv), bl_pack2_bf16(s.y[2] * inv, s.y[3] * inv)};
     if (n.y < 0) u = (bl_v2u){0x7fc07fc0u, 0x7fc07fc0u};      /* more queries than the launch was made for */
@@ -1404,7 +1480,7 @@ __global__ __launch_bounds__(AT_THREADS, 2) void bl_attn_any(at_args A, int many
     if ((int)blockIdx.x < many) at_many<KIND, D>(A, (int)blockIdx.x, ((lds_t*)lds)->many);
     else at_few<KIND, D, WIDE, ITEM, false>(A, (int)blockIdx.x - many, lds);
 }
-/* Requests that share prefixes: workgroups of the prefixes, of many rows behind them, and of few. */
+/* Requests that share prefixes: workgroups of many rows of a request, of the prefixes, and of few rows behind them. */
 template <int KIND, int D, bool WIDE, bool MANY>
 __global__ __launch_bounds__(AT_THREADS, 2) void bl_attn_shared(at_args A, int prefix, int many) {
     union lds_t {
@@ -1413,8 +1489,8 @@ __global__ __launch_bounds__(AT_THREADS, 2) void bl_attn_shared(at_args A, int p
     };
     __shared__ __attribute__((aligned(16))) uint8_t lds[sizeof(lds_t)];
     const int x = (int)blockIdx.x;
-    if (x < prefix) at_many<KIND, D, AT_PREFIX>(A, x, ((lds_t*)lds)->many);
-    else if (MANY && x < prefix + many) at_many<KIND, D, AT_OWN>(A, x - prefix, ((lds_t*)lds)->many);
+    if (MANY && x < many) at_many<KIND, D, AT_OWN>(A, x, ((lds_t*)lds)->many);
+    else if (x < prefix + many) at_many<KIND, D, AT_PREFIX>(A, x - many, ((lds_t*)lds)->many);
     else at_few<KIND, D, WIDE, AT_WAVES, !MANY, true>(A, x - prefix - many, lds);
 }
 /* Partial results of both: `few` workgroups for those of at_few, turns x AT_STREAM_GROUPS, the others for a split. */
@@ -1586,17 +1662,19 @@ static at_shared_plan at_make_shared_plan(const bl_attn_shared_desc* s) {
     int64_t own = s->max_own > 0 ? s->max_own : a->max_len > 0 ? a->max_len : (int64_t)a->max_blocks * a->cache.block;
     const int64_t wide = (int64_t)a->window + (a->max_q < AT_MANY ? a->max_q : AT_MANY);
     if (a->window && own > wide) own = wide;
-    auto pieces = [](int64_t items, int64_t tokens, int64_t each, int64_t most) -> int {
-        int64_t n = items < 512 ? 512 / items : 1;
-        n = n < tokens / each ? n : tokens / each;
+    /* Pieces of `items` items of `tokens`: until there are `fill` workgroups, of four tiles at least; fewer tiles while not every unit has a workgroup. */
+    auto pieces = [](int64_t items, int64_t tokens, int64_t fill, int64_t each, int64_t most) -> int {
+        const int64_t full = fill / items < tokens / (4 * AT_TILE) ? fill / items : tokens / (4 * AT_TILE), tiles = (tokens + each * AT_TILE - 1) / (each * AT_TILE);
+        const int64_t some = 128 / items < tiles ? 128 / items : tiles, n = full > some ? full : some;
         return (int)(n < 1 ? 1 : n < most ? n : most);
     };
-    p.group_splits = pieces(tiles * a->cache.n_kv, (int64_t)s->max_shared * a->cache.block, 4 * AT_TILE, 64);
-    p.few_splits = p.few ? pieces(part * a->cache.n_kv, own, 4 * AT_TILE, 32) : 0;
-    p.many_splits = p.many ? pieces(tiles * a->cache.n_kv, own, 4 * AT_TILE, 32) : 0;
+    const int64_t most = a->T * G < part * (AT_APART - 1) ? a->T * G : part * (AT_APART - 1);          /* rows that groups can have */
+    p.prefix_tiles = most / AT_MANY + groups;
+    p.group_splits = pieces((most + AT_MANY - 1) / AT_MANY * a->cache.n_kv, (int64_t)s->max_shared * a->cache.block, 512, 1, 64);
+    p.few_splits = p.few ? pieces(part * a->cache.n_kv, own, 512, 4, 32) : 0;
+    p.many_splits = p.many ? pieces(tiles * a->cache.n_kv, own, 512, 4, 32) : 0;
     p.splits = p.group_splits + (p.few_splits > p.many_splits ? p.few_splits : p.many_splits);
-    if (p.many) p.many_splits = p.splits - p.group_splits;
-    p.prefix_tiles = a->T * G / AT_MANY + groups, p.many_tiles = p.many ? a->T * G / AT_MANY + part : 0;
+    p.many_tiles = p.many ? a->T * G / AT_MANY + part : 0;
     p.pieces = ((size_t)a->T * sizeof(int2) + 255) / 256 * 256;
     p.bytes = p.pieces + (size_t)p.splits * a->T * a->n_q * (D + 2) * sizeof(float);
     return p;
@@ -1613,7 +1691,8 @@ static void at_shared_launch(const at_args& A, const at_shared_plan& p, hipStrea
     if (p.many) bl_attn_shared<KIND, D, WIDE, true><<<(unsigned)(prefix + many + few), AT_THREADS, 0, st>>>(A, prefix, many);
     else bl_attn_shared<KIND, D, WIDE, false><<<(unsigned)(prefix + few), AT_THREADS, 0, st>>>(A, prefix, 0);
     const int64_t rows = (int64_t)A.T * A.n_q, per = AT_THREADS / (D / 4);
-    bl_attn_shared_join<D><<<(unsigned)((rows + per - 1) / per), AT_THREADS, 0, st>>>(A);
+    if (p.splits <= 4) bl_attn_shared_join<D, 1><<<(unsigned)((rows + per - 1) / per), AT_THREADS, 0, st>>>(A);
+    else bl_attn_shared_join<D, 4><<<(unsigned)((rows * 4 + per - 1) / per), AT_THREADS, 0, st>>>(A);
 }
 
 extern "C" bl_status bl_attn_kv8_shared(const bl_attn_shared_desc* s, bl_stream stream) {
@@ -1625,7 +1704,7 @@ extern "C" bl_status bl_attn_kv8_shared(const bl_attn_shared_desc* s, bl_stream 
     const bl_kv_cache& c = a->cache;
     if (c.n_kv * (p.prefix_tiles * p.group_splits + p.many_tiles * p.many_splits + a->B * p.few_splits) > 0x7fff0000) return BL_ERR_SHAPE;
     at_args A = at_make_args(a);
-    A.few_rows = p.few ? AT_FEW : 0, A.splits = p.splits, A.group_splits = p.group_splits, A.few_splits = p.few_splits;
+    A.few_rows = p.few ? AT_FEW : 0, A.splits = p.splits, A.group_splits = p.group_splits, A.few_splits = p.few_splits, A.many_splits = p.many_splits;
     A.group = s->group, A.shared_blocks = s->shared_blocks, A.shared_table = s->shared_table, A.shared_stride = s->shared_stride;
     A.n_groups = (int)s->n_groups, A.max_shared = s->max_shared;
     A.pieces = (int2*)a->workspace, A.many_part = (float*)((char*)a->workspace + p.pieces);
