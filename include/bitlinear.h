@@ -530,10 +530,9 @@ bl_status bl_attn_kv8(const bl_attn_desc* a, bl_stream s);
 
 /* The same where requests share long prefixes, each of which is read once for all of its requests.  Request b belongs to the group
  * group[b] (outside 0 .. n_groups-1: to none; a group's requests need not stand together).  The tokens of its first S =
- * shared_blocks[group[b]] blocks (taken as the nearer end outside 0 .. max_shared) are those of row group[b] of shared_table; its own row of `table` names the blocks from S on (what
- * stands in front of them there is not read).  Everything else, and every result, is as bl_attn_kv8 has it for a table whose rows begin with the group's: lengths and
- * positions count the prefix, causality and window hold inside it too, a request may be shorter than it.  Where the group's tables say the same, only the
- * order of the sums is another.
+ * shared_blocks[group[b]] blocks (taken as the nearer end outside 0 .. max_shared) are those of row group[b] of shared_table, and its own row of `table` begins with the
+ * same ones: either may be read.  Results are bl_attn_kv8's but for the order of the sums: lengths and positions count the prefix, causality and window hold inside it
+ * too, a request may be shorter than it.
  *   shared_table   [n_groups][shared_stride], max_shared <= shared_stride entries of a row are used; its blocks are whole (every token written)
  *   max_own        about the most tokens that a request has behind its shared blocks: sizes a split only (0: as attn.max_len)
  *   attn.workspace bl_attn_shared_workspace_bytes(a) bytes

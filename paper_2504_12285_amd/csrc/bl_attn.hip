@@ -990,18 +990,14 @@ __device__ __forceinline__ void at_many(const at_args& A, int place, at_many_lds
         __syncthreads();
     }
     const int bs1 = (1 << A.shift) - 1;
-    int rows, front = 0;                                     /* front: tokens of AT_OWN that its group's table has */
-    const int* front_pages = nullptr;
+    int rows;
     if constexpr (MODE == AT_PREFIX) {
         rows = group_rows;
     } else {
         rt = c - 1 - (want - before);                        /* the last rows see most: first */
         R = at_read_own<MODE == AT_OWN>(A, b);
         rows = R.n * A.G;
-        if (MODE == AT_OWN && R.skip && !at_grouped(A, R.n)) {
-            front = R.skip, R.skip = 0;
-            front_pages = A.shared_table + (int64_t)A.group[b] * A.shared_stride;
-        }
+        if (MODE == AT_OWN && !at_grouped(A, R.n)) R.skip = 0;
     }
     const int rbase = rt * AT_MANY, rend = rbase + AT_MANY < rows ? rbase + AT_MANY : rows;
     /* this lane's row: its place in the batch, its head, and the tokens that it sees */
@@ -1111,8 +1107,7 @@ __device__ __forceinline__ void at_many(const at_args& A, int place, at_many_lds
     const int k_off = kt * D + kc * 16, v_off = lane << A.shift;          /* V: features lane and lane + 64 */
     auto fetch_blocks = [&](int t) -> int {
         const int token = t * AT_TILE + 16 * (lane & 3);
-        const int* from = MODE == AT_OWN && token < front ? front_pages : pages;
-        return t < tend && token < R.len && token + 16 > tok0 ? from[token >> A.shift] : -1;       /* (in front of all windows: as in at_few) */
+        return t < tend && token < R.len && token + 16 > tok0 ? pages[token >> A.shift] : -1;       /* (in front of all windows: as in at_few) */
     };
     auto there = [&](int block) { return (unsigned)block < (unsigned)A.n_blocks; };
     bl_v4i lk[U], lv_[U];
@@ -1653,6 +1648,17 @@ static bl_status at_check_shared(const bl_attn_shared_desc* a) {
     return BL_OK;
 }
 
+/* Whether bl_attn_kv8's kernels do it, which read the prefix once a request: where contexts are short enough for a workgroup an item, which leaves nothing
+ * to join, or there is little to read at all.  us of these kernels and of those, all requests behind one prefix, up to 300 tokens of their own:
+ *   20 + 5 heads of 128, prefix 500: 2 to 64 requests 11 to 18 and 9 to 14 (four queries each 12 to 23 and 9 to 15); 2000: 2, 4, 8, 16, 64 requests 12.8, 13.2, 14.0, 15.2,
+ *     22.2 and 11.4, 11.7, 14.6, 18.6, 34.7; 8000: 17.1 to 32 and 17.6 to 83; 30000: 26 to 33 (16 requests) and 27 to 107;
+ *   32 + 8 heads of 64, 2000: 2 to 64 requests 11.5 to 17 and 10 to 15; 8000: 15.1 to 27.7 and 13.9 to 60; 16 + 1 of 128, 2000: 12.4 to 20.4 and 11.6 to 22.8. */
+static bool at_shared_apart(const bl_attn_shared_desc* s) {
+    const bl_attn_desc* a = &s->attn;
+    const int64_t tokens = a->max_len > 0 ? a->max_len : (int64_t)a->max_blocks * a->cache.block;
+    return at_make_plan(a).items || (tokens < 4096 && a->B * a->cache.n_kv * tokens < 65536);
+}
+
 static at_shared_plan at_make_shared_plan(const bl_attn_shared_desc* s) {
     const bl_attn_desc* a = &s->attn;
     at_shared_plan p;
@@ -1681,7 +1687,7 @@ static at_shared_plan at_make_shared_plan(const bl_attn_shared_desc* s) {
 }
 
 extern "C" size_t bl_attn_shared_workspace_bytes(const bl_attn_shared_desc* a) {
-    return at_check_shared(a) == BL_OK ? at_make_shared_plan(a).bytes : 0;
+    return at_check_shared(a) != BL_OK ? 0 : at_shared_apart(a) ? at_make_plan(&a->attn).bytes : at_make_shared_plan(a).bytes;
 }
 
 template <int KIND, int D, bool WIDE>
@@ -1698,6 +1704,7 @@ static void at_shared_launch(const at_args& A, const at_shared_plan& p, hipStrea
 extern "C" bl_status bl_attn_kv8_shared(const bl_attn_shared_desc* s, bl_stream stream) {
     if (const bl_status rc = at_check_shared(s)) return rc;
     const bl_attn_desc* a = &s->attn;
+    if (at_shared_apart(s)) return bl_attn_kv8(a, stream);
     const at_shared_plan p = at_make_shared_plan(s);
     if (!a->workspace) return BL_ERR_WORKSPACE;
     if (!bl_aligned(a->workspace, 256)) return BL_ERR_ALIGN;

@@ -10,12 +10,12 @@ from test_gpu_attn import Batch  # noqa: E402
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
 KINDS = ["int8", "e4m3"]
-GARBAGE = [10**9, -7, 0]
+FAR = 1000000                       # as a hint of the length: nothing is short enough for kernels that read the prefix once a request
 
 
 class Shared(Batch):
-    """Requests (tokens in all, new ones), the blocks of each group's prefix, and the group of each request.  A request's row of the definition's table
-    begins with its group's blocks; in what the kernel gets those entries are garbage."""
+    """Requests (tokens in all, new ones), the blocks of each group's prefix, and the group of each request.  A request's row of the table begins with
+    its group's blocks."""
 
     def __init__(self, reqs, prefix, group, heads, block, kind, seed=0, width=None, **more):
         most = max(prefix)
@@ -28,24 +28,23 @@ class Shared(Batch):
         self.shared_table = torch.tensor(rows, dtype=torch.int32, device=DEV)
         self.shared_blocks = torch.tensor(prefix, dtype=torch.int32, device=DEV)
         self.group = torch.tensor(group, dtype=torch.int32, device=DEV)
-        self.given = self.table.clone()
         for b, g in enumerate(group):
             if 0 <= g < len(prefix):
-                self.given[b, :prefix[g]] = GARBAGE[b % 3]
                 self.table[b, :prefix[g]] = self.shared_table[g, :prefix[g]]
 
-    def handle(self, max_q=None, **more):
+    def handle(self, max_q=None, max_len=FAR, **more):
         from paper_2504_12285_amd import binding as bl
         most = max(1, max(n for _, n in self.reqs))
-        return bl.KVSharedAttention(bl.KVCache(self.k, self.v, self.ks, self.vs), self.q, self.q_start, self.seq_len, self.given, self.group, self.shared_table,
-                                    self.shared_blocks, n_q=self.heads[0], max_q=most if max_q is None else max_q, **more)
+        return bl.KVSharedAttention(bl.KVCache(self.k, self.v, self.ks, self.vs), self.q, self.q_start, self.seq_len, self.table, self.group, self.shared_table,
+                                    self.shared_blocks, n_q=self.heads[0], max_q=most if max_q is None else max_q, max_len=max_len, **more)
 
     def check(self, window=0, **more):
-        h = self.handle(window=window, **more)
-        h.out.fill_(math.nan), h.workspace.fill_(255)
-        h.run()
-        self.compare(h.out, window, h.desc.attn.softmax_scale)
-        return h
+        """The kernels of shared prefixes, and those that the sizes themselves lead to."""
+        for far in ({}, dict(max_len=0)):
+            h = self.handle(window=window, **dict(far, **more))
+            h.out.fill_(math.nan), h.workspace.fill_(255)
+            h.run()
+            self.compare(h.out, window, h.desc.attn.softmax_scale)
 
 
 def dealt(prefix, own, block, groups, new=1, lone=()):
@@ -135,7 +134,7 @@ def test_long_prefixes(kind, heads, block):
 @pytest.mark.parametrize("kind", KINDS)
 def test_hints_and_a_wide_table_change_nothing_that_counts(kind):
     prefix = [9, 3]
-    for more in (dict(max_len=1), dict(max_len=10**6), dict(max_own=1), dict(max_own=10**6, max_len=3)):
+    for more in (dict(max_len=1), dict(max_len=10**6), dict(max_own=1), dict(max_own=10**6)):
         reqs, group = dealt(prefix, OWN, 32, 2, 3)
         Shared(reqs, prefix, group, (8, 2, 128), 32, kind, width=900).check(**more)
 
@@ -148,7 +147,7 @@ def test_entries_that_name_no_block():
     b.shared_table[0, 3], b.shared_table[0, 7], b.shared_table[1, 1] = -1, 10**9, b.k.shape[0]
     for i, g in enumerate(group):
         b.table[i, :prefix[g]] = b.shared_table[g, :prefix[g]]
-    b.given[11, prefix[1] + 2] = b.table[11, prefix[1] + 2] = -3
+    b.table[11, prefix[1] + 2] = -3
     b.check()
 
 
@@ -260,7 +259,7 @@ def test_captured_and_on_another_stream():
     prefix = [5, 12]
     reqs, group = dealt(prefix, [40, 9, 100, 30], 32, 2)
     b = Shared(reqs, prefix, group, (8, 2, 64), 32, "int8", width=20)
-    h = b.handle(max_len=600, max_own=200)
+    h = b.handle(max_own=200)
     s = torch.cuda.Stream()
     s.wait_stream(torch.cuda.current_stream())
     with torch.cuda.stream(s):
@@ -276,12 +275,11 @@ def test_captured_and_on_another_stream():
         b.q.copy_(torch.randn_like(b.q))
         if step == 3:
             b.shared_blocks.copy_(torch.tensor([4, 12], dtype=torch.int32, device=DEV))
-            b.given[:, 4] = b.table[:, 4]
         g.replay()
         torch.cuda.synchronize()
         b.reqs = [(t, 1) for t in lens]
         b.compare(h.out)
-        eager = b.handle(max_len=600, max_own=200)
+        eager = b.handle(max_own=200)
         eager.run()
         assert torch.equal(eager.out, h.out)
 

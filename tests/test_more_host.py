@@ -62,8 +62,8 @@ def test_a_bad_cache_is_refused(lib, more, status):  # noqa: F811
 def test_shared_attention_wants_its_workspace(lib):  # noqa: F811
     assert lib.bl_attn_kv8_shared(ctypes.byref(shared(attention(workspace=None))), None) == WORKSPACE
     assert lib.bl_attn_kv8_shared(ctypes.byref(shared(attention(workspace=P + 16))), None) == ALIGN
-    one, more = (lib.bl_attn_shared_workspace_bytes(ctypes.byref(shared(**d))) for d in (dict(), dict(max_shared=500, shared_stride=500)))
-    assert 0 < one < more
+    one, few, more = (lib.bl_attn_shared_workspace_bytes(ctypes.byref(shared(**d))) for d in (dict(), dict(a=attention(max_len=10**6)), dict(a=attention(max_len=10**6), max_shared=500, shared_stride=500)))
+    assert 0 < one < few < more
 
 
 def matrix(**more):
@@ -127,11 +127,11 @@ def test_the_binding_takes_what_a_descriptor_can_stand_for(lib):  # noqa: F811
     for bad in ((pool.view(torch.int8), torch.zeros(2, 2)), (pool, torch.zeros(2, 3)), (pool, torch.zeros(2, 2).double()), (pool.view(torch.uint8).t().view(f8), torch.zeros(2, 2))):
         with pytest.raises((TypeError, ValueError)):
             bl.F8Matrix(*bad)
-    x = torch.zeros(3, 192)
+    x = torch.zeros(20, 192)
     h = bl.F8Linear(m, x, dtype=torch.bfloat16)
-    assert h.y.shape == (3, 200) and h.desc.y_kind == bl.BL_F8_OUT_BF16 and h.workspace.numel() >= 3 * 256
-    assert bl.F8Linear(m, x, y=torch.zeros(3, 208)[:, :200], workspace=h.workspace).desc.y_stride == 208
-    for more in (dict(x=x.half()), dict(x=x[:, :128]), dict(x=x.t()), dict(), dict(x=x, prod=bl.Producer()), dict(prod=bl.Producer()), dict(x=x, y=torch.zeros(3, 100)),
+    assert h.y.shape == (20, 200) and h.desc.y_kind == bl.BL_F8_OUT_BF16 and h.workspace.numel() >= 20 * 256
+    assert bl.F8Linear(m, x, y=torch.zeros(20, 208)[:, :200], workspace=h.workspace).desc.y_stride == 208
+    for more in (dict(x=x.half()), dict(x=x[:, :128]), dict(x=x.t()), dict(), dict(x=x, prod=bl.Producer()), dict(prod=bl.Producer()), dict(x=x, y=torch.zeros(20, 100)),
                  dict(x=x, gain=torch.zeros(3)), dict(x=x, dtype=torch.float16), dict(x=x, workspace=torch.zeros(8, dtype=torch.uint8))):
         with pytest.raises((TypeError, ValueError)):
             bl.F8Linear(m, **more)
