@@ -60,6 +60,9 @@ __device__ __forceinline__ bl_v4f f8_product(const f8_halves& w, const f8_halves
     return p;
 }
 
+/* A number that the whole wave reads, through the scalar cache: its load is none of those that are counted. */
+__device__ __forceinline__ float f8_uniform(const float* p) { return *(const float __attribute__((address_space(4)))*)(uintptr_t)p; }
+
 /* ---- rows to codes ----------------------------------------------------------------------------------------------------- */
 
 /* The scale of a group whose largest |value| is g (a NaN counts as the largest; fmaxf then gives the floor, and the NaN's own code
@@ -128,33 +131,51 @@ __device__ __forceinline__ void f8_store4(const f8_args& A, int m, int n, const 
 /* ---- stream: few tokens ---------------------------------------------------------------------------------------------------- */
 
 /* Up to 16 * MT tokens.  A workgroup of eight waves walks strips of 16 weight rows; wave w has the blocks w, w + 8, .. of k (KB of them at most), for
- * which it keeps the tokens' codes and scales in registers, and meets the others' sums in LDS.  The next strip's codes are in flight while one is
- * multiplied; one barrier a strip.  FUSED: the rows are made here, by every workgroup: a lane has what its token needs for
- * its own blocks, so that only the sum of squares of a norm crosses waves. */
+ * which it keeps the tokens' codes and scales in registers, and meets the others' sums in LDS; one barrier a strip.  A block's 2 KB go to LDS in whole lines (eight
+ * rows of 128 bytes a load) and from there to the lanes; a wave has AHEAD of them in flight, in a ring of its own.  FUSED: the rows are made here, by every workgroup: a lane has
+ * what its token needs for its own blocks, so that only the sum of squares of a norm crosses waves. */
 #define F8_WAVES 8
+template <int MT, int KB>
+struct f8_stream_shape {
+    static constexpr int groups = KB * MT <= 4 ? 2 : 1;       /* workgroups a unit */
+    static constexpr int waves = 2 * groups;                  /* a SIMD */
+    static constexpr int ahead = groups == 2 ? 3 : MT <= 3 ? 5 : 4;
+    static constexpr int ring = (ahead + 1) * 2048, sums = 2 * F8_WAVES * MT * 16 * 16 * 4, bytes = F8_WAVES * ring + sums;
+};
 template <int MT, int KB, bool FUSED>
-__global__ __launch_bounds__(F8_WAVES * 64, KB * (MT + 1) <= 6 ? 4 : 2) void bl_f8_stream(f8_args A, bl_prod_dev P) {
-    __shared__ __attribute__((aligned(16))) float red[2][F8_WAVES][MT * 16][16];
+__global__ __launch_bounds__(F8_WAVES * 64, (f8_stream_shape<MT, KB>::waves)) void bl_f8_stream(f8_args A, bl_prod_dev P) {
+    typedef f8_stream_shape<MT, KB> shape;
+    constexpr int AHEAD = shape::ahead;
+    extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
+    typedef float sums_t[F8_WAVES][MT * 16][16];
+    sums_t* red = (sums_t*)(lds + F8_WAVES * shape::ring);
     __shared__ double squares[F8_WAVES][16];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 15, g = lane >> 4;
     const int strips = (A.N + 15) / 16, stride = (int)gridDim.x;
     const bl_v4i zero = {0, 0, 0, 0};
-    bl_v4i w[KB][2];
-    float ws[KB];
-    /* slot j of a strip: loaded for the next as soon as it has been read */
-    auto load = [&](int strip, int j) {
-        const int n = strip * 16 + r, b = wave + F8_WAVES * j;
-        w[j][0] = w[j][1] = zero, ws[j] = 0.0f;
-        if (b < A.nb) {
-            const uint8_t* at = A.w + (n < A.N ? n : A.N - 1) * A.w_stride + g * 16 + b * F8_BLOCK;
-            w[j][0] = __builtin_nontemporal_load(bl_gc<bl_v4i>(at));
-            if (b * F8_BLOCK + 64 < A.K) w[j][1] = __builtin_nontemporal_load(bl_gc<bl_v4i>(at + 64));
-            ws[j] = A.ws[(int64_t)(strip >> 3) * A.ws_stride + b];
+    int strip = (int)blockIdx.x;
+    /* The ring: block j of a strip is 16 rows of 128 bytes; unit u of row q lies at unit u ^ (q / 2 % 8).  Behind the wave's last block its first is asked for
+     * again, so that the number in flight is always the same.  (Units behind a K that is no multiple of 128: as in the tiles.) */
+    const int blocks = (A.nb - wave + F8_WAVES - 1) / F8_WAVES;             /* of this wave; may be none */
+    uint8_t* const ring = lds + wave * shape::ring;
+    const int lrow = lane >> 3, lunit = (lane & 7) ^ (lrow >> 1), lunit2 = lunit ^ 4;       /* rows lrow and lrow + 8 */
+    int load_strip = strip, load_j = 0, load_slot = 0, slot = 0;
+    auto load = [&]() {
+        const int b = wave + F8_WAVES * load_j, n = load_strip * 16 + lrow;
+        const bool half = (b + 1) * F8_BLOCK > A.K;
+        const uint8_t* at = A.w + (int64_t)b * F8_BLOCK;
+        uint8_t* to = ring + load_slot * 2048;
+        __builtin_amdgcn_global_load_lds((bl_gptr)(at + (n < A.N ? n : A.N - 1) * A.w_stride + (half ? lunit & 3 : lunit) * 16), (bl_lptr)to, 16, 0, 2);
+        __builtin_amdgcn_global_load_lds((bl_gptr)(at + (n + 8 < A.N ? n + 8 : A.N - 1) * A.w_stride + (half ? lunit2 & 3 : lunit2) * 16), (bl_lptr)(to + 1024), 16, 0, 2);
+        load_slot = load_slot == AHEAD ? 0 : load_slot + 1;
+        if (++load_j == blocks) {
+            load_j = 0;
+            if (load_strip + stride < strips) load_strip += stride;
         }
     };
-    int strip = (int)blockIdx.x;
+    if (blocks > 0)
 #pragma unroll
-    for (int j = 0; j < KB; ++j) load(strip, j);
+        for (int i = 0; i < AHEAD; ++i) load();
     f8_v8i x[MT][KB] = {};
     float xs[MT][KB] = {};
     if constexpr (FUSED) {
@@ -227,7 +248,6 @@ __global__ __launch_bounds__(F8_WAVES * 64, KB * (MT + 1) <= 6 ? 4 : 2) void bl_
         for (int t = 0; t < MT; ++t)
 #pragma unroll
             for (int j = 0; j < KB; ++j) asm volatile("" : "+v"(x[t][j]));
-        const int next = strip + stride < strips ? strip + stride : strip;
         bl_v4f acc[MT], p[2][MT];
         float f[2][MT];
 #pragma unroll
@@ -240,14 +260,30 @@ __global__ __launch_bounds__(F8_WAVES * 64, KB * (MT + 1) <= 6 ? 4 : 2) void bl_
         };
 #pragma unroll
         for (int j = 0; j < KB; ++j) {
-            const f8_halves h = f8_open(f8_join(w[j][0], w[j][1]));
+            if (j < blocks) {
+                const float ws = f8_uniform(A.ws + (int64_t)(strip >> 3) * A.ws_stride + wave + F8_WAVES * j);
+                BL_WAIT_VM(2 * (AHEAD - 1));
+                asm volatile("" ::: "memory");
+                const uint8_t* row = ring + slot * 2048 + r * F8_BLOCK;
+                const f8_v8i c = f8_join(*(const bl_v4i*)(row + ((g ^ (r >> 1)) << 4)), *(const bl_v4i*)(row + (((g + 4) ^ (r >> 1)) << 4)));
+                BL_WAIT_LGKM0();
+                asm volatile("" ::: "memory");
+                load();                                       /* (into the slot read before this one) */
+                slot = slot == AHEAD ? 0 : slot + 1;
+                const f8_halves h = f8_open(c);
 #pragma unroll
-            for (int t = 0; t < MT; ++t) f[j & 1][t] = xs[t][j] * ws[j];
-            load(next, j);
+                for (int t = 0; t < MT; ++t) f[j & 1][t] = xs[t][j] * ws;
 #pragma unroll
-            for (int t = 0; t < MT; ++t) p[j & 1][t] = f8_product(h, f8_open(x[t][j]));
+                for (int t = 0; t < MT; ++t) p[j & 1][t] = f8_product(h, f8_open(x[t][j]));
+            } else {
+#pragma unroll
+                for (int t = 0; t < MT; ++t) p[j & 1][t] = (bl_v4f){0, 0, 0, 0}, f[j & 1][t] = 0.0f;
+            }
             __builtin_amdgcn_sched_barrier(0);                /* (four products at least between a block's last and its first reader) */
-            if (j > 0) add((j - 1) & 1);
+            if (j > 0) {
+                if (j >= blocks) bl_mfma_fence();
+                add((j - 1) & 1);
+            }
             __builtin_amdgcn_sched_barrier(0);
         }
         bl_mfma_fence();
@@ -271,6 +307,7 @@ __global__ __launch_bounds__(F8_WAVES * 64, KB * (MT + 1) <= 6 ? 4 : 2) void bl_
             }
         }
     }
+    BL_WAIT_VM(0);                                            /* (what is still on its way to LDS must not outlive the workgroup) */
 }
 
 /* ---- tiles: any number of tokens ------------------------------------------------------------------------------------------ */
@@ -519,12 +556,20 @@ extern "C" size_t bl_f8_workspace_bytes(const bl_f8_product* p) {
 }
 
 template <int MT, int KB, bool FUSED>
-static void f8_stream_kernel(const f8_args& A, const bl_prod_dev& P, hipStream_t st) {
-    const int strips = (A.N + 15) / 16, most = KB * (MT + 1) <= 6 ? 512 : 256;
-    bl_f8_stream<MT, KB, FUSED><<<(unsigned)(strips < most ? strips : most), F8_WAVES * 64, 0, st>>>(A, P);
+static bl_status f8_stream_kernel(const f8_args& A, const bl_prod_dev& P, hipStream_t st) {
+    typedef f8_stream_shape<MT, KB> shape;
+    const auto kern = bl_f8_stream<MT, KB, FUSED>;
+    static std::atomic<bool> attr_set;
+    if (!attr_set.load(std::memory_order_acquire)) {
+        if (hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, shape::bytes) != hipSuccess) return BL_ERR_HIP;
+        attr_set.store(true, std::memory_order_release);
+    }
+    const int strips = (A.N + 15) / 16, most = 256 * shape::groups;
+    kern<<<(unsigned)(strips < most ? strips : most), F8_WAVES * 64, shape::bytes, st>>>(A, P);
+    return hipGetLastError() == hipSuccess ? BL_OK : BL_ERR_HIP;
 }
 static bl_status f8_stream_launch(const f8_args& A, const bl_prod_dev& P, const f8_plan& q, hipStream_t st) {
-#define F8_STREAM(T, B) case (T) * 16 + (B): f8_stream_kernel<T, B, (T) == 1>(A, P, st); break
+#define F8_STREAM(T, B) case (T) * 16 + (B): return f8_stream_kernel<T, B, (T) == 1>(A, P, st)
     switch (q.tokens * 16 + q.blocks) {
         F8_STREAM(1, 1); F8_STREAM(1, 2); F8_STREAM(1, 3); F8_STREAM(1, 4); F8_STREAM(1, 6); F8_STREAM(1, 8);
         F8_STREAM(2, 1); F8_STREAM(2, 2); F8_STREAM(2, 3); F8_STREAM(2, 4); F8_STREAM(2, 6);
@@ -533,7 +578,6 @@ static bl_status f8_stream_launch(const f8_args& A, const bl_prod_dev& P, const 
         default: return BL_ERR_SHAPE;
     }
 #undef F8_STREAM
-    return hipGetLastError() == hipSuccess ? BL_OK : BL_ERR_HIP;
 }
 template <int BM, int BN, int WM, int WN, int S>
 static bl_status f8_tile_launch(f8_args& A, hipStream_t st) {
