@@ -388,9 +388,12 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void bl_f8_tile(f8_args A) {
             const uint8_t* p = at + base + t * 16 * F8_BLOCK;
             return f8_join(*(const bl_v4i*)(p + ((g ^ swz) << 4)), *(const bl_v4i*)(p + (((g + 4) ^ swz) << 4)));
         };
-        f8_halves x[TM];
+        /* One step a group of 16 weight rows: its products, and between them the next group's codes are opened and the one's before it are added. */
+        f8_v8i raw[2] = {part(w_at, 0), part(w_at, TN > 1 ? 1 : 0)};
+        f8_halves x[TM], w[2];
 #pragma unroll
         for (int t = 0; t < TM; ++t) x[t] = f8_open(part(x_at, t));
+        w[0] = f8_open(raw[0]);
         float f[TM];
 #pragma unroll
         for (int t = 0; t < TM; ++t) f[t] = xs[t] * ws;
@@ -401,17 +404,26 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void bl_f8_tile(f8_args A) {
 #pragma unroll
                 for (int v = 0; v < 4; ++v) acc[i][t][v] = __builtin_fmaf(p[i & 1][t][v], f[t], acc[i][t][v]);
         };
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int i = 0; i < TN; ++i) {
-            const f8_halves w = f8_open(part(w_at, i));
+            if (i + 2 < TN) raw[i & 1] = part(w_at, i + 2);
 #pragma unroll
             for (int t = 0; t < TM; ++t) p[i & 1][t] = (bl_v4f){0, 0, 0, 0};
 #pragma unroll
             for (int k = 0; k < 4; ++k)
 #pragma unroll
-                for (int t = 0; t < TM; ++t) p[i & 1][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(w.v[k], x[t].v[k], p[i & 1][t], 0, 0, 0);
-            __builtin_amdgcn_sched_barrier(0);                /* (a group of products between another's last and its first reader) */
+                for (int t = 0; t < TM; ++t) p[i & 1][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(w[i & 1].v[k], x[t].v[k], p[i & 1][t], 0, 0, 0);
+            if (i + 1 < TN) w[(i + 1) & 1] = f8_open(raw[(i + 1) & 1]);
             if (i > 0) add(i - 1);
+            if (i + 2 < TN) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+            __builtin_amdgcn_sched_group_barrier(0x008, TM, 0);          /* (so many between another group's last product and its first reader) */
+#pragma unroll
+            for (int k = 0; k < 3 * TM; ++k) {
+                __builtin_amdgcn_sched_group_barrier(0x002, 3, 0);
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            }
+            __builtin_amdgcn_sched_barrier(0);
         }
         bl_mfma_fence();
         add(TN - 1);
@@ -510,7 +522,7 @@ static bl_status f8_check(const bl_f8_matrix* w) {
 
 struct f8_plan {
     int splits, tokens, blocks;    /* of the stream: tiles of 16 tokens (0: not it), blocks of k a wave */
-    bool fused;
+    bool fused, small;             /* small: tiles of 64 x 64 */
     size_t codes, scales, bytes;   /* of the workspace: bytes of the codes, of the scales behind them, of all */
 };
 static size_t f8_round(size_t n) { return (n + 255) / 256 * 256; }
@@ -529,10 +541,12 @@ static f8_plan f8_make_plan(const bl_f8_product* p) {
         return q;
     }
     q.codes = f8_round((size_t)p->M * nb * F8_BLOCK), q.scales = f8_round((size_t)p->M * nb * sizeof(float));
-    const int64_t tiles = ((p->M + 127) / 128) * ((p->w.N + 127) / 128);
-    int64_t s = tiles < 256 ? 256 / tiles : 1;
-    if (s > nb / 4) s = nb / 4;
-    q.splits = s < 1 ? 1 : s > 16 ? 16 : (int)s;
+    const int64_t large = ((p->M + 127) / 128) * ((p->w.N + 127) / 128), small = ((p->M + 63) / 64) * ((p->w.N + 63) / 64);
+    q.small = large < 192;
+    const int64_t tiles = q.small ? small : large;
+    int64_t s = tiles < 512 ? 512 / tiles : 1;
+    if (s > nb / 2) s = nb / 2;
+    q.splits = s < 1 || !q.small ? 1 : s > 16 ? 16 : (int)s;
     q.bytes = q.codes + q.scales + (q.splits > 1 ? (size_t)q.splits * p->M * p->w.N * sizeof(float) : 0);
     return q;
 }
@@ -607,7 +621,7 @@ extern "C" bl_status bl_f8_linear(const bl_f8_product* p, bl_stream s) {
     const hipStream_t st = (hipStream_t)s;
     if (!q.fused) bl_f8_rows<<<(unsigned)A.M, 256, 0, st>>>(A, prod);
     if (q.tokens) return f8_stream_launch(A, prod, q, st);
-    const bl_status rc = f8_tile_launch<128, 128, 2, 2, 2>(A, st);
+    const bl_status rc = q.small ? f8_tile_launch<64, 64, 2, 2, 4>(A, st) : f8_tile_launch<128, 128, 2, 2, 2>(A, st);
     if (rc) return rc;
     if (A.splits > 1) {
         const int64_t blocks = ((int64_t)A.M * A.N + 255) / 256;
