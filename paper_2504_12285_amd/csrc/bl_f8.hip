@@ -7,6 +7,7 @@
  * and four consecutive weight rows, which is a run of the output.  A lane's 32 codes of a block are 16 from offset 16 g and 16 from 64 + 16 g,
  * g = lane / 16: the order of k inside a block is free as long as both operands have the same. */
 #include <atomic>
+#include <type_traits>
 
 #include "bl_device.h"
 #include "bl_host.h"
@@ -137,9 +138,10 @@ __device__ __forceinline__ void f8_store4(const f8_args& A, int m, int n, const 
 #define F8_WAVES 8
 template <int MT, int KB>
 struct f8_stream_shape {
-    static constexpr int groups = KB * MT <= 4 ? 2 : 1;       /* workgroups a unit */
+    static constexpr bool open = KB * MT <= 9;
+    static constexpr int groups = MT <= 2 && KB * MT <= 4 ? 2 : 1;          /* workgroups a unit, by registers; by LDS: */
     static constexpr int waves = 2 * groups;                  /* a SIMD */
-    static constexpr int ahead = groups == 2 ? 3 : MT <= 3 ? 5 : 4;
+    static constexpr int ahead = groups == 2 ? 4 - MT : 5;
     static constexpr int ring = (ahead + 1) * 2048, sums = 2 * F8_WAVES * MT * 16 * 16 * 4, bytes = F8_WAVES * ring + sums;
 };
 template <int MT, int KB, bool FUSED>
@@ -176,27 +178,37 @@ __global__ __launch_bounds__(F8_WAVES * 64, (f8_stream_shape<MT, KB>::waves)) vo
     if (blocks > 0)
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i) load();
-    f8_v8i x[MT][KB] = {};
-    float xs[MT][KB] = {};
+    /* the tokens' codes, opened once where the registers are there (as fp16 they take twice as many), else for every strip again */
+    std::conditional_t<shape::open, f8_halves, f8_v8i> x[MT][KB];
+    float xs[MT][KB];
+    auto keep = [&](int t, int j, f8_v8i c) {
+        if constexpr (shape::open) x[t][j] = f8_open(c);
+        else x[t][j] = c;
+    };
     if constexpr (FUSED) {
-        static_assert(MT == 1, "rows are made for one tile of tokens");
-        float rn = 0.0f;
-        if (P.norm) {
-            double ss = 0.0;
-            if (r < A.M) {
-#pragma unroll 1
-                for (int j = 0; j < KB; ++j) {
-                    const int b = wave + F8_WAVES * j;
+        static_assert(MT == 1 && KB == 1, "rows are made for one tile of tokens and a block a wave");
+        /* everything the lane needs at once, so that it hangs on one round of loads */
+        float v[KB][2][16];
 #pragma unroll
-                    for (int i = 0; i < 2; ++i)
-                        if (b * F8_BLOCK + 64 * i < A.K) {
-                            float v[16];
-                            bl_produce16_f32(P, r, b * 8 + 4 * i + g, A.K, false, v);
+        for (int j = 0; j < KB; ++j)
 #pragma unroll
-                            for (int e = 0; e < 16; ++e) ss += (double)v[e] * (double)v[e];
-                        }
+            for (int i = 0; i < 2; ++i) {
+                const int b = wave + F8_WAVES * j;
+                if (r < A.M && b * F8_BLOCK + 64 * i < A.K) {
+                    bl_produce16_f32(P, r, b * 8 + 4 * i + g, A.K, blockIdx.x == 0, v[j][i]);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) v[j][i][e] = 0.0f;
                 }
             }
+        if (P.norm) {
+            double ss = 0.0;
+#pragma unroll
+            for (int j = 0; j < KB; ++j)
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) ss += (double)v[j][i][e] * (double)v[j][i][e];
             ss += __shfl_xor(ss, 16);
             ss += __shfl_xor(ss, 32);
             if (lane < 16) squares[wave][lane] = ss;
@@ -204,26 +216,38 @@ __global__ __launch_bounds__(F8_WAVES * 64, (f8_stream_shape<MT, KB>::waves)) vo
             double sum = 0.0;
 #pragma unroll
             for (int w = 0; w < F8_WAVES; ++w) sum += squares[w][r];
-            rn = (float)(1.0 / sqrt(sum / (double)A.K + (double)P.eps));
-        }
-#pragma unroll 1
-        for (int at = 0; at < KB; ++at) {                     /* (one block's values in registers at a time) */
-            const int b = wave + F8_WAVES * at;
-            uint4 lo[2], hi[2];
-            float most = 0.0f;
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                lo[i] = hi[i] = make_uint4(0, 0, 0, 0);
-                if (r < A.M && b * F8_BLOCK + 64 * i < A.K) bl_produce16<true>(P, r, b * 8 + 4 * i + g, A.K, blockIdx.x == 0, rn, lo[i], hi[i]);
-                most = bl_max_pos(most, f8_largest16(lo[i], hi[i]));
-            }
-            most = bl_max_pos(most, __shfl_xor(most, 16));
-            most = bl_max_pos(most, __shfl_xor(most, 32));
-            const float scale = f8_scale(most), inv = bl_div_rn(1.0f, scale);
-            const f8_v8i c = f8_join(f8_codes16(lo[0], hi[0], inv), f8_codes16(lo[1], hi[1], inv));
+            const float rn = (float)(1.0 / sqrt(sum / (double)A.K + (double)P.eps));
 #pragma unroll
             for (int j = 0; j < KB; ++j)
-                if (j == at) x[0][j] = c, xs[0][j] = scale;
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const int b = wave + F8_WAVES * j, u = b * 8 + 4 * i + g;
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) v[j][i][e] *= rn;
+                    if (P.gain && b * F8_BLOCK + 64 * i < A.K) {
+#pragma unroll
+                        for (int e = 0; e < 16; e += 4) {
+                            const bl_v4f x = *bl_gc<bl_v4f>(P.gain + (int64_t)u * 16 + e);
+                            v[j][i][e] *= x[0], v[j][i][e + 1] *= x[1], v[j][i][e + 2] *= x[2], v[j][i][e + 3] *= x[3];
+                        }
+                    }
+                }
+        }
+#pragma unroll
+        for (int j = 0; j < KB; ++j) {
+            uint4 lo[2], hi[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const float (&y)[16] = v[j][i];
+                lo[i] = make_uint4(bl_pack2_bf16(y[0], y[1]), bl_pack2_bf16(y[2], y[3]), bl_pack2_bf16(y[4], y[5]), bl_pack2_bf16(y[6], y[7]));
+                hi[i] = make_uint4(bl_pack2_bf16(y[8], y[9]), bl_pack2_bf16(y[10], y[11]), bl_pack2_bf16(y[12], y[13]), bl_pack2_bf16(y[14], y[15]));
+            }
+            float most = bl_max_pos(f8_largest16(lo[0], hi[0]), f8_largest16(lo[1], hi[1]));
+            most = bl_max_pos(most, __shfl_xor(most, 16));
+            most = bl_max_pos(most, __shfl_xor(most, 32));
+            xs[0][j] = f8_scale(most);
+            const float inv = bl_div_rn(1.0f, xs[0][j]);
+            keep(0, j, f8_join(f8_codes16(lo[0], hi[0], inv), f8_codes16(lo[1], hi[1], inv)));
         }
     } else {
 #pragma unroll
@@ -233,21 +257,24 @@ __global__ __launch_bounds__(F8_WAVES * 64, (f8_stream_shape<MT, KB>::waves)) vo
 #pragma unroll
             for (int j = 0; j < KB; ++j) {
                 const int b = wave + F8_WAVES * j;
-                x[t][j] = f8_join(zero, zero), xs[t][j] = 0.0f;
+                f8_v8i c = f8_join(zero, zero);
+                xs[t][j] = 0.0f;
                 if (b < A.nb) {
-                    x[t][j] = f8_join(*bl_gc<bl_v4i>(row + b * F8_BLOCK), *bl_gc<bl_v4i>(row + b * F8_BLOCK + 64));
+                    c = f8_join(*bl_gc<bl_v4i>(row + b * F8_BLOCK), *bl_gc<bl_v4i>(row + b * F8_BLOCK + 64));
                     xs[t][j] = A.scales[(int64_t)b * A.M + m];
                 }
+                keep(t, j, c);
             }
         }
     }
     int buf = 0;
     for (; strip < strips; strip += stride, buf ^= 1) {
-        /* (the tokens' codes are opened again for every strip: as fp16 they would take twice the registers) */
+        if constexpr (!shape::open) {                         /* (or the compiler opens them in front of the loop) */
 #pragma unroll
-        for (int t = 0; t < MT; ++t)
+            for (int t = 0; t < MT; ++t)
 #pragma unroll
-            for (int j = 0; j < KB; ++j) asm volatile("" : "+v"(x[t][j]));
+                for (int j = 0; j < KB; ++j) asm volatile("" : "+v"(x[t][j]));
+        }
         bl_v4f acc[MT], p[2][MT];
         float f[2][MT];
 #pragma unroll
@@ -274,7 +301,10 @@ __global__ __launch_bounds__(F8_WAVES * 64, (f8_stream_shape<MT, KB>::waves)) vo
 #pragma unroll
                 for (int t = 0; t < MT; ++t) f[j & 1][t] = xs[t][j] * ws;
 #pragma unroll
-                for (int t = 0; t < MT; ++t) p[j & 1][t] = f8_product(h, f8_open(x[t][j]));
+                for (int t = 0; t < MT; ++t) {
+                    if constexpr (shape::open) p[j & 1][t] = f8_product(h, x[t][j]);
+                    else p[j & 1][t] = f8_product(h, f8_open(x[t][j]));
+                }
             } else {
 #pragma unroll
                 for (int t = 0; t < MT; ++t) p[j & 1][t] = (bl_v4f){0, 0, 0, 0}, f[j & 1][t] = 0.0f;
@@ -331,28 +361,36 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void bl_f8_tile(f8_args A) {
     const int split = place % A.splits, tile = place / A.splits, m0 = tile % A.tiles_m * BM, n0 = tile / A.tiles_m * BN;
     const int b0 = (int)((int64_t)A.nb * split / A.splits), b1 = (int)((int64_t)A.nb * (split + 1) / A.splits);
     const int half = A.K % F8_BLOCK ? A.nb - 1 : -1;          /* the block of which only half is there */
-    const uint8_t* from[LOADS];
-    int unit[LOADS];
+    const uint8_t* from[LOADS];                               /* what the lane loads of the next block */
 #pragma unroll
     for (int j = 0; j < LOADS; ++j) {
         const int p = j * NW + wave;                          /* 1024 bytes, eight rows */
         const bool is_x = p < BM / 8;
         const int row = (is_x ? p : p - BM / 8) * 8 + lane / 8;
-        unit[j] = (lane & 7) ^ (row >> 1 & 7);
         if (is_x) {
             const int m = m0 + row < A.M ? m0 + row : A.M - 1;
-            from[j] = A.codes + (int64_t)m * A.nb * F8_BLOCK;
+            from[j] = A.codes + ((int64_t)m * A.nb + b0) * F8_BLOCK;
         } else {
             const int n = n0 + row < A.N ? n0 + row : A.N - 1;
-            from[j] = A.w + n * A.w_stride;
+            from[j] = A.w + n * A.w_stride + (int64_t)b0 * F8_BLOCK;
         }
+        from[j] += ((lane & 7) ^ (row >> 1 & 7)) * 16;
     }
-    auto load = [&](int b, int stage) {
+    int loaded = b0;
+    auto load = [&](int stage) {
         uint8_t* to = lds + stage * STAGE;
+        if (loaded == half) {
 #pragma unroll
-        for (int j = 0; j < LOADS; ++j) {
-            const int p = j * NW + wave, u = b == half && p >= BM / 8 ? unit[j] & 3 : unit[j];
-            __builtin_amdgcn_global_load_lds((bl_gptr)(from[j] + (int64_t)b * F8_BLOCK + u * 16), (bl_lptr)(to + p * 1024), 16, 0, 0);
+            for (int j = 0; j < LOADS; ++j) {
+                const int p = j * NW + wave, row = (p - BM / 8) * 8 + lane / 8;
+                if (p >= BM / 8 && (((lane & 7) ^ (row >> 1 & 7)) & 4)) from[j] -= 64;
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < LOADS; ++j) __builtin_amdgcn_global_load_lds((bl_gptr)from[j], (bl_lptr)(to + (j * NW + wave) * 1024), 16, 0, 0);
+        if (++loaded < b1) {                                  /* (behind the last block it is loaded again, for nobody) */
+#pragma unroll
+            for (int j = 0; j < LOADS; ++j) from[j] += F8_BLOCK;
         }
     };
     float xs[TM], xn[TM], ws, wsn;
@@ -370,7 +408,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void bl_f8_tile(f8_args A) {
         for (int t = 0; t < TM; ++t) acc[i][t] = (bl_v4f){0, 0, 0, 0};
     load_scales(b0);
 #pragma unroll
-    for (int s = 0; s < S - 1; ++s) load(b0 + s < b1 ? b0 + s : b1 - 1, s);
+    for (int s = 0; s < S - 1; ++s) load(s);
     const int x_at = (wm * (BM / WM) + r) * F8_BLOCK, w_at = BM * F8_BLOCK + (wn * (BN / WN) + r) * F8_BLOCK, swz = (r >> 1) & 7;
     int stage = 0;
     for (int b = b0; b < b1; ++b) {
@@ -382,7 +420,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void bl_f8_tile(f8_args A) {
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
         load_scales(b + 1 < b1 ? b + 1 : b);
-        load(b + S - 1 < b1 ? b + S - 1 : b1 - 1, stage == 0 ? S - 1 : stage - 1);
+        load(stage == 0 ? S - 1 : stage - 1);
         const uint8_t* at = lds + stage * STAGE;
         auto part = [&](int base, int t) {
             const uint8_t* p = at + base + t * 16 * F8_BLOCK;
@@ -405,6 +443,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void bl_f8_tile(f8_args A) {
                 for (int v = 0; v < 4; ++v) acc[i][t][v] = __builtin_fmaf(p[i & 1][t][v], f[t], acc[i][t][v]);
         };
         __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_setprio(1);                        /* (the other workgroup's wave opens its codes meanwhile) */
 #pragma unroll
         for (int i = 0; i < TN; ++i) {
             if (i + 2 < TN) raw[i & 1] = part(w_at, i + 2);
@@ -425,6 +464,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void bl_f8_tile(f8_args A) {
             }
             __builtin_amdgcn_sched_barrier(0);
         }
+        __builtin_amdgcn_s_setprio(0);
         bl_mfma_fence();
         add(TN - 1);
         BL_WAIT_LGKM0();
@@ -530,11 +570,11 @@ static f8_plan f8_make_plan(const bl_f8_product* p) {
     f8_plan q;
     const int64_t nb = (p->w.K + F8_BLOCK - 1) / F8_BLOCK;
     q.splits = 1;
-    /* the stream, while a wave's registers hold its blocks of every token beside two strips' */
-    q.tokens = (int)((p->M + 15) / 16 < 5 ? (p->M + 15) / 16 : 0), q.blocks = (int)((nb + F8_WAVES - 1) / F8_WAVES < 9 ? (nb + F8_WAVES - 1) / F8_WAVES : 9);
-    q.blocks = q.blocks <= 4 ? q.blocks : q.blocks <= 6 ? 6 : q.blocks <= 8 ? 8 : 9;
-    if (q.tokens * q.blocks == 0 || q.blocks > 8 || q.blocks * (q.tokens + 1) > 18) q.tokens = 0;
-    q.fused = q.tokens == 1;
+    /* the stream, while a wave's registers hold its blocks of every token */
+    const int64_t each = (nb + F8_WAVES - 1) / F8_WAVES;
+    q.tokens = p->M <= 64 ? (int)((p->M + 15) / 16) : 0, q.blocks = each > 8 ? 16 : each <= 4 ? (int)each : each <= 6 ? 6 : 8;
+    if (q.tokens * q.blocks > 12) q.tokens = 0;
+    q.fused = q.tokens == 1 && q.blocks == 1;
     if (q.tokens) {
         q.codes = q.fused ? 0 : f8_round((size_t)p->M * nb * F8_BLOCK), q.scales = q.fused ? 0 : f8_round((size_t)p->M * nb * sizeof(float));
         q.bytes = q.codes + q.scales;
@@ -569,7 +609,7 @@ extern "C" size_t bl_f8_workspace_bytes(const bl_f8_product* p) {
     return f8_check_product(p, &prod) == BL_OK ? f8_make_plan(p).bytes : 0;
 }
 
-template <int MT, int KB, bool FUSED>
+template <int MT, int KB, bool FUSED = false>
 static bl_status f8_stream_kernel(const f8_args& A, const bl_prod_dev& P, hipStream_t st) {
     typedef f8_stream_shape<MT, KB> shape;
     const auto kern = bl_f8_stream<MT, KB, FUSED>;
@@ -583,7 +623,8 @@ static bl_status f8_stream_kernel(const f8_args& A, const bl_prod_dev& P, hipStr
     return hipGetLastError() == hipSuccess ? BL_OK : BL_ERR_HIP;
 }
 static bl_status f8_stream_launch(const f8_args& A, const bl_prod_dev& P, const f8_plan& q, hipStream_t st) {
-#define F8_STREAM(T, B) case (T) * 16 + (B): return f8_stream_kernel<T, B, (T) == 1>(A, P, st)
+    if (q.fused) return f8_stream_kernel<1, 1, true>(A, P, st);
+#define F8_STREAM(T, B) case (T) * 16 + (B): return f8_stream_kernel<T, B>(A, P, st)
     switch (q.tokens * 16 + q.blocks) {
         F8_STREAM(1, 1); F8_STREAM(1, 2); F8_STREAM(1, 3); F8_STREAM(1, 4); F8_STREAM(1, 6); F8_STREAM(1, 8);
         F8_STREAM(2, 1); F8_STREAM(2, 2); F8_STREAM(2, 3); F8_STREAM(2, 4); F8_STREAM(2, 6);
