@@ -74,8 +74,10 @@ class Producer(ctypes.Structure):
 
 
 def make_producer(kind, in0, in1=None, aux_out=None, n_q=0, n_kv=0, head_dim=0, norm=False, gain=None, eps=1e-5):
-    """norm=True: RMS normalisation (optional fp32 gains [K]) in front of the quantiser."""
+    """norm=True: RMS normalisation (optional fp32 gains [K]) in front of the quantiser.  The descriptor keeps its tensors alive: memory of a temporary
+    would else be free again before the call that reads it, for an output of that call among others."""
     p = Producer()
+    p.tensors = (in0, in1, aux_out, gain)
     p.kind, p.in0, p.in1, p.aux_out = int(kind), _ptr(in0), _ptr(in1), _ptr(aux_out)
     p.n_q, p.n_kv, p.head_dim = int(n_q), int(n_kv), int(head_dim)
     p.norm, p.gain, p.eps = int(bool(norm)), _ptr(gain), float(eps)
@@ -776,7 +778,7 @@ def _f8_kind(dtype):
 
 class F8Linear(_KVCall):
     """y = rows times the matrix's transpose (bl_f8_linear).  x: bf16 or fp32 [M][K], with norm=True normalised on the way (gain fp32 [K] or
-    None); or prod, a producer of make_producer whose tensors the caller keeps, and M.  Output: y [M][N] of `dtype` (or of y's).  The workspace
+    None); or prod, a producer of make_producer, and M.  Output: y [M][N] of `dtype` (or of y's).  The workspace
     may serve several handles whose runs follow each other on one stream."""
     _which, _where = 7, "bl_f8_linear"
 
@@ -797,7 +799,7 @@ class F8Linear(_KVCall):
             y = torch.empty((M, matrix.N), dtype=torch.float32 if dtype is None else dtype, device=dev)
         else:
             _wants(y, "y", y.dtype if dtype is None else dtype, dev, (M, matrix.N), rows=True)
-        self.matrix, self.x, self.gain, self.y = matrix, x, gain, y
+        self.matrix, self.prod, self.y = matrix, prod, y
         self.desc = F8ProductDesc(matrix.desc, prod, M, _row_stride(y), _ptr(y), _f8_kind(y.dtype), None)
         self.workspace = _space_of(load().bl_f8_workspace_bytes(ctypes.byref(self.desc)), workspace, dev)
         self.desc.workspace = _ptr(self.workspace)

@@ -159,3 +159,17 @@ def test_the_binding_takes_what_a_descriptor_can_stand_for(lib):  # noqa: F811
     for more in (dict(held=n[:2]), dict(held=n, max_new=0)):
         with pytest.raises((TypeError, ValueError)):
             bl.KVTables(n, n, table, torch.zeros(9, dtype=i32), torch.zeros(1, dtype=i32), 16, 5, **more)
+
+
+def test_a_producer_keeps_its_tensors():
+    import gc
+    import weakref
+    tensors = [torch.zeros(3, 192) for _ in range(4)]
+    refs = [weakref.ref(t) for t in tensors]
+    p = bl.make_producer(bl.BL_PROD_RESIDUAL, tensors[0], tensors[1], tensors[2], norm=True, gain=tensors[3])
+    del tensors
+    gc.collect()
+    assert all(r() is not None for r in refs)
+    del p
+    gc.collect()
+    assert all(r() is None for r in refs)
