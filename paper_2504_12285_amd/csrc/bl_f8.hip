@@ -112,6 +112,23 @@ __global__ __launch_bounds__(256) void bl_f8_rows(f8_args A, bl_prod_dev P) {
     }
 }
 
+/* The same without a norm, where nothing crosses a group: the units of all rows in one line. */
+__global__ __launch_bounds__(256) void bl_f8_units(f8_args A, bl_prod_dev P) {
+    const int groups = A.K / 16, all = A.nb * 8;
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= (int64_t)A.M * all) return;                      /* (groups of eight threads, whole ones) */
+    const int m = (int)(i / all), u = (int)(i - (int64_t)m * all);
+    uint4 lo = make_uint4(0, 0, 0, 0), hi = lo;
+    if (u < groups) bl_produce16<false>(P, m, u, A.K, true, 0.0f, lo, hi);
+    float g = f8_largest16(lo, hi);
+    g = bl_max_pos(g, bl_dppf<BL_DPP_QUAD_XOR1>(g));
+    g = bl_max_pos(g, bl_dppf<BL_DPP_QUAD_XOR2>(g));
+    g = bl_max_pos(g, bl_dppf<BL_DPP_ROW_HALF_MIRROR>(g));
+    const float s = f8_scale(g);
+    *(bl_v4i*)(A.codes + i * 16) = f8_codes16(lo, hi, bl_div_rn(1.0f, s));
+    if ((u & 7) == 0) A.scales[(int64_t)(u >> 3) * A.M + m] = s;
+}
+
 /* ---- output -------------------------------------------------------------------------------------------------------------- */
 
 __device__ __forceinline__ uint16_t f8_bf16(float v) { return (uint16_t)bl_pack2_bf16(v, v); }
@@ -340,6 +357,9 @@ __global__ __launch_bounds__(F8_WAVES * 64, (f8_stream_shape<MT, KB>::waves)) vo
     BL_WAIT_VM(0);                                            /* (what is still on its way to LDS must not outlive the workgroup) */
 }
 
+/* Values from a row to the next of the pieces of a split k loop: whole vectors. */
+__host__ __device__ static __forceinline__ int64_t f8_part_stride(int64_t N) { return (N + 3) / 4 * 4; }
+
 /* ---- tiles: any number of tokens ------------------------------------------------------------------------------------------ */
 
 /* BM tokens x BN weight rows a workgroup, WM x WN waves, S stages of one block of k (128) in LDS.  Rows of 128 bytes; unit u (16 bytes) of row r lies
@@ -348,7 +368,7 @@ __global__ __launch_bounds__(F8_WAVES * 64, (f8_stream_shape<MT, KB>::waves)) vo
  * NaN among them spoils the row anyway). */
 template <int BM, int BN, int WM, int WN, int S>
 __global__ __launch_bounds__(WM * WN * 64, 2) void bl_f8_tile(f8_args A) {
-    constexpr int NW = WM * WN, TM = BM / WM / 16, TN = BN / WN / 16, STAGE = (BM + BN) * F8_BLOCK, LOADS = (BM + BN) / 8 / NW;
+    constexpr int NW = WM * WN, TM = BM / WM / 16, TN = BN / WN / 16, SCALES = (BM + BN) * F8_BLOCK, STAGE = SCALES + BM * 4, LOADS = (BM + BN) / 8 / NW;
     extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 15, g = lane >> 4;
     const int wm = wave % WM, wn = wave / WM;
@@ -376,6 +396,9 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void bl_f8_tile(f8_args A) {
         }
         from[j] += ((lane & 7) ^ (row >> 1 & 7)) * 16;
     }
+    /* and the tokens' scales of the block, 64 a load: a wave loads some of them (others the same again), so that all waves count the same */
+    const int sm = wave % (BM / 64) * 64;
+    const float* scales = A.scales + (int64_t)b0 * A.M + (m0 + sm + lane < A.M ? m0 + sm + lane : A.M - 1);
     int loaded = b0;
     auto load = [&](int stage) {
         uint8_t* to = lds + stage * STAGE;
@@ -388,38 +411,30 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void bl_f8_tile(f8_args A) {
         }
 #pragma unroll
         for (int j = 0; j < LOADS; ++j) __builtin_amdgcn_global_load_lds((bl_gptr)from[j], (bl_lptr)(to + (j * NW + wave) * 1024), 16, 0, 0);
+        __builtin_amdgcn_global_load_lds((bl_gptr)scales, (bl_lptr)(to + SCALES + sm * 4), 4, 0, 0);
         if (++loaded < b1) {                                  /* (behind the last block it is loaded again, for nobody) */
 #pragma unroll
             for (int j = 0; j < LOADS; ++j) from[j] += F8_BLOCK;
+            scales += A.M;
         }
     };
-    float xs[TM], xn[TM], ws, wsn;
     const int mrow = m0 + wm * (BM / WM) + r;
     const float* wscale = A.ws + (int64_t)((n0 + wn * (BN / WN)) / F8_BLOCK < (A.N - 1) / F8_BLOCK ? (n0 + wn * (BN / WN)) / F8_BLOCK : (A.N - 1) / F8_BLOCK) * A.ws_stride;
-    auto load_scales = [&](int b) {
-#pragma unroll
-        for (int t = 0; t < TM; ++t) xn[t] = A.scales[(int64_t)b * A.M + (mrow + 16 * t < A.M ? mrow + 16 * t : A.M - 1)];
-        wsn = wscale[b];
-    };
     bl_v4f acc[TN][TM];
 #pragma unroll
     for (int i = 0; i < TN; ++i)
 #pragma unroll
         for (int t = 0; t < TM; ++t) acc[i][t] = (bl_v4f){0, 0, 0, 0};
-    load_scales(b0);
 #pragma unroll
     for (int s = 0; s < S - 1; ++s) load(s);
     const int x_at = (wm * (BM / WM) + r) * F8_BLOCK, w_at = BM * F8_BLOCK + (wn * (BN / WN) + r) * F8_BLOCK, swz = (r >> 1) & 7;
     int stage = 0;
     for (int b = b0; b < b1; ++b) {
-#pragma unroll
-        for (int t = 0; t < TM; ++t) xs[t] = xn[t];
-        ws = wsn;
-        BL_WAIT_VM((S - 2) * LOADS);
+        const float ws = f8_uniform(wscale + b);
+        BL_WAIT_VM((S - 2) * (LOADS + 1));
         asm volatile("" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
-        load_scales(b + 1 < b1 ? b + 1 : b);
         load(stage == 0 ? S - 1 : stage - 1);
         const uint8_t* at = lds + stage * STAGE;
         auto part = [&](int base, int t) {
@@ -434,7 +449,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void bl_f8_tile(f8_args A) {
         w[0] = f8_open(raw[0]);
         float f[TM];
 #pragma unroll
-        for (int t = 0; t < TM; ++t) f[t] = xs[t] * ws;
+        for (int t = 0; t < TM; ++t) f[t] = *(const float*)(at + SCALES + (wm * (BM / WM) + 16 * t + r) * 4) * ws;
         bl_v4f p[2][TM];
         auto add = [&](int i) {
 #pragma unroll
@@ -483,22 +498,29 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void bl_f8_tile(f8_args A) {
             if (A.splits == 1) {
                 f8_store4(A, m, n, v);
             } else {
-                float* to = A.part + ((int64_t)split * A.M + m) * A.N + n;
-                for (int j = 0; j < 4 && n + j < A.N; ++j) to[j] = v[j];
+                *bl_g((bl_v4f*)(A.part + ((int64_t)split * A.M + m) * f8_part_stride(A.N) + n)) = acc[i][t];
             }
         }
     }
 }
 
-/* The pieces of a split k loop, added in their order. */
+/* The pieces of a split k loop, added in their order, four columns a thread. */
 __global__ __launch_bounds__(256) void bl_f8_join(f8_args A) {
-    const int64_t all = (int64_t)A.M * A.N;
+    const int units = (A.N + 3) / 4;
+    const int64_t all = (int64_t)A.M * units, stride = f8_part_stride(A.N);
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
-        float v = A.part[i];
-        for (int s = 1; s < A.splits; ++s) v += A.part[s * all + i];
-        const int64_t at = i / A.N * A.y_stride + i % A.N;
-        if (A.bf16) ((uint16_t*)A.y)[at] = f8_bf16(v);
-        else ((float*)A.y)[at] = v;
+        const int m = (int)(i / units), n = (int)(i - (int64_t)m * units) * 4;
+        const float* from = A.part + m * stride + n;
+        bl_v4f x = {0, 0, 0, 0};
+        for (int s = 0; s < A.splits; s += 4) {               /* four in flight */
+            bl_v4f y[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) y[k] = s + k < A.splits ? *bl_gc<bl_v4f>(from + (s + k) * A.M * stride) : (bl_v4f){0, 0, 0, 0};
+#pragma unroll
+            for (int k = 0; k < 4; ++k) x += y[k];
+        }
+        const float v[4] = {x[0], x[1], x[2], x[3]};
+        f8_store4(A, m, n, v);
     }
 }
 
@@ -587,7 +609,7 @@ static f8_plan f8_make_plan(const bl_f8_product* p) {
     int64_t s = tiles < 512 ? 512 / tiles : 1;
     if (s > nb / 2) s = nb / 2;
     q.splits = s < 1 || !q.small ? 1 : s > 16 ? 16 : (int)s;
-    q.bytes = q.codes + q.scales + (q.splits > 1 ? (size_t)q.splits * p->M * p->w.N * sizeof(float) : 0);
+    q.bytes = q.codes + q.scales + (q.splits > 1 ? (size_t)q.splits * p->M * f8_part_stride(p->w.N) * sizeof(float) : 0);
     return q;
 }
 
@@ -636,7 +658,7 @@ static bl_status f8_stream_launch(const f8_args& A, const bl_prod_dev& P, const 
 }
 template <int BM, int BN, int WM, int WN, int S>
 static bl_status f8_tile_launch(f8_args& A, hipStream_t st) {
-    constexpr int bytes = S * (BM + BN) * F8_BLOCK;
+    constexpr int bytes = S * ((BM + BN) * F8_BLOCK + BM * 4);
     const auto kern = bl_f8_tile<BM, BN, WM, WN, S>;
     static std::atomic<bool> attr_set;
     if (!attr_set.load(std::memory_order_acquire)) {
@@ -660,12 +682,14 @@ extern "C" bl_status bl_f8_linear(const bl_f8_product* p, bl_stream s) {
     A.y = p->y, A.y_stride = p->y_stride, A.M = (int)p->M, A.N = (int)p->w.N, A.K = (int)p->w.K, A.nb = (A.K + F8_BLOCK - 1) / F8_BLOCK;
     A.bf16 = p->y_kind == BL_F8_OUT_BF16, A.wide = bl_aligned(p->y, 16) && p->y_stride % (A.bf16 ? 8 : 4) == 0, A.splits = q.splits;
     const hipStream_t st = (hipStream_t)s;
-    if (!q.fused) bl_f8_rows<<<(unsigned)A.M, 256, 0, st>>>(A, prod);
+    const int64_t units = ((int64_t)A.M * A.nb * 8 + 255) / 256;
+    if (!q.fused && (prod.norm || units > 0x7fffffff)) bl_f8_rows<<<(unsigned)A.M, 256, 0, st>>>(A, prod);
+    else if (!q.fused) bl_f8_units<<<(unsigned)units, 256, 0, st>>>(A, prod);
     if (q.tokens) return f8_stream_launch(A, prod, q, st);
     const bl_status rc = q.small ? f8_tile_launch<64, 64, 2, 2, 4>(A, st) : f8_tile_launch<128, 128, 2, 2, 2>(A, st);
     if (rc) return rc;
     if (A.splits > 1) {
-        const int64_t blocks = ((int64_t)A.M * A.N + 255) / 256;
+        const int64_t blocks = ((int64_t)A.M * ((A.N + 3) / 4) + 255) / 256;
         bl_f8_join<<<(unsigned)(blocks < 65536 ? blocks : 65536), 256, 0, st>>>(A);
     }
     return hipGetLastError() == hipSuccess ? BL_OK : BL_ERR_HIP;
