@@ -604,7 +604,7 @@ static f8_plan f8_make_plan(const bl_f8_product* p) {
     }
     q.codes = f8_round((size_t)p->M * nb * F8_BLOCK), q.scales = f8_round((size_t)p->M * nb * sizeof(float));
     const int64_t large = ((p->M + 127) / 128) * ((p->w.N + 127) / 128), small = ((p->M + 63) / 64) * ((p->w.N + 63) / 64);
-    q.small = large < 192;
+    q.small = large < 192 || p->M <= 64;
     const int64_t tiles = q.small ? small : large;
     int64_t s = tiles < 512 ? 512 / tiles : 1;
     if (s > nb / 2) s = nb / 2;
@@ -686,7 +686,7 @@ extern "C" bl_status bl_f8_linear(const bl_f8_product* p, bl_stream s) {
     if (!q.fused && (prod.norm || units > 0x7fffffff)) bl_f8_rows<<<(unsigned)A.M, 256, 0, st>>>(A, prod);
     else if (!q.fused) bl_f8_units<<<(unsigned)units, 256, 0, st>>>(A, prod);
     if (q.tokens) return f8_stream_launch(A, prod, q, st);
-    const bl_status rc = q.small ? f8_tile_launch<64, 64, 2, 2, 4>(A, st) : f8_tile_launch<128, 128, 2, 2, 2>(A, st);
+    const bl_status rc = q.small ? f8_tile_launch<64, 64, 2, 2, 2>(A, st) : f8_tile_launch<128, 128, 2, 2, 2>(A, st);
     if (rc) return rc;
     if (A.splits > 1) {
         const int64_t blocks = ((int64_t)A.M * ((A.N + 3) / 4) + 255) / 256;
