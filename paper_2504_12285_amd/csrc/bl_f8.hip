@@ -31,7 +31,7 @@ struct f8_args {
     int64_t y_stride;
     float* part;                   /* [splits][M][N] where the k loop is split */
     int M, N, K, nb;
-    int bf16, wide;                /* output type; rows of y are 16-byte aligned */
+    int bf16;                      /* output type */
     int splits, tiles_m, tiles_n;
 };
 
@@ -80,35 +80,66 @@ __device__ __forceinline__ float f8_largest16(const uint4& lo, const uint4& hi) 
     return bl_max_pos(bl_absmax8_bf16<false>(lo), bl_absmax8_bf16<false>(hi));
 }
 
-/* A workgroup a token, a thread 16 values: eight threads have a group of 128.  Zeros behind K in the last block. */
+/* A thread's unit of 16 values: eight threads have a group of 128. */
+__device__ __forceinline__ void f8_put_unit(const f8_args& A, int m, int u, const uint4& lo, const uint4& hi) {
+    float g = f8_largest16(lo, hi);
+    g = bl_max_pos(g, bl_dppf<BL_DPP_QUAD_XOR1>(g));
+    g = bl_max_pos(g, bl_dppf<BL_DPP_QUAD_XOR2>(g));
+    g = bl_max_pos(g, bl_dppf<BL_DPP_ROW_HALF_MIRROR>(g));
+    const float s = f8_scale(g);
+    *(bl_v4i*)(A.codes + ((int64_t)m * A.nb * 8 + u) * 16) = f8_codes16(lo, hi, bl_div_rn(1.0f, s));
+    if ((u & 7) == 0) A.scales[(int64_t)(u >> 3) * A.M + m] = s;
+}
+/* Normed rows of up to 1024 values: a wave a row, which is read once and meets nobody (803 rows of 256 values: a workgroup a row 22 us, so 5). */
+__global__ __launch_bounds__(256) void bl_f8_wave_rows(f8_args A, bl_prod_dev P) {
+    const int m = (int)blockIdx.x * 4 + (threadIdx.x >> 6), u = threadIdx.x & 63, groups = A.K / 16;
+    if (m >= A.M) return;
+    float v[16];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) v[e] = 0.0f;
+    double ss = 0.0;
+    if (u < groups) {
+        bl_produce16_f32(P, m, u, A.K, true, v);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) ss += (double)v[e] * (double)v[e];
+    }
+#pragma unroll
+    for (int x = 1; x < 64; x <<= 1) ss += __shfl_xor(ss, x);
+    const float rn = (float)(1.0 / sqrt(ss / (double)A.K + (double)P.eps));
+    if (u >= A.nb * 8) return;                                /* (groups of eight lanes, whole ones) */
+    if (u < groups) {                                         /* (a row that is NaN: not its padding) */
+#pragma unroll
+        for (int e = 0; e < 16; ++e) v[e] *= rn;
+        if (P.gain) {
+#pragma unroll
+            for (int e = 0; e < 16; e += 4) {
+                const bl_v4f x = *bl_gc<bl_v4f>(P.gain + (int64_t)u * 16 + e);
+                v[e] *= x[0], v[e + 1] *= x[1], v[e + 2] *= x[2], v[e + 3] *= x[3];
+            }
+        }
+    }
+    f8_put_unit(A, m, u, make_uint4(bl_pack2_bf16(v[0], v[1]), bl_pack2_bf16(v[2], v[3]), bl_pack2_bf16(v[4], v[5]), bl_pack2_bf16(v[6], v[7])),
+                make_uint4(bl_pack2_bf16(v[8], v[9]), bl_pack2_bf16(v[10], v[11]), bl_pack2_bf16(v[12], v[13]), bl_pack2_bf16(v[14], v[15])));
+}
+/* Longer rows: a workgroup a row.  Zeros behind K in the last block. */
 __global__ __launch_bounds__(256) void bl_f8_rows(f8_args A, bl_prod_dev P) {
     __shared__ double s4[4];
     const int m = (int)blockIdx.x, tid = threadIdx.x, groups = A.K / 16, all = A.nb * 8;
     uint4 xv[4];
     float rn = 0.0f;
     if (P.norm) rn = bl_norm_produce2(P, m, A.K, true, s4, xv);
-    uint8_t* to = A.codes + (int64_t)m * all * 16;
-    auto unit = [&](int u, uint4 lo, uint4 hi) {
-        float g = f8_largest16(lo, hi);
-        g = bl_max_pos(g, bl_dppf<BL_DPP_QUAD_XOR1>(g));
-        g = bl_max_pos(g, bl_dppf<BL_DPP_QUAD_XOR2>(g));
-        g = bl_max_pos(g, bl_dppf<BL_DPP_ROW_HALF_MIRROR>(g));
-        const float s = f8_scale(g);
-        *(bl_v4i*)(to + (int64_t)u * 16) = f8_codes16(lo, hi, bl_div_rn(1.0f, s));
-        if ((u & 7) == 0) A.scales[(int64_t)(u >> 3) * A.M + m] = s;
-    };
     const uint4 zero = make_uint4(0, 0, 0, 0);
     if (P.norm) {
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
             const int u = tid + 256 * j;
-            if (u < all) unit(u, u < groups ? xv[2 * j] : zero, u < groups ? xv[2 * j + 1] : zero);
+            if (u < all) f8_put_unit(A, m, u, u < groups ? xv[2 * j] : zero, u < groups ? xv[2 * j + 1] : zero);
         }
     }
     for (int u = tid + (P.norm ? 512 : 0); u < all; u += 256) {
         uint4 lo = zero, hi = zero;
         if (u < groups) bl_produce16<true>(P, m, u, A.K, !P.norm, rn, lo, hi);
-        unit(u, lo, hi);
+        f8_put_unit(A, m, u, lo, hi);
     }
 }
 
@@ -120,24 +151,20 @@ __global__ __launch_bounds__(256) void bl_f8_units(f8_args A, bl_prod_dev P) {
     const int m = (int)(i / all), u = (int)(i - (int64_t)m * all);
     uint4 lo = make_uint4(0, 0, 0, 0), hi = lo;
     if (u < groups) bl_produce16<false>(P, m, u, A.K, true, 0.0f, lo, hi);
-    float g = f8_largest16(lo, hi);
-    g = bl_max_pos(g, bl_dppf<BL_DPP_QUAD_XOR1>(g));
-    g = bl_max_pos(g, bl_dppf<BL_DPP_QUAD_XOR2>(g));
-    g = bl_max_pos(g, bl_dppf<BL_DPP_ROW_HALF_MIRROR>(g));
-    const float s = f8_scale(g);
-    *(bl_v4i*)(A.codes + i * 16) = f8_codes16(lo, hi, bl_div_rn(1.0f, s));
-    if ((u & 7) == 0) A.scales[(int64_t)(u >> 3) * A.M + m] = s;
+    f8_put_unit(A, m, u, lo, hi);
 }
 
 /* ---- output -------------------------------------------------------------------------------------------------------------- */
 
 __device__ __forceinline__ uint16_t f8_bf16(float v) { return (uint16_t)bl_pack2_bf16(v, v); }
-/* Four consecutive outputs n .. n + 3 of row m. */
+/* Four consecutive outputs n .. n + 3 of row m: one store, whatever the row's alignment (the memory takes vectors at any element). */
+typedef uint32_t f8_out2 __attribute__((ext_vector_type(2), aligned(2)));
+typedef float f8_out4 __attribute__((ext_vector_type(4), aligned(4)));
 __device__ __forceinline__ void f8_store4(const f8_args& A, int m, int n, const float (&v)[4]) {
     const int64_t at = (int64_t)m * A.y_stride + n;
-    if (A.wide && n + 4 <= A.N) {
-        if (A.bf16) *bl_g((bl_v2u*)((uint16_t*)A.y + at)) = (bl_v2u){bl_pack2_bf16(v[0], v[1]), bl_pack2_bf16(v[2], v[3])};
-        else *bl_g((bl_v4f*)((float*)A.y + at)) = (bl_v4f){v[0], v[1], v[2], v[3]};
+    if (n + 4 <= A.N) {
+        if (A.bf16) *bl_g((f8_out2*)((uint16_t*)A.y + at)) = (f8_out2){bl_pack2_bf16(v[0], v[1]), bl_pack2_bf16(v[2], v[3])};
+        else *bl_g((f8_out4*)((float*)A.y + at)) = (f8_out4){v[0], v[1], v[2], v[3]};
     } else {
         for (int i = 0; i < 4 && n + i < A.N; ++i) {
             if (A.bf16) ((uint16_t*)A.y)[at + i] = f8_bf16(v[i]);
@@ -680,10 +707,11 @@ extern "C" bl_status bl_f8_linear(const bl_f8_product* p, bl_stream s) {
     A.w = p->w.codes, A.ws = p->w.scale, A.w_stride = p->w.stride, A.ws_stride = p->w.scale_stride;
     A.codes = (uint8_t*)p->workspace, A.scales = (float*)(A.codes + q.codes), A.part = (float*)(A.codes + q.codes + q.scales);
     A.y = p->y, A.y_stride = p->y_stride, A.M = (int)p->M, A.N = (int)p->w.N, A.K = (int)p->w.K, A.nb = (A.K + F8_BLOCK - 1) / F8_BLOCK;
-    A.bf16 = p->y_kind == BL_F8_OUT_BF16, A.wide = bl_aligned(p->y, 16) && p->y_stride % (A.bf16 ? 8 : 4) == 0, A.splits = q.splits;
+    A.bf16 = p->y_kind == BL_F8_OUT_BF16, A.splits = q.splits;
     const hipStream_t st = (hipStream_t)s;
     const int64_t units = ((int64_t)A.M * A.nb * 8 + 255) / 256;
-    if (!q.fused && (prod.norm || units > 0x7fffffff)) bl_f8_rows<<<(unsigned)A.M, 256, 0, st>>>(A, prod);
+    if (!q.fused && prod.norm && A.K <= 1024) bl_f8_wave_rows<<<(unsigned)((A.M + 3) / 4), 256, 0, st>>>(A, prod);
+    else if (!q.fused && (prod.norm || units > 0x7fffffff)) bl_f8_rows<<<(unsigned)A.M, 256, 0, st>>>(A, prod);
     else if (!q.fused) bl_f8_units<<<(unsigned)units, 256, 0, st>>>(A, prod);
     if (q.tokens) return f8_stream_launch(A, prod, q, st);
     const bl_status rc = q.small ? f8_tile_launch<64, 64, 2, 2, 2>(A, st) : f8_tile_launch<128, 128, 2, 2, 2>(A, st);
