@@ -564,9 +564,10 @@ enum { BL_F8_OUT_F32 = 0, BL_F8_OUT_BF16 = 1 };
  *   operation, ties to even;
  *   y[m][n] = sum over the groups b of (s[m][b] * scale[n / 128][b]) * sum_k code[m][k] * codes[n][k], in fp32, then to the output's type.
  * A row with a NaN or an infinity in it is NaN.
- *   y          fp32 or bf16 [M][N], rows y_stride values apart (16-byte aligned rows are faster)
+ *   y          fp32 or bf16 [M][N], rows y_stride values apart, aligned to its type
  *   workspace  bl_f8_workspace_bytes(p) bytes, 256-byte aligned; no content is expected
- * M, N, K <= 2^24 and (M / 128) * (N / 128) * 16 < 2^31, both rounded up. */
+ * y, the workspace and a producer's aux_out share no byte with each other or with what is read (BL_ERR_VALUE): a sum is not stored in place.
+ * M < 2^24, N and K <= 2^24, and (M / 128) * (N / 128) < 2^24, both rounded up. */
 typedef struct {
     bl_f8_matrix w;
     bl_producer prod;

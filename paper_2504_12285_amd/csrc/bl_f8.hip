@@ -90,38 +90,7 @@ __device__ __forceinline__ void f8_put_unit(const f8_args& A, int m, int u, cons
     *(bl_v4i*)(A.codes + ((int64_t)m * A.nb * 8 + u) * 16) = f8_codes16(lo, hi, bl_div_rn(1.0f, s));
     if ((u & 7) == 0) A.scales[(int64_t)(u >> 3) * A.M + m] = s;
 }
-/* Normed rows of up to 1024 values: a wave a row, which is read once and meets nobody (803 rows of 256 values: a workgroup a row 22 us, so 5). */
-__global__ __launch_bounds__(256) void bl_f8_wave_rows(f8_args A, bl_prod_dev P) {
-    const int m = (int)blockIdx.x * 4 + (threadIdx.x >> 6), u = threadIdx.x & 63, groups = A.K / 16;
-    if (m >= A.M) return;
-    float v[16];
-#pragma unroll
-    for (int e = 0; e < 16; ++e) v[e] = 0.0f;
-    double ss = 0.0;
-    if (u < groups) {
-        bl_produce16_f32(P, m, u, A.K, true, v);
-#pragma unroll
-        for (int e = 0; e < 16; ++e) ss += (double)v[e] * (double)v[e];
-    }
-#pragma unroll
-    for (int x = 1; x < 64; x <<= 1) ss += __shfl_xor(ss, x);
-    const float rn = (float)(1.0 / sqrt(ss / (double)A.K + (double)P.eps));
-    if (u >= A.nb * 8) return;                                /* (groups of eight lanes, whole ones) */
-    if (u < groups) {                                         /* (a row that is NaN: not its padding) */
-#pragma unroll
-        for (int e = 0; e < 16; ++e) v[e] *= rn;
-        if (P.gain) {
-#pragma unroll
-            for (int e = 0; e < 16; e += 4) {
-                const bl_v4f x = *bl_gc<bl_v4f>(P.gain + (int64_t)u * 16 + e);
-                v[e] *= x[0], v[e + 1] *= x[1], v[e + 2] *= x[2], v[e + 3] *= x[3];
-            }
-        }
-    }
-    f8_put_unit(A, m, u, make_uint4(bl_pack2_bf16(v[0], v[1]), bl_pack2_bf16(v[2], v[3]), bl_pack2_bf16(v[4], v[5]), bl_pack2_bf16(v[6], v[7])),
-                make_uint4(bl_pack2_bf16(v[8], v[9]), bl_pack2_bf16(v[10], v[11]), bl_pack2_bf16(v[12], v[13]), bl_pack2_bf16(v[14], v[15])));
-}
-/* Longer rows: a workgroup a row.  Zeros behind K in the last block. */
+/* A workgroup a row, whose norm meets in it.  Zeros behind K in the last block. */
 __global__ __launch_bounds__(256) void bl_f8_rows(f8_args A, bl_prod_dev P) {
     __shared__ double s4[4];
     const int m = (int)blockIdx.x, tid = threadIdx.x, groups = A.K / 16, all = A.nb * 8;
@@ -645,12 +614,35 @@ static bl_status f8_check_product(const bl_f8_product* p, bl_prod_dev* prod) {
     if (const bl_status rc = f8_check(&p->w)) return rc;
     if (!p->y || !p->prod.in0) return BL_ERR_NULL;
     if (p->y_kind != BL_F8_OUT_F32 && p->y_kind != BL_F8_OUT_BF16) return BL_ERR_VALUE;
-    if (p->M < 1 || p->M > BL_MAX_DIM || p->y_stride < p->w.N || p->y_stride > ((int64_t)1 << 40)) return BL_ERR_SHAPE;
+    if (p->M < 1 || p->M >= BL_MAX_DIM || p->y_stride < p->w.N || p->y_stride > ((int64_t)1 << 40)) return BL_ERR_SHAPE;
     if (!bl_aligned(p->y, p->y_kind == BL_F8_OUT_F32 ? 4 : 2)) return BL_ERR_ALIGN;
     if (!bl_make_prod(p->prod, nullptr, p->w.K, prod)) return BL_ERR_VALUE;
-    /* (tiles are counted in 32 bits) */
-    if (((p->M + 127) / 128) * ((p->w.N + 127) / 128) * 16 > 0x7fffffff) return BL_ERR_SHAPE;
+    /* (a launch counts its threads in 32 bits) */
+    if (((p->M + 127) / 128) * ((p->w.N + 127) / 128) >= 1 << 24) return BL_ERR_SHAPE;
     return BL_OK;
+}
+
+/* What is written may not be what is read: several workgroups make the same rows where the stream makes them, and long normed rows are made twice. */
+struct f8_range {
+    uintptr_t at;
+    uint64_t bytes;
+};
+static bool f8_meet(const f8_range& a, const f8_range& b) { return a.at && b.at && a.at < b.at + b.bytes && b.at < a.at + a.bytes; }
+static bool f8_overlap(const bl_f8_product* p, const f8_plan& q) {
+    const uint64_t MK = (uint64_t)p->M * (uint64_t)p->w.K;
+    const int kind = p->prod.kind;
+    const bool sum = kind == BL_PROD_RESIDUAL;
+    const uint64_t row = (uint64_t)(p->prod.n_q + 2 * (int64_t)p->prod.n_kv) * p->prod.head_dim;
+    const f8_range y = {(uintptr_t)p->y, ((uint64_t)(p->M - 1) * p->y_stride + p->w.N) * (p->y_kind == BL_F8_OUT_BF16 ? 2 : 4)};
+    const f8_range aux = {sum ? (uintptr_t)p->prod.aux_out : 0, MK * 4}, space = {q.bytes ? (uintptr_t)p->workspace : 0, q.bytes};
+    const f8_range in[] = {{(uintptr_t)p->prod.in0, kind == BL_PROD_BF16 ? MK * 2 : kind == BL_PROD_ATTN_V ? p->M * row * 4 : kind == BL_PROD_RELU2_GATE ? MK * 8 : MK * 4},
+                           {sum ? (uintptr_t)p->prod.in1 : 0, MK * 4},
+                           {p->prod.norm ? (uintptr_t)p->prod.gain : 0, (uint64_t)p->w.K * 4},
+                           {(uintptr_t)p->w.codes, (uint64_t)(p->w.N - 1) * p->w.stride + p->w.K},
+                           {(uintptr_t)p->w.scale, ((uint64_t)((p->w.N + 127) / 128 - 1) * p->w.scale_stride + (p->w.K + 127) / 128) * 4}};
+    for (const f8_range& x : in)
+        if (f8_meet(x, y) || f8_meet(x, aux) || f8_meet(x, space)) return true;
+    return f8_meet(y, aux) || f8_meet(y, space) || f8_meet(aux, space);
 }
 
 extern "C" size_t bl_f8_workspace_bytes(const bl_f8_product* p) {
@@ -703,6 +695,7 @@ extern "C" bl_status bl_f8_linear(const bl_f8_product* p, bl_stream s) {
     const f8_plan q = f8_make_plan(p);
     if (q.bytes && !p->workspace) return BL_ERR_WORKSPACE;
     if (!bl_aligned(p->workspace, 256)) return BL_ERR_ALIGN;
+    if (f8_overlap(p, q)) return BL_ERR_VALUE;
     f8_args A = {};
     A.w = p->w.codes, A.ws = p->w.scale, A.w_stride = p->w.stride, A.ws_stride = p->w.scale_stride;
     A.codes = (uint8_t*)p->workspace, A.scales = (float*)(A.codes + q.codes), A.part = (float*)(A.codes + q.codes + q.scales);
@@ -710,8 +703,7 @@ extern "C" bl_status bl_f8_linear(const bl_f8_product* p, bl_stream s) {
     A.bf16 = p->y_kind == BL_F8_OUT_BF16, A.splits = q.splits;
     const hipStream_t st = (hipStream_t)s;
     const int64_t units = ((int64_t)A.M * A.nb * 8 + 255) / 256;
-    if (!q.fused && prod.norm && A.K <= 1024) bl_f8_wave_rows<<<(unsigned)((A.M + 3) / 4), 256, 0, st>>>(A, prod);
-    else if (!q.fused && (prod.norm || units > 0x7fffffff)) bl_f8_rows<<<(unsigned)A.M, 256, 0, st>>>(A, prod);
+    if (!q.fused && (prod.norm || units >= 1 << 24)) bl_f8_rows<<<(unsigned)A.M, 256, 0, st>>>(A, prod);
     else if (!q.fused) bl_f8_units<<<(unsigned)units, 256, 0, st>>>(A, prod);
     if (q.tokens) return f8_stream_launch(A, prod, q, st);
     const bl_status rc = q.small ? f8_tile_launch<64, 64, 2, 2, 2>(A, st) : f8_tile_launch<128, 128, 2, 2, 2>(A, st);

@@ -173,3 +173,22 @@ def test_a_producer_keeps_its_tensors():
     del p
     gc.collect()
     assert all(r() is None for r in refs)
+
+
+def test_product_refuses_to_write_what_it_reads(lib):  # noqa: F811
+    """Addresses far apart, then one of them moved into another's bytes: every pair of a written and a read one, ends included."""
+    at = {k: P + (i << 32) for i, k in enumerate(("in0", "in1", "aux", "gain", "codes", "scale", "y", "space"))}
+
+    def call(**moved):
+        a = dict(at, **moved)
+        prod = bl.Producer(kind=bl.BL_PROD_RESIDUAL, in0=a["in0"], in1=a["in1"], aux_out=a["aux"], norm=1, gain=a["gain"], eps=1e-5)
+        return lib.bl_f8_linear(ctypes.byref(product(matrix(codes=a["codes"], scale=a["scale"], K=192), prod, M=300, y=a["y"], workspace=a["space"])), None)
+
+    length = dict(in0=300 * 192 * 4, in1=300 * 192 * 4, aux=300 * 192 * 4, gain=192 * 4, codes=200 * 192, scale=16, y=300 * 200 * 4)
+    for out in ("aux", "y", "space"):
+        for other in at:
+            if other == out or other == "space":
+                continue
+            assert call(**{out: at[other]}) == VALUE, (out, other)
+            last = at[other] + length[other] - 1
+            assert call(**{out: last - last % 256}) == VALUE or last - last % 256 < at[other], (out, other)
