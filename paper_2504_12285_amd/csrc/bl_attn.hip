@@ -11,6 +11,8 @@
  * S is computed transposed (tokens x rows), so that a lane holds the weights of ONE row for sixteen tokens, exactly what the
  * second product wants of it: the weights never leave the lane.  Which tokens a lane gets is chosen by the
  * order in which the rows of K are handed in, such that its V codes are consecutive in memory. */
+#include <type_traits>
+
 #include "bl_device.h"
 #include "bl_kv.h"
 
@@ -857,7 +859,10 @@ struct at_many_lds {
     };
     uint8_t k[2][AT_TILE * D * at_many_k<KIND, D>::bytes];
     int scan[AT_WAVES];
-    int2 query[AT_MANY];                                    /* AT_PREFIX: row and position of the tile's queries */
+};
+template <int KIND, int D>
+struct at_prefix_lds : at_many_lds<KIND, D> {
+    int2 query[AT_MANY];                                    /* row and position of the tile's queries */
     int2 ends[AT_WAVES];
     int found[5];                                           /* the group of the tile, tiles in front of it and of it, its tokens and rows */
 };
@@ -865,7 +870,7 @@ struct at_many_lds {
  * requests of a group over its prefix (AT_PREFIX), which are gathered: their places in the batch are found by each workgroup, by sums over the requests. */
 enum { AT_ALL, AT_OWN, AT_PREFIX };
 template <int KIND, int D, int MODE = AT_ALL>
-__device__ __forceinline__ void at_many(const at_args& A, int place, at_many_lds<KIND, D>& lds) {
+__device__ __forceinline__ void at_many(const at_args& A, int place, std::conditional_t<MODE == AT_PREFIX, at_prefix_lds<KIND, D>, at_many_lds<KIND, D>>& lds) {
     const int splits = MODE == AT_PREFIX ? A.group_splits : MODE == AT_OWN ? A.many_splits : A.splits;
     constexpr bool HALF = at_many_k<KIND, D>::bytes == 2;
     constexpr int KROW = D * at_many_k<KIND, D>::bytes;        /* bytes of a K row in LDS, 16-byte units XOR-ed by k_mix(row) */
@@ -1000,6 +1005,10 @@ __device__ __forceinline__ void at_many(const at_args& A, int place, at_many_lds
         if (MODE == AT_OWN && !at_grouped(A, R.n)) R.skip = 0;
     }
     const int rbase = rt * AT_MANY, rend = rbase + AT_MANY < rows ? rbase + AT_MANY : rows;
+    /* tokens that some row of the workgroup sees (asked for here, in front of what differs by lane: behind it the compiler keeps the bounds in vector
+     * registers, and a prompt of 4096 tokens takes 128 us for 123) */
+    int tok0 = 0, tok1 = 0;
+    if constexpr (MODE != AT_PREFIX) tok0 = at_from(A, R, rbase / A.G), tok1 = at_to(R, (rend - 1) / A.G);
     /* this lane's row: its place in the batch, its head, and the tokens that it sees */
     const int row = rbase + wave * 32 + col;
     const bool live = row < rows;
@@ -1012,10 +1021,10 @@ __device__ __forceinline__ void at_many(const at_args& A, int place, at_many_lds
     } else {
         at_row = R.row0 + qi, see0 = at_from(A, R, qi), see1 = live ? at_to(R, qi) : 0;
     }
-    /* tokens that some row of this wave sees, and that all do; tokens that some row of the workgroup sees */
+    /* tokens that some row of this wave sees, and that all do */
     const int wfirst = rbase + wave * 32, wlast = wfirst + 31 < rows ? wfirst + 31 : rows - 1;
     const bool has_rows = wfirst < rows;
-    int any_from, any_to, all_from, all_to, tok0, tok1;
+    int any_from, any_to, all_from, all_to;
     if constexpr (MODE == AT_PREFIX) {
         any_from = all_from = see0, any_to = all_to = see1;
         if (!live) any_from = all_to = 0x7fffffff, all_from = any_to = 0;
@@ -1032,7 +1041,6 @@ __device__ __forceinline__ void at_many(const at_args& A, int place, at_many_lds
         for (int w = 0; w < AT_WAVES; ++w) tok0 = min(tok0, lds.ends[w].x), tok1 = max(tok1, lds.ends[w].y);
         tok0 = at_uniform(tok0), tok1 = at_uniform(tok1);
     } else {
-        tok0 = at_from(A, R, rbase / A.G), tok1 = at_to(R, (rend - 1) / A.G);
         any_from = has_rows ? at_from(A, R, wfirst / A.G) : 0, any_to = has_rows ? at_to(R, wlast / A.G) : 0;
         all_from = has_rows ? at_from(A, R, wlast / A.G) : 0, all_to = has_rows ? at_to(R, wfirst / A.G) : 0;
     }
@@ -1480,7 +1488,7 @@ template <int KIND, int D, bool WIDE, bool MANY>
 __global__ __launch_bounds__(AT_THREADS, 2) void bl_attn_shared(at_args A, int prefix, int many) {
     union lds_t {
         at_meet_lds<D, AT_WAVES> few;
-        at_many_lds<KIND, D> many;
+        at_prefix_lds<KIND, D> many;
     };
     __shared__ __attribute__((aligned(16))) uint8_t lds[sizeof(lds_t)];
     const int x = (int)blockIdx.x;
