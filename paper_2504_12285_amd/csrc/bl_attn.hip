@@ -59,8 +59,11 @@ struct at_args {
     const int* shared_blocks;
     const int* shared_table;
     int64_t shared_stride;
-    int2* pieces;                  /* [T] of each row: partial results of its group's prefix, and of its own tokens (none of both: it is done; -1: no numbers) */
-    int n_groups, max_shared, group_splits, few_splits, many_splits;
+    int2* pieces;                  /* [T] of each row: at_pieces, and at_query */
+    float* part_ml;                /* reference and sum of each partial result */
+    int64_t part_stride, own_at;   /* results a piece of a prefix or of at_few's has, and in front of those of at_many's own pieces */
+    int n_groups, max_shared, group_splits, few_splits, many_splits, by_request;
+    int apart;                     /* rows of a request and kv head from which it is no part of its group */
 };
 
 /* ---- what both kernels share --------------------------------------------------------------------------------------- */
@@ -73,8 +76,6 @@ struct at_request {
     int row0, n, len;
     int skip = 0;                  /* tokens in front that its group has */
 };
-/* Rows of a request and kv head from which it is no part of its group: they fill tiles of at_many by themselves, which read the prefix from the caches then. */
-#define AT_APART AT_MANY
 __device__ __forceinline__ at_request at_read(const at_args& A, int b) {
     at_request r;
     const int a = A.q_start[b], e = A.q_start[b + 1];
@@ -91,7 +92,7 @@ __device__ __forceinline__ int at_shared_tokens(const at_args& A, int g) {
     const int s = A.shared_blocks[g];
     return (s < 0 ? 0 : s > A.max_shared ? A.max_shared : s) << A.shift;
 }
-__device__ __forceinline__ bool at_grouped(const at_args& A, int n) { return n * A.G < AT_APART; }
+__device__ __forceinline__ bool at_grouped(const at_args& A, int n) { return n * A.G < A.apart; }
 template <bool SHARED>
 __device__ __forceinline__ at_request at_read_own(const at_args& A, int b) {
     at_request r = at_read(A, b);
@@ -260,8 +261,18 @@ __device__ __forceinline__ int at_piece_count(int tiles, int splits) {
     const int each = at_piece(tiles, splits);
     return each ? (tiles + each - 1) / each : 0;
 }
-/* Where piece `piece` of (row, head) stands among the partial results: at * D values, and at * 2 for its reference and sum behind all of these. */
-__device__ __forceinline__ int64_t at_part_at(const at_args& A, int piece, int row, int head) { return ((int64_t)piece * A.T + row) * A.n_q + head; }
+/* A row's partial results: `prefix` of its group's prefix and `own` of its own tokens, whose sum is its output where there are any (0: it is done); many: the
+ * own ones are at_many's.  AT_NO_NUMBERS: more queries than the launch was made for. */
+#define AT_NO_NUMBERS -1
+__device__ __forceinline__ int at_pieces(int prefix, int own, bool many) { return prefix | own << 8 | (many ? 1 << 16 : 0); }
+/* Query i of request b, where partial results stand by requests: fewer than `apart` rows of each have some, however many a prompt beside them brings (one of
+ * 8192 beside seven decoding requests: 0.1 GB for 3.9 by rows of the batch). */
+__device__ __forceinline__ int at_query(const at_args& A, int b, int i) { return b * A.apart + i; }
+/* Where the first piece of (row, head) stands among the partial results. */
+__device__ __forceinline__ int64_t at_part_at(const at_args& A, int query, int row, int head) {
+    if (!A.by_request) return (int64_t)row * A.n_q + head;
+    return ((int64_t)(query / A.apart) * A.n_kv + head / A.G) * A.apart + query % A.apart * A.G + head % A.G;
+}
 /* Tiles a wave does, of `all` in the launch. */
 __device__ __forceinline__ int at_share(int all) {
     const int s = (all + AT_STREAMS - 1) / AT_STREAMS;
@@ -358,7 +369,7 @@ __device__ __forceinline__ void at_few(const at_args& A, int group, uint8_t* lds
         if (!cur.c) {
             if (SHARED) {
                 if (ALONE && piece == 0 && cur.h == 0)
-                    for (int i = tid; i < mine.n; i += AT_THREADS) A.pieces[mine.row0 + i] = make_int2(-1, -1);
+                    for (int i = tid; i < mine.n; i += AT_THREADS) A.pieces[mine.row0 + i] = make_int2(AT_NO_NUMBERS, 0);
             } else if (ALONE) {
                 at_no_rows<D>(A, mine, cur.h, tid, WAVES * BL_WAVE);
             }
@@ -369,7 +380,7 @@ __device__ __forceinline__ void at_few(const at_args& A, int group, uint8_t* lds
             const int each = at_piece(cur.c, A.few_splits), all = cur.c, n = at_piece_count(all, A.few_splits);
             whole_item = mine.skip == 0 && n == 1;
             if (piece == 0 && cur.h == 0 && tid < mine.n)
-                A.pieces[mine.row0 + tid] = whole_item ? make_int2(0, 0) : make_int2(at_piece_count((mine.skip + AT_TILE - 1) / AT_TILE, A.group_splits), n);
+                A.pieces[mine.row0 + tid] = make_int2(whole_item ? 0 : at_pieces(at_piece_count((mine.skip + AT_TILE - 1) / AT_TILE, A.group_splits), n, false), at_query(A, cur.b, tid));
             cur.tile0 += piece * each;
             cur.c = all - piece * each < each ? all - piece * each : each;
             if (cur.c <= 0) return;
@@ -679,11 +690,11 @@ __device__ __forceinline__ void at_few(const at_args& A, int group, uint8_t* lds
         for (int j = 0; j < PER; ++j) y[j] += meet.o[w][r][d0 + j] * f;
     }
     if (SHARED && !whole_item) {
-        const int64_t at = at_part_at(A, A.group_splits + piece, R.row0 + r / A.G, cur.h * A.G + r % A.G);
+        const int64_t at = (A.group_splits + piece) * A.part_stride + at_part_at(A, at_query(A, cur.b, r / A.G), R.row0 + r / A.G, cur.h * A.G + r % A.G);
         float* to = A.many_part + at * D + d0;
 #pragma unroll
         for (int j = 0; j < PER; j += 4) *bl_g((bl_v4f*)(to + j)) = (bl_v4f){y[j], y[j + 1], y[j + 2], y[j + 3]};
-        if (d0 == 0) *bl_g((bl_v2f*)(A.many_part + (int64_t)A.splits * A.T * A.n_q * D + 2 * at)) = (bl_v2f){top, sum};
+        if (d0 == 0) *bl_g((bl_v2f*)(A.part_ml + 2 * at)) = (bl_v2f){top, sum};
     } else if (ITEM || alone) {                              /* (SHARED: nobody else has a part of it) */
         const float inv = sum == 0.0f ? 0.0f : bl_div_rn(1.0f, sum);
         uint32_t* to = (uint32_t*)(A.out + (R.row0 + r / A.G) * A.out_stride + (cur.h * A.G + r % A.G) * D + d0);
@@ -862,7 +873,8 @@ struct at_many_lds {
 };
 template <int KIND, int D>
 struct at_prefix_lds : at_many_lds<KIND, D> {
-    int2 query[AT_MANY];                                    /* row and position of the tile's queries */
+    int2 query[AT_MANY];                                    /* row and position of the tile's queries, */
+    int slot[AT_MANY];                                      /* and at_query */
     int2 ends[AT_WAVES];
     int found[5];                                           /* the group of the tile, tiles in front of it and of it, its tokens and rows */
 };
@@ -896,8 +908,9 @@ __device__ __forceinline__ void at_many(const at_args& A, int place, std::condit
         int* s_upto = lds.upto;
         /* Which group has this tile, and the batch rows of the tile's queries: sums over the groups, then over the requests.  A thread has one of each where there
          * are no more than threads, so that all of it hangs on one round of loads. */
-        auto queries = [&](int q0, int q1, int begin, int end, int row0, int len) {
-            for (int j = begin > q0 ? begin : q0; j < (end < q1 ? end : q1); ++j) lds.query[j - q0] = make_int2(row0 + j - begin, len - (end - begin) + j - begin);
+        auto queries = [&](int q0, int q1, int begin, int end, int request, int row0, int len) {
+            for (int j = begin > q0 ? begin : q0; j < (end < q1 ? end : q1); ++j)
+                lds.query[j - q0] = make_int2(row0 + j - begin, len - (end - begin) + j - begin), lds.slot[j - q0] = at_query(A, request, j - begin);
         };
         auto range = [&](int& q0, int& q1) {
             rt = c - 1 - (want - before);
@@ -934,7 +947,7 @@ __device__ __forceinline__ void at_many(const at_args& A, int place, std::condit
             int q0, q1;
             range(q0, q1);
             const int n = group == b ? r.n : 0, end = sums(n, &all);
-            if (n) queries(q0, q1, end - n, end, r.row0, r.len);
+            if (n) queries(q0, q1, end - n, end, tid, r.row0, r.len);
             __syncthreads();
         } else {
             auto news = [&](int i) {
@@ -969,7 +982,7 @@ __device__ __forceinline__ void at_many(const at_args& A, int place, std::condit
                 const int end = s_upto[i], begin = i ? s_upto[i - 1] : 0;
                 if (end <= q0 || begin >= q1 || end == begin) continue;
                 const at_request r = at_read(A, i);
-                queries(q0, q1, begin, end, r.row0, r.len);
+                queries(q0, q1, begin, end, i, r.row0, r.len);
             }
             __syncthreads();
         }
@@ -1013,9 +1026,10 @@ __device__ __forceinline__ void at_many(const at_args& A, int place, std::condit
     const int row = rbase + wave * 32 + col;
     const bool live = row < rows;
     const int qi = live ? row / A.G : 0, qh_i = h * A.G + (live ? row % A.G : 0);
-    int at_row, see0, see1;
+    int at_row, see0, see1, slot = 0;
     if constexpr (MODE == AT_PREFIX) {
         const int2 q = lds.query[live ? qi - rbase / A.G : 0];
+        slot = lds.slot[live ? qi - rbase / A.G : 0];
         const int from = A.window ? q.y - A.window + 1 : 0;
         at_row = q.x, see0 = from > 0 ? from : 0, see1 = !live || q.y < 0 ? 0 : q.y + 1 < R.len ? q.y + 1 : R.len;
     } else {
@@ -1343,7 +1357,7 @@ __device__ __forceinline__ void at_many(const at_args& A, int place, std::condit
     if (!live) return;
     const bool whole_rows = MODE == AT_ALL ? A.splits == 1 : MODE == AT_OWN && R.skip == 0 && splits == 1;
     if (MODE == AT_OWN && h == 0 && piece == 0 && half == 0 && row % A.G == 0)
-        A.pieces[at_row] = whole_rows ? make_int2(0, 0) : make_int2(at_piece_count((R.skip + AT_TILE - 1) / AT_TILE, A.group_splits), splits);
+        A.pieces[at_row] = make_int2(whole_rows ? 0 : at_pieces(at_piece_count((R.skip + AT_TILE - 1) / AT_TILE, A.group_splits), splits, true), R.skip ? at_query(A, b, qi) : 0);
     if (whole_rows) {
         const float inv = l == 0.0f ? 0.0f : bl_div_rn(1.0f, l);
         uint16_t* to = A.out + at_row * A.out_stride + qh_i * D;
@@ -1355,14 +1369,15 @@ __device__ __forceinline__ void at_many(const at_args& A, int place, std::condit
                 *bl_g((bl_v2u*)(to + 32 * i + 2 * j + 4 * half)) = u;
             }
     } else {
-        const int64_t at = at_part_at(A, MODE == AT_OWN ? A.group_splits + piece : piece, at_row, qh_i);
+        const int64_t at = MODE == AT_PREFIX ? piece * A.part_stride + at_part_at(A, slot, at_row, qh_i)
+                                             : (MODE == AT_OWN ? A.own_at : 0) + ((int64_t)piece * A.T + at_row) * A.n_q + qh_i;
         float* to = A.many_part + at * D;
 #pragma unroll
         for (int i = 0; i < DT; ++i)
 #pragma unroll
             for (int j = 0; j < 16; j += 4) *bl_g((bl_v4f*)(to + 32 * i + 2 * j + 4 * half)) = (bl_v4f){o[i][j], o[i][j + 1], o[i][j + 2], o[i][j + 3]};
         if (half == 0) {
-            float* ml = A.many_part + (int64_t)A.splits * A.T * A.n_q * D + 2 * at;
+            float* ml = (MODE == AT_ALL ? A.many_part + (int64_t)A.splits * A.T * A.n_q * D : A.part_ml) + 2 * at;
             ml[0] = m, ml[1] = l;
         }
     }
@@ -1411,7 +1426,7 @@ __device__ __forceinline__ void at_many_join(const at_args& A, int group) {
     *bl_g((bl_v2u*)(A.out + row * A.out_stride + (at % A.n_q) * D + d0)) = u;
 }
 
-/* The same for rows of requests that share prefixes: pieces 0 .. of the prefix and group_splits .. of the rest, as many as the row's entry says.  LANES groups of
+/* The same for rows of requests that share prefixes: the pieces of the prefix and those of the rest, as many as the row's entry says.  LANES groups of
  * D / 4 threads share a row's pieces and meet in LDS. */
 template <int D, int LANES>
 __global__ __launch_bounds__(AT_THREADS) void bl_attn_shared_join(at_args A) {
@@ -1421,11 +1436,14 @@ __global__ __launch_bounds__(AT_THREADS) void bl_attn_shared_join(at_args A) {
     const int group = threadIdx.x / TPR, part = group / ROWS;               /* (a wave's groups have other rows: their loads are of neighbours) */
     const int64_t at = (int64_t)blockIdx.x * ROWS + group % ROWS, all = (int64_t)A.T * A.n_q;
     const int row = (int)(at / A.n_q), d0 = (threadIdx.x % TPR) * 4;
-    int2 n = {0, 0};
-    if (at < all && row >= A.q_start[0] && row < A.q_start[A.B]) n = A.pieces[row];
-    n.x = min(n.x, A.group_splits), n.y = min(n.y, A.splits - A.group_splits);       /* (first rows that do not ascend lead to no place outside) */
-    const float* ml = A.many_part + A.splits * all * D;
-    const int count = max(n.x, 0) + max(n.y, 0);
+    int2 entry = {0, 0};
+    if (at < all && row >= A.q_start[0] && row < A.q_start[A.B]) entry = A.pieces[row];
+    /* (first rows that do not ascend leave entries unwritten: no content of them leads outside) */
+    const bool none = entry.x == AT_NO_NUMBERS, many = entry.x >> 16 & 1;
+    const int prefix = none ? 0 : min(entry.x & 255, A.G < A.apart ? A.group_splits : 0), own = none ? 0 : min(entry.x >> 8 & 255, many ? A.many_splits : A.few_splits), count = prefix + own;
+    const int slot = (unsigned)entry.y < (unsigned)(A.B * A.apart) && (entry.y % A.apart + 1) * A.G <= A.apart ? entry.y : 0;
+    const int64_t first = at_part_at(A, slot, row, (int)(at % A.n_q)), step = many ? all : A.part_stride;
+    const int64_t first_own = (many ? A.own_at + at : A.group_splits * A.part_stride + first) - prefix * step;
     at_sum s = {-INFINITY, 0.0f, {0, 0, 0, 0}};
     for (int i = part; i < count; i += IN * LANES) {
         at_sum x[IN];
@@ -1434,8 +1452,8 @@ __global__ __launch_bounds__(AT_THREADS) void bl_attn_shared_join(at_args A) {
             x[u] = {-INFINITY, 0.0f, {0, 0, 0, 0}};
             const int p = i + u * LANES;
             if (p < count) {
-                const int64_t from = (p < n.x ? p : A.group_splits + p - n.x) * all + at;
-                const bl_v2f t = *bl_gc<bl_v2f>(ml + 2 * from);
+                const int64_t from = p < prefix ? first + p * A.part_stride : first_own + p * step;
+                const bl_v2f t = *bl_gc<bl_v2f>(A.part_ml + 2 * from);
                 x[u].m = t[0], x[u].l = t[1], x[u].y = *bl_gc<bl_v4f>(A.many_part + from * D + d0);
             }
         }
@@ -1450,10 +1468,10 @@ __global__ __launch_bounds__(AT_THREADS) void bl_attn_shared_join(at_args A) {
 #pragma unroll
         for (int j = 1; j < LANES; ++j) s = at_add(s, {s_m[j * ROWS + group], s_l[j * ROWS + group], *(const bl_v4f*)&s_y[j * ROWS + group][d0]});
     }
-    if (n.x == 0 && n.y == 0) return;                        /* of no request, or done */
+    if (count == 0 && !none) return;                          /* of no request, or done */
     const float inv = s.l == 0.0f ? 0.0f : bl_div_rn(1.0f, s.l);
     bl_v2u u = {bl_pack2_bf16(s.y[0] * inv, s.y[1] * inv), bl_pack2_bf16(s.y[2] * inv, s.y[3] * inv)};
-    if (n.y < 0) u = (bl_v2u){0x7fc07fc0u, 0x7fc07fc0u};      /* more queries than the launch was made for */
+    if (none) u = (bl_v2u){0x7fc07fc0u, 0x7fc07fc0u};         /* more queries than the launch was made for */
     *bl_g((bl_v2u*)(A.out + row * A.out_stride + (at % A.n_q) * D + d0)) = u;
 }
 
@@ -1640,8 +1658,8 @@ extern "C" bl_status bl_attn_kv8(const bl_attn_desc* a, bl_stream s) {
 
 struct at_shared_plan {
     bool few, many;
-    int group_splits, few_splits, many_splits, splits;
-    int64_t prefix_tiles, many_tiles;
+    int group_splits, few_splits, many_splits, apart;
+    int64_t prefix_tiles, many_tiles, part_stride, own_at, parts;
     size_t pieces, bytes;          /* of the rows' entries in front, and in all */
 };
 
@@ -1673,8 +1691,9 @@ static at_shared_plan at_make_shared_plan(const bl_attn_shared_desc* s) {
     const int G = a->n_q / a->cache.n_kv, D = a->cache.head_dim;
     p.many = (int64_t)(a->max_q < a->T ? a->max_q : a->T) * G > AT_FEW, p.few = G <= AT_FEW;
     const int64_t tiles = (a->T * G + AT_MANY - 1) / AT_MANY, part = a->T < a->B ? a->T : a->B, groups = s->n_groups < part ? s->n_groups : part;
-    int64_t own = s->max_own > 0 ? s->max_own : a->max_len > 0 ? a->max_len : (int64_t)a->max_blocks * a->cache.block;
+    int64_t tokens = a->max_len > 0 ? a->max_len : (int64_t)a->max_blocks * a->cache.block, own = s->max_own > 0 ? s->max_own : tokens;
     const int64_t wide = (int64_t)a->window + (a->max_q < AT_MANY ? a->max_q : AT_MANY);
+    if (a->window && tokens > wide) tokens = wide;
     if (a->window && own > wide) own = wide;
     /* Pieces of `items` items of `tokens`: until there are `fill` workgroups, of four tiles at least; fewer tiles while not every unit has a workgroup. */
     auto pieces = [](int64_t items, int64_t tokens, int64_t fill, int64_t each, int64_t most) -> int {
@@ -1682,15 +1701,22 @@ static at_shared_plan at_make_shared_plan(const bl_attn_shared_desc* s) {
         const int64_t some = 128 / items < tiles ? 128 / items : tiles, n = full > some ? full : some;
         return (int)(n < 1 ? 1 : n < most ? n : most);
     };
-    const int64_t most = a->T * G < part * (AT_APART - 1) ? a->T * G : part * (AT_APART - 1);          /* rows that groups can have */
+    /* Where a request may fill tiles of at_many by itself, which read the prefix from the caches then, all of more than AT_FEW rows are apart; else they are of
+     * their groups.  us of this and of the other, 20 + 5 heads: 8 chunks of 300 beside 16 decoding requests behind 4096 tokens 124 and 135, 4 of 300 beside 60
+     * behind 8000 110 and 127; 30 queries of each of 16 requests behind 32000 216 and 293, 20 of 24 behind 4096 59 and 68. */
+    const bool prompts = p.many && (int64_t)a->max_q * G >= AT_MANY;
+    p.apart = prompts ? AT_FEW + 1 : AT_MANY;
+    const int64_t most = a->T * G < part * (p.apart - 1) ? a->T * G : part * (p.apart - 1);            /* rows that groups can have */
     p.prefix_tiles = most / AT_MANY + groups;
     p.group_splits = pieces((most + AT_MANY - 1) / AT_MANY * a->cache.n_kv, (int64_t)s->max_shared * a->cache.block, 512, 1, 64);
     p.few_splits = p.few ? pieces(part * a->cache.n_kv, own, 512, 4, 32) : 0;
-    p.many_splits = p.many ? pieces(tiles * a->cache.n_kv, own, 512, 4, 32) : 0;
-    p.splits = p.group_splits + (p.few_splits > p.many_splits ? p.few_splits : p.many_splits);
+    /* (prompts read the prefix too: two of 600 over 32000 tokens beside 14 of one, cut by their own tokens 790 us, by all 370) */
+    p.many_splits = p.many ? pieces(tiles * a->cache.n_kv, prompts ? tokens : own, 512, 4, 32) : 0;
     p.many_tiles = p.many ? a->T * G / AT_MANY + part : 0;
     p.pieces = ((size_t)a->T * sizeof(int2) + 255) / 256 * 256;
-    p.bytes = p.pieces + (size_t)p.splits * a->T * a->n_q * (D + 2) * sizeof(float);
+    p.part_stride = p.many ? a->B * a->cache.n_kv * p.apart : a->T * a->n_q;
+    p.own_at = (p.group_splits + p.few_splits) * p.part_stride, p.parts = p.own_at + p.many_splits * a->T * a->n_q;
+    p.bytes = p.pieces + (size_t)p.parts * (D + 2) * sizeof(float);
     return p;
 }
 
@@ -1698,6 +1724,8 @@ extern "C" size_t bl_attn_shared_workspace_bytes(const bl_attn_shared_desc* a) {
     return at_check_shared(a) != BL_OK ? 0 : at_shared_apart(a) ? at_make_plan(&a->attn).bytes : at_make_shared_plan(a).bytes;
 }
 
+/* Workgroups up to which the join takes four groups of threads a row (24 requests, 80 rows: 38.6 us, with one 40.7; 1467 rows: 147.7, so 134.5). */
+#define AT_JOIN_LANES 4096
 template <int KIND, int D, bool WIDE>
 static void at_shared_launch(const at_args& A, const at_shared_plan& p, hipStream_t st) {
     const int prefix = (int)(p.prefix_tiles * A.n_kv * p.group_splits), many = (int)(p.many_tiles * A.n_kv * p.many_splits);
@@ -1705,7 +1733,7 @@ static void at_shared_launch(const at_args& A, const at_shared_plan& p, hipStrea
     if (p.many) bl_attn_shared<KIND, D, WIDE, true><<<(unsigned)(prefix + many + few), AT_THREADS, 0, st>>>(A, prefix, many);
     else bl_attn_shared<KIND, D, WIDE, false><<<(unsigned)(prefix + few), AT_THREADS, 0, st>>>(A, prefix, 0);
     const int64_t rows = (int64_t)A.T * A.n_q, per = AT_THREADS / (D / 4);
-    if (p.splits <= 4) bl_attn_shared_join<D, 1><<<(unsigned)((rows + per - 1) / per), AT_THREADS, 0, st>>>(A);
+    if (p.group_splits + (p.few_splits > p.many_splits ? p.few_splits : p.many_splits) <= 4 || rows * 4 / per > AT_JOIN_LANES) bl_attn_shared_join<D, 1><<<(unsigned)((rows + per - 1) / per), AT_THREADS, 0, st>>>(A);
     else bl_attn_shared_join<D, 4><<<(unsigned)((rows * 4 + per - 1) / per), AT_THREADS, 0, st>>>(A);
 }
 
@@ -1717,12 +1745,15 @@ extern "C" bl_status bl_attn_kv8_shared(const bl_attn_shared_desc* s, bl_stream 
     if (!a->workspace) return BL_ERR_WORKSPACE;
     if (!bl_aligned(a->workspace, 256)) return BL_ERR_ALIGN;
     const bl_kv_cache& c = a->cache;
-    if (c.n_kv * (p.prefix_tiles * p.group_splits + p.many_tiles * p.many_splits + a->B * p.few_splits) > 0x7fff0000) return BL_ERR_SHAPE;
+    /* (a launch counts its threads in 32 bits) */
+    if (c.n_kv * (p.prefix_tiles * p.group_splits + p.many_tiles * p.many_splits + a->B * p.few_splits) >= 1 << 24 || a->T * a->n_q * (c.head_dim / 4) >= (int64_t)1 << 30)
+        return BL_ERR_SHAPE;
     at_args A = at_make_args(a);
-    A.few_rows = p.few ? AT_FEW : 0, A.splits = p.splits, A.group_splits = p.group_splits, A.few_splits = p.few_splits, A.many_splits = p.many_splits;
+    A.few_rows = p.few ? AT_FEW : 0, A.group_splits = p.group_splits, A.few_splits = p.few_splits, A.many_splits = p.many_splits;
     A.group = s->group, A.shared_blocks = s->shared_blocks, A.shared_table = s->shared_table, A.shared_stride = s->shared_stride;
     A.n_groups = (int)s->n_groups, A.max_shared = s->max_shared;
-    A.pieces = (int2*)a->workspace, A.many_part = (float*)((char*)a->workspace + p.pieces);
+    A.pieces = (int2*)a->workspace, A.many_part = (float*)((char*)a->workspace + p.pieces), A.part_ml = A.many_part + p.parts * c.head_dim;
+    A.part_stride = p.part_stride, A.own_at = p.own_at, A.by_request = p.many, A.apart = p.apart;
     const hipStream_t st = (hipStream_t)stream;
 #define AT(K, D) (c.block == 128 ? at_shared_launch<K, D, true>(A, p, st) : at_shared_launch<K, D, false>(A, p, st))
     if (c.kind == BL_KV_INT8) c.head_dim == 128 ? AT(BL_KV_INT8, 128) : AT(BL_KV_INT8, 64);

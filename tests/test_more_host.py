@@ -66,6 +66,13 @@ def test_shared_attention_wants_its_workspace(lib):  # noqa: F811
     assert 0 < one < few < more
 
 
+def test_shared_attention_s_workspace_stays_small_beside_a_prompt(lib):  # noqa: F811
+    """Partial results stand for the rows that have some: a prompt of thousands of rows beside seven decoding requests takes what its own pieces need."""
+    a = attention(B=8, T=8192 + 7, max_q=8192, max_len=30000)
+    n = lib.bl_attn_shared_workspace_bytes(ctypes.byref(shared(a, max_own=9000)))
+    assert 0 < n <= (a.T * a.n_q + 60 * a.B * a.cache.n_kv * 16) * 130 * 4 + a.T * 8 + 512
+
+
 def matrix(**more):
     return bl.F8MatrixDesc(**dict(dict(codes=P, scale=P, N=200, K=192, stride=192, scale_stride=2), **more))
 
