@@ -536,7 +536,7 @@ bl_status bl_attn_kv8(const bl_attn_desc* a, bl_stream s);
  *   shared_table   [n_groups][shared_stride], max_shared <= shared_stride entries of a row are used; its blocks are whole (every token written)
  *   max_own        about the most tokens that a request has behind its shared blocks: sizes a split only (0: as attn.max_len)
  *   attn.workspace bl_attn_shared_workspace_bytes(a) bytes
- * 1 <= n_groups <= BL_KV_MAX_REQUESTS, max_shared >= 1 (max_shared * block at most 2^30). */
+ * 1 <= n_groups <= BL_KV_MAX_REQUESTS, max_shared >= 1 (max_shared * block at most 2^30), T * n_q * head_dim < 2^34. */
 typedef struct {
     bl_attn_desc attn;
     const int32_t* group;

@@ -1746,7 +1746,7 @@ extern "C" bl_status bl_attn_kv8_shared(const bl_attn_shared_desc* s, bl_stream 
     if (!bl_aligned(a->workspace, 256)) return BL_ERR_ALIGN;
     const bl_kv_cache& c = a->cache;
     /* (a launch counts its threads in 32 bits) */
-    if (c.n_kv * (p.prefix_tiles * p.group_splits + p.many_tiles * p.many_splits + a->B * p.few_splits) >= 1 << 24 || a->T * a->n_q * (c.head_dim / 4) >= (int64_t)1 << 30)
+    if (c.n_kv * (p.prefix_tiles * p.group_splits + p.many_tiles * p.many_splits + a->B * p.few_splits) >= 1 << 24 || a->T * a->n_q * (c.head_dim / 4) >= (int64_t)1 << 32)
         return BL_ERR_SHAPE;
     at_args A = at_make_args(a);
     A.few_rows = p.few ? AT_FEW : 0, A.group_splits = p.group_splits, A.few_splits = p.few_splits, A.many_splits = p.many_splits;

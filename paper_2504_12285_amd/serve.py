@@ -134,16 +134,17 @@ class CachedLayers:
         return self.run()
 
 
-    def _free_group(self, group):
-        if self.prefix[group]:
-            raise ValueError("group %d has a prefix" % group)
+    # These three stand between steps and read back what they check.
 
     def share(self, group, place, blocks):
         """The first `blocks` blocks of the request at `place`, whole ones, become the group's prefix.  They belong to the group from now on: the request
-        may go on or end, and release gives them back."""
-        if not 0 < blocks <= self.shared_table.shape[1]:
-            raise ValueError("a prefix has 1 to %d blocks, not %d" % (self.shared_table.shape[1], blocks))
-        self._free_group(group)
+        may go on or end, and release gives them back.  The request is in no group so far."""
+        if self.prefix[group]:
+            raise ValueError("group %d has a prefix" % group)
+        if not 0 < blocks <= int(self.seq_len[place]) // self.block:
+            raise ValueError("a prefix has 1 to %d of the blocks at place %d, not %d" % (int(self.seq_len[place]) // self.block, place, blocks))
+        if int(self.group[place]) >= 0:
+            raise ValueError("the request at place %d is in group %d" % (place, int(self.group[place])))
         self.shared_table[group, :blocks] = self.table[place, :blocks]
         self.shared_blocks[group], self.prefix[group] = blocks, blocks
         self.held[place] = blocks
@@ -152,13 +153,19 @@ class CachedLayers:
     def join(self, place, group):
         """The next request at `place`, which is empty, begins behind the group's prefix."""
         n = self.prefix[group]
+        if not n:
+            raise ValueError("group %d has no prefix" % group)
+        if int(self.seq_len[place]):
+            raise ValueError("place %d has a request" % place)
         self.table[place, :n] = self.shared_table[group, :n]
         self.held[place], self.group[place] = n, group
         self.seq_len[place] = n * self.block
 
     def release(self, group):
-        """Gives the group's blocks back.  No request may be in it any more."""
+        """Gives the group's blocks back, once no request is in it any more."""
         n = self.prefix[group]
+        if bool((self.group == group).any()):
+            raise ValueError("group %d has requests" % group)
         at = self.free_count.long() + torch.arange(n, device=self.table.device)
         self.free_list.scatter_(0, at, self.shared_table[group, :n])
         self.free_count += n

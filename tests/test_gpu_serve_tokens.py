@@ -103,8 +103,11 @@ def test_requests_behind_a_prompt(model, kind):
     tokens.step(some_ids(0, 100, 0), ints([-1, -1, -1, -1]))
     assert int(layers.free_count) == 28
     layers.release(1)
+    with pytest.raises(ValueError):
+        layers.join(0, 1)
     assert int(layers.free_count) == 30 and sorted(layers.free_list.tolist()) == list(range(30)) and layers.shared_blocks.tolist() == [0, 0]
-    layers.share(1, 0, 1)
+    tokens.step(some_ids(40, 100, 22), ints([0, 40, 0, 0]))
+    layers.share(1, 1, 1)
 
 
 def test_refusals(model):
@@ -116,9 +119,21 @@ def test_refusals(model):
         tokens.step(ints([1, 2]), ints([1, 1]))
     tokens.step(ints([3, WORDS, -1, -1, -1, -1, -1, -1, -1, -1]), ints([1, 1]))
     assert int(tokens.bad) == 1
-    layers.share(0, 0, 1)
-    with pytest.raises(ValueError):
-        layers.share(0, 1, 1)
+
+
+def test_groups_are_what_they_are_made_for(model):
+    """A prefix is of whole blocks of a request that is in no group; places are joined empty, to a group with a prefix, which is given back when nobody is in it."""
+    layers, tokens = served(model, 3, 80, groups=2)
+    tokens.step(some_ids(75, 80, 5), ints([70, 5, 0]))
+    for group, place, blocks in ((0, 0, 3), (0, 1, 1), (0, 2, 1)):
+        with pytest.raises(ValueError):
+            layers.share(group, place, blocks)
+    layers.share(0, 0, 2)
+    for call in (lambda: layers.share(0, 1, 1), lambda: layers.share(1, 0, 1), lambda: layers.join(1, 0), lambda: layers.join(2, 1), lambda: layers.release(0)):
+        with pytest.raises(ValueError):
+            call()
+    layers.join(2, 0)
+    assert layers.seq_len.tolist() == [70, 5, 64] and layers.group.tolist() == [0, -1, 0] and layers.held.tolist() == [2, 0, 2]
 
 
 def test_captured_generation_is_the_eager_one(model):
