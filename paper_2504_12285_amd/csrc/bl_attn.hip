@@ -11,6 +11,7 @@
  * S is computed transposed (tokens x rows), so that a lane holds the weights of ONE row for sixteen tokens, exactly what the
  * second product wants of it: the weights never leave the lane.  Which tokens a lane gets is chosen by the
  * order in which the rows of K are handed in, such that its V codes are consecutive in memory. */
+#include <algorithm>
 #include <type_traits>
 
 #include "bl_device.h"
@@ -288,7 +289,8 @@ struct at_slot {                    /* a wave's partial result: rows x (D sums, 
  * workspace (at most two such: at its ends) and bl_attn_join adds it up.  The four pieces of a workgroup that lie in one item
  * (at_together) are taken tile by tile in turn instead, and meet in LDS: a quarter of the partial results.
  * ITEM (0, or the waves of a workgroup): a workgroup has one item whole, so that nothing is left to join (short contexts).
- * SHARED: a workgroup has one of `few_splits` pieces of what an item has behind its group's prefix, and leaves a partial result.
+ * SHARED: a workgroup has one of `few_splits` pieces of what an item has behind its group's prefix, and leaves a partial result (as items, not in streams: what
+ * a request has of its own is short, and a row's pieces are then known by its tiles alone).
  * ALONE: no at_many stands beside it; requests of more than AT_FEW rows then get no numbers (in the streams' form a lane's own work: an error's speed).
  * K rows of a tile go straight from memory into the registers that the matrix cores read (four 16 x 128 products of
  * codes against the two pieces of q), then V the same way.  V of a tile and K of the next are in flight while one computes,
@@ -879,7 +881,10 @@ struct at_prefix_lds : at_many_lds<KIND, D> {
     int found[5];                                           /* the group of the tile, tiles in front of it and of it, its tokens and rows */
 };
 /* What a workgroup of at_many has: rows of a request over all that they see; over what stands behind their group's prefix (AT_OWN); or rows of all
- * requests of a group over its prefix (AT_PREFIX), which are gathered: their places in the batch are found by each workgroup, by sums over the requests. */
+ * requests of a group over its prefix (AT_PREFIX), which are gathered: their places in the batch are found by each workgroup, by sums over the requests.
+ * A prefix's rows fill tiles together (128 of them for one read of K and V), in equal pieces over its tokens, so that every row of a group has as many partial results and
+ * the join needs no list.  Bound by the instructions of a wave's tiles one after the other, not by memory: 16 requests of 32 + 8 heads behind 65536 tokens, e4m3, 134 MB of codes,
+ * 50 us (without loads 47, without products 40; at_few reads them for each request: 337).  Two tiles of K in flight, pairs of waves on one tile's rows: 49 and 47. */
 enum { AT_ALL, AT_OWN, AT_PREFIX };
 template <int KIND, int D, int MODE = AT_ALL>
 __device__ __forceinline__ void at_many(const at_args& A, int place, std::conditional_t<MODE == AT_PREFIX, at_prefix_lds<KIND, D>, at_many_lds<KIND, D>>& lds) {
@@ -1427,7 +1432,7 @@ __device__ __forceinline__ void at_many_join(const at_args& A, int group) {
 }
 
 /* The same for rows of requests that share prefixes: the pieces of the prefix and those of the rest, as many as the row's entry says.  LANES groups of
- * D / 4 threads share a row's pieces and meet in LDS. */
+ * D / 4 threads share a row's pieces and meet in LDS.  Bound by the chain entry -> references -> sums: 64 rows of 20 heads, 16 + 4 pieces, 5.0 us; 16 of 32, 64 + 2, 6.7. */
 template <int D, int LANES>
 __global__ __launch_bounds__(AT_THREADS) void bl_attn_shared_join(at_args A) {
     constexpr int TPR = D / 4, IN = 4, GROUPS = AT_THREADS / TPR, ROWS = GROUPS / LANES;
@@ -1695,10 +1700,10 @@ static at_shared_plan at_make_shared_plan(const bl_attn_shared_desc* s) {
     const int64_t wide = (int64_t)a->window + (a->max_q < AT_MANY ? a->max_q : AT_MANY);
     if (a->window && tokens > wide) tokens = wide;
     if (a->window && own > wide) own = wide;
-    /* Pieces of `items` items of `tokens`: until there are `fill` workgroups, of four tiles at least; fewer tiles while not every unit has a workgroup. */
-    auto pieces = [](int64_t items, int64_t tokens, int64_t fill, int64_t each, int64_t most) -> int {
-        const int64_t full = fill / items < tokens / (4 * AT_TILE) ? fill / items : tokens / (4 * AT_TILE), tiles = (tokens + each * AT_TILE - 1) / (each * AT_TILE);
-        const int64_t some = 128 / items < tiles ? 128 / items : tiles, n = full > some ? full : some;
+    /* Pieces of `items` items of `tokens`: until there are 512 workgroups while a piece has `deep` tiles, 256 while it has four, 128 while it has `each`. */
+    auto pieces = [](int64_t items, int64_t tokens, int64_t deep, int64_t each, int64_t most) -> int {
+        auto until = [&](int64_t groups, int64_t of) { return std::min(groups / items, (tokens + (of == 1 ? AT_TILE - 1 : 0)) / (of * AT_TILE)); };
+        const int64_t n = std::max(std::max(until(512, deep), until(256, 4)), until(128, each));
         return (int)(n < 1 ? 1 : n < most ? n : most);
     };
     /* Where a request may fill tiles of at_many by itself, which read the prefix from the caches then, all of more than AT_FEW rows are apart; else they are of
@@ -1708,10 +1713,13 @@ static at_shared_plan at_make_shared_plan(const bl_attn_shared_desc* s) {
     p.apart = prompts ? AT_FEW + 1 : AT_MANY;
     const int64_t most = a->T * G < part * (p.apart - 1) ? a->T * G : part * (p.apart - 1);            /* rows that groups can have */
     p.prefix_tiles = most / AT_MANY + groups;
-    p.group_splits = pieces((most + AT_MANY - 1) / AT_MANY * a->cache.n_kv, (int64_t)s->max_shared * a->cache.block, 512, 1, 64);
-    p.few_splits = p.few ? pieces(part * a->cache.n_kv, own, 512, 4, 32) : 0;
+    /* (64 requests behind 4096 tokens, 256 with pieces of three tiles 33.0, of four 28.5.  Heads of 128, two workgroups a unit: the second pays for itself where it has sixteen tiles.  us so and with 512 of four tiles: 64 requests behind 16000 tokens, 5, 8
+     * and 1 kv heads 38, 48, 37 and 47, 55, 40, 128 behind 8000 42, 56, 39 and 51, 66, 43; 512 and 256 where there are sixteen: 16 behind 65536, 8 kv heads, 56 and 67.
+     * Heads of 64, three a unit: 64 behind 16000 34.5 with 512, 38 with 256) */
+    p.group_splits = pieces((most + AT_MANY - 1) / AT_MANY * a->cache.n_kv, (int64_t)s->max_shared * a->cache.block, D == 128 ? 16 : 4, 1, 64);
+    p.few_splits = p.few ? pieces(part * a->cache.n_kv, own, 4, 4, 32) : 0;
     /* (prompts read the prefix too: two of 600 over 32000 tokens beside 14 of one, cut by their own tokens 790 us, by all 370) */
-    p.many_splits = p.many ? pieces(tiles * a->cache.n_kv, prompts ? tokens : own, 512, 4, 32) : 0;
+    p.many_splits = p.many ? pieces(tiles * a->cache.n_kv, prompts ? tokens : own, 4, 4, 32) : 0;
     p.many_tiles = p.many ? a->T * G / AT_MANY + part : 0;
     p.pieces = ((size_t)a->T * sizeof(int2) + 255) / 256 * 256;
     p.part_stride = p.many ? a->B * a->cache.n_kv * p.apart : a->T * a->n_q;

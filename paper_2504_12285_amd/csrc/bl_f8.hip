@@ -90,7 +90,8 @@ __device__ __forceinline__ void f8_put_unit(const f8_args& A, int m, int u, cons
     *(bl_v4i*)(A.codes + ((int64_t)m * A.nb * 8 + u) * 16) = f8_codes16(lo, hi, bl_div_rn(1.0f, s));
     if ((u & 7) == 0) A.scales[(int64_t)(u >> 3) * A.M + m] = s;
 }
-/* A workgroup a row, whose norm meets in it.  Zeros behind K in the last block. */
+/* A workgroup a row, whose norm meets in it.  Zeros behind K in the last block.  Bound by the launch and the chain row -> sum -> root -> codes: one row 2.4 to 4.7 us, 1025 rows of
+ * 3328 7.6, with the sum, the root or the scales' stores left out 7.3 to 7.8. */
 __global__ __launch_bounds__(256) void bl_f8_rows(f8_args A, bl_prod_dev P) {
     __shared__ double s4[4];
     const int m = (int)blockIdx.x, tid = threadIdx.x, groups = A.K / 16, all = A.nb * 8;
@@ -112,7 +113,7 @@ __global__ __launch_bounds__(256) void bl_f8_rows(f8_args A, bl_prod_dev P) {
     }
 }
 
-/* The same without a norm, where nothing crosses a group: the units of all rows in one line. */
+/* The same without a norm, where nothing crosses a group: the units of all rows in one line (2048 rows of 2560 from bf16, 16 MB, 6.4 us). */
 __global__ __launch_bounds__(256) void bl_f8_units(f8_args A, bl_prod_dev P) {
     const int groups = A.K / 16, all = A.nb * 8;
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
@@ -146,7 +147,9 @@ __device__ __forceinline__ void f8_store4(const f8_args& A, int m, int n, const 
 
 /* Up to 16 * MT tokens.  A workgroup of eight waves walks strips of 16 weight rows; wave w has the blocks w, w + 8, .. of k (KB of them at most), for
  * which it keeps the tokens' codes and scales in registers, and meets the others' sums in LDS; one barrier a strip.  A block's 2 KB go to LDS in whole lines (eight
- * rows of 128 bytes a load) and from there to the lanes; a wave has AHEAD of them in flight, in a ring of its own.  FUSED: the rows are made here, by every workgroup: a lane has
+ * rows of 128 bytes a load) and from there to the lanes; a wave has AHEAD of them in flight, in a ring of its own.  Bound by HBM: 128256 x 2560, 328 MB, one row 48 us = 6.8 TB/s
+ * (straight to the lanes, whose rows are lines of their own, 78), 48 rows 73 with 25 MB of outputs written beside it.
+ * (Four waves along k instead of eight: 48 rows 79 for 81 then, and 18 kernels more.)  FUSED: the rows are made here, by every workgroup: a lane has
  * what its token needs for its own blocks, so that only the sum of squares of a norm crosses waves. */
 #define F8_WAVES 8
 template <int MT, int KB>
@@ -361,7 +364,11 @@ __host__ __device__ static __forceinline__ int64_t f8_part_stride(int64_t N) { r
 /* BM tokens x BN weight rows a workgroup, WM x WN waves, S stages of one block of k (128) in LDS.  Rows of 128 bytes; unit u (16 bytes) of row r lies
  * at unit u ^ (r / 2 % 8), so that sixteen lanes of a read fall on all banks; the loads that go straight to LDS pick their units accordingly.
  * In the last block of a K that is no multiple of 128 the units behind K are the weights' first four again: their codes meet zeros (and a
- * NaN among them spoils the row anyway). */
+ * NaN among them spoils the row anyway).
+ * Bound by issue: 2048 rows x 13824 x 2560, 145 GFLOP, 141 to 147 us without the rows' kernel = 990 to 1030 TFLOP/s (the library's bf16 product 1190): two conversions
+ * and a multiply-add of four stand beside each matrix product.  Of 169 us then, without the conversions of x 157, without loads 146, without the adds 163: none is all of it.  Two workgroups
+ * of two stages a unit, so that one computes while the other opens.  Tiles of 128 x 256 and 256 x 128 with eight waves: 187 to 190 for 161; codes as they are into the 8-bit
+ * instructions (fewer bits, see f8_open), one workgroup of three stages: 283. */
 template <int BM, int BN, int WM, int WN, int S>
 __global__ __launch_bounds__(WM * WN * 64, 2) void bl_f8_tile(f8_args A) {
     constexpr int NW = WM * WN, TM = BM / WM / 16, TN = BN / WN / 16, SCALES = (BM + BN) * F8_BLOCK, STAGE = SCALES + BM * 4, LOADS = (BM + BN) / 8 / NW;
@@ -532,7 +539,7 @@ struct f8_lookup_args {
     int N, units;                  /* units of a row, 16 bytes of the output each */
     float multiplier;
 };
-/* A thread 16 bytes of the output. */
+/* A thread 16 bytes of the output.  Bound by HBM: 8000 rows of 2560 to bf16, 61 MB, 12.7 us = 4.8 TB/s (a large copy's rate); eight rows by the launch and the chain id -> codes: 3.8. */
 template <bool BF16>
 __global__ __launch_bounds__(256) void bl_f8_embed_kernel(f8_lookup_args A) {
     constexpr int V = BF16 ? 8 : 4;
@@ -588,10 +595,13 @@ static f8_plan f8_make_plan(const bl_f8_product* p) {
     f8_plan q;
     const int64_t nb = (p->w.K + F8_BLOCK - 1) / F8_BLOCK;
     q.splits = 1;
-    /* the stream, while a wave's registers hold its blocks of every token */
+    /* The stream, while a wave's registers hold its blocks of every token, and where they hold them opened or there are few rows of tiles.  us of it and of tiles:
+     * 2560 x 2560 17 to 64 rows 8.6 to 11.9 and 11.4 to 13.9; 128256 x 2560 17, 48, 64 rows 61, 72, 94 and 71, 80, 86; 40000 x 2560 48, 64 rows 28.8, 36.2 and 26.2,
+     * 26.6; x 4096 17, 48 rows 36.6, 44.9 and 37.3, 37.4; 4096 x 4096 48 rows 14.2 and 15.0, 8192 16.9 and 16.1.  (16 rows: the stream at every size.) */
     const int64_t each = (nb + F8_WAVES - 1) / F8_WAVES;
     q.tokens = p->M <= 64 ? (int)((p->M + 15) / 16) : 0, q.blocks = each > 8 ? 16 : each <= 4 ? (int)each : each <= 6 ? 6 : 8;
-    if (q.tokens * q.blocks > 12) q.tokens = 0;
+    if (q.tokens * q.blocks > (p->w.N >= 8192 ? 9 : 12)) q.tokens = 0;
+    /* rows made in the stream itself: 300 x 320 4.1 us, 5.5 with a launch of their own, 1000 x 1024 4.8 and 5.7 (longer rows spill: 2560 x 2560 22.9, so 6.5) */
     q.fused = q.tokens == 1 && q.blocks == 1;
     if (q.tokens) {
         q.codes = q.fused ? 0 : f8_round((size_t)p->M * nb * F8_BLOCK), q.scales = q.fused ? 0 : f8_round((size_t)p->M * nb * sizeof(float));
@@ -600,11 +610,18 @@ static f8_plan f8_make_plan(const bl_f8_product* p) {
     }
     q.codes = f8_round((size_t)p->M * nb * F8_BLOCK), q.scales = f8_round((size_t)p->M * nb * sizeof(float));
     const int64_t large = ((p->M + 127) / 128) * ((p->w.N + 127) / 128), small = ((p->M + 63) / 64) * ((p->w.N + 63) / 64);
+    /* Tiles of 64 x 64 while those of 128 x 128 are fewer than the units, or would be half empty.  us of the small and the large (neither cut along k where there are
+     * enough): 13824 x 2560 65, 512 rows 20, 53 and 32, 43, 2048 rows 198 and 151; 4096 x 8192 256, 2048 rows 34, 187 and 89, 128; 32000 x 4096 64, 65, 256 rows 29, 47, 88 and
+     * 48, 48, 64; 2560 x 2560 2048 rows 47.4 and 45.6. */
     q.small = large < 192 || p->M <= 64;
+    /* Pieces of k until there are 512 workgroups, two a unit, of two blocks at least, where k is long enough to pay for the join.  us with and without:
+     * 2560 x 6912 65, 200, 512 rows 18, 24, 44 and 38, 40, 45; 337 x 6784 65 to 2048 13 to 38 and 38 to 48; 2560 x 2560 65, 200 rows 13.5, 16.9 and 18.0, 18.6;
+     * 1188 x 1920 65, 512 rows 11.3, 16.9 and 14.7, 16.1; 1000 x 1024 65, 512, 1024 rows 9.8, 14.8, 17.2 and 10.7, 11.4, 12.6.  For 256 workgroups: 4096 x 8192 200 rows
+     * 33 and 46. */
     const int64_t tiles = q.small ? small : large;
     int64_t s = tiles < 512 ? 512 / tiles : 1;
     if (s > nb / 2) s = nb / 2;
-    q.splits = s < 1 || !q.small ? 1 : s > 16 ? 16 : (int)s;
+    q.splits = s < 1 || nb < 12 || !q.small ? 1 : s > 16 ? 16 : (int)s;
     q.bytes = q.codes + q.scales + (q.splits > 1 ? (size_t)q.splits * p->M * f8_part_stride(p->w.N) * sizeof(float) : 0);
     return q;
 }
