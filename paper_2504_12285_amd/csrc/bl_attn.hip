@@ -1439,15 +1439,17 @@ __global__ __launch_bounds__(AT_THREADS) void bl_attn_shared_join(at_args A) {
     __shared__ float s_m[GROUPS], s_l[GROUPS];
     __shared__ __attribute__((aligned(16))) float s_y[GROUPS][D];
     const int group = threadIdx.x / TPR, part = group / ROWS;               /* (a wave's groups have other rows: their loads are of neighbours) */
-    const int64_t at = (int64_t)blockIdx.x * ROWS + group % ROWS, all = (int64_t)A.T * A.n_q;
-    const int row = (int)(at / A.n_q), d0 = (threadIdx.x % TPR) * 4;
+    const uint32_t at = blockIdx.x * ROWS + group % ROWS, all = (uint32_t)A.T * A.n_q;                  /* (below 2^28) */
+    const int row = (int)(at / (uint32_t)A.n_q), head = (int)(at % (uint32_t)A.n_q), d0 = (threadIdx.x % TPR) * 4;
     int2 entry = {0, 0};
-    if (at < all && row >= A.q_start[0] && row < A.q_start[A.B]) entry = A.pieces[row];
+    if (at < all) entry = A.pieces[row];
+    if (row < A.q_start[0] || row >= A.q_start[A.B]) entry = {0, 0};
+    if (LANES == 1 && entry.x == 0) return;
     /* (first rows that do not ascend leave entries unwritten: no content of them leads outside) */
     const bool none = entry.x == AT_NO_NUMBERS, many = entry.x >> 16 & 1;
     const int prefix = none ? 0 : min(entry.x & 255, A.G < A.apart ? A.group_splits : 0), own = none ? 0 : min(entry.x >> 8 & 255, many ? A.many_splits : A.few_splits), count = prefix + own;
     const int slot = (unsigned)entry.y < (unsigned)(A.B * A.apart) && (entry.y % A.apart + 1) * A.G <= A.apart ? entry.y : 0;
-    const int64_t first = at_part_at(A, slot, row, (int)(at % A.n_q)), step = many ? all : A.part_stride;
+    const int64_t first = at_part_at(A, slot, row, head), step = many ? (int64_t)all : A.part_stride;
     const int64_t first_own = (many ? A.own_at + at : A.group_splits * A.part_stride + first) - prefix * step;
     at_sum s = {-INFINITY, 0.0f, {0, 0, 0, 0}};
     for (int i = part; i < count; i += IN * LANES) {
@@ -1477,7 +1479,7 @@ __global__ __launch_bounds__(AT_THREADS) void bl_attn_shared_join(at_args A) {
     const float inv = s.l == 0.0f ? 0.0f : bl_div_rn(1.0f, s.l);
     bl_v2u u = {bl_pack2_bf16(s.y[0] * inv, s.y[1] * inv), bl_pack2_bf16(s.y[2] * inv, s.y[3] * inv)};
     if (none) u = (bl_v2u){0x7fc07fc0u, 0x7fc07fc0u};         /* more queries than the launch was made for */
-    *bl_g((bl_v2u*)(A.out + row * A.out_stride + (at % A.n_q) * D + d0)) = u;
+    *bl_g((bl_v2u*)(A.out + row * A.out_stride + head * D + d0)) = u;
 }
 
 /* ---- launches ---------------------------------------------------------------------------------------------------------- */
