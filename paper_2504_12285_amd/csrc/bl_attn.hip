@@ -102,8 +102,8 @@ __device__ __forceinline__ at_request at_read_own(const at_args& A, int b) {
 }
 /* First token that query i sees, and the one behind its last. */
 __device__ __forceinline__ int at_from(const at_args& A, const at_request& r, int i) {
-    const int p = r.len - r.n + i - A.window + 1, f = A.window && p > 0 ? p : 0;
-    return f > r.skip ? f : r.skip;
+    const int p = A.window ? r.len - r.n + i - A.window + 1 : 0;
+    return p > r.skip ? p : r.skip;
 }
 __device__ __forceinline__ int at_to(const at_request& r, int i) {
     const int e = r.len - r.n + i + 1;
