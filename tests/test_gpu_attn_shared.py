@@ -123,6 +123,28 @@ def test_many_requests_and_groups(kind):
     Shared(reqs, prefix, group, (8, 2, 64), 16, kind).check()
 
 
+@pytest.mark.parametrize("new", [1, 3, 30, 70])
+@pytest.mark.parametrize("B, groups", [(300, 4), (40, 270), (257, 257)])
+def test_more_requests_or_groups_than_threads(B, groups, new):
+    """One token each, a few, and requests of many rows among them that are of their groups (30 of 2 heads) or apart (70)."""
+    prefix = [(5 * g) % 7 for g in range(groups)]
+    reqs, group = dealt(prefix, [(b * 37) % 50 + 1 + (new if b % 60 == 7 else 0) for b in range(B)], 16, groups)
+    reqs = [(t, min(t, new) if b % 60 == 7 else 1 + b % min(new, 2)) for b, (t, n) in enumerate(reqs)]
+    reqs = [(max(t, n), n) for t, n in reqs]
+    Shared(reqs, prefix, group, (4, 2, 64), 16, "int8", seed=new).check()
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("heads, counts", [((20, 5, 128), (1, 4, 5, 20, 31)), ((20, 5, 128), (1, 4, 5, 31, 32, 40, 200)), ((8, 8, 64), (16, 17, 127, 1)), ((8, 8, 64), (16, 17, 127, 128, 1, 260)),
+                                           ((34, 2, 64), (1, 2, 7)), ((34, 2, 64), (1, 8, 30))])
+def test_many_and_few_rows_in_one_batch(kind, heads, counts):
+    """Numbers of rows on both sides of what a few, a group's and a prompt's are."""
+    prefix = [20, 6]
+    reqs = [(prefix[b % 2] * 32 + n + 10 * b, n) for b, n in enumerate(counts * 2)]
+    Shared(reqs, prefix, [b % 2 if b != 3 else -1 for b in range(len(reqs))], heads, 32, kind, seed=len(counts)).check()
+    Shared(reqs, prefix, [b % 2 for b in range(len(reqs))], heads, 32, kind, seed=len(counts)).check(window=300, max_own=1)
+
+
 @pytest.mark.parametrize("kind", KINDS)
 @pytest.mark.parametrize("heads, block", [((20, 5, 128), 64), ((32, 8, 64), 128)])
 def test_long_prefixes(kind, heads, block):

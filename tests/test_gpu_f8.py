@@ -133,6 +133,11 @@ def test_long_rows(M):
 def test_many_rows_and_columns():
     linear(777, 2000, 1216, dtype=torch.bfloat16, out=torch.bfloat16)
     linear(1025, 1409, 704)
+    for M in (48, 49, 64, 65):                                # (the widest choices of each kind of kernel)
+        linear(M, 8300, 2560, out=torch.bfloat16)
+        linear(M, 8192, 4096, norm=True)
+    for K in (1344, 1408, 1472, 1536):
+        linear(200, 300, K, dtype=torch.bfloat16, norm=K == 1408)
 
 
 @pytest.mark.parametrize("M", [1, 20, 70])
