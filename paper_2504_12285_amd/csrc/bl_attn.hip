@@ -266,8 +266,8 @@ __device__ __forceinline__ int at_piece_count(int tiles, int splits) {
  * own ones are at_many's.  AT_NO_NUMBERS: more queries than the launch was made for. */
 #define AT_NO_NUMBERS -1
 __device__ __forceinline__ int at_pieces(int prefix, int own, bool many) { return prefix | own << 8 | (many ? 1 << 16 : 0); }
-/* Query i of request b, where partial results stand by requests: fewer than `apart` rows of each have some, however many a prompt beside them brings (one of
- * 8192 beside seven decoding requests: 0.1 GB for 3.9 by rows of the batch). */
+/* Query i of request b, where partial results stand by requests, not by rows of the batch, because that is less: fewer than `apart` rows of each have some, however
+ * many a prompt beside them brings (one of 8192 beside seven decoding requests: 0.1 GB for 3.9). */
 __device__ __forceinline__ int at_query(const at_args& A, int b, int i) { return b * A.apart + i; }
 /* Where the first piece of (row, head) stands among the partial results. */
 __device__ __forceinline__ int64_t at_part_at(const at_args& A, int query, int row, int head) {
@@ -1664,7 +1664,7 @@ extern "C" bl_status bl_attn_kv8(const bl_attn_desc* a, bl_stream s) {
 /* ---- shared prefixes, host ------------------------------------------------------------------------------------------------ */
 
 struct at_shared_plan {
-    bool few, many;
+    bool few, many, by_request;
     int group_splits, few_splits, many_splits, apart;
     int64_t prefix_tiles, many_tiles, part_stride, own_at, parts;
     size_t pieces, bytes;          /* of the rows' entries in front, and in all */
@@ -1702,10 +1702,10 @@ static at_shared_plan at_make_shared_plan(const bl_attn_shared_desc* s) {
     const int64_t wide = (int64_t)a->window + (a->max_q < AT_MANY ? a->max_q : AT_MANY);
     if (a->window && tokens > wide) tokens = wide;
     if (a->window && own > wide) own = wide;
-    /* Pieces of `items` items of `tokens`: until there are 512 workgroups while a piece has `deep` tiles, 256 while it has four, 128 while it has `each`. */
+    /* Pieces of `items` items of `tokens`: until there are 512 workgroups while a piece has `deep` tiles, 256 while it has four, 128 while all but the last have `each`. */
     auto pieces = [](int64_t items, int64_t tokens, int64_t deep, int64_t each, int64_t most) -> int {
-        auto until = [&](int64_t groups, int64_t of) { return std::min(groups / items, (tokens + (of == 1 ? AT_TILE - 1 : 0)) / (of * AT_TILE)); };
-        const int64_t n = std::max(std::max(until(512, deep), until(256, 4)), until(128, each));
+        auto until = [&](int64_t groups, int64_t pieces) { return std::min(groups / items, pieces); };
+        const int64_t n = std::max(std::max(until(512, tokens / (deep * AT_TILE)), until(256, tokens / (4 * AT_TILE))), until(128, (tokens + each * AT_TILE - 1) / (each * AT_TILE)));
         return (int)(n < 1 ? 1 : n < most ? n : most);
     };
     /* Where a request may fill tiles of at_many by itself, which read the prefix from the caches then, all of more than AT_FEW rows are apart; else they are of
@@ -1717,14 +1717,17 @@ static at_shared_plan at_make_shared_plan(const bl_attn_shared_desc* s) {
     p.prefix_tiles = most / AT_MANY + groups;
     /* (64 requests behind 4096 tokens, 256 with pieces of three tiles 33.0, of four 28.5.  Heads of 128, two workgroups a unit: the second pays for itself where it has sixteen tiles.  us so and with 512 of four tiles: 64 requests behind 16000 tokens, 5, 8
      * and 1 kv heads 38, 48, 37 and 47, 55, 40, 128 behind 8000 42, 56, 39 and 51, 66, 43; 512 and 256 where there are sixteen: 16 behind 65536, 8 kv heads, 56 and 67.
-     * Heads of 64, three a unit: 64 behind 16000 34.5 with 512, 38 with 256) */
-    p.group_splits = pieces((most + AT_MANY - 1) / AT_MANY * a->cache.n_kv, (int64_t)s->max_shared * a->cache.block, D == 128 ? 16 : 4, 1, 64);
+     * Not where one piece is half of the 256 (200 requests, 30 of them with 30 queries, behind 2000, 170 items: one piece 105, three 77), or prompts are on the units too (four of
+     * 300 tokens beside 60 behind 8000: 116 and 107).  Heads of 64, three a unit: 64 behind 16000 34.5 with 512, 38 with 256) */
+    const int64_t items = (most + AT_MANY - 1) / AT_MANY * a->cache.n_kv;
+    p.group_splits = pieces(items, (int64_t)s->max_shared * a->cache.block, D == 128 && items <= 128 && !prompts ? 16 : 4, 1, 64);
     p.few_splits = p.few ? pieces(part * a->cache.n_kv, own, 4, 4, 32) : 0;
     /* (prompts read the prefix too: two of 600 over 32000 tokens beside 14 of one, cut by their own tokens 790 us, by all 370) */
     p.many_splits = p.many ? pieces(tiles * a->cache.n_kv, prompts ? tokens : own, 4, 4, 32) : 0;
     p.many_tiles = p.many ? a->T * G / AT_MANY + part : 0;
     p.pieces = ((size_t)a->T * sizeof(int2) + 255) / 256 * 256;
-    p.part_stride = p.many ? a->B * a->cache.n_kv * p.apart : a->T * a->n_q;
+    p.by_request = a->B * a->cache.n_kv * p.apart < a->T * a->n_q;
+    p.part_stride = p.by_request ? a->B * a->cache.n_kv * p.apart : a->T * a->n_q;
     p.own_at = (p.group_splits + p.few_splits) * p.part_stride, p.parts = p.own_at + p.many_splits * a->T * a->n_q;
     p.bytes = p.pieces + (size_t)p.parts * (D + 2) * sizeof(float);
     return p;
@@ -1763,7 +1766,7 @@ extern "C" bl_status bl_attn_kv8_shared(const bl_attn_shared_desc* s, bl_stream 
     A.group = s->group, A.shared_blocks = s->shared_blocks, A.shared_table = s->shared_table, A.shared_stride = s->shared_stride;
     A.n_groups = (int)s->n_groups, A.max_shared = s->max_shared;
     A.pieces = (int2*)a->workspace, A.many_part = (float*)((char*)a->workspace + p.pieces), A.part_ml = A.many_part + p.parts * c.head_dim;
-    A.part_stride = p.part_stride, A.own_at = p.own_at, A.by_request = p.many, A.apart = p.apart;
+    A.part_stride = p.part_stride, A.own_at = p.own_at, A.by_request = p.by_request, A.apart = p.apart;
     const hipStream_t st = (hipStream_t)stream;
 #define AT(K, D) (c.block == 128 ? at_shared_launch<K, D, true>(A, p, st) : at_shared_launch<K, D, false>(A, p, st))
     if (c.kind == BL_KV_INT8) c.head_dim == 128 ? AT(BL_KV_INT8, 128) : AT(BL_KV_INT8, 64);

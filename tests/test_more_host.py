@@ -71,6 +71,9 @@ def test_shared_attention_s_workspace_stays_small_beside_a_prompt(lib):  # noqa:
     a = attention(B=8, T=8192 + 7, max_q=8192, max_len=30000)
     n = lib.bl_attn_shared_workspace_bytes(ctypes.byref(shared(a, max_own=9000)))
     assert 0 < n <= (a.T * a.n_q + 60 * a.B * a.cache.n_kv * 16) * 130 * 4 + a.T * 8 + 512
+    a = attention(B=4096, T=4200, max_q=50, max_len=30000)
+    n = lib.bl_attn_shared_workspace_bytes(ctypes.byref(shared(a, max_own=100)))
+    assert 0 < n <= 3 * a.T * a.n_q * 130 * 4 + a.T * 8 + 512
 
 
 def matrix(**more):
