@@ -108,7 +108,7 @@ __global__ __launch_bounds__(256) void bl_f8_rows(f8_args A, bl_prod_dev P) {
     }
     for (int u = tid + (P.norm ? 512 : 0); u < all; u += 256) {
         uint4 lo = zero, hi = zero;
-        if (u < groups) bl_produce16<true>(P, m, u, A.K, !P.norm, rn, lo, hi);
+        if (u < groups) bl_produce16<true>(P, m, u, A.K, true, rn, lo, hi);     /* (behind a norm's 512 units nobody has stored the sum) */
         f8_put_unit(A, m, u, lo, hi);
     }
 }

@@ -285,3 +285,18 @@ def test_quantised_matrix_stands_for_its_numbers():
     h.run()
     step = m.scale.repeat_interleave(128, 0)[:300].repeat_interleave(128, 1)[:, :320]
     assert bool(((h.out - W).abs() <= (2.0 ** -4 + 2.0 ** -22) * W.abs() + 2.0 ** -10 * step).all())
+
+
+@pytest.mark.parametrize("K", [8192, 8256, 9024, 20480])
+@pytest.mark.parametrize("M", [1, 3, 20, 100])
+def test_the_sum_that_a_producer_leaves_is_whole(M, K):
+    """Rows on both sides of the 8192 values that a workgroup keeps between their norm and their codes: every value of the sum is written."""
+    from paper_2504_12285_amd import binding as bl
+    codes, scale = matrix(70, K)
+    a, b = rows(M, K, 1), rows(M, K, 2)
+    for norm in (True, False):
+        aux = torch.full_like(a, math.nan)
+        h = bl.F8Linear(bl.F8Matrix(codes, scale), prod=bl.make_producer(bl.BL_PROD_RESIDUAL, a, b, aux, norm=norm, eps=2.0 ** -17), M=M)
+        h.run()
+        assert torch.equal(aux, a + b)
+        check(h, codes, scale, a + b, norm)
