@@ -136,9 +136,17 @@ class CachedLayers:
 
     # These three stand between steps and read back what they check.
 
+    def _within(self, group, place=0):
+        """A negative number would be that of another group or place, and as a request's group that of none."""
+        if not 0 <= group < self.groups:
+            raise ValueError("group %d of %d" % (group, self.groups))
+        if not 0 <= place < self.seq_len.shape[0]:
+            raise ValueError("place %d of %d" % (place, self.seq_len.shape[0]))
+
     def share(self, group, place, blocks):
         """The first `blocks` blocks of the request at `place`, whole ones, become the group's prefix.  They belong to the group from now on: the request
         may go on or end, and release gives them back.  The request is in no group so far."""
+        self._within(group, place)
         if self.prefix[group]:
             raise ValueError("group %d has a prefix" % group)
         if not 0 < blocks <= int(self.seq_len[place]) // self.block:
@@ -152,6 +160,7 @@ class CachedLayers:
 
     def join(self, place, group):
         """The next request at `place`, which is empty, begins behind the group's prefix."""
+        self._within(group, place)
         n = self.prefix[group]
         if not n:
             raise ValueError("group %d has no prefix" % group)
@@ -163,6 +172,7 @@ class CachedLayers:
 
     def release(self, group):
         """Gives the group's blocks back, once no request is in it any more."""
+        self._within(group)
         n = self.prefix[group]
         if bool((self.group == group).any()):
             raise ValueError("group %d has requests" % group)

@@ -202,3 +202,46 @@ def test_product_refuses_to_write_what_it_reads(lib):  # noqa: F811
             assert call(**{out: at[other]}) == VALUE, (out, other)
             last = at[other] + length[other] - 1
             assert call(**{out: last - last % 256}) == VALUE or last - last % 256 < at[other], (out, other)
+
+
+def layers_of_nothing(**more):
+    """The tables and groups of served layers, without a layer: three places, the first with a request of 70 tokens in blocks of 32."""
+    from paper_2504_12285_amd import serve
+    layers = serve.CachedLayers([], [], 3, 80, max_blocks=8, n_blocks=30, device=torch.device("cpu"), block=32, **more)
+    layers.seq_len[0] = 70
+    layers.table[0, :3] = torch.tensor([7, 8, 9], dtype=torch.int32)
+    layers.free_count[0] = 27
+    return layers
+
+
+def state(layers):
+    return [t.clone() for t in (layers.seq_len, layers.table, layers.held, layers.group, layers.shared_table, layers.shared_blocks, layers.free_list, layers.free_count)]
+
+
+def test_groups_and_places_are_the_layers_own():
+    """Numbers outside the groups and places are refused, negative ones too (they would be those of another), and change nothing."""
+    layers = layers_of_nothing(groups=2)
+    before = state(layers)
+    for group, place in ((-1, 0), (2, 0), (-2, 0), (0, -1), (0, -3), (0, 3), (1, 10)):
+        with pytest.raises(ValueError):
+            layers.share(group, place, 2)
+    assert all(torch.equal(a, b) for a, b in zip(before, state(layers))) and layers.prefix == [0, 0]
+    layers.share(1, 0, 2)
+    assert layers.group.tolist() == [1, -1, -1] and layers.prefix == [0, 2]
+    before = state(layers)
+    for group, place in ((-1, 1), (3, 1), (1, -1), (1, -2), (1, 3)):
+        with pytest.raises(ValueError):
+            layers.join(place, group)
+    for group in (-1, -2, 2, 10):
+        with pytest.raises(ValueError):
+            layers.release(group)
+    assert all(torch.equal(a, b) for a, b in zip(before, state(layers))) and layers.prefix == [0, 2]
+    layers.join(2, 1)
+    assert layers.seq_len.tolist() == [70, 0, 64] and layers.table[2, :2].tolist() == [7, 8] and layers.held.tolist() == [2, 0, 2]
+
+
+def test_layers_without_groups_share_nothing():
+    layers = layers_of_nothing()
+    for call in (lambda: layers.share(0, 0, 1), lambda: layers.join(1, 0), lambda: layers.release(0)):
+        with pytest.raises(ValueError):
+            call()
