@@ -84,6 +84,23 @@ def make_producer(kind, in0, in1=None, aux_out=None, n_q=0, n_kv=0, head_dim=0, 
     return p
 
 
+def _producer_parts(p, K):
+    """The tensors of a producer of rows of K values, as its kind reads and writes them: (name, tensor, whether bf16, values a row; None: K values in all).
+    Nothing for a descriptor that was filled in by hand, or that the call itself refuses."""
+    tensors = getattr(p, "tensors", None)
+    wide = {BL_PROD_BF16: K, BL_PROD_F32: K, BL_PROD_RESIDUAL: K, BL_PROD_RELU2_GATE: 2 * K,
+            BL_PROD_ATTN_V: (p.n_q + 2 * p.n_kv) * p.head_dim if p.n_q * p.head_dim == K else None}.get(p.kind)
+    if tensors is None or wide is None:
+        return []
+    in0, in1, aux_out, gain = tensors
+    parts = [("in0", in0, p.kind == BL_PROD_BF16, wide)]
+    if p.kind == BL_PROD_RESIDUAL:
+        parts += [("in1", in1, False, K), ("aux_out", aux_out, False, K)]
+    if p.norm:
+        parts.append(("gain", gain, False, None))
+    return [part for part in parts if part[1] is not None]
+
+
 class DecodeDesc(ctypes.Structure):
     """Mirror of bl_decode_desc."""
     _fields_ = [("packed", _vp), ("beta", _vp), ("X", _vp), ("q", _vp), ("scale", _vp), ("rowsum", _vp),
@@ -547,6 +564,15 @@ def _wants(t, what, dtype, device, shape=None, rows=False):
     return t
 
 
+def _wants_producer(p, M, K, device):
+    """A producer whose tensors have M rows at least, each as wide as its kind has it (its values may be in several dimensions)."""
+    torch = _get_torch()
+    for name, t, bf16, wide in _producer_parts(p, K):
+        _wants(t, name, torch.bfloat16 if bf16 else torch.float32, device, None if wide else (K,))
+        if wide and (t.numel() < M * wide or (t.numel() % wide if t.dim() == 1 else wide not in (math.prod(t.shape[i:]) for i in range(t.dim())))):
+            raise ValueError("%s must have %d rows of %d values, has the shape %s" % (name, M, wide, tuple(t.shape)))
+
+
 def _row_stride(t):
     """Elements from a row to the next (a single row may carry any stride, and there may be none)."""
     return t.stride(0) if t.shape[0] > 1 else math.prod(t.shape[1:])
@@ -778,7 +804,7 @@ def _f8_kind(dtype):
 
 class F8Linear(_KVCall):
     """y = rows times the matrix's transpose (bl_f8_linear).  x: bf16 or fp32 [M][K], with norm=True normalised on the way (gain fp32 [K] or
-    None); or prod, a producer of make_producer, and M.  Output: y [M][N] of `dtype` (or of y's).  The workspace
+    None); or prod, a producer of make_producer whose tensors have M rows at least, and M.  Output: y [M][N] of `dtype` (or of y's).  The workspace
     may serve several handles whose runs follow each other on one stream."""
     _which, _where = 7, "bl_f8_linear"
 
@@ -795,6 +821,8 @@ class F8Linear(_KVCall):
                 _wants(gain, "gain", torch.float32, dev, (matrix.K,))
             M = x.shape[0]
             prod = make_producer(BL_PROD_F32 if x.dtype == torch.float32 else BL_PROD_BF16, x, norm=norm, gain=gain, eps=eps)
+        else:
+            _wants_producer(prod, M, matrix.K, dev)
         if y is None:
             y = torch.empty((M, matrix.N), dtype=torch.float32 if dtype is None else dtype, device=dev)
         else:

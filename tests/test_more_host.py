@@ -245,3 +245,47 @@ def test_layers_without_groups_share_nothing():
     for call in (lambda: layers.share(0, 0, 1), lambda: layers.join(1, 0), lambda: layers.release(0)):
         with pytest.raises(ValueError):
             call()
+
+
+PRODUCERS = [                              # kind, what it reads and writes of 3 rows of 192 values: name, type, values a row
+    (bl.BL_PROD_BF16, dict(in0=(torch.bfloat16, 192)), {}),
+    (bl.BL_PROD_F32, dict(in0=(torch.float32, 192)), {}),
+    (bl.BL_PROD_RESIDUAL, dict(in0=(torch.float32, 192), in1=(torch.float32, 192), aux_out=(torch.float32, 192)), {}),
+    (bl.BL_PROD_RELU2_GATE, dict(in0=(torch.float32, 384)), {}),
+    (bl.BL_PROD_ATTN_V, dict(in0=(torch.float32, 320)), dict(n_q=3, n_kv=1, head_dim=64)),
+]
+
+
+@pytest.mark.parametrize("kind, parts, more", PRODUCERS)
+def test_product_takes_producers_of_its_rows(lib, kind, parts, more):  # noqa: F811
+    """A producer's tensors against the matrix and M: nothing is taken that would be read, or written, past its end, as another type or in another order."""
+    m = bl.F8Matrix(torch.zeros(200, 192, dtype=torch.uint8).view(torch.float8_e4m3fn), torch.zeros(2, 2))
+
+    def call(M=3, gain=None, norm=True, **other):
+        tensors = {name: torch.zeros(3, width, dtype=dtype) for name, (dtype, width) in parts.items()}
+        tensors.update(other)
+        return bl.F8Linear(m, prod=bl.make_producer(kind, norm=norm, gain=gain, **tensors, **more), M=M)
+    assert call().y.shape == (3, 200) and call(M=1).y.shape == (1, 200) and call(gain=torch.zeros(192)).desc.prod.gain
+    for bad in (dict(M=4), dict(gain=torch.zeros(191)), dict(gain=torch.zeros(192).double())):
+        with pytest.raises((TypeError, ValueError)):
+            call(**bad)
+    for name, (dtype, width) in parts.items():
+        for shape in ((5, width), (width * 3,), (1, 3, width), (3, width // 64, 64)):     # (more rows than are used, and the same values in other shapes)
+            call(**{name: torch.zeros(shape, dtype=dtype)})
+        wrong = [torch.zeros(2, width, dtype=dtype), torch.zeros(3, width + 64, dtype=dtype), torch.zeros(4, width - 16, dtype=dtype), torch.zeros(width * 3 - 1, dtype=dtype),
+                 torch.zeros(3, width + 64, dtype=dtype)[:, :width], torch.zeros(width, 3, dtype=dtype).t(), torch.zeros(1, width, dtype=dtype).expand(3, width),
+                 torch.zeros(3, width, dtype=torch.float16), torch.zeros(3, width, dtype=torch.float32 if dtype == torch.bfloat16 else torch.bfloat16)]
+        for t in wrong:
+            with pytest.raises((TypeError, ValueError)):
+                call(**{name: t})
+    if "aux_out" in parts:
+        call(aux_out=None)
+
+
+def test_producers_without_tensors_and_refused_ones_are_the_call_s_own(lib):  # noqa: F811
+    """What the call itself refuses, with its status, is left to it; so is a descriptor that was filled in by hand."""
+    m = bl.F8Matrix(torch.zeros(200, 192, dtype=torch.uint8).view(torch.float8_e4m3fn), torch.zeros(2, 2))
+    x = torch.zeros(3, 192)
+    for prod in (bl.make_producer(9, x), bl.make_producer(bl.BL_PROD_RESIDUAL, x), bl.make_producer(bl.BL_PROD_ATTN_V, x, n_q=3, n_kv=1, head_dim=32)):
+        assert lib.bl_f8_linear(ctypes.byref(bl.F8Linear(m, prod=prod, M=3).desc), None) == VALUE
+    bl.F8Linear(m, prod=bl.Producer(kind=bl.BL_PROD_F32, in0=x.data_ptr()), M=3)
