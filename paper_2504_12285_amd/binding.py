@@ -84,21 +84,12 @@ def make_producer(kind, in0, in1=None, aux_out=None, n_q=0, n_kv=0, head_dim=0, 
     return p
 
 
-def _producer_parts(p, K):
-    """The tensors of a producer of rows of K values, as its kind reads and writes them: (name, tensor, whether bf16, values a row; None: K values in all).
-    Nothing for a descriptor that was filled in by hand, or that the call itself refuses."""
-    tensors = getattr(p, "tensors", None)
-    wide = {BL_PROD_BF16: K, BL_PROD_F32: K, BL_PROD_RESIDUAL: K, BL_PROD_RELU2_GATE: 2 * K,
-            BL_PROD_ATTN_V: (p.n_q + 2 * p.n_kv) * p.head_dim if p.n_q * p.head_dim == K else None}.get(p.kind)
-    if tensors is None or wide is None:
-        return []
-    in0, in1, aux_out, gain = tensors
-    parts = [("in0", in0, p.kind == BL_PROD_BF16, wide)]
-    if p.kind == BL_PROD_RESIDUAL:
-        parts += [("in1", in1, False, K), ("aux_out", aux_out, False, K)]
-    if p.norm:
-        parts.append(("gain", gain, False, None))
-    return [part for part in parts if part[1] is not None]
+def _producer_width(p, K):
+    """Values of a row of in0 where a producer's rows have K; None where the call itself refuses it."""
+    kind = p.kind
+    if kind == BL_PROD_ATTN_V:
+        return (p.n_q + 2 * p.n_kv) * p.head_dim if p.n_q * p.head_dim == K else None
+    return K if kind in (BL_PROD_BF16, BL_PROD_F32, BL_PROD_RESIDUAL) else 2 * K if kind == BL_PROD_RELU2_GATE else None
 
 
 class DecodeDesc(ctypes.Structure):
@@ -275,7 +266,7 @@ class _PythonForm:
     def quant(*args):
         return NotImplemented
 
-    product = decode = run = kv = quant
+    product = decode = run = kv = holds = quant
 
 
 def _first_native():
@@ -437,6 +428,22 @@ def bl_bitlinear_decode(packed, beta, layout, X, N, want_acc=False, want_y=True,
     return acc, y, q, scale
 
 
+_QUANT_TENSORS = ("in0", "in1", "aux_out", "gain", "q", "scale", "rowsum")
+
+
+def _hold(names, *pairs):
+    """Each tensor (or None) has so many bytes of memory from its first value on: pairs of them, names for the errors."""
+    short = (_native or _first_native()).holds(*pairs)
+    if short is NotImplemented:
+        short = next((i for i, (t, n) in enumerate(zip(pairs[::2], pairs[1::2])) if t is not None and n > _memory(t)), -1)
+    if short >= 0:
+        raise ValueError("%s has %d bytes, %d are needed" % (names[short], _memory(pairs[2 * short]), pairs[2 * short + 1]))
+
+
+def _memory(t):
+    return t.untyped_storage().nbytes() - t.storage_offset() * t.element_size()
+
+
 def make_decode_descs(items):
     """items: list of dicts with tensor values for the bl_decode_desc fields
     (packed, beta, X or q/scale/rowsum, acc, y, q_out, scale_out) and int N, K.
@@ -458,7 +465,7 @@ def bl_bitlinear_decode_group(descs, layout, M):
 
 
 def bl_quant_act_ex(prod, M, K, device, want_rowsum=True, q=None, scale=None, rowsum=None):
-    """Producer + quantiser (prefill side).  prod: Producer from make_producer.
+    """Producer + quantiser (prefill side).  prod: Producer from make_producer, whose tensors have memory for M rows.
     Returns (q int8 [M][K], scale fp32 [M], rowsum int32 [M] or None)."""
     torch = _get_torch()
     if q is None:
@@ -467,6 +474,10 @@ def bl_quant_act_ex(prod, M, K, device, want_rowsum=True, q=None, scale=None, ro
         scale = torch.empty(M, dtype=torch.float32, device=device)
     if rowsum is None and want_rowsum:
         rowsum = torch.empty(M, dtype=torch.int32, device=device)
+    in0, in1, aux_out, gain = getattr(prod, "tensors", (None,) * 4)
+    width, both = _producer_width(prod, K) or 0, M * K * 4 if prod.kind == BL_PROD_RESIDUAL else 0
+    _hold(_QUANT_TENSORS, in0, M * width * (2 if prod.kind == BL_PROD_BF16 else 4), in1, both, aux_out, both, gain, K * 4 if prod.norm else 0,
+          q, M * K, scale, M * 4, rowsum, M * 4)
     _check(load().bl_quant_act_ex(ctypes.byref(prod), M, K, _ptr(q), _ptr(scale), _ptr(rowsum), _stream()),
            "bl_quant_act_ex")
     return q, scale, rowsum
@@ -565,12 +576,22 @@ def _wants(t, what, dtype, device, shape=None, rows=False):
 
 
 def _wants_producer(p, M, K, device):
-    """A producer whose tensors have M rows at least, each as wide as its kind has it (its values may be in several dimensions)."""
+    """A producer whose tensors have M rows at least, each as wide as its kind has it (its values may be in several dimensions).  What the call itself
+    refuses, and a descriptor that was filled in by hand, are left to it."""
     torch = _get_torch()
-    for name, t, bf16, wide in _producer_parts(p, K):
-        _wants(t, name, torch.bfloat16 if bf16 else torch.float32, device, None if wide else (K,))
-        if wide and (t.numel() < M * wide or (t.numel() % wide if t.dim() == 1 else wide not in (math.prod(t.shape[i:]) for i in range(t.dim())))):
+    width = _producer_width(p, K)
+    if width is None or not hasattr(p, "tensors"):
+        return
+    in0, in1, aux_out, gain = p.tensors
+    parts = [("in0", in0, width)] + ([("in1", in1, K), ("aux_out", aux_out, K)] if p.kind == BL_PROD_RESIDUAL else [])
+    for name, t, wide in parts:
+        if t is None:
+            continue
+        _wants(t, name, torch.bfloat16 if p.kind == BL_PROD_BF16 else torch.float32, device)
+        if t.numel() < M * wide or (t.numel() % wide if t.dim() == 1 else wide not in (math.prod(t.shape[i:]) for i in range(t.dim()))):
             raise ValueError("%s must have %d rows of %d values, has the shape %s" % (name, M, wide, tuple(t.shape)))
+    if p.norm and gain is not None:
+        _wants(gain, "gain", torch.float32, device, (K,))
 
 
 def _row_stride(t):

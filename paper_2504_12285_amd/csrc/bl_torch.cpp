@@ -203,6 +203,20 @@ PyObject* kv(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
+/* tensor or None, bytes that it has to have from its first value on, and so on: the place of the first that has less, or -1 */
+PyObject* holds(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded([&]() -> PyObject* {
+        if (n % 2 || !plain()) return nullptr;
+        for (Py_ssize_t i = 0; i < n; i += 2) {
+            const at::Tensor* t;
+            int64_t want;
+            if (!get(a[i], &t) || !get(a[i + 1], &want)) return nullptr;
+            if (t && want > (int64_t)t->storage().nbytes() - t->storage_offset() * (int64_t)t->element_size()) return PyLong_FromSsize_t(i / 2);
+        }
+        return PyLong_FromLong(-1);
+    });
+}
+
 /* The addresses of bl_quant_act_int8, bl_gemv_w158a8, bl_gemm_w158a8, bl_bitlinear_decode and bl_stack_run in the
  * loaded library. */
 PyObject* bind(PyObject*, PyObject* args) {
@@ -233,6 +247,7 @@ PyMethodDef methods[] = {{"quant", (PyCFunction)(void (*)(void))quant, METH_FAST
                          {"decode", (PyCFunction)(void (*)(void))decode, METH_FASTCALL, nullptr},
                          {"run", (PyCFunction)(void (*)(void))run, METH_FASTCALL, nullptr},
                          {"kv", (PyCFunction)(void (*)(void))kv, METH_FASTCALL, nullptr},
+                         {"holds", (PyCFunction)(void (*)(void))holds, METH_FASTCALL, nullptr},
                          {"bind", bind, METH_VARARGS, nullptr},
                          {"bind_kv", bind_kv, METH_VARARGS, nullptr},
                          {"current_stream", current_stream, METH_NOARGS, nullptr},

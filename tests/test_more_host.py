@@ -289,3 +289,28 @@ def test_producers_without_tensors_and_refused_ones_are_the_call_s_own(lib):  # 
     for prod in (bl.make_producer(9, x), bl.make_producer(bl.BL_PROD_RESIDUAL, x), bl.make_producer(bl.BL_PROD_ATTN_V, x, n_q=3, n_kv=1, head_dim=32)):
         assert lib.bl_f8_linear(ctypes.byref(bl.F8Linear(m, prod=prod, M=3).desc), None) == VALUE
     bl.F8Linear(m, prod=bl.Producer(kind=bl.BL_PROD_F32, in0=x.data_ptr()), M=3)
+
+
+@pytest.mark.parametrize("native", [True, False])
+@pytest.mark.parametrize("kind, parts, more", PRODUCERS)
+def test_the_quantiser_s_tensors_hold_its_rows(monkeypatch, native, kind, parts, more):
+    """What would be read or written behind the memory of a tensor is refused before anything else, by the native form as by the Python form; views into
+    longer memory are taken as before."""
+    monkeypatch.setattr(bl, "_native", None if native else bl._PythonForm())
+    def call(M=3, gain=None, **other):
+        tensors = {name: torch.zeros(3, width, dtype=dtype) for name, (dtype, width) in parts.items()}
+        tensors.update((k, other.pop(k)) for k in list(other) if k in tensors)
+        bl.bl_quant_act_ex(bl.make_producer(kind, norm=True, gain=gain, **tensors, **more), M, 192, "cpu", **other)
+    wrong = [dict(M=4), dict(gain=torch.zeros(191)), dict(q=torch.zeros(2, 192, dtype=torch.int8)), dict(scale=torch.zeros(2)), dict(rowsum=torch.zeros(2, dtype=torch.int32))]
+    wrong += [{name: t} for name, (dtype, width) in parts.items()
+              for t in (torch.zeros(2, width, dtype=dtype), torch.zeros(3 * width - 1, dtype=dtype), torch.zeros(1, width, dtype=dtype).expand(3, width),
+                        torch.zeros(4, width, dtype=dtype)[2:])]
+    for bad in wrong:
+        with pytest.raises(ValueError, match="bytes"):
+            call(**bad)
+    hold = (bl._native or bl._first_native()).holds
+    x = torch.zeros(9, 4)
+    for fits in ((), (None, 5), (x, 144, None, 1 << 40), (x[3:], 96), (x[:, :2], 144), (x[:3], 144)):
+        assert hold(*fits) == (-1 if native else NotImplemented) and bl._hold("ab", *fits) is None
+    with pytest.raises(ValueError, match="b has 96 bytes, 97"):
+        bl._hold("ab", x, 1, x[3:], 97)
