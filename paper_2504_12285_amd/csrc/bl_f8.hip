@@ -127,14 +127,15 @@ __global__ __launch_bounds__(256) void bl_f8_units(f8_args A, bl_prod_dev P) {
 /* ---- output -------------------------------------------------------------------------------------------------------------- */
 
 __device__ __forceinline__ uint16_t f8_bf16(float v) { return (uint16_t)bl_pack2_bf16(v, v); }
-/* Four consecutive outputs n .. n + 3 of row m: one store, whatever the row's alignment (the memory takes vectors at any element). */
+/* Four consecutive outputs n .. n + 3 of row m: one store, whatever the row's alignment (the memory takes vectors at any element; the types say so, and
+ * bl_g would not hand it on). */
 typedef uint32_t f8_out2 __attribute__((ext_vector_type(2), aligned(2)));
 typedef float f8_out4 __attribute__((ext_vector_type(4), aligned(4)));
 __device__ __forceinline__ void f8_store4(const f8_args& A, int m, int n, const float (&v)[4]) {
     const int64_t at = (int64_t)m * A.y_stride + n;
     if (n + 4 <= A.N) {
-        if (A.bf16) *bl_g((f8_out2*)((uint16_t*)A.y + at)) = (f8_out2){bl_pack2_bf16(v[0], v[1]), bl_pack2_bf16(v[2], v[3])};
-        else *bl_g((f8_out4*)((float*)A.y + at)) = (f8_out4){v[0], v[1], v[2], v[3]};
+        if (A.bf16) *(f8_out2 BL_G*)((uint16_t*)A.y + at) = (f8_out2){bl_pack2_bf16(v[0], v[1]), bl_pack2_bf16(v[2], v[3])};
+        else *(f8_out4 BL_G*)((float*)A.y + at) = (f8_out4){v[0], v[1], v[2], v[3]};
     } else {
         for (int i = 0; i < 4 && n + i < A.N; ++i) {
             if (A.bf16) ((uint16_t*)A.y)[at + i] = f8_bf16(v[i]);

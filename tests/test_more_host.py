@@ -1,10 +1,13 @@
 """Calls of the 8-bit float matrix, of shared prefixes and of the append with norms on the host: every refusal comes before any GPU work, sizes are
 right, and the binding takes only tensors that a descriptor can stand for.  Needs no GPU."""
 import ctypes
+import os
+import subprocess
 
 import pytest
 
 from paper_2504_12285_amd import binding as bl
+from paper_2504_12285_amd import build as hip_build
 from test_kv_host import ALIGN, BAD_ATTENTION, BAD_CACHES, NULL, P, SHAPE, VALUE, WORKSPACE, attention, cache, lib, tables, tokens  # noqa: F401
 
 torch = pytest.importorskip("torch")
@@ -314,3 +317,14 @@ def test_the_quantiser_s_tensors_hold_its_rows(monkeypatch, native, kind, parts,
         assert hold(*fits) == (-1 if native else NotImplemented) and bl._hold("ab", *fits) is None
     with pytest.raises(ValueError, match="b has 96 bytes, 97"):
         bl._hold("ab", x, 1, x[3:], 97)
+
+
+@pytest.mark.parametrize("source", [s for s in hip_build.SOURCES if s.endswith(".hip")])
+def test_vectors_have_the_alignment_that_their_types_say(source):
+    """No kernel hands an address of a lower alignment to an access of a higher one (outputs may begin at any value)."""
+    hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
+    if not os.path.exists(hipcc):
+        pytest.skip("no hipcc")
+    done = subprocess.run([hipcc, "--offload-arch=gfx950", "-std=c++17", "--cuda-device-only", "-fsyntax-only", "-Werror=align-mismatch", "-I", hip_build.INCLUDE,
+                           "-I", hip_build.CSRC, os.path.join(hip_build.CSRC, source)], capture_output=True, text=True)
+    assert done.returncode == 0, done.stderr[-2000:]
