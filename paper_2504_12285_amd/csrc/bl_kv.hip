@@ -132,10 +132,8 @@ __global__ __launch_bounds__(THREADS) void bl_kv_tables_kernel(tab_args A) {
     int64_t there = b.free_count[0];
     int old[PER], n[PER], hold[PER];                          /* hold: blocks in front that an ended request does not give back */
     int64_t rows = 0, back = 0;
-    auto gives = [&](int i) -> int {
-        const int have = (int)(((int64_t)old[i] + bs1) >> shift);
-        return n[i] >= 0 ? 0 : !HELD ? have : have > hold[i] ? have - hold[i] : 0;
-    };
+    auto blocks = [&](int i) -> int64_t { return ((int64_t)old[i] + bs1) >> shift; };      /* of request i */
+    auto gives = [&](int i) -> int64_t { return !HELD ? blocks(i) : blocks(i) > hold[i] ? blocks(i) - hold[i] : 0; };       /* at its end */
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
         const int r = tid * per + i;
@@ -159,7 +157,7 @@ __global__ __launch_bounds__(THREADS) void bl_kv_tables_kernel(tab_args A) {
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             if (i >= per) break;
-            const int r = tid * per + i, have = gives(i);
+            const int r = tid * per + i, have = n[i] < 0 ? (int)gives(i) : 0;
             if (HELD && have > 0) s_start[r] = hold[i];       /* (for now) */
             if (have > 0 && at + have > cap) atomicAdd(&s_bad, 1);
             if (have > 0) s_from[r] = (int)(at < cap ? at : cap), s_n[r] = at < cap ? (int)(cap - at < have ? cap - at : have) : 0;
