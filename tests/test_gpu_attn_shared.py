@@ -311,3 +311,43 @@ def test_without_groups_it_is_the_attention_of_its_tables(new):
     reqs = [(t + 20, min(t, new)) for t in OWN]
     b = Shared(reqs, [3], [-1, 1, 5, -9] * 3, (8, 2, 64), 32, "int8")
     b.check()
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("block, heads", [(16, (8, 2, 128)), (64, (20, 5, 128)), (128, (8, 2, 64))])
+@pytest.mark.parametrize("new", [1, 6, 40])
+def test_scales_and_codes_of_nobody_s_blocks(kind, block, heads, new):
+    """Blocks of no request have NaN for scales and the lowest codes, block 0 among them, whose scales stand in where a tile has no block; so have places
+    behind the last tokens the lowest codes.  (e4m3: 0xff, a NaN.)"""
+    prefix = [9, 3] if block < 64 else [3, 1]
+    low = -128 if kind == "int8" else 0xff
+    for window, far in ((0, FAR), (70, FAR), (0, 0), (70, 0)):
+        reqs, group = dealt(prefix, OWN, block, 2, new, lone=(3,))
+        b = Shared(reqs, prefix, group, heads, block, kind, seed=new)
+        clean = [t.clone() for t in (b.k, b.v, b.ks, b.vs)]
+        k, v = (t.view(torch.int8 if kind == "int8" else torch.uint8) for t in (b.k, b.v))
+        seen = set()
+        for r, (t, n) in enumerate(reqs):
+            first = max(0, t - n + 1 - window) if window else 0
+            for p in range(-(-t // block)):
+                page = int(b.table[r, p])
+                if p * block + block > first:
+                    seen.add(page)
+                if t - p * block < block:
+                    k[page, :, t - p * block:], v[page, :, :, t - p * block:] = low, low
+        nobody = set(range(k.shape[0])) - seen
+        if 0 in seen:                                         # (another block takes its place)
+            other = max(nobody)
+            for x in (k, v, b.ks, b.vs, *(x.view(torch.uint8) if x.element_size() == 1 else x for x in clean)):
+                x[other] = x[0].clone()
+            for x in (b.table, b.shared_table):
+                x[x == 0] = other
+            nobody = nobody - {other} | {0}
+        for page in nobody:
+            k[page], v[page] = low, low
+            b.ks[page] = b.vs[page] = math.nan
+        h = b.handle(window=window, max_len=far)
+        h.out.fill_(math.nan), h.workspace.fill_(255)
+        h.run()
+        b.k, b.v, b.ks, b.vs = clean
+        b.compare(h.out, window)

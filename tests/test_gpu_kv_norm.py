@@ -129,3 +129,58 @@ def test_large_and_small_numbers():
 
 def test_captured():
     run("e4m3", "bf16", (20, 5, 128), 64, [(3, 20), (70, 1), (200, 64)], captured=True)
+
+
+def nan_in_queries(x):
+    x[5, 1, 7] = np.nan
+
+
+def infinity_in_queries(x):
+    x[6, 2, 40] = -np.inf
+    x[7, 0, 3] = np.inf
+
+
+def none_in_keys(x):
+    x[6, 4, 60] = np.nan
+    x[8, 5, 1] = np.inf
+
+
+def beyond_squares(x):
+    x[:, ::2] *= F(1e25)
+    x[:, 1::2] *= F(1e-25)
+
+
+@pytest.mark.parametrize("heads", [(4, 2, 64), (4, 2, 128)])
+@pytest.mark.parametrize("rotate", [True, False])
+@pytest.mark.parametrize("spoil", [nan_in_queries, infinity_in_queries, none_in_keys, beyond_squares])
+def test_queries_beside_numbers_that_are_none_and_of_far_ones(spoil, rotate, heads):
+    """Every query bit for bit, but for the NaN's own bits: what spoils a head reaches no other head and no other token."""
+    from paper_2504_12285_amd import binding as bl
+    n_q, H, D = heads
+    r = np.random.RandomState(D)
+    T, eps = 23, 1e-30
+    x = r.randn(T, n_q + 2 * H, D).astype(F)
+    spoil(x)
+    angle = r.rand(60, D // 2) * 6.3
+    cos, sin = np.cos(angle).astype(F), np.sin(angle).astype(F)
+    positions, slots = r.randint(0, 60, T).astype(np.int32), np.arange(5, 5 + T, dtype=np.int32)
+    qg, kg = ((1 + 0.3 * r.randn(D)).astype(F) for _ in range(2))
+
+    def t(a):
+        return torch.from_numpy(a).cuda()
+    h = bl.KVNormAppend(bl.KVCache.empty(4, H, 16, D, torch.device("cuda:0")), t(x.reshape(T, -1)), n_q, t(slots), t(positions), t(cos) if rotate else None,
+                        t(sin) if rotate else None, q_gain=t(qg), k_gain=t(kg), eps=eps)
+    h.q.fill_(7.0)
+    h.run()
+    y = normed(x[:, :n_q], qg, eps)
+    if rotate:
+        c, s = cos[positions][:, None], sin[positions][:, None]
+        a, b = y[..., :D // 2], y[..., D // 2:]
+        with np.errstate(all="ignore"):
+            y = np.concatenate([a * c - b * s, b * c + a * s], -1)
+    want = torch.from_numpy(y).to(torch.bfloat16).view(T, -1)
+    got = h.q.cpu().view(T, -1)
+    none = want.isnan()
+    assert bool(none.any()) == (spoil in (nan_in_queries, infinity_in_queries))
+    assert torch.equal(got.isnan(), none)
+    assert torch.equal(got.view(torch.int16)[~none], want.view(torch.int16)[~none])
