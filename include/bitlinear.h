@@ -532,7 +532,8 @@ bl_status bl_attn_kv8(const bl_attn_desc* a, bl_stream s);
  * group[b] (outside 0 .. n_groups-1: to none; a group's requests need not stand together).  The tokens of its first S =
  * shared_blocks[group[b]] blocks (taken as the nearer end outside 0 .. max_shared) are those of row group[b] of shared_table, and its own row of `table` begins with the
  * same ones: either may be read.  Results are bl_attn_kv8's but for the order of the sums: lengths and positions count the prefix, causality and window hold inside it
- * too, a request may be shorter than it.
+ * too, a request may be shorter than it.  What shares a read: all requests of less than 128 rows (queries times n_q / n_kv), but where max_q lets one bring 128 or more, those of up to
+ * 16 rows; others read the prefix for themselves, and so do all in short contexts.  So max_q is worth giving: with the batch's rows in its place, requests of few queries may share nothing.
  *   shared_table   [n_groups][shared_stride], max_shared <= shared_stride entries of a row are used; its blocks are whole (every token written)
  *   max_own        about the most tokens that a request has behind its shared blocks: sizes a split only (0: as attn.max_len)
  *   attn.workspace bl_attn_shared_workspace_bytes(a) bytes
@@ -563,7 +564,8 @@ enum { BL_F8_OUT_F32 = 0, BL_F8_OUT_BF16 = 1 };
  *   g = max |X| of the group; s = max(g, 1e-5f) * (1.0f / 448.0f); code = e4m3(X * (1.0f / s)), every step one rounded fp32
  *   operation, ties to even;
  *   y[m][n] = sum over the groups b of (s[m][b] * scale[n / 128][b]) * sum_k code[m][k] * codes[n][k], in fp32, then to the output's type.
- * A row with a NaN or an infinity in it is NaN.
+ * A row with a NaN or an infinity in it is NaN.  The norm's sum of squares has one order per kernel: up to 16 rows of up to 1024 values are made in the product's own, whose order is another
+ * than the other producers'; r is the same but for a row in about 10^8.
  *   y          fp32 or bf16 [M][N], rows y_stride values apart, aligned to its type
  *   workspace  bl_f8_workspace_bytes(p) bytes, 256-byte aligned; no content is expected
  * y, the workspace and a producer's aux_out share no byte with each other or with what is read (BL_ERR_VALUE): a sum is not stored in place.

@@ -763,7 +763,8 @@ def _space_of(nbytes, workspace, dev):
 class KVSharedAttention(KVAttention):
     """KVAttention where requests share prefixes, each read once for all of its requests (bl_attn_kv8_shared).  group: int32 [B], the group of
     each request (outside 0 .. n_groups - 1: none); shared_table int32 [n_groups][max_shared], shared_blocks int32 [n_groups]: the blocks of a
-    group's prefix.  max_own: about the most tokens of a request behind its prefix.  Everything else is KVAttention's."""
+    group's prefix.  max_own: about the most tokens of a request behind its prefix.  max_q decides what shares a read, so it is worth giving (None: as if one request
+    brought all rows; from 128 rows of n_q / n_kv heads on only requests of up to 16 rows share).  Everything else is KVAttention's."""
     _which, _where = 6, "bl_attn_kv8_shared"
 
     def __init__(self, cache, q, q_start, seq_len, table, group, shared_table, shared_blocks, n_q=None, max_q=None, max_len=0, max_own=0,

@@ -883,8 +883,9 @@ struct at_prefix_lds : at_many_lds<KIND, D> {
 /* What a workgroup of at_many has: rows of a request over all that they see; over what stands behind their group's prefix (AT_OWN); or rows of all
  * requests of a group over its prefix (AT_PREFIX), which are gathered: their places in the batch are found by each workgroup, by sums over the requests.
  * A prefix's rows fill tiles together (128 of them for one read of K and V), in equal pieces over its tokens, so that every row of a group has as many partial results and
- * the join needs no list.  Bound by the instructions of a wave's tiles one after the other, not by memory: 16 requests of 32 + 8 heads behind 65536 tokens, e4m3, 134 MB of codes,
- * 50 us (without loads 47, without products 40; at_few reads them for each request: 337).  Two tiles of K in flight, pairs of waves on one tile's rows: 49 and 47. */
+ * the join needs no list.  Not bound by memory, nor by any one of a tile's parts: 16 requests of 32 + 8 heads behind 65536 tokens, e4m3, 134 MB of codes,
+ * 50 us, without loads 47, without products 40: a wave's tiles one after the other, on two waves a SIMD (at_few reads them for each request: 337).  Two tiles of K in flight, pairs
+ * of waves on one tile's rows: 49 and 47. */
 enum { AT_ALL, AT_OWN, AT_PREFIX };
 template <int KIND, int D, int MODE = AT_ALL>
 __device__ __forceinline__ void at_many(const at_args& A, int place, std::conditional_t<MODE == AT_PREFIX, at_prefix_lds<KIND, D>, at_many_lds<KIND, D>>& lds) {
@@ -1685,7 +1686,8 @@ static bl_status at_check_shared(const bl_attn_shared_desc* a) {
  * to join, or there is little to read at all.  us of these kernels and of those, all requests behind one prefix, up to 300 tokens of their own:
  *   20 + 5 heads of 128, prefix 500: 2 to 64 requests 11 to 18 and 9 to 14 (four queries each 12 to 23 and 9 to 15); 2000: 2, 4, 8, 16, 64 requests 12.8, 13.2, 14.0, 15.2,
  *     22.2 and 11.4, 11.7, 14.6, 18.6, 34.7; 8000: 17.1 to 32 and 17.6 to 83; 30000: 26 to 33 (16 requests) and 27 to 107;
- *   32 + 8 heads of 64, 2000: 2 to 64 requests 11.5 to 17 and 10 to 15; 8000: 15.1 to 27.7 and 13.9 to 60; 16 + 1 of 128, 2000: 12.4 to 20.4 and 11.6 to 22.8. */
+ *   32 + 8 heads of 64, 2000: 2 to 64 requests 11.5 to 17 and 10 to 15; 3000: 16, 64 requests 14.2, 20 and 11, 19 to 21, 48 of four queries, one group and five, 29 and 34 and 18 to 21; 3500:
+ *     14.7, 20 and 12, 21 to 23; 4096: 15, 21.7 and 19, 37; 8000: 15.1 to 27.7 and 13.9 to 60; 16 + 1 of 128, 2000: 12.4 to 20.4 and 11.6 to 22.8. */
 static bool at_shared_apart(const bl_attn_shared_desc* s) {
     const bl_attn_desc* a = &s->attn;
     const int64_t tokens = a->max_len > 0 ? a->max_len : (int64_t)a->max_blocks * a->cache.block;
@@ -1710,7 +1712,8 @@ static at_shared_plan at_make_shared_plan(const bl_attn_shared_desc* s) {
     };
     /* Where a request may fill tiles of at_many by itself, which read the prefix from the caches then, all of more than AT_FEW rows are apart; else they are of
      * their groups.  us of this and of the other, 20 + 5 heads: 8 chunks of 300 beside 16 decoding requests behind 4096 tokens 124 and 135, 4 of 300 beside 60
-     * behind 8000 110 and 127; 30 queries of each of 16 requests behind 32000 216 and 293, 20 of 24 behind 4096 59 and 68. */
+     * behind 8000 110 and 127; 30 queries of each of 16 requests behind 32000 216 and 293, 20 of 24 behind 4096 59 and 68.  What it costs: requests of 17 to 127 rows beside a prompt read the
+     * prefix each for itself then, 60 of five queries (20 rows) beside one chunk of 300 behind 8000 and 32000 tokens 217 and 750, bl_attn_kv8 208 and 692, without the chunk 71 and 149. */
     const bool prompts = p.many && (int64_t)a->max_q * G >= AT_MANY;
     p.apart = prompts ? AT_FEW + 1 : AT_MANY;
     const int64_t most = a->T * G < part * (p.apart - 1) ? a->T * G : part * (p.apart - 1);            /* rows that groups can have */

@@ -598,7 +598,9 @@ static f8_plan f8_make_plan(const bl_f8_product* p) {
     q.splits = 1;
     /* The stream, while a wave's registers hold its blocks of every token, and where they hold them opened or there are few rows of tiles.  us of it and of tiles:
      * 2560 x 2560 17 to 64 rows 8.6 to 11.9 and 11.4 to 13.9; 128256 x 2560 17, 48, 64 rows 61, 72, 94 and 71, 80, 86; 40000 x 2560 48, 64 rows 28.8, 36.2 and 26.2,
-     * 26.6; x 4096 17, 48 rows 36.6, 44.9 and 37.3, 37.4; 4096 x 4096 48 rows 14.2 and 15.0, 8192 16.9 and 16.1.  (16 rows: the stream at every size.) */
+     * 26.6; x 4096 17, 48 rows 36.6, 44.9 and 37.3, 37.4; 4096 x 4096 48 rows 14.2 and 15.0, 8192 16.9 and 16.1.  Up to 16 rows: the stream up to K = 8192, the most that a wave's
+     * registers hold; behind it tiles, most of whose rows are copies then: 4096 x 8192 and x 9216 one row 9.0 and 14.8, 16 rows 11.8 and 15.8, 128256 x 8192 and x 9216 one row 159 and 226
+     * (a large copy's rate: 221 and 249). */
     const int64_t each = (nb + F8_WAVES - 1) / F8_WAVES;
     q.tokens = p->M <= 64 ? (int)((p->M + 15) / 16) : 0, q.blocks = each > 8 ? 16 : each <= 4 ? (int)each : each <= 6 ? 6 : 8;
     if (q.tokens * q.blocks > (p->w.N >= 8192 ? 9 : 12)) q.tokens = 0;

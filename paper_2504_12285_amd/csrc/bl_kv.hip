@@ -245,7 +245,7 @@ __global__ __launch_bounds__(256) void bl_kv_slots_kernel(tab_args A) {
 }
 
 /* LIMIT: with a most of new tokens a request (a kernel of its own: above 1024 requests the comparison costs the others 1.2 us).
- * HELD: with blocks in front that are not given back (a kernel of its own too: 64 and 1000 requests 3.05 and 5.71 us, without 3.01 and 5.62). */
+ * HELD: with blocks in front that are not given back (a kernel of its own too: 8, 64 and 1000 requests 3.1, 3.13 and 5.72 us, without 2.9, 3.12 and 5.69). */
 template <bool LIMIT, bool HELD = false>
 static bl_status tab_launch(const bl_kv_batch* b, int max_new, bl_stream s, const int32_t* held = nullptr) {
     if (!b->seq_len || !b->new_len || !b->free_count || !b->table || (!b->free_list && b->free_cap) || !b->seq_len_out || !b->free_count_out || !b->start ||
@@ -312,8 +312,9 @@ __device__ __forceinline__ double app_sum(double v) {
 }
 /* RMS norm of a head whose D values lie in G lanes, 2 * N each: the mean square in 64 bits (its squares are exact there), so that the factor of 32 bits is
  * the same whatever the order of the sum; then two rounded products.  In the append's own pass, which has the row in registers: one token 4.5 us (the append alone 4.2),
- * 20 thousand rows of 32 + 8 heads of 64 63 and 55, with the state of other work in the caches 77 (bytes alone 42): the sum of 64 bits and its exchanges between
- * loads and stores of a wave.  (Root and quotient by an approximation and a step of third order: 62 of 63, and a factor that is not the formula's once in 10^8 heads: not taken.) */
+ * 20 thousand rows of 32 + 8 heads of 64 62 and 54, with the state of other work in the caches 77 (bytes alone 42).  Of the 8 us the sum and the root of 64 bits are 2.5 (both in
+ * 32 bits 59.7, neither of them 59.6, the root alone in 32 bits 60.4): the rest is the two products and the gains between a row's load and its rotation.  (Root and quotient by an
+ * approximation and a step of third order: 1 us less, and a factor that is not the formula's once in 10^8 heads: not taken.) */
 template <int G, int D, int N>
 __device__ __forceinline__ void app_norm(float (&a)[N], float (&b)[N], float eps, const float* gain, int i) {
     double ss = 0.0;
